@@ -493,6 +493,172 @@ typedef struct hwsel_cands_out {
 int hwsel_catalogue_candidates(const hwsel_problem_t *problems, int32_t P, const int64_t *seg_offsets,
                                const int32_t *point, int64_t R, const hwsel_cands_out_t *out, void *stream);
 
+/*
+ * 8-bit floating-point matrices with block scales: the operands of
+ * hwsel_fp8_matmul and hwsel_fp8_layer, and the form in which activations
+ * are kept between a forward and a backward pass.
+ *   value[r][c] = code(q[r][c]) * 2^(scale[r / block_rows][c / 128] - 127)
+ *   rows, cols  sizes of the logical matrix (>= 1).
+ *   q           codes, uint8 [rows][ld], 16-byte aligned, ld % 16 == 0, ld >=
+ *               cols rounded up to 128; the columns from cols up to that hold
+ *               code 0 (the entry points that write a matrix write them so).
+ *   scale       exponent bytes, uint8 [ceil(rows / block_rows)][ld_scale],
+ *               4-byte aligned, ld_scale % 4 == 0, ld_scale >= ceil(cols /
+ *               128); 255 stands for NaN.  Bytes past the blocks are not
+ *               used.
+ *   format      HWSEL_FP8_E4M3 (largest value 448, no infinity) or
+ *               HWSEL_FP8_E5M2 (57344, with infinities).
+ *   block_rows  1 (a scale for each row's 128 columns: activations,
+ *               gradients) or 128 (for 128 rows by 128 columns: weights).
+ * A power of two as the scale loses nothing (the codes are floating point)
+ * and makes scaling exact; the matrix cores apply it themselves.  The struct
+ * is read on the host.  Every entry point that takes one returns HWSEL_EINVAL
+ * for null pointers, sizes < 1, a bad stride, alignment, format or
+ * block_rows, and HWSEL_EUNSUPPORTED for rows > 2^30, cols > 2^23 or ld >=
+ * 2^24.
+ */
+enum { HWSEL_FP8_E4M3 = 0, HWSEL_FP8_E5M2 = 1 };
+#define HWSEL_FP8_BLOCK 128
+typedef struct hwsel_fp8 {
+    int64_t rows, cols;
+    uint8_t *q;
+    int64_t ld;
+    uint8_t *scale;
+    int64_t ld_scale;
+    int32_t format, block_rows;
+} hwsel_fp8_t;
+
+/*
+ * Quantising.  out = X (transposed == 0; X is [rows][ld], ld >= cols) or X
+ * transposed (X is [cols][ld], ld >= rows), X of dtype HWSEL_DTYPE_FP32 or
+ * HWSEL_DTYPE_BF16, aligned to its elements, ld in elements.  For each block
+ * of out with amax = m 2^x (1 <= m < 2) the largest magnitude among its finite
+ * elements, the exponent is e = x - 8 where m <= 1.75, else x - 7 (E4M3; x -
+ * 15 and x - 14 for E5M2): the least that keeps amax within the format.  The
+ * byte is e + 127 limited to [1, 254], 1 for a block of zeros; each code is
+ * X 2^-e rounded to nearest, ties to even.  A NaN becomes the format's NaN;
+ * an infinity becomes NaN in E4M3 and stays one in E5M2; neither touches the
+ * block's other elements.
+ *   mean, inv_std: fp32 [cols] or both NULL.  Given, the matrix quantised is
+ *   (clean(X) - mean) * inv_std (fp32, two operations; clean maps NaN and
+ *   +-inf to 0), as hwsel_mlp_score standardises.
+ * Returns HWSEL_EINVAL for null pointers, sizes < 1, a bad ld, alignment,
+ * format or block_rows; HWSEL_EUNSUPPORTED for another dtype, and for mean
+ * with transposed or block_rows 128.
+ */
+int hwsel_fp8_quantise(const void *X, int32_t dtype, int64_t ld, int32_t transposed, const float *mean,
+                       const float *inv_std, const hwsel_fp8_t *out, void *stream);
+
+/*
+ * Restoring.  X[r][c] = the value of in[r][c], rounded to nearest even in
+ * bf16 (exact for what hwsel_fp8_quantise writes, bar bf16 subnormals).  X of
+ * dtype HWSEL_DTYPE_FP32 or HWSEL_DTYPE_BF16, row-major [rows][ld], aligned to
+ * its elements.
+ * Returns HWSEL_EINVAL and HWSEL_EUNSUPPORTED as hwsel_fp8_quantise does.
+ */
+int hwsel_fp8_dequantise(const hwsel_fp8_t *in, void *X, int32_t dtype, int64_t ld, void *stream);
+
+/*
+ * The transposed matrix, quantised again along its own rows (in's columns):
+ * out = what hwsel_fp8_quantise would write of in's values, transposed.  The
+ * operand of a weight gradient from activations kept in 8 bits, without a
+ * wider copy of them.  out->rows == in->cols, out->cols == in->rows; out must
+ * not overlap in.
+ * Returns HWSEL_EINVAL as hwsel_fp8_quantise does and for sizes that differ.
+ */
+int hwsel_fp8_transpose(const hwsel_fp8_t *in, const hwsel_fp8_t *out, void *stream);
+
+/*
+ * Matrix product of two 8-bit matrices, both row-major along the summed
+ * dimension (A [M][K], B [N][K]):
+ *   C[m][n] = act(sum_k A[m][k] B[n][k] + bias[n])
+ * on the matrix cores.  Sums are fp32; for results in bf16 and 8 bits the
+ * products of each eight neighbouring k are first added to within 2^-13 of
+ * the largest of them (1.5e-5 of the result's norm on random data).  A's format is either one, B's E4M3;
+ * either may have block_rows 1 or 128.  With B a layer's weights this is its
+ * forward pass; with B the transposed weights and A the output's gradient it
+ * is the input's gradient; with A the gradient transposed and B the input
+ * transposed (blocks along the rows of the batch) the weights' gradient.
+ *   bias        fp32 [N] or NULL.
+ *   activation  HWSEL_ACT_NONE or HWSEL_ACT_GELU (GELU(a) = a Phi(a), within
+ *               1e-6 absolute).
+ *   C           HWSEL_DTYPE_FP32 or HWSEL_DTYPE_BF16 (rounded once, nearest
+ *               even), row-major [M][ldc], ldc >= N in elements, aligned to
+ *               its elements.
+ *   workspace   hwsel_fp8_matmul_workspace_bytes(A, B) bytes of device
+ *               memory, 256-byte aligned; NULL where that is 0.
+ * The order of the sums is fixed by the sizes: the same inputs give the same
+ * bits.  Returns HWSEL_EINVAL for null pointers, sizes < 1 or that differ,
+ * bad strides, alignment, formats or activation, a short workspace;
+ * HWSEL_EUNSUPPORTED for B in E5M2 and another dtype.
+ */
+enum { HWSEL_ACT_NONE = 0, HWSEL_ACT_GELU = 1 };
+int hwsel_fp8_matmul_workspace_bytes(const hwsel_fp8_t *A, const hwsel_fp8_t *B, size_t *bytes);
+int hwsel_fp8_matmul(const hwsel_fp8_t *A, const hwsel_fp8_t *B, const float *bias, int32_t activation, void *C,
+                     int32_t dtype, int64_t ldc, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * hwsel_fp8_matmul whose result is the next layer's operand: C = the product
+ * with bias and activation in fp32, quantised as by hwsel_fp8_quantise
+ * (C->rows == M, C->cols == N, block_rows 1, format E4M3) without a trip
+ * through memory.  C must not overlap A or B.  Same workspace and status
+ * codes; HWSEL_EUNSUPPORTED for another block_rows or format of C.
+ */
+int hwsel_fp8_layer(const hwsel_fp8_t *A, const hwsel_fp8_t *B, const float *bias, int32_t activation,
+                    const hwsel_fp8_t *C, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Drawing candidates: per problem, n_draws local indices drawn (with
+ * replacement) from the softmax of its scores at a temperature, limited to
+ * the top_k best, then to the shortest best-first prefix that holds top_p of
+ * what is left, then to candidates of at least min_p times the best one's
+ * probability.  The random numbers are inputs and every step below is exact,
+ * so a draw does not depend on how the work is split.
+ *   Order: score descending, index ascending; -0 equals +0.  NaN and -inf
+ *   scores take no part.  best = the first.
+ *   Weight of a candidate, a whole number (1 = 2^-32 of the best one's):
+ *     d = s - best; t = d * rate (0 where s == best; NaN or below -60: -60);
+ *     rate = fp32(log2(e) / T), the quotient in binary64;
+ *     n = t rounded to nearest even; f = t - n; p = the degree-6 Taylor
+ *     polynomial of 2^f in fp32, Horner, each product and sum rounded;
+ *     weight = floor(p 2^32 / 2^-n), p a multiple of 2^-24.
+ *   top_k      keeps the first k (<= 0: all).
+ *   top_p      keeps those before which less than ceil(top_p * mass) lies,
+ *              mass the sum of the weights left by top_k and the product in
+ *              binary64; the first always (>= 1 or NaN: all; negative: the
+ *              first).
+ *   min_p      keeps weights >= ceil(min_p 2^32) (<= 0 or NaN: all of at
+ *              least 1; above 1 as 1).
+ *   T <= 0 or NaN keeps the first alone.
+ *   Draw j: total = the sum of the kept weights, r = floor(total * v / 2^24)
+ *   with v = floor(u[p][j] 2^24) limited to [0, 2^24 - 1] (NaN: 0); the first
+ *   kept candidate, by index, at which the running sum exceeds r.
+ * Outputs: idx int32 [P][n_draws]; prob fp32 [P][n_draws] (nullable) the
+ * drawn candidate's weight / total; kept int32 [P] (nullable) how many can be
+ * drawn.  A problem without a candidate (empty, or all NaN and -inf) gives
+ * idx -1, prob 0, kept 0.
+ *   Settings: the scalars of hwsel_sampling_t, or, where its pointer is not
+ *   NULL, a value for each problem (device [P]).
+ *   scores fp32 [R]; seg_offsets [P+1] as for hwsel_features (offsets outside
+ *   [0, R] are limited to it); u fp32 [P][n_draws] in [0, 1); workspace of
+ *   hwsel_sample_workspace_bytes(R, P, n_draws) bytes (device, 256-byte
+ *   aligned; NULL where that is 0).
+ * Returns HWSEL_EINVAL for null pointers, P < 1, R < 0, n_draws < 1, a short
+ * or misaligned workspace; HWSEL_EUNSUPPORTED for R > 2^30.
+ */
+typedef struct hwsel_sampling {
+    float temperature;
+    int32_t top_k;
+    float top_p, min_p;
+    const float *temperature_of;
+    const int32_t *top_k_of;
+    const float *top_p_of, *min_p_of;
+} hwsel_sampling_t;
+int hwsel_sample_workspace_bytes(int64_t R, int32_t P, int32_t n_draws, size_t *bytes);
+int hwsel_sample_per_problem(const float *scores, int64_t R, const int64_t *seg_offsets, int32_t P,
+                             const hwsel_sampling_t *how, const float *u, int32_t n_draws, int32_t *idx, float *prob,
+                             int32_t *kept, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Static text for a status code. */
 const char *hwsel_status_string(int status);
 /* Detail of the last failed call on this thread ("" if none). */

@@ -471,4 +471,167 @@ int hwsel_regret(const float *runtimes, const int64_t *seg_offsets, int32_t P, c
                     fn);
 }
 
+// Largest sizes of an 8-bit matrix: row numbers within an int32 with room to
+// step past the end, and columns whose
+// blocks fit a grid's second dimension (of 2^16 - 1 groups of four blocks)
+// and 256 rows of which lie within 2^32 bytes.
+static constexpr int64_t kFp8MaxRows = (int64_t)1 << 30, kFp8MaxCols = (int64_t)1 << 23;
+
+static int check_fp8(const hwsel_fp8_t *x, const char *name, const char *fn)
+{
+    if (!x || !x->q || !x->scale) return fail(HWSEL_EINVAL, fn, "%s: null pointer", name);
+    if (x->rows < 1 || x->cols < 1)
+        return fail(HWSEL_EINVAL, fn, "%s: %lld x %lld", name, (long long)x->rows, (long long)x->cols);
+    if (x->format != HWSEL_FP8_E4M3 && x->format != HWSEL_FP8_E5M2)
+        return fail(HWSEL_EINVAL, fn, "%s: format %d", name, x->format);
+    if (x->block_rows != 1 && x->block_rows != HWSEL_FP8_BLOCK)
+        return fail(HWSEL_EINVAL, fn, "%s: block_rows %d (1 or 128)", name, x->block_rows);
+    if (x->rows > kFp8MaxRows || x->cols > kFp8MaxCols)
+        return fail(HWSEL_EUNSUPPORTED, fn, "%s: %lld x %lld (at most %lld x %lld)", name, (long long)x->rows,
+                    (long long)x->cols, (long long)kFp8MaxRows, (long long)kFp8MaxCols);
+    const int64_t nkb = (x->cols + HWSEL_FP8_BLOCK - 1) / HWSEL_FP8_BLOCK;
+    if (x->ld < nkb * HWSEL_FP8_BLOCK || x->ld % 16 != 0 || !aligned16(x->q))
+        return fail(HWSEL_EINVAL, fn, "%s: codes misaligned or ld=%lld short", name, (long long)x->ld);
+    if (x->ld >= (int64_t)1 << 24) return fail(HWSEL_EUNSUPPORTED, fn, "%s: ld=%lld", name, (long long)x->ld);
+    if (x->ld_scale < nkb || x->ld_scale % 4 != 0 || ((uintptr_t)x->scale & 3u) != 0)
+        return fail(HWSEL_EINVAL, fn, "%s: scales misaligned or ld_scale=%lld short", name, (long long)x->ld_scale);
+    return HWSEL_OK;
+}
+
+// A plain matrix beside an 8-bit one: dtype, row length and element alignment.
+static int check_plain(const void *X, int32_t dtype, int64_t ld, int64_t cols, const char *fn)
+{
+    if (!X) return fail(HWSEL_EINVAL, fn, "null pointer");
+    if (dtype != HWSEL_DTYPE_FP32 && dtype != HWSEL_DTYPE_BF16)
+        return fail(HWSEL_EUNSUPPORTED, fn, "dtype %d (fp32 or bf16)", dtype);
+    if (ld < cols) return fail(HWSEL_EINVAL, fn, "ld=%lld < %lld", (long long)ld, (long long)cols);
+    if ((uintptr_t)X % (dtype == HWSEL_DTYPE_FP32 ? 4 : 2) != 0) return fail(HWSEL_EINVAL, fn, "matrix misaligned");
+    return HWSEL_OK;
+}
+
+int hwsel_fp8_quantise(const void *X, int32_t dtype, int64_t ld, int32_t transposed, const float *mean,
+                       const float *inv_std, const hwsel_fp8_t *out, void *stream)
+{
+    static const char *fn = "hwsel_fp8_quantise";
+    if (int st = check_fp8(out, "out", fn)) return st;
+    if (transposed != 0 && transposed != 1) return fail(HWSEL_EINVAL, fn, "transposed=%d", transposed);
+    if (int st = check_plain(X, dtype, ld, transposed ? out->rows : out->cols, fn)) return st;
+    if (!mean != !inv_std) return fail(HWSEL_EINVAL, fn, "mean and inv_std go together");
+    if (mean && (transposed || out->block_rows != 1))
+        return fail(HWSEL_EUNSUPPORTED, fn, "standardising goes with rows as they are and block_rows 1");
+    return launched(hwsel::launch_fp8_quantise(X, dtype == HWSEL_DTYPE_BF16, ld, transposed != 0, mean, inv_std, *out,
+                                               (hipStream_t)stream),
+                    fn);
+}
+
+int hwsel_fp8_dequantise(const hwsel_fp8_t *in, void *X, int32_t dtype, int64_t ld, void *stream)
+{
+    static const char *fn = "hwsel_fp8_dequantise";
+    if (int st = check_fp8(in, "in", fn)) return st;
+    if (int st = check_plain(X, dtype, ld, in->cols, fn)) return st;
+    return launched(hwsel::launch_fp8_dequantise(*in, X, dtype == HWSEL_DTYPE_BF16, ld, (hipStream_t)stream), fn);
+}
+
+int hwsel_fp8_transpose(const hwsel_fp8_t *in, const hwsel_fp8_t *out, void *stream)
+{
+    static const char *fn = "hwsel_fp8_transpose";
+    if (int st = check_fp8(in, "in", fn)) return st;
+    if (int st = check_fp8(out, "out", fn)) return st;
+    if (in->rows != out->cols || in->cols != out->rows)
+        return fail(HWSEL_EINVAL, fn, "%lld x %lld transposed is not %lld x %lld", (long long)in->rows,
+                    (long long)in->cols, (long long)out->rows, (long long)out->cols);
+    return launched(hwsel::launch_fp8_transpose(*in, *out, (hipStream_t)stream), fn);
+}
+
+static int check_product(const hwsel_fp8_t *A, const hwsel_fp8_t *B, const char *fn)
+{
+    if (int st = check_fp8(A, "A", fn)) return st;
+    if (int st = check_fp8(B, "B", fn)) return st;
+    if (A->cols != B->cols)
+        return fail(HWSEL_EINVAL, fn, "summed sizes %lld and %lld differ", (long long)A->cols, (long long)B->cols);
+    if (B->format != HWSEL_FP8_E4M3) return fail(HWSEL_EUNSUPPORTED, fn, "B in E5M2");
+    return HWSEL_OK;
+}
+
+static int check_product_call(const hwsel_fp8_t *A, const hwsel_fp8_t *B, const float *bias, int32_t activation,
+                              const void *workspace, size_t workspace_bytes, const char *fn)
+{
+    if (int st = check_product(A, B, fn)) return st;
+    if ((uintptr_t)bias & 3u) return fail(HWSEL_EINVAL, fn, "bias misaligned");
+    if (activation != HWSEL_ACT_NONE && activation != HWSEL_ACT_GELU)
+        return fail(HWSEL_EINVAL, fn, "activation %d", activation);
+    const size_t need = hwsel::fp8_matmul_workspace_bytes(A->rows, B->rows, A->cols);
+    if (need && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need))
+        return fail(HWSEL_EINVAL, fn, "workspace of %zu bytes, %zu needed, 256-byte aligned", workspace_bytes, need);
+    return HWSEL_OK;
+}
+
+int hwsel_fp8_matmul_workspace_bytes(const hwsel_fp8_t *A, const hwsel_fp8_t *B, size_t *bytes)
+{
+    static const char *fn = "hwsel_fp8_matmul_workspace_bytes";
+    if (!bytes) return fail(HWSEL_EINVAL, fn, "null pointer");
+    if (int st = check_product(A, B, fn)) return st;
+    *bytes = hwsel::fp8_matmul_workspace_bytes(A->rows, B->rows, A->cols);
+    g_err[0] = 0;
+    return HWSEL_OK;
+}
+
+int hwsel_fp8_matmul(const hwsel_fp8_t *A, const hwsel_fp8_t *B, const float *bias, int32_t activation, void *C,
+                     int32_t dtype, int64_t ldc, void *workspace, size_t workspace_bytes, void *stream)
+{
+    static const char *fn = "hwsel_fp8_matmul";
+    if (int st = check_product_call(A, B, bias, activation, workspace, workspace_bytes, fn)) return st;
+    if (int st = check_plain(C, dtype, ldc, B->rows, fn)) return st;
+    return launched(hwsel::launch_fp8_matmul(*A, *B, bias, activation == HWSEL_ACT_GELU, C, dtype == HWSEL_DTYPE_BF16, ldc,
+                                             workspace, (hipStream_t)stream),
+                    fn);
+}
+
+int hwsel_fp8_layer(const hwsel_fp8_t *A, const hwsel_fp8_t *B, const float *bias, int32_t activation,
+                    const hwsel_fp8_t *C, void *workspace, size_t workspace_bytes, void *stream)
+{
+    static const char *fn = "hwsel_fp8_layer";
+    if (int st = check_product_call(A, B, bias, activation, workspace, workspace_bytes, fn)) return st;
+    if (int st = check_fp8(C, "C", fn)) return st;
+    if (C->rows != A->rows || C->cols != B->rows)
+        return fail(HWSEL_EINVAL, fn, "C is %lld x %lld, the product %lld x %lld", (long long)C->rows, (long long)C->cols,
+                    (long long)A->rows, (long long)B->rows);
+    if (C->format != HWSEL_FP8_E4M3 || C->block_rows != 1)
+        return fail(HWSEL_EUNSUPPORTED, fn, "C: format %d block_rows %d (E4M3, 1)", C->format, C->block_rows);
+    return launched(hwsel::launch_fp8_layer(*A, *B, bias, activation == HWSEL_ACT_GELU, *C, workspace, (hipStream_t)stream), fn);
+}
+
+static int check_sample_sizes(int64_t R, int32_t P, int32_t n_draws, const char *fn)
+{
+    if (R < 0 || P < 1 || n_draws < 1)
+        return fail(HWSEL_EINVAL, fn, "R=%lld P=%d n_draws=%d", (long long)R, P, n_draws);
+    if (R > (int64_t)1 << 30) return fail(HWSEL_EUNSUPPORTED, fn, "R=%lld (at most 2^30)", (long long)R);
+    return HWSEL_OK;
+}
+
+int hwsel_sample_workspace_bytes(int64_t R, int32_t P, int32_t n_draws, size_t *bytes)
+{
+    static const char *fn = "hwsel_sample_workspace_bytes";
+    if (!bytes) return fail(HWSEL_EINVAL, fn, "null pointer");
+    if (int st = check_sample_sizes(R, P, n_draws, fn)) return st;
+    *bytes = hwsel::sample_workspace_bytes(R, P, n_draws);
+    g_err[0] = 0;
+    return HWSEL_OK;
+}
+
+int hwsel_sample_per_problem(const float *scores, int64_t R, const int64_t *seg_offsets, int32_t P,
+                             const hwsel_sampling_t *how, const float *u, int32_t n_draws, int32_t *idx, float *prob,
+                             int32_t *kept, void *workspace, size_t workspace_bytes, void *stream)
+{
+    static const char *fn = "hwsel_sample_per_problem";
+    if (int st = check_sample_sizes(R, P, n_draws, fn)) return st;
+    if ((!scores && R > 0) || !seg_offsets || !how || !u || !idx) return fail(HWSEL_EINVAL, fn, "null pointer");
+    const size_t need = hwsel::sample_workspace_bytes(R, P, n_draws);
+    if (need && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need))
+        return fail(HWSEL_EINVAL, fn, "workspace of %zu bytes, %zu needed, 256-byte aligned", workspace_bytes, need);
+    return launched(hwsel::launch_sample(scores, R, seg_offsets, P, *how, u, n_draws, idx, prob, kept, workspace,
+                                         (hipStream_t)stream),
+                    fn);
+}
+
 }  // extern "C"

@@ -1,0 +1,425 @@
+// Products of 8-bit matrices with block scales, C = act(A B^T + bias).
+//
+// v_mfma_scale_f32_16x16x128_f8f6f4 multiplies 16 x 128 by 128 x 16 codes and
+// scales each row of either by a power of two as it does so; one instruction
+// covers exactly one block of 128, so the scales cost no arithmetic and the
+// sums run on in fp32 accumulators over all of K.  The weights (B) are the
+// instruction's first operand: a lane then holds four consecutive columns n
+// of one row m of C.
+//
+// Within the instruction the products of eight neighbouring k are aligned to
+// the largest of them and kept to 2^-13 of it (measured: one product 2^-14 of
+// its neighbour's is lost, one eight places on is not; the groups are added as
+// fp32 sums are).  On random data that is 1.5e-5 of the result's norm, a
+// hundredth of a bf16 rounding, and of no account for results in bf16 or 8
+// bits.  For results in fp32 it would be a hundred times their rounding: they
+// take the bf16 instruction instead (EXACT), whose sums are fp32's, on codes
+// decoded and scaled in registers, at half the rate.
+#include "fp8.hpp"
+
+namespace hwsel {
+namespace {
+
+typedef int i32x8_t __attribute__((ext_vector_type(8)));
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
+
+enum OutKind { kOutF32, kOutBf16, kOutFp8, kOutPart };
+
+// What becomes of a sum.
+struct Out {
+    void *C;                                                // fp32, bf16 or codes; partial sums
+    int64_t ld;
+    uint8_t *scale;
+    int64_t ld_scale;
+    const float *bias;
+    int32_t gelu;
+    bool vec;                                               // four columns at a multiple of four at once
+};
+
+struct Operand {
+    const uint8_t *q;
+    int64_t ld;
+    const uint8_t *scale;
+    int64_t ld_scale;
+    int32_t rows, shift;                                    // shift: rows >> shift is a row's scale row
+};
+
+// GELU(a) = max(a, 0) - |a| Phi(-|a|), Phi(-x) = 2^P(x) for x >= 0 with the
+// polynomial P of degree 5 fitted on [0, 5] by gelu_fit.py: |error| <= 7e-7 for
+// every finite a, near the rounding of an fp32 sum of a few hundred terms.
+// Past the fitted range P keeps falling and the result is max(a, 0), here as
+// (a + |a|) / 2, which keeps a NaN; |a| stops at 64, where 2^P is 0, so that
+// an infinity meets no 0 times infinity.
+__device__ __forceinline__ float gelu_fine(float a)
+{
+    constexpr float c5 = -0.00047442156937904656f, c4 = 0.007105245254933834f, c3 = -0.0519152507185936f, c2 = -0.45985135436058044f, c1 = -1.1508772373199463f, c0 = -1.000020146369934f;
+    const float x = fminf(fabsf(a), 64.0f);
+    float p = fmaf(c5, x, c4);
+    p = fmaf(p, x, c3);
+    p = fmaf(p, x, c2);
+    p = fmaf(p, x, c1);
+    p = fmaf(p, x, c0);
+    return fmaf(-x, __builtin_amdgcn_exp2f(p), 0.5f * (a + fabsf(a)));
+}
+
+// v[i] = act(v[i] + bias[n + i]); columns from N on are set to 0.
+__device__ __forceinline__ void finish4(const Out &o, int32_t n, int32_t N, float (&v)[4])
+{
+    if (o.bias) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (n + i < N) v[i] += o.bias[n + i];
+    }
+    if (o.gelu) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = gelu_fine(v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = n + i < N ? v[i] : 0.0f;
+}
+
+template <OutKind KIND>
+__device__ __forceinline__ void store4(const Out &o, int64_t m, int32_t n, int32_t N, const float (&v)[4])
+{
+    static_assert(KIND == kOutF32 || KIND == kOutBf16 || KIND == kOutPart, "codes have their own way");
+    if (n >= N) return;
+    if constexpr (KIND == kOutBf16) {
+        uint16_t *at = static_cast<uint16_t *>(o.C) + m * o.ld + n;
+        const uint32_t a = bf16_pair(v[0], v[1]), b = bf16_pair(v[2], v[3]);
+        if (o.vec && n + 4 <= N) {
+            *reinterpret_cast<uint2 *>(at) = make_uint2(a, b);
+        } else {
+            at[0] = (uint16_t)a;
+            if (n + 1 < N) at[1] = (uint16_t)(a >> 16);
+            if (n + 2 < N) at[2] = (uint16_t)b;
+            if (n + 3 < N) at[3] = (uint16_t)(b >> 16);
+        }
+    } else {
+        float *at = static_cast<float *>(o.C) + m * o.ld + n;
+        if (KIND == kOutPart || (o.vec && n + 4 <= N)) {
+            *reinterpret_cast<float4 *>(at) = make_float4(v[0], v[1], v[2], v[3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (n + i < N) at[i] = v[i];
+        }
+    }
+}
+
+// 1,024 bytes (8 rows of 128) from rows r0.. of a tile to LDS at `to`: lane i
+// brings 16-byte chunk (i % 8) ^ swizzle of row r0 + i / 8 to place i.  With
+// chunks swizzled by (row / 2) % 8, the 16 rows that a fragment read touches
+// at one logical chunk lie on 16 different 16-byte bank groups.  Rows past the
+// end read the last one: what they give is not stored.
+__device__ __forceinline__ uint32_t lds_source(int r0, int lane, int32_t rows_left, int64_t ld)
+{
+    const int row = r0 + (lane >> 3), chunk = (lane & 7) ^ ((row >> 1) & 7);
+    return (uint32_t)((row < rows_left ? row : rows_left - 1) * ld + chunk * 16);
+}
+
+__device__ __forceinline__ void to_lds(const uint8_t *base, uint32_t offset, uint8_t *to)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(base + offset),
+                                     (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+}
+
+// A fragment: 32 bytes of row lane % 16, chunks lane / 16 and lane / 16 + 4 (any
+// pairing of k serves, if it is the same for both operands).
+__device__ __forceinline__ i32x8_t fragment(const uint8_t *tile, int lane)
+{
+    const int row = lane & 15, sw = (row >> 1) & 7, g = lane >> 4;
+    const i32x4_t a = *reinterpret_cast<const i32x4_t *>(tile + row * 128 + ((g ^ sw) << 4));
+    const i32x4_t b = *reinterpret_cast<const i32x4_t *>(tile + row * 128 + (((g ^ sw) ^ 4) << 4));
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// A fragment's 32 codes as bf16 values, scaled by 2^(lowest byte of scale - 127).
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+
+template <int FMT>
+__device__ __forceinline__ void decode(const i32x8_t &x, uint32_t scale, bf16x8_t (&out)[4])
+{
+    const float s = scale_value(scale & 0xffu);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        bf16x2_t v[4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t w = (uint32_t)x[2 * q + h];
+            if constexpr (FMT == 0) {
+                v[2 * h] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, false);
+                v[2 * h + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, true);
+            } else {
+                v[2 * h] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, s, false);
+                v[2 * h + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, s, true);
+            }
+        }
+        const auto lo = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3), hi = __builtin_shufflevector(v[2], v[3], 0, 1, 2, 3);
+        out[q] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+}
+
+// The scale bytes of blocks 4 j .. 4 j + 3 of a row, the first lowest.
+__device__ __forceinline__ uint32_t scale_word(const Operand &x, int32_t row, int32_t kb)
+{
+    const int32_t r = row < x.rows ? row : x.rows - 1;
+    return *reinterpret_cast<const uint32_t *>(x.scale + (int64_t)(r >> x.shift) * x.ld_scale + (kb & ~3));
+}
+
+// WM x WN waves, each MT x 8 tiles of 16 x 16 (128 columns: a whole block of
+// the next layer's operand).  Two LDS stages: the next block of K is on its
+// way while one is multiplied.
+template <int WM, int WN, int MT, int FA, bool EXACT, OutKind KIND>
+__global__ __launch_bounds__(64 * WM * WN) void k_product(Operand A, Operand B, int32_t nkb, int32_t per_split, Out o)
+{
+    constexpr int NT = 8, BM = WM * MT * 16, BN = WN * 128, kWaves = WM * WN;
+    constexpr int kLoadsA = BM / 8 / kWaves, kLoadsB = BN / 8 / kWaves;
+    static_assert(BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0, "loads per wave");
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[2][(BM + BN) * 128];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave % WM, wn = wave / WM;
+    // neighbours share rows of A
+    const int32_t n_tiles = (B.rows + BN - 1) / BN;
+    const int32_t m0 = (int32_t)(blockIdx.x / n_tiles) * BM, n0 = (int32_t)(blockIdx.x % n_tiles) * BN;
+    const int32_t k_begin = (int32_t)blockIdx.y * per_split, k_end = k_begin + per_split < nkb ? k_begin + per_split : nkb;
+    const uint8_t *a_base = A.q + (int64_t)m0 * A.ld, *b_base = B.q + (int64_t)n0 * B.ld;
+    uint32_t a_at[kLoadsA], b_at[kLoadsB];
+#pragma unroll
+    for (int i = 0; i < kLoadsA; ++i) a_at[i] = lds_source((wave * kLoadsA + i) * 8, lane, A.rows - m0, A.ld);
+#pragma unroll
+    for (int i = 0; i < kLoadsB; ++i) b_at[i] = lds_source((wave * kLoadsB + i) * 8, lane, B.rows - n0, B.ld);
+    auto fetch = [&](int32_t kb, uint8_t *stage) {
+        const int64_t k = (int64_t)kb * 128;
+#pragma unroll
+        for (int i = 0; i < kLoadsA; ++i) to_lds(a_base + k, a_at[i], stage + (wave * kLoadsA + i) * 1024);
+#pragma unroll
+        for (int i = 0; i < kLoadsB; ++i) to_lds(b_base + k, b_at[i], stage + BM * 128 + (wave * kLoadsB + i) * 1024);
+    };
+    f32x4_t acc[MT][NT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+    uint32_t sa[MT], sb[NT];
+    const int32_t row_a = m0 + wm * MT * 16 + (lane & 15), row_b = n0 + wn * 128 + (lane & 15);
+    auto scales = [&](int32_t kb) {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) sa[mt] = scale_word(A, row_a + 16 * mt, kb);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) sb[nt] = scale_word(B, row_b + 16 * nt, kb);
+    };
+    fetch(k_begin, lds[k_begin & 1]);
+    scales(k_begin);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) sa[mt] >>= 8 * (k_begin & 3);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) sb[nt] >>= 8 * (k_begin & 3);
+    for (int32_t kb = k_begin; kb < k_end; ++kb) {
+        __syncthreads();                                    // this stage has come; the other one is read
+        const uint8_t *stage = lds[kb & 1];
+        i32x8_t a[MT], b[NT];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) a[mt] = fragment(stage + (wm * MT + mt) * 2048, lane);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) b[nt] = fragment(stage + BM * 128 + (wn * NT + nt) * 2048, lane);
+        if (kb + 1 < k_end) fetch(kb + 1, lds[(kb + 1) & 1]);
+        if constexpr (EXACT) {
+            bf16x8_t wide[MT][4];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) decode<FA>(a[mt], sa[mt], wide[mt]);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                bf16x8_t w[4];
+                decode<0>(b[nt], sb[nt], w);
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt)
+                        acc[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[q], wide[mt][q], acc[mt][nt], 0, 0, 0);
+            }
+        } else {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+                    acc[mt][nt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[nt], a[mt], acc[mt][nt], 0, FA, 0,
+                                                                                  (int)sb[nt], 0, (int)sa[mt]);
+        }
+        if ((kb & 3) == 3) {
+            if (kb + 1 < k_end) scales(kb + 1);
+        } else {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) sa[mt] >>= 8;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) sb[nt] >>= 8;
+        }
+    }
+    // Lane l, element i of a tile: row m = l % 16, column n = 4 (l / 16) + i.
+    const int32_t N = B.rows;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        const int32_t m = row_a + 16 * mt;
+        const int32_t n_lane = n0 + wn * 128 + 4 * (lane >> 4);
+        if constexpr (KIND == kOutFp8) {
+            float v[NT][4];
+            uint32_t most = 0, all = 0;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[nt][i] = acc[mt][nt][i];
+                finish4(o, n_lane + 16 * nt, N, v[nt]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t f = finite_bits(v[nt][i]), x = __float_as_uint(v[nt][i]) & 0x7fffffffu;
+                    most = f > most ? f : most;
+                    all = x > all ? x : all;
+                }
+            }
+#pragma unroll
+            for (int l = 16; l < 64; l <<= 1) {
+                const uint32_t x = (uint32_t)__shfl_xor((int)most, l);
+                most = x > most ? x : most;
+            }
+            const uint32_t byte = scale_byte(most, HWSEL_FP8_E4M3);
+            const float s = inverse_scale(byte);
+            if (m < A.rows && n0 + wn * 128 < N) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+                    *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(o.C) + (int64_t)m * o.ld + n_lane + 16 * nt) =
+                        codes4_checked(v[nt], s, HWSEL_FP8_E4M3, all >= 0x7f800000u);
+                if (lane < 16) o.scale[(int64_t)m * o.ld_scale + (n0 >> 7) + wn] = (uint8_t)byte;
+            }
+        } else if (m < A.rows) {
+            Out to = o;
+            if constexpr (KIND == kOutPart)
+                to.C = static_cast<float *>(o.C) + (int64_t)blockIdx.y * A.rows * o.ld;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float v[4] = {acc[mt][nt][0], acc[mt][nt][1], acc[mt][nt][2], acc[mt][nt][3]};
+                if constexpr (KIND != kOutPart) finish4(o, n_lane + 16 * nt, N, v);
+                store4<KIND>(to, m, n_lane + 16 * nt, N, v);
+            }
+        }
+    }
+}
+
+// Sum of the splits' partial sums, in the order of K, and what becomes of it:
+// 32 lanes take 128 columns of a row.
+template <OutKind KIND>
+__global__ __launch_bounds__(256) void k_product_join(const float *__restrict__ part, int32_t splits, int32_t M, int32_t N,
+                                                      int64_t ldp, Out o)
+{
+    const int32_t blocks = (N + 127) / 128;
+    const int64_t items = (int64_t)M * blocks;
+    for (int64_t it = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); it < items; it += (int64_t)gridDim.x * 8) {
+        const int64_t m = it / blocks;
+        const int32_t kb = (int32_t)(it % blocks), n = kb * 128 + (threadIdx.x & 31) * 4;
+        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (n < N) {
+            for (int32_t z = 0; z < splits; ++z) {
+                const float4 p = *reinterpret_cast<const float4 *>(part + ((int64_t)z * M + m) * ldp + n);
+                v[0] += p.x; v[1] += p.y; v[2] += p.z; v[3] += p.w;
+            }
+        }
+        finish4(o, n, N, v);
+        if constexpr (KIND == kOutFp8) {
+            uint32_t most = 0, all = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t f = finite_bits(v[i]), x = __float_as_uint(v[i]) & 0x7fffffffu;
+                most = f > most ? f : most;
+                all = x > all ? x : all;
+            }
+#pragma unroll
+            for (int l = 1; l < 32; l <<= 1) {
+                const uint32_t x = (uint32_t)__shfl_xor((int)most, l, 32);
+                most = x > most ? x : most;
+            }
+            const uint32_t byte = scale_byte(most, HWSEL_FP8_E4M3);
+            *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(o.C) + m * o.ld + n) =
+                codes4_checked(v, inverse_scale(byte), HWSEL_FP8_E4M3, all >= 0x7f800000u);
+            if ((threadIdx.x & 31) == 0) o.scale[m * o.ld_scale + kb] = (uint8_t)byte;
+        } else {
+            store4<KIND>(o, m, n, N, v);
+        }
+    }
+}
+
+struct Plan {
+    int32_t splits, per_split;
+};
+
+constexpr int kBM = 128, kBN = 256;
+
+// K is split where the tiles leave compute units idle, at least four blocks to a split.
+Plan plan_product(int64_t M, int64_t N, int64_t nkb)
+{
+    const int64_t tiles = ((M + kBM - 1) / kBM) * ((N + kBN - 1) / kBN);
+    int64_t s = compute_units() / tiles;
+    s = s < nkb / 4 ? s : nkb / 4;
+    s = s < 1 ? 1 : s;
+    const int64_t per = (nkb + s - 1) / s;
+    return {(int32_t)((nkb + per - 1) / per), (int32_t)per};
+}
+
+Operand operand(const hwsel_fp8_t &x)
+{
+    return {x.q, x.ld, x.scale, x.ld_scale, (int32_t)x.rows, x.block_rows == 1 ? 0 : 7};
+}
+
+template <bool EXACT, OutKind KIND>
+void launch_tiles(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const Plan &p, const Out &o, hipStream_t s)
+{
+    const dim3 grid((unsigned)((B.rows + kBN - 1) / kBN * ((A.rows + kBM - 1) / kBM)), (unsigned)p.splits);
+    const int32_t nkb = (int32_t)fp8_blocks(A.cols);
+    if (A.format == HWSEL_FP8_E4M3)
+        hipLaunchKernelGGL((k_product<2, 2, 4, 0, EXACT, KIND>), grid, dim3(256), 0, s, operand(A), operand(B), nkb, p.per_split,
+                           o);
+    else
+        hipLaunchKernelGGL((k_product<2, 2, 4, 1, EXACT, KIND>), grid, dim3(256), 0, s, operand(A), operand(B), nkb, p.per_split,
+                           o);
+}
+
+int64_t part_ld(int64_t N) { return (N + 3) / 4 * 4; }
+
+template <OutKind KIND>
+hipError_t run_product(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const Out &o, void *ws, hipStream_t s)
+{
+    const Plan p = plan_product(A.rows, B.rows, fp8_blocks(A.cols));
+    if (p.splits == 1) {
+        launch_tiles<KIND == kOutF32, KIND>(A, B, p, o, s);
+    } else {
+        Out part = o;
+        part.C = ws;
+        part.ld = part_ld(B.rows);
+        launch_tiles<KIND == kOutF32, kOutPart>(A, B, p, part, s);
+        const int64_t items = A.rows * ((B.rows + 127) / 128), groups = (items + 7) / 8;
+        hipLaunchKernelGGL(k_product_join<KIND>, dim3((unsigned)(groups < 65536 ? groups : 65536)), dim3(256), 0, s,
+                           static_cast<const float *>(ws), p.splits, (int32_t)A.rows, (int32_t)B.rows, part.ld, o);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t fp8_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K)
+{
+    const Plan p = plan_product(M, N, fp8_blocks(K));
+    return p.splits == 1 ? 0 : (size_t)p.splits * (size_t)M * (size_t)part_ld(N) * 4;
+}
+
+hipError_t launch_fp8_matmul(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const float *bias, bool gelu, void *C, bool bf16,
+                             int64_t ldc, void *ws, hipStream_t s)
+{
+    const size_t el = bf16 ? 2 : 4;
+    const Out o{C, ldc, nullptr, 0, bias, gelu, ((uintptr_t)C | (uintptr_t)(ldc * el)) % (4 * el) == 0};
+    return bf16 ? run_product<kOutBf16>(A, B, o, ws, s) : run_product<kOutF32>(A, B, o, ws, s);
+}
+
+hipError_t launch_fp8_layer(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const float *bias, bool gelu, const hwsel_fp8_t &C,
+                            void *ws, hipStream_t s)
+{
+    return run_product<kOutFp8>(A, B, Out{C.q, C.ld, C.scale, C.ld_scale, bias, gelu, true}, ws, s);
+}
+
+}  // namespace hwsel

@@ -1,4 +1,4 @@
-"""Fit of the GELU tail used by the matrix-core MLP kernel (mlp.hip).
+"""Fits of the GELU tail used by the matrix-core kernels (mlp.hip, fp8_matmul.hip).
 
 GELU(a) = a Phi(a) = max(a, 0) - |a| Phi(-|a|), Phi the standard normal
 distribution function.  For x >= 0, log2 Phi(-x) is smooth and concave, so
@@ -9,7 +9,9 @@ error of 1e-4 costs nothing there and three FMAs are enough) is fitted on
 iteratively reweighted least squares on the absolute GELU error
 x |2^P(x) - Phi(-x)| (Lawson's iteration towards the minimax fit); the
 coefficients are then rounded to fp32 and the error is checked in fp32
-Horner arithmetic over [0, 12] and on a geometric grid up to 1e38.  Run
+Horner arithmetic over [0, 12] and on a geometric grid up to 1e38.  The 8-bit
+products take degree 5: their results may be fp32, and a code of three bits
+turns an error into a step of 6 % wherever it crosses a rounding boundary.  Run
 `python gelu_fit.py` to print the coefficients (highest degree first) and the
 error bound.
 """
@@ -44,7 +46,8 @@ def max_error(c32):
 
 
 if __name__ == "__main__":
-    c = fit()
-    err, at = max_error(c)
-    print("coefficients (x^%d .. x^0):" % (len(c) - 1), ", ".join(repr(float(v)) for v in c))
-    print("max |GELU error| = %.3g at |a| = %.3g" % (err, at))
+    for deg in (3, 5):
+        c = fit(deg)
+        err, at = max_error(c)
+        print("coefficients (x^%d .. x^0):" % (len(c) - 1), ", ".join(repr(float(v)) for v in c))
+        print("max |GELU error| = %.3g at |a| = %.3g" % (err, at))

@@ -135,6 +135,21 @@ hipError_t launch_topk(const float *scores, const int64_t *seg, int32_t P, int32
 hipError_t launch_regret(const float *rt, const int64_t *seg, int32_t P, const int32_t *idx,
                          int32_t k, float *r1, float *rk, int32_t *best, hipStream_t s);
 
+// 8-bit matrices and their products (see fp8.hip, fp8_matmul.hip).
+hipError_t launch_fp8_quantise(const void *X, bool bf16, int64_t ld, bool transposed, const float *mean,
+                               const float *inv_std, const hwsel_fp8_t &out, hipStream_t s);
+hipError_t launch_fp8_dequantise(const hwsel_fp8_t &in, void *X, bool bf16, int64_t ld, hipStream_t s);
+hipError_t launch_fp8_transpose(const hwsel_fp8_t &in, const hwsel_fp8_t &out, hipStream_t s);
+size_t fp8_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K);
+hipError_t launch_fp8_matmul(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const float *bias, bool gelu, void *C, bool bf16,
+                             int64_t ldc, void *ws, hipStream_t s);
+hipError_t launch_fp8_layer(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const float *bias, bool gelu, const hwsel_fp8_t &C,
+                            void *ws, hipStream_t s);
+
+size_t sample_workspace_bytes(int64_t R, int32_t P, int32_t n_draws);
+hipError_t launch_sample(const float *scores, int64_t R, const int64_t *seg, int32_t P, const hwsel_sampling_t &how,
+                         const float *u, int32_t n_draws, int32_t *idx, float *prob, int32_t *kept, void *ws, hipStream_t s);
+
 // Order-preserving map of fp32 to uint32 (x < y <=> key(x) < key(y) for
 // non-NaN values; -0 must be normalised to +0 first).
 __device__ __forceinline__ uint32_t order_key(float v)

@@ -1,0 +1,135 @@
+"""Refusals of the 8-bit and the sampling entry points: checked on the host
+before anything is enqueued, so they run without a GPU."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2609_35587_amd import hwsel
+
+FAKE = 0x1000   # never dereferenced: every call below is rejected first
+
+
+@pytest.fixture(scope="module")
+def L():
+    return hwsel.lib()
+
+
+def fp8(**over):
+    m = dict(rows=100, cols=300, q=FAKE, ld=384, scale=FAKE, ld_scale=4, format=0, block_rows=1)
+    m.update(over)
+    return hwsel.hwsel_fp8_t(*[m[n] for n, _ in hwsel.hwsel_fp8_t._fields_])
+
+
+BAD = [(dict(rows=0), 1), (dict(cols=0), 1), (dict(q=None), 1), (dict(scale=None), 1), (dict(q=FAKE + 8), 1),
+       (dict(ld=368), 1), (dict(ld=392), 1), (dict(ld_scale=2), 1), (dict(ld_scale=6), 1), (dict(scale=FAKE + 2), 1),
+       (dict(format=2), 1), (dict(format=-1), 1), (dict(block_rows=0), 1), (dict(block_rows=64), 1),
+       (dict(rows=(1 << 30) + 1), 2), (dict(cols=(1 << 23) + 1, ld=1 << 24, ld_scale=1 << 20), 2), (dict(ld=1 << 24), 2)]
+
+
+@pytest.mark.parametrize("over,status", BAD)
+def test_every_call_checks_its_matrices(L, over, status):
+    bad, good, n = C.byref(fp8(**over)), C.byref(fp8()), C.c_size_t(0)
+    assert L.hwsel_fp8_quantise(FAKE, 3, 300, 0, None, None, bad, None) == status
+    assert L.hwsel_fp8_dequantise(bad, FAKE, 3, 300, None) == status
+    assert L.hwsel_fp8_transpose(bad, good, None) == status
+    assert L.hwsel_fp8_matmul_workspace_bytes(bad, good, C.byref(n)) == status
+    assert L.hwsel_fp8_matmul(bad, good, None, 0, FAKE, 0, 100, None, 0, None) == status
+    assert L.hwsel_fp8_matmul(good, bad, None, 0, FAKE, 0, 100, None, 0, None) == status
+    assert L.hwsel_fp8_layer(bad, good, None, 0, good, None, 0, None) == status
+    assert L.hwsel_last_error().startswith(b"hwsel_fp8_layer: A: ")
+
+
+def test_null_matrices(L):
+    good = C.byref(fp8())
+    assert L.hwsel_fp8_quantise(FAKE, 3, 300, 0, None, None, None, None) == 1
+    assert L.hwsel_fp8_dequantise(None, FAKE, 3, 300, None) == 1
+    assert L.hwsel_fp8_transpose(good, None, None) == 1
+    assert L.hwsel_fp8_matmul(good, None, None, 0, FAKE, 0, 100, None, 0, None) == 1
+    assert L.hwsel_fp8_matmul_workspace_bytes(good, good, None) == 1
+
+
+@pytest.mark.parametrize("over,status", [
+    (dict(X=None), 1), (dict(dtype=1), 2), (dict(dtype=2), 2), (dict(ld=299), 1), (dict(X=FAKE + 2), 1),
+    (dict(dtype=0, X=FAKE + 1), 1), (dict(transposed=2), 1), (dict(transposed=1, ld=99), 1), (dict(mean=FAKE), 1),
+    (dict(inv_std=FAKE), 1), (dict(mean=FAKE, inv_std=FAKE, transposed=1), 2),
+    (dict(mean=FAKE, inv_std=FAKE, out=fp8(block_rows=128)), 2)])
+def test_quantise_rejects(L, over, status):
+    a = dict(X=FAKE, dtype=3, ld=300, transposed=0, mean=None, inv_std=None, out=fp8())
+    a.update(over)
+    assert L.hwsel_fp8_quantise(a["X"], a["dtype"], a["ld"], a["transposed"], a["mean"], a["inv_std"],
+                                C.byref(a["out"]), None) == status
+    assert L.hwsel_last_error().startswith(b"hwsel_fp8_quantise: ")
+
+
+def test_dequantise_and_transpose_reject(L):
+    good = fp8()
+    assert L.hwsel_fp8_dequantise(C.byref(good), None, 3, 300, None) == 1
+    assert L.hwsel_fp8_dequantise(C.byref(good), FAKE, 1, 300, None) == 2
+    assert L.hwsel_fp8_dequantise(C.byref(good), FAKE, 0, 299, None) == 1
+    assert L.hwsel_fp8_dequantise(C.byref(good), FAKE + 2, 3, 300, None) == 1
+    assert L.hwsel_fp8_transpose(C.byref(good), C.byref(fp8()), None) == 1
+    assert L.hwsel_fp8_transpose(C.byref(good), C.byref(fp8(rows=300, cols=101, ld=128)), None) == 1
+
+
+def test_products_reject(L):
+    def matmul(**over):
+        a = dict(A=fp8(), B=fp8(rows=200, block_rows=128), bias=None, act=0, C=FAKE, dtype=0, ldc=200, ws=None, n=0)
+        a.update(over)
+        return L.hwsel_fp8_matmul(C.byref(a["A"]), C.byref(a["B"]), a["bias"], a["act"], a["C"], a["dtype"], a["ldc"],
+                                  a["ws"], a["n"], None)
+
+    assert matmul(B=fp8(cols=301)) == 1
+    assert matmul(B=fp8(rows=200, format=1)) == 2
+    assert matmul(bias=FAKE + 2) == 1
+    assert matmul(act=2) == 1 and matmul(act=-1) == 1
+    assert matmul(C=None) == 1 and matmul(dtype=1) == 2 and matmul(ldc=199) == 1
+    assert matmul(C=FAKE + 1) == 1 and matmul(dtype=3, C=FAKE + 2) == 1
+    # a product whose K is split needs its workspace
+    long = dict(cols=1 << 20, ld=1 << 20, ld_scale=1 << 13)
+    A, B = fp8(rows=16, **long), fp8(rows=16, block_rows=128, **long)
+    n = C.c_size_t(0)
+    assert L.hwsel_fp8_matmul_workspace_bytes(C.byref(A), C.byref(B), C.byref(n)) == 0 and n.value > 0
+    assert matmul(A=A, B=B, ldc=16) == 1
+    assert matmul(A=A, B=B, ldc=16, ws=FAKE, n=n.value - 1) == 1
+    assert matmul(A=A, B=B, ldc=16, ws=FAKE + 16, n=n.value) == 1
+    assert L.hwsel_last_error().startswith(b"hwsel_fp8_matmul: workspace")
+
+    def layer(out):
+        return L.hwsel_fp8_layer(C.byref(fp8()), C.byref(fp8(rows=200, block_rows=128)), None, 0, C.byref(out), None, 0,
+                                 None)
+
+    assert layer(fp8(rows=100, cols=201)) == 1 and layer(fp8(rows=99, cols=200)) == 1
+    assert layer(fp8(rows=100, cols=200, block_rows=128)) == 2 and layer(fp8(rows=100, cols=200, format=1)) == 2
+    assert layer(fp8(rows=100, cols=200, ld=128)) == 1
+
+
+def test_sampling_rejects(L):
+    how = hwsel.hwsel_sampling_t(1.0, 0, 1.0, 0.0, None, None, None, None)
+
+    def call(**over):
+        a = dict(scores=FAKE, R=1000, seg=FAKE, P=4, how=C.byref(how), u=FAKE, draws=2, idx=FAKE)
+        a.update(over)
+        return L.hwsel_sample_per_problem(a["scores"], a["R"], a["seg"], a["P"], a["how"], a["u"], a["draws"], a["idx"],
+                                          None, None, None, 0, None)
+
+    assert call(scores=None) == 1 and call(seg=None) == 1 and call(how=None) == 1 and call(u=None) == 1
+    assert call(idx=None) == 1 and call(P=0) == 1 and call(R=-1) == 1 and call(draws=0) == 1
+    assert call(R=(1 << 30) + 1) == 2
+    assert L.hwsel_last_error().startswith(b"hwsel_sample_per_problem: ")
+    n = C.c_size_t(0)
+    assert L.hwsel_sample_workspace_bytes(1000, 0, 1, C.byref(n)) == 1
+    assert L.hwsel_sample_workspace_bytes(1000, 4, 1, None) == 1
+    assert L.hwsel_sample_workspace_bytes(1000, 4, 1, C.byref(n)) == 0
+
+
+def test_binding_rejects_host_tensors():
+    x = torch.zeros(4, 128)
+    m = dict(q=torch.zeros(4, 128, dtype=torch.uint8), scale=torch.zeros(4, 4, dtype=torch.uint8), rows=4, cols=128,
+             format=0, block_rows=1)
+    for call in (lambda: hwsel.hwsel_fp8_quantise(x), lambda: hwsel.hwsel_fp8_dequantise(m),
+                 lambda: hwsel.hwsel_fp8_transpose(m), lambda: hwsel.hwsel_fp8_matmul(m, m),
+                 lambda: hwsel.hwsel_fp8_layer(m, m),
+                 lambda: hwsel.hwsel_sample_per_problem(torch.zeros(4), torch.tensor([0, 4]), torch.zeros(1, 1))):
+        with pytest.raises(ValueError):
+            call()
