@@ -22,6 +22,7 @@ namespace {
 
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
 typedef int i32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 
 enum OutKind { kOutF32, kOutBf16, kOutFp8, kOutPart };
 
@@ -117,10 +118,16 @@ __device__ __forceinline__ uint32_t lds_source(int r0, int lane, int32_t rows_le
     return (uint32_t)((row < rows_left ? row : rows_left - 1) * ld + chunk * 16);
 }
 
-__device__ __forceinline__ void to_lds(const uint8_t *base, uint32_t offset, uint8_t *to)
+// The codes from a tile's first row on as a buffer: its base and the step along
+// K stay in scalar registers.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_buffer(const uint8_t *base)
 {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(base + offset),
-                                     (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(base), 0, 0xffffffff, 0x00027000);
+}
+
+__device__ __forceinline__ void to_lds(__amdgpu_buffer_rsrc_t tile, uint32_t offset, uint32_t k, uint8_t *to)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(tile, (__attribute__((address_space(3))) void *)to, 16, offset, k, 0, 0);
 }
 
 // A fragment: 32 bytes of row lane % 16, chunks lane / 16 and lane / 16 + 4 (any
@@ -166,6 +173,59 @@ __device__ __forceinline__ uint32_t scale_word(const Operand &x, int32_t row, in
     return *reinterpret_cast<const uint32_t *>(x.scale + (int64_t)(r >> x.shift) * x.ld_scale + (kb & ~3));
 }
 
+// What becomes of a wave's MT x 8 tiles, rows from m0, columns from n0 (a whole
+// block).  Lane l, element i of a tile: row m = l % 16, column n = 4 (l / 16) + i.
+template <int MT, OutKind KIND>
+__device__ __forceinline__ void finish_tiles(const f32x4_t (&acc)[MT][8], int32_t m0, int32_t n0, int32_t M, int32_t N,
+                                             int32_t split, const Out &o, int lane)
+{
+    constexpr int NT = 8;
+    const int32_t n_lane = n0 + 4 * (lane >> 4);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        const int32_t m = m0 + 16 * mt + (lane & 15);
+        if constexpr (KIND == kOutFp8) {
+            float v[NT][4];
+            uint32_t most = 0, all = 0;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[nt][i] = acc[mt][nt][i];
+                finish4(o, n_lane + 16 * nt, N, v[nt]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t f = finite_bits(v[nt][i]), x = __float_as_uint(v[nt][i]) & 0x7fffffffu;
+                    most = f > most ? f : most;
+                    all = x > all ? x : all;
+                }
+            }
+#pragma unroll
+            for (int l = 16; l < 64; l <<= 1) {
+                const uint32_t x = (uint32_t)__shfl_xor((int)most, l);
+                most = x > most ? x : most;
+            }
+            const uint32_t byte = scale_byte(most, HWSEL_FP8_E4M3);
+            const float s = inverse_scale(byte);
+            if (m < M && n0 < N) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+                    *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(o.C) + (int64_t)m * o.ld + n_lane + 16 * nt) =
+                        codes4_checked(v[nt], s, HWSEL_FP8_E4M3, all >= 0x7f800000u);
+                if (lane < 16) o.scale[(int64_t)m * o.ld_scale + (n0 >> 7)] = (uint8_t)byte;
+            }
+        } else if (m < M) {
+            Out to = o;
+            if constexpr (KIND == kOutPart) to.C = static_cast<float *>(o.C) + (int64_t)split * M * o.ld;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float v[4] = {acc[mt][nt][0], acc[mt][nt][1], acc[mt][nt][2], acc[mt][nt][3]};
+                if constexpr (KIND != kOutPart) finish4(o, n_lane + 16 * nt, N, v);
+                store4<KIND>(to, m, n_lane + 16 * nt, N, v);
+            }
+        }
+    }
+}
+
 // WM x WN waves, each MT x 8 tiles of 16 x 16 (128 columns: a whole block of
 // the next layer's operand).  Two LDS stages: the next block of K is on its
 // way while one is multiplied.
@@ -182,18 +242,18 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(Operand A, Operand B, 
     const int32_t n_tiles = (B.rows + BN - 1) / BN;
     const int32_t m0 = (int32_t)(blockIdx.x / n_tiles) * BM, n0 = (int32_t)(blockIdx.x % n_tiles) * BN;
     const int32_t k_begin = (int32_t)blockIdx.y * per_split, k_end = k_begin + per_split < nkb ? k_begin + per_split : nkb;
-    const uint8_t *a_base = A.q + (int64_t)m0 * A.ld, *b_base = B.q + (int64_t)n0 * B.ld;
+    const auto a_tile = tile_buffer(A.q + (int64_t)m0 * A.ld), b_tile = tile_buffer(B.q + (int64_t)n0 * B.ld);
     uint32_t a_at[kLoadsA], b_at[kLoadsB];
 #pragma unroll
     for (int i = 0; i < kLoadsA; ++i) a_at[i] = lds_source((wave * kLoadsA + i) * 8, lane, A.rows - m0, A.ld);
 #pragma unroll
     for (int i = 0; i < kLoadsB; ++i) b_at[i] = lds_source((wave * kLoadsB + i) * 8, lane, B.rows - n0, B.ld);
     auto fetch = [&](int32_t kb, uint8_t *stage) {
-        const int64_t k = (int64_t)kb * 128;
+        const uint32_t k = (uint32_t)kb * 128;
 #pragma unroll
-        for (int i = 0; i < kLoadsA; ++i) to_lds(a_base + k, a_at[i], stage + (wave * kLoadsA + i) * 1024);
+        for (int i = 0; i < kLoadsA; ++i) to_lds(a_tile, a_at[i], k, stage + (wave * kLoadsA + i) * 1024);
 #pragma unroll
-        for (int i = 0; i < kLoadsB; ++i) to_lds(b_base + k, b_at[i], stage + BM * 128 + (wave * kLoadsB + i) * 1024);
+        for (int i = 0; i < kLoadsB; ++i) to_lds(b_tile, b_at[i], k, stage + BM * 128 + (wave * kLoadsB + i) * 1024);
     };
     f32x4_t acc[MT][NT];
 #pragma unroll
@@ -254,53 +314,135 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(Operand A, Operand B, 
             for (int nt = 0; nt < NT; ++nt) sb[nt] >>= 8;
         }
     }
-    // Lane l, element i of a tile: row m = l % 16, column n = 4 (l / 16) + i.
-    const int32_t N = B.rows;
+    finish_tiles<MT, KIND>(acc, m0 + wm * MT * 16, n0 + wn * 128, A.rows, B.rows, (int32_t)blockIdx.y, o, lane);
+}
+
+// The tile that workgroup b of n works on: the eight XCDs take consecutive
+// ranges of the tiles, so that neighbours share an L2, and within those
+// 8 tiles along m go with every n before the next 8.
+__device__ __forceinline__ void tile_of(int32_t b, int32_t m_tiles, int32_t n_tiles, int32_t &mt, int32_t &nt)
+{
+    const int32_t n = m_tiles * n_tiles, q = n / 8, r = n % 8, x = b % 8;
+    const int32_t t = x * q + (x < r ? x : r) + b / 8, band = t / (8 * n_tiles), first = band * 8;
+    const int32_t rows = m_tiles - first < 8 ? m_tiles - first : 8, in = t - band * 8 * n_tiles;
+    mt = first + in % rows;
+    nt = in / rows;
+}
+
+// 256 x 256 tiles by eight waves in two groups, a wave of each on every SIMD.
+// A step of K has two phases with a barrier after each: while one group reads
+// its fragments from LDS the other one multiplies, so the matrix cores and LDS
+// are both busy all the time.  The second group runs a phase behind.
+template <int FA, OutKind KIND>
+__global__ __launch_bounds__(512) void k_product_deep(Operand A, Operand B, int32_t nkb, int32_t per_split, Out o)
+{
+    constexpr int MT = 4, NT = 8, BM = 256, BN = 256, kStage = (BM + BN) * 128;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kStage];
+    // Exponent bytes of four blocks of K: [block][A: wave rows, row % 16, tile][B: alike],
+    // so that one read brings a lane the bytes of its row of every tile.
+    __shared__ __attribute__((aligned(16))) uint8_t scale_lds[2][4][512];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool second = wave >= 4;                          // the second group: rows 128 .. 255
+    const int wm = wave >> 1, wn = wave & 1;                // the wave's 64 rows and 128 columns
+    int32_t m_tile, n_tile;
+    tile_of(blockIdx.x, (A.rows + BM - 1) / BM, (B.rows + BN - 1) / BN, m_tile, n_tile);
+    const int32_t m0 = m_tile * BM, n0 = n_tile * BN;
+    // (splits start at multiples of four blocks)
+    const int32_t k_begin = (int32_t)blockIdx.y * per_split, k_end = k_begin + per_split < nkb ? k_begin + per_split : nkb;
+    const auto a_tile = tile_buffer(A.q + (int64_t)m0 * A.ld), b_tile = tile_buffer(B.q + (int64_t)n0 * B.ld);
+    // a wave brings 32 rows of A, those of its own group; a wave of the first group 64 of B
+    uint32_t a_at[4], b_at[8];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-        const int32_t m = row_a + 16 * mt;
-        const int32_t n_lane = n0 + wn * 128 + 4 * (lane >> 4);
-        if constexpr (KIND == kOutFp8) {
-            float v[NT][4];
-            uint32_t most = 0, all = 0;
+    for (int i = 0; i < 4; ++i) a_at[i] = lds_source(wave * 32 + i * 8, lane, A.rows - m0, A.ld);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
+    for (int i = 0; i < 8; ++i) b_at[i] = lds_source((wave & 3) * 64 + i * 8, lane, B.rows - n0, B.ld);
+    // (past the end the last block is brought again, to a stage that is not read)
+    auto k_of = [&](int32_t kb) { return (uint32_t)(kb < k_end ? kb : k_end - 1) * 128; };
+    // thread t brings the bytes of row t of A's 256, then of B's
+    const int32_t own = (int32_t)threadIdx.x & 255;
+    const bool of_b = threadIdx.x >= 256;
+    const int scale_at = of_b ? 256 + (own & 128) + (own & 15) * 8 + ((own >> 4) & 7) : (own & 192) + (own & 15) * 4 + ((own >> 4) & 3);
+    auto load_scales = [&](int32_t kb) -> uint32_t {        // (of the last blocks again past the end)
+        kb = kb < nkb ? kb : nkb - 1;
+        return of_b ? scale_word(B, n0 + own, kb) : scale_word(A, m0 + own, kb);
+    };
+    auto put_scales = [&](int32_t kb, uint32_t w) {
+        uint8_t *to = &scale_lds[(kb >> 2) & 1][0][scale_at];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[nt][i] = acc[mt][nt][i];
-                finish4(o, n_lane + 16 * nt, N, v[nt]);
+        for (int i = 0; i < 4; ++i) to[512 * i] = (uint8_t)(w >> (8 * i));
+    };
+    f32x4_t acc[MT][NT];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t f = finite_bits(v[nt][i]), x = __float_as_uint(v[nt][i]) & 0x7fffffffu;
-                    most = f > most ? f : most;
-                    all = x > all ? x : all;
-                }
-            }
+    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int l = 16; l < 64; l <<= 1) {
-                const uint32_t x = (uint32_t)__shfl_xor((int)most, l);
-                most = x > most ? x : most;
-            }
-            const uint32_t byte = scale_byte(most, HWSEL_FP8_E4M3);
-            const float s = inverse_scale(byte);
-            if (m < A.rows && n0 + wn * 128 < N) {
+        for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+    auto barrier = [] {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    auto fetch_a = [&](int32_t kb, int i) { to_lds(a_tile, a_at[i], k_of(kb), lds + (kb & 1) * kStage + (wave * 4 + i) * 1024); };
+    auto fetch_b = [&](int32_t kb) {
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-                    *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(o.C) + (int64_t)m * o.ld + n_lane + 16 * nt) =
-                        codes4_checked(v[nt], s, HWSEL_FP8_E4M3, all >= 0x7f800000u);
-                if (lane < 16) o.scale[(int64_t)m * o.ld_scale + (n0 >> 7) + wn] = (uint8_t)byte;
-            }
-        } else if (m < A.rows) {
-            Out to = o;
-            if constexpr (KIND == kOutPart)
-                to.C = static_cast<float *>(o.C) + (int64_t)blockIdx.y * A.rows * o.ld;
+        for (int i = 0; i < 8; ++i)
+            to_lds(b_tile, b_at[i], k_of(kb), lds + (kb & 1) * kStage + BM * 128 + ((wave & 3) * 8 + i) * 1024);
+    };
+    auto lds_done = [] { __builtin_amdgcn_s_waitcnt(0xc07f); };           // lgkmcnt(0)
+    if (!second) fetch_b(k_begin);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                float v[4] = {acc[mt][nt][0], acc[mt][nt][1], acc[mt][nt][2], acc[mt][nt][3]};
-                if constexpr (KIND != kOutPart) finish4(o, n_lane + 16 * nt, N, v);
-                store4<KIND>(to, m, n_lane + 16 * nt, N, v);
-            }
-        }
+    for (int i = 0; i < 4; ++i) fetch_a(k_begin, i);
+    put_scales(k_begin, load_scales(k_begin));
+    if (!second) fetch_b(k_begin + 1);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) fetch_a(k_begin + 1, i);
+    __builtin_amdgcn_s_waitcnt(0x0f70);                     // vmcnt(0)
+    lds_done();
+    barrier();
+    if (second) barrier();
+    uint32_t next_scales = 0;
+    for (int32_t kb = k_begin; kb < k_end; ++kb) {
+        const uint8_t *stage = lds + (kb & 1) * kStage;
+        const uint8_t *sc = scale_lds[(kb >> 2) & 1][kb & 3];
+        i32x8_t a[MT], b[NT];
+        const uint32_t sa = *reinterpret_cast<const uint32_t *>(sc + wm * 64 + (lane & 15) * 4);
+        const u32x2_t sb = *reinterpret_cast<const u32x2_t *>(sc + 256 + wn * 128 + (lane & 15) * 8);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) a[mt] = fragment(stage + (wm * MT + mt) * 2048, lane);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) b[nt] = fragment(stage + BM * 128 + (wn * NT + nt) * 2048, lane);
+        __builtin_amdgcn_sched_barrier(0);
+        // the other stage: the second group has read it in the phase before
+        if (!second && kb > k_begin) fetch_b(kb + 1);
+        if ((kb & 3) == 2) put_scales(kb + 2, next_scales);
+        lds_done();                                         // the fragments are here
+        barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        if ((kb & 3) == 1) next_scales = load_scales(kb + 3);
+        __builtin_amdgcn_s_setprio(1);
+#define TILE(nt, mt)                                                                                                          \
+    acc[mt][nt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[nt], a[mt], acc[mt][nt], 0, FA, (nt) & 3,                 \
+                                                                   (int)((nt) < 4 ? sb.x : sb.y), mt, (int)sa)
+#define TILES(nt) TILE(nt, 0); TILE(nt, 1); TILE(nt, 2); TILE(nt, 3)
+#define STEP(i)                                                                                                               \
+    TILES(2 * i);                                                                                                             \
+    __builtin_amdgcn_sched_barrier(0);                                                                                        \
+    fetch_a(kb + 2, i);                                                                                                       \
+    __builtin_amdgcn_sched_barrier(0);                                                                                        \
+    TILES(2 * i + 1)
+        // this stage's rows of A: the group itself has read them
+        STEP(0); STEP(1); STEP(2); STEP(3);
+#undef STEP
+#undef TILES
+#undef TILE
+        __builtin_amdgcn_s_setprio(0);
+        // all but the four loads just made have landed
+        __builtin_amdgcn_s_waitcnt(0x0f74);
+        __builtin_amdgcn_sched_barrier(0);
+        barrier();
     }
+    if (!second) barrier();
+    __builtin_amdgcn_s_waitcnt(0x0f70);                     // (no load to LDS outlives the workgroup)
+    finish_tiles<MT, KIND>(acc, m0 + wm * 64, n0 + wn * 128, A.rows, B.rows, (int32_t)blockIdx.y, o, lane);
 }
 
 // Sum of the splits' partial sums, in the order of K, and what becomes of it:
@@ -351,6 +493,8 @@ struct Plan {
 
 constexpr int kBM = 128, kBN = 256;
 
+bool deep(int64_t M, int64_t N, bool exact) { return !exact && M >= 256 && N >= 256; }
+
 // K is split where the tiles leave compute units idle, at least four blocks to a split.
 Plan plan_product(int64_t M, int64_t N, int64_t nkb)
 {
@@ -358,7 +502,7 @@ Plan plan_product(int64_t M, int64_t N, int64_t nkb)
     int64_t s = compute_units() / tiles;
     s = s < nkb / 4 ? s : nkb / 4;
     s = s < 1 ? 1 : s;
-    const int64_t per = (nkb + s - 1) / s;
+    const int64_t per = (nkb + 4 * s - 1) / (4 * s) * 4;    // multiples of four blocks
     return {(int32_t)((nkb + per - 1) / per), (int32_t)per};
 }
 
@@ -370,8 +514,18 @@ Operand operand(const hwsel_fp8_t &x)
 template <bool EXACT, OutKind KIND>
 void launch_tiles(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const Plan &p, const Out &o, hipStream_t s)
 {
-    const dim3 grid((unsigned)((B.rows + kBN - 1) / kBN * ((A.rows + kBM - 1) / kBM)), (unsigned)p.splits);
     const int32_t nkb = (int32_t)fp8_blocks(A.cols);
+    if constexpr (!EXACT) {
+        if (deep(A.rows, B.rows, EXACT)) {
+            const dim3 grid((unsigned)((B.rows + 255) / 256 * ((A.rows + 255) / 256)), (unsigned)p.splits);
+            if (A.format == HWSEL_FP8_E4M3)
+                hipLaunchKernelGGL((k_product_deep<0, KIND>), grid, dim3(512), 0, s, operand(A), operand(B), nkb, p.per_split, o);
+            else
+                hipLaunchKernelGGL((k_product_deep<1, KIND>), grid, dim3(512), 0, s, operand(A), operand(B), nkb, p.per_split, o);
+            return;
+        }
+    }
+    const dim3 grid((unsigned)((B.rows + kBN - 1) / kBN * ((A.rows + kBM - 1) / kBM)), (unsigned)p.splits);
     if (A.format == HWSEL_FP8_E4M3)
         hipLaunchKernelGGL((k_product<2, 2, 4, 0, EXACT, KIND>), grid, dim3(256), 0, s, operand(A), operand(B), nkb, p.per_split,
                            o);
