@@ -63,6 +63,16 @@ __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, i
     return (uint32_t)w;
 }
 
+// Four finite values or NaN to E4M3 codes, divided by the power of two s on the way.
+__device__ __forceinline__ uint32_t scaled_codes4(const float *v, float s)
+{
+    typedef short s16x2_t __attribute__((ext_vector_type(2)));
+    s16x2_t w = {0, 0};
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, v[0], v[1], s, false);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, v[2], v[3], s, true);
+    return __builtin_bit_cast(uint32_t, w);
+}
+
 // The code of a NaN or an infinity.
 __device__ __forceinline__ uint32_t odd_code(float v, int32_t format)
 {

@@ -34,7 +34,7 @@ struct Out {
     int64_t ld_scale;
     const float *bias;
     int32_t gelu;
-    bool vec;                                               // four columns at a multiple of four at once
+    bool vec, wide;                                         // four columns at a multiple of four, eight of eight at once
 };
 
 struct Operand {
@@ -48,19 +48,20 @@ struct Operand {
 // GELU(a) = max(a, 0) - |a| Phi(-|a|), Phi(-x) = 2^P(x) for x >= 0 with the
 // polynomial P of degree 5 fitted on [0, 5] by gelu_fit.py: |error| <= 7e-7 for
 // every finite a, near the rounding of an fp32 sum of a few hundred terms.
-// Past the fitted range P keeps falling and the result is max(a, 0), here as
-// (a + |a|) / 2, which keeps a NaN; |a| stops at 64, where 2^P is 0, so that
-// an infinity meets no 0 times infinity.
+// Past the fitted range P keeps falling and the result is max(a, 0); the
+// maximum is the one that keeps a NaN, and |a| stops at 64, where 2^P is 0, so
+// that an infinity meets no 0 times infinity.  Nine instructions.
 __device__ __forceinline__ float gelu_fine(float a)
 {
-    constexpr float c5 = -0.00047442156937904656f, c4 = 0.007105245254933834f, c3 = -0.0519152507185936f, c2 = -0.45985135436058044f, c1 = -1.1508772373199463f, c0 = -1.000020146369934f;
+    constexpr float c5 = -0.00047442156937904656f, c4 = 0.007105245254933834f, c3 = -0.0519152507185936f,
+                    c2 = -0.45985135436058044f, c1 = -1.1508772373199463f, c0 = -1.000020146369934f;
     const float x = fminf(fabsf(a), 64.0f);
     float p = fmaf(c5, x, c4);
     p = fmaf(p, x, c3);
     p = fmaf(p, x, c2);
     p = fmaf(p, x, c1);
     p = fmaf(p, x, c0);
-    return fmaf(-x, __builtin_amdgcn_exp2f(p), 0.5f * (a + fabsf(a)));
+    return fmaf(-x, __builtin_amdgcn_exp2f(p), __builtin_elementwise_maximum(a, 0.0f));
 }
 
 // v[i] = act(v[i] + bias[n + i]); columns from N on are set to 0.
@@ -115,7 +116,7 @@ __device__ __forceinline__ void store4(const Out &o, int64_t m, int32_t n, int32
 __device__ __forceinline__ uint32_t lds_source(int r0, int lane, int32_t rows_left, int64_t ld)
 {
     const int row = r0 + (lane >> 3), chunk = (lane & 7) ^ ((row >> 1) & 7);
-    return (uint32_t)((row < rows_left ? row : rows_left - 1) * ld + chunk * 16);
+    return __umul24((uint32_t)(row < rows_left ? row : rows_left - 1), (uint32_t)ld) + chunk * 16;
 }
 
 // The codes from a tile's first row on as a buffer: its base and the step along
@@ -173,64 +174,162 @@ __device__ __forceinline__ uint32_t scale_word(const Operand &x, int32_t row, in
     return *reinterpret_cast<const uint32_t *>(x.scale + (int64_t)(r >> x.shift) * x.ld_scale + (kb & ~3));
 }
 
+// Four registers seen by the four groups of 16 lanes as a 4 x 4 matrix, transposed:
+// x[j] of group g becomes x[g] of group j.
+__device__ __forceinline__ void transpose_groups(uint32_t &a, uint32_t &b, uint32_t &c, uint32_t &d)
+{
+    const auto ac = __builtin_amdgcn_permlane32_swap(a, c, false, false), bd = __builtin_amdgcn_permlane32_swap(b, d, false, false);
+    const auto lo = __builtin_amdgcn_permlane16_swap(ac[0], bd[0], false, false),
+               hi = __builtin_amdgcn_permlane16_swap(ac[1], bd[1], false, false);
+    a = lo[0];
+    b = lo[1];
+    c = hi[0];
+    d = hi[1];
+}
+
+// Maximum over the four groups of 16 lanes, in every lane.
+__device__ __forceinline__ float groups_max(float v)
+{
+    const uint32_t u = __float_as_uint(v);
+    const auto h = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const uint32_t m = __float_as_uint(fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1])));
+    const auto q = __builtin_amdgcn_permlane16_swap(m, m, false, false);
+    return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
+}
+
+// The sums' first values: the bias, for a product that ends in this launch.
+template <int MT, OutKind KIND>
+__device__ __forceinline__ void start_tiles(f32x4_t (&acc)[MT][8], int32_t n0, int32_t N, const Out &o, int lane)
+{
+    const int32_t n_lane = n0 + 4 * (lane >> 4);
+#pragma unroll
+    for (int nt = 0; nt < 8; ++nt) {
+        f32x4_t v = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (KIND != kOutPart && o.bias) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int32_t n = n_lane + 16 * nt + i;
+                v[i] = o.bias[n < N ? n : N - 1];
+            }
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) acc[mt][nt] = v;
+    }
+}
+
 // What becomes of a wave's MT x 8 tiles, rows from m0, columns from n0 (a whole
 // block).  Lane l, element i of a tile: row m = l % 16, column n = 4 (l / 16) + i.
+// The lanes of a row exchange what they hold so that each stores 16 bytes.
 template <int MT, OutKind KIND>
 __device__ __forceinline__ void finish_tiles(const f32x4_t (&acc)[MT][8], int32_t m0, int32_t n0, int32_t M, int32_t N,
                                              int32_t split, const Out &o, int lane)
 {
     constexpr int NT = 8;
-    const int32_t n_lane = n0 + 4 * (lane >> 4);
+    if (n0 >= N || m0 >= M) return;                         // (the whole wave)
+    const int32_t g = lane >> 4, n_lane = n0 + 4 * g;
+    const bool whole = n0 + 128 <= N;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
         const int32_t m = m0 + 16 * mt + (lane & 15);
+        float v[NT][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[nt][i] = acc[mt][nt][i];
+        if (KIND != kOutPart && o.gelu) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[nt][i] = gelu_fine(v[nt][i]);
+        }
         if constexpr (KIND == kOutFp8) {
-            float v[NT][4];
-            uint32_t most = 0, all = 0;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[nt][i] = acc[mt][nt][i];
-                finish4(o, n_lane + 16 * nt, N, v[nt]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t f = finite_bits(v[nt][i]), x = __float_as_uint(v[nt][i]) & 0x7fffffffu;
-                    most = f > most ? f : most;
-                    all = x > all ? x : all;
-                }
-            }
-#pragma unroll
-            for (int l = 16; l < 64; l <<= 1) {
-                const uint32_t x = (uint32_t)__shfl_xor((int)most, l);
-                most = x > most ? x : most;
-            }
-            const uint32_t byte = scale_byte(most, HWSEL_FP8_E4M3);
-            const float s = inverse_scale(byte);
-            if (m < M && n0 < N) {
+            if (!whole) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
-                    *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(o.C) + (int64_t)m * o.ld + n_lane + 16 * nt) =
-                        codes4_checked(v[nt], s, HWSEL_FP8_E4M3, all >= 0x7f800000u);
-                if (lane < 16) o.scale[(int64_t)m * o.ld_scale + (n0 >> 7)] = (uint8_t)byte;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[nt][i] = n_lane + 16 * nt + i < N ? v[nt][i] : 0.0f;
+            }
+            float most = 0.0f;                              // (NaN do not count)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                most = fmaxf(fmaxf(fabsf(v[nt][0]), fabsf(v[nt][1])), most);
+                most = fmaxf(fmaxf(fabsf(v[nt][2]), fabsf(v[nt][3])), most);
+            }
+            most = groups_max(most);
+            uint32_t w[NT], byte;
+            if (__any(most == __builtin_inff())) {          // infinities do not count either
+                uint32_t bits = 0;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t f = finite_bits(v[nt][i]);
+                        bits = f > bits ? f : bits;
+                    }
+                byte = scale_byte(__float_as_uint(groups_max(__uint_as_float(bits))), HWSEL_FP8_E4M3);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) w[nt] = codes4_checked(v[nt], inverse_scale(byte), HWSEL_FP8_E4M3, true);
+            } else {
+                byte = scale_byte(__float_as_uint(most), HWSEL_FP8_E4M3);
+                const float s = __uint_as_float(byte << 23);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) w[nt] = scaled_codes4(v[nt], s);
+            }
+            transpose_groups(w[0], w[1], w[2], w[3]);
+            transpose_groups(w[4], w[5], w[6], w[7]);
+            if (m < M) {
+                uint8_t *at = static_cast<uint8_t *>(o.C) + (int64_t)m * o.ld + n0 + 16 * g;
+                *reinterpret_cast<uint4 *>(at) = make_uint4(w[0], w[1], w[2], w[3]);
+                *reinterpret_cast<uint4 *>(at + 64) = make_uint4(w[4], w[5], w[6], w[7]);
+                if (g == 0) o.scale[(int64_t)m * o.ld_scale + (n0 >> 7)] = (uint8_t)byte;
+            }
+        } else if (KIND == kOutBf16 && whole && o.wide) {
+            uint32_t lo[NT], hi[NT];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                lo[nt] = bf16_pair(v[nt][0], v[nt][1]);
+                hi[nt] = bf16_pair(v[nt][2], v[nt][3]);
+            }
+#pragma unroll
+            for (int h = 0; h < NT; h += 4) {
+                transpose_groups(lo[h], lo[h + 1], lo[h + 2], lo[h + 3]);
+                transpose_groups(hi[h], hi[h + 1], hi[h + 2], hi[h + 3]);
+            }
+            if (m < M) {
+#pragma unroll
+                for (int h = 0; h < NT; h += 4) {
+                    uint4 *at = reinterpret_cast<uint4 *>(static_cast<uint16_t *>(o.C) + (int64_t)m * o.ld + n0 + 16 * (h + g));
+                    at[0] = make_uint4(lo[h], hi[h], lo[h + 1], hi[h + 1]);
+                    at[1] = make_uint4(lo[h + 2], hi[h + 2], lo[h + 3], hi[h + 3]);
+                }
             }
         } else if (m < M) {
             Out to = o;
             if constexpr (KIND == kOutPart) to.C = static_cast<float *>(o.C) + (int64_t)split * M * o.ld;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                float v[4] = {acc[mt][nt][0], acc[mt][nt][1], acc[mt][nt][2], acc[mt][nt][3]};
-                if constexpr (KIND != kOutPart) finish4(o, n_lane + 16 * nt, N, v);
-                store4<KIND>(to, m, n_lane + 16 * nt, N, v);
-            }
+            for (int nt = 0; nt < NT; ++nt) store4<KIND>(to, m, n_lane + 16 * nt, N, v[nt]);
         }
+        __builtin_amdgcn_sched_barrier(0);                  // (one row of tiles at a time: registers)
     }
+}
+
+// The tile that workgroup b of n works on: the eight XCDs take consecutive
+// ranges of the tiles, so that neighbours share an L2, and within those
+// 8 tiles along m go with every n before the next 8.
+__device__ __forceinline__ void tile_of(int32_t b, int32_t m_tiles, int32_t n_tiles, int32_t &mt, int32_t &nt)
+{
+    const int32_t n = m_tiles * n_tiles, q = n / 8, r = n % 8, x = b % 8;
+    const int32_t t = x * q + (x < r ? x : r) + b / 8, band = t / (8 * n_tiles), first = band * 8;
+    const int32_t rows = m_tiles - first < 8 ? m_tiles - first : 8, in = t - band * 8 * n_tiles;
+    mt = first + in % rows;
+    nt = in / rows;
 }
 
 // WM x WN waves, each MT x 8 tiles of 16 x 16 (128 columns: a whole block of
 // the next layer's operand).  Two LDS stages: the next block of K is on its
 // way while one is multiplied.
 template <int WM, int WN, int MT, int FA, bool EXACT, OutKind KIND>
-__global__ __launch_bounds__(64 * WM * WN) void k_product(Operand A, Operand B, int32_t nkb, int32_t per_split, Out o)
+__global__ __launch_bounds__(64 * WM * WN, 2) void k_product(Operand A, Operand B, int32_t nkb, int32_t per_split, Out o)
 {
     constexpr int NT = 8, BM = WM * MT * 16, BN = WN * 128, kWaves = WM * WN;
     constexpr int kLoadsA = BM / 8 / kWaves, kLoadsB = BN / 8 / kWaves;
@@ -238,9 +337,9 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(Operand A, Operand B, 
     __shared__ __attribute__((aligned(1024))) uint8_t lds[2][(BM + BN) * 128];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % WM, wn = wave / WM;
-    // neighbours share rows of A
-    const int32_t n_tiles = (B.rows + BN - 1) / BN;
-    const int32_t m0 = (int32_t)(blockIdx.x / n_tiles) * BM, n0 = (int32_t)(blockIdx.x % n_tiles) * BN;
+    int32_t m_tile, n_tile;
+    tile_of(blockIdx.x, (A.rows + BM - 1) / BM, (B.rows + BN - 1) / BN, m_tile, n_tile);
+    const int32_t m0 = m_tile * BM, n0 = n_tile * BN;
     const int32_t k_begin = (int32_t)blockIdx.y * per_split, k_end = k_begin + per_split < nkb ? k_begin + per_split : nkb;
     const auto a_tile = tile_buffer(A.q + (int64_t)m0 * A.ld), b_tile = tile_buffer(B.q + (int64_t)n0 * B.ld);
     uint32_t a_at[kLoadsA], b_at[kLoadsB];
@@ -256,10 +355,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(Operand A, Operand B, 
         for (int i = 0; i < kLoadsB; ++i) to_lds(b_tile, b_at[i], k, stage + BM * 128 + (wave * kLoadsB + i) * 1024);
     };
     f32x4_t acc[MT][NT];
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+    start_tiles<MT, KIND>(acc, n0 + wn * 128, B.rows, o, lane);
     uint32_t sa[MT], sb[NT];
     const int32_t row_a = m0 + wm * MT * 16 + (lane & 15), row_b = n0 + wn * 128 + (lane & 15);
     auto scales = [&](int32_t kb) {
@@ -317,18 +413,6 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(Operand A, Operand B, 
     finish_tiles<MT, KIND>(acc, m0 + wm * MT * 16, n0 + wn * 128, A.rows, B.rows, (int32_t)blockIdx.y, o, lane);
 }
 
-// The tile that workgroup b of n works on: the eight XCDs take consecutive
-// ranges of the tiles, so that neighbours share an L2, and within those
-// 8 tiles along m go with every n before the next 8.
-__device__ __forceinline__ void tile_of(int32_t b, int32_t m_tiles, int32_t n_tiles, int32_t &mt, int32_t &nt)
-{
-    const int32_t n = m_tiles * n_tiles, q = n / 8, r = n % 8, x = b % 8;
-    const int32_t t = x * q + (x < r ? x : r) + b / 8, band = t / (8 * n_tiles), first = band * 8;
-    const int32_t rows = m_tiles - first < 8 ? m_tiles - first : 8, in = t - band * 8 * n_tiles;
-    mt = first + in % rows;
-    nt = in / rows;
-}
-
 // 256 x 256 tiles by eight waves in two groups, a wave of each on every SIMD.
 // A step of K has two phases with a barrier after each: while one group reads
 // its fragments from LDS the other one multiplies, so the matrix cores and LDS
@@ -351,11 +435,9 @@ __global__ __launch_bounds__(512) void k_product_deep(Operand A, Operand B, int3
     const int32_t k_begin = (int32_t)blockIdx.y * per_split, k_end = k_begin + per_split < nkb ? k_begin + per_split : nkb;
     const auto a_tile = tile_buffer(A.q + (int64_t)m0 * A.ld), b_tile = tile_buffer(B.q + (int64_t)n0 * B.ld);
     // a wave brings 32 rows of A, those of its own group; a wave of the first group 64 of B
-    uint32_t a_at[4], b_at[8];
+    uint32_t a_at[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) a_at[i] = lds_source(wave * 32 + i * 8, lane, A.rows - m0, A.ld);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) b_at[i] = lds_source((wave & 3) * 64 + i * 8, lane, B.rows - n0, B.ld);
     // (past the end the last block is brought again, to a stage that is not read)
     auto k_of = [&](int32_t kb) { return (uint32_t)(kb < k_end ? kb : k_end - 1) * 128; };
     // thread t brings the bytes of row t of A's 256, then of B's
@@ -372,10 +454,7 @@ __global__ __launch_bounds__(512) void k_product_deep(Operand A, Operand B, int3
         for (int i = 0; i < 4; ++i) to[512 * i] = (uint8_t)(w >> (8 * i));
     };
     f32x4_t acc[MT][NT];
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+    start_tiles<MT, KIND>(acc, n0 + wn * 128, B.rows, o, lane);
     auto barrier = [] {
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
@@ -383,9 +462,11 @@ __global__ __launch_bounds__(512) void k_product_deep(Operand A, Operand B, int3
     };
     auto fetch_a = [&](int32_t kb, int i) { to_lds(a_tile, a_at[i], k_of(kb), lds + (kb & 1) * kStage + (wave * 4 + i) * 1024); };
     auto fetch_b = [&](int32_t kb) {
+        int l = lane;                                       // (offsets made anew each time: no registers to keep them)
+        asm volatile("" : "+v"(l));
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            to_lds(b_tile, b_at[i], k_of(kb), lds + (kb & 1) * kStage + BM * 128 + ((wave & 3) * 8 + i) * 1024);
+            to_lds(b_tile, lds_source((wave & 3) * 64 + i * 8, l, B.rows - n0, B.ld), k_of(kb), lds + (kb & 1) * kStage + BM * 128 + ((wave & 3) * 8 + i) * 1024);
     };
     auto lds_done = [] { __builtin_amdgcn_s_waitcnt(0xc07f); };           // lgkmcnt(0)
     if (!second) fetch_b(k_begin);
@@ -491,9 +572,9 @@ struct Plan {
     int32_t splits, per_split;
 };
 
-constexpr int kBM = 128, kBN = 256;
+constexpr int kBM = 128, kBN = 128;
 
-bool deep(int64_t M, int64_t N, bool exact) { return !exact && M >= 256 && N >= 256; }
+bool deep(int64_t M, int64_t N, int64_t K, bool exact) { return !exact && M >= 256 && N >= 256 && K >= 1536; }
 
 // K is split where the tiles leave compute units idle, at least four blocks to a split.
 Plan plan_product(int64_t M, int64_t N, int64_t nkb)
@@ -516,7 +597,7 @@ void launch_tiles(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const Plan &p, con
 {
     const int32_t nkb = (int32_t)fp8_blocks(A.cols);
     if constexpr (!EXACT) {
-        if (deep(A.rows, B.rows, EXACT)) {
+        if (deep(A.rows, B.rows, A.cols, EXACT)) {
             const dim3 grid((unsigned)((B.rows + 255) / 256 * ((A.rows + 255) / 256)), (unsigned)p.splits);
             if (A.format == HWSEL_FP8_E4M3)
                 hipLaunchKernelGGL((k_product_deep<0, KIND>), grid, dim3(512), 0, s, operand(A), operand(B), nkb, p.per_split, o);
@@ -527,10 +608,10 @@ void launch_tiles(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const Plan &p, con
     }
     const dim3 grid((unsigned)((B.rows + kBN - 1) / kBN * ((A.rows + kBM - 1) / kBM)), (unsigned)p.splits);
     if (A.format == HWSEL_FP8_E4M3)
-        hipLaunchKernelGGL((k_product<2, 2, 4, 0, EXACT, KIND>), grid, dim3(256), 0, s, operand(A), operand(B), nkb, p.per_split,
+        hipLaunchKernelGGL((k_product<4, 1, 2, 0, EXACT, KIND>), grid, dim3(256), 0, s, operand(A), operand(B), nkb, p.per_split,
                            o);
     else
-        hipLaunchKernelGGL((k_product<2, 2, 4, 1, EXACT, KIND>), grid, dim3(256), 0, s, operand(A), operand(B), nkb, p.per_split,
+        hipLaunchKernelGGL((k_product<4, 1, 2, 1, EXACT, KIND>), grid, dim3(256), 0, s, operand(A), operand(B), nkb, p.per_split,
                            o);
 }
 
@@ -566,14 +647,15 @@ hipError_t launch_fp8_matmul(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const f
                              int64_t ldc, void *ws, hipStream_t s)
 {
     const size_t el = bf16 ? 2 : 4;
-    const Out o{C, ldc, nullptr, 0, bias, gelu, ((uintptr_t)C | (uintptr_t)(ldc * el)) % (4 * el) == 0};
+    const Out o{C, ldc, nullptr, 0, bias, gelu, ((uintptr_t)C | (uintptr_t)(ldc * el)) % (4 * el) == 0,
+                ((uintptr_t)C | (uintptr_t)(ldc * el)) % (8 * el) == 0};
     return bf16 ? run_product<kOutBf16>(A, B, o, ws, s) : run_product<kOutF32>(A, B, o, ws, s);
 }
 
 hipError_t launch_fp8_layer(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const float *bias, bool gelu, const hwsel_fp8_t &C,
                             void *ws, hipStream_t s)
 {
-    return run_product<kOutFp8>(A, B, Out{C.q, C.ld, C.scale, C.ld_scale, bias, gelu, true}, ws, s);
+    return run_product<kOutFp8>(A, B, Out{C.q, C.ld, C.scale, C.ld_scale, bias, gelu, true, true}, ws, s);
 }
 
 }  // namespace hwsel

@@ -111,7 +111,13 @@ def test_products_are_exact_where_sums_are():
         x = torch.randint(-3, 4, (M, K), generator=g, device="cuda").float()
         w = torch.randint(-2, 3, (N, K), generator=g, device="cuda").float()
         a, b = hwsel.hwsel_fp8_quantise(x), hwsel.hwsel_fp8_quantise(w, block_rows=128)
-        assert torch.equal(hwsel.hwsel_fp8_matmul(a, b, torch.float32).double(), x.double() @ w.double().t())
+        y = x.double() @ w.double().t()
+        assert torch.equal(hwsel.hwsel_fp8_matmul(a, b, torch.float32).double(), y)
+        assert torch.equal(hwsel.hwsel_fp8_matmul(a, b).double(), y.bfloat16().double())
+        m = hwsel.hwsel_fp8_layer(a, b)
+        want, e = grid_values(y, E4M3)
+        assert same_values(code_values(m), want)
+        assert torch.equal(m["scale"][:, :-(-N // 128)].to(torch.int32) - 127, e.to(torch.int32))
 
 
 def test_rows_keep_to_themselves():
