@@ -581,7 +581,7 @@ int hwsel_fp8_transpose(const hwsel_fp8_t *in, const hwsel_fp8_t *out, void *str
  * transposed (blocks along the rows of the batch) the weights' gradient.
  *   bias        fp32 [N] or NULL.
  *   activation  HWSEL_ACT_NONE or HWSEL_ACT_GELU (GELU(a) = a Phi(a), within
- *               1e-6 absolute).
+ *               1e-6 absolute for results in fp32, else 1e-5).
  *   C           HWSEL_DTYPE_FP32 or HWSEL_DTYPE_BF16 (rounded once, nearest
  *               even), row-major [M][ldc], ldc >= N in elements, aligned to
  *               its elements.

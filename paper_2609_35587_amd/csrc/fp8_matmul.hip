@@ -55,7 +55,7 @@ __device__ __forceinline__ float gelu_fine(float a)
 {
     constexpr float c5 = -0.00047442156937904656f, c4 = 0.007105245254933834f, c3 = -0.0519152507185936f,
                     c2 = -0.45985135436058044f, c1 = -1.1508772373199463f, c0 = -1.000020146369934f;
-    const float x = fminf(fabsf(a), 64.0f);
+    const float x = __builtin_amdgcn_fmed3f(fabsf(a), 0.0f, 64.0f);
     float p = fmaf(c5, x, c4);
     p = fmaf(p, x, c3);
     p = fmaf(p, x, c2);
@@ -64,7 +64,26 @@ __device__ __forceinline__ float gelu_fine(float a)
     return fmaf(-x, __builtin_amdgcn_exp2f(p), __builtin_elementwise_maximum(a, 0.0f));
 }
 
+// The same with degree 4 and |a| up to 5.5, where 2^P is 2e-8: |error| <= 8.4e-6,
+// for results in bf16 and 8 bits, where it is no more than the products' own
+// (see above) and an instruction in eleven is worth having.
+__device__ __forceinline__ float gelu_short(float a)
+{
+    constexpr float c4 = 0.00369689567014575f, c3 = -0.04334138706326485f, c2 = -0.4690028131008148f,
+                    c1 = -1.146939754486084f, c0 = -1.000515103340149f;
+    const float x = __builtin_amdgcn_fmed3f(fabsf(a), 0.0f, 5.5f);
+    float p = fmaf(c4, x, c3);
+    p = fmaf(p, x, c2);
+    p = fmaf(p, x, c1);
+    p = fmaf(p, x, c0);
+    return fmaf(-x, __builtin_amdgcn_exp2f(p), __builtin_elementwise_maximum(a, 0.0f));
+}
+
+template <OutKind KIND>
+__device__ __forceinline__ float gelu(float a) { return KIND == kOutF32 ? gelu_fine(a) : gelu_short(a); }
+
 // v[i] = act(v[i] + bias[n + i]); columns from N on are set to 0.
+template <OutKind KIND>
 __device__ __forceinline__ void finish4(const Out &o, int32_t n, int32_t N, float (&v)[4])
 {
     if (o.bias) {
@@ -74,7 +93,7 @@ __device__ __forceinline__ void finish4(const Out &o, int32_t n, int32_t N, floa
     }
     if (o.gelu) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = gelu_fine(v[i]);
+        for (int i = 0; i < 4; ++i) v[i] = gelu<KIND>(v[i]);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = n + i < N ? v[i] : 0.0f;
@@ -129,6 +148,13 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_buffer(const uint8_t *bas
 __device__ __forceinline__ void to_lds(__amdgpu_buffer_rsrc_t tile, uint32_t offset, uint32_t k, uint8_t *to)
 {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(tile, (__attribute__((address_space(3))) void *)to, 16, offset, k, 0, 0);
+}
+
+// One word a lane to LDS.
+__device__ __forceinline__ void word_to_lds(const uint8_t *from, uint8_t *to)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
+                                     (__attribute__((address_space(3))) void *)to, 4, 0, 0);
 }
 
 // A fragment: 32 bytes of row lane % 16, chunks lane / 16 and lane / 16 + 4 (any
@@ -187,14 +213,13 @@ __device__ __forceinline__ void transpose_groups(uint32_t &a, uint32_t &b, uint3
     d = hi[1];
 }
 
-// Maximum over the four groups of 16 lanes, in every lane.
-__device__ __forceinline__ float groups_max(float v)
+// Maximum over the four groups of 16 lanes, in every lane, of bits of floats >= 0.
+__device__ __forceinline__ uint32_t groups_max(uint32_t v)
 {
-    const uint32_t u = __float_as_uint(v);
-    const auto h = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    const uint32_t m = __float_as_uint(fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1])));
+    const auto h = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    const uint32_t m = h[0] > h[1] ? h[0] : h[1];
     const auto q = __builtin_amdgcn_permlane16_swap(m, m, false, false);
-    return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
+    return q[0] > q[1] ? q[0] : q[1];
 }
 
 // The sums' first values: the bias, for a product that ends in this launch.
@@ -240,7 +265,7 @@ __device__ __forceinline__ void finish_tiles(const f32x4_t (&acc)[MT][8], int32_
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[nt][i] = gelu_fine(v[nt][i]);
+                for (int i = 0; i < 4; ++i) v[nt][i] = gelu<KIND>(v[nt][i]);
         }
         if constexpr (KIND == kOutFp8) {
             if (!whole) {
@@ -255,9 +280,9 @@ __device__ __forceinline__ void finish_tiles(const f32x4_t (&acc)[MT][8], int32_
                 most = fmaxf(fmaxf(fabsf(v[nt][0]), fabsf(v[nt][1])), most);
                 most = fmaxf(fmaxf(fabsf(v[nt][2]), fabsf(v[nt][3])), most);
             }
-            most = groups_max(most);
+            const uint32_t top = groups_max(__float_as_uint(most));
             uint32_t w[NT], byte;
-            if (__any(most == __builtin_inff())) {          // infinities do not count either
+            if (__any(top == 0x7f800000u)) {                // infinities do not count either
                 uint32_t bits = 0;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
@@ -266,11 +291,11 @@ __device__ __forceinline__ void finish_tiles(const f32x4_t (&acc)[MT][8], int32_
                         const uint32_t f = finite_bits(v[nt][i]);
                         bits = f > bits ? f : bits;
                     }
-                byte = scale_byte(__float_as_uint(groups_max(__uint_as_float(bits))), HWSEL_FP8_E4M3);
+                byte = scale_byte(groups_max(bits), HWSEL_FP8_E4M3);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) w[nt] = codes4_checked(v[nt], inverse_scale(byte), HWSEL_FP8_E4M3, true);
             } else {
-                byte = scale_byte(__float_as_uint(most), HWSEL_FP8_E4M3);
+                byte = scale_byte(top, HWSEL_FP8_E4M3);
                 const float s = __uint_as_float(byte << 23);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) w[nt] = scaled_codes4(v[nt], s);
@@ -526,6 +551,127 @@ __global__ __launch_bounds__(512) void k_product_deep(Operand A, Operand B, int3
     finish_tiles<MT, KIND>(acc, m0 + wm * 64, n0 + wn * 128, A.rows, B.rows, (int32_t)blockIdx.y, o, lane);
 }
 
+// Short sums (K up to 128 NKB), many rows.  A wave keeps its MT x 16 rows of A in
+// registers, all of K, and goes through the columns 128 at a time; B comes by
+// in LDS, a ring of four stages of 128 columns by one block of K that runs on
+// from one 128 columns to the next, three stages ahead; their exponent bytes and bias come by the same way.
+// Blocks of K past the
+// end are zeros of A against the last block of B, both with scale 1.
+template <int NKB, int MT, int FA, OutKind KIND>
+__global__ __launch_bounds__(256, 2) void k_product_rows(Operand A, Operand B, int32_t nkb, int32_t tiles_each, Out o)
+{
+    constexpr int NT = 8, BM = 64 * MT, kStage = 128 * 128, kAhead = 3;
+    static_assert(MT * NKB <= 8, "registers");
+    constexpr int kWords = (NKB + 3) / 4, kSide = 512 * (kWords + 1);      // exponent words and bias of 128 columns
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * kStage + 4 * kSide];
+    uint8_t *side = lds + 4 * kStage;                       // of tile t at t % 4
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
+    const int32_t N = B.rows, n_tiles = (N + 127) / 128;
+    const int32_t m0 = (int32_t)blockIdx.x * BM + wave * MT * 16;
+    const int32_t t_begin = (int32_t)blockIdx.y * tiles_each, t_end = t_begin + tiles_each < n_tiles ? t_begin + tiles_each : n_tiles;
+    const int32_t stages = (t_end - t_begin) * NKB;
+    uint32_t b_at[4];                                       // (made anew for a last tile of fewer columns)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) b_at[i] = lds_source(wave * 32 + i * 8, lane, N - t_begin * 128, B.ld);
+    auto fetch = [&](int32_t at) {                          // (past the end the last stage again: it is not read)
+        const int32_t s = at < stages ? at : stages - 1, n0 = (t_begin + s / NKB) * 128, kb = s % NKB;
+        const auto tile = tile_buffer(B.q + (int64_t)n0 * B.ld);
+        if (kb == 0) {                                      // 64 words a load: words 64 i .. of the tile's
+            const int32_t t = at / NKB;
+            if (n0 + 128 > N) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) b_at[i] = lds_source(wave * 32 + i * 8, lane, N - n0, B.ld);
+            }
+#pragma unroll
+            for (int i = wave; i < 2 * (kWords + 1); i += 4) {
+                const int j = i >> 1;
+                int32_t n = n0 + (i & 1) * 64 + lane;
+                n = n < N ? n : N - 1;
+                uint8_t *to = side + (t & 3) * kSide + i * 256;
+                if (j < kWords)
+                    word_to_lds(B.scale + (int64_t)(n >> B.shift) * B.ld_scale + (4 * j < nkb ? 4 * j : 0), to);
+                else if (o.bias)
+                    word_to_lds(reinterpret_cast<const uint8_t *>(o.bias + n), to);
+            }
+        }
+        uint8_t *to = lds + (at & 3) * kStage + wave * 4096;
+        const uint32_t k = (uint32_t)(kb < nkb ? kb : nkb - 1) * 128;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to_lds(tile, b_at[i], k, to + i * 1024);
+    };
+    auto barrier = [] {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) fetch(s);
+    auto clean = [&](uint32_t w, int j) {                   // bytes past the blocks may be anything
+        if (nkb == NKB) return w;
+        const int32_t have = nkb - 4 * j;
+        const uint32_t mask = have >= 4 ? 0xffffffffu : have > 0 ? (1u << (8 * have)) - 1u : 0u;
+        return (w & mask) | (0x7f7f7f7fu & ~mask);
+    };
+    i32x8_t a[MT][NKB];
+    uint32_t sa[MT][(NKB + 3) / 4];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        const int32_t row = m0 + 16 * mt + (lane & 15), r = row < A.rows ? row : A.rows - 1;
+        const uint8_t *at = A.q + (int64_t)r * A.ld + g * 16;
+#pragma unroll
+        for (int kb = 0; kb < NKB; ++kb) {
+            const int32_t k = (kb < nkb ? kb : nkb - 1) * 128;
+            const i32x4_t lo = *reinterpret_cast<const i32x4_t *>(at + k), hi = *reinterpret_cast<const i32x4_t *>(at + k + 64);
+            a[mt][kb] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            if (kb >= nkb) a[mt][kb] = (i32x8_t){0, 0, 0, 0, 0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int j = 0; j < (NKB + 3) / 4; ++j) sa[mt][j] = clean(scale_word(A, row, 4 * j < nkb ? 4 * j : 0), j);
+    }
+    for (int32_t t = t_begin; t < t_end; ++t) {
+        const int32_t n0 = t * 128;
+        f32x4_t acc[MT][NT];
+        uint32_t sb[NT][kWords];
+#define BLOCK(kb)                                                                                                             \
+    if constexpr ((kb) < NKB) {                                                                                               \
+        const int32_t s = (t - t_begin) * NKB + (kb);                                                                         \
+        __builtin_amdgcn_s_waitcnt(0x0f78);                 /* vmcnt(8): all but the next two stages' */                      \
+        barrier();                                                                                                            \
+        fetch(s + kAhead);                                                                                                    \
+        __builtin_amdgcn_sched_barrier(0);                                                                                    \
+        if constexpr ((kb) == 0) {                                                                                            \
+            const uint8_t *own = side + ((t - t_begin) & 3) * kSide;                                                          \
+            _Pragma("unroll") for (int nt = 0; nt < NT; ++nt)                                                                 \
+            {                                                                                                                 \
+                f32x4_t first = {0.0f, 0.0f, 0.0f, 0.0f};                                                                     \
+                if (o.bias) first = *reinterpret_cast<const f32x4_t *>(own + 512 * kWords + nt * 64 + g * 16);                \
+                _Pragma("unroll") for (int mt = 0; mt < MT; ++mt) acc[mt][nt] = first;                                        \
+                _Pragma("unroll") for (int j = 0; j < kWords; ++j)                                                            \
+                    sb[nt][j] = clean(*reinterpret_cast<const uint32_t *>(own + 512 * j + nt * 64 + (lane & 15) * 4), j);     \
+            }                                                                                                                 \
+        }                                                                                                                     \
+        const uint8_t *stage = lds + (s & 3) * kStage;                                                                        \
+        _Pragma("unroll") for (int nt = 0; nt < NT; ++nt)                                                                     \
+        {                                                                                                                     \
+            const i32x8_t b = fragment(stage + nt * 2048, lane);                                                              \
+            _Pragma("unroll") for (int mt = 0; mt < MT; ++mt) acc[mt][nt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4( \
+                b, a[mt][kb], acc[mt][nt], 0, FA, (kb) & 3, (int)sb[nt][(kb) / 4], (kb) & 3, (int)sa[mt][(kb) / 4]);          \
+        }                                                                                                                     \
+    }
+        BLOCK(0) BLOCK(1) BLOCK(2) BLOCK(3) BLOCK(4) BLOCK(5) BLOCK(6) BLOCK(7)
+#undef BLOCK
+        // the sums are taken here: left to itself the compiler moves every product
+        // behind the last barrier, with all fragments kept in registers till then
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) asm volatile("" : "+v"(acc[mt][nt]));
+        __builtin_amdgcn_sched_barrier(0);
+        finish_tiles<MT, KIND>(acc, m0, n0, A.rows, N, 0, o, lane);
+    }
+    __builtin_amdgcn_s_waitcnt(0x0f70);                     // (no load to LDS outlives the workgroup)
+}
+
 // Sum of the splits' partial sums, in the order of K, and what becomes of it:
 // 32 lanes take 128 columns of a row.
 template <OutKind KIND>
@@ -544,7 +690,7 @@ __global__ __launch_bounds__(256) void k_product_join(const float *__restrict__ 
                 v[0] += p.x; v[1] += p.y; v[2] += p.z; v[3] += p.w;
             }
         }
-        finish4(o, n, N, v);
+        finish4<KIND>(o, n, N, v);
         if constexpr (KIND == kOutFp8) {
             uint32_t most = 0, all = 0;
 #pragma unroll
@@ -596,6 +742,25 @@ template <bool EXACT, OutKind KIND>
 void launch_tiles(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const Plan &p, const Out &o, hipStream_t s)
 {
     const int32_t nkb = (int32_t)fp8_blocks(A.cols);
+    if constexpr (!EXACT && KIND != kOutPart) {
+        if (nkb <= 4 && p.splits == 1) {
+            const int32_t n_tiles = (int32_t)((B.rows + 127) / 128), m_tiles = (int32_t)((A.rows + 127) / 128);
+            int32_t each = (int32_t)((int64_t)m_tiles * n_tiles / (4 * compute_units()));
+            each = each < 1 ? 1 : each > n_tiles ? n_tiles : each;
+            const dim3 grid((unsigned)m_tiles, (unsigned)((n_tiles + each - 1) / each));
+            auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, operand(A), operand(B), nkb, each, o); };
+            if (A.format == HWSEL_FP8_E4M3) {
+                if (nkb == 1) go(k_product_rows<1, 2, 0, KIND>);
+                else if (nkb == 2) go(k_product_rows<2, 2, 0, KIND>);
+                else go(k_product_rows<4, 2, 0, KIND>);
+            } else {
+                if (nkb == 1) go(k_product_rows<1, 2, 1, KIND>);
+                else if (nkb == 2) go(k_product_rows<2, 2, 1, KIND>);
+                else go(k_product_rows<4, 2, 1, KIND>);
+            }
+            return;
+        }
+    }
     if constexpr (!EXACT) {
         if (deep(A.rows, B.rows, A.cols, EXACT)) {
             const dim3 grid((unsigned)((B.rows + 255) / 256 * ((A.rows + 255) / 256)), (unsigned)p.splits);

@@ -10,8 +10,9 @@ iteratively reweighted least squares on the absolute GELU error
 x |2^P(x) - Phi(-x)| (Lawson's iteration towards the minimax fit); the
 coefficients are then rounded to fp32 and the error is checked in fp32
 Horner arithmetic over [0, 12] and on a geometric grid up to 1e38.  The 8-bit
-products take degree 5: their results may be fp32, and a code of three bits
-turns an error into a step of 6 % wherever it crosses a rounding boundary.  Run
+products take degree 5 for results in fp32, and degree 4 with the argument
+limited to 5.5 for the others: a code of three bits turns an error into a step
+of 6 % wherever it crosses a rounding boundary.  Run
 `python gelu_fit.py` to print the coefficients (highest degree first) and the
 error bound.
 """
@@ -35,19 +36,20 @@ def fit(deg=3, xmax=5.0, iters=30):
     return c.astype(np.float32)
 
 
-def max_error(c32):
+def max_error(c32, limit=np.inf):
     xs = np.concatenate([np.linspace(0.0, 12.0, 400001), np.geomspace(12.0, 1e38, 10000)]).astype(np.float32)
     with np.errstate(over="ignore", under="ignore", invalid="ignore"):
+        at = np.minimum(xs, np.float32(limit))
         p = np.full_like(xs, c32[0])
         for ci in c32[1:]:
-            p = (p * xs + ci).astype(np.float32)
-        e = np.abs(xs.astype(np.float64) * (np.exp2(p.astype(np.float64)) - phi_neg(xs.astype(np.float64))))
+            p = (p * at + ci).astype(np.float32)
+        e = np.abs(at.astype(np.float64) * np.exp2(p.astype(np.float64)) - xs.astype(np.float64) * phi_neg(xs.astype(np.float64)))
     return float(e.max()), float(xs[e.argmax()])
 
 
 if __name__ == "__main__":
-    for deg in (3, 5):
-        c = fit(deg)
-        err, at = max_error(c)
+    for deg, xmax, iters, limit in ((3, 5.0, 30, np.inf), (5, 5.0, 30, np.inf), (4, 5.5, 100, 5.5)):
+        c = fit(deg, xmax, iters)
+        err, at = max_error(c, limit)
         print("coefficients (x^%d .. x^0):" % (len(c) - 1), ", ".join(repr(float(v)) for v in c))
         print("max |GELU error| = %.3g at |a| = %.3g" % (err, at))
