@@ -3,28 +3,54 @@
 //
 // Weights are whole numbers, so sums do not depend on their order and every
 // comparison is exact.  The kept set is a prefix of the order (score
-// descending, index ascending) without sorting: the key of its last score is
-// found digit by digit from histograms of count and mass (11 + 11 + 10 bits),
-// the ones tied with it are kept from the lowest index on.
+// descending, index ascending), found without sorting: a histogram of count
+// and mass over the exponents t = (score - best) rate, which fall as scores
+// fall, names the bin in which the prefix ends, and the few scores of that bin
+// are ranked.  A draw is the first candidate at which the running sum of kept
+// weights passes a point: sums of 256 candidates are kept, and the 256 that a
+// draw falls into are weighed again.
+//
+// A workgroup takes a problem; a wave has consecutive candidates of it, 256 a
+// step.  Scores are read once from HBM; as many as LDS has room for stay there,
+// first as scores, then as weights, the others are read and weighed again.
+// (Kept in registers instead, 64 a thread, the unrolled passes were 24,000
+// instructions with spills: 121 us for 256 problems of 65,536.)
+// Bound by latency for short segments, for long ones by some 60 instructions a
+// candidate.
 #include "internal.hpp"
 
 namespace hwsel {
 namespace {
-
-constexpr int kThreads = 1024, kWaves = kThreads / 64, kBins = 2048;
 
 struct Settings {
     hwsel_sampling_t how;
     int32_t n_draws;
 };
 
-// floor(2^32 2^t) in stated steps, t = (s - best) * rate (compiled without
-// multiply-add contraction: every product and sum rounds).
-__device__ __forceinline__ uint64_t weight_of(float s, float best, float rate)
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x4u_t __attribute__((ext_vector_type(4), aligned(4)));   // four scores from any segment's start
+
+// What is known of a problem once its scores have been read.
+struct Problem {
+    const float *s;
+    int32_t n;
+    float best, rate;
+};
+
+// t = (s - best) * rate of a score, by stated steps (compiled without
+// multiply-add contraction: every product and sum rounds).  NaN, as of a NaN
+// score, and -inf end at -60, where weights are 0; the best score is at 0 also
+// where it or the rate is infinite.
+__device__ __forceinline__ float exponent_of(const Problem &q, float s)
 {
-    float t = (s - best) * rate;
-    t = s == best ? 0.0f : t;
-    t = t > -60.0f ? t : -60.0f;
+    const float t = fmaxf((s - q.best) * q.rate, -60.0f);
+    return s == q.best ? 0.0f : t;
+}
+
+// floor(2^32 2^t) for t in [-60, 0], 2^32 itself as 2^32 - 1 (no other weight
+// is: above 2^31 they are multiples of 2^8).
+__device__ __forceinline__ uint32_t weight32(float t)
+{
     const float n = rintf(t), f = t - n;
     float p = 1.5403530e-04f;                               // ln(2)^i / i!, i = 6 .. 0
     p = p * f + 1.3333558e-03f;
@@ -33,276 +59,718 @@ __device__ __forceinline__ uint64_t weight_of(float s, float best, float rate)
     p = p * f + 2.4022651e-01f;
     p = p * f + 6.9314718e-01f;
     p = p * f + 1.0f;
-    return ((uint64_t)(uint32_t)(p * 16777216.0f) << 8) >> (int)-n;
+    const float w = __builtin_amdgcn_ldexpf(p, (int)n + 32);
+    return w < 4294967296.0f ? (uint32_t)w : 0xffffffffu;
 }
 
+__device__ __forceinline__ uint64_t whole(uint32_t w) { return (uint64_t)w + (w == 0xffffffffu); }
+
+// Neither NaN nor -inf.  (Not s > -inf: of a ballot over that the compiler makes
+// "not equal to -inf", which a NaN passes.)
+__device__ __forceinline__ bool takes_part(float s) { return s >= -3.402823466e+38f; }
+
 // Key of a score that takes part (larger is better), 0 for NaN and -inf.
-__device__ __forceinline__ uint32_t key_of(float s) { return s > -__builtin_inff() ? order_key(s + 0.0f) : 0u; }
+__device__ __forceinline__ uint32_t key_of(float s) { return takes_part(s) ? order_key(s + 0.0f) : 0u; }
 
 __device__ __forceinline__ float score_of(uint32_t key)
 {
     return __uint_as_float((key & 0x80000000u) ? key ^ 0x80000000u : ~key);
 }
 
-template <class T>
-__device__ __forceinline__ T wave_sum(T v)
+// Sums and maxima over a wave by lane moves: scans within rows of 16, then row
+// broadcasts (through LDS, as shuffles go, each of their six steps waits for a
+// round trip).
+template <int CTRL, int ROW_MASK, bool ZERO_FILL>
+__device__ __forceinline__ uint32_t dpp_plus(uint32_t v)
 {
-#pragma unroll
-    for (int l = 1; l < 64; l <<= 1) v += __shfl_xor(v, l);
-    return v;
+    return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROW_MASK, 0xf, ZERO_FILL);
 }
 
-template <class T>
-__device__ __forceinline__ T wave_scan(T v, int lane)      // inclusive
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v)  // inclusive
 {
-#pragma unroll
-    for (int l = 1; l < 64; l <<= 1) {
-        const T o = __shfl_up(v, l);
-        v += lane >= l ? o : T(0);
-    }
-    return v;
+    v = dpp_plus<0x111, 0xf, true>(v);
+    v = dpp_plus<0x112, 0xf, true>(v);
+    v = dpp_plus<0x114, 0xf, true>(v);
+    v = dpp_plus<0x118, 0xf, true>(v);
+    v = dpp_plus<0x142, 0xa, false>(v);
+    return dpp_plus<0x143, 0xc, false>(v);
 }
 
+__device__ __forceinline__ uint32_t wave_sum(uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)wave_scan(v), 63); }
+
+// Of values below 2^58, as numbers of 26 bits.
+__device__ __forceinline__ uint64_t wave_scan(uint64_t v)
+{
+    const uint32_t a = wave_scan((uint32_t)v & 0x3ffffffu), b = wave_scan((uint32_t)(v >> 26) & 0x3ffffffu),
+                   c = wave_scan((uint32_t)(v >> 52));
+    return ((uint64_t)c << 52) + ((uint64_t)b << 26) + a;
+}
+
+// Of values below 2^52.
+__device__ __forceinline__ uint64_t wave_scan52(uint64_t v)
+{
+    const uint32_t a = wave_scan((uint32_t)v & 0x3ffffffu), b = wave_scan((uint32_t)(v >> 26));
+    return ((uint64_t)b << 26) + a;
+}
+
+__device__ __forceinline__ uint64_t lane_u64(uint64_t v, int l)
+{
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, l);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), l);
+    return ((uint64_t)hi << 32) | lo;
+}
+
+__device__ __forceinline__ uint64_t wave_sum(uint64_t v) { return lane_u64(wave_scan(v), 63); }
+
+template <int CTRL, int ROW_MASK, bool ZERO_FILL>
+__device__ __forceinline__ uint32_t dpp_most(uint32_t v)
+{
+    const uint32_t w = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROW_MASK, 0xf, ZERO_FILL);
+    return w > v ? w : v;
+}
+
+__device__ __forceinline__ uint32_t wave_max(uint32_t v)
+{
+    v = dpp_most<0x111, 0xf, true>(v);
+    v = dpp_most<0x112, 0xf, true>(v);
+    v = dpp_most<0x114, 0xf, true>(v);
+    v = dpp_most<0x118, 0xf, true>(v);
+    v = dpp_most<0x142, 0xa, false>(v);
+    v = dpp_most<0x143, 0xc, false>(v);
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+
+constexpr int kParts = 256;                                 // sums of consecutive candidates, at most
+
+template <int NT, int BINS, int CACHED>
 struct Lds {
-    uint64_t mass[kBins];
-    uint32_t count[kBins];
-    uint64_t wave_mass[kWaves];
-    uint32_t wave_count[kWaves];
-    uint64_t found_mass;                                    // above the found digit
-    uint32_t found_count, found_bin;
+    static constexpr int kList = BINS / 2;                  // scores around a bin that are ranked at once
+    // Running sums after each lane's four candidates of a step, once the bins are done with.
+    static constexpr int kFine = (BINS * 12 + kList * 16) / 8 / 64 * 64;
+    uint32_t cache[CACHED];
+    union {
+        struct {
+            uint64_t mass[BINS + 1], list[kList], sorted[kList];
+            uint32_t count[BINS + 1];
+        };
+        uint64_t fine[kFine];
+    };
+    uint64_t part[kParts + 1];
+    uint64_t wave_mass[NT / 64], cut, found_mass;
+    uint32_t near[kList], wave_count[NT / 64], found_count, found_bin, n_near;
+    float wave_best[NT / 64], wave_least[NT / 64];
 };
 
-// The largest key K at which the count (BY_MASS: the mass) of scores with keys
-// >= K reaches `want`, which the whole does; count and mass strictly above K.
-template <bool BY_MASS>
-__device__ __forceinline__ uint32_t descend(const float *__restrict__ s, int32_t n, float best, float rate, uint64_t want,
-                                            uint32_t &above_count, uint64_t &above_mass, Lds &lds)
+// The end of the kept prefix: a candidate is in it if its score's key is
+// greater, or equal and its index is at most `last`.
+struct Cut {
+    uint32_t key;
+    int32_t last;
+};
+
+__device__ __forceinline__ bool within(const Cut &c, uint32_t key, int32_t i)
 {
-    uint32_t prefix = 0;
-    above_count = 0;
-    above_mass = 0;
-    constexpr int kShift[3] = {21, 10, 0}, kBits[3] = {11, 11, 10};
-    for (int level = 0; level < 3; ++level) {
-        const int shift = kShift[level], bits = kBits[level];
-        for (int b = threadIdx.x; b < kBins; b += kThreads) {
+    return key > c.key || (key == c.key && key != 0 && i <= c.last);
+}
+
+struct Limits {
+    uint32_t k;
+    float top_p;
+    uint64_t least;
+};
+
+// A problem's settings, as the header defines their odd values.
+__device__ __forceinline__ void read_settings(const Settings &set, int32_t p, float best, Problem &q, Limits &lim)
+{
+    const float T = set.how.temperature_of ? set.how.temperature_of[p] : set.how.temperature;
+    const int32_t k = set.how.top_k_of ? set.how.top_k_of[p] : set.how.top_k;
+    const float min_p = set.how.min_p_of ? set.how.min_p_of[p] : set.how.min_p;
+    const bool cold = !(T > 0.0f);
+    lim.k = cold ? 1u : k > 0 ? (uint32_t)k : 0xffffffffu;
+    lim.top_p = set.how.top_p_of ? set.how.top_p_of[p] : set.how.top_p;
+    lim.least = (uint64_t)ceil(min_p > 0.0f ? (min_p < 1.0f ? (double)min_p : 1.0) * 4294967296.0 : 0.0);
+    lim.least = lim.least < 1 ? 1 : lim.least;
+    q.best = best + 0.0f;
+    q.rate = cold ? 1.0f : (float)(1.4426950408889634 / (double)T);
+}
+
+// The mass before which top_p keeps.
+__device__ __forceinline__ uint64_t share_of(const Limits &lim, uint64_t mass)
+{
+    const uint64_t need = (uint64_t)ceil((double)mass * (double)(lim.top_p > 0.0f ? lim.top_p : 0.0f));
+    return need < 1 ? 1 : need;
+}
+
+// How a workgroup of NT threads goes through n candidates: a wave has `steps`
+// steps of 256, from `base` on; `each` steps are one part.
+struct Walk {
+    int32_t n, steps, base, each, per_wave;                 // per_wave: parts of a wave
+};
+
+template <int NT>
+__device__ __forceinline__ Walk walk_of(int32_t n, int wave)
+{
+    constexpr int kWaves = NT / 64, kMost = kParts / kWaves;
+    Walk w;
+    w.n = n;
+    w.steps = (int32_t)(((int64_t)n + 256 * kWaves - 1) / (256 * kWaves));
+    w.base = (int32_t)((int64_t)wave * w.steps * 256 < n ? wave * w.steps * 256 : n);
+    w.each = (w.steps + kMost - 1) / kMost;
+    w.per_wave = w.each > 0 ? (w.steps + w.each - 1) / w.each : 0;
+    return w;
+}
+
+// body(step, the lane's four scores, -inf past the end): four steps' loads at a
+// time while they are whole.
+template <class F>
+__device__ __forceinline__ void each_step(const float *__restrict__ s, const Walk &w, int32_t first, int32_t last, F &&body)
+{
+    const int lane = threadIdx.x & 63;
+    int32_t i = first;
+    for (; i + 4 <= last && (int64_t)w.base + (i + 4) * 256 <= w.n; i += 4) {
+        f32x4u_t t[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) t[j] = *reinterpret_cast<const f32x4u_t *>(s + w.base + (i + j) * 256 + lane * 4);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) body(i + j, t[j]);
+    }
+#pragma unroll 1
+    for (; i < last; ++i) {
+        const int64_t at = (int64_t)w.base + i * 256 + lane * 4;
+        f32x4u_t t;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) t[c] = at + c < w.n ? s[at + c] : -__builtin_inff();
+        body(i, t);
+    }
+}
+
+// Sums to sums before: part[e] becomes the sum of part[0 .. e), part[n] the whole.
+__device__ __forceinline__ void sums_before(uint64_t *part, int n)
+{
+    if (threadIdx.x < 64) {
+        uint64_t run = 0;
+        for (int e0 = 0; e0 < n; e0 += 64) {
+            const int e = e0 + (int)threadIdx.x;
+            const uint64_t v = e < n ? part[e] : 0, scan = wave_scan(v);
+            if (e < n) part[e] = run + scan - v;
+            run += lane_u64(scan, 63);
+        }
+        if (threadIdx.x == 0) part[n] = run;
+    }
+}
+
+// Which bin, from the best one down, takes the running count (by_mass: mass)
+// to `want`; count and mass of the bins before it.
+template <int NT, int BINS, class L>
+__device__ __forceinline__ void find_bin(L &lds, bool by_mass, uint64_t want, uint32_t &bin, uint32_t &before_count,
+                                         uint64_t &before_mass)
+{
+    constexpr int kEach = BINS / NT;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint64_t m[kEach], m_sum = 0;
+    uint32_t c[kEach], c_sum = 0;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        m[j] = lds.mass[threadIdx.x * kEach + j];
+        c[j] = lds.count[threadIdx.x * kEach + j];
+        m_sum += m[j];
+        c_sum += c[j];
+    }
+    const uint64_t m_scan = wave_scan(m_sum);
+    const uint32_t c_scan = wave_scan(c_sum);
+    if (lane == 63) {
+        lds.wave_mass[wave] = m_scan;
+        lds.wave_count[wave] = c_scan;
+    }
+    __syncthreads();
+    uint64_t m_at = m_scan - m_sum;
+    uint32_t c_at = c_scan - c_sum;
+    for (int w = 0; w < wave; ++w) {
+        m_at += lds.wave_mass[w];
+        c_at += lds.wave_count[w];
+    }
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        const uint64_t at = by_mass ? m_at : (uint64_t)c_at, with = at + (by_mass ? m[j] : (uint64_t)c[j]);
+        if (at < want && with >= want) {
+            lds.found_bin = threadIdx.x * kEach + j;
+            lds.found_mass = m_at;
+            lds.found_count = c_at;
+        }
+        m_at += m[j];
+        c_at += c[j];
+    }
+    __syncthreads();
+    bin = lds.found_bin;
+    before_mass = lds.found_mass;
+    before_count = lds.found_count;
+    __syncthreads();
+}
+
+// The cut by digits, where a bin holds too many to rank: the largest key K at
+// which the count (by_mass: mass) of scores with keys >= K reaches `want`, by 11
+// or 10 bits at a time over all scores, then the last of those tied with it
+// that is needed; the mass up to there.
+template <int NT, int BINS, class L>
+__device__ __forceinline__ Cut cut_by_digits(const Problem &q, const Walk &walk, bool by_mass, uint64_t want, uint64_t &mass,
+                                             L &lds)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t prefix = 0, above_count = 0;
+    uint64_t above_mass = 0;
+    constexpr int kBits = BINS == 2048 ? 11 : 10;
+#pragma unroll 1
+    for (int left = 32; left > 0;) {
+        const int bits = left < kBits ? left : kBits, shift = left - bits;
+        for (int b = threadIdx.x; b < BINS; b += NT) {
             lds.mass[b] = 0;
             lds.count[b] = 0;
         }
         __syncthreads();
-        for (int32_t i = threadIdx.x; i < n; i += kThreads) {
-            const float v = s[i];
+#pragma unroll 1
+        for (int32_t i = threadIdx.x; i < q.n; i += NT) {
+            const float v = q.s[i];
             const uint32_t key = key_of(v);
-            const uint32_t high = level == 0 ? 0u : key >> (shift + bits);
-            if (key == 0 || high != prefix) continue;
-            const uint32_t bin = (key >> shift) & ((1u << bits) - 1);
-            atomicAdd(&lds.count[bin], 1u);
-            atomicAdd((unsigned long long *)&lds.mass[bin], (unsigned long long)weight_of(v, best, rate));
-        }
-        __syncthreads();
-        // from the top bin down: thread t has bins kBins - 1 - 2 t and the one below
-        const int hi = kBins - 1 - 2 * (int)threadIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        const uint64_t m2 = lds.mass[hi] + lds.mass[hi - 1];
-        const uint32_t c2 = lds.count[hi] + lds.count[hi - 1];
-        const uint64_t m_scan = wave_scan(m2, lane);
-        const uint32_t c_scan = wave_scan(c2, lane);
-        if (lane == 63) {
-            lds.wave_mass[wave] = m_scan;
-            lds.wave_count[wave] = c_scan;
-        }
-        __syncthreads();
-        uint64_t m_at = above_mass + m_scan - m2;           // above this thread's bins
-        uint32_t c_at = above_count + c_scan - c2;
-        for (int w = 0; w < wave; ++w) {
-            m_at += lds.wave_mass[w];
-            c_at += lds.wave_count[w];
-        }
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const uint64_t m = lds.mass[hi - j];
-            const uint32_t c = lds.count[hi - j];
-            const bool here = BY_MASS ? m_at < want && m_at + m >= want : c_at < want && (uint64_t)c_at + c >= want;
-            if (here) {
-                lds.found_bin = (uint32_t)(hi - j);
-                lds.found_mass = m_at;
-                lds.found_count = c_at;
+            const bool in = key != 0 && (left == 32 || key >> left == prefix);
+            const uint32_t bin = (1u << bits) - 1 - ((key >> shift) & ((1u << bits) - 1));     // best first
+            const uint64_t w = whole(weight32(exponent_of(q, v)));
+            const uint64_t lanes = __ballot(in);
+            if (lanes == 0) continue;
+            // one add for the lanes that agree with the first (equal scores)
+            const int first = __builtin_ctzll(lanes);
+            const bool same = in && key == (uint32_t)__builtin_amdgcn_readlane((int)key, first);
+            const uint64_t agree = __ballot(same);
+            if (same && lane == first) {
+                atomicAdd(&lds.count[bin], (uint32_t)__popcll(agree));
+                atomicAdd((unsigned long long *)&lds.mass[bin], (unsigned long long)(w * __popcll(agree)));
+            } else if (in && !same) {
+                atomicAdd(&lds.count[bin], 1u);
+                atomicAdd((unsigned long long *)&lds.mass[bin], (unsigned long long)w);
             }
-            m_at += m;
-            c_at += c;
         }
         __syncthreads();
-        prefix = (prefix << bits) | lds.found_bin;
-        above_mass = lds.found_mass;
-        above_count = lds.found_count;
+        uint32_t bin, c;
+        uint64_t m;
+        find_bin<NT, BINS>(lds, by_mass, want - (by_mass ? above_mass : (uint64_t)above_count), bin, c, m);
+        above_count += c;
+        above_mass += m;
+        prefix = (prefix << bits) | ((1u << bits) - 1 - bin);
+        left = shift;
+    }
+    const uint64_t w = whole(weight32(exponent_of(q, score_of(prefix))));
+    const uint64_t ties = by_mass ? (want - above_mass + w - 1) / w : want - above_count;
+    mass = above_mass + ties * w;
+    // index of the ties-th candidate with this key: its part, then its place there
+    const int n_parts = NT / 64 * walk.per_wave;
+#pragma unroll 1
+    for (int e = 0; e < walk.per_wave; ++e) {
+        const int32_t b = e * walk.each, end = b + walk.each < walk.steps ? b + walk.each : walk.steps;
+        uint32_t n = 0;
+        each_step(q.s, walk, b, end, [&](int32_t, const f32x4u_t &t) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) n += key_of(t[c]) == prefix;
+        });
+        n = wave_sum(n);
+        if (lane == 0) lds.part[wave * walk.per_wave + e] = n;
     }
     __syncthreads();
-    return prefix;
+    sums_before(lds.part, n_parts);
+    __syncthreads();
+#pragma unroll 1
+    for (int e = 0; e < walk.per_wave; ++e) {
+        const int part = wave * walk.per_wave + e;
+        if (!(lds.part[part] < ties && lds.part[part + 1] >= ties)) continue;
+        uint32_t left = (uint32_t)(ties - lds.part[part]);
+        for (int32_t i0 = walk.base + e * walk.each * 256; i0 < q.n; i0 += 64) {
+            const int32_t i = i0 + lane;
+            uint64_t tied = __ballot(i < q.n && key_of(q.s[i < q.n ? i : i0]) == prefix);
+            const uint32_t here = (uint32_t)__popcll(tied);
+            if (left <= here) {
+                for (; left > 1; --left) tied &= tied - 1;
+                if (lane == 0) lds.found_bin = (uint32_t)(i0 + __builtin_ctzll(tied));
+                break;
+            }
+            left -= here;
+        }
+    }
+    __syncthreads();
+    const int32_t last = (int32_t)lds.found_bin;
+    __syncthreads();
+    return {prefix, last};
 }
 
-__global__ __launch_bounds__(kThreads) void k_sample(const float *__restrict__ scores, int64_t R,
-                                                     const int64_t *__restrict__ seg, Settings set,
-                                                     const float *__restrict__ u, int32_t *__restrict__ idx,
-                                                     float *__restrict__ prob, int32_t *__restrict__ kept_out)
+// Weights of scores around one whose weight is w: a smaller score never weighs
+// more by over 2^-23 of it.
+__device__ __forceinline__ void near_weights(uint32_t w, uint32_t &lo, uint32_t &hi)
 {
-    __shared__ Lds lds;
-    const int32_t p = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t slack = (w >> 19) + 1;
+    lo = w > slack ? w - slack : 1u;
+    hi = w < 0xffffffffu - slack ? w + slack : 0xffffffffu;
+}
+
+// The cut among the m candidates listed in lds.near: those of the bin are
+// ranked.  The count (by_mass: mass) before the bin is given.
+template <int NT, class L>
+__device__ __forceinline__ Cut rank_bin(const Problem &q, float bin_scale, uint32_t bin, uint32_t m, bool by_mass,
+                                        uint32_t before_count, uint64_t before_mass, uint64_t want, uint64_t &mass, L &lds)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t in_bin = 0;
+    for (uint32_t e = threadIdx.x; e < m; e += NT) {
+        const uint32_t i = lds.near[e];
+        const float v = q.s[i];
+        const bool in = (uint32_t)(-exponent_of(q, v) * bin_scale) == bin;
+        lds.list[e] = in ? ((uint64_t)key_of(v) << 32) | (0xffffffffu - i) : 0;
+        in_bin += in;
+    }
+    in_bin = wave_sum(in_bin);
+    if (lane == 0) lds.wave_count[wave] = in_bin;
+    __syncthreads();
+    in_bin = 0;
+#pragma unroll
+    for (int o = 0; o < NT / 64; ++o) in_bin += lds.wave_count[o];
+    for (uint32_t e = threadIdx.x; e < m; e += NT) {
+        const uint64_t v = lds.list[e];
+        uint32_t rank = 0;
+#pragma unroll 8
+        for (uint32_t o = 0; o < m; ++o) rank += lds.list[o] > v;
+        if (v != 0) lds.sorted[rank] = v;
+    }
+    __syncthreads();
+    uint64_t run = before_mass;
+    for (uint32_t e0 = 0; e0 < in_bin; e0 += NT) {          // (block-uniform)
+        const uint32_t e = e0 + threadIdx.x;
+        const uint64_t v = e < in_bin ? lds.sorted[e] : 0;
+        const uint64_t w = e < in_bin ? whole(weight32(exponent_of(q, score_of((uint32_t)(v >> 32))))) : 0;
+        const uint64_t scan = wave_scan52(w);
+        if (lane == 63) lds.wave_mass[wave] = scan;
+        __syncthreads();
+        uint64_t upto = run + scan;
+        for (int o = 0; o < NT / 64; ++o) {
+            if (o < wave) upto += lds.wave_mass[o];
+            run += lds.wave_mass[o];
+        }
+        if (e < in_bin && (by_mass ? upto - w < want && upto >= want : (uint64_t)before_count + e + 1 == want)) {
+            lds.cut = v;
+            lds.found_mass = upto;
+        }
+        __syncthreads();
+    }
+    const uint64_t cut = lds.cut;
+    mass = lds.found_mass;
+    __syncthreads();
+    return {(uint32_t)(cut >> 32), (int32_t)(0xffffffffu - (uint32_t)cut)};
+}
+
+// A draw's point in the running sum.
+__device__ __forceinline__ uint64_t point_of(float u, uint64_t total)
+{
+    const float v = floorf(u * 16777216.0f);
+    const uint32_t u24 = v > 0.0f ? (v < 16777215.0f ? (uint32_t)v : 16777215u) : 0u;
+    return (total >> 24) * u24 + (((total & 0xffffffull) * u24) >> 24);
+}
+
+// Kept weights of four consecutive candidates from i on.
+__device__ __forceinline__ void kept_weights(const Problem &q, const Cut &cut, uint64_t least, const f32x4u_t &t, int32_t i,
+                                             uint64_t (&w)[4])
+{
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        const uint64_t v = within(cut, key_of(t[c]), i + c) ? whole(weight32(exponent_of(q, t[c]))) : 0;
+        w[c] = v >= least ? v : 0;
+    }
+}
+
+// Draw j in the part of steps [first, last) of a walk, r into its running sum.
+__device__ __forceinline__ void draw_in(const Problem &q, const Cut &cut, uint64_t least, const Walk &walk, int32_t first,
+                                        int32_t last, uint64_t r, uint64_t total, int32_t *idx, float *prob)
+{
+    const int lane = threadIdx.x & 63;
+    for (int32_t i = first; i < last; ++i) {
+        const int64_t at = (int64_t)walk.base + i * 256 + lane * 4;
+        f32x4u_t t;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) t[c] = at + c < walk.n ? q.s[at + c] : -__builtin_inff();
+        uint64_t w[4];
+        kept_weights(q, cut, least, t, (int32_t)at, w);
+        const uint64_t sum = w[0] + w[1] + w[2] + w[3], scan = wave_scan52(sum), over = __ballot(scan > r);
+        if (over) {
+            if (lane == __builtin_ctzll(over)) {
+                uint64_t run = scan - sum;
+                int c = 0;
+                while (c < 3 && run + w[c] <= r) run += w[c++];
+                *idx = (int32_t)at + c;
+                if (prob) *prob = (float)((double)w[c] / (double)total);
+            }
+            return;
+        }
+        r -= lane_u64(scan, 63);
+    }
+}
+
+template <int NT, int BINS, int CACHED>
+__global__ __launch_bounds__(NT) void k_sample(const float *__restrict__ scores, int64_t R,
+                                               const int64_t *__restrict__ seg, Settings set,
+                                               const float *__restrict__ u, int32_t *__restrict__ idx,
+                                               float *__restrict__ prob, int32_t *__restrict__ kept_out)
+{
+    __shared__ Lds<NT, BINS, CACHED> lds;
+    constexpr int kWaves = NT / 64;
+    constexpr uint32_t kList = Lds<NT, BINS, CACHED>::kList;
+    const int32_t p = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int64_t lo = seg[p], hi = seg[p + 1];
     lo = lo < 0 ? 0 : lo > R ? R : lo;
     hi = hi < lo ? lo : hi > R ? R : hi;
-    const float *s = scores + lo;
-    const int32_t n = (int32_t)(hi - lo);
+    Problem q{scores + lo, (int32_t)(hi - lo), 0.0f, 1.0f};
     u += (int64_t)p * set.n_draws;
     idx += (int64_t)p * set.n_draws;
     if (prob) prob += (int64_t)p * set.n_draws;
+    const Walk walk = walk_of<NT>(q.n, wave);
+    const int32_t cached = walk.steps < CACHED / (NT * 4) ? walk.steps : CACHED / (NT * 4);    // steps in LDS
+    auto slot = [&](int32_t i) { return reinterpret_cast<u32x4_t *>(lds.cache + (i * NT + (int)threadIdx.x) * 4); };
 
-    // the best score, and how many take part
-    uint32_t best_key = 0, alive = 0;
-    for (int32_t i = threadIdx.x; i < n; i += kThreads) {
-        const uint32_t k = key_of(s[i]);
-        best_key = k > best_key ? k : best_key;
-        alive += k != 0;
+    // the best score, the least that takes part, and how many do
+    for (int b = threadIdx.x; b < BINS; b += NT) {
+        lds.mass[b] = 0;
+        lds.count[b] = 0;
     }
+    if (threadIdx.x == 0) lds.n_near = 0;
+    float most = -__builtin_inff(), least_score = __builtin_inff();
+    uint32_t alive = 0;
+    each_step(q.s, walk, 0, walk.steps, [&](int32_t i, const f32x4u_t &t) {
 #pragma unroll
-    for (int l = 1; l < 64; l <<= 1) {
-        const uint32_t o = (uint32_t)__shfl_xor((int)best_key, l);
-        best_key = o > best_key ? o : best_key;
-    }
+        for (int c = 0; c < 4; ++c) {
+            const bool in = takes_part(t[c]);
+            alive += in;
+            most = fmaxf(most, t[c]);
+            least_score = fminf(least_score, in ? t[c] : __builtin_inff());
+        }
+        if (i < cached) *slot(i) = __builtin_bit_cast(u32x4_t, t);
+    });
+    most = score_of(wave_max(order_key(most + 0.0f)));
+    least_score = -score_of(wave_max(order_key(0.0f - least_score)));
     alive = wave_sum(alive);
     if (lane == 0) {
-        lds.count[wave] = best_key;
+        lds.wave_best[wave] = most;
+        lds.wave_least[wave] = least_score;
         lds.wave_count[wave] = alive;
     }
     __syncthreads();
     alive = 0;
+#pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-        best_key = lds.count[w] > best_key ? lds.count[w] : best_key;
+        most = fmaxf(most, lds.wave_best[w]);
+        least_score = fminf(least_score, lds.wave_least[w]);
         alive += lds.wave_count[w];
     }
     __syncthreads();
     if (alive == 0) {
-        for (int32_t j = threadIdx.x; j < set.n_draws; j += kThreads) {
+        for (int32_t j = threadIdx.x; j < set.n_draws; j += NT) {
             idx[j] = -1;
             if (prob) prob[j] = 0.0f;
         }
         if (threadIdx.x == 0 && kept_out) kept_out[p] = 0;
         return;
     }
-    const float best = score_of(best_key);
-    const float T = set.how.temperature_of ? set.how.temperature_of[p] : set.how.temperature;
-    const int32_t k_set = set.how.top_k_of ? set.how.top_k_of[p] : set.how.top_k;
-    const float top_p = set.how.top_p_of ? set.how.top_p_of[p] : set.how.top_p;
-    const float min_p = set.how.min_p_of ? set.how.min_p_of[p] : set.how.min_p;
-    const bool cold = !(T > 0.0f);
-    const float rate = cold ? 1.0f : (float)(1.4426950408889634 / (double)T);
-    const uint32_t k = cold ? 1u : k_set > 0 ? (uint32_t)k_set : 0xffffffffu;
+    Limits lim;
+    read_settings(set, p, most, q, lim);
 
-    // the prefix: keys above `cut`, and the first `ties` of those equal to it
-    uint32_t cut = 0, ties = 0xffffffffu, above_count;
-    uint64_t above_mass, mass;
-    if (k < alive) {
-        cut = descend<false>(s, n, best, rate, k, above_count, above_mass, lds);
-        ties = k - above_count;
-        mass = above_mass + ties * weight_of(score_of(cut), best, rate);
-    } else if (top_p < 1.0f) {
-        mass = 0;
-        for (int32_t i = threadIdx.x; i < n; i += kThreads) mass += key_of(s[i]) ? weight_of(s[i], best, rate) : 0;
-        mass = wave_sum(mass);
-        if (lane == 0) lds.wave_mass[wave] = mass;
-        __syncthreads();
-        mass = 0;
-        for (int w = 0; w < kWaves; ++w) mass += lds.wave_mass[w];
-        __syncthreads();
-    }
-    if (top_p < 1.0f) {
-        const double share = (double)mass * (double)(top_p > 0.0f ? top_p : 0.0f);
-        uint64_t need = (uint64_t)ceil(share);
-        need = need < 1 ? 1 : need;
-        cut = descend<true>(s, n, best, rate, need, above_count, above_mass, lds);
-        const uint64_t w = weight_of(score_of(cut), best, rate), t = (need - above_mass + w - 1) / w;
-        ties = t < 0xffffffffull ? (uint32_t)t : 0xffffffffu;
-    }
-    const double floor_p = min_p > 0.0f ? (min_p < 1.0f ? (double)min_p : 1.0) * 4294967296.0 : 0.0;
-    uint64_t least = (uint64_t)ceil(floor_p);
-    least = least < 1 ? 1 : least;
-
-    // A wave has a range of consecutive candidates; last: the index of the last
-    // tied one that is kept.
-    const int32_t range = (n + kThreads - 1) / kThreads * 64, w_lo = wave * range < n ? wave * range : n,
-                  w_hi = w_lo + range < n ? w_lo + range : n;
-    int32_t last = n;
-    if (ties != 0xffffffffu) {
-        uint32_t c = 0;
-        for (int32_t i = w_lo + lane; i < w_hi; i += 64) c += key_of(s[i]) == cut;
-        c = wave_sum(c);
-        if (lane == 0) lds.wave_count[wave] = c;
-        if (threadIdx.x == 0) lds.found_bin = (uint32_t)n;
-        __syncthreads();
-        uint32_t before = 0;
-        for (int w = 0; w < wave; ++w) before += lds.wave_count[w];
-        if (before < ties && before + c >= ties) {
-            for (int32_t i0 = w_lo; i0 < w_hi; i0 += 64) {
-                const int32_t i = i0 + lane;
-                const uint64_t tied = __ballot(i < w_hi && key_of(s[i < w_hi ? i : i0]) == cut);
-                const uint32_t here = (uint32_t)__popcll(tied);
-                if (before + here >= ties) {
-                    uint64_t left = tied;
-                    for (uint32_t j = 1; j < ties - before; ++j) left &= left - 1;
-                    if (lane == 0) lds.found_bin = (uint32_t)(i0 + __builtin_ctzll(left));
-                    break;
-                }
-                before += here;
+    // weights, and count and mass of each bin if a prefix is wanted
+    const bool by_count = lim.k < alive, by_mass = lim.top_p < 1.0f;
+    const float t_least = -exponent_of(q, least_score), span = t_least < 34.0f ? t_least : 34.0f;
+    const float bin_scale = span > 0.0f ? fminf((float)(BINS - 1) / span, 1e30f) : 1.0f;
+    Cut cut{0, 0x7fffffff};
+    if (by_count || by_mass) {
+        auto weigh = [&](const f32x4u_t &t) -> u32x4_t {
+            u32x4_t w;
+            uint32_t bin[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const float e = exponent_of(q, t[c]);
+                w[c] = weight32(e);
+                bin[c] = w[c] != 0 ? (uint32_t)(-e * bin_scale) : BINS;   // (a place for those of no bin)
             }
+            if (by_mass) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (w[c] != 0) atomicAdd((unsigned long long *)&lds.mass[bin[c]], (unsigned long long)whole(w[c]));
+            }
+            if (by_count) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (w[c] != 0) atomicAdd(&lds.count[bin[c]], 1u);
+            }
+            return w;
+        };
+#pragma unroll 2
+        for (int32_t i = 0; i < cached; ++i) *slot(i) = weigh(__builtin_bit_cast(f32x4u_t, *slot(i)));
+        each_step(q.s, walk, cached, walk.steps, [&](int32_t, const f32x4u_t &t) { weigh(t); });
+        __syncthreads();
+        // (scores that weigh nothing are in no bin: there may be fewer in the bins than k)
+        uint64_t mass = 0, upto;
+        uint32_t in_bins = 0;
+        for (int b = threadIdx.x; b < BINS; b += NT) {
+            in_bins += lds.count[b];
+            mass += lds.mass[b];
+        }
+        in_bins = wave_sum(in_bins);
+        mass = wave_sum(mass);
+        if (lane == 0) {
+            lds.wave_count[wave] = in_bins;
+            lds.wave_mass[wave] = mass;
         }
         __syncthreads();
-        last = (int32_t)lds.found_bin;
+        in_bins = 0;
+        mass = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            in_bins += lds.wave_count[w];
+            mass += lds.wave_mass[w];
+        }
         __syncthreads();
+        bool bins_left = true;
+        // first the k best, then the share of their mass
+#pragma unroll 1
+        for (int turn = by_count && lim.k < in_bins ? 0 : 1; turn < (by_mass ? 2 : 1); ++turn) {
+            const uint64_t want = turn ? share_of(lim, mass) : lim.k;
+            uint32_t bin, c, m = kList + 1;
+            uint64_t before;
+            if (bins_left) {
+                find_bin<NT, BINS>(lds, turn, want, bin, c, before);
+                // the candidates whose weights lie around the bin's, with room for the rounding of either side
+                const float top = exp2f(-(float)bin / bin_scale + 32.0f) * (1.0f + 4e-6f) + 1.0f,
+                            low = exp2f(-(float)(bin + 1) / bin_scale + 32.0f) * (1.0f - 4e-6f) - 1.0f;
+                const uint32_t w_hi = top < 4294967040.0f ? (uint32_t)top : 0xffffffffu,
+                               w_lo = low > 1.0f ? (uint32_t)low : 1u;
+                auto list = [&](int32_t i) {
+                    const uint32_t at = atomicAdd(&lds.n_near, 1u);
+                    if (at < kList) lds.near[at] = (uint32_t)i;
+                };
+                for (int32_t i = 0; i < cached; ++i) {
+                    const u32x4_t w = *slot(i);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (w[e] >= w_lo && w[e] <= w_hi) list(walk.base + i * 256 + lane * 4 + e);
+                }
+                each_step(q.s, walk, cached, walk.steps, [&](int32_t i, const f32x4u_t &t) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (takes_part(t[e]) && (uint32_t)(-exponent_of(q, t[e]) * bin_scale) == bin)
+                            list(walk.base + i * 256 + lane * 4 + e);
+                });
+                __syncthreads();
+                m = lds.n_near;
+                __syncthreads();
+                if (threadIdx.x == 0) lds.n_near = 0;
+            }
+            if (m <= kList) {
+                cut = rank_bin<NT>(q, bin_scale, bin, m, turn, c, before, want, upto, lds);
+            } else {
+                cut = cut_by_digits<NT, BINS>(q, walk, turn, want, upto, lds);
+                bins_left = false;                          // (it used their place)
+            }
+            mass = upto;
+        }
+    } else {
+        for (int32_t i = 0; i < cached; ++i) {
+            const f32x4u_t t = __builtin_bit_cast(f32x4u_t, *slot(i));
+            u32x4_t w;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) w[c] = weight32(exponent_of(q, t[c]));
+            *slot(i) = w;
+        }
     }
-    auto kept_weight = [&](int32_t i) -> uint64_t {
-        const uint32_t key = key_of(s[i]);
-        if (key == 0 || key < cut || (key == cut && i > last)) return 0;
-        const uint64_t w = weight_of(s[i], best, rate);
-        return w >= least ? w : 0;
-    };
-    uint64_t sum = 0;
-    uint32_t kept = 0;
-    for (int32_t i = w_lo + lane; i < w_hi; i += 64) {
-        const uint64_t w = kept_weight(i);
-        sum += w;
-        kept += w != 0;
+
+    // Sums of what is kept, a part's at a time.  A weight tells whether its
+    // candidate is, but for those around the cut's.
+    const uint32_t floor32 = lim.least < 0xffffffffull ? (uint32_t)lim.least : 0xffffffffu;
+    uint32_t near_lo = 0, near_hi = 0, kept = 0;
+    if (cut.key != 0) near_weights(weight32(exponent_of(q, score_of(cut.key))), near_lo, near_hi);
+    // many draws of a problem that is all in LDS: running sums for every lane and step
+    const bool fine = set.n_draws > kWaves && walk.steps <= cached && walk.steps * NT <= Lds<NT, BINS, CACHED>::kFine;
+    __syncthreads();                                        // (the bins are read)
+#pragma unroll 1
+    for (int e = 0; e < walk.per_wave; ++e) {
+        const int32_t first = e * walk.each, last = first + walk.each < walk.steps ? first + walk.each : walk.steps;
+        uint64_t sum = 0;
+        int32_t i = first;
+        for (; i < last && i < cached; ++i) {
+            u32x4_t w = *slot(i);
+            uint64_t four = 0;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                bool in = w[c] >= floor32 && w[c] >= near_lo;
+                if (w[c] >= near_lo && w[c] <= near_hi) {
+                    const int32_t at = walk.base + i * 256 + lane * 4 + c;
+                    in = in && at < q.n && within(cut, key_of(q.s[at < q.n ? at : 0]), at);
+                }
+                w[c] = in ? w[c] : 0;
+                four += whole(w[c]);
+                kept += in;
+            }
+            sum += four;
+            if (fine) {                                     // (a part is a step: at most kParts of them fit)
+                *slot(i) = w;
+                lds.fine[i * NT + threadIdx.x] = wave_scan52(four);
+            }
+        }
+        each_step(q.s, walk, i, last, [&](int32_t at, const f32x4u_t &t) {
+            uint64_t w[4];
+            kept_weights(q, cut, lim.least, t, walk.base + at * 256 + lane * 4, w);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                sum += w[c];
+                kept += w[c] != 0;
+            }
+        });
+        sum = wave_sum(sum);
+        if (lane == 0) lds.part[wave * walk.per_wave + e] = sum;
     }
-    sum = wave_sum(sum);
     kept = wave_sum(kept);
-    if (lane == 0) {
-        lds.wave_mass[wave] = sum;
-        lds.wave_count[wave] = kept;
+    if (lane == 0) lds.wave_count[wave] = kept;
+    __syncthreads();
+    const int n_parts = kWaves * walk.per_wave;
+    sums_before(lds.part, n_parts);
+    if (threadIdx.x == 0 && kept_out) {
+        kept = 0;
+        for (int w = 0; w < kWaves; ++w) kept += lds.wave_count[w];
+        kept_out[p] = (int32_t)kept;
     }
     __syncthreads();
-    uint64_t total = 0;
-    kept = 0;
-    for (int w = 0; w < kWaves; ++w) {
-        total += lds.wave_mass[w];
-        kept += lds.wave_count[w];
-    }
-    if (threadIdx.x == 0 && kept_out) kept_out[p] = (int32_t)kept;
-    for (int32_t j = wave; j < set.n_draws; j += kWaves) {
-        const float v = floorf(u[j] * 16777216.0f);
-        const uint32_t u24 = v > 0.0f ? (v < 16777215.0f ? (uint32_t)v : 16777215u) : 0u;
-        uint64_t r = (total >> 24) * u24 + (((total & 0xffffffull) * u24) >> 24);
-        int w = 0;
-        while (w < kWaves - 1 && r >= lds.wave_mass[w]) r -= lds.wave_mass[w++];
-        const int32_t b = w * range, e = b + range < n ? b + range : n;
-        for (int32_t i0 = b; i0 < e; i0 += 64) {
-            const uint64_t mine = i0 + lane < e ? kept_weight(i0 + lane) : 0, scan = wave_scan(mine, lane);
-            const uint64_t over = __ballot(scan > r);
-            if (over) {
-                const int l = __builtin_ctzll(over);
-                if (lane == l) {
-                    idx[j] = i0 + l;
-                    if (prob) prob[j] = (float)((double)mine / (double)total);
+    const uint64_t total = lds.part[n_parts];
+    if (fine) {                                             // a thread a draw
+        for (int32_t j = threadIdx.x; j < set.n_draws; j += NT) {
+            uint64_t r = point_of(u[j], total);
+            int part = 0, four = 0;
+            for (int step = kParts; step > 0; step >>= 1)   // parts that end at or before the point
+                if (part + step < n_parts && lds.part[part + step] <= r) part += step;
+            r -= lds.part[part];
+            const int of = part / walk.steps, i = part % walk.steps, first = i * NT + of * 64;
+            for (int step = 32; step > 0; step >>= 1)
+                if (lds.fine[first + four + step - 1] <= r) four += step;
+            r -= four ? lds.fine[first + four - 1] : 0;
+            const u32x4_t w = *reinterpret_cast<const u32x4_t *>(lds.cache + (first + four) * 4);
+            int c = 0;
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+                if (c == e && whole(w[e]) <= r) {
+                    r -= whole(w[e]);
+                    ++c;
                 }
-                break;
-            }
-            r -= __shfl(scan, 63);
+            idx[j] = (of * walk.steps + i) * 256 + four * 4 + c;
+            if (prob) prob[j] = (float)((double)whole(w[c]) / (double)total);
         }
+        return;
+    }
+    for (int32_t j = wave; j < set.n_draws; j += kWaves) {
+        uint64_t r = point_of(u[j], total);
+        int part = 0;                                       // parts that end at or before the point
+        for (int e = lane; e < ((n_parts + 63) & ~63); e += 64) part += __popcll(__ballot(e < n_parts && lds.part[e + 1] <= r));
+        r -= lds.part[part];
+        const Walk of = walk_of<NT>(q.n, part / walk.per_wave);
+        const int32_t first = part % walk.per_wave * walk.each;
+        draw_in(q, cut, lim.least, of, first, first + walk.each < walk.steps ? first + walk.each : walk.steps, r, total, idx + j,
+                prob ? prob + j : nullptr);
     }
 }
 
@@ -310,8 +778,9 @@ __global__ __launch_bounds__(kThreads) void k_sample(const float *__restrict__ s
 
 size_t sample_workspace_bytes(int64_t, int32_t, int32_t) { return 0; }
 
-hipError_t launch_sample(const float *scores, int64_t R, const int64_t *seg, int32_t P, const hwsel_sampling_t &how,
-                         const float *u, int32_t n_draws, int32_t *idx, float *prob, int32_t *kept, void *, hipStream_t s)
+template <int NT, int BINS, int CACHED>
+static void launch_problems(const float *scores, int64_t R, const int64_t *seg, int32_t P, const hwsel_sampling_t &how,
+                            const float *u, int32_t n_draws, int32_t *idx, float *prob, int32_t *kept, hipStream_t s)
 {
     each_span(P, [&](int32_t p0, int32_t n) {
         hwsel_sampling_t h = how;
@@ -320,9 +789,17 @@ hipError_t launch_sample(const float *scores, int64_t R, const int64_t *seg, int
         if (h.top_p_of) h.top_p_of += p0;
         if (h.min_p_of) h.min_p_of += p0;
         const int64_t o = (int64_t)p0 * n_draws;
-        hipLaunchKernelGGL(k_sample, dim3(n), dim3(kThreads), 0, s, scores, R, seg + p0, Settings{h, n_draws}, u + o, idx + o,
-                           prob ? prob + o : nullptr, kept ? kept + p0 : nullptr);
+        hipLaunchKernelGGL((k_sample<NT, BINS, CACHED>), dim3(n), dim3(NT), 0, s, scores, R, seg + p0, Settings{h, n_draws}, u + o,
+                           idx + o, prob ? prob + o : nullptr, kept ? kept + p0 : nullptr);
     });
+}
+
+// Segment lengths are not known here; their mean is.
+hipError_t launch_sample(const float *scores, int64_t R, const int64_t *seg, int32_t P, const hwsel_sampling_t &how,
+                         const float *u, int32_t n_draws, int32_t *idx, float *prob, int32_t *kept, void *, hipStream_t s)
+{
+    if (R / P <= 8192) launch_problems<512, 1024, 8192>(scores, R, seg, P, how, u, n_draws, idx, prob, kept, s);
+    else launch_problems<1024, 2048, 24576>(scores, R, seg, P, how, u, n_draws, idx, prob, kept, s);
     return hipGetLastError();
 }
 
