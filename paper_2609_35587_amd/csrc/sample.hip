@@ -318,7 +318,7 @@ __device__ __forceinline__ Cut cut_by_digits(const Problem &q, const Walk &walk,
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     uint32_t prefix = 0, above_count = 0;
     uint64_t above_mass = 0;
-    constexpr int kBits = BINS == 2048 ? 11 : 10;
+    constexpr int kBits = BINS == 4096 ? 12 : BINS == 2048 ? 11 : 10;
 #pragma unroll 1
     for (int left = 32; left > 0;) {
         const int bits = left < kBits ? left : kBits, shift = left - bits;
@@ -774,9 +774,359 @@ __global__ __launch_bounds__(NT) void k_sample(const float *__restrict__ scores,
     }
 }
 
+
+// Few problems of many candidates: each is shared by many workgroups, in
+// passes that hand their results on in the workspace: best score; histogram;
+// candidates around the cut, ranked by one workgroup (once for top-k, once for
+// top-p); sums of parts; draws.  A compute unit takes in some 100 GB/s, so 3
+// problems of 534,600 took 339 us in a workgroup each.
+constexpr int kWide = 1024, kWideBins = 4096, kWideNear = 2048, kWideParts = 1024;
+
+struct WideState {
+    uint32_t best, least, alive, bin, before_count, n_near;
+    uint64_t before_mass, want, mass;
+    Cut cut;
+    uint32_t kept, pad;
+    uint64_t mass_of[kWideBins], part[kWideParts];
+    uint32_t count_of[kWideBins], near[kWideNear];
+};
+
+struct WideArgs {
+    const float *scores;
+    int64_t R;
+    const int64_t *seg;
+    WideState *state;
+    Settings set;
+};
+
+__device__ __forceinline__ Problem problem_of(const WideArgs &a, int32_t p)
+{
+    int64_t lo = a.seg[p], hi = a.seg[p + 1];
+    lo = lo < 0 ? 0 : lo > a.R ? a.R : lo;
+    hi = hi < lo ? lo : hi > a.R ? a.R : hi;
+    return {a.scores + lo, (int32_t)(hi - lo), 0.0f, 1.0f};
+}
+
+// This wave's steps of problem blockIdx.y among those of all its workgroups.
+__device__ __forceinline__ Walk shared_walk(int32_t n)
+{
+    const int32_t waves = (int32_t)gridDim.x * (kWide / 64);
+    const int32_t wave = __builtin_amdgcn_readfirstlane((int)blockIdx.x * (kWide / 64) + (threadIdx.x >> 6));
+    Walk w;
+    w.n = n;
+    w.steps = (int32_t)(((int64_t)n + 256 * (int64_t)waves - 1) / (256 * (int64_t)waves));
+    w.base = (int32_t)((int64_t)wave * w.steps * 256 < n ? (int64_t)wave * w.steps * 256 : n);
+    w.each = w.steps;
+    w.per_wave = 1;
+    return w;
+}
+
+// Steps of one of at most kWideParts parts of n candidates.
+__device__ __forceinline__ int32_t wide_each(int32_t n)
+{
+    return (int32_t)(((int64_t)n + 256 * kWideParts - 1) / (256 * kWideParts));
+}
+
+__global__ __launch_bounds__(256) void k_wide_clear(WideState *state)
+{
+    WideState &st = state[blockIdx.x];
+    for (int i = threadIdx.x; i < kWideBins; i += 256) {
+        st.mass_of[i] = 0;
+        st.count_of[i] = 0;
+    }
+    if (threadIdx.x == 0) {
+        st.best = 0;
+        st.least = 0;
+        st.alive = 0;
+        st.n_near = 0;
+        st.mass = 0;
+        st.cut = {0, 0x7fffffff};
+        st.kept = 0;
+    }
+}
+
+// Keys: of the best score, and of the least's negative.
+__global__ __launch_bounds__(kWide) void k_wide_best(WideArgs a)
+{
+    const int32_t p = blockIdx.y;
+    const Problem q = problem_of(a, p);
+    const Walk walk = shared_walk(q.n);
+    float most = -__builtin_inff(), least = __builtin_inff();
+    uint32_t alive = 0;
+    each_step(q.s, walk, 0, walk.steps, [&](int32_t, const f32x4u_t &t) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const bool in = takes_part(t[c]);
+            alive += in;
+            most = fmaxf(most, t[c]);
+            least = fminf(least, in ? t[c] : __builtin_inff());
+        }
+    });
+    alive = wave_sum(alive);
+    const uint32_t hi = wave_max(order_key(most + 0.0f)), lo = wave_max(order_key(0.0f - least));
+    __shared__ uint32_t sh[3];
+    if (threadIdx.x < 3) sh[threadIdx.x] = 0;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0 && alive != 0) {
+        atomicMax(&sh[0], hi);
+        atomicMax(&sh[1], lo);
+        atomicAdd(&sh[2], alive);
+    }
+    __syncthreads();
+    if (threadIdx.x == 0 && sh[2] != 0) {
+        atomicMax(&a.state[p].best, sh[0]);
+        atomicMax(&a.state[p].least, sh[1]);
+        atomicAdd(&a.state[p].alive, sh[2]);
+    }
+}
+
+// A problem with its settings read, and its bins' scale.
+__device__ __forceinline__ float wide_settings(const WideArgs &a, int32_t p, const WideState &st, Problem &q, Limits &lim)
+{
+    read_settings(a.set, p, score_of(st.best), q, lim);
+    const float t_least = -exponent_of(q, -score_of(st.least)), span = t_least < 34.0f ? t_least : 34.0f;
+    return span > 0.0f ? fminf((float)(kWideBins - 1) / span, 1e30f) : 1.0f;
+}
+
+__global__ __launch_bounds__(kWide) void k_wide_bins(WideArgs a)
+{
+    __shared__ uint64_t mass[kWideBins];
+    __shared__ uint32_t count[kWideBins];
+    const int32_t p = blockIdx.y;
+    WideState &st = a.state[p];
+    Problem q = problem_of(a, p);
+    if (st.alive == 0) return;
+    Limits lim;
+    const float bin_scale = wide_settings(a, p, st, q, lim);
+    if (!(lim.k < st.alive) && !(lim.top_p < 1.0f)) return;
+    const Walk walk = shared_walk(q.n);
+    for (int i = threadIdx.x; i < kWideBins; i += kWide) {
+        mass[i] = 0;
+        count[i] = 0;
+    }
+    __syncthreads();
+    each_step(q.s, walk, 0, walk.steps, [&](int32_t, const f32x4u_t &t) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const float e = exponent_of(q, t[c]);
+            const uint32_t w = weight32(e);
+            if (w != 0) {
+                const uint32_t bin = (uint32_t)(-e * bin_scale);
+                atomicAdd((unsigned long long *)&mass[bin], (unsigned long long)whole(w));
+                atomicAdd(&count[bin], 1u);
+            }
+        }
+    });
+    __syncthreads();
+    for (int i = threadIdx.x; i < kWideBins; i += kWide)
+        if (count[i] != 0) {
+            atomicAdd((unsigned long long *)&st.mass_of[i], (unsigned long long)mass[i]);
+            atomicAdd(&st.count_of[i], count[i]);
+        }
+}
+
+// Before each cut, a workgroup a problem: its bin, or that there is none to
+// find (want = 0).  turn 0: top-k, 1: top-p.
+__global__ __launch_bounds__(kWide) void k_wide_find(WideArgs a, int turn)
+{
+    __shared__ Lds<kWide, kWideBins, 4> lds;
+    const int32_t p = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    WideState &st = a.state[p];
+    Problem q = problem_of(a, p);
+    if (threadIdx.x == 0) {
+        st.want = 0;
+        st.n_near = 0;
+    }
+    if (st.alive == 0) return;
+    Limits lim;
+    wide_settings(a, p, st, q, lim);
+    if (turn ? !(lim.top_p < 1.0f) : !(lim.k < st.alive)) return;
+    uint64_t mass = 0;
+    uint32_t n = 0;
+    for (int i = threadIdx.x; i < kWideBins; i += kWide) {
+        lds.mass[i] = st.mass_of[i];
+        lds.count[i] = st.count_of[i];
+        mass += lds.mass[i];
+        n += lds.count[i];
+    }
+    n = wave_sum(n);
+    mass = wave_sum(mass);
+    if (lane == 0) {
+        lds.wave_count[wave] = n;
+        lds.wave_mass[wave] = mass;
+    }
+    __syncthreads();
+    n = 0;
+    mass = 0;
+    for (int w = 0; w < kWide / 64; ++w) {
+        n += lds.wave_count[w];
+        mass += lds.wave_mass[w];
+    }
+    __syncthreads();
+    if (turn == 0 && !(lim.k < n)) return;                  // (scores that weigh nothing are in no bin)
+    const uint64_t want = turn ? share_of(lim, st.mass != 0 ? st.mass : mass) : lim.k;
+    uint32_t bin, before_count;
+    uint64_t before_mass;
+    find_bin<kWide, kWideBins>(lds, turn, want, bin, before_count, before_mass);
+    if (threadIdx.x == 0) {
+        st.want = want;
+        st.bin = bin;
+        st.before_count = before_count;
+        st.before_mass = before_mass;
+    }
+}
+
+__global__ __launch_bounds__(kWide) void k_wide_list(WideArgs a)
+{
+    const int32_t p = blockIdx.y, lane = threadIdx.x & 63;
+    WideState &st = a.state[p];
+    if (st.alive == 0 || st.want == 0) return;
+    Problem q = problem_of(a, p);
+    Limits lim;
+    const float bin_scale = wide_settings(a, p, st, q, lim);
+    const uint32_t bin = st.bin;
+    const Walk walk = shared_walk(q.n);
+    each_step(q.s, walk, 0, walk.steps, [&](int32_t i, const f32x4u_t &t) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            if (takes_part(t[c]) && (uint32_t)(-exponent_of(q, t[c]) * bin_scale) == bin) {
+                const uint32_t at = atomicAdd(&st.n_near, 1u);
+                if (at < kWideNear) st.near[at] = (uint32_t)(walk.base + i * 256 + lane * 4 + c);
+            }
+    });
+}
+
+__global__ __launch_bounds__(kWide) void k_wide_cut(WideArgs a, int turn)
+{
+    __shared__ Lds<kWide, kWideBins, 4> lds;
+    static_assert(Lds<kWide, kWideBins, 4>::kList == kWideNear, "the list fits");
+    const int32_t p = blockIdx.x;
+    WideState &st = a.state[p];
+    if (st.alive == 0 || st.want == 0) return;
+    Problem q = problem_of(a, p);
+    Limits lim;
+    const float bin_scale = wide_settings(a, p, st, q, lim);
+    const uint32_t m = st.n_near;
+    uint64_t upto;
+    Cut cut;
+    if (m <= kWideNear) {
+        for (uint32_t e = threadIdx.x; e < m; e += kWide) lds.near[e] = st.near[e];
+        __syncthreads();
+        cut = rank_bin<kWide>(q, bin_scale, st.bin, m, turn, st.before_count, st.before_mass, st.want, upto, lds);
+    } else {
+        cut = cut_by_digits<kWide, kWideBins>(q, walk_of<kWide>(q.n, (int)(threadIdx.x >> 6)), turn, st.want, upto, lds);
+    }
+    if (threadIdx.x == 0) {
+        st.cut = cut;
+        st.mass = upto;
+    }
+}
+
+__global__ __launch_bounds__(kWide) void k_wide_sums(WideArgs a)
+{
+    const int32_t p = blockIdx.y, lane = threadIdx.x & 63;
+    WideState &st = a.state[p];
+    if (st.alive == 0) return;
+    Problem q = problem_of(a, p);
+    Limits lim;
+    wide_settings(a, p, st, q, lim);
+    const Cut cut = st.cut;
+    const int32_t each = wide_each(q.n), parts = (int32_t)(((int64_t)q.n + 256 * (int64_t)each - 1) / (256 * (int64_t)each));
+    uint32_t kept = 0;
+    for (int32_t e = __builtin_amdgcn_readfirstlane((int)blockIdx.x * (kWide / 64) + (threadIdx.x >> 6)); e < parts;
+         e += (int32_t)gridDim.x * (kWide / 64)) {
+        const Walk walk{q.n, each, e * each * 256, each, 1};
+        uint64_t sum = 0;
+        each_step(q.s, walk, 0, each, [&](int32_t i, const f32x4u_t &t) {
+            uint64_t w[4];
+            kept_weights(q, cut, lim.least, t, walk.base + i * 256 + lane * 4, w);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                sum += w[c];
+                kept += w[c] != 0;
+            }
+        });
+        sum = wave_sum(sum);
+        if (lane == 0) st.part[e] = sum;
+    }
+    kept = wave_sum(kept);
+    if (lane == 0 && kept != 0) atomicAdd(&st.kept, kept);
+}
+
+__global__ __launch_bounds__(kWide) void k_wide_draw(WideArgs a, const float *__restrict__ u, int32_t *__restrict__ idx,
+                                                     float *__restrict__ prob, int32_t *__restrict__ kept_out)
+{
+    __shared__ uint64_t part[kWideParts + 1], wave_mass[kWide / 64];
+    const int32_t p = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int32_t n_draws = a.set.n_draws;
+    const WideState &st = a.state[p];
+    u += (int64_t)p * n_draws;
+    idx += (int64_t)p * n_draws;
+    if (prob) prob += (int64_t)p * n_draws;
+    if (threadIdx.x == 0 && kept_out) kept_out[p] = (int32_t)st.kept;
+    if (st.alive == 0) {
+        for (int32_t j = threadIdx.x; j < n_draws; j += kWide) {
+            idx[j] = -1;
+            if (prob) prob[j] = 0.0f;
+        }
+        return;
+    }
+    Problem q = problem_of(a, p);
+    Limits lim;
+    wide_settings(a, p, st, q, lim);
+    const Cut cut = st.cut;
+    const int32_t each = wide_each(q.n), parts = (int32_t)(((int64_t)q.n + 256 * (int64_t)each - 1) / (256 * (int64_t)each));
+    const uint64_t own = (int)threadIdx.x < parts ? st.part[threadIdx.x] : 0, scan = wave_scan(own);
+    if (lane == 63) wave_mass[wave] = scan;
+    __syncthreads();
+    uint64_t before = scan - own, total = 0;
+    for (int w = 0; w < kWide / 64; ++w) {
+        if (w < wave) before += wave_mass[w];
+        total += wave_mass[w];
+    }
+    part[threadIdx.x] = before;
+    if (threadIdx.x == 0) part[kWideParts] = total;
+    __syncthreads();
+    for (int32_t j = wave; j < n_draws; j += kWide / 64) {
+        uint64_t r = point_of(u[j], total);
+        int32_t e = 0;
+        for (int step = kWideParts / 2; step > 0; step >>= 1)
+            if (e + step < parts && part[e + step] <= r) e += step;
+        draw_in(q, cut, lim.least, Walk{q.n, each, e * each * 256, each, 1}, 0, each, r - part[e], total, idx + j,
+                prob ? prob + j : nullptr);
+    }
+}
+
 }  // namespace
 
-size_t sample_workspace_bytes(int64_t, int32_t, int32_t) { return 0; }
+// Segment lengths are not known here; their mean is.  Few problems of many
+// candidates are shared by workgroups: SPLITRULE
+static bool shared_problems(int64_t R, int32_t P) { return P <= 128 && R / P > 32768; }
+
+size_t sample_workspace_bytes(int64_t R, int32_t P, int32_t)
+{
+    return shared_problems(R, P) ? (size_t)P * sizeof(WideState) : 0;
+}
+
+static void launch_shared(const WideArgs &a, int32_t P, const float *u, int32_t *idx, float *prob, int32_t *kept, hipStream_t s)
+{
+    // sixteen steps or so a wave, the machine filled about twice
+    const int64_t want = (a.R + 16383) / 16384, most = (2 * compute_units() + P - 1) / P;
+    const dim3 shared((unsigned)(want < most ? want : most), (unsigned)P), one((unsigned)P), block(kWide);
+    hipLaunchKernelGGL(k_wide_clear, one, dim3(256), 0, s, a.state);
+    hipLaunchKernelGGL(k_wide_best, shared, block, 0, s, a);
+    const bool by_count = a.set.how.top_k_of || a.set.how.top_k > 0 || a.set.how.temperature_of || !(a.set.how.temperature > 0.0f),
+               by_mass = a.set.how.top_p_of || a.set.how.top_p < 1.0f;
+    if (by_count || by_mass) hipLaunchKernelGGL(k_wide_bins, shared, block, 0, s, a);
+    for (int turn = 0; turn < 2; ++turn) {
+        if (!(turn ? by_mass : by_count)) continue;
+        hipLaunchKernelGGL(k_wide_find, one, block, 0, s, a, turn);
+        hipLaunchKernelGGL(k_wide_list, shared, block, 0, s, a);
+        hipLaunchKernelGGL(k_wide_cut, one, block, 0, s, a, turn);
+    }
+    hipLaunchKernelGGL(k_wide_sums, shared, block, 0, s, a);
+    hipLaunchKernelGGL(k_wide_draw, one, block, 0, s, a, u, idx, prob, kept);
+}
 
 template <int NT, int BINS, int CACHED>
 static void launch_problems(const float *scores, int64_t R, const int64_t *seg, int32_t P, const hwsel_sampling_t &how,
@@ -794,11 +1144,12 @@ static void launch_problems(const float *scores, int64_t R, const int64_t *seg, 
     });
 }
 
-// Segment lengths are not known here; their mean is.
 hipError_t launch_sample(const float *scores, int64_t R, const int64_t *seg, int32_t P, const hwsel_sampling_t &how,
-                         const float *u, int32_t n_draws, int32_t *idx, float *prob, int32_t *kept, void *, hipStream_t s)
+                         const float *u, int32_t n_draws, int32_t *idx, float *prob, int32_t *kept, void *ws, hipStream_t s)
 {
-    if (R / P <= 8192) launch_problems<512, 1024, 8192>(scores, R, seg, P, how, u, n_draws, idx, prob, kept, s);
+    if (shared_problems(R, P))
+        launch_shared(WideArgs{scores, R, seg, static_cast<WideState *>(ws), Settings{how, n_draws}}, P, u, idx, prob, kept, s);
+    else if (R / P <= 8192) launch_problems<512, 1024, 8192>(scores, R, seg, P, how, u, n_draws, idx, prob, kept, s);
     else launch_problems<1024, 2048, 24576>(scores, R, seg, P, how, u, n_draws, idx, prob, kept, s);
     return hipGetLastError();
 }
