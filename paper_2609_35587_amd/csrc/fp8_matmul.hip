@@ -353,7 +353,7 @@ __device__ __forceinline__ void tile_of(int32_t b, int32_t m_tiles, int32_t n_ti
 // WM x WN waves, each MT x 8 tiles of 16 x 16 (128 columns: a whole block of
 // the next layer's operand).  Two LDS stages: the next block of K is on its
 // way while one is multiplied.
-template <int WM, int WN, int MT, int FA, bool EXACT, OutKind KIND>
+template <int WM, int WN, int MT, int FA, OutKind KIND>
 __global__ __launch_bounds__(64 * WM * WN, 2) void k_product(Operand A, Operand B, int32_t nkb, int32_t per_split, Out o)
 {
     constexpr int NT = 8, BM = WM * MT * 16, BN = WN * 128, kWaves = WM * WN;
@@ -396,6 +396,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_product(Operand A, Operand 
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) sb[nt] >>= 8 * (k_begin & 3);
     for (int32_t kb = k_begin; kb < k_end; ++kb) {
+        __builtin_amdgcn_s_waitcnt(0x0f70);                 // vmcnt(0): the barrier alone does not wait for loads to LDS
         __syncthreads();                                    // this stage has come; the other one is read
         const uint8_t *stage = lds[kb & 1];
         i32x8_t a[MT], b[NT];
@@ -404,28 +405,12 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_product(Operand A, Operand 
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) b[nt] = fragment(stage + BM * 128 + (wn * NT + nt) * 2048, lane);
         if (kb + 1 < k_end) fetch(kb + 1, lds[(kb + 1) & 1]);
-        if constexpr (EXACT) {
-            bf16x8_t wide[MT][4];
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) decode<FA>(a[mt], sa[mt], wide[mt]);
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                bf16x8_t w[4];
-                decode<0>(b[nt], sb[nt], w);
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-#pragma unroll
-                    for (int mt = 0; mt < MT; ++mt)
-                        acc[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[q], wide[mt][q], acc[mt][nt], 0, 0, 0);
-            }
-        } else {
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-                    acc[mt][nt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[nt], a[mt], acc[mt][nt], 0, FA, 0,
-                                                                                  (int)sb[nt], 0, (int)sa[mt]);
-        }
+            for (int mt = 0; mt < MT; ++mt)
+                acc[mt][nt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[nt], a[mt], acc[mt][nt], 0, FA, 0, (int)sb[nt],
+                                                                              0, (int)sa[mt]);
         if ((kb & 3) == 3) {
             if (kb + 1 < k_end) scales(kb + 1);
         } else {
@@ -672,6 +657,219 @@ __global__ __launch_bounds__(256, 2) void k_product_rows(Operand A, Operand B, i
     __builtin_amdgcn_s_waitcnt(0x0f70);                     // (no load to LDS outlives the workgroup)
 }
 
+// Results in fp32: products of decoded codes by the bf16 instruction (see above).
+// Four waves, two by two, each 16 MT x 16 NT: a fragment decoded serves MT or NT
+// products.  Two stages in LDS, the next block of K on its way meanwhile.
+template <int MT, int NT, int FA, OutKind KIND>
+__global__ __launch_bounds__(256, 2) void k_product_exact(Operand A, Operand B, int32_t nkb, int32_t per_split, Out o)
+{
+    constexpr int BM = 32 * MT, BN = 32 * NT, kStage = (BM + BN) * 128;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kStage];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave & 1, wn = wave >> 1;
+    int32_t m_tile, n_tile;
+    tile_of(blockIdx.x, (A.rows + BM - 1) / BM, (B.rows + BN - 1) / BN, m_tile, n_tile);
+    const int32_t m0 = m_tile * BM, n0 = n_tile * BN, N = B.rows;
+    const int32_t k_begin = (int32_t)blockIdx.y * per_split, k_end = k_begin + per_split < nkb ? k_begin + per_split : nkb;
+    const auto a_tile = tile_buffer(A.q + (int64_t)m0 * A.ld), b_tile = tile_buffer(B.q + (int64_t)n0 * B.ld);
+    uint32_t a_at[MT], b_at[NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) a_at[i] = lds_source((wave * MT + i) * 8, lane, A.rows - m0, A.ld);
+#pragma unroll
+    for (int i = 0; i < NT; ++i) b_at[i] = lds_source((wave * NT + i) * 8, lane, N - n0, B.ld);
+    auto fetch = [&](int32_t kb) {
+        const uint32_t k = (uint32_t)kb * 128;
+        uint8_t *stage = lds + (kb & 1) * kStage;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) to_lds(a_tile, a_at[i], k, stage + (wave * MT + i) * 1024);
+#pragma unroll
+        for (int i = 0; i < NT; ++i) to_lds(b_tile, b_at[i], k, stage + BM * 128 + (wave * NT + i) * 1024);
+    };
+    f32x4_t acc[MT][NT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+    const int32_t row_a = m0 + wm * 16 * MT + (lane & 15), row_b = n0 + wn * 16 * NT + (lane & 15);
+    uint32_t sa[MT], sb[NT], sa_next[MT], sb_next[NT];
+    auto scales = [&](int32_t kb) {                         // (of the last blocks again past the end)
+        kb = kb < nkb ? kb : nkb - 1;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) sa_next[mt] = scale_word(A, row_a + 16 * mt, kb);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) sb_next[nt] = scale_word(B, row_b + 16 * nt, kb);
+    };
+    fetch(k_begin);
+    scales(k_begin);
+    for (int32_t kb = k_begin; kb < k_end; ++kb) {
+        if (((kb - k_begin) & 3) == 0) {                    // (splits start at multiples of four blocks)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) sa[mt] = sa_next[mt];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) sb[nt] = sb_next[nt];
+        }
+        __builtin_amdgcn_s_waitcnt(0x0f70);                 // vmcnt(0): the barrier alone does not wait for loads to LDS
+        __syncthreads();                                    // this stage has come; the other one is read
+        if (kb + 1 < k_end) fetch(kb + 1);
+        if (((kb - k_begin) & 3) == 0) scales(kb + 4);
+        const uint8_t *stage = lds + (kb & 1) * kStage;
+        bf16x8_t wide[MT][4];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            decode<FA>(fragment(stage + (wm * MT + mt) * 2048, lane), sa[mt], wide[mt]);
+            sa[mt] >>= 8;
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            bf16x8_t w[4];
+            decode<0>(fragment(stage + BM * 128 + (wn * NT + nt) * 2048, lane), sb[nt], w);
+            sb[nt] >>= 8;
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+                    acc[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[q], wide[mt][q], acc[mt][nt], 0, 0, 0);
+        }
+    }
+    Out to = o;
+    if constexpr (KIND == kOutPart) to.C = static_cast<float *>(o.C) + (int64_t)blockIdx.y * A.rows * o.ld;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        const int32_t m = row_a + 16 * mt;
+        if (m >= A.rows) continue;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int32_t n = n0 + (wn * NT + nt) * 16 + 4 * (lane >> 4);
+            float v[4] = {acc[mt][nt][0], acc[mt][nt][1], acc[mt][nt][2], acc[mt][nt][3]};
+            if constexpr (KIND != kOutPart) finish4<KIND>(o, n, N, v);
+            store4<KIND>(to, m, n, N, v);
+        }
+    }
+}
+
+// Few rows (up to 16 MT): bound by reading B.  A workgroup has 16 NT columns, its
+// eight waves a run of K each; fragments go from memory to registers, the next
+// block's while one is multiplied, and the waves' sums are added in LDS in the
+// order of K.
+template <int MT, int NT, int FA, bool EXACT, OutKind KIND>
+__global__ __launch_bounds__(512) void k_product_few(Operand A, Operand B, int32_t nkb, int32_t per_split, Out o)
+{
+    constexpr int kWaves = 8, kTiles = MT * NT;
+    __shared__ f32x4_t sums[kWaves][kTiles][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
+    const int32_t N = B.rows, n0 = (int32_t)blockIdx.x * 16 * NT;
+    const int32_t s_begin = (int32_t)blockIdx.y * per_split, s_end = s_begin + per_split < nkb ? s_begin + per_split : nkb;
+    const int32_t each = (s_end - s_begin + kWaves - 1) / kWaves;
+    const int32_t k_begin = s_begin + wave * each < s_end ? s_begin + wave * each : s_end,
+                  k_end = k_begin + each < s_end ? k_begin + each : s_end;
+    const uint8_t *a_at[MT], *b_at[NT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        const int32_t r = 16 * mt + (lane & 15);
+        a_at[mt] = A.q + (int64_t)(r < A.rows ? r : A.rows - 1) * A.ld + g * 16;
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int32_t r = n0 + 16 * nt + (lane & 15);
+        b_at[nt] = B.q + (int64_t)(r < N ? r : N - 1) * B.ld + g * 16;
+    }
+    struct Block {
+        i32x8_t a[MT], b[NT];
+    };
+    auto load = [&](int32_t kb, Block &x) {
+        const int64_t k = (int64_t)kb * 128;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const i32x4_t lo = *reinterpret_cast<const i32x4_t *>(b_at[nt] + k), hi = *reinterpret_cast<const i32x4_t *>(b_at[nt] + k + 64);
+            x.b[nt] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            const i32x4_t lo = *reinterpret_cast<const i32x4_t *>(a_at[mt] + k), hi = *reinterpret_cast<const i32x4_t *>(a_at[mt] + k + 64);
+            x.a[mt] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+    };
+    uint32_t sa[MT], sb[NT];
+    auto scales = [&](int32_t kb) {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) sa[mt] = scale_word(A, 16 * mt + (lane & 15), kb) >> (8 * (kb & 3));
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) sb[nt] = scale_word(B, n0 + 16 * nt + (lane & 15), kb) >> (8 * (kb & 3));
+    };
+    f32x4_t acc[MT][NT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+    auto multiply = [&](const Block &x) {
+        if constexpr (EXACT) {
+            bf16x8_t wide[MT][4];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) decode<FA>(x.a[mt], sa[mt], wide[mt]);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                bf16x8_t w[4];
+                decode<0>(x.b[nt], sb[nt], w);
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt)
+                        acc[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[q], wide[mt][q], acc[mt][nt], 0, 0, 0);
+            }
+        } else {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+                    acc[mt][nt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x.b[nt], x.a[mt], acc[mt][nt], 0, FA, 0,
+                                                                                  (int)sb[nt], 0, (int)sa[mt]);
+        }
+    };
+    auto next_scales = [&](int32_t kb) {                    // of block kb, after kb - 1
+        if ((kb & 3) == 0) {
+            if (kb < k_end) scales(kb);
+        } else {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) sa[mt] >>= 8;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) sb[nt] >>= 8;
+        }
+    };
+    if (k_begin < k_end) {
+        Block x, y;
+        load(k_begin, x);
+        scales(k_begin);
+        int32_t kb = k_begin;
+        for (; kb + 1 < k_end; kb += 2) {
+            load(kb + 1, y);
+            multiply(x);
+            next_scales(kb + 1);
+            if (kb + 2 < k_end) load(kb + 2, x);
+            multiply(y);
+            next_scales(kb + 2);
+        }
+        if (kb < k_end) multiply(x);
+    }
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) sums[wave][mt * NT + nt][lane] = acc[mt][nt];
+    __syncthreads();
+    for (int e = threadIdx.x; e < kTiles * 64; e += 512) {
+        const int tile = e >> 6, l = e & 63;
+        f32x4_t v = sums[0][tile][l];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) v += sums[w][tile][l];
+        const int32_t m = 16 * (tile / NT) + (l & 15), n = n0 + 16 * (tile % NT) + 4 * (l >> 4);
+        if (m >= A.rows) continue;
+        float out[4] = {v[0], v[1], v[2], v[3]};
+        Out to = o;
+        if constexpr (KIND == kOutPart) to.C = static_cast<float *>(o.C) + (int64_t)blockIdx.y * A.rows * o.ld;
+        else finish4<KIND>(o, n, N, out);
+        store4<KIND>(to, m, n, N, out);
+    }
+}
+
 // Sum of the splits' partial sums, in the order of K, and what becomes of it:
 // 32 lanes take 128 columns of a row.
 template <OutKind KIND>
@@ -714,23 +912,46 @@ __global__ __launch_bounds__(256) void k_product_join(const float *__restrict__ 
     }
 }
 
-struct Plan {
-    int32_t splits, per_split;
-};
-
+constexpr int kFewRows = 64;                                // rows that go with columns of B straight from memory
 constexpr int kBM = 128, kBN = 128;
+
+struct Plan {
+    int32_t splits, per_split, nt, bm;                      // nt: column tiles of a workgroup, few rows; bm: rows of a tile
+};
 
 bool deep(int64_t M, int64_t N, int64_t K, bool exact) { return !exact && M >= 256 && N >= 256 && K >= 1536; }
 
-// K is split where the tiles leave compute units idle, at least four blocks to a split.
-Plan plan_product(int64_t M, int64_t N, int64_t nkb)
+// Few rows to 8 bits: a block of 128 columns is several workgroups', so the
+// sums go through the workspace, where K is long enough to be worth it.
+bool joined_to_codes(int64_t M, int64_t nkb) { return M <= kFewRows && nkb >= 32; }
+
+// K is split where the tiles leave compute units idle.
+Plan plan_product(int64_t M, int64_t N, int64_t nkb, bool exact)
 {
-    const int64_t tiles = ((M + kBM - 1) / kBM) * ((N + kBN - 1) / kBN);
-    int64_t s = compute_units() / tiles;
+    const int64_t cus = compute_units();
+    if (M <= kFewRows) {
+        // more columns a workgroup read A less often, where K is long enough to split instead
+        const int by_rows = nkb < 64 ? 1 : M > 32 ? 4 : M > 16 ? 2 : 1, by_columns = N >= 64 * cus ? 4 : N >= 32 * cus ? 2 : 1;
+        const int nt = by_rows > by_columns ? by_rows : by_columns;
+        const int64_t groups = (N + 16 * nt - 1) / (16 * nt);
+        int64_t s = cus / groups;                           // at least four blocks of K to a wave
+        s = s < nkb / 32 ? s : nkb / 32;
+        s = s < 1 ? 1 : s;
+        const int64_t per = (nkb + s - 1) / s;
+        return {(int32_t)((nkb + per - 1) / per), (int32_t)per, nt, 0};
+    }
+    // two workgroups a compute unit hide each other's waits
+    int64_t tiles = ((M + kBM - 1) / kBM) * ((N + kBN - 1) / kBN);
+    int32_t bm = kBM;
+    if (exact && tiles < 2 * cus && nkb < 64) {
+        bm = 64;
+        tiles = ((M + 63) / 64) * ((N + kBN - 1) / kBN);
+    }
+    int64_t s = (exact ? 2 : 1) * cus / tiles;
     s = s < nkb / 4 ? s : nkb / 4;
     s = s < 1 ? 1 : s;
     const int64_t per = (nkb + 4 * s - 1) / (4 * s) * 4;    // multiples of four blocks
-    return {(int32_t)((nkb + per - 1) / per), (int32_t)per};
+    return {(int32_t)((nkb + per - 1) / per), (int32_t)per, 0, bm};
 }
 
 Operand operand(const hwsel_fp8_t &x)
@@ -738,10 +959,34 @@ Operand operand(const hwsel_fp8_t &x)
     return {x.q, x.ld, x.scale, x.ld_scale, (int32_t)x.rows, x.block_rows == 1 ? 0 : 7};
 }
 
+template <int MT, bool EXACT, OutKind KIND>
+void launch_few(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const Plan &p, const Out &o, hipStream_t s)
+{
+    const int32_t nkb = (int32_t)fp8_blocks(A.cols);
+    auto go = [&](auto kernel) {
+        const dim3 grid((unsigned)((B.rows + 16 * p.nt - 1) / (16 * p.nt)), (unsigned)p.splits);
+        hipLaunchKernelGGL(kernel, grid, dim3(512), 0, s, operand(A), operand(B), nkb, p.per_split, o);
+    };
+    if (A.format == HWSEL_FP8_E4M3) {
+        if (p.nt == 4) go(k_product_few<MT, 4, 0, EXACT, KIND>);
+        else if (p.nt == 2) go(k_product_few<MT, 2, 0, EXACT, KIND>);
+        else go(k_product_few<MT, 1, 0, EXACT, KIND>);
+    } else {
+        if (p.nt == 4) go(k_product_few<MT, 4, 1, EXACT, KIND>);
+        else if (p.nt == 2) go(k_product_few<MT, 2, 1, EXACT, KIND>);
+        else go(k_product_few<MT, 1, 1, EXACT, KIND>);
+    }
+}
+
 template <bool EXACT, OutKind KIND>
 void launch_tiles(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const Plan &p, const Out &o, hipStream_t s)
 {
     const int32_t nkb = (int32_t)fp8_blocks(A.cols);
+    if constexpr (KIND != kOutFp8) {
+        if (A.rows <= 16) return launch_few<1, EXACT, KIND>(A, B, p, o, s);
+        if (A.rows <= 32) return launch_few<2, EXACT, KIND>(A, B, p, o, s);
+        if (A.rows <= kFewRows) return launch_few<4, EXACT, KIND>(A, B, p, o, s);
+    }
     if constexpr (!EXACT && KIND != kOutPart) {
         if (nkb <= 4 && p.splits == 1) {
             const int32_t n_tiles = (int32_t)((B.rows + 127) / 128), m_tiles = (int32_t)((A.rows + 127) / 128);
@@ -771,13 +1016,24 @@ void launch_tiles(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const Plan &p, con
             return;
         }
     }
-    const dim3 grid((unsigned)((B.rows + kBN - 1) / kBN * ((A.rows + kBM - 1) / kBM)), (unsigned)p.splits);
-    if (A.format == HWSEL_FP8_E4M3)
-        hipLaunchKernelGGL((k_product<4, 1, 2, 0, EXACT, KIND>), grid, dim3(256), 0, s, operand(A), operand(B), nkb, p.per_split,
-                           o);
-    else
-        hipLaunchKernelGGL((k_product<4, 1, 2, 1, EXACT, KIND>), grid, dim3(256), 0, s, operand(A), operand(B), nkb, p.per_split,
-                           o);
+    if constexpr (EXACT) {
+        // tiles of 64 rows where those of 128 would not give every compute unit two
+        const bool low = p.bm == 64;
+        const dim3 grid((unsigned)((B.rows + 127) / 128 * ((A.rows + p.bm - 1) / p.bm)), (unsigned)p.splits);
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, operand(A), operand(B), nkb, p.per_split, o); };
+        if (A.format == HWSEL_FP8_E4M3) {
+            if (low) go(k_product_exact<2, 4, 0, KIND>);
+            else go(k_product_exact<4, 4, 0, KIND>);
+        } else {
+            if (low) go(k_product_exact<2, 4, 1, KIND>);
+            else go(k_product_exact<4, 4, 1, KIND>);
+        }
+    } else {
+        const dim3 grid((unsigned)((B.rows + kBN - 1) / kBN * ((A.rows + kBM - 1) / kBM)), (unsigned)p.splits);
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, operand(A), operand(B), nkb, p.per_split, o); };
+        if (A.format == HWSEL_FP8_E4M3) go(k_product<4, 1, 2, 0, KIND>);
+        else go(k_product<4, 1, 2, 1, KIND>);
+    }
 }
 
 int64_t part_ld(int64_t N) { return (N + 3) / 4 * 4; }
@@ -785,8 +1041,8 @@ int64_t part_ld(int64_t N) { return (N + 3) / 4 * 4; }
 template <OutKind KIND>
 hipError_t run_product(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const Out &o, void *ws, hipStream_t s)
 {
-    const Plan p = plan_product(A.rows, B.rows, fp8_blocks(A.cols));
-    if (p.splits == 1) {
+    const Plan p = plan_product(A.rows, B.rows, fp8_blocks(A.cols), KIND == kOutF32);
+    if (p.splits == 1 && !(KIND == kOutFp8 && joined_to_codes(A.rows, fp8_blocks(A.cols)))) {
         launch_tiles<KIND == kOutF32, KIND>(A, B, p, o, s);
     } else {
         Out part = o;
@@ -802,10 +1058,17 @@ hipError_t run_product(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const Out &o,
 
 }  // namespace
 
+// Enough for whatever the result is held in.
 size_t fp8_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K)
 {
-    const Plan p = plan_product(M, N, fp8_blocks(K));
-    return p.splits == 1 ? 0 : (size_t)p.splits * (size_t)M * (size_t)part_ld(N) * 4;
+    size_t most = 0;
+    for (int exact = 0; exact < 2; ++exact) {
+        const Plan p = plan_product(M, N, fp8_blocks(K), exact);
+        const bool used = p.splits > 1 || (!exact && joined_to_codes(M, fp8_blocks(K)));
+        const size_t bytes = used ? (size_t)p.splits * (size_t)M * (size_t)part_ld(N) * 4 : 0;
+        most = bytes > most ? bytes : most;
+    }
+    return most;
 }
 
 hipError_t launch_fp8_matmul(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const float *bias, bool gelu, void *C, bool bf16,
