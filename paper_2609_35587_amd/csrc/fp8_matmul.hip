@@ -930,9 +930,7 @@ Plan plan_product(int64_t M, int64_t N, int64_t nkb, bool exact)
 {
     const int64_t cus = compute_units();
     if (M <= kFewRows) {
-        // more columns a workgroup read A less often, where K is long enough to split instead
-        const int by_rows = nkb < 64 ? 1 : M > 32 ? 4 : M > 16 ? 2 : 1, by_columns = N >= 64 * cus ? 4 : N >= 32 * cus ? 2 : 1;
-        const int nt = by_rows > by_columns ? by_rows : by_columns;
+        const int nt = N >= 64 * cus ? 4 : N >= 32 * cus ? 2 : 1;
         const int64_t groups = (N + 16 * nt - 1) / (16 * nt);
         int64_t s = cus / groups;                           // at least four blocks of K to a wave
         s = s < nkb / 32 ? s : nkb / 32;
