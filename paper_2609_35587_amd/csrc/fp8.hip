@@ -114,26 +114,14 @@ struct TileIn {
     bool vec;                                               // four elements at a multiple of four can be read at once
 };
 
+// Four elements of a row in fp32 or bf16, zeros outside.
 template <Source S>
 __device__ __forceinline__ void load4(const TileIn &in, int64_t r, int64_t c, float (&v)[4])
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = 0.0f;
     if (r >= in.rows || c >= in.cols) return;
-    if constexpr (S == Source::fp8) {
-        // rows are padded with zeros to whole blocks, so four codes can always be read
-        const int w = *reinterpret_cast<const int *>(static_cast<const uint8_t *>(in.X) + r * in.ld + c);
-        const float s = scale_value(in.scale[(in.block_rows == 1 ? r : r / kFp8Block) * in.ld_scale + c / kFp8Block]);
-        f32x2_t a, b;
-        if (in.format == HWSEL_FP8_E4M3) {
-            a = __builtin_amdgcn_cvt_pk_f32_fp8(w, false);
-            b = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
-        } else {
-            a = __builtin_amdgcn_cvt_pk_f32_bf8(w, false);
-            b = __builtin_amdgcn_cvt_pk_f32_bf8(w, true);
-        }
-        v[0] = a.x * s; v[1] = a.y * s; v[2] = b.x * s; v[3] = b.y * s;
-    } else if (in.vec && c + 4 <= in.cols) {
+    if (in.vec && c + 4 <= in.cols) {
         if constexpr (S == Source::fp32) {
             const float4 w = *reinterpret_cast<const float4 *>(static_cast<const float *>(in.X) + r * in.ld + c);
             v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
@@ -165,23 +153,65 @@ __global__ __launch_bounds__(kThreads) void k_quantise_tiles(TileIn in, hwsel_fp
     constexpr int kRow = 144;
     __shared__ uint32_t part[8][128];
     __shared__ __attribute__((aligned(16))) uint8_t lds[TRANSPOSED ? 128 * kRow : 16];
+    __shared__ __attribute__((aligned(16))) float row_scale[S == Source::fp8 ? 128 : 4];
     const int64_t n_ct = (in.cols + 127) / 128, n_tiles = (in.rows + 127) / 128 * n_ct;
     const int c4 = (threadIdx.x & 31) * 4, group = threadIdx.x >> 5;
     for (int64_t tile = blockIdx.x; tile < n_tiles; tile += gridDim.x) {
         const int64_t rt = tile / n_ct, ct = tile % n_ct, c = ct * 128 + c4;
         float v[16][4];
+        if constexpr (S == Source::fp8) {
+            // sixteen loads on their way at once, from the last row where the tile goes past it; rows are
+            // padded with zeros to whole blocks, so four codes can always be read
+            const uint8_t *q = static_cast<const uint8_t *>(in.X) + c;
+            const int64_t r0 = rt * 128 + 16 * group;
+            int w[16];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) load4<S>(in, rt * 128 + 16 * group + j, c, v[j]);
-        uint32_t m[4] = {0, 0, 0, 0}, all = 0;
+            for (int j = 0; j < 16; ++j)
+                w[j] = *reinterpret_cast<const int *>(q + (r0 + j < in.rows ? r0 + j : in.rows - 1) * in.ld);
+            if (threadIdx.x < 128) {
+                int64_t r = rt * 128 + threadIdx.x;
+                r = r < in.rows ? r : in.rows - 1;
+                row_scale[threadIdx.x] = scale_value(in.scale[(in.block_rows == 1 ? r : rt) * in.ld_scale + ct]);
+            }
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const float s = row_scale[16 * group + j];
+                const int u = r0 + j < in.rows ? w[j] : 0;
+                f32x2_t a, b;
+                if (in.format == HWSEL_FP8_E4M3) {
+                    a = __builtin_amdgcn_cvt_pk_f32_fp8(u, false);
+                    b = __builtin_amdgcn_cvt_pk_f32_fp8(u, true);
+                } else {
+                    a = __builtin_amdgcn_cvt_pk_f32_bf8(u, false);
+                    b = __builtin_amdgcn_cvt_pk_f32_bf8(u, true);
+                }
+                v[j][0] = a.x * s; v[j][1] = a.y * s; v[j][2] = b.x * s; v[j][3] = b.y * s;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) load4<S>(in, rt * 128 + 16 * group + j, c, v[j]);
+        }
+        uint32_t m[4] = {0, 0, 0, 0};
 #pragma unroll
         for (int j = 0; j < 16; ++j)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint32_t a = __float_as_uint(v[j][i]) & 0x7fffffffu, f = a < 0x7f800000u ? a : 0u;
-                all = a > all ? a : all;
-                m[i] = f > m[i] ? f : m[i];
+                const uint32_t a = __float_as_uint(v[j][i]) & 0x7fffffffu;
+                m[i] = a > m[i] ? a : m[i];
             }
-        const bool odd = all >= 0x7f800000u;
+        const bool odd = (m[0] > m[1] ? m[0] : m[1]) >= 0x7f800000u || (m[2] > m[3] ? m[2] : m[3]) >= 0x7f800000u;
+        if (odd) {                                          // scales go by the finite elements
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                m[i] = 0;
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const uint32_t f = finite_bits(v[j][i]);
+                    m[i] = f > m[i] ? f : m[i];
+                }
+            }
+        }
         *reinterpret_cast<uint4 *>(&part[group][c4]) = make_uint4(m[0], m[1], m[2], m[3]);
         __syncthreads();
         uint32_t byte[4];

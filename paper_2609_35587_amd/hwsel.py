@@ -145,8 +145,8 @@ def _ptr(t) -> int | None:
 
 
 def _stream(stream) -> int | None:
-    if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+    if stream is None:                                      # (0.3 us; 2.7 through a Stream object)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -685,19 +685,19 @@ def hwsel_fp8_empty(rows: int, cols: int, format: int = FP8_E4M3, block_rows: in
 
 
 def _fp8(m: dict, name: str, like: torch.Tensor | None = None) -> hwsel_fp8_t:
-    q, s, rows, block_rows = m["q"], m["scale"], int(m["rows"]), int(m["block_rows"])
+    q, s, rows, cols, block_rows = m["q"], m["scale"], int(m["rows"]), int(m["cols"]), int(m["block_rows"])
     for t, part in ((q, "q"), (s, "scale")):
         if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2 or t.dtype != torch.uint8 or \
-                (t.shape[1] > 1 and t.stride(1) != 1):
+                (t.stride(1) != 1 and t.shape[1] > 1):
             raise ValueError(f"{name}.{part} must be a 2-D uint8 device tensor with unit column stride")
-        if t.device != (q if like is None else like).device:
+        if t.get_device() != (q if like is None else like).get_device():
             raise ValueError(f"{name}.{part} is on {t.device}, the other operands on {(q if like is None else like).device}")
-    blocks = -(-int(m["cols"]) // FP8_BLOCK)
-    if q.shape[0] < rows or q.shape[1] < blocks * FP8_BLOCK or \
-            s.shape[0] < -(-rows // max(block_rows, 1)) or s.shape[1] < -(-blocks // 4) * 4:
-        raise ValueError(f"{name}: buffers {tuple(q.shape)}, {tuple(s.shape)} are short of {rows} x {m['cols']}")
-    return hwsel_fp8_t(rows, int(m["cols"]), q.data_ptr(), q.stride(0), s.data_ptr(), s.stride(0), int(m["format"]),
-                       block_rows)
+    blocks = -(-cols // FP8_BLOCK)
+    (q_rows, q_cols), (s_rows, s_cols) = q.shape, s.shape
+    if q_rows < rows or q_cols < blocks * FP8_BLOCK or s_rows < -(-rows // max(block_rows, 1)) or \
+            s_cols < -(-blocks // 4) * 4:
+        raise ValueError(f"{name}: buffers {tuple(q.shape)}, {tuple(s.shape)} are short of {rows} x {cols}")
+    return hwsel_fp8_t(rows, cols, q.data_ptr(), q.stride(0), s.data_ptr(), s.stride(0), int(m["format"]), block_rows)
 
 
 def _plain(X, name: str, rows: int, cols: int, like: torch.Tensor) -> int:
