@@ -428,7 +428,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_product(Operand A, Operand 
 // its fragments from LDS the other one multiplies, so the matrix cores and LDS
 // are both busy all the time.  The second group runs a phase behind.
 template <int FA, OutKind KIND>
-__global__ __launch_bounds__(512) void k_product_deep(Operand A, Operand B, int32_t nkb, int32_t per_split, Out o)
+__global__ __launch_bounds__(512) void k_product_deep(Operand A, Operand B, int32_t nkb, Out o)
 {
     constexpr int MT = 4, NT = 8, BM = 256, BN = 256, kStage = (BM + BN) * 128;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kStage];
@@ -441,15 +441,13 @@ __global__ __launch_bounds__(512) void k_product_deep(Operand A, Operand B, int3
     int32_t m_tile, n_tile;
     tile_of(blockIdx.x, (A.rows + BM - 1) / BM, (B.rows + BN - 1) / BN, m_tile, n_tile);
     const int32_t m0 = m_tile * BM, n0 = n_tile * BN;
-    // (splits start at multiples of four blocks)
-    const int32_t k_begin = (int32_t)blockIdx.y * per_split, k_end = k_begin + per_split < nkb ? k_begin + per_split : nkb;
     const auto a_tile = tile_buffer(A.q + (int64_t)m0 * A.ld), b_tile = tile_buffer(B.q + (int64_t)n0 * B.ld);
     // a wave brings 32 rows of A, those of its own group; a wave of the first group 64 of B
     uint32_t a_at[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) a_at[i] = lds_source(wave * 32 + i * 8, lane, A.rows - m0, A.ld);
     // (past the end the last block is brought again, to a stage that is not read)
-    auto k_of = [&](int32_t kb) { return (uint32_t)(kb < k_end ? kb : k_end - 1) * 128; };
+    auto k_of = [&](int32_t kb) { return (uint32_t)(kb < nkb ? kb : nkb - 1) * 128; };
     // thread t brings the bytes of row t of A's 256, then of B's
     const int32_t own = (int32_t)threadIdx.x & 255;
     const bool of_b = threadIdx.x >= 256;
@@ -479,19 +477,19 @@ __global__ __launch_bounds__(512) void k_product_deep(Operand A, Operand B, int3
             to_lds(b_tile, lds_source((wave & 3) * 64 + i * 8, l, B.rows - n0, B.ld), k_of(kb), lds + (kb & 1) * kStage + BM * 128 + ((wave & 3) * 8 + i) * 1024);
     };
     auto lds_done = [] { __builtin_amdgcn_s_waitcnt(0xc07f); };           // lgkmcnt(0)
-    if (!second) fetch_b(k_begin);
+    if (!second) fetch_b(0);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) fetch_a(k_begin, i);
-    put_scales(k_begin, load_scales(k_begin));
-    if (!second) fetch_b(k_begin + 1);
+    for (int i = 0; i < 4; ++i) fetch_a(0, i);
+    put_scales(0, load_scales(0));
+    if (!second) fetch_b(0 + 1);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) fetch_a(k_begin + 1, i);
+    for (int i = 0; i < 4; ++i) fetch_a(0 + 1, i);
     __builtin_amdgcn_s_waitcnt(0x0f70);                     // vmcnt(0)
     lds_done();
     barrier();
     if (second) barrier();
     uint32_t next_scales = 0;
-    for (int32_t kb = k_begin; kb < k_end; ++kb) {
+    for (int32_t kb = 0; kb < nkb; ++kb) {
         const uint8_t *stage = lds + (kb & 1) * kStage;
         const uint8_t *sc = scale_lds[(kb >> 2) & 1][kb & 3];
         i32x8_t a[MT], b[NT];
@@ -503,7 +501,7 @@ __global__ __launch_bounds__(512) void k_product_deep(Operand A, Operand B, int3
         for (int nt = 0; nt < NT; ++nt) b[nt] = fragment(stage + BM * 128 + (wn * NT + nt) * 2048, lane);
         __builtin_amdgcn_sched_barrier(0);
         // the other stage: the second group has read it in the phase before
-        if (!second && kb > k_begin) fetch_b(kb + 1);
+        if (!second && kb > 0) fetch_b(kb + 1);
         if ((kb & 3) == 2) put_scales(kb + 2, next_scales);
         lds_done();                                         // the fragments are here
         barrier();
@@ -533,7 +531,7 @@ __global__ __launch_bounds__(512) void k_product_deep(Operand A, Operand B, int3
     }
     if (!second) barrier();
     __builtin_amdgcn_s_waitcnt(0x0f70);                     // (no load to LDS outlives the workgroup)
-    finish_tiles<MT, KIND>(acc, m0 + wm * 64, n0 + wn * 128, A.rows, B.rows, (int32_t)blockIdx.y, o, lane);
+    finish_tiles<MT, KIND>(acc, m0 + wm * 64, n0 + wn * 128, A.rows, B.rows, 0, o, lane);
 }
 
 // Short sums (K up to 128 NKB), many rows.  A wave keeps its MT x 16 rows of A in
@@ -912,44 +910,52 @@ __global__ __launch_bounds__(256) void k_product_join(const float *__restrict__ 
     }
 }
 
-constexpr int kFewRows = 64;                                // rows that go with columns of B straight from memory
 constexpr int kBM = 128, kBN = 128;
 
+enum class Way { few, rows, deep, tiles };                  // the kernels above
+
 struct Plan {
+    Way way;
     int32_t splits, per_split, nt, bm;                      // nt: column tiles of a workgroup, few rows; bm: rows of a tile
 };
 
-bool deep(int64_t M, int64_t N, int64_t K, bool exact) { return !exact && M >= 256 && N >= 256 && K >= 1536; }
-
-// Few rows to 8 bits: a block of 128 columns is several workgroups', so the
-// sums go through the workspace, where K is long enough to be worth it.
-bool joined_to_codes(int64_t M, int64_t nkb) { return M <= kFewRows && nkb >= 32; }
-
-// K is split where the tiles leave compute units idle.
+// The kernel, and how many parts K is split into, by sizes alone.  us are of
+// calls in a graph, results in bf16 where nothing else is said.
 Plan plan_product(int64_t M, int64_t N, int64_t nkb, bool exact)
 {
     const int64_t cus = compute_units();
-    if (M <= kFewRows) {
-        const int nt = N >= 64 * cus ? 4 : N >= 32 * cus ? 2 : 1;
-        const int64_t groups = (N + 16 * nt - 1) / (16 * nt);
-        int64_t s = cus / groups;                           // at least four blocks of K to a wave
-        s = s < nkb / 32 ? s : nkb / 32;
+    auto plan = [&](Way way, int64_t s, int64_t unit, int32_t nt, int32_t bm) {
         s = s < 1 ? 1 : s;
-        const int64_t per = (nkb + s - 1) / s;
-        return {(int32_t)((nkb + per - 1) / per), (int32_t)per, nt, 0};
+        const int64_t per = (nkb + unit * s - 1) / (unit * s) * unit;
+        return Plan{way, (int32_t)((nkb + per - 1) / per), (int32_t)per, nt, bm};
+    };
+    // Few rows.  K = N = 8,192: 13.6 us (1 row), 14.9 (16), 19.4 (32), where tiles take 20.2, 20.5 and 20.7.  With
+    // 64 rows, a weight for four products, only small B: 64 x 1,024 x 1,024 4.9 (tiles 8.4), 64 x 4,096 x 4,096 13.0
+    // (14.3), but 64 x 8,192 x 8,192 39 (22).  Wider workgroups read A less often, where there are columns enough:
+    // 16 x 16,384 x 4,096 18.1, 15.4 and 13.3 with 1, 2 and 4 tiles of columns, 16 x 8,192 x 8,192 18.1, 14.8 and
+    // 16.2, 32 x 16,384 x 16,384 97, 67 and 92 (registers), 32 x 4,096 x 4,096 8.5, 10.6 and 21.
+    if (M <= 32 || (M <= 64 && N * nkb < (1 << 17))) {
+        const int nt = M <= 16 && N >= 64 * cus ? 4 : M <= 32 && N >= 32 * cus ? 2 : 1;
+        const int64_t s = cus / ((N + 16 * nt - 1) / (16 * nt));
+        return plan(Way::few, s < nkb / 32 ? s : nkb / 32, 1, nt, 0);
     }
-    // two workgroups a compute unit hide each other's waits
-    int64_t tiles = ((M + kBM - 1) / kBM) * ((N + kBN - 1) / kBN);
-    int32_t bm = kBM;
-    if (exact && tiles < 2 * cus && nkb < 64) {
-        bm = 64;
-        tiles = ((M + 63) / 64) * ((N + kBN - 1) / kBN);
-    }
-    int64_t s = (exact ? 2 : 1) * cus / tiles;
-    s = s < nkb / 4 ? s : nkb / 4;
-    s = s < 1 ? 1 : s;
-    const int64_t per = (nkb + 4 * s - 1) / (4 * s) * 4;    // multiples of four blocks
-    return {(int32_t)((nkb + per - 1) / per), (int32_t)per, 0, bm};
+    auto tiles_of = [&](int64_t m, int64_t n) { return (M + m - 1) / m * ((N + n - 1) / n); };
+    // Tiles of 256 x 256, if they fill five compute units in eight: 2,816 x 4,096 x 4,096 47 us (128 x 128: 62),
+    // 8,192 x 8,192 x 2,048 128 (155), 4,096 x 4,096 x 1,024 23.1 (24.0), but 2,048 x 4,096 x 4,096 44 (37) and
+    // 4,096 x 4,096 x 768 20.9 (21.3), where their start weighs as much as they win.
+    if (!exact && M >= 256 && N >= 256 && nkb >= 8 && tiles_of(256, 256) * 8 >= cus * 5) return plan(Way::deep, 1, 4, 0, 256);
+    // Short sums over many tiles: 65,536 x 1,024 x 512 53.9 us (tiles one by one: 57.2), with K = 128 30.8 (35.9),
+    // 262,144 x 1,024 x 512 to 8 bits 210 (277), but 32,768 x 1,024 x 512 33.6 (31.0) and 8,192 13.5 (11.4).
+    if (!exact && nkb <= 4 && tiles_of(kBM, kBN) >= 12 * cus) return plan(Way::rows, 1, 4, 0, kBM);
+    // Lower tiles in fp32, where there would be fewer than two workgroups a compute unit and K is too short to
+    // split instead: 4,099 x 1,000 x 2,500 41 us (128 rows: 46), 1,024 x 1,024 x 1,024 13 (15); with 65,536 of K
+    // 512 x 1,024 takes 89 (78).
+    const int32_t bm = exact && nkb < 64 && tiles_of(kBM, kBN) < 2 * cus ? 64 : kBM;
+    // K in parts, two workgroups a compute unit, eight blocks at least: 1,024 x 1,024 x 8,192 26 us (whole: 77),
+    // 100 x 4,096 x 4,096 15.5 (25; parts of four blocks 17.4), 64 x 16,384 x 16,384 54 (one workgroup: 78);
+    // 1,024 x 1,024 x 1,024 in fp32 10.6 whole and 12.9 in two.
+    const int64_t s = 2 * cus / tiles_of(bm, kBN);
+    return plan(Way::tiles, s < nkb / 8 ? s : nkb / 8, 4, 0, bm);
 }
 
 Operand operand(const hwsel_fp8_t &x)
@@ -965,28 +971,29 @@ void launch_few(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const Plan &p, const
         const dim3 grid((unsigned)((B.rows + 16 * p.nt - 1) / (16 * p.nt)), (unsigned)p.splits);
         hipLaunchKernelGGL(kernel, grid, dim3(512), 0, s, operand(A), operand(B), nkb, p.per_split, o);
     };
-    if (A.format == HWSEL_FP8_E4M3) {
-        if (p.nt == 4) go(k_product_few<MT, 4, 0, EXACT, KIND>);
-        else if (p.nt == 2) go(k_product_few<MT, 2, 0, EXACT, KIND>);
-        else go(k_product_few<MT, 1, 0, EXACT, KIND>);
-    } else {
-        if (p.nt == 4) go(k_product_few<MT, 4, 1, EXACT, KIND>);
-        else if (p.nt == 2) go(k_product_few<MT, 2, 1, EXACT, KIND>);
-        else go(k_product_few<MT, 1, 1, EXACT, KIND>);
-    }
+    auto by_columns = [&](auto fa) {
+        constexpr int FA = decltype(fa)::value;
+        if constexpr (MT == 1)
+            if (p.nt == 4) return go(k_product_few<MT, 4, FA, EXACT, KIND>);
+        if constexpr (MT <= 2)
+            if (p.nt == 2) return go(k_product_few<MT, 2, FA, EXACT, KIND>);
+        go(k_product_few<MT, 1, FA, EXACT, KIND>);
+    };
+    if (A.format == HWSEL_FP8_E4M3) by_columns(std::integral_constant<int, 0>{});
+    else by_columns(std::integral_constant<int, 1>{});
 }
 
 template <bool EXACT, OutKind KIND>
 void launch_tiles(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const Plan &p, const Out &o, hipStream_t s)
 {
     const int32_t nkb = (int32_t)fp8_blocks(A.cols);
-    if constexpr (KIND != kOutFp8) {
-        if (A.rows <= 16) return launch_few<1, EXACT, KIND>(A, B, p, o, s);
-        if (A.rows <= 32) return launch_few<2, EXACT, KIND>(A, B, p, o, s);
-        if (A.rows <= kFewRows) return launch_few<4, EXACT, KIND>(A, B, p, o, s);
+    if constexpr (KIND != kOutFp8) {                        // (to 8 bits through the workspace)
+        if (p.way == Way::few)
+            return A.rows <= 16 ? launch_few<1, EXACT, KIND>(A, B, p, o, s)
+                 : A.rows <= 32 ? launch_few<2, EXACT, KIND>(A, B, p, o, s) : launch_few<4, EXACT, KIND>(A, B, p, o, s);
     }
     if constexpr (!EXACT && KIND != kOutPart) {
-        if (nkb <= 4 && p.splits == 1) {
+        if (p.way == Way::rows) {
             const int32_t n_tiles = (int32_t)((B.rows + 127) / 128), m_tiles = (int32_t)((A.rows + 127) / 128);
             int32_t each = (int32_t)((int64_t)m_tiles * n_tiles / (4 * compute_units()));
             each = each < 1 ? 1 : each > n_tiles ? n_tiles : each;
@@ -1003,14 +1010,12 @@ void launch_tiles(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const Plan &p, con
             }
             return;
         }
-    }
-    if constexpr (!EXACT) {
-        if (deep(A.rows, B.rows, A.cols, EXACT)) {
-            const dim3 grid((unsigned)((B.rows + 255) / 256 * ((A.rows + 255) / 256)), (unsigned)p.splits);
+        if (p.way == Way::deep) {
+            const dim3 grid((unsigned)((B.rows + 255) / 256 * ((A.rows + 255) / 256)));
             if (A.format == HWSEL_FP8_E4M3)
-                hipLaunchKernelGGL((k_product_deep<0, KIND>), grid, dim3(512), 0, s, operand(A), operand(B), nkb, p.per_split, o);
+                hipLaunchKernelGGL((k_product_deep<0, KIND>), grid, dim3(512), 0, s, operand(A), operand(B), nkb, o);
             else
-                hipLaunchKernelGGL((k_product_deep<1, KIND>), grid, dim3(512), 0, s, operand(A), operand(B), nkb, p.per_split, o);
+                hipLaunchKernelGGL((k_product_deep<1, KIND>), grid, dim3(512), 0, s, operand(A), operand(B), nkb, o);
             return;
         }
     }
@@ -1040,7 +1045,7 @@ template <OutKind KIND>
 hipError_t run_product(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const Out &o, void *ws, hipStream_t s)
 {
     const Plan p = plan_product(A.rows, B.rows, fp8_blocks(A.cols), KIND == kOutF32);
-    if (p.splits == 1 && !(KIND == kOutFp8 && joined_to_codes(A.rows, fp8_blocks(A.cols)))) {
+    if (p.splits == 1 && !(KIND == kOutFp8 && p.way == Way::few)) {
         launch_tiles<KIND == kOutF32, KIND>(A, B, p, o, s);
     } else {
         Out part = o;
@@ -1062,7 +1067,7 @@ size_t fp8_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K)
     size_t most = 0;
     for (int exact = 0; exact < 2; ++exact) {
         const Plan p = plan_product(M, N, fp8_blocks(K), exact);
-        const bool used = p.splits > 1 || (!exact && joined_to_codes(M, fp8_blocks(K)));
+        const bool used = p.splits > 1 || (!exact && p.way == Way::few);
         const size_t bytes = used ? (size_t)p.splits * (size_t)M * (size_t)part_ld(N) * 4 : 0;
         most = bytes > most ? bytes : most;
     }

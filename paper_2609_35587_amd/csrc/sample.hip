@@ -779,7 +779,7 @@ __global__ __launch_bounds__(NT) void k_sample(const float *__restrict__ scores,
 // passes that hand their results on in the workspace: best score; histogram;
 // candidates around the cut, ranked by one workgroup (once for top-k, once for
 // top-p); sums of parts; draws.  A compute unit takes in some 100 GB/s, so 3
-// problems of 534,600 took 339 us in a workgroup each.
+// problems of 534,600 took 339 us in a workgroup each, 73 so.
 constexpr int kWide = 1024, kWideBins = 4096, kWideNear = 2048, kWideParts = 1024;
 
 struct WideState {
@@ -1100,8 +1100,10 @@ __global__ __launch_bounds__(kWide) void k_wide_draw(WideArgs a, const float *__
 }  // namespace
 
 // Segment lengths are not known here; their mean is.  Few problems of many
-// candidates are shared by workgroups: SPLITRULE
-static bool shared_problems(int64_t R, int32_t P) { return P <= 128 && R / P > 32768; }
+// candidates are shared by workgroups, which costs eleven launches: 8 problems
+// of 49,152 38 us (a workgroup each: 44), 8 of 32,768 38 (32); 64 of 131,072 70
+// (98), 64 of 65,536 62 (56); 128 of 262,144 159 (187), 128 of 65,536 69 (57).
+static bool shared_problems(int64_t R, int32_t P) { return P <= 128 && R / P > 40960 + 768 * (int64_t)P; }
 
 size_t sample_workspace_bytes(int64_t R, int32_t P, int32_t)
 {
@@ -1149,7 +1151,10 @@ hipError_t launch_sample(const float *scores, int64_t R, const int64_t *seg, int
 {
     if (shared_problems(R, P))
         launch_shared(WideArgs{scores, R, seg, static_cast<WideState *>(ws), Settings{how, n_draws}}, P, u, idx, prob, kept, s);
-    else if (R / P <= 8192) launch_problems<512, 1024, 8192>(scores, R, seg, P, how, u, n_draws, idx, prob, kept, s);
+    // Two workgroups of 512 threads a compute unit wait less than one of 1,024, which keeps three times as many
+    // candidates in LDS: 600 problems of 8,192 29 us (51), 600 of 24,576 70 (79), 128 of 8,192 15 (18), 8 of
+    // 12,288 19.8 (20.6), but 256 of 24,576 32 (27).
+    else if (R / P <= 12288 || P > compute_units()) launch_problems<512, 1024, 8192>(scores, R, seg, P, how, u, n_draws, idx, prob, kept, s);
     else launch_problems<1024, 2048, 24576>(scores, R, seg, P, how, u, n_draws, idx, prob, kept, s);
     return hipGetLastError();
 }
