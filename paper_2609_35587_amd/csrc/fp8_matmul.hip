@@ -656,32 +656,34 @@ __global__ __launch_bounds__(256, 2) void k_product_rows(Operand A, Operand B, i
 }
 
 // Results in fp32: products of decoded codes by the bf16 instruction (see above).
-// Four waves, two by two, each 16 MT x 16 NT: a fragment decoded serves MT or NT
-// products.  Two stages in LDS, the next block of K on its way meanwhile.
-template <int MT, int NT, int FA, OutKind KIND>
+// Four waves, WM along the rows, each 16 MT x 16 NT: a fragment decoded serves MT
+// or NT products.  Two stages in LDS, the next block of K on its way meanwhile.
+template <int WM, int MT, int FA, OutKind KIND>
 __global__ __launch_bounds__(256, 2) void k_product_exact(Operand A, Operand B, int32_t nkb, int32_t per_split, Out o)
 {
-    constexpr int BM = 32 * MT, BN = 32 * NT, kStage = (BM + BN) * 128;
+    constexpr int NT = 2 * WM, BM = 16 * WM * MT, BN = 128, kStage = (BM + BN) * 128;
+    constexpr int kLoadsA = (BM / 8 + 3) / 4, kLoadsB = BN / 8 / 4;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kStage];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = wave & 1, wn = wave >> 1;
+    const int wm = wave % WM, wn = wave / WM;
     int32_t m_tile, n_tile;
     tile_of(blockIdx.x, (A.rows + BM - 1) / BM, (B.rows + BN - 1) / BN, m_tile, n_tile);
     const int32_t m0 = m_tile * BM, n0 = n_tile * BN, N = B.rows;
     const int32_t k_begin = (int32_t)blockIdx.y * per_split, k_end = k_begin + per_split < nkb ? k_begin + per_split : nkb;
     const auto a_tile = tile_buffer(A.q + (int64_t)m0 * A.ld), b_tile = tile_buffer(B.q + (int64_t)n0 * B.ld);
-    uint32_t a_at[MT], b_at[NT];
+    uint32_t a_at[kLoadsA], b_at[kLoadsB];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) a_at[i] = lds_source((wave * MT + i) * 8, lane, A.rows - m0, A.ld);
+    for (int i = 0; i < kLoadsA; ++i) a_at[i] = lds_source((wave * kLoadsA + i) * 8, lane, A.rows - m0, A.ld);
 #pragma unroll
-    for (int i = 0; i < NT; ++i) b_at[i] = lds_source((wave * NT + i) * 8, lane, N - n0, B.ld);
+    for (int i = 0; i < kLoadsB; ++i) b_at[i] = lds_source((wave * kLoadsB + i) * 8, lane, N - n0, B.ld);
     auto fetch = [&](int32_t kb) {
         const uint32_t k = (uint32_t)kb * 128;
         uint8_t *stage = lds + (kb & 1) * kStage;
 #pragma unroll
-        for (int i = 0; i < MT; ++i) to_lds(a_tile, a_at[i], k, stage + (wave * MT + i) * 1024);
+        for (int i = 0; i < kLoadsA; ++i)
+            if (BM % 32 == 0 || wave * kLoadsA + i < BM / 8) to_lds(a_tile, a_at[i], k, stage + (wave * kLoadsA + i) * 1024);
 #pragma unroll
-        for (int i = 0; i < NT; ++i) to_lds(b_tile, b_at[i], k, stage + BM * 128 + (wave * NT + i) * 1024);
+        for (int i = 0; i < kLoadsB; ++i) to_lds(b_tile, b_at[i], k, stage + BM * 128 + (wave * kLoadsB + i) * 1024);
     };
     f32x4_t acc[MT][NT];
 #pragma unroll
@@ -947,10 +949,20 @@ Plan plan_product(int64_t M, int64_t N, int64_t nkb, bool exact)
     // Short sums over many tiles: 65,536 x 1,024 x 512 53.9 us (tiles one by one: 57.2), with K = 128 30.8 (35.9),
     // 262,144 x 1,024 x 512 to 8 bits 210 (277), but 32,768 x 1,024 x 512 33.6 (31.0) and 8,192 13.5 (11.4).
     if (!exact && nkb <= 4 && tiles_of(kBM, kBN) >= 12 * cus) return plan(Way::rows, 1, 4, 0, kBM);
-    // Lower tiles in fp32, where there would be fewer than two workgroups a compute unit and K is too short to
-    // split instead: 4,099 x 1,000 x 2,500 41 us (128 rows: 46), 1,024 x 1,024 x 1,024 13 (15); with 65,536 of K
-    // 512 x 1,024 takes 89 (78).
-    const int32_t bm = exact && nkb < 64 && tiles_of(kBM, kBN) < 2 * cus ? 64 : kBM;
+    // Heights in fp32, where K is too short to split instead: the rows that the busiest compute unit gets, a tenth
+    // and a fifth more work to a row in the lower ones (8,192 x 8,192 x 2,048: 128 rows 272 us, 64 304, 48 333), and
+    // a workgroup alone has no other to hide its waits.  4,099 x 1,000 x 2,500: 43.9, 39.5 and 34.6 us; 4,096 x
+    // 1,024 x 4,096: 47.0, 43.2, 47.5; 8,192 x 1,000 x 2,500: 45.7, 49.8, 58.5; 1,024 x 1,024 x 1,024: 15.1, 10.1,
+    // 8.7; 512 x 1,024 x 65,536, split: 75.5, 80.8, 99.0.
+    int32_t bm = kBM;
+    if (exact && nkb < 64) {
+        auto cost = [&](int64_t m) {
+            const int64_t each = (tiles_of(m, kBN) + cus - 1) / cus;
+            return (each > 1 ? 4 * each : 5) * m * (m == 128 ? 10 : m == 64 ? 11 : 12);
+        };
+        for (const int32_t m : {64, 48})
+            if (cost(m) < cost(bm)) bm = m;
+    }
     // K in parts, two workgroups a compute unit, eight blocks at least: 1,024 x 1,024 x 8,192 26 us (whole: 77),
     // 100 x 4,096 x 4,096 15.5 (25; parts of four blocks 17.4), 64 x 16,384 x 16,384 54 (one workgroup: 78);
     // 1,024 x 1,024 x 1,024 in fp32 10.6 whole and 12.9 in two.
@@ -1020,17 +1032,16 @@ void launch_tiles(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const Plan &p, con
         }
     }
     if constexpr (EXACT) {
-        // tiles of 64 rows where those of 128 would not give every compute unit two
-        const bool low = p.bm == 64;
-        const dim3 grid((unsigned)((B.rows + 127) / 128 * ((A.rows + p.bm - 1) / p.bm)), (unsigned)p.splits);
+        const dim3 grid((unsigned)((B.rows + kBN - 1) / kBN * ((A.rows + p.bm - 1) / p.bm)), (unsigned)p.splits);
         auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, operand(A), operand(B), nkb, p.per_split, o); };
-        if (A.format == HWSEL_FP8_E4M3) {
-            if (low) go(k_product_exact<2, 4, 0, KIND>);
-            else go(k_product_exact<4, 4, 0, KIND>);
-        } else {
-            if (low) go(k_product_exact<2, 4, 1, KIND>);
-            else go(k_product_exact<4, 4, 1, KIND>);
-        }
+        auto by_rows = [&](auto fa) {
+            constexpr int FA = decltype(fa)::value;
+            if (p.bm == 48) go(k_product_exact<1, 3, FA, KIND>);
+            else if (p.bm == 64) go(k_product_exact<1, 4, FA, KIND>);
+            else go(k_product_exact<2, 4, FA, KIND>);
+        };
+        if (A.format == HWSEL_FP8_E4M3) by_rows(std::integral_constant<int, 0>{});
+        else by_rows(std::integral_constant<int, 1>{});
     } else {
         const dim3 grid((unsigned)((B.rows + kBN - 1) / kBN * ((A.rows + kBM - 1) / kBM)), (unsigned)p.splits);
         auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, operand(A), operand(B), nkb, p.per_split, o); };
