@@ -350,21 +350,19 @@ __device__ __forceinline__ void tile_of(int32_t b, int32_t m_tiles, int32_t n_ti
     nt = in / rows;
 }
 
-// WM x WN waves, each MT x 8 tiles of 16 x 16 (128 columns: a whole block of
-// the next layer's operand).  Two LDS stages: the next block of K is on its
-// way while one is multiplied.
-template <int WM, int WN, int MT, int FA, OutKind KIND>
-__global__ __launch_bounds__(64 * WM * WN, 2) void k_product(Operand A, Operand B, int32_t nkb, int32_t per_split, Out o)
+// Four waves, each MT x 8 tiles of 16 x 16: 128 columns, a whole block of the
+// next layer's operand.  Two LDS stages: the next block of K is on its way while
+// one is multiplied.  (Three and four stages, eight waves or two: no faster
+// anywhere from 300 x 300 x 2,000 to 8,192 x 1,024 x 1,024.)
+template <int MT, int FA, OutKind KIND>
+__global__ __launch_bounds__(256, 2) void k_product(Operand A, Operand B, int32_t nkb, int32_t per_split, Out o)
 {
-    constexpr int NT = 8, BM = WM * MT * 16, BN = WN * 128, kWaves = WM * WN;
-    constexpr int kLoadsA = BM / 8 / kWaves, kLoadsB = BN / 8 / kWaves;
-    static_assert(BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0, "loads per wave");
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[2][(BM + BN) * 128];
+    constexpr int NT = 8, BM = 64 * MT, kStage = (BM + 128) * 128, kLoadsA = BM / 8 / 4, kLoadsB = 4;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kStage];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = wave % WM, wn = wave / WM;
     int32_t m_tile, n_tile;
-    tile_of(blockIdx.x, (A.rows + BM - 1) / BM, (B.rows + BN - 1) / BN, m_tile, n_tile);
-    const int32_t m0 = m_tile * BM, n0 = n_tile * BN;
+    tile_of(blockIdx.x, (A.rows + BM - 1) / BM, (B.rows + 127) / 128, m_tile, n_tile);
+    const int32_t m0 = m_tile * BM, n0 = n_tile * 128;
     const int32_t k_begin = (int32_t)blockIdx.y * per_split, k_end = k_begin + per_split < nkb ? k_begin + per_split : nkb;
     const auto a_tile = tile_buffer(A.q + (int64_t)m0 * A.ld), b_tile = tile_buffer(B.q + (int64_t)n0 * B.ld);
     uint32_t a_at[kLoadsA], b_at[kLoadsB];
@@ -372,55 +370,56 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_product(Operand A, Operand 
     for (int i = 0; i < kLoadsA; ++i) a_at[i] = lds_source((wave * kLoadsA + i) * 8, lane, A.rows - m0, A.ld);
 #pragma unroll
     for (int i = 0; i < kLoadsB; ++i) b_at[i] = lds_source((wave * kLoadsB + i) * 8, lane, B.rows - n0, B.ld);
-    auto fetch = [&](int32_t kb, uint8_t *stage) {
+    auto fetch = [&](int32_t kb) {
         const uint32_t k = (uint32_t)kb * 128;
+        uint8_t *stage = lds + (kb & 1) * kStage;
 #pragma unroll
         for (int i = 0; i < kLoadsA; ++i) to_lds(a_tile, a_at[i], k, stage + (wave * kLoadsA + i) * 1024);
 #pragma unroll
         for (int i = 0; i < kLoadsB; ++i) to_lds(b_tile, b_at[i], k, stage + BM * 128 + (wave * kLoadsB + i) * 1024);
     };
-    f32x4_t acc[MT][NT];
-    start_tiles<MT, KIND>(acc, n0 + wn * 128, B.rows, o, lane);
-    uint32_t sa[MT], sb[NT];
-    const int32_t row_a = m0 + wm * MT * 16 + (lane & 15), row_b = n0 + wn * 128 + (lane & 15);
-    auto scales = [&](int32_t kb) {
+    const int32_t row_a = m0 + wave * MT * 16 + (lane & 15), row_b = n0 + (lane & 15);
+    uint32_t sa[MT], sb[NT], sa_next[MT], sb_next[NT];
+    auto scales = [&](int32_t kb) {                         // (of the last blocks again past the end)
+        kb = kb < nkb ? kb : nkb - 1;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) sa[mt] = scale_word(A, row_a + 16 * mt, kb);
+        for (int mt = 0; mt < MT; ++mt) sa_next[mt] = scale_word(A, row_a + 16 * mt, kb);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) sb[nt] = scale_word(B, row_b + 16 * nt, kb);
+        for (int nt = 0; nt < NT; ++nt) sb_next[nt] = scale_word(B, row_b + 16 * nt, kb);
     };
-    fetch(k_begin, lds[k_begin & 1]);
+    fetch(k_begin);
     scales(k_begin);
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) sa[mt] >>= 8 * (k_begin & 3);
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) sb[nt] >>= 8 * (k_begin & 3);
+    f32x4_t acc[MT][NT];
+    start_tiles<MT, KIND>(acc, n0, B.rows, o, lane);
     for (int32_t kb = k_begin; kb < k_end; ++kb) {
+        if (((kb - k_begin) & 3) == 0) {                    // (splits start at multiples of four blocks)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) sa[mt] = sa_next[mt];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) sb[nt] = sb_next[nt];
+        }
         __builtin_amdgcn_s_waitcnt(0x0f70);                 // vmcnt(0): the barrier alone does not wait for loads to LDS
         __syncthreads();                                    // this stage has come; the other one is read
-        const uint8_t *stage = lds[kb & 1];
-        i32x8_t a[MT], b[NT];
+        if (kb + 1 < k_end) fetch(kb + 1);
+        if (((kb - k_begin) & 3) == 0) scales(kb + 4);
+        const uint8_t *stage = lds + (kb & 1) * kStage;
+        i32x8_t a[MT];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) a[mt] = fragment(stage + (wm * MT + mt) * 2048, lane);
+        for (int mt = 0; mt < MT; ++mt) a[mt] = fragment(stage + (wave * MT + mt) * 2048, lane);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) b[nt] = fragment(stage + BM * 128 + (wn * NT + nt) * 2048, lane);
-        if (kb + 1 < k_end) fetch(kb + 1, lds[(kb + 1) & 1]);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt) {
+            const i32x8_t b = fragment(stage + BM * 128 + nt * 2048, lane);
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
-                acc[mt][nt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[nt], a[mt], acc[mt][nt], 0, FA, 0, (int)sb[nt],
-                                                                              0, (int)sa[mt]);
-        if ((kb & 3) == 3) {
-            if (kb + 1 < k_end) scales(kb + 1);
-        } else {
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) sa[mt] >>= 8;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) sb[nt] >>= 8;
+                acc[mt][nt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a[mt], acc[mt][nt], 0, FA, 0, (int)sb[nt], 0,
+                                                                              (int)sa[mt]);
         }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) sa[mt] >>= 8;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) sb[nt] >>= 8;
     }
-    finish_tiles<MT, KIND>(acc, m0 + wm * MT * 16, n0 + wn * 128, A.rows, B.rows, (int32_t)blockIdx.y, o, lane);
+    finish_tiles<MT, KIND>(acc, m0 + wave * MT * 16, n0, A.rows, B.rows, (int32_t)blockIdx.y, o, lane);
 }
 
 // 256 x 256 tiles by eight waves in two groups, a wave of each on every SIMD.
@@ -949,12 +948,14 @@ Plan plan_product(int64_t M, int64_t N, int64_t nkb, bool exact)
     // Short sums over many tiles: 65,536 x 1,024 x 512 53.9 us (tiles one by one: 57.2), with K = 128 30.8 (35.9),
     // 262,144 x 1,024 x 512 to 8 bits 210 (277), but 32,768 x 1,024 x 512 33.6 (31.0) and 8,192 13.5 (11.4).
     if (!exact && nkb <= 4 && tiles_of(kBM, kBN) >= 12 * cus) return plan(Way::rows, 1, 4, 0, kBM);
+    // Lower tiles where there are no more than compute units: 1,024 x 1,024 x 1,024 6.7 us (128 rows: 8.3), 2,048 x
+    // 2,048 x 4,096 26 (32), 512 x 8,192 x 8,192 46 (49), but 8,192 x 1,024 x 1,024 18.7 (15.4).
+    int32_t bm = !exact && tiles_of(kBM, kBN) <= cus ? 64 : kBM;
     // Heights in fp32, where K is too short to split instead: the rows that the busiest compute unit gets, a tenth
     // and a fifth more work to a row in the lower ones (8,192 x 8,192 x 2,048: 128 rows 272 us, 64 304, 48 333), and
     // a workgroup alone has no other to hide its waits.  4,099 x 1,000 x 2,500: 43.9, 39.5 and 34.6 us; 4,096 x
     // 1,024 x 4,096: 47.0, 43.2, 47.5; 8,192 x 1,000 x 2,500: 45.7, 49.8, 58.5; 1,024 x 1,024 x 1,024: 15.1, 10.1,
     // 8.7; 512 x 1,024 x 65,536, split: 75.5, 80.8, 99.0.
-    int32_t bm = kBM;
     if (exact && nkb < 64) {
         auto cost = [&](int64_t m) {
             const int64_t each = (tiles_of(m, kBN) + cus - 1) / cus;
@@ -1031,9 +1032,9 @@ void launch_tiles(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const Plan &p, con
             return;
         }
     }
+    const dim3 grid((unsigned)((B.rows + kBN - 1) / kBN * ((A.rows + p.bm - 1) / p.bm)), (unsigned)p.splits);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, operand(A), operand(B), nkb, p.per_split, o); };
     if constexpr (EXACT) {
-        const dim3 grid((unsigned)((B.rows + kBN - 1) / kBN * ((A.rows + p.bm - 1) / p.bm)), (unsigned)p.splits);
-        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, operand(A), operand(B), nkb, p.per_split, o); };
         auto by_rows = [&](auto fa) {
             constexpr int FA = decltype(fa)::value;
             if (p.bm == 48) go(k_product_exact<1, 3, FA, KIND>);
@@ -1042,11 +1043,12 @@ void launch_tiles(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const Plan &p, con
         };
         if (A.format == HWSEL_FP8_E4M3) by_rows(std::integral_constant<int, 0>{});
         else by_rows(std::integral_constant<int, 1>{});
+    } else if (A.format == HWSEL_FP8_E4M3) {
+        if (p.bm == 64) go(k_product<1, 0, KIND>);
+        else go(k_product<2, 0, KIND>);
     } else {
-        const dim3 grid((unsigned)((B.rows + kBN - 1) / kBN * ((A.rows + kBM - 1) / kBM)), (unsigned)p.splits);
-        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, operand(A), operand(B), nkb, p.per_split, o); };
-        if (A.format == HWSEL_FP8_E4M3) go(k_product<4, 1, 2, 0, KIND>);
-        else go(k_product<4, 1, 2, 1, KIND>);
+        if (p.bm == 64) go(k_product<1, 1, KIND>);
+        else go(k_product<2, 1, KIND>);
     }
 }
 
