@@ -51,7 +51,8 @@ __device__ __forceinline__ float exponent_of(const Problem &q, float s)
 // is: above 2^31 they are multiples of 2^8).
 __device__ __forceinline__ uint32_t weight32(float t)
 {
-    const float n = rintf(t), f = t - n;
+    // 1.5 2^23 + 32: the sum is rounded to a whole number, n + 32 in its low bits
+    const float shifted = t + 12582944.0f, f = t - (shifted - 12582944.0f);
     float p = 1.5403530e-04f;                               // ln(2)^i / i!, i = 6 .. 0
     p = p * f + 1.3333558e-03f;
     p = p * f + 9.6181291e-03f;
@@ -59,8 +60,10 @@ __device__ __forceinline__ uint32_t weight32(float t)
     p = p * f + 2.4022651e-01f;
     p = p * f + 6.9314718e-01f;
     p = p * f + 1.0f;
-    const float w = __builtin_amdgcn_ldexpf(p, (int)n + 32);
-    return w < 4294967296.0f ? (uint32_t)w : 0xffffffffu;
+    const float v = __uint_as_float((__float_as_uint(shifted) << 23) + __float_as_uint(p));  // p 2^(n + 32)
+    uint32_t w;
+    asm("v_cvt_u32_f32 %0, %1" : "=v"(w) : "v"(v));         // (saturates; in C++ 2^32 would be undefined)
+    return w;
 }
 
 __device__ __forceinline__ uint64_t whole(uint32_t w) { return (uint64_t)w + (w == 0xffffffffu); }
@@ -144,7 +147,7 @@ constexpr int kParts = 256;                                 // sums of consecuti
 
 template <int NT, int BINS, int CACHED>
 struct Lds {
-    static constexpr int kList = BINS / 2;                  // scores around a bin that are ranked at once
+    static constexpr int kList = BINS * 3 / 8;              // scores around a bin that are ranked at once
     // Running sums after each lane's four candidates of a step, once the bins are done with.
     static constexpr int kFine = (BINS * 12 + kList * 16) / 8 / 64 * 64;
     uint32_t cache[CACHED];
@@ -155,9 +158,12 @@ struct Lds {
         };
         uint64_t fine[kFine];
     };
-    uint64_t part[kParts + 1];
+    union {                                                 // (the cut is found before parts are summed)
+        uint64_t part[kParts + 1];
+        uint32_t near[kList];
+    };
     uint64_t wave_mass[NT / 64], cut, found_mass;
-    uint32_t near[kList], wave_count[NT / 64], found_count, found_bin, n_near;
+    uint32_t wave_count[NT / 64], found_count, found_bin, n_near;
     float wave_best[NT / 64], wave_least[NT / 64];
 };
 
@@ -508,8 +514,9 @@ __device__ __forceinline__ void draw_in(const Problem &q, const Cut &cut, uint64
     }
 }
 
-template <int NT, int BINS, int CACHED>
-__global__ __launch_bounds__(NT) void k_sample(const float *__restrict__ scores, int64_t R,
+// WAVES: of a SIMD.
+template <int NT, int BINS, int CACHED, int WAVES>
+__global__ __launch_bounds__(NT, WAVES) void k_sample(const float *__restrict__ scores, int64_t R,
                                                const int64_t *__restrict__ seg, Settings set,
                                                const float *__restrict__ u, int32_t *__restrict__ idx,
                                                float *__restrict__ prob, int32_t *__restrict__ kept_out)
@@ -602,7 +609,6 @@ __global__ __launch_bounds__(NT) void k_sample(const float *__restrict__ scores,
             }
             return w;
         };
-#pragma unroll 2
         for (int32_t i = 0; i < cached; ++i) *slot(i) = weigh(__builtin_bit_cast(f32x4u_t, *slot(i)));
         each_step(q.s, walk, cached, walk.steps, [&](int32_t, const f32x4u_t &t) { weigh(t); });
         __syncthreads();
@@ -689,43 +695,49 @@ __global__ __launch_bounds__(NT) void k_sample(const float *__restrict__ scores,
     // many draws of a problem that is all in LDS: running sums for every lane and step
     const bool fine = set.n_draws > kWaves && walk.steps <= cached && walk.steps * NT <= Lds<NT, BINS, CACHED>::kFine;
     __syncthreads();                                        // (the bins are read)
-#pragma unroll 1
-    for (int e = 0; e < walk.per_wave; ++e) {
-        const int32_t first = e * walk.each, last = first + walk.each < walk.steps ? first + walk.each : walk.steps;
-        uint64_t sum = 0;
-        int32_t i = first;
-        for (; i < last && i < cached; ++i) {
-            u32x4_t w = *slot(i);
-            uint64_t four = 0;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                bool in = w[c] >= floor32 && w[c] >= near_lo;
-                if (w[c] >= near_lo && w[c] <= near_hi) {
-                    const int32_t at = walk.base + i * 256 + lane * 4 + c;
-                    in = in && at < q.n && within(cut, key_of(q.s[at < q.n ? at : 0]), at);
-                }
-                w[c] = in ? w[c] : 0;
-                four += whole(w[c]);
-                kept += in;
-            }
-            sum += four;
-            if (fine) {                                     // (a part is a step: at most kParts of them fit)
-                *slot(i) = w;
-                lds.fine[i * NT + threadIdx.x] = wave_scan52(four);
-            }
-        }
-        each_step(q.s, walk, i, last, [&](int32_t at, const f32x4u_t &t) {
-            uint64_t w[4];
-            kept_weights(q, cut, lim.least, t, walk.base + at * 256 + lane * 4, w);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                sum += w[c];
-                kept += w[c] != 0;
-            }
-        });
+    uint64_t sum = 0;
+    int32_t part = wave * walk.per_wave, left = walk.each;  // the part that is summed, its steps to come
+    auto stepped = [&](int32_t i) {
+        if (--left > 0 && i + 1 < walk.steps) return;
         sum = wave_sum(sum);
-        if (lane == 0) lds.part[wave * walk.per_wave + e] = sum;
+        if (lane == 0) lds.part[part] = sum;
+        ++part;
+        left = walk.each;
+        sum = 0;
+    };
+#pragma unroll 1
+    for (int32_t i = 0; i < cached; ++i) {
+        u32x4_t w = *slot(i);
+        uint64_t four = 0;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            bool in = w[c] >= floor32 && w[c] >= near_lo;
+            if (w[c] >= near_lo && w[c] <= near_hi) {
+                const int32_t at = walk.base + i * 256 + lane * 4 + c;
+                in = in && at < q.n && within(cut, key_of(q.s[at < q.n ? at : 0]), at);
+            }
+            w[c] = in ? w[c] : 0;
+            four += whole(w[c]);
+            kept += in;
+        }
+        sum += four;
+        if (fine) {                                         // (a part is a step: at most kParts of them fit)
+            *slot(i) = w;
+            lds.fine[i * NT + threadIdx.x] = wave_scan52(four);
+        }
+        stepped(i);
     }
+    each_step(q.s, walk, cached, walk.steps, [&](int32_t i, const f32x4u_t &t) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const uint32_t w = weight32(exponent_of(q, t[c]));
+            bool in = w >= floor32 && w >= near_lo;
+            if (w >= near_lo && w <= near_hi) in = in && within(cut, key_of(t[c]), walk.base + i * 256 + lane * 4 + c);
+            sum += in ? whole(w) : 0;
+            kept += in;
+        }
+        stepped(i);
+    });
     kept = wave_sum(kept);
     if (lane == 0) lds.wave_count[wave] = kept;
     __syncthreads();
@@ -779,8 +791,8 @@ __global__ __launch_bounds__(NT) void k_sample(const float *__restrict__ scores,
 // passes that hand their results on in the workspace: best score; histogram;
 // candidates around the cut, ranked by one workgroup (once for top-k, once for
 // top-p); sums of parts; draws.  A compute unit takes in some 100 GB/s, so 3
-// problems of 534,600 took 339 us in a workgroup each, 73 so.
-constexpr int kWide = 1024, kWideBins = 4096, kWideNear = 2048, kWideParts = 1024;
+// problems of 534,600 take 881 us in a workgroup each, 70 so.
+constexpr int kWide = 1024, kWideBins = 4096, kWideNear = 1536, kWideParts = 1024;
 
 struct WideState {
     uint32_t best, least, alive, bin, before_count, n_near;
@@ -1101,9 +1113,9 @@ __global__ __launch_bounds__(kWide) void k_wide_draw(WideArgs a, const float *__
 
 // Segment lengths are not known here; their mean is.  Few problems of many
 // candidates are shared by workgroups, which costs eleven launches: 8 problems
-// of 49,152 38 us (a workgroup each: 44), 8 of 32,768 38 (32); 64 of 131,072 70
-// (98), 64 of 65,536 62 (56); 128 of 262,144 159 (187), 128 of 65,536 69 (57).
-static bool shared_problems(int64_t R, int32_t P) { return P <= 128 && R / P > 40960 + 768 * (int64_t)P; }
+// of 49,152 38 us (a workgroup each: 40), 8 of 32,768 35 (30); 64 of 131,072 74
+// (83), 64 of 65,536 65 (50); 128 of 262,144 157 (163), 128 of 131,072 101 (92).
+static bool shared_problems(int64_t R, int32_t P) { return P <= 128 && R / P > 36864 + 1280 * (int64_t)P; }
 
 size_t sample_workspace_bytes(int64_t R, int32_t P, int32_t)
 {
@@ -1130,7 +1142,7 @@ static void launch_shared(const WideArgs &a, int32_t P, const float *u, int32_t 
     hipLaunchKernelGGL(k_wide_draw, one, block, 0, s, a, u, idx, prob, kept);
 }
 
-template <int NT, int BINS, int CACHED>
+template <int NT, int BINS, int CACHED, int WAVES>
 static void launch_problems(const float *scores, int64_t R, const int64_t *seg, int32_t P, const hwsel_sampling_t &how,
                             const float *u, int32_t n_draws, int32_t *idx, float *prob, int32_t *kept, hipStream_t s)
 {
@@ -1141,7 +1153,7 @@ static void launch_problems(const float *scores, int64_t R, const int64_t *seg, 
         if (h.top_p_of) h.top_p_of += p0;
         if (h.min_p_of) h.min_p_of += p0;
         const int64_t o = (int64_t)p0 * n_draws;
-        hipLaunchKernelGGL((k_sample<NT, BINS, CACHED>), dim3(n), dim3(NT), 0, s, scores, R, seg + p0, Settings{h, n_draws}, u + o,
+        hipLaunchKernelGGL((k_sample<NT, BINS, CACHED, WAVES>), dim3(n), dim3(NT), 0, s, scores, R, seg + p0, Settings{h, n_draws}, u + o,
                            idx + o, prob ? prob + o : nullptr, kept ? kept + p0 : nullptr);
     });
 }
@@ -1151,11 +1163,13 @@ hipError_t launch_sample(const float *scores, int64_t R, const int64_t *seg, int
 {
     if (shared_problems(R, P))
         launch_shared(WideArgs{scores, R, seg, static_cast<WideState *>(ws), Settings{how, n_draws}}, P, u, idx, prob, kept, s);
-    // Two workgroups of 512 threads a compute unit wait less than one of 1,024, which keeps three times as many
-    // candidates in LDS: 600 problems of 8,192 29 us (51), 600 of 24,576 70 (79), 128 of 8,192 15 (18), 8 of
-    // 12,288 19.8 (20.6), but 256 of 24,576 32 (27).
-    else if (R / P <= 12288 || P > compute_units()) launch_problems<512, 1024, 8192>(scores, R, seg, P, how, u, n_draws, idx, prob, kept, s);
-    else launch_problems<1024, 2048, 24576>(scores, R, seg, P, how, u, n_draws, idx, prob, kept, s);
+    // Where problems outnumber compute units, three workgroups of 512 threads share one, in 80 registers; up to
+    // 8,192 candidates otherwise, 512 threads wait for each other less than 1,024, which keep three times as many
+    // candidates in LDS.  600 problems of 8,192 27 us (1,024 threads: 49), 600 of 24,576 56 (75), 300 of 65,536 99
+    // (108); 128 of 8,192 16.8 (17.6), but 8 of 12,288 21.2 (19.4) and 256 of 24,576 33 (26).
+    else if (P > compute_units()) launch_problems<512, 1024, 8192, 6>(scores, R, seg, P, how, u, n_draws, idx, prob, kept, s);
+    else if (R / P <= 8192) launch_problems<512, 1024, 8192, 4>(scores, R, seg, P, how, u, n_draws, idx, prob, kept, s);
+    else launch_problems<1024, 2048, 24576, 4>(scores, R, seg, P, how, u, n_draws, idx, prob, kept, s);
     return hipGetLastError();
 }
 
