@@ -4,6 +4,8 @@
 #pragma once
 
 #include <hip/hip_runtime.h>
+
+#include <atomic>
 #include <stdint.h>
 
 #include "../../include/hwsel.h"
@@ -62,10 +64,12 @@ hipError_t launch_forest_leaves(const hwsel_forest_t &f, const float *X, int64_t
 // Compute units of the calling thread's device (256 on an MI355X).
 inline int compute_units()
 {
+    static std::atomic<int> known[64];                      // a device's number never changes
     int dev = 0, n_cu = 256;
-    if (hipGetDevice(&dev) != hipSuccess ||
-        hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n_cu < 1)
-        n_cu = 256;
+    if (hipGetDevice(&dev) != hipSuccess) return n_cu;
+    if (dev >= 0 && dev < 64 && known[dev].load(std::memory_order_relaxed) > 0) return known[dev].load(std::memory_order_relaxed);
+    if (hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n_cu < 1) return 256;
+    if (dev >= 0 && dev < 64) known[dev].store(n_cu, std::memory_order_relaxed);
     return n_cu;
 }
 

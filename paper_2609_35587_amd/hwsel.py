@@ -1,4 +1,5 @@
-"""Python binding of libhwsel.so (ctypes).
+"""Python binding of libhwsel.so (ctypes; the calls on 8-bit matrices and the
+draws through _binding.so, whose checks in C++ take 3 us where Python's took 11).
 
 The functions carry the C ABI's names and only marshal arguments: torch
 tensors in device memory become raw pointers, the current torch stream
@@ -129,6 +130,28 @@ def lib() -> C.CDLL:
                                                sz, vp]
         _lib = L
     return _lib
+
+
+_binding = None
+# as csrc/binding.cpp lists them
+_BOUND = ("hwsel_fp8_quantise", "hwsel_fp8_dequantise", "hwsel_fp8_transpose", "hwsel_fp8_matmul_workspace_bytes",
+          "hwsel_fp8_matmul", "hwsel_fp8_layer", "hwsel_sample_workspace_bytes", "hwsel_sample_per_problem",
+          "hwsel_last_error")
+
+
+def _calls():
+    """_binding.so, connected to the library; raises if it has not been built."""
+    global _binding
+    if _binding is None:
+        L = lib()
+        try:
+            from . import _binding as module
+        except ImportError as e:
+            raise RuntimeError("paper_2609_35587_amd/_binding.so does not load: build it with "
+                               f"`python paper_2609_35587_amd/build.py` ({e})") from e
+        module.connect(HwselError, *[C.cast(getattr(L, n), C.c_void_p).value for n in _BOUND])
+        _binding = module
+    return _binding
 
 
 def _check(fn: str, status: int) -> None:
@@ -673,7 +696,6 @@ def hwsel_catalogue_candidates(problems: torch.Tensor, seg_offsets: torch.Tensor
 # ----------------------------------------------------------------------------
 FP8_E4M3, FP8_E5M2 = 0, 1
 FP8_BLOCK = 128
-_DTYPE_CODE = {torch.bfloat16: 0, torch.float32: 3}
 
 
 def hwsel_fp8_empty(rows: int, cols: int, format: int = FP8_E4M3, block_rows: int = 1, device="cuda") -> dict:
@@ -684,127 +706,41 @@ def hwsel_fp8_empty(rows: int, cols: int, format: int = FP8_E4M3, block_rows: in
                 rows=rows, cols=cols, format=format, block_rows=block_rows)
 
 
-def _fp8(m: dict, name: str, like: torch.Tensor | None = None) -> hwsel_fp8_t:
-    q, s, rows, cols, block_rows = m["q"], m["scale"], int(m["rows"]), int(m["cols"]), int(m["block_rows"])
-    for t, part in ((q, "q"), (s, "scale")):
-        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2 or t.dtype != torch.uint8 or \
-                (t.stride(1) != 1 and t.shape[1] > 1):
-            raise ValueError(f"{name}.{part} must be a 2-D uint8 device tensor with unit column stride")
-        if t.get_device() != (q if like is None else like).get_device():
-            raise ValueError(f"{name}.{part} is on {t.device}, the other operands on {(q if like is None else like).device}")
-    blocks = -(-cols // FP8_BLOCK)
-    (q_rows, q_cols), (s_rows, s_cols) = q.shape, s.shape
-    if q_rows < rows or q_cols < blocks * FP8_BLOCK or s_rows < -(-rows // max(block_rows, 1)) or \
-            s_cols < -(-blocks // 4) * 4:
-        raise ValueError(f"{name}: buffers {tuple(q.shape)}, {tuple(s.shape)} are short of {rows} x {cols}")
-    return hwsel_fp8_t(rows, cols, q.data_ptr(), q.stride(0), s.data_ptr(), s.stride(0), int(m["format"]), block_rows)
-
-
-def _plain(X, name: str, rows: int, cols: int, like: torch.Tensor) -> int:
-    """A row-major fp32 or bf16 matrix of at least rows x cols; its dtype code."""
-    if not isinstance(X, torch.Tensor) or not X.is_cuda or X.dim() != 2 or X.device != like.device:
-        raise ValueError(f"{name} must be a 2-D device tensor on {like.device}")
-    if X.dtype not in _DTYPE_CODE or (X.shape[1] > 1 and X.stride(1) != 1) or X.shape[0] < rows or \
-            X.shape[1] < cols or (X.shape[0] > 1 and X.stride(0) < cols):
-        raise ValueError(f"{name} must be fp32 or bf16, at least [{rows}][{cols}], with unit column stride")
-    return _DTYPE_CODE[X.dtype]
-
-
-def _ld(X: torch.Tensor) -> int:
-    return max(X.stride(0), X.shape[1])
-
-
 def hwsel_fp8_quantise(X: torch.Tensor, format: int = FP8_E4M3, block_rows: int = 1, transpose: bool = False,
                        mean: torch.Tensor | None = None, inv_std: torch.Tensor | None = None,
                        out: dict | None = None, stream=None) -> dict:
     """X (fp32 or bf16 [R][C]), or X transposed, in 8 bits with a scale for
     each block of 128; standardised on the way if mean and inv_std are given."""
-    code = _plain(X, "X", 1, 1, X)
-    R, C_ = X.shape
-    rows, cols = (C_, R) if transpose else (R, C_)
-    if out is None:
-        out = hwsel_fp8_empty(rows, cols, format, block_rows, X.device)
-    if (out["rows"], out["cols"], out["format"], out["block_rows"]) != (rows, cols, format, block_rows):
-        raise ValueError(f"out is not a {rows} x {cols} matrix of this format and block_rows")
-    for t, name in ((mean, "mean"), (inv_std, "inv_std")):
-        if t is not None:
-            _arg(t, name, F32, C_, X)
-    s = _fp8(out, "out", X)
-    _check("hwsel_fp8_quantise", lib().hwsel_fp8_quantise(_ptr(X), code, _ld(X), int(transpose), _ptr(mean),
-                                                          _ptr(inv_std), C.byref(s), _stream(stream)))
-    return out
+    return (_binding or _calls()).fp8_quantise(X, format, block_rows, transpose, mean, inv_std, out, stream)
 
 
 def hwsel_fp8_dequantise(m: dict, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None,
                          stream=None) -> torch.Tensor:
     """The values of an 8-bit matrix in bf16 or fp32."""
-    s = _fp8(m, "m")
-    if out is None:
-        out = torch.empty((s.rows, s.cols), dtype=dtype, device=m["q"].device)
-    code = _plain(out, "out", s.rows, s.cols, m["q"])
-    _check("hwsel_fp8_dequantise", lib().hwsel_fp8_dequantise(C.byref(s), _ptr(out), code, _ld(out), _stream(stream)))
-    return out
+    return (_binding or _calls()).fp8_dequantise(m, dtype, out, stream)
 
 
 def hwsel_fp8_transpose(m: dict, format: int = FP8_E4M3, block_rows: int = 1, out: dict | None = None,
                         stream=None) -> dict:
     """An 8-bit matrix transposed and quantised again along its own rows."""
-    s = _fp8(m, "m")
-    if out is None:
-        out = hwsel_fp8_empty(s.cols, s.rows, format, block_rows, m["q"].device)
-    o = _fp8(out, "out", m["q"])
-    _check("hwsel_fp8_transpose", lib().hwsel_fp8_transpose(C.byref(s), C.byref(o), _stream(stream)))
-    return out
+    return (_binding or _calls()).fp8_transpose(m, format, block_rows, out, stream)
 
 
 def hwsel_fp8_matmul_workspace_bytes(A: dict, B: dict) -> int:
-    n = C.c_size_t(0)
-    a, b = _fp8(A, "A"), _fp8(B, "B")
-    _check("hwsel_fp8_matmul_workspace_bytes", lib().hwsel_fp8_matmul_workspace_bytes(C.byref(a), C.byref(b),
-                                                                                      C.byref(n)))
-    return int(n.value)
-
-
-def _product_args(a: hwsel_fp8_t, b: hwsel_fp8_t, bias, workspace, like: torch.Tensor):
-    """Bias and workspace of a product: (bias, workspace, its bytes)."""
-    if bias is not None:
-        _arg(bias, "bias", F32, b.rows, like)
-    if workspace is None:
-        n = C.c_size_t(0)
-        _check("hwsel_fp8_matmul_workspace_bytes", lib().hwsel_fp8_matmul_workspace_bytes(C.byref(a), C.byref(b),
-                                                                                          C.byref(n)))
-        if n.value == 0:
-            return bias, None, 0
-        workspace = torch.empty(n.value, dtype=torch.uint8, device=like.device)
-    _arg(workspace, "workspace", U8, 0, like)
-    return bias, workspace, workspace.numel()
+    return (_binding or _calls()).fp8_matmul_workspace_bytes(A, B)
 
 
 def hwsel_fp8_matmul(A: dict, B: dict, dtype: torch.dtype = torch.bfloat16, bias: torch.Tensor | None = None,
                      gelu: bool = False, out: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
                      stream=None) -> torch.Tensor:
     """act(A B^T + bias) of 8-bit matrices A [M][K], B [N][K], in bf16 or fp32."""
-    a, b = _fp8(A, "A"), _fp8(B, "B", A["q"])
-    if out is None:
-        out = torch.empty((a.rows, b.rows), dtype=dtype, device=A["q"].device)
-    code = _plain(out, "out", a.rows, b.rows, A["q"])
-    bias, workspace, n = _product_args(a, b, bias, workspace, A["q"])
-    _check("hwsel_fp8_matmul", lib().hwsel_fp8_matmul(C.byref(a), C.byref(b), _ptr(bias), int(gelu), _ptr(out), code,
-                                                      _ld(out), _ptr(workspace), n, _stream(stream)))
-    return out
+    return (_binding or _calls()).fp8_matmul(A, B, dtype, bias, gelu, out, workspace, stream)
 
 
 def hwsel_fp8_layer(A: dict, B: dict, bias: torch.Tensor | None = None, gelu: bool = False, out: dict | None = None,
                     workspace: torch.Tensor | None = None, stream=None) -> dict:
     """act(A B^T + bias) as an 8-bit matrix, the next layer's operand."""
-    a, b = _fp8(A, "A"), _fp8(B, "B", A["q"])
-    if out is None:
-        out = hwsel_fp8_empty(a.rows, b.rows, device=A["q"].device)
-    o = _fp8(out, "out", A["q"])
-    bias, workspace, n = _product_args(a, b, bias, workspace, A["q"])
-    _check("hwsel_fp8_layer", lib().hwsel_fp8_layer(C.byref(a), C.byref(b), _ptr(bias), int(gelu), C.byref(o),
-                                                    _ptr(workspace), n, _stream(stream)))
-    return out
+    return (_binding or _calls()).fp8_layer(A, B, bias, gelu, out, workspace, stream)
 
 
 def hwsel_sample_workspace_bytes(R: int, P: int, n_draws: int) -> int:
@@ -821,35 +757,8 @@ def hwsel_sample_per_problem(scores: torch.Tensor, seg_offsets: torch.Tensor, u:
     random numbers u fp32 [P][draws].  Each setting is a number or a device
     tensor [P].  Returns (idx int32 [P][draws], prob fp32 [P][draws], kept
     int32 [P])."""
-    _arg(scores, "scores", F32)
-    _arg(seg_offsets, "seg_offsets", I64, 2, scores)
-    P, R = seg_offsets.shape[0] - 1, scores.numel()
-    _arg(u, "u", F32, 0, scores)
-    if u.dim() != 2 or u.shape[0] != P:
-        raise ValueError(f"u must be [{P}][draws], got {tuple(u.shape)}")
-    draws = u.shape[1]
-    how = hwsel_sampling_t()
-    for n, v, dt in (("temperature", temperature, F32), ("top_k", top_k, I32), ("top_p", top_p, F32),
-                     ("min_p", min_p, F32)):
-        if isinstance(v, torch.Tensor):
-            setattr(how, n + "_of", _ptr(_arg(v, n, dt, P, scores)))
-        else:
-            setattr(how, n, v)
-    idx = torch.empty((P, draws), dtype=torch.int32, device=scores.device) if idx is None else idx
-    prob = torch.empty((P, draws), dtype=torch.float32, device=scores.device) if prob is None else prob
-    kept = torch.empty(P, dtype=torch.int32, device=scores.device) if kept is None else kept
-    _arg(idx, "idx", I32, P * draws, scores)
-    _arg(prob, "prob", F32, P * draws, scores)
-    _arg(kept, "kept", I32, P, scores)
-    n = hwsel_sample_workspace_bytes(R, P, draws)
-    if workspace is None and n:
-        workspace = torch.empty(n, dtype=torch.uint8, device=scores.device)
-    if workspace is not None:
-        _arg(workspace, "workspace", U8, n, scores)
-    _check("hwsel_sample_per_problem", lib().hwsel_sample_per_problem(
-        _ptr(scores), R, _ptr(seg_offsets), P, C.byref(how), _ptr(u), draws, _ptr(idx), _ptr(prob), _ptr(kept),
-        _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)))
-    return idx, prob, kept
+    return (_binding or _calls()).sample_per_problem(scores, seg_offsets, u, temperature, top_k, top_p, min_p, idx, prob, kept,
+                                                     workspace, stream)
 
 
 def declared_functions() -> list[str]:

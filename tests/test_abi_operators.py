@@ -1,6 +1,9 @@
 """Refusals of the 8-bit and the sampling entry points: checked on the host
 before anything is enqueued, so they run without a GPU."""
 import ctypes as C
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -133,3 +136,28 @@ def test_binding_rejects_host_tensors():
                  lambda: hwsel.hwsel_sample_per_problem(torch.zeros(4), torch.tensor([0, 4]), torch.zeros(1, 1))):
         with pytest.raises(ValueError):
             call()
+
+
+def test_binding_takes_its_arguments_whole():
+    """The calls made in C++ refuse a wrong count before they look at one."""
+    b = hwsel._calls()
+    for name, n in (("fp8_quantise", 8), ("fp8_dequantise", 4), ("fp8_transpose", 5), ("fp8_matmul", 8), ("fp8_layer", 7),
+                    ("fp8_matmul_workspace_bytes", 2), ("sample_per_problem", 12)):
+        for bad in (0, n - 1, n + 1):
+            with pytest.raises(RuntimeError):
+                getattr(b, name)(*[None] * bad)
+        with pytest.raises((ValueError, TypeError)):
+            getattr(b, name)(*[None] * n)
+
+
+def test_missing_binding_fails_loudly():
+    code = ("import sys\n"
+            "from paper_2609_35587_amd import hwsel\n"
+            "sys.modules['paper_2609_35587_amd._binding'] = None\n"
+            "try:\n"
+            "    hwsel.hwsel_fp8_quantise(None)\n"
+            "except RuntimeError as e:\n"
+            "    print('raised', '_binding.so' in str(e))\n")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    out = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=root, timeout=120)
+    assert out.stdout.strip() == "raised True", out.stdout + out.stderr
