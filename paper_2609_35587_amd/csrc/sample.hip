@@ -10,9 +10,10 @@
 // weights passes a point: sums of 256 candidates are kept, and the 256 that a
 // draw falls into are weighed again.
 //
-// A workgroup takes a problem; a wave has consecutive candidates of it, 256 a
-// step.  Scores are read once from HBM; as many as LDS has room for stay there,
-// first as scores, then as weights, the others are read and weighed again.
+// A workgroup takes a problem (a wave one of up to 1,024 candidates); a wave has
+// consecutive candidates of it, 256 a step.  Scores are read once from HBM; as
+// many as LDS has room for stay there, first as scores, then as weights, the
+// others are read and weighed again.
 // (Kept in registers instead, 64 a thread, the unrolled passes were 24,000
 // instructions with spills: 121 us for 256 problems of 65,536.)
 // Bound by latency for short segments, for long ones by some 60 instructions a
@@ -205,6 +206,15 @@ __device__ __forceinline__ uint64_t share_of(const Limits &lim, uint64_t mass)
 {
     const uint64_t need = (uint64_t)ceil((double)mass * (double)(lim.top_p > 0.0f ? lim.top_p : 0.0f));
     return need < 1 ? 1 : need;
+}
+
+// Problem p's candidates, its best score not known yet.
+__device__ __forceinline__ Problem problem_of(const float *scores, int64_t R, const int64_t *seg, int32_t p)
+{
+    int64_t lo = seg[p], hi = seg[p + 1];
+    lo = lo < 0 ? 0 : lo > R ? R : lo;
+    hi = hi < lo ? lo : hi > R ? R : hi;
+    return {scores + lo, (int32_t)(hi - lo), 0.0f, 1.0f};
 }
 
 // How a workgroup of NT threads goes through n candidates: a wave has `steps`
@@ -514,21 +524,17 @@ __device__ __forceinline__ void draw_in(const Problem &q, const Cut &cut, uint64
     }
 }
 
-// WAVES: of a SIMD.
-template <int NT, int BINS, int CACHED, int WAVES>
-__global__ __launch_bounds__(NT, WAVES) void k_sample(const float *__restrict__ scores, int64_t R,
-                                               const int64_t *__restrict__ seg, Settings set,
+// A workgroup's work on problem p.
+template <int NT, int BINS, int CACHED>
+__device__ __forceinline__ void sample_problem(Lds<NT, BINS, CACHED> &lds, int32_t p, const float *__restrict__ scores, int64_t R,
+                                               const int64_t *__restrict__ seg, const Settings &set,
                                                const float *__restrict__ u, int32_t *__restrict__ idx,
                                                float *__restrict__ prob, int32_t *__restrict__ kept_out)
 {
-    __shared__ Lds<NT, BINS, CACHED> lds;
     constexpr int kWaves = NT / 64;
     constexpr uint32_t kList = Lds<NT, BINS, CACHED>::kList;
-    const int32_t p = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    int64_t lo = seg[p], hi = seg[p + 1];
-    lo = lo < 0 ? 0 : lo > R ? R : lo;
-    hi = hi < lo ? lo : hi > R ? R : hi;
-    Problem q{scores + lo, (int32_t)(hi - lo), 0.0f, 1.0f};
+    const int32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Problem q = problem_of(scores, R, seg, p);
     u += (int64_t)p * set.n_draws;
     idx += (int64_t)p * set.n_draws;
     if (prob) prob += (int64_t)p * set.n_draws;
@@ -786,6 +792,340 @@ __global__ __launch_bounds__(NT, WAVES) void k_sample(const float *__restrict__ 
     }
 }
 
+// WAVES: of a SIMD.
+template <int NT, int BINS, int CACHED, int WAVES>
+__global__ __launch_bounds__(NT, WAVES) void k_sample(const float *__restrict__ scores, int64_t R,
+                                                      const int64_t *__restrict__ seg, Settings set,
+                                                      const float *__restrict__ u, int32_t *__restrict__ idx,
+                                                      float *__restrict__ prob, int32_t *__restrict__ kept_out)
+{
+    __shared__ Lds<NT, BINS, CACHED> lds;
+    sample_problem<NT, BINS, CACHED>(lds, blockIdx.x, scores, R, seg, set, u, idx, prob, kept_out);
+}
+
+// Up to 1,024 candidates: a wave has a problem to itself, its scores and
+// weights in registers, and waits for no other.  The steps are those above, the
+// histogram one of 256 bins; the candidates of a bin are compared all with all.
+constexpr int kSmall = 1024, kSmallBins = 256, kSmallList = 64;
+
+union SmallLds {                                            // a wave's
+    struct {
+        uint64_t mass[kSmallBins], list[kSmallList];
+        uint32_t count[kSmallBins];
+    };
+    struct {
+        uint64_t run[kSmall / 4];                           // running sums after each four candidates
+        uint32_t w[kSmall];
+    };
+};
+
+// What this wave has written to LDS is there for all its lanes.
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// The index of a lane's candidate e.
+__device__ __forceinline__ int32_t small_index(int lane, int e) { return (e >> 2) * 256 + lane * 4 + (e & 3); }
+
+// The candidate at which the count (by_mass: mass), best first, reaches `want`,
+// 1 <= want <= all of it; the mass up to there.
+template <int EACH>
+__device__ __forceinline__ Cut small_cut(const Problem &q, const float (&s)[EACH], const uint32_t (&w)[EACH],
+                                         float bin_scale, bool by_mass, uint64_t want, uint64_t &mass, SmallLds &lds)
+{
+    const int lane = threadIdx.x & 63;
+    uint64_t m[4], m_sum = 0;
+    uint32_t c[4], c_sum = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        m[j] = lds.mass[lane * 4 + j];
+        c[j] = lds.count[lane * 4 + j];
+        m_sum += m[j];
+        c_sum += c[j];
+    }
+    const uint64_t m_scan = wave_scan52(m_sum);
+    const uint32_t c_scan = wave_scan(c_sum);
+    uint64_t m_at = m_scan - m_sum;
+    uint32_t c_at = c_scan - c_sum;
+    const uint64_t from = by_mass ? m_at : (uint64_t)c_at, to = by_mass ? m_scan : (uint64_t)c_scan;
+    const int owner = __builtin_ctzll(__ballot(from < want && to >= want));
+    int j_at = 0;
+#pragma unroll
+    for (int j = 0; j < 3; ++j)
+        if (j_at == j && (by_mass ? m_at + m[j] : (uint64_t)(c_at + c[j])) < want) {
+            m_at += m[j];
+            c_at += c[j];
+            ++j_at;
+        }
+    const uint32_t bin = 4 * owner + (uint32_t)__builtin_amdgcn_readlane(j_at, owner);
+    const uint64_t before_mass = lane_u64(m_at, owner);
+    const uint32_t before_count = (uint32_t)__builtin_amdgcn_readlane((int)c_at, owner);
+
+    uint32_t in_bin = 0, members = 0;                       // members: bit e, this lane's candidate e
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        const bool in = w[e] != 0 && (uint32_t)(-exponent_of(q, s[e]) * bin_scale) == bin;
+        const uint64_t lanes = __ballot(in);
+        const uint32_t at = in_bin + __builtin_amdgcn_mbcnt_hi((uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, 0));
+        if (in && at < kSmallList) lds.list[at] = ((uint64_t)key_of(s[e]) << 32) | (0xffffffffu - (uint32_t)small_index(lane, e));
+        in_bin += (uint32_t)__popcll(lanes);
+        members |= (uint32_t)in << e;
+    }
+    if (in_bin <= kSmallList) {                             // a lane each
+        wave_sync();
+        const bool own = (uint32_t)lane < in_bin;
+        const uint64_t v = own ? lds.list[lane] : 0;
+        const uint64_t v_w = own ? whole(weight32(exponent_of(q, score_of((uint32_t)(v >> 32))))) : 0;
+        uint64_t mass_at = before_mass;
+        uint32_t count_at = before_count;
+        for (uint32_t o = 0; o < in_bin; ++o) {
+            const uint64_t other = lane_u64(v, (int)o), other_w = lane_u64(v_w, (int)o);
+            mass_at += other > v ? other_w : 0;
+            count_at += other > v;
+        }
+        const uint64_t at = by_mass ? mass_at : (uint64_t)count_at, with = by_mass ? mass_at + v_w : (uint64_t)count_at + 1;
+        const int at_lane = __builtin_ctzll(__ballot(own && at < want && with >= want));
+        const uint64_t cut = lane_u64(v, at_lane);
+        mass = lane_u64(mass_at + v_w, at_lane);
+        return {(uint32_t)(cut >> 32), (int32_t)(0xffffffffu - (uint32_t)cut)};
+    }
+    // Many in a bin (equal scores): the largest key from which on `want` is reached, by halving.
+    uint32_t hi = 0, lo = 0;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        const uint32_t key = members >> e & 1 ? key_of(s[e]) : 0;
+        hi = key > hi ? key : hi;
+        lo = key != 0 && ~key > lo ? ~key : lo;
+    }
+    hi = wave_max(hi);
+    lo = ~wave_max(lo);
+    auto from_key = [&](uint32_t key, uint64_t &n, uint64_t &sum) {        // of the bin, and of those before it
+        uint64_t lane_n = 0, lane_sum = 0;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const bool in = (members >> e & 1) && key_of(s[e]) >= key;
+            lane_n += in;
+            lane_sum += in ? whole(w[e]) : 0;
+        }
+        n = before_count + wave_sum((uint32_t)lane_n);
+        sum = before_mass + lane_u64(wave_scan52(lane_sum), 63);
+    };
+    uint64_t n, sum;
+#pragma unroll 1
+    while (lo < hi) {
+        const uint32_t mid = hi - (hi - lo) / 2;            // above lo
+        from_key(mid, n, sum);
+        if ((by_mass ? sum : n) >= want) lo = mid;
+        else hi = mid - 1;
+    }
+    from_key(lo + 1, n, sum);                               // (no key is 2^32 - 1: it would be a NaN's)
+    const uint64_t each = whole(weight32(exponent_of(q, score_of(lo))));
+    uint32_t left = (uint32_t)(by_mass ? (want - sum + each - 1) / each : want - n);       // of those with this key
+    mass = sum + left * each;
+    int32_t last = 0;
+    bool found = false;
+#pragma unroll
+    for (int i = 0; i < EACH / 4; ++i) {
+        uint32_t tied = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) tied += key_of(s[4 * i + e]) == lo;
+        const uint32_t scan = wave_scan(tied), here = (uint32_t)__builtin_amdgcn_readlane((int)scan, 63);
+        if (!found && left <= here) {
+            const int at_lane = __builtin_ctzll(__ballot(scan >= left));
+            uint32_t run = scan - tied;
+            int at = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                run += key_of(s[4 * i + e]) == lo;
+                at += run < left;
+            }
+            last = i * 256 + at_lane * 4 + __builtin_amdgcn_readlane(at, at_lane);
+            found = true;
+        }
+        left -= found ? 0 : here;
+    }
+    return {lo, last};
+}
+
+// EACH: candidates a lane.
+template <int EACH>
+__device__ __forceinline__ void sample_small(Problem q, int32_t p, const Settings &set, const float *__restrict__ u,
+                                             int32_t *__restrict__ idx, float *__restrict__ prob, int32_t *__restrict__ kept_out,
+                                             SmallLds &lds)
+{
+    const int lane = threadIdx.x & 63;
+    u += (int64_t)p * set.n_draws;
+    idx += (int64_t)p * set.n_draws;
+    if (prob) prob += (int64_t)p * set.n_draws;
+    float s[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH / 4; ++i) {
+        const int32_t at = i * 256 + lane * 4;
+        if (i * 256 + 256 <= q.n) {
+            const f32x4u_t t = *reinterpret_cast<const f32x4u_t *>(q.s + at);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) s[4 * i + c] = t[c];
+        } else {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) s[4 * i + c] = at + c < q.n ? q.s[at + c] : -__builtin_inff();
+        }
+    }
+    const float u_first = lane < set.n_draws ? u[lane] : 0.0f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        lds.mass[lane * 4 + j] = 0;
+        lds.count[lane * 4 + j] = 0;
+    }
+    float most = -__builtin_inff(), least_score = __builtin_inff();
+    uint32_t alive = 0;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        const bool in = takes_part(s[e]);
+        alive += (uint32_t)__popcll(__ballot(in));
+        most = fmaxf(most, s[e]);
+        least_score = fminf(least_score, in ? s[e] : __builtin_inff());
+    }
+    if (alive == 0) {
+        for (int32_t j = lane; j < set.n_draws; j += 64) {
+            idx[j] = -1;
+            if (prob) prob[j] = 0.0f;
+        }
+        if (lane == 0 && kept_out) kept_out[p] = 0;
+        return;
+    }
+    most = score_of(wave_max(order_key(most + 0.0f)));
+    least_score = -score_of(wave_max(order_key(0.0f - least_score)));
+    Limits lim;
+    read_settings(set, p, most, q, lim);
+    uint32_t w[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) w[e] = weight32(exponent_of(q, s[e]));
+
+    const bool by_count = lim.k < alive, by_mass = lim.top_p < 1.0f;
+    Cut cut{0, 0x7fffffff};
+    if (by_count || by_mass) {
+        const float t_least = -exponent_of(q, least_score), span = t_least < 34.0f ? t_least : 34.0f;
+        const float bin_scale = span > 0.0f ? fminf((float)(kSmallBins - 1) / span, 1e30f) : 1.0f;
+        uint32_t in_bins = 0;
+        uint64_t mass = 0;
+        wave_sync();
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            if (w[e] != 0) {
+                const uint32_t bin = (uint32_t)(-exponent_of(q, s[e]) * bin_scale);
+                atomicAdd((unsigned long long *)&lds.mass[bin], (unsigned long long)whole(w[e]));
+                atomicAdd(&lds.count[bin], 1u);
+                mass += whole(w[e]);
+            }
+            in_bins += (uint32_t)__popcll(__ballot(w[e] != 0));
+        }
+        wave_sync();
+        mass = lane_u64(wave_scan52(mass), 63);
+        // first the k best, then the share of their mass
+#pragma unroll 1
+        for (int turn = by_count && lim.k < in_bins ? 0 : 1; turn < (by_mass ? 2 : 1); ++turn)
+            cut = small_cut(q, s, w, bin_scale, turn, turn ? share_of(lim, mass) : lim.k, mass, lds);
+        wave_sync();                                        // (the histogram is read)
+    }
+
+    const uint32_t floor32 = lim.least < 0xffffffffull ? (uint32_t)lim.least : 0xffffffffu;
+    uint32_t kept = 0;
+    uint64_t four[EACH / 4], run[EACH / 4], total = 0;
+#pragma unroll
+    for (int i = 0; i < EACH / 4; ++i) {
+        four[i] = 0;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const int e = 4 * i + c;
+            const bool in = w[e] >= floor32 && within(cut, key_of(s[e]), small_index(lane, e));
+            kept += (uint32_t)__popcll(__ballot(in));
+            w[e] = in ? w[e] : 0;
+            four[i] += whole(w[e]);
+        }
+        run[i] = total + wave_scan52(four[i]);
+        total = lane_u64(run[i], 63);
+    }
+    if (lane == 0 && kept_out) kept_out[p] = (int32_t)kept;
+    if (set.n_draws <= 8) {                                 // the wave finds one after another
+        for (int32_t j = 0; j < set.n_draws; ++j) {
+            const uint64_t r = point_of(__uint_as_float((uint32_t)__builtin_amdgcn_readlane(__float_as_int(u_first), j)), total);
+            bool found = false;
+#pragma unroll
+            for (int i = 0; i < EACH / 4; ++i) {
+                const uint64_t over = found ? 0 : __ballot(run[i] > r);
+                if (over == 0) continue;
+                found = true;
+                if (lane != __builtin_ctzll(over)) continue;
+                uint64_t left = r - (run[i] - four[i]);
+                int c = 0;
+                uint32_t at = w[4 * i];
+#pragma unroll
+                for (int e = 0; e < 3; ++e)
+                    if (c == e && whole(w[4 * i + e]) <= left) {
+                        left -= whole(w[4 * i + e]);
+                        at = w[4 * i + e + 1];
+                        ++c;
+                    }
+                idx[j] = small_index(lane, 4 * i + c);
+                if (prob) prob[j] = (float)((double)whole(at) / (double)total);
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < EACH / 4; ++i) {
+        lds.run[i * 64 + lane] = run[i];
+        *reinterpret_cast<u32x4_t *>(lds.w + (i * 64 + lane) * 4) = (u32x4_t){w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
+    }
+    wave_sync();
+    for (int32_t j = lane; j < set.n_draws; j += 64) {      // a lane a draw
+        uint64_t r = point_of(j < 64 ? u_first : u[j], total);
+        int at = 0;
+#pragma unroll
+        for (int step = EACH * 8; step > 0; step >>= 1)
+            if (lds.run[at + step - 1] <= r) at += step;
+        r -= at ? lds.run[at - 1] : 0;
+        const u32x4_t v = *reinterpret_cast<const u32x4_t *>(lds.w + at * 4);
+        int c = 0;
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (c == e && whole(v[e]) <= r) {
+                r -= whole(v[e]);
+                ++c;
+            }
+        idx[j] = at * 4 + c;
+        if (prob) prob[j] = (float)((double)whole(v[c]) / (double)total);
+    }
+}
+
+// `each` problems a workgroup: those of up to kSmall candidates a wave each,
+// then the others by the whole workgroup, one after another.
+template <int NT, int BINS, int CACHED>
+__global__ __launch_bounds__(NT, 3) void k_sample_waves(const float *__restrict__ scores, int64_t R, const int64_t *__restrict__ seg,
+                                                        int32_t P, int32_t each, Settings set, const float *__restrict__ u,
+                                                        int32_t *__restrict__ idx, float *__restrict__ prob,
+                                                        int32_t *__restrict__ kept_out)
+{
+    __shared__ union {
+        Lds<NT, BINS, CACHED> lds;
+        SmallLds small[NT / 64];
+    } sh;
+    const int32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), p0 = (int32_t)blockIdx.x * each;
+    if (wave < each && p0 + wave < P) {
+        const Problem q = problem_of(scores, R, seg, p0 + wave);
+        if (q.n <= 256) sample_small<4>(q, p0 + wave, set, u, idx, prob, kept_out, sh.small[wave]);
+        else if (q.n <= 512) sample_small<8>(q, p0 + wave, set, u, idx, prob, kept_out, sh.small[wave]);
+        else if (q.n <= kSmall) sample_small<16>(q, p0 + wave, set, u, idx, prob, kept_out, sh.small[wave]);
+    }
+#pragma unroll 1
+    for (int32_t p = p0; p < p0 + each && p < P; ++p) {
+        if (problem_of(scores, R, seg, p).n <= kSmall) continue;           // (the same for all threads)
+        __syncthreads();                                    // (LDS is free again)
+        sample_problem<NT, BINS, CACHED>(sh.lds, p, scores, R, seg, set, u, idx, prob, kept_out);
+    }
+}
 
 // Few problems of many candidates: each is shared by many workgroups, in
 // passes that hand their results on in the workspace: best score; histogram;
@@ -810,14 +1150,6 @@ struct WideArgs {
     WideState *state;
     Settings set;
 };
-
-__device__ __forceinline__ Problem problem_of(const WideArgs &a, int32_t p)
-{
-    int64_t lo = a.seg[p], hi = a.seg[p + 1];
-    lo = lo < 0 ? 0 : lo > a.R ? a.R : lo;
-    hi = hi < lo ? lo : hi > a.R ? a.R : hi;
-    return {a.scores + lo, (int32_t)(hi - lo), 0.0f, 1.0f};
-}
 
 // This wave's steps of problem blockIdx.y among those of all its workgroups.
 __device__ __forceinline__ Walk shared_walk(int32_t n)
@@ -861,7 +1193,7 @@ __global__ __launch_bounds__(256) void k_wide_clear(WideState *state)
 __global__ __launch_bounds__(kWide) void k_wide_best(WideArgs a)
 {
     const int32_t p = blockIdx.y;
-    const Problem q = problem_of(a, p);
+    const Problem q = problem_of(a.scores, a.R, a.seg, p);
     const Walk walk = shared_walk(q.n);
     float most = -__builtin_inff(), least = __builtin_inff();
     uint32_t alive = 0;
@@ -906,7 +1238,7 @@ __global__ __launch_bounds__(kWide) void k_wide_bins(WideArgs a)
     __shared__ uint32_t count[kWideBins];
     const int32_t p = blockIdx.y;
     WideState &st = a.state[p];
-    Problem q = problem_of(a, p);
+    Problem q = problem_of(a.scores, a.R, a.seg, p);
     if (st.alive == 0) return;
     Limits lim;
     const float bin_scale = wide_settings(a, p, st, q, lim);
@@ -944,7 +1276,7 @@ __global__ __launch_bounds__(kWide) void k_wide_find(WideArgs a, int turn)
     __shared__ Lds<kWide, kWideBins, 4> lds;
     const int32_t p = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     WideState &st = a.state[p];
-    Problem q = problem_of(a, p);
+    Problem q = problem_of(a.scores, a.R, a.seg, p);
     if (threadIdx.x == 0) {
         st.want = 0;
         st.n_near = 0;
@@ -993,7 +1325,7 @@ __global__ __launch_bounds__(kWide) void k_wide_list(WideArgs a)
     const int32_t p = blockIdx.y, lane = threadIdx.x & 63;
     WideState &st = a.state[p];
     if (st.alive == 0 || st.want == 0) return;
-    Problem q = problem_of(a, p);
+    Problem q = problem_of(a.scores, a.R, a.seg, p);
     Limits lim;
     const float bin_scale = wide_settings(a, p, st, q, lim);
     const uint32_t bin = st.bin;
@@ -1015,7 +1347,7 @@ __global__ __launch_bounds__(kWide) void k_wide_cut(WideArgs a, int turn)
     const int32_t p = blockIdx.x;
     WideState &st = a.state[p];
     if (st.alive == 0 || st.want == 0) return;
-    Problem q = problem_of(a, p);
+    Problem q = problem_of(a.scores, a.R, a.seg, p);
     Limits lim;
     const float bin_scale = wide_settings(a, p, st, q, lim);
     const uint32_t m = st.n_near;
@@ -1039,7 +1371,7 @@ __global__ __launch_bounds__(kWide) void k_wide_sums(WideArgs a)
     const int32_t p = blockIdx.y, lane = threadIdx.x & 63;
     WideState &st = a.state[p];
     if (st.alive == 0) return;
-    Problem q = problem_of(a, p);
+    Problem q = problem_of(a.scores, a.R, a.seg, p);
     Limits lim;
     wide_settings(a, p, st, q, lim);
     const Cut cut = st.cut;
@@ -1083,7 +1415,7 @@ __global__ __launch_bounds__(kWide) void k_wide_draw(WideArgs a, const float *__
         }
         return;
     }
-    Problem q = problem_of(a, p);
+    Problem q = problem_of(a.scores, a.R, a.seg, p);
     Limits lim;
     wide_settings(a, p, st, q, lim);
     const Cut cut = st.cut;
@@ -1117,6 +1449,12 @@ __global__ __launch_bounds__(kWide) void k_wide_draw(WideArgs a, const float *__
 // (83), 64 of 65,536 65 (50); 128 of 262,144 157 (163), 128 of 131,072 101 (92).
 static bool shared_problems(int64_t R, int32_t P) { return P <= 128 && R / P > 36864 + 1280 * (int64_t)P; }
 
+// A wave a problem, for problems of up to kSmall candidates on average: 16 problems of 64 6.3 us (512 threads each:
+// 12.7), of 512 7.7 (12.8), of 1,000 11.3 (12.9); 4,096 of 64 13 (90), of 512 17.6 (90), of 1,000 50 (93).  Longer
+// ones among them go by 256 threads: 600 of up to 1,400 17.4 (23.5), 1,000 of up to 2,000 27.0 (34.4), but 100 of up
+// to 1,400 14.0 (13.6).
+constexpr int64_t kSmallMean = kSmall;
+
 size_t sample_workspace_bytes(int64_t R, int32_t P, int32_t)
 {
     return shared_problems(R, P) ? (size_t)P * sizeof(WideState) : 0;
@@ -1142,9 +1480,10 @@ static void launch_shared(const WideArgs &a, int32_t P, const float *u, int32_t 
     hipLaunchKernelGGL(k_wide_draw, one, block, 0, s, a, u, idx, prob, kept);
 }
 
-template <int NT, int BINS, int CACHED, int WAVES>
-static void launch_problems(const float *scores, int64_t R, const int64_t *seg, int32_t P, const hwsel_sampling_t &how,
-                            const float *u, int32_t n_draws, int32_t *idx, float *prob, int32_t *kept, hipStream_t s)
+// launch(problems, seg, settings, u, idx, prob, kept) for spans of problems.
+template <class F>
+static void each_problems(const int64_t *seg, int32_t P, const hwsel_sampling_t &how, const float *u, int32_t n_draws, int32_t *idx,
+                          float *prob, int32_t *kept, F &&launch)
 {
     each_span(P, [&](int32_t p0, int32_t n) {
         hwsel_sampling_t h = how;
@@ -1153,8 +1492,28 @@ static void launch_problems(const float *scores, int64_t R, const int64_t *seg, 
         if (h.top_p_of) h.top_p_of += p0;
         if (h.min_p_of) h.min_p_of += p0;
         const int64_t o = (int64_t)p0 * n_draws;
-        hipLaunchKernelGGL((k_sample<NT, BINS, CACHED, WAVES>), dim3(n), dim3(NT), 0, s, scores, R, seg + p0, Settings{h, n_draws}, u + o,
-                           idx + o, prob ? prob + o : nullptr, kept ? kept + p0 : nullptr);
+        launch(n, seg + p0, Settings{h, n_draws}, u + o, idx + o, prob ? prob + o : nullptr, kept ? kept + p0 : nullptr);
+    });
+}
+
+template <int NT, int BINS, int CACHED, int WAVES>
+static void launch_problems(const float *scores, int64_t R, const int64_t *seg, int32_t P, const hwsel_sampling_t &how,
+                            const float *u, int32_t n_draws, int32_t *idx, float *prob, int32_t *kept, hipStream_t s)
+{
+    each_problems(seg, P, how, u, n_draws, idx, prob, kept, [&](int32_t n, auto... rest) {
+        hipLaunchKernelGGL((k_sample<NT, BINS, CACHED, WAVES>), dim3(n), dim3(NT), 0, s, scores, R, rest...);
+    });
+}
+
+// Enough workgroups for every compute unit first, then as many problems as a workgroup has waves, but one where half
+// of the problems may be longer and follow each other (1,000 of up to 2,000: 27 us, four by four 49).
+static void launch_waves(const float *scores, int64_t R, const int64_t *seg, int32_t P, const hwsel_sampling_t &how, const float *u,
+                         int32_t n_draws, int32_t *idx, float *prob, int32_t *kept, hipStream_t s)
+{
+    constexpr int NT = 256;
+    each_problems(seg, P, how, u, n_draws, idx, prob, kept, [&](int32_t n, const int64_t *seg_n, auto... rest) {
+        const int32_t cus = compute_units(), each = n <= cus || R / P > kSmall / 2 ? 1 : n >= cus * (NT / 64) ? NT / 64 : (n + cus - 1) / cus;
+        hipLaunchKernelGGL((k_sample_waves<NT, 1024, 4096>), dim3((n + each - 1) / each), dim3(NT), 0, s, scores, R, seg_n, n, each, rest...);
     });
 }
 
@@ -1163,11 +1522,12 @@ hipError_t launch_sample(const float *scores, int64_t R, const int64_t *seg, int
 {
     if (shared_problems(R, P))
         launch_shared(WideArgs{scores, R, seg, static_cast<WideState *>(ws), Settings{how, n_draws}}, P, u, idx, prob, kept, s);
-    // Where problems outnumber compute units, three workgroups of 512 threads share one, in 80 registers; up to
-    // 8,192 candidates otherwise, 512 threads wait for each other less than 1,024, which keep three times as many
-    // candidates in LDS.  600 problems of 8,192 27 us (1,024 threads: 49), 600 of 24,576 56 (75), 300 of 65,536 99
-    // (108); 128 of 8,192 16.8 (17.6), but 8 of 12,288 21.2 (19.4) and 256 of 24,576 33 (26).
-    else if (P > compute_units()) launch_problems<512, 1024, 8192, 6>(scores, R, seg, P, how, u, n_draws, idx, prob, kept, s);
+    else if (R / P <= kSmallMean) launch_waves(scores, R, seg, P, how, u, n_draws, idx, prob, kept, s);
+    // Where problems outnumber compute units, three workgroups of 256 threads share one; up to 8,192 candidates otherwise,
+    // 512 threads wait for each other less than 1,024, which keep three times as many candidates in LDS.  600 problems
+    // of up to 8,192 with 64 draws 26.8 us (512 threads: 29.6), 600 of 4,000 21.1 (26.8), 2,000 of 8,192 72 (72), 600 of up to 16,384 42 (44); 16 of 4,000 15.0 (256 threads: 16.9), 128 of 8,192 16.8 (1,024
+    // threads: 17.6), but 8 of 12,288 21.2 (19.4) and 256 of 24,576 33 (26).
+    else if (P > compute_units()) launch_problems<256, 1024, 8192, 3>(scores, R, seg, P, how, u, n_draws, idx, prob, kept, s);
     else if (R / P <= 8192) launch_problems<512, 1024, 8192, 4>(scores, R, seg, P, how, u, n_draws, idx, prob, kept, s);
     else launch_problems<1024, 2048, 24576, 4>(scores, R, seg, P, how, u, n_draws, idx, prob, kept, s);
     return hipGetLastError();
