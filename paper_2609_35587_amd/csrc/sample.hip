@@ -236,20 +236,21 @@ __device__ __forceinline__ Walk walk_of(int32_t n, int wave)
     return w;
 }
 
-// body(step, the lane's four scores, -inf past the end): four steps' loads at a
+// body(step, the lane's four scores, -inf past the end): AHEAD steps' loads at a
 // time while they are whole.
-template <class F>
+template <int AHEAD = 4, class F>
 __device__ __forceinline__ void each_step(const float *__restrict__ s, const Walk &w, int32_t first, int32_t last, F &&body)
 {
     const int lane = threadIdx.x & 63;
     int32_t i = first;
-    for (; i + 4 <= last && (int64_t)w.base + (i + 4) * 256 <= w.n; i += 4) {
-        f32x4u_t t[4];
+    if constexpr (AHEAD > 1)
+        for (; i + AHEAD <= last && (int64_t)w.base + (i + AHEAD) * 256 <= w.n; i += AHEAD) {
+            f32x4u_t t[AHEAD];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) t[j] = *reinterpret_cast<const f32x4u_t *>(s + w.base + (i + j) * 256 + lane * 4);
+            for (int j = 0; j < AHEAD; ++j) t[j] = *reinterpret_cast<const f32x4u_t *>(s + w.base + (i + j) * 256 + lane * 4);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) body(i + j, t[j]);
-    }
+            for (int j = 0; j < AHEAD; ++j) body(i + j, t[j]);
+        }
 #pragma unroll 1
     for (; i < last; ++i) {
         const int64_t at = (int64_t)w.base + i * 256 + lane * 4;
@@ -323,6 +324,52 @@ __device__ __forceinline__ void find_bin(L &lds, bool by_mass, uint64_t want, ui
     __syncthreads();
 }
 
+// A key that many of a bin's candidates share (a model of few leaves gives many
+// equal scores): they are counted instead of listed.  0: none.
+struct Tied {
+    uint32_t key, count;
+};
+
+// The key that most lanes hold (0: a lane without one).
+__device__ __forceinline__ uint32_t commonest(uint32_t key)
+{
+    uint32_t same = 0;
+#pragma unroll 8
+    for (int l = 0; l < 64; ++l) same += key != 0 && key == (uint32_t)__builtin_amdgcn_readlane((int)key, l);
+    const uint32_t most = wave_max((same << 6) | (threadIdx.x & 63));
+    return (uint32_t)__builtin_amdgcn_readlane((int)key, (int)(most & 63));
+}
+
+// The index of the left-th candidate with this key in a wave's steps (it is there).
+template <int AHEAD>
+__device__ __forceinline__ int32_t tied_at(const Problem &q, const Walk &walk, int32_t first, int32_t last, uint32_t key, uint32_t left)
+{
+    int32_t at = 0;
+    bool found = false;
+    each_step<AHEAD>(q.s, walk, first, last, [&](int32_t i, const f32x4u_t &t) {
+        uint32_t tied = 0;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tied += key_of(t[c]) == key;
+        const uint32_t scan = wave_scan(tied), here = (uint32_t)__builtin_amdgcn_readlane((int)scan, 63);
+        if (found) return;
+        if (left > here) {
+            left -= here;
+            return;
+        }
+        found = true;
+        const int lane = __builtin_ctzll(__ballot(scan >= left));
+        uint32_t run = scan - tied;
+        int c_at = 0;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            run += key_of(t[c]) == key;
+            c_at += run < left;
+        }
+        at = walk.base + i * 256 + lane * 4 + __builtin_amdgcn_readlane(c_at, lane);
+    });
+    return at;
+}
+
 // The cut by digits, where a bin holds too many to rank: the largest key K at
 // which the count (by_mass: mass) of scores with keys >= K reaches `want`, by 11
 // or 10 bits at a time over all scores, then the last of those tied with it
@@ -343,27 +390,29 @@ __device__ __forceinline__ Cut cut_by_digits(const Problem &q, const Walk &walk,
             lds.count[b] = 0;
         }
         __syncthreads();
+        each_step<1>(q.s, walk, 0, walk.steps, [&](int32_t, const f32x4u_t &t) {
 #pragma unroll 1
-        for (int32_t i = threadIdx.x; i < q.n; i += NT) {
-            const float v = q.s[i];
-            const uint32_t key = key_of(v);
-            const bool in = key != 0 && (left == 32 || key >> left == prefix);
-            const uint32_t bin = (1u << bits) - 1 - ((key >> shift) & ((1u << bits) - 1));     // best first
-            const uint64_t w = whole(weight32(exponent_of(q, v)));
-            const uint64_t lanes = __ballot(in);
-            if (lanes == 0) continue;
-            // one add for the lanes that agree with the first (equal scores)
-            const int first = __builtin_ctzll(lanes);
-            const bool same = in && key == (uint32_t)__builtin_amdgcn_readlane((int)key, first);
-            const uint64_t agree = __ballot(same);
-            if (same && lane == first) {
-                atomicAdd(&lds.count[bin], (uint32_t)__popcll(agree));
-                atomicAdd((unsigned long long *)&lds.mass[bin], (unsigned long long)(w * __popcll(agree)));
-            } else if (in && !same) {
-                atomicAdd(&lds.count[bin], 1u);
-                atomicAdd((unsigned long long *)&lds.mass[bin], (unsigned long long)w);
+            for (int c = 0; c < 4; ++c) {
+                const float v = c == 0 ? t[0] : c == 1 ? t[1] : c == 2 ? t[2] : t[3];
+                const uint32_t key = key_of(v);
+                const bool in = key != 0 && (left == 32 || key >> left == prefix);
+                const uint64_t lanes = __ballot(in);
+                if (lanes == 0) continue;
+                const uint32_t bin = (1u << bits) - 1 - ((key >> shift) & ((1u << bits) - 1));     // best first
+                const uint64_t w = whole(weight32(exponent_of(q, v)));
+                // one add for the lanes that agree with the first (equal scores)
+                const int first = __builtin_ctzll(lanes);
+                const bool same = in && key == (uint32_t)__builtin_amdgcn_readlane((int)key, first);
+                const uint64_t agree = __ballot(same);
+                if (same && lane == first) {
+                    atomicAdd(&lds.count[bin], (uint32_t)__popcll(agree));
+                    atomicAdd((unsigned long long *)&lds.mass[bin], (unsigned long long)(w * __popcll(agree)));
+                } else if (in && !same) {
+                    atomicAdd(&lds.count[bin], 1u);
+                    atomicAdd((unsigned long long *)&lds.mass[bin], (unsigned long long)w);
+                }
             }
-        }
+        });
         __syncthreads();
         uint32_t bin, c;
         uint64_t m;
@@ -382,7 +431,7 @@ __device__ __forceinline__ Cut cut_by_digits(const Problem &q, const Walk &walk,
     for (int e = 0; e < walk.per_wave; ++e) {
         const int32_t b = e * walk.each, end = b + walk.each < walk.steps ? b + walk.each : walk.steps;
         uint32_t n = 0;
-        each_step(q.s, walk, b, end, [&](int32_t, const f32x4u_t &t) {
+        each_step<1>(q.s, walk, b, end, [&](int32_t, const f32x4u_t &t) {
 #pragma unroll
             for (int c = 0; c < 4; ++c) n += key_of(t[c]) == prefix;
         });
@@ -396,18 +445,9 @@ __device__ __forceinline__ Cut cut_by_digits(const Problem &q, const Walk &walk,
     for (int e = 0; e < walk.per_wave; ++e) {
         const int part = wave * walk.per_wave + e;
         if (!(lds.part[part] < ties && lds.part[part + 1] >= ties)) continue;
-        uint32_t left = (uint32_t)(ties - lds.part[part]);
-        for (int32_t i0 = walk.base + e * walk.each * 256; i0 < q.n; i0 += 64) {
-            const int32_t i = i0 + lane;
-            uint64_t tied = __ballot(i < q.n && key_of(q.s[i < q.n ? i : i0]) == prefix);
-            const uint32_t here = (uint32_t)__popcll(tied);
-            if (left <= here) {
-                for (; left > 1; --left) tied &= tied - 1;
-                if (lane == 0) lds.found_bin = (uint32_t)(i0 + __builtin_ctzll(tied));
-                break;
-            }
-            left -= here;
-        }
+        const int32_t b = e * walk.each, end = b + walk.each < walk.steps ? b + walk.each : walk.steps;
+        const int32_t at = tied_at<1>(q, walk, b, end, prefix, (uint32_t)(ties - lds.part[part]));
+        if (lane == 0) lds.found_bin = (uint32_t)at;
     }
     __syncthreads();
     const int32_t last = (int32_t)lds.found_bin;
@@ -424,11 +464,14 @@ __device__ __forceinline__ void near_weights(uint32_t w, uint32_t &lo, uint32_t 
     hi = w < 0xffffffffu - slack ? w + slack : 0xffffffffu;
 }
 
-// The cut among the m candidates listed in lds.near: those of the bin are
-// ranked.  The count (by_mass: mass) before the bin is given.
+// The cut among the m candidates listed in lds.near, those of the bin, and the
+// tied ones: they are ranked.  The count (by_mass: mass) before the bin is given.
+// If the cut is among the tied ones its index is left open: ties says the
+// how-manieth of them it is (else 0).
 template <int NT, class L>
-__device__ __forceinline__ Cut rank_bin(const Problem &q, float bin_scale, uint32_t bin, uint32_t m, bool by_mass,
-                                        uint32_t before_count, uint64_t before_mass, uint64_t want, uint64_t &mass, L &lds)
+__device__ __forceinline__ Cut rank_bin(const Problem &q, float bin_scale, uint32_t bin, uint32_t m, const Tied &tied, bool by_mass,
+                                        uint32_t before_count, uint64_t before_mass, uint64_t want, uint64_t &mass, uint32_t &ties,
+                                        L &lds)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     uint32_t in_bin = 0;
@@ -441,8 +484,12 @@ __device__ __forceinline__ Cut rank_bin(const Problem &q, float bin_scale, uint3
     }
     in_bin = wave_sum(in_bin);
     if (lane == 0) lds.wave_count[wave] = in_bin;
+    if (tied.key != 0) {                                    // one entry for all of them
+        if (threadIdx.x == 0) lds.list[m] = (uint64_t)tied.key << 32;
+        ++m;
+    }
     __syncthreads();
-    in_bin = 0;
+    in_bin = tied.key != 0;
 #pragma unroll
     for (int o = 0; o < NT / 64; ++o) in_bin += lds.wave_count[o];
     for (uint32_t e = threadIdx.x; e < m; e += NT) {
@@ -454,26 +501,44 @@ __device__ __forceinline__ Cut rank_bin(const Problem &q, float bin_scale, uint3
     }
     __syncthreads();
     uint64_t run = before_mass;
+    uint32_t run_count = before_count;
     for (uint32_t e0 = 0; e0 < in_bin; e0 += NT) {          // (block-uniform)
         const uint32_t e = e0 + threadIdx.x;
         const uint64_t v = e < in_bin ? lds.sorted[e] : 0;
-        const uint64_t w = e < in_bin ? whole(weight32(exponent_of(q, score_of((uint32_t)(v >> 32))))) : 0;
-        const uint64_t scan = wave_scan52(w);
-        if (lane == 63) lds.wave_mass[wave] = scan;
+        const uint32_t key = (uint32_t)(v >> 32), n = e >= in_bin ? 0 : key == tied.key ? tied.count : 1;
+        const uint64_t each = e < in_bin ? whole(weight32(exponent_of(q, score_of(key)))) : 0, w = each * n;
+        const uint64_t scan = wave_scan(w);
+        const uint32_t scan_n = wave_scan(n);
+        if (lane == 63) {
+            lds.wave_mass[wave] = scan;
+            lds.wave_count[wave] = scan_n;
+        }
         __syncthreads();
         uint64_t upto = run + scan;
+        uint32_t upto_n = run_count + scan_n;
         for (int o = 0; o < NT / 64; ++o) {
-            if (o < wave) upto += lds.wave_mass[o];
+            if (o < wave) {
+                upto += lds.wave_mass[o];
+                upto_n += lds.wave_count[o];
+            }
             run += lds.wave_mass[o];
+            run_count += lds.wave_count[o];
         }
-        if (e < in_bin && (by_mass ? upto - w < want && upto >= want : (uint64_t)before_count + e + 1 == want)) {
+        if (e < in_bin && (by_mass ? upto - w < want && upto >= want : upto_n - n < want && upto_n >= want)) {
+            uint32_t of = 0;
+            if (key == tied.key) {
+                of = (uint32_t)(by_mass ? (want - (upto - w) + each - 1) / each : want - (upto_n - n));
+                upto -= (n - of) * each;
+            }
             lds.cut = v;
             lds.found_mass = upto;
+            lds.found_count = of;
         }
         __syncthreads();
     }
     const uint64_t cut = lds.cut;
     mass = lds.found_mass;
+    ties = lds.found_count;
     __syncthreads();
     return {(uint32_t)(cut >> 32), (int32_t)(0xffffffffu - (uint32_t)cut)};
 }
@@ -645,8 +710,9 @@ __device__ __forceinline__ void sample_problem(Lds<NT, BINS, CACHED> &lds, int32
 #pragma unroll 1
         for (int turn = by_count && lim.k < in_bins ? 0 : 1; turn < (by_mass ? 2 : 1); ++turn) {
             const uint64_t want = turn ? share_of(lim, mass) : lim.k;
-            uint32_t bin, c, m = kList + 1;
+            uint32_t bin, c, m = kList + 1, tied_here = 0, tied_before = 0;      // of this wave, of the waves before it
             uint64_t before;
+            Tied tied{0, 0};
             if (bins_left) {
                 find_bin<NT, BINS>(lds, turn, want, bin, c, before);
                 // the candidates whose weights lie around the bin's, with room for the rounding of either side
@@ -658,6 +724,7 @@ __device__ __forceinline__ void sample_problem(Lds<NT, BINS, CACHED> &lds, int32
                     const uint32_t at = atomicAdd(&lds.n_near, 1u);
                     if (at < kList) lds.near[at] = (uint32_t)i;
                 };
+                auto in_bin = [&](float v) { return takes_part(v) && (uint32_t)(-exponent_of(q, v) * bin_scale) == bin; };
                 for (int32_t i = 0; i < cached; ++i) {
                     const u32x4_t w = *slot(i);
 #pragma unroll
@@ -667,16 +734,57 @@ __device__ __forceinline__ void sample_problem(Lds<NT, BINS, CACHED> &lds, int32
                 each_step(q.s, walk, cached, walk.steps, [&](int32_t i, const f32x4u_t &t) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (takes_part(t[e]) && (uint32_t)(-exponent_of(q, t[e]) * bin_scale) == bin)
-                            list(walk.base + i * 256 + lane * 4 + e);
+                        if (in_bin(t[e])) list(walk.base + i * 256 + lane * 4 + e);
                 });
                 __syncthreads();
                 m = lds.n_near;
+                if (m > kList) {                            // again without those of the commonest score
+                    tied.key = commonest(key_of(q.s[lds.near[lane * (kList / 64)]]));
+                    __syncthreads();
+                    if (threadIdx.x == 0) lds.n_near = 0;
+                    __syncthreads();
+                    auto sort_out = [&](int32_t i, float v) {
+                        if (!in_bin(v)) return;
+                        if (key_of(v) == tied.key) ++tied_here;
+                        else list(i);
+                    };
+                    for (int32_t i = 0; i < cached; ++i) {
+                        const u32x4_t w = *slot(i);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int32_t at = walk.base + i * 256 + lane * 4 + e;
+                            if (w[e] >= w_lo && w[e] <= w_hi) sort_out(at, q.s[at]);
+                        }
+                    }
+                    each_step(q.s, walk, cached, walk.steps, [&](int32_t i, const f32x4u_t &t) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sort_out(walk.base + i * 256 + lane * 4 + e, t[e]);
+                    });
+                    tied_here = wave_sum(tied_here);
+                    if (lane == 0) lds.wave_count[wave] = tied_here;
+                    __syncthreads();
+                    m = lds.n_near;
+                    for (int w = 0; w < kWaves; ++w) {
+                        tied.count += lds.wave_count[w];
+                        tied_before += w < wave ? lds.wave_count[w] : 0;
+                    }
+                    if (tied.count == 0) tied.key = 0;      // (of a weight near the bin's, but outside it)
+                }
                 __syncthreads();
                 if (threadIdx.x == 0) lds.n_near = 0;
             }
-            if (m <= kList) {
-                cut = rank_bin<NT>(q, bin_scale, bin, m, turn, c, before, want, upto, lds);
+            if (m + (tied.key != 0) <= kList) {
+                uint32_t ties;
+                cut = rank_bin<NT>(q, bin_scale, bin, m, tied, turn, c, before, want, upto, ties, lds);
+                if (ties != 0) {
+                    if (ties > tied_before && ties <= tied_before + tied_here) {
+                        const int32_t at = tied_at<4>(q, walk, 0, walk.steps, cut.key, ties - tied_before);
+                        if (lane == 0) lds.found_bin = (uint32_t)at;
+                    }
+                    __syncthreads();
+                    cut.last = (int32_t)lds.found_bin;
+                    __syncthreads();
+                }
             } else {
                 cut = cut_by_digits<NT, BINS>(q, walk, turn, want, upto, lds);
                 bins_left = false;                          // (it used their place)
@@ -1132,15 +1240,15 @@ __global__ __launch_bounds__(NT, 3) void k_sample_waves(const float *__restrict_
 // candidates around the cut, ranked by one workgroup (once for top-k, once for
 // top-p); sums of parts; draws.  A compute unit takes in some 100 GB/s, so 3
 // problems of 534,600 take 881 us in a workgroup each, 70 so.
-constexpr int kWide = 1024, kWideBins = 4096, kWideNear = 1536, kWideParts = 1024;
+constexpr int kWide = 1024, kWideBins = 4096, kWideNear = 1536, kWideParts = 1024, kWideBlocks = 512;
 
 struct WideState {
-    uint32_t best, least, alive, bin, before_count, n_near;
+    uint32_t best, least, alive, bin, before_count, n_near, tied_key, pad;
     uint64_t before_mass, want, mass;
     Cut cut;
-    uint32_t kept, pad;
     uint64_t mass_of[kWideBins], part[kWideParts];
-    uint32_t count_of[kWideBins], near[kWideNear];
+    uint32_t count_of[kWideBins], near[kWideNear], kept_of[kWideParts];
+    uint32_t tied_of[kWideBlocks * (kWide / 64)];           // of each wave
 };
 
 struct WideArgs {
@@ -1185,7 +1293,6 @@ __global__ __launch_bounds__(256) void k_wide_clear(WideState *state)
         st.n_near = 0;
         st.mass = 0;
         st.cut = {0, 0x7fffffff};
-        st.kept = 0;
     }
 }
 
@@ -1242,7 +1349,8 @@ __global__ __launch_bounds__(kWide) void k_wide_bins(WideArgs a)
     if (st.alive == 0) return;
     Limits lim;
     const float bin_scale = wide_settings(a, p, st, q, lim);
-    if (!(lim.k < st.alive) && !(lim.top_p < 1.0f)) return;
+    const bool by_count = lim.k < st.alive;
+    if (!by_count && !(lim.top_p < 1.0f)) return;
     const Walk walk = shared_walk(q.n);
     for (int i = threadIdx.x; i < kWideBins; i += kWide) {
         mass[i] = 0;
@@ -1257,15 +1365,15 @@ __global__ __launch_bounds__(kWide) void k_wide_bins(WideArgs a)
             if (w != 0) {
                 const uint32_t bin = (uint32_t)(-e * bin_scale);
                 atomicAdd((unsigned long long *)&mass[bin], (unsigned long long)whole(w));
-                atomicAdd(&count[bin], 1u);
+                if (by_count) atomicAdd(&count[bin], 1u);
             }
         }
     });
     __syncthreads();
     for (int i = threadIdx.x; i < kWideBins; i += kWide)
-        if (count[i] != 0) {
+        if (mass[i] != 0) {
             atomicAdd((unsigned long long *)&st.mass_of[i], (unsigned long long)mass[i]);
-            atomicAdd(&st.count_of[i], count[i]);
+            if (by_count) atomicAdd(&st.count_of[i], count[i]);
         }
 }
 
@@ -1283,8 +1391,17 @@ __global__ __launch_bounds__(kWide) void k_wide_find(WideArgs a, int turn)
     }
     if (st.alive == 0) return;
     Limits lim;
-    wide_settings(a, p, st, q, lim);
+    const float bin_scale = wide_settings(a, p, st, q, lim);
     if (turn ? !(lim.top_p < 1.0f) : !(lim.k < st.alive)) return;
+    // 4,096 scores from here and there, among which one that many share will be found (16,384 singly: 14 us more)
+    constexpr int kLook = 4;
+    float look[kLook];
+#pragma unroll
+    for (int j = 0; j < kLook; ++j) {
+        const int64_t at = (int64_t)wave * q.n / (kWide / 64) + lane * kLook + j;
+        look[j] = q.s[at < q.n ? at : q.n - 1];
+    }
+    if (threadIdx.x == 0) lds.n_near = 0;
     uint64_t mass = 0;
     uint32_t n = 0;
     for (int i = threadIdx.x; i < kWideBins; i += kWide) {
@@ -1312,8 +1429,17 @@ __global__ __launch_bounds__(kWide) void k_wide_find(WideArgs a, int turn)
     uint32_t bin, before_count;
     uint64_t before_mass;
     find_bin<kWide, kWideBins>(lds, turn, want, bin, before_count, before_mass);
+#pragma unroll
+    for (int j = 0; j < kLook; ++j)
+        if (takes_part(look[j]) && (uint32_t)(-exponent_of(q, look[j]) * bin_scale) == bin) {
+            const uint32_t at = atomicAdd(&lds.n_near, 1u);
+            if (at < 64) lds.near[at] = key_of(look[j]);
+        }
+    __syncthreads();
+    const uint32_t tied_key = commonest((uint32_t)lane < lds.n_near ? lds.near[lane] : 0);
     if (threadIdx.x == 0) {
         st.want = want;
+        st.tied_key = tied_key;
         st.bin = bin;
         st.before_count = before_count;
         st.before_mass = before_mass;
@@ -1328,19 +1454,26 @@ __global__ __launch_bounds__(kWide) void k_wide_list(WideArgs a)
     Problem q = problem_of(a.scores, a.R, a.seg, p);
     Limits lim;
     const float bin_scale = wide_settings(a, p, st, q, lim);
-    const uint32_t bin = st.bin;
+    const uint32_t bin = st.bin, tied_key = st.tied_key;
     const Walk walk = shared_walk(q.n);
+    uint32_t tied = 0;
     each_step(q.s, walk, 0, walk.steps, [&](int32_t i, const f32x4u_t &t) {
 #pragma unroll
         for (int c = 0; c < 4; ++c)
             if (takes_part(t[c]) && (uint32_t)(-exponent_of(q, t[c]) * bin_scale) == bin) {
+                if (key_of(t[c]) == tied_key) {
+                    ++tied;
+                    continue;
+                }
                 const uint32_t at = atomicAdd(&st.n_near, 1u);
                 if (at < kWideNear) st.near[at] = (uint32_t)(walk.base + i * 256 + lane * 4 + c);
             }
     });
+    tied = wave_sum(tied);
+    if (lane == 0) st.tied_of[(int)blockIdx.x * (kWide / 64) + (int)(threadIdx.x >> 6)] = tied;
 }
 
-__global__ __launch_bounds__(kWide) void k_wide_cut(WideArgs a, int turn)
+__global__ __launch_bounds__(kWide) void k_wide_cut(WideArgs a, int turn, int32_t blocks)
 {
     __shared__ Lds<kWide, kWideBins, 4> lds;
     static_assert(Lds<kWide, kWideBins, 4>::kList == kWideNear, "the list fits");
@@ -1353,10 +1486,48 @@ __global__ __launch_bounds__(kWide) void k_wide_cut(WideArgs a, int turn)
     const uint32_t m = st.n_near;
     uint64_t upto;
     Cut cut;
-    if (m <= kWideNear) {
+    // the tied ones: a thread takes consecutive waves of k_wide_list
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blocks * (kWide / 64), own = (waves + kWide - 1) / kWide;
+    Tied tied{st.tied_key, 0};
+    uint32_t here = 0;
+    for (int i = 0; i < own; ++i) {
+        const int w = (int)threadIdx.x * own + i;
+        here += w < waves ? st.tied_of[w] : 0;
+    }
+    const uint32_t scan = wave_scan(here);
+    if (lane == 63) lds.wave_count[wave] = scan;
+    __syncthreads();
+    uint32_t before = scan - here;
+    for (int w = 0; w < kWide / 64; ++w) {
+        before += w < wave ? lds.wave_count[w] : 0;
+        tied.count += lds.wave_count[w];
+    }
+    if (tied.count == 0) tied.key = 0;
+    __syncthreads();
+    if (m + (tied.key != 0) <= kWideNear) {
         for (uint32_t e = threadIdx.x; e < m; e += kWide) lds.near[e] = st.near[e];
         __syncthreads();
-        cut = rank_bin<kWide>(q, bin_scale, st.bin, m, turn, st.before_count, st.before_mass, st.want, upto, lds);
+        uint32_t ties;
+        cut = rank_bin<kWide>(q, bin_scale, st.bin, m, tied, turn, st.before_count, st.before_mass, st.want, upto, ties, lds);
+        if (ties != 0) {                                    // which wave's it is, and what is before that wave
+            if (ties > before && ties <= before + here) {
+                int w = (int)threadIdx.x * own;
+                while (ties > before + st.tied_of[w]) before += st.tied_of[w++];
+                lds.found_bin = (uint32_t)w;
+                lds.found_count = ties - before;
+            }
+            __syncthreads();
+            const uint32_t w = lds.found_bin, left = lds.found_count;
+            __syncthreads();
+            if (wave == 0) {
+                const int32_t steps = (int32_t)(((int64_t)q.n + 256 * (int64_t)waves - 1) / (256 * (int64_t)waves));
+                const Walk walk{q.n, steps, (int32_t)w * steps * 256, steps, 1};
+                const int32_t at = tied_at<4>(q, walk, 0, steps, cut.key, left);
+                if (lane == 0) lds.found_bin = (uint32_t)at;
+            }
+            __syncthreads();
+            cut.last = (int32_t)lds.found_bin;
+        }
     } else {
         cut = cut_by_digits<kWide, kWideBins>(q, walk_of<kWide>(q.n, (int)(threadIdx.x >> 6)), turn, st.want, upto, lds);
     }
@@ -1376,11 +1547,11 @@ __global__ __launch_bounds__(kWide) void k_wide_sums(WideArgs a)
     wide_settings(a, p, st, q, lim);
     const Cut cut = st.cut;
     const int32_t each = wide_each(q.n), parts = (int32_t)(((int64_t)q.n + 256 * (int64_t)each - 1) / (256 * (int64_t)each));
-    uint32_t kept = 0;
     for (int32_t e = __builtin_amdgcn_readfirstlane((int)blockIdx.x * (kWide / 64) + (threadIdx.x >> 6)); e < parts;
          e += (int32_t)gridDim.x * (kWide / 64)) {
         const Walk walk{q.n, each, e * each * 256, each, 1};
         uint64_t sum = 0;
+        uint32_t kept = 0;
         each_step(q.s, walk, 0, each, [&](int32_t i, const f32x4u_t &t) {
             uint64_t w[4];
             kept_weights(q, cut, lim.least, t, walk.base + i * 256 + lane * 4, w);
@@ -1391,24 +1562,27 @@ __global__ __launch_bounds__(kWide) void k_wide_sums(WideArgs a)
             }
         });
         sum = wave_sum(sum);
-        if (lane == 0) st.part[e] = sum;
+        kept = wave_sum(kept);
+        if (lane == 0) {
+            st.part[e] = sum;
+            st.kept_of[e] = kept;
+        }
     }
-    kept = wave_sum(kept);
-    if (lane == 0 && kept != 0) atomicAdd(&st.kept, kept);
 }
 
 __global__ __launch_bounds__(kWide) void k_wide_draw(WideArgs a, const float *__restrict__ u, int32_t *__restrict__ idx,
                                                      float *__restrict__ prob, int32_t *__restrict__ kept_out)
 {
     __shared__ uint64_t part[kWideParts + 1], wave_mass[kWide / 64];
+    __shared__ uint32_t wave_kept[kWide / 64];
     const int32_t p = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int32_t n_draws = a.set.n_draws;
     const WideState &st = a.state[p];
     u += (int64_t)p * n_draws;
     idx += (int64_t)p * n_draws;
     if (prob) prob += (int64_t)p * n_draws;
-    if (threadIdx.x == 0 && kept_out) kept_out[p] = (int32_t)st.kept;
     if (st.alive == 0) {
+        if (threadIdx.x == 0 && kept_out) kept_out[p] = 0;
         for (int32_t j = threadIdx.x; j < n_draws; j += kWide) {
             idx[j] = -1;
             if (prob) prob[j] = 0.0f;
@@ -1421,13 +1595,20 @@ __global__ __launch_bounds__(kWide) void k_wide_draw(WideArgs a, const float *__
     const Cut cut = st.cut;
     const int32_t each = wide_each(q.n), parts = (int32_t)(((int64_t)q.n + 256 * (int64_t)each - 1) / (256 * (int64_t)each));
     const uint64_t own = (int)threadIdx.x < parts ? st.part[threadIdx.x] : 0, scan = wave_scan(own);
-    if (lane == 63) wave_mass[wave] = scan;
+    uint32_t kept = wave_sum((int)threadIdx.x < parts ? st.kept_of[threadIdx.x] : 0);
+    if (lane == 63) {
+        wave_mass[wave] = scan;
+        wave_kept[wave] = kept;
+    }
     __syncthreads();
     uint64_t before = scan - own, total = 0;
+    kept = 0;
     for (int w = 0; w < kWide / 64; ++w) {
         if (w < wave) before += wave_mass[w];
         total += wave_mass[w];
+        kept += wave_kept[w];
     }
+    if (threadIdx.x == 0 && kept_out) kept_out[p] = (int32_t)kept;
     part[threadIdx.x] = before;
     if (threadIdx.x == 0) part[kWideParts] = total;
     __syncthreads();
@@ -1463,8 +1644,9 @@ size_t sample_workspace_bytes(int64_t R, int32_t P, int32_t)
 static void launch_shared(const WideArgs &a, int32_t P, const float *u, int32_t *idx, float *prob, int32_t *kept, hipStream_t s)
 {
     // sixteen steps or so a wave, the machine filled about twice
-    const int64_t want = (a.R + 16383) / 16384, most = (2 * compute_units() + P - 1) / P;
-    const dim3 shared((unsigned)(want < most ? want : most), (unsigned)P), one((unsigned)P), block(kWide);
+    int64_t blocks = (a.R + 16383) / 16384;
+    for (const int64_t most : {(2 * (int64_t)compute_units() + P - 1) / P, (int64_t)kWideBlocks}) blocks = blocks < most ? blocks : most;
+    const dim3 shared((unsigned)blocks, (unsigned)P), one((unsigned)P), block(kWide);
     hipLaunchKernelGGL(k_wide_clear, one, dim3(256), 0, s, a.state);
     hipLaunchKernelGGL(k_wide_best, shared, block, 0, s, a);
     const bool by_count = a.set.how.top_k_of || a.set.how.top_k > 0 || a.set.how.temperature_of || !(a.set.how.temperature > 0.0f),
@@ -1474,7 +1656,7 @@ static void launch_shared(const WideArgs &a, int32_t P, const float *u, int32_t 
         if (!(turn ? by_mass : by_count)) continue;
         hipLaunchKernelGGL(k_wide_find, one, block, 0, s, a, turn);
         hipLaunchKernelGGL(k_wide_list, shared, block, 0, s, a);
-        hipLaunchKernelGGL(k_wide_cut, one, block, 0, s, a, turn);
+        hipLaunchKernelGGL(k_wide_cut, one, block, 0, s, a, turn, (int32_t)blocks);
     }
     hipLaunchKernelGGL(k_wide_sums, shared, block, 0, s, a);
     hipLaunchKernelGGL(k_wide_draw, one, block, 0, s, a, u, idx, prob, kept);
