@@ -11,23 +11,21 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// Eight consecutive elements of a row, zeros from column C on.  vec: the row
-// starts allow 16-byte loads.
+// Eight consecutive elements of a row, zeros from column C on.
 template <bool BF16>
-__device__ __forceinline__ void load8(const void *X, int64_t row_at, int64_t c0, int64_t C, bool vec, float (&v)[8])
+__device__ __forceinline__ void load8(const void *X, int64_t row_at, int64_t c0, int64_t C, float (&v)[8])
 {
-    if (vec && c0 + 8 <= C) {
+    if (c0 + 8 <= C) {
         if constexpr (BF16) {
-            const uint4 w = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(X) + row_at + c0);
-            const uint32_t p[4] = {w.x, w.y, w.z, w.w};
+            const u32x4_any_t w = *reinterpret_cast<const u32x4_any_t *>(static_cast<const uint16_t *>(X) + row_at + c0);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                v[2 * i] = __uint_as_float(p[i] << 16);
-                v[2 * i + 1] = __uint_as_float(p[i] & 0xffff0000u);
+                v[2 * i] = __uint_as_float(w[i] << 16);
+                v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
             }
         } else {
-            const float4 *at = reinterpret_cast<const float4 *>(static_cast<const float *>(X) + row_at + c0);
-            const float4 a = at[0], b = at[1];
+            const f32x4_any_t *at = reinterpret_cast<const f32x4_any_t *>(static_cast<const float *>(X) + row_at + c0);
+            const f32x4_any_t a = at[0], b = at[1];
             v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
             v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
         }
@@ -51,8 +49,7 @@ __device__ __forceinline__ void load8(const void *X, int64_t row_at, int64_t c0,
 constexpr int kRowsInFlight = 2;
 
 template <bool BF16, bool STD, int KBW>
-__global__ __launch_bounds__(kThreads) void k_quantise_rows(const void *__restrict__ X, int64_t ld, bool vec,
-                                                             const float *__restrict__ mean,
+__global__ __launch_bounds__(kThreads) void k_quantise_rows(const void *__restrict__ X, int64_t ld, const float *__restrict__ mean,
                                                              const float *__restrict__ inv_std, hwsel_fp8_t out)
 {
     constexpr int kRows = 4 / KBW;                          // rows of one wave step
@@ -84,8 +81,8 @@ __global__ __launch_bounds__(kThreads) void k_quantise_rows(const void *__restri
         const int64_t first = r0 + (int64_t)wave * kRows * kRowsInFlight + (lane >> 4) / KBW;
 #pragma unroll
         for (int j = 0; j < kRowsInFlight; ++j) {
-            const int64_t r = first + j * kRows;
-            load8<BF16>(X, r * ld, c0, r < out.rows ? out.cols : 0, vec, v[j]);
+            const int64_t r = first + j * kRows;            // (past the end the last row again: its codes are not stored)
+            load8<BF16>(X, (r < out.rows ? r : out.rows - 1) * ld, c0, out.cols, v[j]);
         }
 #pragma unroll
         for (int j = 0; j < kRowsInFlight; ++j) {
@@ -127,35 +124,45 @@ struct TileIn {
     const uint8_t *scale;                                   // of an 8-bit source
     int64_t ld_scale;
     int32_t format, block_rows;
-    bool vec;                                               // four elements at a multiple of four can be read at once
 };
 
-// Four elements of a row in fp32 or bf16, zeros outside.
+// Four columns of sixteen rows in fp32 or bf16, zeros outside.
 template <Source S>
-__device__ __forceinline__ void load4(const TileIn &in, int64_t r, int64_t c, float (&v)[4])
+__device__ __forceinline__ void load16x4(const TileIn &in, int64_t r0, int64_t c, float (&v)[16][4])
 {
+    if (c + 4 <= in.cols) {                                 // all on their way at once; the last row again past the end
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = 0.0f;
-    if (r >= in.rows || c >= in.cols) return;
-    if (in.vec && c + 4 <= in.cols) {
-        if constexpr (S == Source::fp32) {
-            const float4 w = *reinterpret_cast<const float4 *>(static_cast<const float *>(in.X) + r * in.ld + c);
-            v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
-        } else {
-            const uint2 w = *reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(in.X) + r * in.ld + c);
-            v[0] = __uint_as_float(w.x << 16);
-            v[1] = __uint_as_float(w.x & 0xffff0000u);
-            v[2] = __uint_as_float(w.y << 16);
-            v[3] = __uint_as_float(w.y & 0xffff0000u);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (c + i < in.cols) {
-                if constexpr (S == Source::fp32) v[i] = static_cast<const float *>(in.X)[r * in.ld + c + i];
-                else v[i] = bf16_value(static_cast<const uint16_t *>(in.X)[r * in.ld + c + i]);
+        for (int j = 0; j < 16; ++j) {
+            const int64_t at = (r0 + j < in.rows ? r0 + j : in.rows - 1) * in.ld + c;
+            if constexpr (S == Source::fp32) {
+                const f32x4_any_t w = *reinterpret_cast<const f32x4_any_t *>(static_cast<const float *>(in.X) + at);
+                v[j][0] = w.x; v[j][1] = w.y; v[j][2] = w.z; v[j][3] = w.w;
+            } else {
+                const u32x2_any_t w = *reinterpret_cast<const u32x2_any_t *>(static_cast<const uint16_t *>(in.X) + at);
+                v[j][0] = __uint_as_float(w.x << 16);
+                v[j][1] = __uint_as_float(w.x & 0xffff0000u);
+                v[j][2] = __uint_as_float(w.y << 16);
+                v[j][3] = __uint_as_float(w.y & 0xffff0000u);
             }
+        }
+        if (r0 + 16 > in.rows) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[j][i] = r0 + j < in.rows ? v[j][i] : 0.0f;
+        }
+        return;
     }
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[j][i] = 0.0f;
+            if (r0 + j < in.rows && c + i < in.cols) {
+                if constexpr (S == Source::fp32) v[j][i] = static_cast<const float *>(in.X)[(r0 + j) * in.ld + c + i];
+                else v[j][i] = bf16_value(static_cast<const uint16_t *>(in.X)[(r0 + j) * in.ld + c + i]);
+            }
+        }
 }
 
 // A workgroup takes tiles of 128 x 128; a thread has 16 rows of four columns,
@@ -205,8 +212,7 @@ __global__ __launch_bounds__(kThreads) void k_quantise_tiles(TileIn in, hwsel_fp
                 v[j][0] = a.x * s; v[j][1] = a.y * s; v[j][2] = b.x * s; v[j][3] = b.y * s;
             }
         } else {
-#pragma unroll
-            for (int j = 0; j < 16; ++j) load4<S>(in, rt * 128 + 16 * group + j, c, v[j]);
+            load16x4<S>(in, rt * 128 + 16 * group, c, v);
         }
         uint32_t m[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -296,7 +302,7 @@ __global__ __launch_bounds__(kThreads) void k_quantise_tiles(TileIn in, hwsel_fp
 
 // Sixteen lanes a block, eight elements each.
 template <bool BF16, int KBW>
-__global__ __launch_bounds__(kThreads) void k_dequantise(hwsel_fp8_t in, void *__restrict__ X, int64_t ld, bool vec)
+__global__ __launch_bounds__(kThreads) void k_dequantise(hwsel_fp8_t in, void *__restrict__ X, int64_t ld)
 {
     constexpr int kRows = 4 / KBW;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -336,14 +342,14 @@ __global__ __launch_bounds__(kThreads) void k_dequantise(hwsel_fp8_t in, void *_
                 v[4 * h + 2] = b.x * s;
                 v[4 * h + 3] = b.y * s;
             }
-            if (vec && c0 + 8 <= in.cols) {
+            if (c0 + 8 <= in.cols) {
                 if constexpr (BF16) {
-                    *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(X) + r * ld + c0) =
-                        make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
+                    *reinterpret_cast<u32x4_any_t *>(static_cast<uint16_t *>(X) + r * ld + c0) =
+                        (u32x4_any_t){bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
                 } else {
-                    float4 *at = reinterpret_cast<float4 *>(static_cast<float *>(X) + r * ld + c0);
-                    at[0] = make_float4(v[0], v[1], v[2], v[3]);
-                    at[1] = make_float4(v[4], v[5], v[6], v[7]);
+                    f32x4_any_t *at = reinterpret_cast<f32x4_any_t *>(static_cast<float *>(X) + r * ld + c0);
+                    at[0] = (f32x4_any_t){v[0], v[1], v[2], v[3]};
+                    at[1] = (f32x4_any_t){v[4], v[5], v[6], v[7]};
                 }
             } else {
 #pragma unroll
@@ -388,43 +394,39 @@ void launch_tiles(const TileIn &in, bool transposed, const hwsel_fp8_t &out, hip
 hipError_t launch_fp8_quantise(const void *X, bool bf16, int64_t ld, bool transposed, const float *mean,
                                const float *inv_std, const hwsel_fp8_t &out, hipStream_t s)
 {
-    const size_t el = bf16 ? 2 : 4;
     if (transposed || out.block_rows != 1) {
-        const TileIn in{X, transposed ? out.cols : out.rows, transposed ? out.rows : out.cols, ld, nullptr, 0, 0, 1,
-                        ((uintptr_t)X | (uintptr_t)(ld * el)) % (4 * el) == 0};
+        const TileIn in{X, transposed ? out.cols : out.rows, transposed ? out.rows : out.cols, ld, nullptr, 0, 0, 1};
         if (bf16) launch_tiles<Source::bf16>(in, transposed, out, s);
         else launch_tiles<Source::fp32>(in, transposed, out, s);
         return hipGetLastError();
     }
-    const bool vec = ((uintptr_t)X | (uintptr_t)(ld * el)) % 16 == 0;
     by_blocks(fp8_blocks(out.cols), [&](auto kbw) {
         constexpr int KBW = decltype(kbw)::value;
         const int64_t chunks = (fp8_blocks(out.cols) + KBW - 1) / KBW;
         const dim3 grid(row_groups(out.rows, 4 * (4 / KBW) * kRowsInFlight, chunks), (unsigned)chunks), block(kThreads);
-        if (mean && bf16) hipLaunchKernelGGL((k_quantise_rows<true, true, KBW>), grid, block, 0, s, X, ld, vec, mean, inv_std, out);
-        else if (mean) hipLaunchKernelGGL((k_quantise_rows<false, true, KBW>), grid, block, 0, s, X, ld, vec, mean, inv_std, out);
-        else if (bf16) hipLaunchKernelGGL((k_quantise_rows<true, false, KBW>), grid, block, 0, s, X, ld, vec, mean, inv_std, out);
-        else hipLaunchKernelGGL((k_quantise_rows<false, false, KBW>), grid, block, 0, s, X, ld, vec, mean, inv_std, out);
+        if (mean && bf16) hipLaunchKernelGGL((k_quantise_rows<true, true, KBW>), grid, block, 0, s, X, ld, mean, inv_std, out);
+        else if (mean) hipLaunchKernelGGL((k_quantise_rows<false, true, KBW>), grid, block, 0, s, X, ld, mean, inv_std, out);
+        else if (bf16) hipLaunchKernelGGL((k_quantise_rows<true, false, KBW>), grid, block, 0, s, X, ld, mean, inv_std, out);
+        else hipLaunchKernelGGL((k_quantise_rows<false, false, KBW>), grid, block, 0, s, X, ld, mean, inv_std, out);
     });
     return hipGetLastError();
 }
 
 hipError_t launch_fp8_transpose(const hwsel_fp8_t &in, const hwsel_fp8_t &out, hipStream_t s)
 {
-    const TileIn t{in.q, in.rows, in.cols, in.ld, in.scale, in.ld_scale, in.format, in.block_rows, true};
+    const TileIn t{in.q, in.rows, in.cols, in.ld, in.scale, in.ld_scale, in.format, in.block_rows};
     launch_tiles<Source::fp8>(t, true, out, s);
     return hipGetLastError();
 }
 
 hipError_t launch_fp8_dequantise(const hwsel_fp8_t &in, void *X, bool bf16, int64_t ld, hipStream_t s)
 {
-    const bool vec = ((uintptr_t)X | (uintptr_t)(ld * (bf16 ? 2 : 4))) % 16 == 0;
     by_blocks(fp8_blocks(in.cols), [&](auto kbw) {
         constexpr int KBW = decltype(kbw)::value;
         const int64_t chunks = (fp8_blocks(in.cols) + KBW - 1) / KBW;
         const dim3 grid(row_groups(in.rows, 4 * (4 / KBW) * kRowsInFlight, chunks), (unsigned)chunks), block(kThreads);
-        if (bf16) hipLaunchKernelGGL((k_dequantise<true, KBW>), grid, block, 0, s, in, X, ld, vec);
-        else hipLaunchKernelGGL((k_dequantise<false, KBW>), grid, block, 0, s, in, X, ld, vec);
+        if (bf16) hipLaunchKernelGGL((k_dequantise<true, KBW>), grid, block, 0, s, in, X, ld);
+        else hipLaunchKernelGGL((k_dequantise<false, KBW>), grid, block, 0, s, in, X, ld);
     });
     return hipGetLastError();
 }

@@ -28,6 +28,13 @@ __device__ __forceinline__ uint32_t finite_bits(float v)
     return a < 0x7f800000u ? a : 0u;
 }
 
+// Rows of a matrix may start at any element: global loads and stores of several
+// elements need no more alignment than one (what the odd rows cost over single
+// elements is at most a second cache line).
+typedef float f32x4_any_t __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x4_any_t __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x2_any_t __attribute__((ext_vector_type(2), aligned(2)));
+
 // The exponent byte of a block whose largest finite magnitude has these bits:
 // the largest code is 1.75 2^8 (E4M3) or 1.75 2^15 (E5M2), so with amax = m 2^x
 // the exponent is x - 8 (x - 15) up to m = 1.75 and one more above.  Subnormal

@@ -34,7 +34,6 @@ struct Out {
     int64_t ld_scale;
     const float *bias;
     int32_t gelu;
-    bool vec, wide;                                         // four columns at a multiple of four, eight of eight at once
 };
 
 struct Operand {
@@ -107,8 +106,8 @@ __device__ __forceinline__ void store4(const Out &o, int64_t m, int32_t n, int32
     if constexpr (KIND == kOutBf16) {
         uint16_t *at = static_cast<uint16_t *>(o.C) + m * o.ld + n;
         const uint32_t a = bf16_pair(v[0], v[1]), b = bf16_pair(v[2], v[3]);
-        if (o.vec && n + 4 <= N) {
-            *reinterpret_cast<uint2 *>(at) = make_uint2(a, b);
+        if (n + 4 <= N) {
+            *reinterpret_cast<u32x2_any_t *>(at) = (u32x2_any_t){a, b};
         } else {
             at[0] = (uint16_t)a;
             if (n + 1 < N) at[1] = (uint16_t)(a >> 16);
@@ -117,8 +116,8 @@ __device__ __forceinline__ void store4(const Out &o, int64_t m, int32_t n, int32
         }
     } else {
         float *at = static_cast<float *>(o.C) + m * o.ld + n;
-        if (KIND == kOutPart || (o.vec && n + 4 <= N)) {
-            *reinterpret_cast<float4 *>(at) = make_float4(v[0], v[1], v[2], v[3]);
+        if (KIND == kOutPart || n + 4 <= N) {
+            *reinterpret_cast<f32x4_any_t *>(at) = (f32x4_any_t){v[0], v[1], v[2], v[3]};
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -308,7 +307,7 @@ __device__ __forceinline__ void finish_tiles(const f32x4_t (&acc)[MT][8], int32_
                 *reinterpret_cast<uint4 *>(at + 64) = make_uint4(w[4], w[5], w[6], w[7]);
                 if (g == 0) o.scale[(int64_t)m * o.ld_scale + (n0 >> 7)] = (uint8_t)byte;
             }
-        } else if (KIND == kOutBf16 && whole && o.wide) {
+        } else if (KIND == kOutBf16 && whole) {
             uint32_t lo[NT], hi[NT];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
@@ -323,9 +322,9 @@ __device__ __forceinline__ void finish_tiles(const f32x4_t (&acc)[MT][8], int32_
             if (m < M) {
 #pragma unroll
                 for (int h = 0; h < NT; h += 4) {
-                    uint4 *at = reinterpret_cast<uint4 *>(static_cast<uint16_t *>(o.C) + (int64_t)m * o.ld + n0 + 16 * (h + g));
-                    at[0] = make_uint4(lo[h], hi[h], lo[h + 1], hi[h + 1]);
-                    at[1] = make_uint4(lo[h + 2], hi[h + 2], lo[h + 3], hi[h + 3]);
+                    auto *at = reinterpret_cast<u32x4_any_t *>(static_cast<uint16_t *>(o.C) + (int64_t)m * o.ld + n0 + 16 * (h + g));
+                    at[0] = (u32x4_any_t){lo[h], hi[h], lo[h + 1], hi[h + 1]};
+                    at[1] = (u32x4_any_t){lo[h + 2], hi[h + 2], lo[h + 3], hi[h + 3]};
                 }
             }
         } else if (m < M) {
@@ -1090,16 +1089,14 @@ size_t fp8_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K)
 hipError_t launch_fp8_matmul(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const float *bias, bool gelu, void *C, bool bf16,
                              int64_t ldc, void *ws, hipStream_t s)
 {
-    const size_t el = bf16 ? 2 : 4;
-    const Out o{C, ldc, nullptr, 0, bias, gelu, ((uintptr_t)C | (uintptr_t)(ldc * el)) % (4 * el) == 0,
-                ((uintptr_t)C | (uintptr_t)(ldc * el)) % (8 * el) == 0};
+    const Out o{C, ldc, nullptr, 0, bias, gelu};
     return bf16 ? run_product<kOutBf16>(A, B, o, ws, s) : run_product<kOutF32>(A, B, o, ws, s);
 }
 
 hipError_t launch_fp8_layer(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const float *bias, bool gelu, const hwsel_fp8_t &C,
                             void *ws, hipStream_t s)
 {
-    return run_product<kOutFp8>(A, B, Out{C.q, C.ld, C.scale, C.ld_scale, bias, gelu, true, true}, ws, s);
+    return run_product<kOutFp8>(A, B, Out{C.q, C.ld, C.scale, C.ld_scale, bias, gelu}, ws, s);
 }
 
 }  // namespace hwsel
