@@ -167,12 +167,15 @@ __device__ __forceinline__ i32x8_t fragment(const uint8_t *tile, int lane)
 }
 
 // A fragment's 32 codes as bf16 values, scaled by 2^(lowest byte of scale - 127).
+// The instruction goes by the exponent bits of its scale alone: 0 is 2^-127 and
+// 255 gives NaN (measured), as the format has it.  (Decoding the next fragment
+// between this one's products, an instruction to each: 3% slower.)
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
 template <int FMT>
 __device__ __forceinline__ void decode(const i32x8_t &x, uint32_t scale, bf16x8_t (&out)[4])
 {
-    const float s = scale_value(scale & 0xffu);
+    const float s = __uint_as_float((scale & 0xffu) << 23);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         bf16x2_t v[4];
@@ -919,9 +922,9 @@ struct Plan {
     int32_t splits, per_split, nt, bm;                      // nt: column tiles of a workgroup, few rows; bm: rows of a tile
 };
 
-// The kernel, and how many parts K is split into, by sizes alone.  us are of
+// The kernel, and how many parts K is split into, by sizes alone (codes: results in 8 bits).  us are of
 // calls in a graph, results in bf16 where nothing else is said.
-Plan plan_product(int64_t M, int64_t N, int64_t nkb, bool exact)
+Plan plan_product(int64_t M, int64_t N, int64_t nkb, bool exact, bool codes = false)
 {
     const int64_t cus = compute_units();
     auto plan = [&](Way way, int64_t s, int64_t unit, int32_t nt, int32_t bm) {
@@ -934,7 +937,9 @@ Plan plan_product(int64_t M, int64_t N, int64_t nkb, bool exact)
     // (14.3), but 64 x 8,192 x 8,192 39 (22).  Wider workgroups read A less often, where there are columns enough:
     // 16 x 16,384 x 4,096 18.1, 15.4 and 13.3 with 1, 2 and 4 tiles of columns, 16 x 8,192 x 8,192 18.1, 14.8 and
     // 16.2, 32 x 16,384 x 16,384 97, 67 and 92 (registers), 32 x 4,096 x 4,096 8.5, 10.6 and 21.
-    if (M <= 32 || (M <= 64 && N * nkb < (1 << 17))) {
+    // Codes need the sums of whole blocks joined, a second launch: up to K = 1,024 a tile does both, 4 x 581 x 126 3.8
+    // us (4.7; called from Python 6.4 and 9.1), 16 x 1,024 x 512 5.1 (5.1), 32 x 1,024 x 1,024 6.9 (6.2; 6.9 and 9.2).
+    if (!(codes && nkb <= 8) && (M <= 32 || (M <= 64 && N * nkb < (1 << 17)))) {
         const int nt = M <= 16 && N >= 64 * cus ? 4 : M <= 32 && N >= 32 * cus ? 2 : 1;
         const int64_t s = cus / ((N + 16 * nt - 1) / (16 * nt));
         return plan(Way::few, s < nkb / 32 ? s : nkb / 32, 1, nt, 0);
@@ -952,8 +957,8 @@ Plan plan_product(int64_t M, int64_t N, int64_t nkb, bool exact)
     int32_t bm = !exact && tiles_of(kBM, kBN) <= cus ? 64 : kBM;
     // Heights in fp32, where K is too short to split instead: the rows that the busiest compute unit gets, a tenth
     // and a fifth more work to a row in the lower ones (8,192 x 8,192 x 2,048: 128 rows 272 us, 64 304, 48 333), and
-    // a workgroup alone has no other to hide its waits.  4,099 x 1,000 x 2,500: 43.9, 39.5 and 34.6 us; 4,096 x
-    // 1,024 x 4,096: 47.0, 43.2, 47.5; 8,192 x 1,000 x 2,500: 45.7, 49.8, 58.5; 1,024 x 1,024 x 1,024: 15.1, 10.1,
+    // a workgroup alone has no other to hide its waits.  4,099 x 1,000 x 2,500: 43.9, 39.5 and 34.6 us (31.5 by now); 4,096 x
+    // 1,024 x 4,096: 47.0, 43.2 (41.2), 47.5; 8,192 x 1,000 x 2,500: 45.7, 49.8, 58.5; 1,024 x 1,024 x 1,024: 15.1, 10.1,
     // 8.7; 512 x 1,024 x 65,536, split: 75.5, 80.8, 99.0.
     if (exact && nkb < 64) {
         auto cost = [&](int64_t m) {
@@ -1056,7 +1061,7 @@ int64_t part_ld(int64_t N) { return (N + 3) / 4 * 4; }
 template <OutKind KIND>
 hipError_t run_product(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const Out &o, void *ws, hipStream_t s)
 {
-    const Plan p = plan_product(A.rows, B.rows, fp8_blocks(A.cols), KIND == kOutF32);
+    const Plan p = plan_product(A.rows, B.rows, fp8_blocks(A.cols), KIND == kOutF32, KIND == kOutFp8);
     if (p.splits == 1 && !(KIND == kOutFp8 && p.way == Way::few)) {
         launch_tiles<KIND == kOutF32, KIND>(A, B, p, o, s);
     } else {
