@@ -1238,11 +1238,18 @@ __global__ __launch_bounds__(NT, 3) void k_sample_waves(const float *__restrict_
 // Few problems of many candidates: each is shared by many workgroups, in
 // passes that hand their results on in the workspace: best score; histogram;
 // candidates around the cut, ranked by one workgroup (once for top-k, once for
-// top-p); sums of parts; draws.  A compute unit takes in some 100 GB/s, so 3
-// problems of 534,600 take 881 us in a workgroup each, 70 so.
+// top-p); sums of parts; draws.  (Ending a pass by its last workgroup instead of a
+// launch: 64 problems of 131,072 82 -> 358 us, its fences write back L2.)  A
+// compute unit takes in some 100 GB/s, so 3
+// problems of 534,600 take 881 us in a workgroup each, 65 so.
 constexpr int kWide = 1024, kWideBins = 4096, kWideNear = 1536, kWideParts = 1024, kWideBlocks = 512;
 
+struct WideBest {                                           // keys of a workgroup's best score and of its least's negative
+    uint32_t best, least, alive, pad;
+};
+
 struct WideState {
+    WideBest best_of[kWideBlocks];
     uint32_t best, least, alive, bin, before_count, n_near, tied_key, pad;
     uint64_t before_mass, want, mass;
     Cut cut;
@@ -1279,29 +1286,18 @@ __device__ __forceinline__ int32_t wide_each(int32_t n)
     return (int32_t)(((int64_t)n + 256 * kWideParts - 1) / (256 * kWideParts));
 }
 
-__global__ __launch_bounds__(256) void k_wide_clear(WideState *state)
-{
-    WideState &st = state[blockIdx.x];
-    for (int i = threadIdx.x; i < kWideBins; i += 256) {
-        st.mass_of[i] = 0;
-        st.count_of[i] = 0;
-    }
-    if (threadIdx.x == 0) {
-        st.best = 0;
-        st.least = 0;
-        st.alive = 0;
-        st.n_near = 0;
-        st.mass = 0;
-        st.cut = {0, 0x7fffffff};
-    }
-}
-
-// Keys: of the best score, and of the least's negative.
+// Best and least score of each workgroup's candidates; clears what the later
+// passes count in.
 __global__ __launch_bounds__(kWide) void k_wide_best(WideArgs a)
 {
     const int32_t p = blockIdx.y;
+    WideState &st = a.state[p];
     const Problem q = problem_of(a.scores, a.R, a.seg, p);
     const Walk walk = shared_walk(q.n);
+    for (int i = (int)blockIdx.x * kWide + (int)threadIdx.x; i < kWideBins; i += (int)gridDim.x * kWide) {
+        st.mass_of[i] = 0;
+        st.count_of[i] = 0;
+    }
     float most = -__builtin_inff(), least = __builtin_inff();
     uint32_t alive = 0;
     each_step(q.s, walk, 0, walk.steps, [&](int32_t, const f32x4u_t &t) {
@@ -1324,18 +1320,21 @@ __global__ __launch_bounds__(kWide) void k_wide_best(WideArgs a)
         atomicAdd(&sh[2], alive);
     }
     __syncthreads();
-    if (threadIdx.x == 0 && sh[2] != 0) {
-        atomicMax(&a.state[p].best, sh[0]);
-        atomicMax(&a.state[p].least, sh[1]);
-        atomicAdd(&a.state[p].alive, sh[2]);
+    if (threadIdx.x == 0) {
+        st.best_of[blockIdx.x] = {sh[0], sh[1], sh[2], 0};
+        if (blockIdx.x == 0) {
+            st.n_near = 0;
+            st.mass = 0;
+            st.cut = {0, 0x7fffffff};
+        }
     }
 }
 
 // A problem with its settings read, and its bins' scale.
-__device__ __forceinline__ float wide_settings(const WideArgs &a, int32_t p, const WideState &st, Problem &q, Limits &lim)
+__device__ __forceinline__ float wide_settings(const WideArgs &a, int32_t p, uint32_t best, uint32_t least, Problem &q, Limits &lim)
 {
-    read_settings(a.set, p, score_of(st.best), q, lim);
-    const float t_least = -exponent_of(q, -score_of(st.least)), span = t_least < 34.0f ? t_least : 34.0f;
+    read_settings(a.set, p, score_of(best), q, lim);
+    const float t_least = -exponent_of(q, -score_of(least)), span = t_least < 34.0f ? t_least : 34.0f;
     return span > 0.0f ? fminf((float)(kWideBins - 1) / span, 1e30f) : 1.0f;
 }
 
@@ -1346,10 +1345,25 @@ __global__ __launch_bounds__(kWide) void k_wide_bins(WideArgs a)
     const int32_t p = blockIdx.y;
     WideState &st = a.state[p];
     Problem q = problem_of(a.scores, a.R, a.seg, p);
-    if (st.alive == 0) return;
+    uint32_t best = 0, least = 0, alive = 0;                // of all workgroups', by each wave
+    for (int i = threadIdx.x & 63; i < (int)gridDim.x; i += 64) {
+        const WideBest b = st.best_of[i];
+        best = b.best > best ? b.best : best;
+        least = b.least > least ? b.least : least;
+        alive += b.alive;
+    }
+    best = wave_max(best);
+    least = wave_max(least);
+    alive = wave_sum(alive);
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        st.best = best;
+        st.least = least;
+        st.alive = alive;
+    }
+    if (alive == 0) return;
     Limits lim;
-    const float bin_scale = wide_settings(a, p, st, q, lim);
-    const bool by_count = lim.k < st.alive;
+    const float bin_scale = wide_settings(a, p, best, least, q, lim);
+    const bool by_count = lim.k < alive;
     if (!by_count && !(lim.top_p < 1.0f)) return;
     const Walk walk = shared_walk(q.n);
     for (int i = threadIdx.x; i < kWideBins; i += kWide) {
@@ -1391,7 +1405,7 @@ __global__ __launch_bounds__(kWide) void k_wide_find(WideArgs a, int turn)
     }
     if (st.alive == 0) return;
     Limits lim;
-    const float bin_scale = wide_settings(a, p, st, q, lim);
+    const float bin_scale = wide_settings(a, p, st.best, st.least, q, lim);
     if (turn ? !(lim.top_p < 1.0f) : !(lim.k < st.alive)) return;
     // 4,096 scores from here and there, among which one that many share will be found (16,384 singly: 14 us more)
     constexpr int kLook = 4;
@@ -1453,7 +1467,7 @@ __global__ __launch_bounds__(kWide) void k_wide_list(WideArgs a)
     if (st.alive == 0 || st.want == 0) return;
     Problem q = problem_of(a.scores, a.R, a.seg, p);
     Limits lim;
-    const float bin_scale = wide_settings(a, p, st, q, lim);
+    const float bin_scale = wide_settings(a, p, st.best, st.least, q, lim);
     const uint32_t bin = st.bin, tied_key = st.tied_key;
     const Walk walk = shared_walk(q.n);
     uint32_t tied = 0;
@@ -1482,7 +1496,7 @@ __global__ __launch_bounds__(kWide) void k_wide_cut(WideArgs a, int turn, int32_
     if (st.alive == 0 || st.want == 0) return;
     Problem q = problem_of(a.scores, a.R, a.seg, p);
     Limits lim;
-    const float bin_scale = wide_settings(a, p, st, q, lim);
+    const float bin_scale = wide_settings(a, p, st.best, st.least, q, lim);
     const uint32_t m = st.n_near;
     uint64_t upto;
     Cut cut;
@@ -1544,7 +1558,7 @@ __global__ __launch_bounds__(kWide) void k_wide_sums(WideArgs a)
     if (st.alive == 0) return;
     Problem q = problem_of(a.scores, a.R, a.seg, p);
     Limits lim;
-    wide_settings(a, p, st, q, lim);
+    wide_settings(a, p, st.best, st.least, q, lim);
     const Cut cut = st.cut;
     const int32_t each = wide_each(q.n), parts = (int32_t)(((int64_t)q.n + 256 * (int64_t)each - 1) / (256 * (int64_t)each));
     for (int32_t e = __builtin_amdgcn_readfirstlane((int)blockIdx.x * (kWide / 64) + (threadIdx.x >> 6)); e < parts;
@@ -1591,7 +1605,7 @@ __global__ __launch_bounds__(kWide) void k_wide_draw(WideArgs a, const float *__
     }
     Problem q = problem_of(a.scores, a.R, a.seg, p);
     Limits lim;
-    wide_settings(a, p, st, q, lim);
+    wide_settings(a, p, st.best, st.least, q, lim);
     const Cut cut = st.cut;
     const int32_t each = wide_each(q.n), parts = (int32_t)(((int64_t)q.n + 256 * (int64_t)each - 1) / (256 * (int64_t)each));
     const uint64_t own = (int)threadIdx.x < parts ? st.part[threadIdx.x] : 0, scan = wave_scan(own);
@@ -1647,11 +1661,10 @@ static void launch_shared(const WideArgs &a, int32_t P, const float *u, int32_t 
     int64_t blocks = (a.R + 16383) / 16384;
     for (const int64_t most : {(2 * (int64_t)compute_units() + P - 1) / P, (int64_t)kWideBlocks}) blocks = blocks < most ? blocks : most;
     const dim3 shared((unsigned)blocks, (unsigned)P), one((unsigned)P), block(kWide);
-    hipLaunchKernelGGL(k_wide_clear, one, dim3(256), 0, s, a.state);
     hipLaunchKernelGGL(k_wide_best, shared, block, 0, s, a);
     const bool by_count = a.set.how.top_k_of || a.set.how.top_k > 0 || a.set.how.temperature_of || !(a.set.how.temperature > 0.0f),
                by_mass = a.set.how.top_p_of || a.set.how.top_p < 1.0f;
-    if (by_count || by_mass) hipLaunchKernelGGL(k_wide_bins, shared, block, 0, s, a);
+    hipLaunchKernelGGL(k_wide_bins, shared, block, 0, s, a);  // (also where no prefix is wanted: it says which score is the best)
     for (int turn = 0; turn < 2; ++turn) {
         if (!(turn ? by_mass : by_count)) continue;
         hipLaunchKernelGGL(k_wide_find, one, block, 0, s, a, turn);
