@@ -1238,10 +1238,10 @@ __global__ __launch_bounds__(NT, 3) void k_sample_waves(const float *__restrict_
 // Few problems of many candidates: each is shared by many workgroups, in
 // passes that hand their results on in the workspace: best score; histogram;
 // candidates around the cut, ranked by one workgroup (once for top-k, once for
-// top-p); sums of parts; draws.  (Ending a pass by its last workgroup instead of a
-// launch: 64 problems of 131,072 82 -> 358 us, its fences write back L2.)  A
-// compute unit takes in some 100 GB/s, so 3
-// problems of 534,600 take 881 us in a workgroup each, 65 so.
+// top-p); sums of parts; draws.  A compute unit takes in some 100 GB/s, so 3
+// problems of 534,600 take 881 us in a workgroup each, 53 so.  (Ending a pass
+// by its last workgroup instead of a launch: 64 problems of 131,072 82 -> 358
+// us, its fences write back L2.)
 constexpr int kWide = 1024, kWideBins = 4096, kWideNear = 1536, kWideParts = 1024, kWideBlocks = 512;
 
 struct WideBest {                                           // keys of a workgroup's best score and of its least's negative
