@@ -504,8 +504,8 @@ int hwsel_catalogue_candidates(const hwsel_problem_t *problems, int32_t P, const
  *               code 0 (the entry points that write a matrix write them so).
  *   scale       exponent bytes, uint8 [ceil(rows / block_rows)][ld_scale],
  *               4-byte aligned, ld_scale % 4 == 0, ld_scale >= ceil(cols /
- *               128); 255 stands for NaN.  Bytes past the blocks are not
- *               used.
+ *               128); 255 stands for NaN.  Bytes past the blocks, up to a
+ *               multiple of four, may be written and are not read.
  *   format      HWSEL_FP8_E4M3 (largest value 448, no infinity) or
  *               HWSEL_FP8_E5M2 (57344, with infinities).
  *   block_rows  1 (a scale for each row's 128 columns: activations,

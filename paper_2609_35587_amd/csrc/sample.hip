@@ -464,32 +464,41 @@ __device__ __forceinline__ void near_weights(uint32_t w, uint32_t &lo, uint32_t 
     hi = w < 0xffffffffu - slack ? w + slack : 0xffffffffu;
 }
 
-// The cut among the m candidates listed in lds.near, those of the bin, and the
-// tied ones: they are ranked.  The count (by_mass: mass) before the bin is given.
-// If the cut is among the tied ones its index is left open: ties says the
-// how-manieth of them it is (else 0).
+// A candidate as it is ranked: the larger, the better.
+__device__ __forceinline__ uint64_t rank_of(float s, uint32_t i) { return ((uint64_t)key_of(s) << 32) | (0xffffffffu - i); }
+
+// The m candidates of lds.near to lds.list, 0 for those that are not of the bin,
+// and how many of each wave's are.
 template <int NT, class L>
-__device__ __forceinline__ Cut rank_bin(const Problem &q, float bin_scale, uint32_t bin, uint32_t m, const Tied &tied, bool by_mass,
-                                        uint32_t before_count, uint64_t before_mass, uint64_t want, uint64_t &mass, uint32_t &ties,
-                                        L &lds)
+__device__ __forceinline__ void list_bin(const Problem &q, float bin_scale, uint32_t bin, uint32_t m, L &lds)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     uint32_t in_bin = 0;
     for (uint32_t e = threadIdx.x; e < m; e += NT) {
         const uint32_t i = lds.near[e];
         const float v = q.s[i];
         const bool in = (uint32_t)(-exponent_of(q, v) * bin_scale) == bin;
-        lds.list[e] = in ? ((uint64_t)key_of(v) << 32) | (0xffffffffu - i) : 0;
+        lds.list[e] = in ? rank_of(v, i) : 0;
         in_bin += in;
     }
     in_bin = wave_sum(in_bin);
-    if (lane == 0) lds.wave_count[wave] = in_bin;
+    if ((threadIdx.x & 63) == 0) lds.wave_count[threadIdx.x >> 6] = in_bin;
+}
+
+// The cut among the m candidates of lds.list and the tied ones: they are ranked.
+// The count (by_mass: mass) before the bin is given.  If the cut is among the
+// tied ones its index is left open: ties says the how-manieth of them it is (else 0).
+template <int NT, class L>
+__device__ __forceinline__ Cut rank_bin(const Problem &q, uint32_t m, const Tied &tied, bool by_mass,
+                                        uint32_t before_count, uint64_t before_mass, uint64_t want, uint64_t &mass, uint32_t &ties,
+                                        L &lds)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (tied.key != 0) {                                    // one entry for all of them
         if (threadIdx.x == 0) lds.list[m] = (uint64_t)tied.key << 32;
         ++m;
     }
     __syncthreads();
-    in_bin = tied.key != 0;
+    uint32_t in_bin = tied.key != 0;
 #pragma unroll
     for (int o = 0; o < NT / 64; ++o) in_bin += lds.wave_count[o];
     for (uint32_t e = threadIdx.x; e < m; e += NT) {
@@ -775,7 +784,8 @@ __device__ __forceinline__ void sample_problem(Lds<NT, BINS, CACHED> &lds, int32
             }
             if (m + (tied.key != 0) <= kList) {
                 uint32_t ties;
-                cut = rank_bin<NT>(q, bin_scale, bin, m, tied, turn, c, before, want, upto, ties, lds);
+                list_bin<NT>(q, bin_scale, bin, m, lds);
+                cut = rank_bin<NT>(q, m, tied, turn, c, before, want, upto, ties, lds);
                 if (ties != 0) {
                     if (ties > tied_before && ties <= tied_before + tied_here) {
                         const int32_t at = tied_at<4>(q, walk, 0, walk.steps, cut.key, ties - tied_before);
@@ -1254,7 +1264,8 @@ struct WideState {
     uint64_t before_mass, want, mass;
     Cut cut;
     uint64_t mass_of[kWideBins], part[kWideParts];
-    uint32_t count_of[kWideBins], near[kWideNear], kept_of[kWideParts];
+    uint64_t near[kWideNear];                               // as they are ranked
+    uint32_t count_of[kWideBins], kept_of[kWideParts];
     uint32_t tied_of[kWideBlocks * (kWide / 64)];           // of each wave
 };
 
@@ -1450,6 +1461,7 @@ __global__ __launch_bounds__(kWide) void k_wide_find(WideArgs a, int turn)
             if (at < 64) lds.near[at] = key_of(look[j]);
         }
     __syncthreads();
+    if (wave != 0) return;
     const uint32_t tied_key = commonest((uint32_t)lane < lds.n_near ? lds.near[lane] : 0);
     if (threadIdx.x == 0) {
         st.want = want;
@@ -1480,7 +1492,7 @@ __global__ __launch_bounds__(kWide) void k_wide_list(WideArgs a)
                     continue;
                 }
                 const uint32_t at = atomicAdd(&st.n_near, 1u);
-                if (at < kWideNear) st.near[at] = (uint32_t)(walk.base + i * 256 + lane * 4 + c);
+                if (at < kWideNear) st.near[at] = rank_of(t[c], (uint32_t)(walk.base + i * 256 + lane * 4 + c));
             }
     });
     tied = wave_sum(tied);
@@ -1493,10 +1505,14 @@ __global__ __launch_bounds__(kWide) void k_wide_cut(WideArgs a, int turn, int32_
     static_assert(Lds<kWide, kWideBins, 4>::kList == kWideNear, "the list fits");
     const int32_t p = blockIdx.x;
     WideState &st = a.state[p];
+    constexpr int kNear = (kWideNear + kWide - 1) / kWide;  // (on their way before it is known how many there are)
+    uint64_t near[kNear];
+#pragma unroll
+    for (int i = 0; i < kNear; ++i) near[i] = threadIdx.x + i * kWide < kWideNear ? st.near[threadIdx.x + i * kWide] : 0;
     if (st.alive == 0 || st.want == 0) return;
     Problem q = problem_of(a.scores, a.R, a.seg, p);
     Limits lim;
-    const float bin_scale = wide_settings(a, p, st.best, st.least, q, lim);
+    wide_settings(a, p, st.best, st.least, q, lim);
     const uint32_t m = st.n_near;
     uint64_t upto;
     Cut cut;
@@ -1519,10 +1535,12 @@ __global__ __launch_bounds__(kWide) void k_wide_cut(WideArgs a, int turn, int32_
     if (tied.count == 0) tied.key = 0;
     __syncthreads();
     if (m + (tied.key != 0) <= kWideNear) {
-        for (uint32_t e = threadIdx.x; e < m; e += kWide) lds.near[e] = st.near[e];
-        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kNear; ++i)
+            if (threadIdx.x + i * kWide < m) lds.list[threadIdx.x + i * kWide] = near[i];
+        if (threadIdx.x < kWide / 64) lds.wave_count[threadIdx.x] = threadIdx.x == 0 ? m : 0;
         uint32_t ties;
-        cut = rank_bin<kWide>(q, bin_scale, st.bin, m, tied, turn, st.before_count, st.before_mass, st.want, upto, ties, lds);
+        cut = rank_bin<kWide>(q, m, tied, turn, st.before_count, st.before_mass, st.want, upto, ties, lds);
         if (ties != 0) {                                    // which wave's it is, and what is before that wave
             if (ties > before && ties <= before + here) {
                 int w = (int)threadIdx.x * own;
