@@ -1736,13 +1736,18 @@ hipError_t launch_sample(const float *scores, int64_t R, const int64_t *seg, int
     if (shared_problems(R, P))
         launch_shared(WideArgs{scores, R, seg, static_cast<WideState *>(ws), Settings{how, n_draws}}, P, u, idx, prob, kept, s);
     else if (R / P <= kSmallMean) launch_waves(scores, R, seg, P, how, u, n_draws, idx, prob, kept, s);
-    // Where problems outnumber compute units, three workgroups of 256 threads share one; up to 8,192 candidates otherwise,
-    // 512 threads wait for each other less than 1,024, which keep three times as many candidates in LDS.  600 problems
-    // of up to 8,192 with 64 draws 26.8 us (512 threads: 29.6), 600 of 4,000 21.1 (26.8), 2,000 of 8,192 72 (72), 600 of up to 16,384 42 (44); 16 of 4,000 15.0 (256 threads: 16.9), 128 of 8,192 16.8 (1,024
-    // threads: 17.6), but 8 of 12,288 21.2 (19.4) and 256 of 24,576 33 (26).
-    else if (P > compute_units()) launch_problems<256, 1024, 8192, 3>(scores, R, seg, P, how, u, n_draws, idx, prob, kept, s);
+    // Where problems outnumber compute units, three workgroups share one, of 256 threads for up to 12,288 candidates and
+    // of 512 (in 80 registers) for more: 600 problems of up to 8,192 with 64 draws 26.8 us (512: 29.6), 600 of 4,000
+    // 21.1 (26.8), 600 of 12,000 37.8 (42.7), 600 of 16,384 44.0 (44.2), but 300 of 16,000 40 (36), 300 of 65,536 134
+    // (103; 1,024 threads: 125), 2,000 of 32,768 218 (193; 305).  Otherwise 512 up to 8,192 candidates, which wait for
+    // each other less than 1,024, which keep more than three times as many candidates in LDS: 16 of 4,000 15.0 (256
+    // threads: 16.9), 128 of 8,192 16.8 (1,024 threads: 17.6), but 8 of 12,288 21.2 (19.4) and 256 of 24,576 33 (26).
+    else if (P > compute_units()) {
+        if (R / P <= 12288) launch_problems<256, 1024, 8192, 3>(scores, R, seg, P, how, u, n_draws, idx, prob, kept, s);
+        else launch_problems<512, 1024, 8192, 6>(scores, R, seg, P, how, u, n_draws, idx, prob, kept, s);
+    }
     else if (R / P <= 8192) launch_problems<512, 1024, 8192, 4>(scores, R, seg, P, how, u, n_draws, idx, prob, kept, s);
-    else launch_problems<1024, 2048, 24576, 4>(scores, R, seg, P, how, u, n_draws, idx, prob, kept, s);
+    else launch_problems<1024, 2048, 28672, 4>(scores, R, seg, P, how, u, n_draws, idx, prob, kept, s);
     return hipGetLastError();
 }
 

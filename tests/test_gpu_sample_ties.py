@@ -46,7 +46,7 @@ def test_against_the_definition(kind, n):
         sample.check(parts, sample.uniform(rng, 2, 3), top_k=k)
 
 
-@pytest.mark.parametrize("n", [900, 4000, 70_000])
+@pytest.mark.parametrize("n", [900, 4000, 13_000, 70_000])
 def test_more_problems_than_compute_units(n):
     """Against the same problems one at a time."""
     P = 300 if n < 50_000 else 20
