@@ -141,14 +141,16 @@ int32_t dtype_code(at::ScalarType t, const char *name)
     return t == at::kFloat ? HWSEL_DTYPE_FP32 : HWSEL_DTYPE_BF16;
 }
 
+// The step between rows goes on as it is where there are several: a matrix whose
+// rows overlap (an unfold view, say) is refused, not read at another step.
 Plain plain(const at::Tensor &t, const char *name, int64_t rows, int64_t cols, int device)
 {
     if (!t.is_cuda() || t.dim() != 2 || t.get_device() != device) refuse("%s must be a 2-D device tensor on device %d", name, device);
     const int32_t code = dtype_code(t.scalar_type(), name);
     const int64_t r = t.size(0), c = t.size(1), step = t.stride(0);
-    if ((c > 1 && t.stride(1) != 1) || r < rows || c < cols || (r > 1 && step < cols))
-        refuse("%s must be at least [%lld][%lld], with unit column stride", name, (long long)rows, (long long)cols);
-    return {t.data_ptr(), code, r, c, step > c ? step : c};
+    if ((c > 1 && t.stride(1) != 1) || r < rows || c < cols || (r > 1 && step < c))
+        refuse("%s must be at least [%lld][%lld], with unit column stride and rows that do not overlap", name, (long long)rows, (long long)cols);
+    return {t.data_ptr(), code, r, c, r > 1 ? step : c};    // (torch gives the step of a single row any value)
 }
 
 const at::Tensor &tensor(PyObject *o, const char *name)
