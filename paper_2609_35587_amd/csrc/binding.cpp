@@ -10,6 +10,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/hip/HIPCachingAllocator.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
@@ -17,6 +18,7 @@
 
 #include <cstdint>
 #include <cstring>
+#include <optional>
 #include <utility>
 
 #include "hwsel.h"
@@ -101,12 +103,54 @@ int32_t int32_of(int64_t v, const char *name)
 hipStream_t stream_of(PyObject *stream)
 {
     if (stream == Py_None) return c10::hip::getCurrentHIPStream().stream();
-    if (PyLong_Check(stream)) return reinterpret_cast<hipStream_t>(PyLong_AsVoidPtr(stream));
-    const Ref s(must(PyObject_GetAttr(stream, k_stream)));
-    void *p = PyLong_AsVoidPtr(s.get());
+    const Ref number(PyLong_Check(stream) ? Py_NewRef(stream) : must(PyObject_GetAttr(stream, k_stream)));
+    void *p = PyLong_AsVoidPtr(number.get());
     if (!p && PyErr_Occurred()) throw Failed{};
     return static_cast<hipStream_t>(p);
 }
+
+// The stream of a call, and what the call allocates.  torch hands memory that was
+// freed to the next allocation of the same stream without waiting, so a call on
+// another stream than the current one allocates on that one: nothing of the
+// current stream still uses what it gets, and its workspace, freed on return,
+// goes to later work of the same stream.  Results are the caller's, who uses
+// them on the current stream: they are noted there too.
+class Queue {
+public:
+    Queue(PyObject *given, int device) : device_(device), stream_(stream_of(given))
+    {
+        if (given == Py_None) return;
+        const auto current = c10::hip::getCurrentHIPStream((c10::DeviceIndex)device);
+        if (current.stream() == stream_) return;
+        current_ = current;
+        c10::hip::setCurrentHIPStream(c10::hip::getStreamFromExternal(stream_, (c10::DeviceIndex)device));
+    }
+    ~Queue()
+    {
+        if (current_) c10::hip::setCurrentHIPStream(*current_);
+    }
+    Queue(const Queue &) = delete;
+    Queue &operator=(const Queue &) = delete;
+
+    hipStream_t stream() const { return stream_; }
+    at::Tensor workspace(int64_t bytes) const { return empty({bytes}, at::kByte); }
+    at::Tensor result(at::IntArrayRef sizes, at::ScalarType type) const
+    {
+        at::Tensor t = empty(sizes, type);
+        if (current_ && t.numel() != 0) c10::hip::HIPCachingAllocator::recordStream(t.storage().data_ptr(), *current_);
+        return t;
+    }
+
+private:
+    at::Tensor empty(at::IntArrayRef sizes, at::ScalarType type) const
+    {
+        return at::empty(sizes, at::TensorOptions().dtype(type).device(at::kCUDA, (c10::DeviceIndex)device_));
+    }
+
+    int device_;
+    hipStream_t stream_;
+    std::optional<c10::hip::HIPStream> current_;            // torch's, where the call is on another
+};
 
 // A contiguous device tensor of dtype `type` with at least numel elements, on
 // device `device` (-1: any).
@@ -197,17 +241,12 @@ Fp8 fp8(PyObject *m, const char *name, int device = -1)
             device};
 }
 
-at::Tensor empty(at::IntArrayRef sizes, at::ScalarType type, int device)
-{
-    return at::empty(sizes, at::TensorOptions().dtype(type).device(at::kCUDA, (c10::DeviceIndex)device));
-}
-
 // Buffers of an 8-bit matrix as a dict, and what the C functions take.
-PyObject *fp8_empty(int64_t rows, int64_t cols, int64_t format, int64_t block_rows, int device, Fp8 &to)
+PyObject *fp8_empty(int64_t rows, int64_t cols, int64_t format, int64_t block_rows, const Queue &queue, int device, Fp8 &to)
 {
     if (rows < 1 || cols < 1) refuse("a matrix of %lld x %lld", (long long)rows, (long long)cols);
     const int64_t width = up(cols, HWSEL_FP8_BLOCK), words = up(width / HWSEL_FP8_BLOCK, 4), high = block_rows > 1 ? block_rows : 1;
-    const at::Tensor q = empty({rows, width}, at::kByte, device), s = empty({(rows + high - 1) / high, words}, at::kByte, device);
+    const at::Tensor q = queue.result({rows, width}, at::kByte), s = queue.result({(rows + high - 1) / high, words}, at::kByte);
     to = {{rows, cols, static_cast<uint8_t *>(q.data_ptr()), width, static_cast<uint8_t *>(s.data_ptr()), words,
            int32_of(format, "format"), int32_of(block_rows, "block_rows")},
           device};
@@ -238,7 +277,7 @@ struct Workspace {
     size_t bytes = 0;
 };
 
-Workspace workspace_of(PyObject *given, size_t need, int device)
+Workspace workspace_of(PyObject *given, size_t need, const Queue &queue, int device)
 {
     Workspace w;
     if (given != Py_None) {
@@ -246,18 +285,18 @@ Workspace workspace_of(PyObject *given, size_t need, int device)
         w.data = t.data_ptr();
         w.bytes = (size_t)t.numel();
     } else if (need != 0) {
-        w.own = empty({(int64_t)need}, at::kByte, device);
+        w.own = queue.workspace((int64_t)need);
         w.data = w.own.data_ptr();
         w.bytes = need;
     }
     return w;
 }
 
-Workspace product_workspace(PyObject *given, const Fp8 &a, const Fp8 &b)
+Workspace product_workspace(PyObject *given, const Fp8 &a, const Fp8 &b, const Queue &queue)
 {
     size_t need = 0;
     if (given == Py_None) check("hwsel_fp8_matmul_workspace_bytes", lib.matmul_workspace_bytes(&a.c, &b.c, &need));
-    return workspace_of(given, need, a.device);
+    return workspace_of(given, need, queue, a.device);
 }
 
 // (X, format, block_rows, transpose, mean, inv_std, out, stream)
@@ -266,6 +305,7 @@ PyObject *quantise(PyObject *const *v)
     const at::Tensor &X = tensor(v[0], "X");
     const Plain x = plain(X, "X", 1, 1, X.is_cuda() ? X.get_device() : 0);
     const int device = X.get_device();
+    const Queue queue(v[7], device);
     const int64_t format = integer(v[1]), block_rows = integer(v[2]);
     const int transpose = PyObject_IsTrue(v[3]);
     if (transpose < 0) throw Failed{};
@@ -275,14 +315,14 @@ PyObject *quantise(PyObject *const *v)
     Fp8 to;
     Ref out;
     if (v[6] == Py_None) {
-        out = Ref(fp8_empty(rows, cols, format, block_rows, device, to));
+        out = Ref(fp8_empty(rows, cols, format, block_rows, queue, device, to));
     } else {
         to = fp8(v[6], "out", device);
         if (to.c.rows != rows || to.c.cols != cols || to.c.format != format || to.c.block_rows != block_rows)
             refuse("out is not a %lld x %lld matrix of this format and block_rows", (long long)rows, (long long)cols);
         out = Ref(keep(v[6]));
     }
-    check("hwsel_fp8_quantise", lib.quantise(x.data, x.dtype, x.ld, transpose, mean, inv_std, &to.c, stream_of(v[7])));
+    check("hwsel_fp8_quantise", lib.quantise(x.data, x.dtype, x.ld, transpose, mean, inv_std, &to.c, queue.stream()));
     return out.release();
 }
 
@@ -293,7 +333,7 @@ at::ScalarType dtype_of(PyObject *o)
 }
 
 // The caller's matrix for a result, or a new one.
-Plain result(PyObject *given, int64_t rows, int64_t cols, PyObject *dtype, int device, Ref &out)
+Plain result(PyObject *given, int64_t rows, int64_t cols, PyObject *dtype, const Queue &queue, int device, Ref &out)
 {
     if (given != Py_None) {
         out = Ref(keep(given));
@@ -301,7 +341,7 @@ Plain result(PyObject *given, int64_t rows, int64_t cols, PyObject *dtype, int d
     }
     const at::ScalarType type = dtype_of(dtype);
     const int32_t code = dtype_code(type, "out");
-    const at::Tensor t = empty({rows, cols}, type, device);
+    const at::Tensor t = queue.result({rows, cols}, type);
     out = Ref(must(THPVariable_Wrap(t)));
     return {t.data_ptr(), code, rows, cols, cols};
 }
@@ -310,9 +350,10 @@ Plain result(PyObject *given, int64_t rows, int64_t cols, PyObject *dtype, int d
 PyObject *dequantise(PyObject *const *v)
 {
     const Fp8 m = fp8(v[0], "m");
+    const Queue queue(v[3], m.device);
     Ref out;
-    const Plain to = result(v[2], m.c.rows, m.c.cols, v[1], m.device, out);
-    check("hwsel_fp8_dequantise", lib.dequantise(&m.c, to.data, to.dtype, to.ld, stream_of(v[3])));
+    const Plain to = result(v[2], m.c.rows, m.c.cols, v[1], queue, m.device, out);
+    check("hwsel_fp8_dequantise", lib.dequantise(&m.c, to.data, to.dtype, to.ld, queue.stream()));
     return out.release();
 }
 
@@ -320,15 +361,16 @@ PyObject *dequantise(PyObject *const *v)
 PyObject *transpose(PyObject *const *v)
 {
     const Fp8 m = fp8(v[0], "m");
+    const Queue queue(v[4], m.device);
     Fp8 to;
     Ref out;
     if (v[3] == Py_None) {
-        out = Ref(fp8_empty(m.c.cols, m.c.rows, integer(v[1]), integer(v[2]), m.device, to));
+        out = Ref(fp8_empty(m.c.cols, m.c.rows, integer(v[1]), integer(v[2]), queue, m.device, to));
     } else {
         to = fp8(v[3], "out", m.device);
         out = Ref(keep(v[3]));
     }
-    check("hwsel_fp8_transpose", lib.transpose(&m.c, &to.c, stream_of(v[4])));
+    check("hwsel_fp8_transpose", lib.transpose(&m.c, &to.c, queue.stream()));
     return out.release();
 }
 
@@ -352,11 +394,12 @@ PyObject *matmul_workspace_bytes(PyObject *const *v)
 PyObject *matmul(PyObject *const *v)
 {
     const Fp8 a = fp8(v[0], "A"), b = fp8(v[1], "B", a.device);
+    const Queue queue(v[7], a.device);
     Ref out;
-    const Plain to = result(v[5], a.c.rows, b.c.rows, v[2], a.device, out);
+    const Plain to = result(v[5], a.c.rows, b.c.rows, v[2], queue, a.device, out);
     const auto *bias = static_cast<const float *>(argument_or_null(v[3], "bias", at::kFloat, b.c.rows, a.device));
-    const Workspace w = product_workspace(v[6], a, b);
-    check("hwsel_fp8_matmul", lib.matmul(&a.c, &b.c, bias, activation(v[4]), to.data, to.dtype, to.ld, w.data, w.bytes, stream_of(v[7])));
+    const Workspace w = product_workspace(v[6], a, b, queue);
+    check("hwsel_fp8_matmul", lib.matmul(&a.c, &b.c, bias, activation(v[4]), to.data, to.dtype, to.ld, w.data, w.bytes, queue.stream()));
     return out.release();
 }
 
@@ -364,17 +407,18 @@ PyObject *matmul(PyObject *const *v)
 PyObject *layer(PyObject *const *v)
 {
     const Fp8 a = fp8(v[0], "A"), b = fp8(v[1], "B", a.device);
+    const Queue queue(v[6], a.device);
     Fp8 to;
     Ref out;
     if (v[4] == Py_None) {
-        out = Ref(fp8_empty(a.c.rows, b.c.rows, HWSEL_FP8_E4M3, 1, a.device, to));
+        out = Ref(fp8_empty(a.c.rows, b.c.rows, HWSEL_FP8_E4M3, 1, queue, a.device, to));
     } else {
         to = fp8(v[4], "out", a.device);
         out = Ref(keep(v[4]));
     }
     const auto *bias = static_cast<const float *>(argument_or_null(v[2], "bias", at::kFloat, b.c.rows, a.device));
-    const Workspace w = product_workspace(v[5], a, b);
-    check("hwsel_fp8_layer", lib.layer(&a.c, &b.c, bias, activation(v[3]), &to.c, w.data, w.bytes, stream_of(v[6])));
+    const Workspace w = product_workspace(v[5], a, b, queue);
+    check("hwsel_fp8_layer", lib.layer(&a.c, &b.c, bias, activation(v[3]), &to.c, w.data, w.bytes, queue.stream()));
     return out.release();
 }
 
@@ -395,6 +439,7 @@ PyObject *sample(PyObject *const *v)
 {
     const at::Tensor &scores = argument(v[0], "scores", at::kFloat, 0, -1);
     const int device = scores.get_device();
+    const Queue queue(v[11], device);
     const at::Tensor &seg = argument(v[1], "seg_offsets", at::kLong, 2, device);
     const at::Tensor &u = argument(v[2], "u", at::kFloat, 0, device);
     const int64_t P = seg.size(0) - 1, R = scores.numel();
@@ -416,7 +461,7 @@ PyObject *sample(PyObject *const *v)
             data = argument(given, name, type, numel, device).data_ptr();
             return Ref(keep(given));
         }
-        const at::Tensor t = empty(sizes, type, device);
+        const at::Tensor t = queue.result(sizes, type);
         data = t.data_ptr();
         return Ref(must(THPVariable_Wrap(t)));
     };
@@ -426,11 +471,11 @@ PyObject *sample(PyObject *const *v)
     size_t need = 0;
     check("hwsel_sample_workspace_bytes", lib.sample_workspace_bytes(R, p32, draws32, &need));
     if (v[10] != Py_None) argument(v[10], "workspace", at::kByte, (int64_t)need, device);
-    const Workspace w = workspace_of(v[10], need, device);
+    const Workspace w = workspace_of(v[10], need, queue, device);
     check("hwsel_sample_per_problem",
           lib.sample(static_cast<const float *>(scores.data_ptr()), R, static_cast<const int64_t *>(seg.data_ptr()), p32, &how,
                      static_cast<const float *>(u.data_ptr()), draws32, static_cast<int32_t *>(idx_at), static_cast<float *>(prob_at),
-                     static_cast<int32_t *>(kept_at), w.data, w.bytes, stream_of(v[11])));
+                     static_cast<int32_t *>(kept_at), w.data, w.bytes, queue.stream()));
     return must(PyTuple_Pack(3, idx.get(), prob.get(), kept.get()));
 }
 
