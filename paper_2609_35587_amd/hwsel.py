@@ -175,6 +175,19 @@ def _stream(stream) -> int | None:
     return stream.cuda_stream
 
 
+def _empty(shape, dtype: torch.dtype, device, stream) -> torch.Tensor:
+    """A result or workspace of a call on ``stream``.  torch hands freed memory
+    to the next allocation of the same stream without waiting, so on a stream
+    other than the current one it is that stream's, noted on the current one."""
+    current = None if stream is None else torch.cuda.current_stream(device)
+    if current is None or _stream(stream) == current.cuda_stream:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(torch.cuda.ExternalStream(_stream(stream), device=device)):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(current)
+    return t
+
+
 def _dev(t: torch.Tensor, name: str) -> torch.Tensor:
     if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous device tensor")
@@ -243,7 +256,7 @@ def hwsel_features(hw: dict, problems: torch.Tensor, seg_offsets: torch.Tensor, 
     P = problems.shape[0]
     R = cands["tile_m"].shape[0]
     if X is None:
-        X = torch.empty((R, n_features), dtype=torch.float32, device=problems.device)
+        X = _empty((R, n_features), torch.float32, problems.device, stream)
     _matrix(X, "X", n_features, like=problems)
     if X.shape[0] < R:
         raise ValueError(f"X has {X.shape[0]} rows, {R} candidates")
@@ -267,7 +280,7 @@ def hwsel_sample_score(hw: dict, problems: torch.Tensor, seg_offsets: torch.Tens
     P = problems.shape[0]
     R = cands["tile_m"].shape[0]
     if scores is None:
-        scores = torch.empty(R, dtype=torch.float32, device=problems.device)
+        scores = _empty(R, torch.float32, problems.device, stream)
     _arg(scores, "scores", F32, R, problems)
     cs = _cands_struct(cands, R, problems)
     _check("hwsel_sample_score", lib().hwsel_sample_score(
@@ -287,7 +300,7 @@ def hwsel_linear_score(lin: dict, X: torch.Tensor, scores: torch.Tensor | None =
     F = int(lin["n_features"])
     _matrix(X, "X", F)
     if scores is None:
-        scores = torch.empty(R, dtype=torch.float32, device=X.device)
+        scores = _empty(R, torch.float32, X.device, stream)
     _arg(scores, "scores", F32, R, X)
     for n in ("mean", "inv_std", "w"):
         _arg(lin[n], n, F32, F, X)
@@ -316,7 +329,7 @@ def hwsel_forest_pack(forest: dict, packed: torch.Tensor | None = None, stream=N
     nbytes = hwsel_forest_pack_bytes(forest)
     _forest_arrays(forest)
     if packed is None:
-        packed = torch.empty(nbytes, dtype=torch.uint8, device=forest["node_feature"].device)
+        packed = _empty(nbytes, torch.uint8, forest["node_feature"].device, stream)
     _arg(packed, "packed", U8, nbytes, forest["node_feature"])
     s = forest_struct(forest)
     _check("hwsel_forest_pack", lib().hwsel_forest_pack(C.byref(s), _ptr(packed), packed.numel(),
@@ -369,13 +382,13 @@ def hwsel_forest_score(forest: dict, X: torch.Tensor, scores: torch.Tensor | Non
     _matrix(X, "X", int(forest["n_features"]))
     _forest_arrays(forest)
     if scores is None:
-        scores = torch.empty(R, dtype=torch.float32, device=X.device)
+        scores = _empty(R, torch.float32, X.device, stream)
     _arg(scores, "scores", F32, R, X)
     ws_bytes = 0
     if packed is not None:
         _packed_image(forest, packed, X)
         if workspace is None:
-            workspace = torch.empty(hwsel_forest_workspace_bytes(forest, R), dtype=torch.uint8, device=X.device)
+            workspace = _empty(hwsel_forest_workspace_bytes(forest, R), torch.uint8, X.device, stream)
         _arg(workspace, "workspace", U8, 0, X)
         ws_bytes = workspace.numel() * workspace.element_size()
     s = forest_struct(forest)
@@ -396,16 +409,16 @@ def hwsel_forest_score_checked(forest: dict, X: torch.Tensor, packed: torch.Tens
     _forest_arrays(forest)
     _packed_image(forest, packed, X)
     if scores is None:
-        scores = torch.empty(R, dtype=torch.float32, device=X.device)
+        scores = _empty(R, torch.float32, X.device, stream)
     _arg(scores, "scores", F32, R, X)
     if workspace is None:
-        workspace = torch.empty(hwsel_forest_workspace_bytes(forest, R), dtype=torch.uint8, device=X.device)
+        workspace = _empty(hwsel_forest_workspace_bytes(forest, R), torch.uint8, X.device, stream)
     _arg(workspace, "workspace", U8, 0, X)
-    lh = torch.empty(R, dtype=torch.int64, device=X.device) if with_hash else None
+    lh = _empty(R, torch.int64, X.device, stream) if with_hash else None
     li, row0, n = None, 0, 0
     if leaf_rows is not None:
         row0, n = leaf_rows
-        li = torch.empty((n, int(forest["n_trees"])), dtype=torch.int16, device=X.device)
+        li = _empty((n, int(forest["n_trees"])), torch.int16, X.device, stream)
     s = forest_struct(forest)
     _check("hwsel_forest_score_checked", lib().hwsel_forest_score_checked(
         C.byref(s), _ptr(packed), _ptr(X), R, X.stride(0), _ptr(scores), _ptr(workspace),
@@ -420,7 +433,7 @@ def hwsel_forest_leaves(forest: dict, X: torch.Tensor, rows: torch.Tensor,
     _forest_arrays(forest)
     _arg(rows, "rows", I64, 0, X)
     if leaf_idx is None:
-        leaf_idx = torch.empty((n, int(forest["n_trees"])), dtype=torch.int16, device=X.device)
+        leaf_idx = _empty((n, int(forest["n_trees"])), torch.int16, X.device, stream)
     _arg(leaf_idx, "leaf_idx", U16, n * int(forest["n_trees"]), X)
     s = forest_struct(forest)
     _check("hwsel_forest_leaves", lib().hwsel_forest_leaves(
@@ -441,7 +454,7 @@ def hwsel_mlp_pack(mlp: dict, packed: torch.Tensor | None = None, stream=None) -
     n = C.c_size_t(0)
     _check("hwsel_mlp_pack_bytes", lib().hwsel_mlp_pack_bytes(C.byref(s), C.byref(n)))
     if packed is None:
-        packed = torch.empty(int(n.value), dtype=torch.uint8, device=mlp["W1"].device)
+        packed = _empty(int(n.value), torch.uint8, mlp["W1"].device, stream)
     _arg(packed, "packed", U8, int(n.value), mlp["W1"])
     _check("hwsel_mlp_pack", lib().hwsel_mlp_pack(C.byref(s), _ptr(packed), packed.numel(), _stream(stream)))
     return packed
@@ -461,7 +474,7 @@ def hwsel_mlp_score(mlp: dict, X: torch.Tensor, scores: torch.Tensor | None = No
     _matrix(X, "X", 128)
     _mlp_arrays(mlp)
     if scores is None:
-        scores = torch.empty(R, dtype=torch.float32, device=X.device)
+        scores = _empty(R, torch.float32, X.device, stream)
     _arg(scores, "scores", F32, R, X)
     if packed is not None:
         n = C.c_size_t(0)
@@ -480,9 +493,9 @@ def hwsel_topk_per_problem(scores: torch.Tensor, seg_offsets: torch.Tensor, k: i
     _arg(scores, "scores", F32)
     _arg(seg_offsets, "seg_offsets", I64, 1, scores)
     if idx is None:
-        idx = torch.empty((P, k), dtype=torch.int32, device=scores.device)
+        idx = _empty((P, k), torch.int32, scores.device, stream)
     if vals is None and with_vals:
-        vals = torch.empty((P, k), dtype=torch.float32, device=scores.device)
+        vals = _empty((P, k), torch.float32, scores.device, stream)
     _arg(idx, "idx", I32, P * k, scores)
     if vals is not None:
         _arg(vals, "vals", F32, P * k, scores)
@@ -500,9 +513,9 @@ def hwsel_regret(runtimes: torch.Tensor, seg_offsets: torch.Tensor, idx: torch.T
     _arg(runtimes, "runtimes", F32)
     _arg(seg_offsets, "seg_offsets", I64, P + 1, runtimes)
     _arg(idx, "idx", I32, P * k, runtimes)
-    r1 = torch.empty(P, dtype=torch.float32, device=dev) if r1 is None else r1
-    rk = torch.empty(P, dtype=torch.float32, device=dev) if rk is None else rk
-    best = torch.empty(P, dtype=torch.int32, device=dev) if best is None else best
+    r1 = _empty(P, torch.float32, dev, stream) if r1 is None else r1
+    rk = _empty(P, torch.float32, dev, stream) if rk is None else rk
+    best = _empty(P, torch.int32, dev, stream) if best is None else best
     _arg(r1, "r1", F32, P, runtimes)
     _arg(rk, "rk", F32, P, runtimes)
     _arg(best, "best", I32, P, runtimes)
@@ -531,12 +544,12 @@ def hwsel_select_forest(hw: dict, problems: torch.Tensor, seg_offsets: torch.Ten
     _forest_arrays(forest)
     _packed_image(forest, packed, problems)
     if workspace is None:
-        workspace = torch.empty(hwsel_select_forest_workspace_bytes(forest, R), dtype=torch.uint8, device=dev)
+        workspace = _empty(hwsel_select_forest_workspace_bytes(forest, R), torch.uint8, dev, stream)
     _arg(workspace, "workspace", U8, 0, problems)
     if idx is None:
-        idx = torch.empty((P, k), dtype=torch.int32, device=dev)
+        idx = _empty((P, k), torch.int32, dev, stream)
     if vals is None and with_vals:
-        vals = torch.empty((P, k), dtype=torch.float32, device=dev)
+        vals = _empty((P, k), torch.float32, dev, stream)
     _arg(idx, "idx", I32, P * k, problems)
     if vals is not None:
         _arg(vals, "vals", F32, P * k, problems)
@@ -567,14 +580,14 @@ def hwsel_evaluate(runtimes: torch.Tensor, seg_offsets: torch.Tensor, idx: torch
     _arg(seg_offsets, "seg_offsets", I64, P + 1, runtimes)
     _arg(idx, "idx", I32, P * k, runtimes)
     if workspace is None:
-        workspace = torch.empty(int(n.value), dtype=torch.uint8, device=dev)
+        workspace = _empty(int(n.value), torch.uint8, dev, stream)
     _arg(workspace, "workspace", U8, 0, runtimes)
-    out = torch.empty(HWSEL_EVAL_FIELDS, dtype=torch.float64, device=dev)
+    out = _empty(HWSEL_EVAL_FIELDS, torch.float64, dev, stream)
     reg = rank = ybar = None
     if per_group:
-        reg = torch.empty(P, dtype=torch.float64, device=dev)
-        rank = torch.empty(P, dtype=torch.int32, device=dev)
-        ybar = torch.empty(P, dtype=torch.float64, device=dev)
+        reg = _empty(P, torch.float64, dev, stream)
+        rank = _empty(P, torch.int32, dev, stream)
+        ybar = _empty(P, torch.float64, dev, stream)
     _check("hwsel_evaluate", lib().hwsel_evaluate(
         _ptr(_dev(runtimes, "runtimes")), _ptr(_dev(seg_offsets, "seg_offsets")), P, _ptr(_dev(idx, "idx")), k,
         _ptr(out), _ptr(reg), _ptr(rank), _ptr(ybar), _ptr(workspace), workspace.numel(), _stream(stream)))
@@ -596,12 +609,12 @@ def hwsel_evaluate_noalloc(runtimes: torch.Tensor, seg_offsets: torch.Tensor, id
     _arg(seg_offsets, "seg_offsets", I64, P + 1, runtimes)
     _arg(idx, "idx", I32, P * k, runtimes)
     if out is None:
-        out = torch.empty(HWSEL_EVAL_FIELDS, dtype=torch.float64, device=dev)
+        out = _empty(HWSEL_EVAL_FIELDS, torch.float64, dev, stream)
     _arg(out, "out", (torch.float64,), HWSEL_EVAL_FIELDS, runtimes)
     if per_group:
-        regret = torch.empty(P, dtype=torch.float64, device=dev) if regret is None else regret
-        rank = torch.empty(P, dtype=torch.int32, device=dev) if rank is None else rank
-        ybar = torch.empty(P, dtype=torch.float64, device=dev) if ybar is None else ybar
+        regret = _empty(P, torch.float64, dev, stream) if regret is None else regret
+        rank = _empty(P, torch.int32, dev, stream) if rank is None else rank
+        ybar = _empty(P, torch.float64, dev, stream) if ybar is None else ybar
     for n, t, dt in (("regret", regret, (torch.float64,)), ("rank", rank, I32), ("ybar", ybar, (torch.float64,))):
         if t is not None:
             _arg(t, n, dt, P, runtimes)
@@ -623,10 +636,10 @@ def hwsel_static_config(runtimes: torch.Tensor, seg_offsets: torch.Tensor, confi
     _arg(seg_offsets, "seg_offsets", I64, P + 1, runtimes)
     _arg(config_id, "config_id", I32, int(runtimes.numel()), runtimes)
     if workspace is None:
-        workspace = torch.empty(int(n.value), dtype=torch.uint8, device=dev)
+        workspace = _empty(int(n.value), torch.uint8, dev, stream)
     _arg(workspace, "workspace", U8, 0, runtimes)
-    best = torch.empty(2, dtype=torch.int32, device=dev)
-    mean_y = torch.empty(1, dtype=torch.float64, device=dev)
+    best = _empty(2, torch.int32, dev, stream)
+    mean_y = _empty(1, torch.float64, dev, stream)
     _check("hwsel_static_config", lib().hwsel_static_config(
         _ptr(_dev(runtimes, "runtimes")), _ptr(_dev(seg_offsets, "seg_offsets")), P,
         _ptr(_dev(config_id, "config_id")), n_configs, _ptr(best), _ptr(mean_y), _ptr(workspace),
@@ -640,9 +653,9 @@ def hwsel_catalogue_mask(hw: dict, problems: torch.Tensor, flags: int = 0, mask:
     P = problems.shape[0]
     dev = problems.device
     if mask is None:
-        mask = torch.empty((P, HWSEL_CATALOGUE_SIZE), dtype=torch.uint8, device=dev)
+        mask = _empty((P, HWSEL_CATALOGUE_SIZE), torch.uint8, dev, stream)
     _arg(mask, "mask", U8, P * HWSEL_CATALOGUE_SIZE, problems)
-    n_valid = torch.empty(P, dtype=torch.int64, device=dev)
+    n_valid = _empty(P, torch.int64, dev, stream)
     _check("hwsel_catalogue_mask", lib().hwsel_catalogue_mask(
         hw_struct(hw), _ptr(_dev(problems, "problems")), P, flags, _ptr(mask), _ptr(n_valid), _stream(stream)))
     return mask, n_valid
@@ -655,9 +668,9 @@ def hwsel_catalogue_compact(mask: torch.Tensor, n_valid: torch.Tensor, capacity:
     dev = mask.device
     _arg(mask, "mask", U8, P * HWSEL_CATALOGUE_SIZE)
     _arg(n_valid, "n_valid", I64, P, mask)
-    seg = torch.empty(P + 1, dtype=torch.int64, device=dev)
+    seg = _empty(P + 1, torch.int64, dev, stream)
     if point is None:
-        point = torch.empty(max(capacity, 1), dtype=torch.int32, device=dev)
+        point = _empty(max(capacity, 1), torch.int32, dev, stream)
     _arg(point, "point", I32, capacity, mask)
     _check("hwsel_catalogue_compact", lib().hwsel_catalogue_compact(
         _ptr(_dev(mask, "mask")), _ptr(_dev(n_valid, "n_valid")), P, _ptr(seg), _ptr(point), capacity,
@@ -673,7 +686,7 @@ def hwsel_catalogue_candidates(problems: torch.Tensor, seg_offsets: torch.Tensor
     dev = problems.device
     wide = ("tile_m", "tile_n", "tile_k", "inst_n")
     if out is None:
-        out = {n: torch.empty(R, dtype=torch.int16 if n in wide else torch.uint8, device=dev) for n in CAND_FIELDS}
+        out = {n: _empty(R, torch.int16 if n in wide else torch.uint8, dev, stream) for n in CAND_FIELDS}
     _arg(seg_offsets, "seg_offsets", I64, P + 1, problems)
     if point is not None:
         _arg(point, "point", I32, R, problems)
