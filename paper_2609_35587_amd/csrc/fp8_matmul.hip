@@ -583,8 +583,13 @@ __global__ __launch_bounds__(256, 2) void k_product_rows(Operand A, Operand B, i
 #pragma unroll
         for (int i = 0; i < 4; ++i) to_lds(tile, b_at[i], k, to + i * 1024);
     };
-    auto barrier = [] {
+    // vmcnt(8): of this wave's loads all but the next two stages' have come.  lgkmcnt(0):
+    // its fragments of the stage before have been read, which is loaded anew behind the
+    // barrier (the products that take them may follow it; without the wait up to a
+    // whole stage's reads were on their way here).
+    auto stage_barrier = [] {
         asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0078);
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
@@ -619,8 +624,7 @@ __global__ __launch_bounds__(256, 2) void k_product_rows(Operand A, Operand B, i
 #define BLOCK(kb)                                                                                                             \
     if constexpr ((kb) < NKB) {                                                                                               \
         const int32_t s = (t - t_begin) * NKB + (kb);                                                                         \
-        __builtin_amdgcn_s_waitcnt(0x0f78);                 /* vmcnt(8): all but the next two stages' */                      \
-        barrier();                                                                                                            \
+        stage_barrier();                                                                                                      \
         fetch(s + kAhead);                                                                                                    \
         __builtin_amdgcn_sched_barrier(0);                                                                                    \
         if constexpr ((kb) == 0) {                                                                                            \
