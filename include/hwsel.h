@@ -590,7 +590,8 @@ int hwsel_fp8_transpose(const hwsel_fp8_t *in, const hwsel_fp8_t *out, void *str
  * The order of the sums is fixed by the sizes: the same inputs give the same
  * bits.  Returns HWSEL_EINVAL for null pointers, sizes < 1 or that differ,
  * bad strides, alignment, formats or activation, a short workspace;
- * HWSEL_EUNSUPPORTED for B in E5M2 and another dtype.
+ * HWSEL_EUNSUPPORTED for B in E5M2, another dtype, and a result of 2^24 or
+ * more tiles of 128 x 128 (a quarter of a terabyte) in fp32 or with K <= 896.
  */
 enum { HWSEL_ACT_NONE = 0, HWSEL_ACT_GELU = 1 };
 int hwsel_fp8_matmul_workspace_bytes(const hwsel_fp8_t *A, const hwsel_fp8_t *B, size_t *bytes);

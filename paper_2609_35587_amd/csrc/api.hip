@@ -554,9 +554,11 @@ static int check_product(const hwsel_fp8_t *A, const hwsel_fp8_t *B, const char 
 }
 
 static int check_product_call(const hwsel_fp8_t *A, const hwsel_fp8_t *B, const float *bias, int32_t activation,
-                              const void *workspace, size_t workspace_bytes, const char *fn)
+                              const void *workspace, size_t workspace_bytes, bool fp32, bool codes, const char *fn)
 {
     if (int st = check_product(A, B, fn)) return st;
+    if (!hwsel::fp8_product_fits(A->rows, B->rows, A->cols, fp32, codes))
+        return fail(HWSEL_EUNSUPPORTED, fn, "a result of %lld x %lld", (long long)A->rows, (long long)B->rows);
     if ((uintptr_t)bias & 3u) return fail(HWSEL_EINVAL, fn, "bias misaligned");
     if (activation != HWSEL_ACT_NONE && activation != HWSEL_ACT_GELU)
         return fail(HWSEL_EINVAL, fn, "activation %d", activation);
@@ -580,7 +582,8 @@ int hwsel_fp8_matmul(const hwsel_fp8_t *A, const hwsel_fp8_t *B, const float *bi
                      int32_t dtype, int64_t ldc, void *workspace, size_t workspace_bytes, void *stream)
 {
     static const char *fn = "hwsel_fp8_matmul";
-    if (int st = check_product_call(A, B, bias, activation, workspace, workspace_bytes, fn)) return st;
+    if (int st = check_product_call(A, B, bias, activation, workspace, workspace_bytes, dtype == HWSEL_DTYPE_FP32, false, fn))
+        return st;
     if (int st = check_plain(C, dtype, ldc, B->rows, fn)) return st;
     return launched(hwsel::launch_fp8_matmul(*A, *B, bias, activation == HWSEL_ACT_GELU, C, dtype == HWSEL_DTYPE_BF16, ldc,
                                              workspace, (hipStream_t)stream),
@@ -591,7 +594,7 @@ int hwsel_fp8_layer(const hwsel_fp8_t *A, const hwsel_fp8_t *B, const float *bia
                     const hwsel_fp8_t *C, void *workspace, size_t workspace_bytes, void *stream)
 {
     static const char *fn = "hwsel_fp8_layer";
-    if (int st = check_product_call(A, B, bias, activation, workspace, workspace_bytes, fn)) return st;
+    if (int st = check_product_call(A, B, bias, activation, workspace, workspace_bytes, false, true, fn)) return st;
     if (int st = check_fp8(C, "C", fn)) return st;
     if (C->rows != A->rows || C->cols != B->rows)
         return fail(HWSEL_EINVAL, fn, "C is %lld x %lld, the product %lld x %lld", (long long)C->rows, (long long)C->cols,

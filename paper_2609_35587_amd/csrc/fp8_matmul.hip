@@ -984,13 +984,38 @@ Operand operand(const hwsel_fp8_t &x)
     return {x.q, x.ld, x.scale, x.ld_scale, (int32_t)x.rows, x.block_rows == 1 ? 0 : 7};
 }
 
+// Rows first .. first + n of an operand (whole blocks before them).
+Operand part_of(Operand x, int64_t first, int64_t n)
+{
+    x.q += first * x.ld;
+    x.scale += (first >> x.shift) * x.ld_scale;
+    x.rows = (int32_t)n;
+    return x;
+}
+
+// A result from column n on.
+template <OutKind KIND>
+Out columns_from(Out o, int64_t n)
+{
+    static_assert(KIND != kOutFp8, "codes have scales beside them");
+    o.C = static_cast<uint8_t *>(o.C) + n * (KIND == kOutBf16 ? 2 : 4);
+    if (o.bias) o.bias += n;
+    return o;
+}
+
 template <int MT, bool EXACT, OutKind KIND>
 void launch_few(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const Plan &p, const Out &o, hipStream_t s)
 {
     const int32_t nkb = (int32_t)fp8_blocks(A.cols);
+    // (a launch has fewer than 2^32 threads: many columns, which leave K whole, go in spans of 2^22 workgroups)
     auto go = [&](auto kernel) {
-        const dim3 grid((unsigned)((B.rows + 16 * p.nt - 1) / (16 * p.nt)), (unsigned)p.splits);
-        hipLaunchKernelGGL(kernel, grid, dim3(512), 0, s, operand(A), operand(B), nkb, p.per_split, o);
+        const int64_t span = ((int64_t)1 << 22) * 16 * p.nt;
+        for (int64_t n0 = 0; n0 < B.rows; n0 += span) {
+            const int64_t n = B.rows - n0 < span ? B.rows - n0 : span;
+            const dim3 grid((unsigned)((n + 16 * p.nt - 1) / (16 * p.nt)), (unsigned)p.splits);
+            hipLaunchKernelGGL(kernel, grid, dim3(512), 0, s, operand(A), part_of(operand(B), n0, n), nkb, p.per_split,
+                               columns_from<KIND>(o, n0));
+        }
     };
     auto by_columns = [&](auto fa) {
         constexpr int FA = decltype(fa)::value;
@@ -1093,6 +1118,12 @@ size_t fp8_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K)
         most = bytes > most ? bytes : most;
     }
     return most;
+}
+
+bool fp8_product_fits(int64_t M, int64_t N, int64_t K, bool fp32, bool codes)
+{
+    const Plan p = plan_product(M, N, fp8_blocks(K), fp32, codes);
+    return p.way != Way::tiles || (M + p.bm - 1) / p.bm * ((N + kBN - 1) / kBN) * p.splits < (int64_t)1 << 24;
 }
 
 hipError_t launch_fp8_matmul(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const float *bias, bool gelu, void *C, bool bf16,

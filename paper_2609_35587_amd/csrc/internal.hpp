@@ -145,6 +145,8 @@ hipError_t launch_fp8_quantise(const void *X, bool bf16, int64_t ld, bool transp
 hipError_t launch_fp8_dequantise(const hwsel_fp8_t &in, void *X, bool bf16, int64_t ld, hipStream_t s);
 hipError_t launch_fp8_transpose(const hwsel_fp8_t &in, const hwsel_fp8_t &out, hipStream_t s);
 size_t fp8_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K);
+// Whether a product's tiles, a workgroup of 256 threads each, stay within a launch's 2^32 threads.
+bool fp8_product_fits(int64_t M, int64_t N, int64_t K, bool fp32, bool codes);
 hipError_t launch_fp8_matmul(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const float *bias, bool gelu, void *C, bool bf16,
                              int64_t ldc, void *ws, hipStream_t s);
 hipError_t launch_fp8_layer(const hwsel_fp8_t &A, const hwsel_fp8_t &B, const float *bias, bool gelu, const hwsel_fp8_t &C,
