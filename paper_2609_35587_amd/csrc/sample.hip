@@ -225,11 +225,12 @@ __device__ __forceinline__ uint32_t first_best(const Problem &q, const f32x4u_t 
     return known;
 }
 
-// The draws of a problem with one candidate left, by N threads.
+// The draws of a problem with one candidate left, by N threads.  (Loops over draws
+// count without a sign, here and below: up to 2^31 - 1 draws and a step more.)
 template <int N>
 __device__ __forceinline__ void write_one(int32_t at, int thread, int32_t n_draws, int32_t *idx, float *prob)
 {
-    for (int32_t j = thread; j < n_draws; j += N) {
+    for (uint32_t j = thread; j < (uint32_t)n_draws; j += N) {
         idx[j] = at;
         if (prob) prob[j] = 1.0f;
     }
@@ -670,7 +671,7 @@ __device__ __forceinline__ void sample_problem(Lds<NT, BINS, CACHED> &lds, int32
     }
     __syncthreads();
     if (alive == 0) {
-        for (int32_t j = threadIdx.x; j < set.n_draws; j += NT) {
+        for (uint32_t j = threadIdx.x; j < (uint32_t)set.n_draws; j += NT) {
             idx[j] = -1;
             if (prob) prob[j] = 0.0f;
         }
@@ -907,7 +908,7 @@ __device__ __forceinline__ void sample_problem(Lds<NT, BINS, CACHED> &lds, int32
     __syncthreads();
     const uint64_t total = lds.part[n_parts];
     if (fine) {                                             // a thread a draw
-        for (int32_t j = threadIdx.x; j < set.n_draws; j += NT) {
+        for (uint32_t j = threadIdx.x; j < (uint32_t)set.n_draws; j += NT) {
             uint64_t r = point_of(u[j], total);
             int part = 0, four = 0;
             for (int step = kParts; step > 0; step >>= 1)   // parts that end at or before the point
@@ -930,7 +931,7 @@ __device__ __forceinline__ void sample_problem(Lds<NT, BINS, CACHED> &lds, int32
         }
         return;
     }
-    for (int32_t j = wave; j < set.n_draws; j += kWaves) {
+    for (uint32_t j = wave; j < (uint32_t)set.n_draws; j += kWaves) {
         uint64_t r = point_of(u[j], total);
         int part = 0;                                       // parts that end at or before the point
         for (int e = lane; e < ((n_parts + 63) & ~63); e += 64) part += __popcll(__ballot(e < n_parts && lds.part[e + 1] <= r));
@@ -1138,7 +1139,7 @@ __device__ __forceinline__ void sample_small(Problem q, int32_t p, const Setting
         least_score = fminf(least_score, in ? s[e] : __builtin_inff());
     }
     if (alive == 0) {
-        for (int32_t j = lane; j < set.n_draws; j += 64) {
+        for (uint32_t j = lane; j < (uint32_t)set.n_draws; j += 64) {
             idx[j] = -1;
             if (prob) prob[j] = 0.0f;
         }
@@ -1239,7 +1240,7 @@ __device__ __forceinline__ void sample_small(Problem q, int32_t p, const Setting
         *reinterpret_cast<u32x4_t *>(lds.w + (i * 64 + lane) * 4) = (u32x4_t){w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
     }
     wave_sync();
-    for (int32_t j = lane; j < set.n_draws; j += 64) {      // a lane a draw
+    for (uint32_t j = lane; j < (uint32_t)set.n_draws; j += 64) {      // a lane a draw
         uint64_t r = point_of(j < 64 ? u_first : u[j], total);
         int at = 0;
 #pragma unroll
@@ -1665,7 +1666,7 @@ __global__ __launch_bounds__(kWide) void k_wide_draw(WideArgs a, const float *__
     if (prob) prob += (int64_t)p * n_draws;
     if (st.alive == 0) {
         if (threadIdx.x == 0 && kept_out) kept_out[p] = 0;
-        for (int32_t j = threadIdx.x; j < n_draws; j += kWide) {
+        for (uint32_t j = threadIdx.x; j < (uint32_t)n_draws; j += kWide) {
             idx[j] = -1;
             if (prob) prob[j] = 0.0f;
         }
@@ -1699,7 +1700,7 @@ __global__ __launch_bounds__(kWide) void k_wide_draw(WideArgs a, const float *__
     part[threadIdx.x] = before;
     if (threadIdx.x == 0) part[kWideParts] = total;
     __syncthreads();
-    for (int32_t j = wave; j < n_draws; j += kWide / 64) {
+    for (uint32_t j = wave; j < (uint32_t)n_draws; j += kWide / 64) {
         uint64_t r = point_of(u[j], total);
         int32_t e = 0;
         for (int step = kWideParts / 2; step > 0; step >>= 1)
