@@ -1,8 +1,9 @@
 // The Python calls of the 8-bit matrices and of drawing candidates: argument
 // checks, results' tensors and the current stream in C++.  A call that takes
 // the GPU 3.5 us (a row through one layer) took the host 13.9 us in Python, most
-// of it in attributes of tensors; it takes 5.9 so, half of it the launch.  Nothing is computed here, and nothing is kept
-// from one call for the next but the addresses of the C functions.
+// of it in attributes of tensors; it takes 5.6 so, half of it the launch.  Nothing
+// is computed here, and nothing is kept from one call for the next but the
+// addresses of the C functions.
 //
 // The functions take their arguments by position, in the order that hwsel.py
 // passes them on.

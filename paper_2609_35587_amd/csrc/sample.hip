@@ -16,8 +16,12 @@
 // others are read and weighed again.
 // (Kept in registers instead, 64 a thread, the unrolled passes were 24,000
 // instructions with spills: 121 us for 256 problems of 65,536.)
-// Bound by latency for short segments, for long ones by some 60 instructions a
-// candidate.
+// Bound by latency: counters show the vector units busy 24 % of the time for 600
+// problems of up to 8,192 and 56 % for 256 of 65,536 (92 vector instructions a
+// candidate: those past LDS are weighed twice), waves waiting 57 % of theirs.
+// The paths for cuts among very many scores are inlined; k_sample<1024> keeps 14
+// vector registers in scratch for them, k_sample<512> of six waves 18 and
+// k_sample_waves 24.
 #include "internal.hpp"
 
 namespace hwsel {
@@ -1713,8 +1717,8 @@ __global__ __launch_bounds__(kWide) void k_wide_draw(WideArgs a, const float *__
 }  // namespace
 
 // Segment lengths are not known here; their mean is.  Few problems of many
-// candidates are shared by workgroups, which costs eleven launches: 8 problems
-// of 49,152 38 us (a workgroup each: 40), 8 of 32,768 35 (30); 64 of 131,072 74
+// candidates are shared by workgroups, which costs seven launches for top-k or
+// top-p and ten for both: 8 problems of 49,152 38 us (a workgroup each: 40), 8 of 32,768 35 (30); 64 of 131,072 74
 // (83), 64 of 65,536 65 (50); 128 of 262,144 157 (163), 128 of 131,072 101 (92).
 static bool shared_problems(int64_t R, int32_t P) { return P <= 128 && R / P > 36864 + 1280 * (int64_t)P; }
 
