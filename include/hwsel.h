@@ -662,6 +662,165 @@ int hwsel_sample_per_problem(const float *scores, int64_t R, const int64_t *seg_
                              const hwsel_sampling_t *how, const float *u, int32_t n_draws, int32_t *idx, float *prob,
                              int32_t *kept, void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * Log probabilities.  A problem's scores stand for the distribution that
+ * hwsel_sample_per_problem draws from without limits:
+ *   p_j = exp((s_j - best) / T) / Z,  Z = the sum of those exponentials,
+ * over the candidates whose score is neither NaN nor -inf; the others have
+ * probability 0 (log probability -inf).  best is the largest score; scores
+ * equal to it have t = 0 also where it is +inf.  T <= 0 or NaN is the limit
+ * T -> 0 with draws' choice among ties: the first best candidate alone.
+ *   logp     fp32 [P][n_picks]: log p of candidate picks[p][i] (local index,
+ *            int32 [P][n_picks], as drawn).  A pick outside the problem (-1:
+ *            none) gives 0.
+ *   entropy  fp32 [P] (nullable): -sum p log p; 0 for a problem without a
+ *            candidate.
+ *   norm     fp32 [P][2] (nullable): best and log Z, what the gradient needs
+ *            of the distribution (-inf, -inf without a candidate): log p_j =
+ *            (s_j - best) / T - log Z.
+ *   top_idx  int32 [P][top], top_logp fp32 [P][top]: the `top` (0..64) best
+ *            candidates in hwsel_topk_per_problem's order with their log
+ *            probabilities; -1 and -inf past the last one that has any.
+ * picks and logp are NULL where n_picks is 0, top_idx and top_logp where top
+ * is 0.  T is `temperature`, or temperature_of[p] (device fp32 [P]) where that
+ * is not NULL.  scores fp32 [R]; seg_offsets [P+1] as for hwsel_features
+ * (offsets outside [0, R] are limited to it); workspace of
+ * hwsel_logprob_workspace_bytes(R, P, top) bytes (device, 256-byte aligned;
+ * NULL where that is 0).  Sums are fp32 in an order fixed by the sizes.
+ * Returns HWSEL_EINVAL for null pointers, P < 1, R < 0, n_picks < 0, top
+ * outside 0..64, a short or misaligned workspace; HWSEL_EUNSUPPORTED for R >
+ * 2^30.
+ */
+int hwsel_logprob_workspace_bytes(int64_t R, int32_t P, int32_t top, size_t *bytes);
+int hwsel_logprob_per_problem(const float *scores, int64_t R, const int64_t *seg_offsets, int32_t P, float temperature,
+                              const float *temperature_of, const int32_t *picks, int32_t n_picks, int32_t top,
+                              float *logp, float *entropy, float *norm, int32_t *top_idx, float *top_logp,
+                              void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Gradient of sum_i d_logp[p][i] logp[p][i] + d_entropy[p] entropy[p] with
+ * respect to the scores, from what hwsel_logprob_per_problem wrote for them:
+ *   d_scores[j] = 1/T (g_j - p_j S - d_entropy p_j (log p_j + entropy)),
+ *   g_j = the sum of d_logp[p][i] over the picks i of candidate j, S = the sum
+ *   over all picks that count (inside the problem, log probability not -inf).
+ * The same candidate may be picked several times; g_j is summed in fixed point
+ * (2^-30 of the largest |d_logp| that counts, or finer), so the order of the picks does not
+ * matter.  Candidates without probability, problems with T <= 0 or NaN and rows of no
+ * problem get 0.  A d_logp or d_entropy that is not finite makes its
+ * problem's gradients not finite.
+ *   d_scores fp32 [R]; picks, d_logp NULL where n_picks is 0; entropy and
+ *   d_entropy (fp32 [P]) both NULL or both given; norm as written.
+ * Returns HWSEL_EINVAL for null pointers, P < 1, R < 0, n_picks < 0;
+ * HWSEL_EUNSUPPORTED for R > 2^30.
+ */
+int hwsel_logprob_gradient(const float *scores, int64_t R, const int64_t *seg_offsets, int32_t P, float temperature,
+                           const float *temperature_of, const float *norm, const int32_t *picks, int32_t n_picks,
+                           const float *d_logp, const float *entropy, const float *d_entropy, float *d_scores,
+                           void *stream);
+
+/*
+ * A plain matrix on the device, row-major: `data` aligned to its elements, ld
+ * elements from row to row (at least its columns), dtype HWSEL_DTYPE_FP32 or
+ * HWSEL_DTYPE_BF16.  Where a call may do without one, a NULL struct or a NULL
+ * data stands for none.  The struct is read on the host.
+ */
+typedef struct hwsel_matrix {
+    void *data;
+    int64_t ld;
+    int32_t dtype;
+} hwsel_matrix_t;
+
+/*
+ * Dropout whose mask is made from a counter, never stored: the mask is a
+ * function of the seed, the offset and an element's place alone, so a
+ * backward pass makes the forward pass's mask again, whatever the types and
+ * strides.  The numbers of the columns 8 g .. 8 g + 7 of row r are the eight
+ * 16-bit halves, low half first, of the four words of Philox4x32-10 (Salmon,
+ * Moraes, Dror, Shaw: Parallel random numbers, as easy as 1, 2, 3; 2011) with
+ * counter (g, r, low word of offset, high word of offset) and key (low word
+ * of seed, high word of seed).  An element is kept where its number is >=
+ * least = p 2^16 rounded to nearest even, and is multiplied by 2^16 / (2^16 -
+ * least) rounded to fp32: p is taken to a multiple of 2^-16, and the mean of
+ * a result is its operand's exactly.  A dropped NaN or infinity leaves 0.
+ *   p in [0, 1]; state: NULL, or device uint64 [2] = (seed, offset) read by the
+ *   kernel in place of the fields (a captured graph gets a new mask on every
+ *   replay if the caller moves the offset between them).
+ */
+typedef struct hwsel_dropout {
+    uint64_t seed, offset;
+    const uint64_t *state;
+    float p;
+} hwsel_dropout_t;
+
+/*
+ * Y = residual + mask(X) / share kept (residual may be none): a product and a
+ * sum in fp32, then rounded to Y's dtype.  Y and residual have one dtype, X its
+ * own.  The gradient of X
+ * is the same call on Y's gradient without a residual; the residual's is Y's
+ * gradient itself.  Y may be X or the residual (same data, ld and dtype); no other overlap.
+ * Returns HWSEL_EINVAL for null pointers, sizes < 1, p outside [0, 1] or NaN,
+ * a bad ld or alignment, a residual of another dtype; HWSEL_EUNSUPPORTED for
+ * another dtype, rows or cols >= 2^31.
+ */
+int hwsel_dropout(const hwsel_dropout_t *how, int64_t rows, int64_t cols, const hwsel_matrix_t *X,
+                  const hwsel_matrix_t *residual, const hwsel_matrix_t *Y, void *stream);
+
+/*
+ * Joining a block of a deep ranker to its residual stream, with the norms
+ * after it and before the next block:
+ *   u  = w_branch * norm(y)            (norm only if post_norm, else y)
+ *   v  = dropout(branch_scale * g * u)   (mask and share kept as hwsel_dropout)
+ *   x1 = stream_scale * x + v
+ *   z  = w_pre * norm(x1)
+ * with norm(a) = a / sqrt(mean of a^2 over the row + eps).  All of it is fp32;
+ * x1 and z are each rounded once (z is made of x1 before its rounding).
+ *   x, x1      [rows][cols], the stream; one dtype.
+ *   y, gate, z the block's result, its gate, the next block's input; one dtype.
+ *   y          may be none: x1 = stream_scale * x (then no gate, no branch).
+ *   gate       gate_cols columns: 0 none (g = 1), 1 (one for a row) or cols;
+ *              g = gate, or 1 / (1 + exp(-gate)) with gate_sigmoid.
+ *   w_branch, w_pre  fp32 [cols] or NULL (ones).
+ *   x1 or z may be none, not both.
+ * x1 may be x itself (same data, ld); outputs overlap nothing else.
+ * Returns HWSEL_EINVAL for null pointers, sizes < 1, eps not > 0, scales that
+ * are not finite, p outside [0, 1], bad flags, ld or alignment, dtypes that
+ * differ where they are to be one; HWSEL_EUNSUPPORTED for another dtype, rows
+ * or cols >= 2^31.
+ */
+typedef struct hwsel_join {
+    int64_t rows, cols;
+    const float *w_branch, *w_pre;
+    float eps, stream_scale, branch_scale;
+    int32_t post_norm, gate_sigmoid;
+    int64_t gate_cols;
+    hwsel_dropout_t dropout;
+} hwsel_join_t;
+int hwsel_block_join(const hwsel_join_t *join, const hwsel_matrix_t *x, const hwsel_matrix_t *y,
+                     const hwsel_matrix_t *gate, const hwsel_matrix_t *x1, const hwsel_matrix_t *z, void *stream);
+
+/*
+ * Gradients of hwsel_block_join.  Nothing is kept between the two but x1 as
+ * it was written (without y: x1 = stream_scale * x): norms are made again from
+ * x1 and y, the mask from its counter.  With d = d_x1 + the gradient of z with
+ * respect to x1 (at the x1 given) applied to d_z:
+ *   dx = stream_scale * d; dy, dgate (gate's shape), dw_branch, dw_pre fp32
+ *   [cols] are those of the sum of d * v, of d_z * z for dw_pre.
+ *   d_x1 (stream dtype) or d_z (block dtype) may be none (zeros), not both; of
+ *   the outputs those that are none or NULL are left out; dw_pre needs d_z, dy,
+ *   dgate and dw_branch need y, dgate a gate.
+ *   workspace  hwsel_block_join_gradient_workspace_bytes(join) bytes of
+ *   device memory, 256-byte aligned (NULL where that is 0).
+ * Sums over rows are fp32 in an order fixed by the sizes.  dx may be d_x1
+ * itself (same data, ld); outputs overlap nothing else.
+ * Returns as hwsel_block_join does, and HWSEL_EINVAL for a short or misaligned
+ * workspace and for an output whose input is missing.
+ */
+int hwsel_block_join_gradient_workspace_bytes(const hwsel_join_t *join, size_t *bytes);
+int hwsel_block_join_gradient(const hwsel_join_t *join, const hwsel_matrix_t *x1, const hwsel_matrix_t *y,
+                              const hwsel_matrix_t *gate, const hwsel_matrix_t *d_x1, const hwsel_matrix_t *d_z,
+                              const hwsel_matrix_t *dx, const hwsel_matrix_t *dy, const hwsel_matrix_t *dgate,
+                              float *dw_branch, float *dw_pre, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Static text for a status code. */
 const char *hwsel_status_string(int status);
 /* Detail of the last failed call on this thread ("" if none). */

@@ -3,8 +3,8 @@
 
 Every translation unit is compiled with hipcc for gfx950 only; packed-fp32
 instructions are disabled; the feature, evaluation and sampling units are also
-compiled without multiply-add contraction (their rounding steps are part of
-their contract).
+compiled without multiply-add contraction, as is dropout's (their rounding steps
+are part of their contract).
 """
 from __future__ import annotations
 
@@ -21,12 +21,12 @@ LIB = os.path.join(HERE, "libhwsel.so")
 CEIL_SRC, CEIL_LIB = "ceilings.hip", os.path.join(HERE, "libhwsel_ceilings.so")
 BINDING_SRC, BINDING = "binding.cpp", os.path.join(HERE, "_binding.so")
 ARCH = "gfx950"
-SOURCES = ["api.hip", "catalogue.hip", "evaluate.hip", "features.hip", "forest.hip", "fp8.hip", "fp8_matmul.hip",
-           "mlp.hip", "sample.hip", "scorers.hip", "select.hip"]
+SOURCES = ["api.hip", "catalogue.hip", "dropout.hip", "evaluate.hip", "features.hip", "forest.hip", "fp8.hip",
+           "fp8_matmul.hip", "join.hip", "logprob.hip", "mlp.hip", "sample.hip", "scorers.hip", "select.hip"]
 COMMON = ["-O3", "-std=c++20", "-fPIC", f"--offload-arch={ARCH}", "-fno-fast-math",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
           "-Wall", "-Wno-unused-function", "-Wno-unknown-pragmas"]
-PER_FILE = {"features.hip": ["-ffp-contract=off"], "evaluate.hip": ["-ffp-contract=off"],
+PER_FILE = {"dropout.hip": ["-ffp-contract=off"], "features.hip": ["-ffp-contract=off"], "evaluate.hip": ["-ffp-contract=off"],
             "sample.hip": ["-ffp-contract=off"]}
 
 

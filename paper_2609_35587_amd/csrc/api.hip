@@ -637,4 +637,189 @@ int hwsel_sample_per_problem(const float *scores, int64_t R, const int64_t *seg_
                     fn);
 }
 
+static int check_logprob_sizes(int64_t R, int32_t P, const char *fn)
+{
+    if (R < 0 || P < 1) return fail(HWSEL_EINVAL, fn, "R=%lld P=%d", (long long)R, P);
+    if (R > (int64_t)1 << 30) return fail(HWSEL_EUNSUPPORTED, fn, "R=%lld (at most 2^30)", (long long)R);
+    return HWSEL_OK;
+}
+
+static int check_top(int32_t top, const char *fn)
+{
+    return top < 0 || top > 64 ? fail(HWSEL_EINVAL, fn, "top=%d (0..64)", top) : HWSEL_OK;
+}
+
+int hwsel_logprob_workspace_bytes(int64_t R, int32_t P, int32_t top, size_t *bytes)
+{
+    static const char *fn = "hwsel_logprob_workspace_bytes";
+    if (!bytes) return fail(HWSEL_EINVAL, fn, "null pointer");
+    if (int st = check_logprob_sizes(R, P, fn)) return st;
+    if (int st = check_top(top, fn)) return st;
+    *bytes = hwsel::logprob_workspace_bytes(R, P, top);
+    g_err[0] = 0;
+    return HWSEL_OK;
+}
+
+int hwsel_logprob_per_problem(const float *scores, int64_t R, const int64_t *seg_offsets, int32_t P, float temperature,
+                              const float *temperature_of, const int32_t *picks, int32_t n_picks, int32_t top,
+                              float *logp, float *entropy, float *norm, int32_t *top_idx, float *top_logp,
+                              void *workspace, size_t workspace_bytes, void *stream)
+{
+    static const char *fn = "hwsel_logprob_per_problem";
+    if (int st = check_logprob_sizes(R, P, fn)) return st;
+    if (n_picks < 0) return fail(HWSEL_EINVAL, fn, "n_picks=%d", n_picks);
+    if (int st = check_top(top, fn)) return st;
+    if ((!scores && R > 0) || !seg_offsets || (n_picks > 0 && (!picks || !logp)) || (top > 0 && (!top_idx || !top_logp)))
+        return fail(HWSEL_EINVAL, fn, "null pointer");
+    const size_t need = hwsel::logprob_workspace_bytes(R, P, top);
+    if (need && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need))
+        return fail(HWSEL_EINVAL, fn, "workspace of %zu bytes, %zu needed, 256-byte aligned", workspace_bytes, need);
+    return launched(hwsel::launch_logprob(scores, R, seg_offsets, P, temperature, temperature_of, picks, n_picks, top, logp, entropy,
+                                          norm, top_idx, top_logp, workspace, (hipStream_t)stream),
+                    fn);
+}
+
+int hwsel_logprob_gradient(const float *scores, int64_t R, const int64_t *seg_offsets, int32_t P, float temperature,
+                           const float *temperature_of, const float *norm, const int32_t *picks, int32_t n_picks,
+                           const float *d_logp, const float *entropy, const float *d_entropy, float *d_scores, void *stream)
+{
+    static const char *fn = "hwsel_logprob_gradient";
+    if (int st = check_logprob_sizes(R, P, fn)) return st;
+    if (n_picks < 0) return fail(HWSEL_EINVAL, fn, "n_picks=%d", n_picks);
+    if (((!scores || !d_scores) && R > 0) || !seg_offsets || !norm || (n_picks > 0 && (!picks || !d_logp)))
+        return fail(HWSEL_EINVAL, fn, "null pointer");
+    if (!entropy != !d_entropy) return fail(HWSEL_EINVAL, fn, "entropy and d_entropy go together");
+    return launched(hwsel::launch_logprob_gradient(scores, R, seg_offsets, P, temperature, temperature_of, norm, picks, n_picks,
+                                                   d_logp, entropy, d_entropy, d_scores, (hipStream_t)stream),
+                    fn);
+}
+
+static const hwsel_matrix_t kNoMatrix = {nullptr, 0, HWSEL_DTYPE_FP32};
+
+static const hwsel_matrix_t &or_none(const hwsel_matrix_t *m) { return m && m->data ? *m : kNoMatrix; }
+
+// Rows and columns of plain matrices are 32-bit numbers in the kernels.
+static int check_plain_sizes(int64_t rows, int64_t cols, const char *fn)
+{
+    if (rows < 1 || cols < 1) return fail(HWSEL_EINVAL, fn, "%lld x %lld", (long long)rows, (long long)cols);
+    if (rows > INT32_MAX || cols > INT32_MAX)
+        return fail(HWSEL_EUNSUPPORTED, fn, "%lld x %lld (below 2^31 each)", (long long)rows, (long long)cols);
+    return HWSEL_OK;
+}
+
+// A matrix that may be absent; its dtype is `dtype` where that is not negative.
+static int check_matrix(const hwsel_matrix_t &m, const char *name, int64_t cols, int32_t dtype, const char *fn)
+{
+    if (!m.data) return HWSEL_OK;
+    if (int st = check_plain(m.data, m.dtype, m.ld, cols, fn)) return st;
+    if (m.ld > (int64_t)1 << 40) return fail(HWSEL_EINVAL, fn, "%s: ld=%lld", name, (long long)m.ld);
+    if (dtype >= 0 && m.dtype != dtype) return fail(HWSEL_EINVAL, fn, "%s: dtype %d, not %d", name, m.dtype, dtype);
+    return HWSEL_OK;
+}
+
+static int check_dropout(const hwsel_dropout_t &d, const char *fn)
+{
+    if (!(d.p >= 0.0f && d.p <= 1.0f)) return fail(HWSEL_EINVAL, fn, "p=%g (0..1)", (double)d.p);
+    if ((uintptr_t)d.state & 7u) return fail(HWSEL_EINVAL, fn, "state misaligned");
+    return HWSEL_OK;
+}
+
+int hwsel_dropout(const hwsel_dropout_t *how, int64_t rows, int64_t cols, const hwsel_matrix_t *X, const hwsel_matrix_t *residual,
+                  const hwsel_matrix_t *Y, void *stream)
+{
+    static const char *fn = "hwsel_dropout";
+    if (!how || !X || !X->data || !Y || !Y->data) return fail(HWSEL_EINVAL, fn, "null pointer");
+    if (int st = check_plain_sizes(rows, cols, fn)) return st;
+    if (int st = check_dropout(*how, fn)) return st;
+    if (int st = check_matrix(*X, "X", cols, -1, fn)) return st;
+    if (int st = check_matrix(*Y, "Y", cols, -1, fn)) return st;
+    if (int st = check_matrix(or_none(residual), "residual", cols, Y->dtype, fn)) return st;
+    return launched(hwsel::launch_dropout(*how, rows, cols, *X, or_none(residual), *Y, (hipStream_t)stream), fn);
+}
+
+// What both passes of a join share.
+static int check_join(const hwsel_join_t *j, const char *fn)
+{
+    if (!j) return fail(HWSEL_EINVAL, fn, "null pointer");
+    if (int st = check_plain_sizes(j->rows, j->cols, fn)) return st;
+    if (int st = check_dropout(j->dropout, fn)) return st;
+    if (!(j->eps > 0.0f) || j->eps > 3.4028235e38f) return fail(HWSEL_EINVAL, fn, "eps=%g", (double)j->eps);
+    if (!(__builtin_fabsf(j->stream_scale) <= 3.4028235e38f) || !(__builtin_fabsf(j->branch_scale) <= 3.4028235e38f))
+        return fail(HWSEL_EINVAL, fn, "scales %g and %g", (double)j->stream_scale, (double)j->branch_scale);
+    if ((j->post_norm != 0 && j->post_norm != 1) || (j->gate_sigmoid != 0 && j->gate_sigmoid != 1))
+        return fail(HWSEL_EINVAL, fn, "post_norm=%d gate_sigmoid=%d", j->post_norm, j->gate_sigmoid);
+    if (j->gate_cols != 0 && j->gate_cols != 1 && j->gate_cols != j->cols)
+        return fail(HWSEL_EINVAL, fn, "gate_cols=%lld (0, 1 or %lld)", (long long)j->gate_cols, (long long)j->cols);
+    if (((uintptr_t)j->w_branch & 3u) || ((uintptr_t)j->w_pre & 3u)) return fail(HWSEL_EINVAL, fn, "weights misaligned");
+    return HWSEL_OK;
+}
+
+static int check_branch(const hwsel_join_t *j, const hwsel_matrix_t &y, const hwsel_matrix_t &gate, const char *fn)
+{
+    if (!y.data && (j->gate_cols != 0 || j->w_branch)) return fail(HWSEL_EINVAL, fn, "a gate or w_branch without y");
+    if ((j->gate_cols != 0) != (gate.data != nullptr)) return fail(HWSEL_EINVAL, fn, "gate_cols=%lld and gate", (long long)j->gate_cols);
+    return HWSEL_OK;
+}
+
+int hwsel_block_join(const hwsel_join_t *j, const hwsel_matrix_t *x, const hwsel_matrix_t *y_, const hwsel_matrix_t *gate_,
+                     const hwsel_matrix_t *x1_, const hwsel_matrix_t *z_, void *stream)
+{
+    static const char *fn = "hwsel_block_join";
+    if (int st = check_join(j, fn)) return st;
+    const hwsel_matrix_t &y = or_none(y_), &gate = or_none(gate_), &x1 = or_none(x1_), &z = or_none(z_);
+    if (!x || !x->data || (!x1.data && !z.data)) return fail(HWSEL_EINVAL, fn, "null pointer");
+    if (int st = check_branch(j, y, gate, fn)) return st;
+    const int32_t block = y.data ? y.dtype : -1;
+    if (int st = check_matrix(*x, "x", j->cols, -1, fn)) return st;
+    if (int st = check_matrix(y, "y", j->cols, -1, fn)) return st;
+    if (int st = check_matrix(gate, "gate", j->gate_cols, block, fn)) return st;
+    if (int st = check_matrix(x1, "x1", j->cols, x->dtype, fn)) return st;
+    if (int st = check_matrix(z, "z", j->cols, block, fn)) return st;
+    const bool bbf = (y.data ? y.dtype : z.dtype) == HWSEL_DTYPE_BF16;
+    return launched(hwsel::launch_block_join(*j, *x, y, gate, x1, z, x->dtype == HWSEL_DTYPE_BF16, bbf, (hipStream_t)stream), fn);
+}
+
+int hwsel_block_join_gradient_workspace_bytes(const hwsel_join_t *j, size_t *bytes)
+{
+    static const char *fn = "hwsel_block_join_gradient_workspace_bytes";
+    if (!bytes) return fail(HWSEL_EINVAL, fn, "null pointer");
+    if (int st = check_join(j, fn)) return st;
+    *bytes = hwsel::join_gradient_workspace_bytes(*j);
+    g_err[0] = 0;
+    return HWSEL_OK;
+}
+
+int hwsel_block_join_gradient(const hwsel_join_t *j, const hwsel_matrix_t *x1, const hwsel_matrix_t *y_, const hwsel_matrix_t *gate_,
+                              const hwsel_matrix_t *d_x1_, const hwsel_matrix_t *d_z_, const hwsel_matrix_t *dx_,
+                              const hwsel_matrix_t *dy_, const hwsel_matrix_t *dgate_, float *dw_branch, float *dw_pre, void *workspace,
+                              size_t workspace_bytes, void *stream)
+{
+    static const char *fn = "hwsel_block_join_gradient";
+    if (int st = check_join(j, fn)) return st;
+    const hwsel_matrix_t &y = or_none(y_), &gate = or_none(gate_), &d_x1 = or_none(d_x1_), &d_z = or_none(d_z_), &dx = or_none(dx_),
+                         &dy = or_none(dy_), &dgate = or_none(dgate_);
+    if (!x1 || !x1->data || (!d_x1.data && !d_z.data)) return fail(HWSEL_EINVAL, fn, "null pointer");
+    if (!dx.data && !dy.data && !dgate.data && !dw_branch && !dw_pre) return fail(HWSEL_EINVAL, fn, "no output");
+    if (int st = check_branch(j, y, gate, fn)) return st;
+    if ((!y.data && (dy.data || dw_branch)) || (!gate.data && dgate.data) || (!d_z.data && dw_pre))
+        return fail(HWSEL_EINVAL, fn, "an output without its input");
+    const int32_t block = y.data ? y.dtype : -1;
+    if (int st = check_matrix(*x1, "x1", j->cols, -1, fn)) return st;
+    if (int st = check_matrix(y, "y", j->cols, -1, fn)) return st;
+    if (int st = check_matrix(gate, "gate", j->gate_cols, block, fn)) return st;
+    if (int st = check_matrix(d_x1, "d_x1", j->cols, x1->dtype, fn)) return st;
+    if (int st = check_matrix(d_z, "d_z", j->cols, block, fn)) return st;
+    if (int st = check_matrix(dx, "dx", j->cols, x1->dtype, fn)) return st;
+    if (int st = check_matrix(dy, "dy", j->cols, block, fn)) return st;
+    if (int st = check_matrix(dgate, "dgate", j->gate_cols, block, fn)) return st;
+    if (((uintptr_t)dw_branch & 3u) || ((uintptr_t)dw_pre & 3u)) return fail(HWSEL_EINVAL, fn, "weights' gradients misaligned");
+    const size_t need = hwsel::join_gradient_workspace_bytes(*j);
+    if (need && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need))
+        return fail(HWSEL_EINVAL, fn, "workspace of %zu bytes, %zu needed, 256-byte aligned", workspace_bytes, need);
+    const bool bbf = (y.data ? y.dtype : d_z.dtype) == HWSEL_DTYPE_BF16;
+    return launched(hwsel::launch_block_join_gradient(*j, *x1, y, gate, d_x1, d_z, dx, dy, dgate, dw_branch, dw_pre, workspace,
+                                                      x1->dtype == HWSEL_DTYPE_BF16, bbf, (hipStream_t)stream),
+                    fn);
+}
+
 }  // extern "C"

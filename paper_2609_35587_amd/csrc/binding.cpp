@@ -1,5 +1,6 @@
-// The Python calls of the 8-bit matrices and of drawing candidates: argument
-// checks, results' tensors and the current stream in C++.  A call that takes
+// The Python calls of the 8-bit matrices, of drawing candidates, of their log
+// probabilities, of dropout and of joins: argument checks, results' tensors and
+// the current stream in C++.  A call that takes
 // the GPU 3.5 us (a row through one layer) took the host 13.9 us in Python, most
 // of it in attributes of tensors; it takes 5.6 so, half of it the launch.  Nothing
 // is computed here, and nothing is kept from one call for the next but the
@@ -37,10 +38,18 @@ struct Functions {
     decltype(&hwsel_fp8_layer) layer;
     decltype(&hwsel_sample_workspace_bytes) sample_workspace_bytes;
     decltype(&hwsel_sample_per_problem) sample;
+    decltype(&hwsel_logprob_workspace_bytes) logprob_workspace_bytes;
+    decltype(&hwsel_logprob_per_problem) logprob;
+    decltype(&hwsel_logprob_gradient) logprob_gradient;
+    decltype(&hwsel_dropout) dropout;
+    decltype(&hwsel_block_join) block_join;
+    decltype(&hwsel_block_join_gradient_workspace_bytes) join_gradient_workspace_bytes;
+    decltype(&hwsel_block_join_gradient) block_join_gradient;
     decltype(&hwsel_last_error) last_error;
 } lib;
 PyObject *error_class;                                      // HwselError
 PyObject *k_q, *k_scale, *k_rows, *k_cols, *k_format, *k_block_rows, *k_stream;
+PyObject *k_post_norm, *k_gate_sigmoid, *k_w_branch, *k_w_pre, *k_eps, *k_stream_scale, *k_branch_scale, *k_p, *k_seed, *k_offset, *k_state;
 
 // A reference owned here.
 class Ref {
@@ -480,6 +489,285 @@ PyObject *sample(PyObject *const *v)
     return must(PyTuple_Pack(3, idx.get(), prob.get(), kept.get()));
 }
 
+// The caller's array for a result, or a new one; its address to `data`.
+template <class T>
+Ref array(PyObject *given, const char *name, at::ScalarType type, at::IntArrayRef sizes, const Queue &queue, int device, T *&data)
+{
+    int64_t numel = 1;
+    for (const int64_t n : sizes) numel *= n;
+    if (given != Py_None) {
+        data = static_cast<T *>(argument(given, name, type, numel, device).data_ptr());
+        return Ref(keep(given));
+    }
+    const at::Tensor t = queue.result(sizes, type);
+    data = static_cast<T *>(t.data_ptr());
+    return Ref(must(THPVariable_Wrap(t)));
+}
+
+// The kernels go to a stream of the current device.
+void on_current_device(int device)
+{
+    const int current = (int)c10::hip::current_device();
+    if (device != current) refuse("the operands are on device %d, the current one is %d", device, current);
+}
+
+// What both log probability calls take: scores, segments, picks [P][n] or None, a temperature.
+struct Scored {
+    int device;
+    const float *scores;
+    int64_t R;
+    const int64_t *seg;
+    int32_t P;
+    const int32_t *picks;
+    int32_t n_picks;
+    float temperature = 0.0f;
+    const float *temperature_of = nullptr;
+};
+
+Scored scored(PyObject *scores, PyObject *seg_offsets, PyObject *picks, PyObject *temperature)
+{
+    Scored q;
+    const at::Tensor &s = argument(scores, "scores", at::kFloat, 0, -1);
+    q.device = s.get_device();
+    on_current_device(q.device);
+    const at::Tensor &seg = argument(seg_offsets, "seg_offsets", at::kLong, 2, q.device);
+    q.scores = static_cast<const float *>(s.data_ptr());
+    q.R = s.numel();
+    q.seg = static_cast<const int64_t *>(seg.data_ptr());
+    q.P = int32_of(seg.numel() - 1, "problems");
+    q.picks = nullptr;
+    q.n_picks = 0;
+    if (picks != Py_None) {
+        const at::Tensor &t = argument(picks, "picks", at::kInt, 0, q.device);
+        if (t.dim() != 2 || t.size(0) != q.P) refuse("picks must be [%lld][picks of a problem]", (long long)q.P);
+        q.n_picks = int32_of(t.size(1), "picks of a problem");
+        if (q.n_picks > 0) q.picks = static_cast<const int32_t *>(t.data_ptr());
+    }
+    setting(temperature, "temperature", q.P, q.device, q.temperature, q.temperature_of);
+    return q;
+}
+
+// (scores, seg_offsets, picks, temperature, top, logp, entropy, norm, top_idx, top_logp, workspace, stream)
+PyObject *logprob(PyObject *const *v)
+{
+    const Scored q = scored(v[0], v[1], v[2], v[3]);
+    const Queue queue(v[11], q.device);
+    const int32_t top = int32_of(integer(v[4]), "top");
+    size_t need = 0;
+    check("hwsel_logprob_workspace_bytes", lib.logprob_workspace_bytes(q.R, q.P, top, &need));
+    float *logp_at = nullptr, *entropy_at, *norm_at, *top_logp_at = nullptr;
+    int32_t *top_idx_at = nullptr;
+    const Ref logp = q.n_picks ? array(v[5], "logp", at::kFloat, {q.P, q.n_picks}, queue, q.device, logp_at) : Ref(keep(Py_None)),
+              entropy = array(v[6], "entropy", at::kFloat, {q.P}, queue, q.device, entropy_at),
+              norm = array(v[7], "norm", at::kFloat, {q.P, 2}, queue, q.device, norm_at),
+              top_idx = top ? array(v[8], "top_idx", at::kInt, {q.P, top}, queue, q.device, top_idx_at) : Ref(keep(Py_None)),
+              top_logp = top ? array(v[9], "top_logp", at::kFloat, {q.P, top}, queue, q.device, top_logp_at) : Ref(keep(Py_None));
+    const Workspace w = workspace_of(v[10], need, queue, q.device);
+    check("hwsel_logprob_per_problem",
+          lib.logprob(q.scores, q.R, q.seg, q.P, q.temperature, q.temperature_of, q.picks, q.n_picks, top, logp_at, entropy_at, norm_at,
+                      top_idx_at, top_logp_at, w.data, w.bytes, queue.stream()));
+    return must(PyTuple_Pack(5, logp.get(), entropy.get(), norm.get(), top_idx.get(), top_logp.get()));
+}
+
+// (scores, seg_offsets, norm, picks, d_logp, entropy, d_entropy, temperature, out, stream)
+PyObject *logprob_gradient(PyObject *const *v)
+{
+    const Scored q = scored(v[0], v[1], v[3], v[7]);
+    const Queue queue(v[9], q.device);
+    const auto *norm = static_cast<const float *>(argument(v[2], "norm", at::kFloat, 2 * (int64_t)q.P, q.device).data_ptr());
+    if ((v[3] == Py_None) != (v[4] == Py_None)) refuse("picks and d_logp go together");
+    const auto *d_logp = static_cast<const float *>(argument_or_null(v[4], "d_logp", at::kFloat, (int64_t)q.P * q.n_picks, q.device));
+    const auto *entropy = static_cast<const float *>(argument_or_null(v[5], "entropy", at::kFloat, q.P, q.device));
+    const auto *d_entropy = static_cast<const float *>(argument_or_null(v[6], "d_entropy", at::kFloat, q.P, q.device));
+    float *out_at;
+    Ref out = array(v[8], "out", at::kFloat, {q.R}, queue, q.device, out_at);
+    check("hwsel_logprob_gradient",
+          lib.logprob_gradient(q.scores, q.R, q.seg, q.P, q.temperature, q.temperature_of, norm, q.picks, q.n_picks, d_logp,
+                               d_entropy ? entropy : nullptr, d_entropy, out_at, queue.stream()));
+    return out.release();
+}
+
+float number(PyObject *o)
+{
+    const double d = PyFloat_AsDouble(o);
+    if (d == -1.0 && PyErr_Occurred()) throw Failed{};
+    return (float)d;
+}
+
+uint64_t word(PyObject *o, const char *name)
+{
+    const Ref i(must(PyNumber_Index(o)));
+    const unsigned long long v = PyLong_AsUnsignedLongLong(i.get());
+    if (v == ~0ull && PyErr_Occurred()) {
+        PyErr_Clear();
+        refuse("%s must be within 0 .. 2^64 - 1", name);
+    }
+    return v;
+}
+
+const uint64_t *state_of(PyObject *o, int device)
+{
+    return static_cast<const uint64_t *>(argument_or_null(o, "state", at::kLong, 2, device));
+}
+
+// A matrix of exactly rows x cols (an operand), or none.
+hwsel_matrix_t operand(PyObject *o, const char *name, int64_t rows, int64_t cols, int device)
+{
+    if (o == Py_None) return {nullptr, 0, HWSEL_DTYPE_FP32};
+    const Plain m = plain(tensor(o, name), name, rows, cols, device);
+    if (m.rows != rows || m.cols != cols)
+        refuse("%s is [%lld][%lld], not [%lld][%lld]", name, (long long)m.rows, (long long)m.cols, (long long)rows, (long long)cols);
+    return {m.data, m.ld, m.dtype};
+}
+
+// The first operand, which gives the sizes and the device.
+hwsel_matrix_t leading(PyObject *o, const char *name, int64_t &rows, int64_t &cols, int &device, at::ScalarType &type)
+{
+    const at::Tensor &t = tensor(o, name);
+    device = t.is_cuda() ? t.get_device() : 0;
+    const Plain m = plain(t, name, 1, 1, device);
+    on_current_device(device);
+    rows = m.rows;
+    cols = m.cols;
+    type = t.scalar_type();
+    return {m.data, m.ld, m.dtype};
+}
+
+// The caller's matrix for a result, or a new one of `type`; none (and None) unless wanted.
+Ref target(bool wanted, PyObject *given, const char *name, int64_t rows, int64_t cols, at::ScalarType type, const Queue &queue, int device,
+           hwsel_matrix_t &to)
+{
+    to = {nullptr, 0, HWSEL_DTYPE_FP32};
+    if (!wanted) return Ref(keep(Py_None));
+    if (given != Py_None) {
+        const Plain m = plain(tensor(given, name), name, rows, cols, device);
+        to = {m.data, m.ld, m.dtype};
+        return Ref(keep(given));
+    }
+    const at::Tensor t = queue.result({rows, cols}, type);
+    to = {t.data_ptr(), cols, dtype_code(type, name)};
+    return Ref(must(THPVariable_Wrap(t)));
+}
+
+// (x, p, seed, offset, state, residual, out, stream)
+PyObject *dropout(PyObject *const *v)
+{
+    int64_t rows, cols;
+    int device;
+    at::ScalarType type;
+    const hwsel_matrix_t x = leading(v[0], "x", rows, cols, device, type);
+    const Queue queue(v[7], device);
+    const hwsel_dropout_t how{word(v[2], "seed"), word(v[3], "offset"), state_of(v[4], device), number(v[1])};
+    const hwsel_matrix_t residual = operand(v[5], "residual", rows, cols, device);
+    if (residual.data) type = tensor(v[5], "residual").scalar_type();
+    hwsel_matrix_t y;
+    Ref out = target(true, v[6], "out", rows, cols, type, queue, device, y);
+    check("hwsel_dropout", lib.dropout(&how, rows, cols, &x, &residual, &y, queue.stream()));
+    return out.release();
+}
+
+bool truth(PyObject *o)
+{
+    const int on = PyObject_IsTrue(o);
+    if (on < 0) throw Failed{};
+    return on != 0;
+}
+
+// A join's settings from its dict; keys that are not there have their usual values, others are refused.
+hwsel_join_t join_of(PyObject *d, int64_t rows, int64_t cols, PyObject *gate, int device)
+{
+    if (!PyDict_Check(d)) refuse("join must be a dict");
+    Py_ssize_t known = 0;
+    auto get = [&](PyObject *key) {
+        PyObject *o = PyDict_GetItemWithError(d, key);
+        if (!o && PyErr_Occurred()) throw Failed{};
+        known += o != nullptr;
+        return o;
+    };
+    auto real = [&](PyObject *key, float usual) {
+        PyObject *o = get(key);
+        return o ? number(o) : usual;
+    };
+    auto flag = [&](PyObject *key) {
+        PyObject *o = get(key);
+        return o && truth(o) ? 1 : 0;
+    };
+    auto weights = [&](PyObject *key, const char *name) {
+        PyObject *o = get(key);
+        return o ? static_cast<const float *>(argument_or_null(o, name, at::kFloat, cols, device)) : nullptr;
+    };
+    auto whole = [&](PyObject *key, const char *name) {
+        PyObject *o = get(key);
+        return o ? word(o, name) : 0;
+    };
+    hwsel_join_t j{};
+    j.rows = rows;
+    j.cols = cols;
+    j.w_branch = weights(k_w_branch, "w_branch");
+    j.w_pre = weights(k_w_pre, "w_pre");
+    j.eps = real(k_eps, 1e-6f);
+    j.stream_scale = real(k_stream_scale, 1.0f);
+    j.branch_scale = real(k_branch_scale, 1.0f);
+    j.post_norm = flag(k_post_norm);
+    j.gate_sigmoid = flag(k_gate_sigmoid);
+    j.dropout.p = real(k_p, 0.0f);
+    j.dropout.seed = whole(k_seed, "seed");
+    j.dropout.offset = whole(k_offset, "offset");
+    PyObject *state = get(k_state);
+    j.dropout.state = state ? state_of(state, device) : nullptr;
+    if (known != PyDict_Size(d)) refuse("join has keys that are none of its settings");
+    if (gate != Py_None) {
+        const at::Tensor &g = tensor(gate, "gate");
+        j.gate_cols = g.dim() == 2 && g.size(1) == 1 ? 1 : cols;
+    }
+    return j;
+}
+
+// (join, x, y, gate, dtype, x1, z, with_x1, with_z, stream)
+PyObject *block_join(PyObject *const *v)
+{
+    int64_t rows, cols;
+    int device;
+    at::ScalarType stream_type;
+    const hwsel_matrix_t x = leading(v[1], "x", rows, cols, device, stream_type);
+    const Queue queue(v[9], device);
+    const hwsel_join_t j = join_of(v[0], rows, cols, v[3], device);
+    const hwsel_matrix_t y = operand(v[2], "y", rows, cols, device), gate = operand(v[3], "gate", rows, j.gate_cols, device);
+    const at::ScalarType block_type = v[4] != Py_None ? dtype_of(v[4]) : y.data ? tensor(v[2], "y").scalar_type() : stream_type;
+    hwsel_matrix_t x1, z;
+    const Ref x1_out = target(truth(v[7]), v[5], "x1", rows, cols, stream_type, queue, device, x1),
+              z_out = target(truth(v[8]), v[6], "z", rows, cols, block_type, queue, device, z);
+    check("hwsel_block_join", lib.block_join(&j, &x, &y, &gate, &x1, &z, queue.stream()));
+    return must(PyTuple_Pack(2, x1_out.get(), z_out.get()));
+}
+
+// (join, x1, y, gate, d_x1, d_z, dx, dy, dgate, dw_branch, dw_pre, workspace, stream)
+PyObject *block_join_gradient(PyObject *const *v)
+{
+    int64_t rows, cols;
+    int device;
+    at::ScalarType stream_type;
+    const hwsel_matrix_t x1 = leading(v[1], "x1", rows, cols, device, stream_type);
+    const Queue queue(v[12], device);
+    const hwsel_join_t j = join_of(v[0], rows, cols, v[3], device);
+    const hwsel_matrix_t y = operand(v[2], "y", rows, cols, device), gate = operand(v[3], "gate", rows, j.gate_cols, device),
+                         d_x1 = operand(v[4], "d_x1", rows, cols, device), d_z = operand(v[5], "d_z", rows, cols, device);
+    const at::ScalarType block_type = y.data ? tensor(v[2], "y").scalar_type() : stream_type;
+    hwsel_matrix_t dx, dy, dgate;
+    const Ref dx_out = target(true, v[6], "dx", rows, cols, stream_type, queue, device, dx),
+              dy_out = target(y.data != nullptr, v[7], "dy", rows, cols, block_type, queue, device, dy),
+              dgate_out = target(gate.data != nullptr, v[8], "dgate", rows, j.gate_cols, block_type, queue, device, dgate);
+    float *dw_branch = nullptr, *dw_pre = nullptr;
+    const Ref wb = j.w_branch ? array(v[9], "dw_branch", at::kFloat, {cols}, queue, device, dw_branch) : Ref(keep(Py_None)),
+              wp = j.w_pre && d_z.data ? array(v[10], "dw_pre", at::kFloat, {cols}, queue, device, dw_pre) : Ref(keep(Py_None));
+    size_t need = 0;
+    check("hwsel_block_join_gradient_workspace_bytes", lib.join_gradient_workspace_bytes(&j, &need));
+    const Workspace w = workspace_of(v[11], need, queue, device);
+    check("hwsel_block_join_gradient", lib.block_join_gradient(&j, &x1, &y, &gate, &d_x1, &d_z, &dx, &dy, &dgate, dw_branch, dw_pre, w.data,
+                                                               w.bytes, queue.stream()));
+    return must(PyTuple_Pack(5, dx_out.get(), dy_out.get(), dgate_out.get(), wb.get(), wp.get()));
+}
+
 template <PyObject *(*F)(PyObject *const *), Py_ssize_t N>
 PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -533,6 +821,11 @@ PyMethodDef methods[] = {
     {"fp8_matmul", entry_of(call<matmul, 8>), METH_FASTCALL, nullptr},
     {"fp8_layer", entry_of(call<layer, 7>), METH_FASTCALL, nullptr},
     {"sample_per_problem", entry_of(call<sample, 12>), METH_FASTCALL, nullptr},
+    {"logprob_per_problem", entry_of(call<logprob, 12>), METH_FASTCALL, nullptr},
+    {"logprob_gradient", entry_of(call<logprob_gradient, 10>), METH_FASTCALL, nullptr},
+    {"dropout", entry_of(call<dropout, 8>), METH_FASTCALL, nullptr},
+    {"block_join", entry_of(call<block_join, 10>), METH_FASTCALL, nullptr},
+    {"block_join_gradient", entry_of(call<block_join_gradient, 13>), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "Calls of libhwsel.so that are made in C++.", -1, methods, nullptr, nullptr, nullptr, nullptr};
@@ -545,7 +838,9 @@ PyMODINIT_FUNC PyInit__binding()
         PyObject **key;
         const char *text;
     } keys[] = {{&k_q, "q"}, {&k_scale, "scale"}, {&k_rows, "rows"}, {&k_cols, "cols"}, {&k_format, "format"},
-                {&k_block_rows, "block_rows"}, {&k_stream, "cuda_stream"}};
+                {&k_block_rows, "block_rows"}, {&k_stream, "cuda_stream"}, {&k_post_norm, "post_norm"}, {&k_gate_sigmoid, "gate_sigmoid"},
+                {&k_w_branch, "w_branch"}, {&k_w_pre, "w_pre"}, {&k_eps, "eps"}, {&k_stream_scale, "stream_scale"},
+                {&k_branch_scale, "branch_scale"}, {&k_p, "p"}, {&k_seed, "seed"}, {&k_offset, "offset"}, {&k_state, "state"}};
     for (const auto &k : keys)
         if (!(*k.key = PyUnicode_InternFromString(k.text))) return nullptr;
     return PyModule_Create(&module);

@@ -156,6 +156,27 @@ size_t sample_workspace_bytes(int64_t R, int32_t P, int32_t n_draws);
 hipError_t launch_sample(const float *scores, int64_t R, const int64_t *seg, int32_t P, const hwsel_sampling_t &how,
                          const float *u, int32_t n_draws, int32_t *idx, float *prob, int32_t *kept, void *ws, hipStream_t s);
 
+// Log probabilities (see logprob.hip).
+size_t logprob_workspace_bytes(int64_t R, int32_t P, int32_t top);
+hipError_t launch_logprob(const float *scores, int64_t R, const int64_t *seg, int32_t P, float temperature, const float *temperature_of,
+                          const int32_t *picks, int32_t n_picks, int32_t top, float *logp, float *entropy, float *norm, int32_t *top_idx,
+                          float *top_logp, void *ws, hipStream_t s);
+hipError_t launch_logprob_gradient(const float *scores, int64_t R, const int64_t *seg, int32_t P, float temperature,
+                                   const float *temperature_of, const float *norm, const int32_t *picks, int32_t n_picks,
+                                   const float *d_logp, const float *entropy, const float *d_entropy, float *d_scores, hipStream_t s);
+
+// Dropout and joins of blocks (see dropout.hip, join.hip).  A matrix that is
+// absent has no data; sbf, bbf: the stream's and the block's matrices are bf16.
+hipError_t launch_dropout(const hwsel_dropout_t &how, int64_t rows, int64_t cols, const hwsel_matrix_t &X,
+                          const hwsel_matrix_t &residual, const hwsel_matrix_t &Y, hipStream_t s);
+hipError_t launch_block_join(const hwsel_join_t &j, const hwsel_matrix_t &x, const hwsel_matrix_t &y, const hwsel_matrix_t &gate,
+                             const hwsel_matrix_t &x1, const hwsel_matrix_t &z, bool sbf, bool bbf, hipStream_t s);
+size_t join_gradient_workspace_bytes(const hwsel_join_t &j);
+hipError_t launch_block_join_gradient(const hwsel_join_t &j, const hwsel_matrix_t &x1, const hwsel_matrix_t &y,
+                                      const hwsel_matrix_t &gate, const hwsel_matrix_t &dx1, const hwsel_matrix_t &dz,
+                                      const hwsel_matrix_t &dx, const hwsel_matrix_t &dy, const hwsel_matrix_t &dgate, float *dwb,
+                                      float *dwp, void *ws, bool sbf, bool bbf, hipStream_t s);
+
 // Order-preserving map of fp32 to uint32 (x < y <=> key(x) < key(y) for
 // non-NaN values; -0 must be normalised to +0 first).
 __device__ __forceinline__ uint32_t order_key(float v)

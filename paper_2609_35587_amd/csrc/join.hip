@@ -1,0 +1,405 @@
+// Joining a block's result to the residual stream, with the norms after the
+// block and before the next one, gate, dropout and scales; and its gradients.
+//   u = w_branch norm(y);  v = dropout(branch g u);  x1 = stream x + v;  z = w_pre norm(x1)
+// With d = d_x1 + r1 (dn - xn mean(dn xn)), dn = d_z w_pre, xn = x1 r1:
+//   dx = stream d;  dv = dropout(branch d);  dg = dv u;  du = dv g;  dw_branch = sum du yn;
+//   dy = r (dn' - yn mean(dn' yn)), dn' = du w_branch;  dw_pre = sum d_z xn
+#include "rows.hpp"
+
+namespace hwsel {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct In {
+    const void *p;
+    int64_t ld;
+};
+
+struct Out {
+    void *p;
+    int64_t ld;
+};
+
+enum { kNoGate = 0, kRowGate = 1, kElementGate = 2 };
+
+struct Common {
+    int64_t cols;
+    int32_t rows;
+    const float *wb, *wp;
+    float eps, inv_cols, stream, branch;
+    int32_t post_norm, gate_kind, sigmoid;
+    Dropout drop;
+    int64_t row0;                                           // the launch's first row
+};
+
+struct Forward {
+    Common c;
+    In x, y, gate;
+    Out x1, z;
+};
+
+struct Backward {
+    Common c;
+    In x1, y, gate, dx1, dz;
+    Out dx, dy, dgate;
+    float *stats;                                           // [rows][4] of the long rows: r1, m1, r, m
+    float *parts;                                           // [parts][2][cols]
+    int32_t n_parts, rows_each, want_wb, want_wp;
+};
+
+__device__ __forceinline__ float norm_factor(float sum, const Common &c) { return 1.0f / __builtin_sqrtf(sum * c.inv_cols + c.eps); }
+
+__device__ __forceinline__ float gate_value(float a, int sigmoid)
+{
+    return sigmoid ? __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * a)) : a;
+}
+
+// The gate's slope: s (1 - s) of a sigmoid, without the difference.
+__device__ __forceinline__ float gate_slope(float a, int sigmoid)
+{
+    const float e = __builtin_amdgcn_exp2f(-kLog2e * __builtin_fabsf(a)), q = __builtin_amdgcn_rcpf(1.0f + e);
+    return sigmoid ? e * q * q : 1.0f;
+}
+
+// Sums of N values over a workgroup, in every thread.
+template <int NT, int N>
+__device__ __forceinline__ void block_sums(float (&v)[N], float (&sh)[N][NT / 64])
+{
+    group_totals<64>(v);
+    __syncthreads();                                        // the last sums have been read
+    if ((threadIdx.x & 63) == 63) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) sh[i][threadIdx.x >> 6] = v[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        v[i] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < NT / 64; ++w) v[i] += sh[i][w];
+    }
+}
+
+__device__ __forceinline__ void weights8(const float *w, int64_t col, int64_t n, float (&v)[8])
+{
+    if (w) {
+        const Eight<false> e = load8<false>(w, col, n);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = e.at(i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 1.0f;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Rows of any length: a workgroup goes through a row several times.
+// ---------------------------------------------------------------------------
+constexpr int kLong = 1024;
+
+template <bool SBF, bool BBF>
+__global__ __launch_bounds__(kLong) void k_join_long(Forward a)
+{
+    __shared__ float sh[1][kLong / 64];
+    const Common &c = a.c;
+    const int64_t row = c.row0 + blockIdx.x;
+    const Mask m = mask_of(c.drop);
+    float r = 1.0f;
+    if (a.y.p && c.post_norm) {
+        float s[1] = {0.0f};
+        for (int64_t col = threadIdx.x * 8; col < c.cols; col += kLong * 8) {
+            const Eight<BBF> y = load8<BBF>(a.y.p, row * a.y.ld + col, c.cols - col);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[0] += y.at(i) * y.at(i);
+        }
+        block_sums<kLong>(s, sh);
+        r = norm_factor(s[0], c);
+    }
+    const float row_gate = c.gate_kind == kRowGate ? gate_value(load1<BBF>(a.gate.p, row * a.gate.ld), c.sigmoid) : 1.0f;
+    auto joined = [&](int64_t col, float (&x1)[8]) {
+        const int64_t n = c.cols - col;
+        const Eight<SBF> x = load8<SBF>(a.x.p, row * a.x.ld + col, n);
+        float v[8] = {};
+        if (a.y.p) {
+            const Eight<BBF> y = load8<BBF>(a.y.p, row * a.y.ld + col, n);
+            float w[8];
+            weights8(c.wb, col, n, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = c.branch * row_gate * (y.at(i) * r * w[i]);
+            if (c.gate_kind == kElementGate) {
+                const Eight<BBF> g = load8<BBF>(a.gate.p, row * a.gate.ld + col, n);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] *= gate_value(g.at(i), c.sigmoid);
+            }
+            if (m.least != 0) drop8(m, (uint32_t)row, (uint32_t)(col >> 3), v);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x1[i] = i < n ? c.stream * x.at(i) + v[i] : 0.0f;
+    };
+    float r1 = 1.0f;
+    if (a.z.p) {
+        float s[1] = {0.0f};
+        for (int64_t col = threadIdx.x * 8; col < c.cols; col += kLong * 8) {
+            float x1[8];
+            joined(col, x1);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[0] += x1[i] * x1[i];
+        }
+        block_sums<kLong>(s, sh);
+        r1 = norm_factor(s[0], c);
+    }
+    for (int64_t col = threadIdx.x * 8; col < c.cols; col += kLong * 8) {
+        const int64_t n = c.cols - col;
+        float x1[8];
+        joined(col, x1);
+        if (a.x1.p) store8<SBF>(a.x1.p, row * a.x1.ld + col, n, x1);
+        if (a.z.p) {
+            float w[8], z[8];
+            weights8(c.wp, col, n, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[i] = x1[i] * r1 * w[i];
+            store8<BBF>(a.z.p, row * a.z.ld + col, n, z);
+        }
+    }
+}
+
+// d of eight columns: d_x1 and the norm before the next block; dn and xn of that.
+template <bool SBF, bool BBF>
+struct Stream8 {
+    Eight<SBF> x1, dx1;
+    Eight<BBF> dz;
+
+    __device__ __forceinline__ void load(const Backward &a, int64_t row, int64_t col, int64_t n)
+    {
+        x1 = load8<SBF>(a.x1.p, row * a.x1.ld + col, n);
+        dx1 = load8<SBF>(a.dx1.p, row * a.dx1.ld + col, a.dx1.p ? n : 0);
+        dz = load8<BBF>(a.dz.p, row * a.dz.ld + col, a.dz.p ? n : 0);
+    }
+    __device__ __forceinline__ float d(int i, float wp, float r1, float m1) const
+    {
+        return dx1.at(i) + r1 * (dz.at(i) * wp - x1.at(i) * r1 * m1);
+    }
+};
+
+// dv of eight columns from their d.
+__device__ __forceinline__ void branch8(const Common &c, const Mask &m, int64_t row, int64_t col, const float (&d)[8], float (&dv)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dv[i] = c.branch * d[i];
+    if (m.least != 0) drop8(m, (uint32_t)row, (uint32_t)(col >> 3), dv);
+}
+
+// What the columns' pass needs of each row, and the gradient of its gate.
+template <bool SBF, bool BBF>
+__global__ __launch_bounds__(kLong) void k_join_long_stats(Backward a)
+{
+    __shared__ float sh3[3][kLong / 64], sh2[2][kLong / 64];
+    const Common &c = a.c;
+    const int64_t row = c.row0 + blockIdx.x;
+    const Mask m = mask_of(c.drop);
+    float s[3] = {};
+    for (int64_t col = threadIdx.x * 8; col < c.cols; col += kLong * 8) {
+        const int64_t n = c.cols - col;
+        if (a.dz.p) {
+            const Eight<SBF> x1 = load8<SBF>(a.x1.p, row * a.x1.ld + col, n);
+            const Eight<BBF> dz = load8<BBF>(a.dz.p, row * a.dz.ld + col, n);
+            float w[8];
+            weights8(c.wp, col, n, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                s[0] += x1.at(i) * x1.at(i);
+                s[1] += dz.at(i) * w[i] * x1.at(i);
+            }
+        }
+        if (a.y.p && c.post_norm) {
+            const Eight<BBF> y = load8<BBF>(a.y.p, row * a.y.ld + col, n);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[2] += y.at(i) * y.at(i);
+        }
+    }
+    block_sums<kLong>(s, sh3);
+    const float r1 = a.dz.p ? norm_factor(s[0], c) : 0.0f, m1 = r1 * s[1] * c.inv_cols;
+    const float r = c.post_norm ? norm_factor(s[2], c) : 1.0f;
+    float t[2] = {};
+    if (a.y.p && (c.post_norm || c.gate_kind == kRowGate)) {
+        const float gate = c.gate_kind == kRowGate ? load1<BBF>(a.gate.p, row * a.gate.ld) : 1.0f;
+        const float row_gate = c.gate_kind == kRowGate ? gate_value(gate, c.sigmoid) : 1.0f;
+        for (int64_t col = threadIdx.x * 8; col < c.cols; col += kLong * 8) {
+            const int64_t n = c.cols - col;
+            Stream8<SBF, BBF> q;
+            q.load(a, row, col, n);
+            const Eight<BBF> y = load8<BBF>(a.y.p, row * a.y.ld + col, n);
+            const Eight<BBF> g = load8<BBF>(a.gate.p, row * a.gate.ld + col, c.gate_kind == kElementGate ? n : 0);
+            float wp[8], wb[8], d[8], dv[8];
+            weights8(c.wp, col, n, wp);
+            weights8(c.wb, col, n, wb);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) d[i] = q.d(i, wp[i], r1, m1);
+            branch8(c, m, row, col, d, dv);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float yn = y.at(i) * r, gi = c.gate_kind == kElementGate ? gate_value(g.at(i), c.sigmoid) : row_gate;
+                t[0] += dv[i] * gi * wb[i] * yn;
+                t[1] += dv[i] * wb[i] * yn;
+            }
+        }
+        block_sums<kLong>(t, sh2);
+        if (threadIdx.x == 0 && a.dgate.p && c.gate_kind == kRowGate) {
+            const float dg = t[1] * gate_slope(gate, c.sigmoid);
+            if constexpr (BBF) static_cast<uint16_t *>(a.dgate.p)[row * a.dgate.ld] = (uint16_t)bf16_pair(dg, 0.0f);
+            else static_cast<float *>(a.dgate.p)[row * a.dgate.ld] = dg;
+        }
+    }
+    if (threadIdx.x == 0) {
+        float *st = a.stats + row * 4;
+        st[0] = r1;
+        st[1] = m1;
+        st[2] = r;
+        st[3] = c.post_norm ? t[0] * c.inv_cols : 0.0f;
+    }
+}
+
+// The gradients of 2,048 columns of some rows, and their sums over those rows.
+constexpr int kTile = 256;
+
+template <bool SBF, bool BBF>
+__global__ __launch_bounds__(kTile) void k_join_long_columns(Backward a)
+{
+    const Common &c = a.c;
+    const int64_t col = ((int64_t)blockIdx.x * kTile + threadIdx.x) * 8, n = c.cols - col;
+    if (n <= 0) return;
+    const Mask m = mask_of(c.drop);
+    float wp[8], wb[8], swb[8] = {}, swp[8] = {};
+    weights8(c.wp, col, n, wp);
+    weights8(c.wb, col, n, wb);
+    const int64_t first = (int64_t)blockIdx.y * a.rows_each, last = first + a.rows_each < c.rows ? first + a.rows_each : c.rows;
+    for (int64_t row = first; row < last; ++row) {
+        const float *st = a.stats + row * 4;
+        const float r1 = st[0], m1 = st[1], r = st[2], mean = st[3];
+        Stream8<SBF, BBF> q;
+        q.load(a, row, col, n);
+        float d[8], o[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            d[i] = q.d(i, wp[i], r1, m1);
+            swp[i] += q.dz.at(i) * (q.x1.at(i) * r1);
+            o[i] = c.stream * d[i];
+        }
+        const Eight<BBF> y = load8<BBF>(a.y.p, row * a.y.ld + col, a.y.p ? n : 0);
+        const Eight<BBF> g = load8<BBF>(a.gate.p, row * a.gate.ld + col, c.gate_kind == kElementGate ? n : 0);
+        if (a.dx.p) store8<SBF>(a.dx.p, row * a.dx.ld + col, n, o);
+        if (!a.y.p) continue;
+        const float row_gate = c.gate_kind == kRowGate ? gate_value(load1<BBF>(a.gate.p, row * a.gate.ld), c.sigmoid) : 1.0f;
+        float dv[8];
+        branch8(c, m, row, col, d, dv);
+        float dg[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float yn = y.at(i) * r, gi = c.gate_kind == kElementGate ? gate_value(g.at(i), c.sigmoid) : row_gate;
+            dg[i] = dv[i] * (yn * wb[i]) * (c.gate_kind == kElementGate ? gate_slope(g.at(i), c.sigmoid) : 0.0f);
+            const float du = dv[i] * gi;
+            swb[i] += du * yn;
+            o[i] = r * (du * wb[i] - yn * mean);
+        }
+        if (a.dy.p) store8<BBF>(a.dy.p, row * a.dy.ld + col, n, o);
+        if (a.dgate.p && c.gate_kind == kElementGate) store8<BBF>(a.dgate.p, row * a.dgate.ld + col, n, dg);
+    }
+    float *part = a.parts + (int64_t)blockIdx.y * 2 * c.cols;
+    if (a.want_wb) store8<false>(part, col, n, swb);
+    if (a.want_wp) store8<false>(part, c.cols + col, n, swp);
+}
+
+// Sums of the parts: dw_branch and dw_pre.
+__global__ __launch_bounds__(kTile) void k_join_sums(const float *__restrict__ parts, int32_t n_parts, int64_t cols, float *dwb, float *dwp)
+{
+    const int64_t col = (int64_t)blockIdx.x * kTile + threadIdx.x;
+    float *out = blockIdx.y ? dwp : dwb;
+    if (col >= cols || !out) return;
+    float s = 0.0f;
+    for (int32_t i = 0; i < n_parts; ++i) s += parts[((int64_t)i * 2 + blockIdx.y) * cols + col];
+    out[col] = s;
+}
+
+Common common_of(const hwsel_join_t &j, bool has_y)
+{
+    Common c{};
+    c.cols = j.cols;
+    c.rows = (int32_t)j.rows;
+    c.wb = j.w_branch;
+    c.wp = j.w_pre;
+    c.eps = j.eps;
+    c.inv_cols = 1.0f / (float)j.cols;
+    c.stream = j.stream_scale;
+    c.branch = j.branch_scale;
+    c.post_norm = has_y && j.post_norm;
+    c.gate_kind = j.gate_cols == 0 ? kNoGate : j.gate_cols == 1 && j.cols != 1 ? kRowGate : kElementGate;
+    c.sigmoid = j.gate_sigmoid;
+    c.drop = dropout_of(j.dropout);
+    return c;
+}
+
+In in_of(const hwsel_matrix_t &m) { return {m.data, m.ld}; }
+Out out_of(const hwsel_matrix_t &m) { return {m.data, m.ld}; }
+
+// go<stream in bf16, block in bf16>()
+template <class F>
+void by_types(bool sbf, bool bbf, F &&go)
+{
+    if (sbf) bbf ? go.template operator()<true, true>() : go.template operator()<true, false>();
+    else bbf ? go.template operator()<false, true>() : go.template operator()<false, false>();
+}
+
+// f(rows) with c.row0 set for spans of rows that are a launch each of kLong threads a row: fewer than 2^32.
+template <class F>
+void each_row_span(Common &c, F &&f)
+{
+    constexpr int64_t kSpan = (int64_t)1 << 21;
+    for (c.row0 = 0; c.row0 < c.rows; c.row0 += kSpan) f((unsigned)(c.rows - c.row0 < kSpan ? c.rows - c.row0 : kSpan));
+    c.row0 = 0;
+}
+
+constexpr int32_t kMostParts = 256;
+
+int32_t parts_of(int64_t rows) { return (int32_t)(rows < kMostParts ? rows : kMostParts); }
+
+size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+}  // namespace
+
+size_t join_gradient_workspace_bytes(const hwsel_join_t &j)
+{
+    return up256((size_t)j.rows * 16) + (size_t)parts_of(j.rows) * 2 * (size_t)j.cols * 4;
+}
+
+hipError_t launch_block_join(const hwsel_join_t &j, const hwsel_matrix_t &x, const hwsel_matrix_t &y, const hwsel_matrix_t &gate,
+                             const hwsel_matrix_t &x1, const hwsel_matrix_t &z, bool sbf, bool bbf, hipStream_t s)
+{
+    Forward a{common_of(j, y.data != nullptr), in_of(x), in_of(y), in_of(gate), out_of(x1), out_of(z)};
+    by_types(sbf, bbf, [&]<bool SBF, bool BBF>() {
+        each_row_span(a.c, [&](unsigned n) { hipLaunchKernelGGL((k_join_long<SBF, BBF>), dim3(n), dim3(kLong), 0, s, a); });
+    });
+    return hipGetLastError();
+}
+
+hipError_t launch_block_join_gradient(const hwsel_join_t &j, const hwsel_matrix_t &x1, const hwsel_matrix_t &y,
+                                      const hwsel_matrix_t &gate, const hwsel_matrix_t &dx1, const hwsel_matrix_t &dz,
+                                      const hwsel_matrix_t &dx, const hwsel_matrix_t &dy, const hwsel_matrix_t &dgate, float *dwb,
+                                      float *dwp, void *ws, bool sbf, bool bbf, hipStream_t s)
+{
+    Backward a{common_of(j, y.data != nullptr), in_of(x1), in_of(y), in_of(gate), in_of(dx1), in_of(dz), out_of(dx), out_of(dy), out_of(dgate),
+               static_cast<float *>(ws), reinterpret_cast<float *>(static_cast<char *>(ws) + up256((size_t)j.rows * 16)), 0, 0,
+               dwb != nullptr, dwp != nullptr};
+    a.rows_each = (int32_t)((j.rows + kMostParts - 1) / kMostParts);
+    a.n_parts = (int32_t)((j.rows + a.rows_each - 1) / a.rows_each);
+    const unsigned strips = (unsigned)((j.cols + kTile * 8 - 1) / (kTile * 8));
+    by_types(sbf, bbf, [&]<bool SBF, bool BBF>() {
+        each_row_span(a.c, [&](unsigned n) { hipLaunchKernelGGL((k_join_long_stats<SBF, BBF>), dim3(n), dim3(kLong), 0, s, a); });
+        hipLaunchKernelGGL((k_join_long_columns<SBF, BBF>), dim3(strips, (unsigned)a.n_parts), dim3(kTile), 0, s, a);
+    });
+    if (dwb || dwp)
+        hipLaunchKernelGGL(k_join_sums, dim3((unsigned)((j.cols + kTile - 1) / kTile), 2), dim3(kTile), 0, s, a.parts, a.n_parts, j.cols, dwb, dwp);
+    return hipGetLastError();
+}
+
+}  // namespace hwsel

@@ -1,5 +1,6 @@
-"""Python binding of libhwsel.so (ctypes; the calls on 8-bit matrices and the
-draws through _binding.so, whose checks in C++ take 3 us where Python's took 11).
+"""Python binding of libhwsel.so (ctypes; the calls on 8-bit matrices, the draws,
+their log probabilities, dropout and joins through _binding.so, whose checks in
+C++ take 3 us where Python's took 11).
 
 The functions carry the C ABI's names and only marshal arguments: torch
 tensors in device memory become raw pointers, the current torch stream
@@ -76,6 +77,20 @@ class hwsel_sampling_t(C.Structure):
                 ("min_p_of", C.c_void_p)]
 
 
+class hwsel_matrix_t(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("ld", C.c_int64), ("dtype", C.c_int32)]
+
+
+class hwsel_dropout_t(C.Structure):
+    _fields_ = [("seed", C.c_uint64), ("offset", C.c_uint64), ("state", C.c_void_p), ("p", C.c_float)]
+
+
+class hwsel_join_t(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("w_branch", C.c_void_p), ("w_pre", C.c_void_p),
+                ("eps", C.c_float), ("stream_scale", C.c_float), ("branch_scale", C.c_float), ("post_norm", C.c_int32),
+                ("gate_sigmoid", C.c_int32), ("gate_cols", C.c_int64), ("dropout", hwsel_dropout_t)]
+
+
 _lib = None
 
 
@@ -128,6 +143,14 @@ def lib() -> C.CDLL:
         L.hwsel_sample_workspace_bytes.argtypes = [i64, i32, i32, C.POINTER(sz)]
         L.hwsel_sample_per_problem.argtypes = [vp, i64, vp, i32, C.POINTER(hwsel_sampling_t), vp, i32, vp, vp, vp, vp,
                                                sz, vp]
+        f32, mat, join = C.c_float, C.POINTER(hwsel_matrix_t), C.POINTER(hwsel_join_t)
+        L.hwsel_logprob_workspace_bytes.argtypes = [i64, i32, i32, C.POINTER(sz)]
+        L.hwsel_logprob_per_problem.argtypes = [vp, i64, vp, i32, f32, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.hwsel_logprob_gradient.argtypes = [vp, i64, vp, i32, f32, vp, vp, vp, i32, vp, vp, vp, vp, vp]
+        L.hwsel_dropout.argtypes = [C.POINTER(hwsel_dropout_t), i64, i64, mat, mat, mat, vp]
+        L.hwsel_block_join.argtypes = [join, mat, mat, mat, mat, mat, vp]
+        L.hwsel_block_join_gradient_workspace_bytes.argtypes = [join, C.POINTER(sz)]
+        L.hwsel_block_join_gradient.argtypes = [join, mat, mat, mat, mat, mat, mat, mat, mat, vp, vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -136,7 +159,8 @@ _binding = None
 # as csrc/binding.cpp lists them
 _BOUND = ("hwsel_fp8_quantise", "hwsel_fp8_dequantise", "hwsel_fp8_transpose", "hwsel_fp8_matmul_workspace_bytes",
           "hwsel_fp8_matmul", "hwsel_fp8_layer", "hwsel_sample_workspace_bytes", "hwsel_sample_per_problem",
-          "hwsel_last_error")
+          "hwsel_logprob_workspace_bytes", "hwsel_logprob_per_problem", "hwsel_logprob_gradient", "hwsel_dropout",
+          "hwsel_block_join", "hwsel_block_join_gradient_workspace_bytes", "hwsel_block_join_gradient", "hwsel_last_error")
 
 
 def _calls():
@@ -772,6 +796,80 @@ def hwsel_sample_per_problem(scores: torch.Tensor, seg_offsets: torch.Tensor, u:
     int32 [P])."""
     return (_binding or _calls()).sample_per_problem(scores, seg_offsets, u, temperature, top_k, top_p, min_p, idx, prob, kept,
                                                      workspace, stream)
+
+
+def hwsel_logprob_workspace_bytes(R: int, P: int, top: int = 0) -> int:
+    n = C.c_size_t(0)
+    _check("hwsel_logprob_workspace_bytes", lib().hwsel_logprob_workspace_bytes(R, P, top, C.byref(n)))
+    return int(n.value)
+
+
+def hwsel_logprob_per_problem(scores: torch.Tensor, seg_offsets: torch.Tensor, picks: torch.Tensor | None = None,
+                              temperature=1.0, top: int = 0, logp: torch.Tensor | None = None,
+                              entropy: torch.Tensor | None = None, norm: torch.Tensor | None = None,
+                              top_idx: torch.Tensor | None = None, top_logp: torch.Tensor | None = None,
+                              workspace: torch.Tensor | None = None, stream=None):
+    """Log probabilities of every problem's candidates picks int32 [P][n] under
+    the softmax of its scores at a temperature (a number or a device tensor
+    [P]).  Returns (logp fp32 [P][n] or None, entropy fp32 [P], norm fp32
+    [P][2], top_idx int32 [P][top] or None, top_logp fp32 [P][top] or None)."""
+    return (_binding or _calls()).logprob_per_problem(scores, seg_offsets, picks, temperature, top, logp, entropy, norm,
+                                                      top_idx, top_logp, workspace, stream)
+
+
+def hwsel_logprob_gradient(scores: torch.Tensor, seg_offsets: torch.Tensor, norm: torch.Tensor,
+                           picks: torch.Tensor | None = None, d_logp: torch.Tensor | None = None,
+                           entropy: torch.Tensor | None = None, d_entropy: torch.Tensor | None = None,
+                           temperature=1.0, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """The scores' gradient fp32 [R] from those of hwsel_logprob_per_problem's
+    logp [P][n] and, given d_entropy [P], of its entropy; norm and entropy as
+    that call wrote them."""
+    return (_binding or _calls()).logprob_gradient(scores, seg_offsets, norm, picks, d_logp, entropy, d_entropy,
+                                                   temperature, out, stream)
+
+
+def hwsel_dropout(x: torch.Tensor, p: float, seed: int = 0, offset: int = 0, state: torch.Tensor | None = None,
+                  residual: torch.Tensor | None = None, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """residual + x with a share p of its elements dropped and the others
+    divided by the share kept; the mask is a function of (seed, offset), or of
+    the device tensor state int64 [2], and an element's place.  The gradient of
+    x is the same call on the result's gradient, without a residual."""
+    return (_binding or _calls()).dropout(x, p, seed, offset, state, residual, out, stream)
+
+
+# ----------------------------------------------------------------------------
+# Joins of blocks to a residual stream.  A join is a dict; its keys and what
+# they are where they are missing: post_norm False, gate_sigmoid False,
+# w_branch None, w_pre None (fp32 [cols]), eps 1e-6, stream_scale 1.0,
+# branch_scale 1.0, p 0.0, seed 0, offset 0, state None (see hwsel_join_t).
+# ----------------------------------------------------------------------------
+def hwsel_block_join(join: dict, x: torch.Tensor, y: torch.Tensor | None = None, gate: torch.Tensor | None = None,
+                     dtype: torch.dtype | None = None, x1: torch.Tensor | None = None, z: torch.Tensor | None = None,
+                     with_x1: bool = True, with_z: bool = True, stream=None):
+    """x1 = stream_scale x + dropout(branch_scale g w_branch norm(y)) and z =
+    w_pre norm(x1).  gate: [rows][cols], [rows][1] or None.  z has y's dtype,
+    without y `dtype` or x's.  Returns (x1 or None, z or None)."""
+    return (_binding or _calls()).block_join(join, x, y, gate, dtype, x1, z, with_x1, with_z, stream)
+
+
+def hwsel_block_join_gradient_workspace_bytes(rows: int, cols: int) -> int:
+    n, j = C.c_size_t(0), hwsel_join_t(rows=rows, cols=cols, eps=1e-6, stream_scale=1.0, branch_scale=1.0)
+    _check("hwsel_block_join_gradient_workspace_bytes",
+           lib().hwsel_block_join_gradient_workspace_bytes(C.byref(j), C.byref(n)))
+    return int(n.value)
+
+
+def hwsel_block_join_gradient(join: dict, x1: torch.Tensor, y: torch.Tensor | None = None,
+                              gate: torch.Tensor | None = None, d_x1: torch.Tensor | None = None,
+                              d_z: torch.Tensor | None = None, dx: torch.Tensor | None = None,
+                              dy: torch.Tensor | None = None, dgate: torch.Tensor | None = None,
+                              dw_branch: torch.Tensor | None = None, dw_pre: torch.Tensor | None = None,
+                              workspace: torch.Tensor | None = None, stream=None):
+    """Gradients of hwsel_block_join from those of x1 and z (either may be
+    None), x1 as it was written.  Returns (dx, dy, dgate, dw_branch, dw_pre),
+    None for what the join does not have."""
+    return (_binding or _calls()).block_join_gradient(join, x1, y, gate, d_x1, d_z, dx, dy, dgate, dw_branch, dw_pre,
+                                                      workspace, stream)
 
 
 def declared_functions() -> list[str]:
