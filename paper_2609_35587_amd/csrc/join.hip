@@ -93,6 +93,290 @@ __device__ __forceinline__ void weights8(const float *w, int64_t col, int64_t n,
     }
 }
 
+// d of eight columns: d_x1 and the norm before the next block; dn and xn of that.
+template <bool SBF, bool BBF>
+struct Stream8 {
+    Eight<SBF> x1, dx1;
+    Eight<BBF> dz;
+
+    __device__ __forceinline__ void load(const Backward &a, int64_t row, int64_t col, int64_t n)
+    {
+        x1 = load8<SBF>(a.x1.p, row * a.x1.ld + col, a.dz.p ? n : 0);   // (of no use without d_z)
+        dx1 = load8<SBF>(a.dx1.p, row * a.dx1.ld + col, a.dx1.p ? n : 0);
+        dz = load8<BBF>(a.dz.p, row * a.dz.ld + col, a.dz.p ? n : 0);
+    }
+    __device__ __forceinline__ float d(int i, float wp, float r1, float m1) const
+    {
+        return dx1.at(i) + r1 * (dz.at(i) * wp - x1.at(i) * r1 * m1);
+    }
+};
+
+// dv of eight columns from their d.
+__device__ __forceinline__ void branch8(const Common &c, const Mask &m, int64_t row, int64_t col, const float (&d)[8], float (&dv)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dv[i] = c.branch * d[i];
+    if (m.least != 0) drop8(m, (uint32_t)row, (uint32_t)(col >> 3), dv);
+}
+
+template <int CTRL>
+__device__ __forceinline__ float ror_add(float v)
+{
+    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+
+// Sums of N values over LANES neighbouring threads, in each of them: rotations
+// within 16 lanes, the four rows of a wave by scalar reads, waves through LDS
+// (two buffers in turn, so that a sum costs one barrier).
+template <int LANES>
+struct Shared {
+    float v[2][4][LANES / 64 > 0 ? LANES / 64 : 1];
+};
+
+template <int LANES, int N>
+__device__ __forceinline__ void lane_sums(float (&v)[N], Shared<LANES> &sh, int &turn)
+{
+    static_assert(N <= 4, "room in Shared");
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = ror_add<0x121>(ror_add<0x122>(ror_add<0x124>(ror_add<0x128>(v[i]))));
+    if constexpr (LANES >= 64) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int b = __float_as_int(v[i]);
+            v[i] = (__int_as_float(__builtin_amdgcn_readlane(b, 0)) + __int_as_float(__builtin_amdgcn_readlane(b, 16))) +
+                   (__int_as_float(__builtin_amdgcn_readlane(b, 32)) + __int_as_float(__builtin_amdgcn_readlane(b, 48)));
+        }
+    }
+    if constexpr (LANES > 64) {
+        constexpr int kWaves = LANES / 64;
+        auto &to = sh.v[turn];
+        turn ^= 1;
+        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) to[i][threadIdx.x >> 6] = v[i];
+        }
+        lds_barrier();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v[i] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) v[i] += to[i][w];
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Rows that fit the registers of LANES threads, 8 K columns each: a row is read
+// once and written once.  Threads keep their columns from row to row.
+// ---------------------------------------------------------------------------
+constexpr int threads_of(int lanes) { return lanes > 256 ? lanes : 256; }
+
+template <int LANES>
+__device__ __forceinline__ int64_t first_row()
+{
+    constexpr int kGroups = threads_of(LANES) / LANES;
+    const int group = (int)threadIdx.x / LANES;
+    return (int64_t)blockIdx.x * kGroups + (LANES >= 64 ? __builtin_amdgcn_readfirstlane(group) : group);
+}
+
+template <bool SBF, bool BBF, int LANES, int K>
+__global__ __launch_bounds__(threads_of(LANES)) void k_join(Forward a)
+{
+    __shared__ Shared<LANES> sh;
+    constexpr int kGroups = threads_of(LANES) / LANES;
+    const Common &c = a.c;
+    const Mask m = mask_of(c.drop);
+    const int64_t col0 = (threadIdx.x % LANES) * 8;
+    auto col_of = [&](int k) { return col0 + (int64_t)k * LANES * 8; };
+    float wb[K][8], wp[K][8];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        weights8(c.wb, col_of(k), c.cols - col_of(k), wb[k]);
+        weights8(c.wp, col_of(k), c.cols - col_of(k), wp[k]);
+    }
+    int turn = 0;
+    for (int64_t row = first_row<LANES>(); row < c.rows; row += (int64_t)gridDim.x * kGroups) {
+        Eight<SBF> x[K];
+        Eight<BBF> y[K], g[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int64_t col = col_of(k), n = c.cols - col;
+            x[k] = load8<SBF>(a.x.p, row * a.x.ld + col, n);
+            if (a.y.p) y[k] = load8<BBF>(a.y.p, row * a.y.ld + col, n);
+            if (c.gate_kind == kElementGate) g[k] = load8<BBF>(a.gate.p, row * a.gate.ld + col, n);
+        }
+        float x1[K][8];
+        if (a.y.p) {
+            const float row_gate = c.gate_kind == kRowGate ? gate_value(load1<BBF>(a.gate.p, row * a.gate.ld), c.sigmoid) : 1.0f;
+            float r = 1.0f;
+            if (c.post_norm) {
+                float t[1] = {0.0f};
+#pragma unroll
+                for (int k = 0; k < K; ++k)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) t[0] += y[k].at(i) * y[k].at(i);
+                lane_sums<LANES>(t, sh, turn);
+                r = norm_factor(t[0], c);
+            }
+            const float scale = c.branch * row_gate * r;
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = scale * (y[k].at(i) * wb[k][i]);
+                if (c.gate_kind == kElementGate) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] *= gate_value(g[k].at(i), c.sigmoid);
+                }
+                if (m.least != 0) drop8(m, (uint32_t)row, (uint32_t)(col_of(k) >> 3), v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x1[k][i] = c.stream * x[k].at(i) + v[i];
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x1[k][i] = c.stream * x[k].at(i);
+        }
+        if (a.x1.p) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) store8<SBF>(a.x1.p, row * a.x1.ld + col_of(k), c.cols - col_of(k), x1[k]);
+        }
+        if (a.z.p) {
+            float t[1] = {0.0f};
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) t[0] += col_of(k) + i < c.cols ? x1[k][i] * x1[k][i] : 0.0f;
+            lane_sums<LANES>(t, sh, turn);
+            const float r1 = norm_factor(t[0], c);
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                float z[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) z[i] = x1[k][i] * r1 * wp[k][i];
+                store8<BBF>(a.z.p, row * a.z.ld + col_of(k), c.cols - col_of(k), z);
+            }
+        }
+    }
+}
+
+// Two rounds of sums a row: x1^2, dn x1 and y^2 together, then what goes by d.
+// A workgroup's sums over its rows go to a part of their own.
+template <bool SBF, bool BBF, int LANES, int K>
+__global__ __launch_bounds__(threads_of(LANES)) void k_join_gradient(Backward a)
+{
+    constexpr int kGroups = threads_of(LANES) / LANES;
+    __shared__ Shared<LANES> sh;
+    __shared__ __attribute__((aligned(16))) float sums[kGroups > 1 ? kGroups : 1][kGroups > 1 ? LANES * 8 * K : 1];
+    const Common &c = a.c;
+    const Mask m = mask_of(c.drop);
+    const int64_t col0 = (threadIdx.x % LANES) * 8;
+    auto col_of = [&](int k) { return col0 + (int64_t)k * LANES * 8; };
+    float wb[K][8], wp[K][8], swb[K][8] = {}, swp[K][8] = {};
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        weights8(c.wb, col_of(k), c.cols - col_of(k), wb[k]);
+        weights8(c.wp, col_of(k), c.cols - col_of(k), wp[k]);
+    }
+    int turn = 0;
+    for (int64_t row = first_row<LANES>(); row < c.rows; row += (int64_t)gridDim.x * kGroups) {
+        Stream8<SBF, BBF> q[K];
+        Eight<BBF> y[K], g[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int64_t col = col_of(k), n = c.cols - col;
+            q[k].load(a, row, col, n);
+            y[k] = load8<BBF>(a.y.p, row * a.y.ld + col, a.y.p ? n : 0);
+            g[k] = load8<BBF>(a.gate.p, row * a.gate.ld + col, c.gate_kind == kElementGate ? n : 0);
+        }
+        float s[3] = {};
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                s[0] += q[k].x1.at(i) * q[k].x1.at(i);
+                s[1] += q[k].dz.at(i) * wp[k][i] * q[k].x1.at(i);
+                s[2] += y[k].at(i) * y[k].at(i);
+            }
+        lane_sums<LANES>(s, sh, turn);
+        const float r1 = a.dz.p ? norm_factor(s[0], c) : 0.0f, m1 = r1 * s[1] * c.inv_cols;
+        float d[K][8];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            float o[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                d[k][i] = q[k].d(i, wp[k][i], r1, m1);
+                swp[k][i] += q[k].dz.at(i) * (q[k].x1.at(i) * r1);
+                o[i] = c.stream * d[k][i];
+            }
+            if (a.dx.p) store8<SBF>(a.dx.p, row * a.dx.ld + col_of(k), c.cols - col_of(k), o);
+        }
+        if (!a.y.p) continue;
+        const float r = c.post_norm ? norm_factor(s[2], c) : 1.0f;
+        const float gate = c.gate_kind == kRowGate ? load1<BBF>(a.gate.p, row * a.gate.ld) : 1.0f;
+        const float row_gate = c.gate_kind == kRowGate ? gate_value(gate, c.sigmoid) : 1.0f;
+        float t[2] = {};                                    // of dn' yn; of dv u, the gradient of a row's gate
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            float dv[8], dg[8];
+            branch8(c, m, row, col_of(k), d[k], dv);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float yn = y[k].at(i) * r, gi = c.gate_kind == kElementGate ? gate_value(g[k].at(i), c.sigmoid) : row_gate;
+                const float u = yn * wb[k][i], du = dv[i] * gi;
+                t[1] += dv[i] * u;
+                dg[i] = dv[i] * u;
+                swb[k][i] += du * yn;
+                d[k][i] = du * wb[k][i];                    // dn' from here on
+                t[0] += d[k][i] * yn;
+            }
+            if (a.dgate.p && c.gate_kind == kElementGate) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) dg[i] *= gate_slope(g[k].at(i), c.sigmoid);
+                store8<BBF>(a.dgate.p, row * a.dgate.ld + col_of(k), c.cols - col_of(k), dg);
+            }
+        }
+        if (c.post_norm || c.gate_kind == kRowGate) lane_sums<LANES>(t, sh, turn);
+        const float mean = c.post_norm ? t[0] * c.inv_cols : 0.0f;
+        if (a.dy.p) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                float o[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[i] = r * (d[k][i] - y[k].at(i) * r * mean);
+                store8<BBF>(a.dy.p, row * a.dy.ld + col_of(k), c.cols - col_of(k), o);
+            }
+        }
+        if (threadIdx.x % LANES == 0 && a.dgate.p && c.gate_kind == kRowGate) {
+            const float dg = t[1] * gate_slope(gate, c.sigmoid);
+            if constexpr (BBF) static_cast<uint16_t *>(a.dgate.p)[row * a.dgate.ld] = (uint16_t)bf16_pair(dg, 0.0f);
+            else static_cast<float *>(a.dgate.p)[row * a.dgate.ld] = dg;
+        }
+    }
+    float *part = a.parts + (int64_t)blockIdx.x * 2 * c.cols;
+    auto hand_on = [&](float (&v)[K][8], float *to) {
+        if constexpr (kGroups > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < K; ++k) store8<false>(&sums[threadIdx.x / LANES][0], (int)col_of(k), 8, v[k]);
+            __syncthreads();
+            for (int col = threadIdx.x; col < LANES * 8 * K && col < c.cols; col += threads_of(LANES)) {
+                float t = sums[0][col];
+#pragma unroll
+                for (int i = 1; i < kGroups; ++i) t += sums[i][col];
+                to[col] = t;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < K; ++k) store8<false>(to, col_of(k), c.cols - col_of(k), v[k]);
+        }
+    };
+    if (a.want_wb) hand_on(swb, part);
+    if (a.want_wp) hand_on(swp, part + c.cols);
+}
+
 // ---------------------------------------------------------------------------
 // Rows of any length: a workgroup goes through a row several times.
 // ---------------------------------------------------------------------------
@@ -162,32 +446,6 @@ __global__ __launch_bounds__(kLong) void k_join_long(Forward a)
             store8<BBF>(a.z.p, row * a.z.ld + col, n, z);
         }
     }
-}
-
-// d of eight columns: d_x1 and the norm before the next block; dn and xn of that.
-template <bool SBF, bool BBF>
-struct Stream8 {
-    Eight<SBF> x1, dx1;
-    Eight<BBF> dz;
-
-    __device__ __forceinline__ void load(const Backward &a, int64_t row, int64_t col, int64_t n)
-    {
-        x1 = load8<SBF>(a.x1.p, row * a.x1.ld + col, n);
-        dx1 = load8<SBF>(a.dx1.p, row * a.dx1.ld + col, a.dx1.p ? n : 0);
-        dz = load8<BBF>(a.dz.p, row * a.dz.ld + col, a.dz.p ? n : 0);
-    }
-    __device__ __forceinline__ float d(int i, float wp, float r1, float m1) const
-    {
-        return dx1.at(i) + r1 * (dz.at(i) * wp - x1.at(i) * r1 * m1);
-    }
-};
-
-// dv of eight columns from their d.
-__device__ __forceinline__ void branch8(const Common &c, const Mask &m, int64_t row, int64_t col, const float (&d)[8], float (&dv)[8])
-{
-#pragma unroll
-    for (int i = 0; i < 8; ++i) dv[i] = c.branch * d[i];
-    if (m.least != 0) drop8(m, (uint32_t)row, (uint32_t)(col >> 3), dv);
 }
 
 // What the columns' pass needs of each row, and the gradient of its gate.
@@ -310,14 +568,29 @@ __global__ __launch_bounds__(kTile) void k_join_long_columns(Backward a)
     if (a.want_wp) store8<false>(part, c.cols + col, n, swp);
 }
 
-// Sums of the parts: dw_branch and dw_pre.
+// Sums of the parts: dw_branch and dw_pre.  A workgroup has 32 columns, eight
+// threads each, every one an eighth of the parts.
+constexpr int kSumCols = 32;
+
 __global__ __launch_bounds__(kTile) void k_join_sums(const float *__restrict__ parts, int32_t n_parts, int64_t cols, float *dwb, float *dwp)
 {
-    const int64_t col = (int64_t)blockIdx.x * kTile + threadIdx.x;
+    constexpr int kSlices = kTile / kSumCols;
+    __shared__ float sh[kSlices][kSumCols];
     float *out = blockIdx.y ? dwp : dwb;
-    if (col >= cols || !out) return;
+    if (!out) return;
+    const int slice = threadIdx.x / kSumCols;
+    const int64_t col = (int64_t)blockIdx.x * kSumCols + threadIdx.x % kSumCols;
     float s = 0.0f;
-    for (int32_t i = 0; i < n_parts; ++i) s += parts[((int64_t)i * 2 + blockIdx.y) * cols + col];
+    if (col < cols) {
+        const float *at = parts + (int64_t)blockIdx.y * cols + col;
+#pragma unroll 8
+        for (int32_t i = slice; i < n_parts; i += kSlices) s += at[(int64_t)i * 2 * cols];
+    }
+    sh[slice][threadIdx.x % kSumCols] = s;
+    __syncthreads();
+    if (slice != 0 || col >= cols) return;
+#pragma unroll
+    for (int i = 1; i < kSlices; ++i) s += sh[i][threadIdx.x];
     out[col] = s;
 }
 
@@ -359,17 +632,45 @@ void each_row_span(Common &c, F &&f)
     c.row0 = 0;
 }
 
-constexpr int32_t kMostParts = 256;
-
-int32_t parts_of(int64_t rows) { return (int32_t)(rows < kMostParts ? rows : kMostParts); }
-
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// The longest rows that registers hold, and workgroups of a compute unit.
+constexpr int64_t kLongestForward = 16384, kLongestBackward = 8192;
+constexpr int32_t kForwardGroups = 8, kBackwardGroups = 4;
+
+// go<LANES, K>() for rows of `cols` columns.
+template <class F>
+void by_length(int64_t cols, F &&go)
+{
+    if (cols <= 128) go.template operator()<16, 1>();
+    else if (cols <= 512) go.template operator()<64, 1>();
+    else if (cols <= 1024) go.template operator()<64, 2>();
+    else if (cols <= 2048) go.template operator()<256, 1>();
+    else if (cols <= 4096) go.template operator()<256, 2>();
+    else go.template operator()<512, 2>();                  // (1,024 threads of 8 columns spill in the gradient)
+}
+
+int rows_at_once(int64_t cols) { return cols <= 128 ? 16 : cols <= 1024 ? 4 : 1; }
+
+// Workgroups of the gradient, each with a part of its own: as many as run at once.
+int32_t gradient_parts(const hwsel_join_t &j)
+{
+    const int64_t most = (int64_t)compute_units() * (j.cols <= 4096 ? kBackwardGroups : 1), need = (j.rows + rows_at_once(j.cols) - 1) / rows_at_once(j.cols);
+    return (int32_t)(need < most ? need : most);
+}
+
+// Of rows that are too long, the columns' pass has its rows in this many parts.
+constexpr int32_t kLongParts = 256;
+
+int32_t long_rows_each(int64_t rows) { return (int32_t)((rows + kLongParts - 1) / kLongParts); }
 
 }  // namespace
 
 size_t join_gradient_workspace_bytes(const hwsel_join_t &j)
 {
-    return up256((size_t)j.rows * 16) + (size_t)parts_of(j.rows) * 2 * (size_t)j.cols * 4;
+    if (j.cols <= kLongestBackward) return (size_t)gradient_parts(j) * 2 * (size_t)j.cols * 4;
+    const int64_t each = long_rows_each(j.rows), parts = (j.rows + each - 1) / each;
+    return up256((size_t)j.rows * 16) + (size_t)parts * 2 * (size_t)j.cols * 4;
 }
 
 hipError_t launch_block_join(const hwsel_join_t &j, const hwsel_matrix_t &x, const hwsel_matrix_t &y, const hwsel_matrix_t &gate,
@@ -377,7 +678,17 @@ hipError_t launch_block_join(const hwsel_join_t &j, const hwsel_matrix_t &x, con
 {
     Forward a{common_of(j, y.data != nullptr), in_of(x), in_of(y), in_of(gate), out_of(x1), out_of(z)};
     by_types(sbf, bbf, [&]<bool SBF, bool BBF>() {
-        each_row_span(a.c, [&](unsigned n) { hipLaunchKernelGGL((k_join_long<SBF, BBF>), dim3(n), dim3(kLong), 0, s, a); });
+        if (j.cols > kLongestForward) {
+            each_row_span(a.c, [&](unsigned n) { hipLaunchKernelGGL((k_join_long<SBF, BBF>), dim3(n), dim3(kLong), 0, s, a); });
+            return;
+        }
+        auto go = [&]<int LANES, int K>() {
+            constexpr int kThreads = threads_of(LANES), kRows = kThreads / LANES;
+            const int64_t need = (j.rows + kRows - 1) / kRows, most = (int64_t)compute_units() * kForwardGroups;
+            hipLaunchKernelGGL((k_join<SBF, BBF, LANES, K>), dim3((unsigned)(need < most ? need : most)), dim3(kThreads), 0, s, a);
+        };
+        if (j.cols > 8192) go.template operator()<1024, 2>();
+        else by_length(j.cols, go);
     });
     return hipGetLastError();
 }
@@ -388,17 +699,27 @@ hipError_t launch_block_join_gradient(const hwsel_join_t &j, const hwsel_matrix_
                                       float *dwp, void *ws, bool sbf, bool bbf, hipStream_t s)
 {
     Backward a{common_of(j, y.data != nullptr), in_of(x1), in_of(y), in_of(gate), in_of(dx1), in_of(dz), out_of(dx), out_of(dy), out_of(dgate),
-               static_cast<float *>(ws), reinterpret_cast<float *>(static_cast<char *>(ws) + up256((size_t)j.rows * 16)), 0, 0,
-               dwb != nullptr, dwp != nullptr};
-    a.rows_each = (int32_t)((j.rows + kMostParts - 1) / kMostParts);
-    a.n_parts = (int32_t)((j.rows + a.rows_each - 1) / a.rows_each);
-    const unsigned strips = (unsigned)((j.cols + kTile * 8 - 1) / (kTile * 8));
-    by_types(sbf, bbf, [&]<bool SBF, bool BBF>() {
-        each_row_span(a.c, [&](unsigned n) { hipLaunchKernelGGL((k_join_long_stats<SBF, BBF>), dim3(n), dim3(kLong), 0, s, a); });
-        hipLaunchKernelGGL((k_join_long_columns<SBF, BBF>), dim3(strips, (unsigned)a.n_parts), dim3(kTile), 0, s, a);
-    });
+               nullptr, static_cast<float *>(ws), 0, 0, dwb != nullptr, dwp != nullptr};
+    if (j.cols <= kLongestBackward) {
+        a.n_parts = gradient_parts(j);
+        by_types(sbf, bbf, [&]<bool SBF, bool BBF>() {
+            by_length(j.cols, [&]<int LANES, int K>() {
+                hipLaunchKernelGGL((k_join_gradient<SBF, BBF, LANES, K>), dim3((unsigned)a.n_parts), dim3(threads_of(LANES)), 0, s, a);
+            });
+        });
+    } else {
+        a.stats = static_cast<float *>(ws);
+        a.parts = reinterpret_cast<float *>(static_cast<char *>(ws) + up256((size_t)j.rows * 16));
+        a.rows_each = long_rows_each(j.rows);
+        a.n_parts = (int32_t)((j.rows + a.rows_each - 1) / a.rows_each);
+        const unsigned strips = (unsigned)((j.cols + kTile * 8 - 1) / (kTile * 8));
+        by_types(sbf, bbf, [&]<bool SBF, bool BBF>() {
+            each_row_span(a.c, [&](unsigned n) { hipLaunchKernelGGL((k_join_long_stats<SBF, BBF>), dim3(n), dim3(kLong), 0, s, a); });
+            hipLaunchKernelGGL((k_join_long_columns<SBF, BBF>), dim3(strips, (unsigned)a.n_parts), dim3(kTile), 0, s, a);
+        });
+    }
     if (dwb || dwp)
-        hipLaunchKernelGGL(k_join_sums, dim3((unsigned)((j.cols + kTile - 1) / kTile), 2), dim3(kTile), 0, s, a.parts, a.n_parts, j.cols, dwb, dwp);
+        hipLaunchKernelGGL(k_join_sums, dim3((unsigned)((j.cols + kSumCols - 1) / kSumCols), 2), dim3(kTile), 0, s, a.parts, a.n_parts, j.cols, dwb, dwp);
     return hipGetLastError();
 }
 
