@@ -2,7 +2,7 @@
 // their gradient with respect to the scores.
 //   t = (s - best) / T;  Z = sum exp t;  log p = t - log Z;  H = log Z - sum(exp(t) t) / Z
 // Scores are read once, with the running best score and the sums that go by it.
-#include "internal.hpp"
+#include "topk.hpp"
 
 namespace hwsel {
 namespace {
@@ -73,19 +73,45 @@ __device__ __forceinline__ void take(Mass &m, const float (&v)[N], float rate)
     }
 }
 
-__device__ __forceinline__ Mass lane_of(const Mass &m, int l)
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ float dpp_max(float v)
 {
-    return {__shfl(m.best, l), __shfl(m.equal, l), __shfl(m.less, l), __shfl(m.weighted, l)};
+    return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(kNone), __float_as_int(v), CTRL, ROW_MASK, 0xf, false)));
 }
 
+__device__ __forceinline__ float wave_max(float v)
+{
+    v = dpp_max<0x111, 0xf>(v);
+    v = dpp_max<0x112, 0xf>(v);
+    v = dpp_max<0x114, 0xf>(v);
+    v = dpp_max<0x118, 0xf>(v);
+    v = dpp_max<0x142, 0xa>(v);
+    v = dpp_max<0x143, 0xc>(v);
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
+// The lanes' candidates together: first the best score, then sums that go by it.
 __device__ __forceinline__ Mass wave_mass(Mass m, float rate)
 {
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) {
-        const Mass o = {__shfl_xor(m.best, d), __shfl_xor(m.equal, d), __shfl_xor(m.less, d), __shfl_xor(m.weighted, d)};
-        m = joined(m, o, rate);
-    }
-    return lane_of(m, 0);
+    const float top = wave_max(m.best);
+    if (m.best < top) m = lowered(m, top, rate);
+    float v[3] = {m.equal, m.less, m.weighted};
+    group_totals<64>(v);
+    auto last = [](float x) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63)); };
+    return {top, last(v[0]), last(v[1]), last(v[2])};
+}
+
+constexpr Mass kNothing = {kNone, 0.0f, 0.0f, 0.0f};
+
+// A workgroup's candidates together, in every thread (part: not in use).
+template <int NT>
+__device__ __forceinline__ Mass block_mass(Mass m, float rate, Mass *part)
+{
+    const int lane = threadIdx.x & 63;
+    m = wave_mass(m, rate);
+    if (lane == 0) part[threadIdx.x >> 6] = m;
+    __syncthreads();
+    return wave_mass(lane < NT / 64 ? part[lane] : kNothing, rate);
 }
 
 // What log probabilities are made from.
@@ -109,27 +135,7 @@ __device__ __forceinline__ float log_probability(const Problem &q, const Norm &z
     return (s == z.best ? 0.0f : (s - z.best) / q.T) - z.log_mass;
 }
 
-__device__ __forceinline__ uint64_t key_of(float s, int32_t j)   // 0: takes no part
-{
-    return s > kNone ? ((uint64_t)order_key(s + 0.0f) << 32) | (0xffffffffu - (uint32_t)j) : 0ull;
-}
-
 constexpr int kThreads = 256;
-
-template <int NT>
-__device__ __forceinline__ uint64_t block_max(uint64_t v, uint64_t *sh)
-{
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) {
-        const uint64_t o = __shfl_xor((unsigned long long)v, d);
-        v = o > v ? o : v;
-    }
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
-    __syncthreads();
-    for (int w = 0; w < NT / 64; ++w) v = sh[w] > v ? sh[w] : v;
-    return v;
-}
 
 struct LogprobArgs {
     const float *scores;
@@ -142,60 +148,296 @@ struct LogprobArgs {
     float *logp, *entropy, *norm;
     int32_t *top_idx;
     float *top_logp;
-    int32_t p0;
+    int32_t P, p0;
 };
 
-// A workgroup has a problem.
-__global__ __launch_bounds__(kThreads) void k_logprob(LogprobArgs a)
+__device__ __forceinline__ Problem problem_of(const LogprobArgs &a, int32_t p)
 {
-    __shared__ Mass part[kThreads / 64];
-    __shared__ uint64_t sh[kThreads / 64];
-    const int32_t p = a.p0 + (int32_t)blockIdx.x;
-    const Problem q = problem_of(a.scores, a.R, a.seg, p, a.temperature, a.temperature_of);
-    const float rate = kLog2e / q.T;
-    Mass m = {kNone, 0.0f, 0.0f, 0.0f};
-    for (int64_t i = threadIdx.x; i < q.n; i += kThreads) {
-        const float v[1] = {taking_part(q.s[i])};
-        take(m, v, rate);
-    }
-    m = wave_mass(m, rate);
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
-    __syncthreads();
-    m = part[0];
-    for (int w = 1; w < kThreads / 64; ++w) m = joined(m, part[w], rate);
-    int32_t first = -1;
-    auto best_below = [&](uint64_t limit) {
-        uint64_t k = 0;
-        for (int64_t i = threadIdx.x; i < q.n; i += kThreads) {
-            const uint64_t v = key_of(q.s[i], (int32_t)i);
-            k = v < limit && v > k ? v : k;
-        }
-        return block_max<kThreads>(k, sh);
-    };
-    if (q.cold) first = (int32_t)(0xffffffffu - (uint32_t)best_below(~0ull));
-    const Norm z = norm_of(m, q, first);
-    if (threadIdx.x == 0) {
+    return problem_of(a.scores, a.R, a.seg, p, a.temperature, a.temperature_of);
+}
+
+// A thread's first pick with its score, on the way while the scores are read.
+struct Pick {
+    int32_t j;
+    float s;
+};
+
+__device__ __forceinline__ Pick pick_of(const LogprobArgs &a, const Problem &q, int32_t p, int32_t i)
+{
+    Pick k = {-1, 0.0f};
+    if (i < a.n_picks) k.j = a.picks[(int64_t)p * a.n_picks + i];
+    if (k.j >= 0 && k.j < q.n) k.s = q.s[k.j];
+    else k.j = -1;
+    return k;
+}
+
+// What N threads (this one the t-th) write of a problem: its norm, its picks; keys: its best candidates, descending, 0 for none.
+template <int N>
+__device__ __forceinline__ void write_problem(const LogprobArgs &a, const Problem &q, int32_t p, const Norm &z, int t, Pick pick, const uint64_t *keys)
+{
+    if (t == 0) {
         if (a.entropy) a.entropy[p] = z.entropy;
         if (a.norm) {
             a.norm[2 * (int64_t)p] = z.best;
             a.norm[2 * (int64_t)p + 1] = z.log_mass;
         }
     }
-    for (int64_t i = threadIdx.x; i < a.n_picks; i += kThreads) {
-        const int32_t j = a.picks[(int64_t)p * a.n_picks + i];
-        a.logp[(int64_t)p * a.n_picks + i] = j < 0 || j >= q.n ? 0.0f : log_probability(q, z, j, q.s[j]);
+    for (uint32_t i = t; i < (uint32_t)a.n_picks; i += N) {
+        if (i >= N) pick = pick_of(a, q, p, (int32_t)i);
+        a.logp[(int64_t)p * a.n_picks + i] = pick.j < 0 ? 0.0f : log_probability(q, z, pick.j, pick.s);
     }
-    uint64_t limit = ~0ull;
-    for (int32_t r = 0; r < a.top; ++r) {
-        const uint64_t k = limit ? best_below(limit) : 0ull;
-        limit = k;
-        if (threadIdx.x == 0) {
-            const int32_t j = (int32_t)(0xffffffffu - (uint32_t)k);
-            const float lp = k ? log_probability(q, z, j, q.s[j]) : kNone;
-            a.top_idx[(int64_t)p * a.top + r] = lp > kNone ? j : -1;
-            a.top_logp[(int64_t)p * a.top + r] = lp;
+    for (int32_t r = t; r < a.top; r += N) {
+        const uint64_t k = keys[r];
+        const uint32_t b = (uint32_t)(k >> 32);
+        const int32_t j = (int32_t)(0xffffffffu - (uint32_t)k);
+        const float s = b & 0x80000000u ? __uint_as_float(b ^ 0x80000000u) : __uint_as_float(~b);   // (NaN for key 0)
+        const float lp = log_probability(q, z, j, s);
+        a.top_idx[(int64_t)p * a.top + r] = lp > kNone ? j : -1;
+        a.top_logp[(int64_t)p * a.top + r] = lp;
+    }
+}
+
+// The scores of a thread's rows of a tile, from their ordered bits.
+template <int NT, int N>
+__device__ __forceinline__ void take_tile(Mass &m, const uint32_t (&bits)[N], uint32_t t0, int32_t n, float rate)
+{
+    float v[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const uint32_t b = bits[i];
+        const float s = __uint_as_float(b ^ (~(uint32_t)((int32_t)b >> 31) | 0x80000000u));
+        v[i] = t0 + threadIdx.x + i * NT < (uint32_t)n ? taking_part(s) : kNone;
+    }
+    take(m, v, rate);
+}
+
+typedef float f32x4u_t __attribute__((ext_vector_type(4), aligned(4)));   // four scores from any segment's start
+
+// n scores by a workgroup, 16 a thread and step.
+template <int NT>
+__device__ __forceinline__ Mass take_all(const float *s, int32_t n, float rate)
+{
+    Mass m = kNothing;
+    constexpr int kStep = 16 * NT;
+    int32_t at = 0;
+    for (; at <= n - kStep; at += kStep) {
+        f32x4u_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const f32x4u_t *>(s + at + (i * NT + (int)threadIdx.x) * 4);
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = taking_part(w[i >> 2][i & 3]);
+        take(m, v, rate);
+    }
+    // the rest: at most 16 a thread
+    if (at < n) {
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int32_t j = at + i * NT + (int)threadIdx.x;
+            v[i] = j < n ? taking_part(s[j]) : kNone;
+        }
+        take(m, v, rate);
+    }
+    return m;
+}
+
+template <int NT>
+struct Lds {
+    TopkLds<NT> topk;
+    uint64_t keys[64];
+    Mass part[NT / 64];
+    int32_t first;
+};
+
+// The sums and best candidates of n scores by a workgroup; first: of a cold problem its best candidate (else -1).
+template <int NT, int TILE, bool TOP>
+__device__ __forceinline__ Mass block_scores(const float *s, int32_t n, int32_t top, bool cold, float rate, Lds<NT> &lds, int32_t &first)
+{
+    first = -1;
+    Mass m = kNothing;
+    if constexpr (TOP) {
+        topk_tiles<NT, TILE>(
+            s, n, top, lds.topk, [&](uint32_t t0, const auto &bits) { take_tile<NT>(m, bits, t0, n, rate); },
+            [&](int32_t j, uint64_t key) { lds.keys[j] = key; });
+        m = block_mass<NT>(m, rate, lds.part);              // (its barrier: the keys are there)
+        if (cold) first = (int32_t)(0xffffffffu - (uint32_t)lds.keys[0]);
+    } else {
+        m = block_mass<NT>(take_all<NT>(s, n, rate), rate, lds.part);
+        if (cold) {
+            if (threadIdx.x == 0) lds.first = 0x7fffffff;
+            __syncthreads();
+            for (int32_t j = threadIdx.x; j < n; j += NT)
+                if (s[j] == m.best) {
+                    atomicMin(&lds.first, j);
+                    break;
+                }
+            __syncthreads();
+            first = lds.first;
         }
     }
+    return m;
+}
+
+// A workgroup has a problem.
+template <int NT, int TILE, bool TOP>
+__device__ __forceinline__ void block_problem(const LogprobArgs &a, int32_t p, Lds<NT> &lds)
+{
+    const Problem q = problem_of(a, p);
+    const Pick pick = pick_of(a, q, p, threadIdx.x);
+    const float rate = kLog2e / q.T;
+    int32_t first;
+    const Mass m = block_scores<NT, TILE, TOP>(q.s, q.n, a.top, q.cold, rate, lds, first);
+    write_problem<NT>(a, q, p, norm_of(m, q, first), threadIdx.x, pick, lds.keys);
+}
+
+template <int NT, bool TOP>
+__global__ __launch_bounds__(NT) void k_logprob(LogprobArgs a)
+{
+    __shared__ Lds<NT> lds;
+    block_problem<NT, kTile, TOP>(a, a.p0 + (int32_t)blockIdx.x, lds);
+}
+
+// A wave has a problem of up to 64 EACH candidates, its scores in registers;
+// longer ones follow, by the whole workgroup.
+template <int EACH, bool TOP>
+__global__ __launch_bounds__(kThreads) void k_logprob_waves(LogprobArgs a)
+{
+    constexpr int kWaves = kThreads / 64;
+    __shared__ Lds<kThreads> lds;
+    __shared__ uint64_t keys[kWaves][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int32_t p0 = a.p0 + (int32_t)blockIdx.x * kWaves, p = p0 + wave;
+    if (p < a.P) {
+        const Problem q = problem_of(a, p);
+        if (q.n <= 64 * EACH) {
+            const Pick pick = pick_of(a, q, p, lane);
+            const float rate = kLog2e / q.T;
+            float v[EACH];
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) v[e] = lane + 64 * e < q.n ? taking_part(q.s[lane + 64 * e]) : kNone;
+            Mass m = kNothing;
+            take(m, v, rate);
+            m = wave_mass(m, rate);
+            int32_t first = -1;
+            const int32_t rounds = TOP ? a.top : q.cold ? 1 : 0;
+            if (rounds > 0) {
+                // the best that is left, round by round: its bits (0: none), the lowest index that has them
+                uint32_t bits[EACH];
+#pragma unroll
+                for (int e = 0; e < EACH; ++e) bits[e] = v[e] > kNone ? order_key(v[e] + 0.0f) : 0u;
+                uint64_t mine = 0;
+                for (int32_t r = 0; r < rounds; ++r) {
+                    uint32_t b = 0, at = 0;
+#pragma unroll
+                    for (int e = EACH - 1; e >= 0; --e) {
+                        at = bits[e] >= b ? (uint32_t)(lane + 64 * e) : at;
+                        b = bits[e] >= b ? bits[e] : b;
+                    }
+                    const uint32_t most = wave_max_u32(b);
+                    if (most == 0) break;
+                    const uint32_t low = wave_max_u32(b == most ? 0xffffffffu - at : 0u);
+                    if (lane == r) mine = ((uint64_t)most << 32) | low;
+                    const uint32_t j = 0xffffffffu - low;
+                    if (r == 0) first = (int32_t)j;
+#pragma unroll
+                    for (int e = 0; e < EACH; ++e) bits[e] = j == (uint32_t)(lane + 64 * e) ? 0u : bits[e];
+                }
+                if constexpr (TOP) keys[wave][lane] = mine;  // (read by its own wave alone)
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+            __builtin_amdgcn_wave_barrier();
+            write_problem<64>(a, q, p, norm_of(m, q, q.cold ? first : -1), lane, pick, keys[wave]);
+        }
+    }
+    for (int32_t i = 0; i < kWaves && p0 + i < a.P; ++i) {
+        if (problem_of(a, p0 + i).n <= 64 * EACH) continue;  // (one answer for the workgroup)
+        block_problem<kThreads, 2048, TOP>(a, p0 + i, lds);
+        __syncthreads();
+    }
+}
+
+// Few long problems: each goes in parts to workgroups of its own, whose sums and
+// best candidates one workgroup joins.
+constexpr int kWide = 1024, kMostParts = 64;
+
+struct Part {
+    Mass m;
+    int32_t first;
+};
+
+struct Parts {
+    Part *part;                                             // [P][n]
+    uint64_t *keys;                                         // [P][n][top]
+    int32_t n;
+};
+
+template <bool TOP>
+__global__ __launch_bounds__(kWide) void k_logprob_parts(LogprobArgs a, Parts to)
+{
+    __shared__ Lds<kWide> lds;
+    const int32_t p = blockIdx.y, g = blockIdx.x;
+    const Problem q = problem_of(a, p);
+    const int32_t each = (q.n + to.n - 1) / to.n, from = g * (int64_t)each < q.n ? g * each : q.n, n = q.n - from < each ? q.n - from : each;
+    int32_t first;
+    const Mass m = block_scores<kWide, kTile, TOP>(q.s + from, n, a.top, q.cold, kLog2e / q.T, lds, first);
+    const int64_t at = (int64_t)p * to.n + g;
+    if (threadIdx.x == 0) to.part[at] = {m, first + from};
+    if constexpr (TOP)
+        for (int32_t r = threadIdx.x; r < a.top; r += kWide) to.keys[at * a.top + r] = lds.keys[r] ? lds.keys[r] - (uint32_t)from : 0ull;
+}
+
+template <bool TOP>
+__global__ __launch_bounds__(kThreads) void k_logprob_join(LogprobArgs a, Parts from)
+{
+    __shared__ uint64_t list[kMostParts * 64], keys[64];
+    __shared__ uint64_t floor_;
+    __shared__ int32_t n_list;
+    const int32_t p = blockIdx.x;
+    const int lane = threadIdx.x & 63;
+    const Problem q = problem_of(a, p);
+    const Pick pick = pick_of(a, q, p, threadIdx.x);
+    const Part mine = lane < from.n ? from.part[(int64_t)p * from.n + lane] : Part{kNothing, -1};
+    const Mass m = wave_mass(mine.m, kLog2e / q.T);
+    // parts are in the candidates' order: the first that has the best score
+    const uint64_t has = __ballot(lane < from.n && mine.m.best == m.best);
+    const int32_t first = __builtin_amdgcn_readlane(mine.first, has ? __builtin_ctzll(has) : 0);
+    if constexpr (TOP) {
+        const uint64_t *k = from.keys + (int64_t)p * from.n * a.top;
+        const int32_t top = a.top;
+        // Keys that the best `top` are not below: the parts' last, and the r-th largest of the parts' j-th, r j >= top.
+        if (threadIdx.x < 64) {
+            const int32_t half = from.n > 1 ? from.n / 2 : 1, j = (top + half - 1) / half, r = (top + j - 1) / j;
+            const uint64_t own = lane < from.n ? k[(int64_t)lane * top + j - 1] : 0ull, last = lane < from.n ? k[(int64_t)lane * top + top - 1] : 0ull;
+            int32_t above = 0;
+            for (int32_t l = 0; l < from.n; ++l) {
+                const uint64_t o = lane_value(own, l);
+                above += o > own || (o == own && l < lane);
+            }
+            const uint64_t bound = lane_value(own, __builtin_ctzll(__ballot(lane < from.n && above == r - 1))), most = wave_max_key(last);
+            if (lane == 0) {
+                floor_ = bound > most ? bound : most;
+                n_list = 0;
+            }
+            if (lane < top) keys[lane] = 0;
+        }
+        __syncthreads();
+        for (int32_t i = threadIdx.x; i < from.n * top; i += kThreads) {
+            const uint64_t v = k[i];
+            if (v != 0 && v >= floor_) list[atomicAdd(&n_list, 1)] = v;
+        }
+        __syncthreads();
+        const int32_t n = n_list;
+        for (int32_t i = threadIdx.x; i < n; i += kThreads) {
+            const uint64_t v = list[i];
+            int32_t rank = 0;
+#pragma unroll 8
+            for (int32_t e = 0; e < n; ++e) rank += list[e] > v;
+            if (rank < top) keys[rank] = v;
+        }
+        __syncthreads();
+    }
+    write_problem<kThreads>(a, q, p, norm_of(m, q, first), threadIdx.x, pick, keys);
 }
 
 struct GradientArgs {
@@ -287,17 +529,56 @@ __global__ __launch_bounds__(kThreads) void k_logprob_gradient(GradientArgs a)
 
 }  // namespace
 
-size_t logprob_workspace_bytes(int64_t, int32_t, int32_t) { return 0; }
+namespace {
+
+// Problems' lengths are not known here; their mean is.
+int32_t parts_of(int64_t R, int32_t P)
+{
+    const int64_t mean = R / P, n_cu = compute_units();
+    if (2 * (int64_t)P > n_cu || mean < 4 * kTile) return 1;
+    const int64_t by_units = 2 * n_cu / P, by_length = mean / kTile, n = by_units < by_length ? by_units : by_length;
+    return (int32_t)(n < kMostParts ? n : kMostParts);
+}
+
+size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+}  // namespace
+
+size_t logprob_workspace_bytes(int64_t R, int32_t P, int32_t top)
+{
+    const int32_t n = parts_of(R, P);
+    return n == 1 ? 0 : up256((size_t)P * n * sizeof(Part)) + (size_t)P * n * top * 8;
+}
 
 hipError_t launch_logprob(const float *scores, int64_t R, const int64_t *seg, int32_t P, float temperature, const float *temperature_of,
                           const int32_t *picks, int32_t n_picks, int32_t top, float *logp, float *entropy, float *norm, int32_t *top_idx,
-                          float *top_logp, void *, hipStream_t s)
+                          float *top_logp, void *ws, hipStream_t s)
 {
-    LogprobArgs a{scores, R, seg, temperature, temperature_of, picks, n_picks, top, logp, entropy, norm, top_idx, top_logp, 0};
-    each_span(P, [&](int32_t p0, int32_t n) {
-        a.p0 = p0;
-        hipLaunchKernelGGL(k_logprob, dim3(n), dim3(kThreads), 0, s, a);
-    });
+    LogprobArgs a{scores, R, seg, temperature, temperature_of, picks, n_picks, top, logp, entropy, norm, top_idx, top_logp, P, 0};
+    const int32_t parts = parts_of(R, P);
+    const int64_t mean = R / P;
+    auto go = [&]<bool TOP>() {
+        if (parts > 1) {
+            const Parts w{static_cast<Part *>(ws), reinterpret_cast<uint64_t *>(static_cast<char *>(ws) + up256((size_t)P * parts * sizeof(Part))), parts};
+            hipLaunchKernelGGL((k_logprob_parts<TOP>), dim3(parts, P), dim3(kWide), 0, s, a, w);
+            hipLaunchKernelGGL((k_logprob_join<TOP>), dim3(P), dim3(kThreads), 0, s, a, w);
+        } else if (mean <= 1024) {
+            each_span(P, [&](int32_t p0, int32_t n) {
+                a.p0 = p0;
+                if (mean <= 128) hipLaunchKernelGGL((k_logprob_waves<4, TOP>), dim3((n + 3) / 4), dim3(kThreads), 0, s, a);
+                else hipLaunchKernelGGL((k_logprob_waves<16, TOP>), dim3((n + 3) / 4), dim3(kThreads), 0, s, a);
+            });
+        } else if (P <= compute_units()) {
+            hipLaunchKernelGGL((k_logprob<1024, TOP>), dim3(P), dim3(1024), 0, s, a);
+        } else {
+            each_span(P, [&](int32_t p0, int32_t n) {
+                a.p0 = p0;
+                hipLaunchKernelGGL((k_logprob<256, TOP>), dim3(n), dim3(256), 0, s, a);
+            });
+        }
+    };
+    if (top > 0) go.template operator()<true>();
+    else go.template operator()<false>();
     return hipGetLastError();
 }
 
