@@ -132,7 +132,8 @@ __device__ __forceinline__ float log_probability(const Problem &q, const Norm &z
 {
     if (!(s > kNone)) return kNone;
     if (q.cold) return j == z.first ? 0.0f : kNone;
-    return (s == z.best ? 0.0f : (s - z.best) / q.T) - z.log_mass;
+    const float t = s == z.best ? 0.0f : (s - z.best) / q.T;
+    return t > kNone ? t - z.log_mass : kNone;              // (NaN: a finite score below +inf at T = inf)
 }
 
 constexpr int kThreads = 256;
@@ -453,77 +454,193 @@ struct GradientArgs {
     float *d_scores;
 };
 
-// A pick that counts: inside the problem, with a probability.
-__device__ __forceinline__ bool counts(const Problem &q, const Norm &z, int32_t j)
+// Waits for a group of THREADS: a wave's own LDS accesses, or a workgroup's.
+template <int THREADS>
+__device__ __forceinline__ void group_barrier()
 {
-    return j >= 0 && j < q.n && log_probability(q, z, j, q.s[j]) > kNone;
+    if constexpr (THREADS > 64) {
+        __syncthreads();
+    } else {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// Picks' gradients in fixed point: sums do not depend on their order.
+template <int PART>
+struct Fixed {
+    unsigned long long acc[PART];
+    unsigned long long total;
+    uint32_t most;
+};
+
+// Candidates [from, to) of a problem by THREADS threads (this one the t-th), PART at a time.
+// The unit is 2^e: the largest |d_logp| is below 2^x, n of them below 2^(62 + e).
+template <int THREADS, int PART, bool PICKS>
+__device__ __forceinline__ void gradient_of(const GradientArgs &a, int32_t p, const Problem &q, int32_t from, int32_t to, int t,
+                                            Fixed<PICKS ? PART : 1> &fx)
+{
+    float *d = a.d_scores + q.at;
+    if (q.cold) {
+        for (int32_t i = from + t; i < to; i += THREADS) d[i] = 0.0f;
+        return;
+    }
+    const Norm z = {a.norm[2 * (int64_t)p], a.norm[2 * (int64_t)p + 1], a.d_entropy ? a.entropy[p] : 0.0f, -1};
+    const float de = a.d_entropy ? a.d_entropy[p] : 0.0f;
+    const int32_t *picks = a.picks + (int64_t)p * a.n_picks;
+    const float *dl = a.d_logp + (int64_t)p * a.n_picks;
+    // a pick's candidate and gradient; -1 where it does not count: outside, or without a probability
+    auto pick_at = [&](uint32_t i, float &g) {
+        int32_t j = picks[i];
+        g = dl[i];
+        if (j < 0 || j >= q.n || !(log_probability(q, z, j, q.s[j]) > kNone)) j = -1;
+        return j;
+    };
+    float S = 0.0f;
+    int32_t own_j = -1;
+    float own_g = 0.0f;
+    int e = 0;
+    bool fine = true;
+    if constexpr (PICKS) {
+        if (t == 0) {
+            fx.most = 0;
+            fx.total = 0;
+        }
+        for (int32_t i = t; i < PART; i += THREADS) fx.acc[i] = 0;
+        if (t < a.n_picks) own_j = pick_at((uint32_t)t, own_g);
+        group_barrier<THREADS>();
+        uint32_t most = own_j >= 0 ? __float_as_uint(own_g) & 0x7fffffffu : 0u;
+        for (uint32_t i = t + THREADS; i < (uint32_t)a.n_picks; i += THREADS) {
+            float g;
+            const uint32_t b = pick_at(i, g) >= 0 ? __float_as_uint(g) & 0x7fffffffu : 0u;
+            most = b > most ? b : most;
+        }
+        most = wave_max_u32(most);
+        if constexpr (THREADS > 64) {
+            if ((threadIdx.x & 63) == 0) atomicMax(&fx.most, most);
+            group_barrier<THREADS>();
+            most = fx.most;
+        }
+        fine = most < 0x7f800000u;
+        e = (int)(most >> 23) - 126 + (32 - __builtin_clz((uint32_t)a.n_picks)) - 62;
+        S = __uint_as_float(most);                          // (as it is where it is not finite)
+    }
+    auto fixed = [&](float v) { return (unsigned long long)(long long)__builtin_rint(__builtin_ldexp((double)v, -e)); };
+    auto value = [&](unsigned long long v) { return (float)__builtin_ldexp((double)(long long)v, e); };
+    const float rate = kLog2e / q.T, by_T = fminf(1.0f / q.T, 3.4028235e38f);
+    const float log2_mass = z.log_mass * kLog2e;
+    for (int32_t part = from; part < to; part += PART) {
+        const int32_t n = to - part < PART ? to - part : PART;
+        if constexpr (PICKS) {
+            if (fine) {                                     // (uniform)
+                auto add = [&](int32_t j, float g, bool first) {
+                    if (j < 0) return;
+                    const unsigned long long v = fixed(g);
+                    if (first) atomicAdd(&fx.total, v);
+                    if (j >= part && j - part < n) atomicAdd(&fx.acc[j - part], v);
+                };
+                add(own_j, own_g, part == from);
+                for (uint32_t i = t + THREADS; i < (uint32_t)a.n_picks; i += THREADS) {
+                    float g;
+                    const int32_t j = pick_at(i, g);
+                    add(j, g, part == from);
+                }
+            }
+            group_barrier<THREADS>();
+            if (fine) S = value(fx.total);
+        }
+        auto grad = [&](int32_t j, float s) {
+            const float delta = s - z.best, lt = s == z.best ? 0.0f : delta * rate;      // log2 of the weight
+            const float pr = __builtin_amdgcn_exp2f(lt - log2_mass);
+            float own = 0.0f, others = S;
+            if constexpr (PICKS) {
+                const unsigned long long f = fx.acc[j - part];
+                if (f != 0) {
+                    // g (1 - p) without the difference where p is nearly 1
+                    const float g = value(f);
+                    own = -g * expm1f(log_probability(q, z, j, s));
+                    others = S - g;
+                }
+            }
+            const float lp = lt * kLn2 - z.log_mass;
+            const float v = own - pr * others - de * (pr > 0.0f ? pr * (lp + z.entropy) : 0.0f);
+            // (a weight below the normal numbers is 0, and so is the gradient but where it was picked)
+            return s > kNone && lt > kNone ? v * by_T : 0.0f;
+        };
+        if (n == PART) {
+#pragma unroll 4
+            for (int32_t i = t * 4; i < PART; i += THREADS * 4) {
+                const f32x4u_t s = *reinterpret_cast<const f32x4u_t *>(q.s + part + i);
+                f32x4u_t o;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) o[k] = grad(part + i + k, s[k]);
+                *reinterpret_cast<f32x4u_t *>(d + part + i) = o;
+            }
+        } else {
+#pragma unroll 4
+            for (int32_t i = t; i < n; i += THREADS) d[part + i] = grad(part + i, q.s[part + i]);
+        }
+        if constexpr (PICKS)
+            if (part + PART < to) {                         // cleared for the next part
+                group_barrier<THREADS>();
+                for (int32_t i = t; i < PART; i += THREADS) fx.acc[i] = 0;
+                group_barrier<THREADS>();
+            }
+    }
+}
+
+__device__ __forceinline__ Problem problem_of(const GradientArgs &a, int32_t p)
+{
+    return problem_of(a.scores, a.R, a.seg, p, a.temperature, a.temperature_of);
+}
+
+// Rows of no problem: a share of them for each of the launch's threads.
+__device__ __forceinline__ void clear_others(const GradientArgs &a, int64_t thread, int64_t threads)
+{
+    const int64_t before = within(a.seg[0], a.R), behind = within(a.seg[a.P], a.R);
+    for (int64_t i = thread; i < before; i += threads) a.d_scores[i] = 0.0f;
+    for (int64_t i = behind + thread; i < a.R; i += threads) a.d_scores[i] = 0.0f;
 }
 
 constexpr int kPart = 4096;                                 // candidates whose picks are summed at once
 
-// A workgroup has a problem, a part of its candidates at a time: the picks'
-// gradients are added in fixed point in LDS, by a unit of 2^-62 n of the largest,
-// so their order does not matter.
+// gridDim.x workgroups have a problem, a part of its candidates each.
+template <bool PICKS>
 __global__ __launch_bounds__(kThreads) void k_logprob_gradient(GradientArgs a)
 {
-    __shared__ unsigned long long acc[kPart];
-    __shared__ unsigned long long total;
-    __shared__ uint32_t largest;
-    const int32_t p = a.p0 + (int32_t)blockIdx.x;
-    // rows of no problem: this workgroup's share
-    const int64_t before = within(a.seg[0], a.R), behind = within(a.seg[a.P], a.R);
-    for (int64_t i = (int64_t)p * kThreads + threadIdx.x; i < before; i += (int64_t)a.P * kThreads) a.d_scores[i] = 0.0f;
-    for (int64_t i = behind + (int64_t)p * kThreads + threadIdx.x; i < a.R; i += (int64_t)a.P * kThreads) a.d_scores[i] = 0.0f;
+    __shared__ Fixed<PICKS ? kPart : 1> fx;
+    const int32_t p = a.p0 + (int32_t)blockIdx.y;
+    clear_others(a, ((int64_t)p * gridDim.x + blockIdx.x) * kThreads + threadIdx.x, (int64_t)a.P * gridDim.x * kThreads);
+    const Problem q = problem_of(a, p);
+    // whole parts to each, the last ones to the last
+    const int32_t parts = (q.n + kPart - 1) / kPart, each = (parts + (int32_t)gridDim.x - 1) / (int32_t)gridDim.x;
+    const int64_t from = (int64_t)blockIdx.x * each * kPart, to = from + (int64_t)each * kPart;
+    if (from >= q.n) return;
+    gradient_of<kThreads, kPart, PICKS>(a, p, q, (int32_t)from, (int32_t)(to < q.n ? to : q.n), threadIdx.x, fx);
+}
 
-    const Problem q = problem_of(a.scores, a.R, a.seg, p, a.temperature, a.temperature_of);
-    const Norm z = {a.norm[2 * (int64_t)p], a.norm[2 * (int64_t)p + 1], a.entropy ? a.entropy[p] : 0.0f, -1};
-    float *d = a.d_scores + q.at;
-    if (q.cold) {
-        for (int64_t i = threadIdx.x; i < q.n; i += kThreads) d[i] = 0.0f;
-        return;
+// A wave has a problem of up to kSmallPart candidates; longer ones follow, by the whole workgroup.
+constexpr int kSmallPart = 1024;
+
+template <bool PICKS>
+__global__ __launch_bounds__(kThreads) void k_logprob_gradient_waves(GradientArgs a)
+{
+    constexpr int kWaves = kThreads / 64;
+    using Small = Fixed<PICKS ? kSmallPart : 1>;
+    using Large = Fixed<PICKS ? kPart : 1>;
+    __shared__ __attribute__((aligned(16))) char lds[sizeof(Large) > kWaves * sizeof(Small) ? sizeof(Large) : kWaves * sizeof(Small)];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int32_t p0 = a.p0 + (int32_t)blockIdx.x * kWaves, p = p0 + wave;
+    if (p < a.P) {
+        clear_others(a, (int64_t)p * 64 + (threadIdx.x & 63), (int64_t)a.P * 64);
+        const Problem q = problem_of(a, p);
+        if (q.n <= kSmallPart) gradient_of<64, kSmallPart, PICKS>(a, p, q, 0, q.n, threadIdx.x & 63, reinterpret_cast<Small *>(lds)[wave]);
     }
-    const int32_t *picks = a.picks + (int64_t)p * a.n_picks;
-    const float *dl = a.d_logp + (int64_t)p * a.n_picks;
-    if (threadIdx.x == 0) {
-        largest = 0;
-        total = 0;
-    }
-    __syncthreads();
-    for (int64_t i = threadIdx.x; i < a.n_picks; i += kThreads)
-        if (counts(q, z, picks[i])) atomicMax(&largest, __float_as_uint(dl[i]) & 0x7fffffffu);
-    __syncthreads();
-    // unit 2^e: the largest is below 2^x, n of them below 2^(62 + e)
-    const uint32_t most = largest;
-    const bool fine = most < 0x7f800000u;
-    const int bits = 32 - __builtin_clz((uint32_t)a.n_picks | 1u);
-    const int e = (int)(most >> 23) - 126 + bits - 62;
-    auto fixed = [&](float v) { return (unsigned long long)(long long)__builtin_rint(__builtin_ldexp((double)v, -e)); };
-    auto value = [&](unsigned long long v) { return (float)__builtin_ldexp((double)(long long)v, e); };
-    if (fine)
-        for (int64_t i = threadIdx.x; i < a.n_picks; i += kThreads)
-            if (counts(q, z, picks[i])) atomicAdd(&total, fixed(dl[i]));
-    __syncthreads();
-    const float S = fine ? value(total) : __uint_as_float(most);
-    const float de = a.d_entropy ? a.d_entropy[p] : 0.0f;
-    for (int64_t part = 0; part < q.n; part += kPart) {
-        const int32_t n = (int32_t)(q.n - part < kPart ? q.n - part : kPart);
+    for (int32_t i = 0; i < kWaves && p0 + i < a.P; ++i) {
+        const Problem q = problem_of(a, p0 + i);
+        if (q.n <= kSmallPart) continue;                    // (one answer for the workgroup)
         __syncthreads();
-        for (int32_t i = threadIdx.x; i < n; i += kThreads) acc[i] = 0;
-        __syncthreads();
-        if (fine)
-            for (int64_t i = threadIdx.x; i < a.n_picks; i += kThreads) {
-                const int64_t j = picks[i] - part;
-                if (j >= 0 && j < n && counts(q, z, picks[i])) atomicAdd(&acc[j], fixed(dl[i]));
-            }
-        __syncthreads();
-        for (int32_t i = threadIdx.x; i < n; i += kThreads) {
-            const float s = q.s[part + i], lp = log_probability(q, z, (int32_t)(part + i), s);
-            const float pr = __builtin_amdgcn_exp2f(lp * kLog2e), g = value(acc[i]);
-            // g (1 - p) without the difference where p is nearly 1
-            const float own = g != 0.0f ? -g * expm1f(lp) : 0.0f;
-            const float v = own - pr * (S - g) - de * (pr > 0.0f ? pr * (lp + z.entropy) : 0.0f);
-            d[part + i] = lp > kNone ? v / q.T : 0.0f;
-        }
+        gradient_of<kThreads, kPart, PICKS>(a, p0 + i, q, 0, q.n, threadIdx.x, *reinterpret_cast<Large *>(lds));
     }
 }
 
@@ -587,10 +704,23 @@ hipError_t launch_logprob_gradient(const float *scores, int64_t R, const int64_t
                                    const float *d_logp, const float *entropy, const float *d_entropy, float *d_scores, hipStream_t s)
 {
     GradientArgs a{scores, R, seg, P, 0, temperature, temperature_of, norm, picks, n_picks, d_logp, entropy, d_entropy, d_scores};
-    each_span(P, [&](int32_t p0, int32_t n) {
-        a.p0 = p0;
-        hipLaunchKernelGGL(k_logprob_gradient, dim3(n), dim3(kThreads), 0, s, a);
-    });
+    const int64_t mean = R / P;
+    auto go = [&]<bool PICKS>() {
+        if (mean <= 1024) {
+            each_span(P, [&](int32_t p0, int32_t n) {
+                a.p0 = p0;
+                hipLaunchKernelGGL((k_logprob_gradient_waves<PICKS>), dim3((n + 3) / 4), dim3(kThreads), 0, s, a);
+            });
+            return;
+        }
+        const int64_t by_length = (2 * mean + kPart - 1) / kPart, each = by_length < 64 ? by_length : 64;
+        for (a.p0 = 0; a.p0 < P; a.p0 += 1 << 15) {         // (a grid's second dimension)
+            const int32_t n = P - a.p0 < 1 << 15 ? P - a.p0 : 1 << 15;
+            hipLaunchKernelGGL((k_logprob_gradient<PICKS>), dim3((unsigned)each, n), dim3(kThreads), 0, s, a);
+        }
+    };
+    if (n_picks > 0) go.template operator()<true>();
+    else go.template operator()<false>();
     return hipGetLastError();
 }
 
