@@ -292,11 +292,11 @@ __device__ __forceinline__ void block_problem(const LogprobArgs &a, int32_t p, L
     write_problem<NT>(a, q, p, norm_of(m, q, first), threadIdx.x, pick, lds.keys);
 }
 
-template <int NT, bool TOP>
+template <int NT, int TILE, bool TOP>
 __global__ __launch_bounds__(NT) void k_logprob(LogprobArgs a)
 {
     __shared__ Lds<NT> lds;
-    block_problem<NT, kTile, TOP>(a, a.p0 + (int32_t)blockIdx.x, lds);
+    block_problem<NT, TILE, TOP>(a, a.p0 + (int32_t)blockIdx.x, lds);
 }
 
 // A wave has a problem of up to 64 EACH candidates, its scores in registers;
@@ -360,7 +360,7 @@ __global__ __launch_bounds__(kThreads) void k_logprob_waves(LogprobArgs a)
 
 // Few long problems: each goes in parts to workgroups of its own, whose sums and
 // best candidates one workgroup joins.
-constexpr int kWide = 1024, kMostParts = 64;
+constexpr int kWide = 512, kWideTile = 4096, kMostKeys = 4096;
 
 struct Part {
     Mass m;
@@ -381,7 +381,7 @@ __global__ __launch_bounds__(kWide) void k_logprob_parts(LogprobArgs a, Parts to
     const Problem q = problem_of(a, p);
     const int32_t each = (q.n + to.n - 1) / to.n, from = g * (int64_t)each < q.n ? g * each : q.n, n = q.n - from < each ? q.n - from : each;
     int32_t first;
-    const Mass m = block_scores<kWide, kTile, TOP>(q.s + from, n, a.top, q.cold, kLog2e / q.T, lds, first);
+    const Mass m = block_scores<kWide, kWideTile, TOP>(q.s + from, n, a.top, q.cold, kLog2e / q.T, lds, first);
     const int64_t at = (int64_t)p * to.n + g;
     if (threadIdx.x == 0) to.part[at] = {m, first + from};
     if constexpr (TOP)
@@ -391,31 +391,45 @@ __global__ __launch_bounds__(kWide) void k_logprob_parts(LogprobArgs a, Parts to
 template <bool TOP>
 __global__ __launch_bounds__(kThreads) void k_logprob_join(LogprobArgs a, Parts from)
 {
-    __shared__ uint64_t list[kMostParts * 64], keys[64];
+    __shared__ uint64_t list[TOP ? kMostKeys : 1], keys[64];
     __shared__ uint64_t floor_;
     __shared__ int32_t n_list;
     const int32_t p = blockIdx.x;
     const int lane = threadIdx.x & 63;
     const Problem q = problem_of(a, p);
     const Pick pick = pick_of(a, q, p, threadIdx.x);
-    const Part mine = lane < from.n ? from.part[(int64_t)p * from.n + lane] : Part{kNothing, -1};
-    const Mass m = wave_mass(mine.m, kLog2e / q.T);
-    // parts are in the candidates' order: the first that has the best score
-    const uint64_t has = __ballot(lane < from.n && mine.m.best == m.best);
-    const int32_t first = __builtin_amdgcn_readlane(mine.first, has ? __builtin_ctzll(has) : 0);
+    // a lane has every 64th part
+    const float rate = kLog2e / q.T;
+    Mass own_mass = kNothing;
+    const Part *part = from.part + (int64_t)p * from.n;
+    for (int32_t g = lane; g < from.n; g += 64) own_mass = joined(own_mass, part[g].m, rate);
+    const Mass m = wave_mass(own_mass, rate);
+    int32_t first = -1;
+    if (q.cold) {                                           // parts are in the candidates' order: the first that has the best score
+        int32_t g = lane;
+        while (g < from.n && part[g].m.best != m.best) g += 64;
+        g = (int32_t)(0xffffffffu - wave_max_u32(0xffffffffu - (uint32_t)g));
+        if (g < from.n) first = part[g].first;
+    }
     if constexpr (TOP) {
         const uint64_t *k = from.keys + (int64_t)p * from.n * a.top;
         const int32_t top = a.top;
-        // Keys that the best `top` are not below: the parts' last, and the r-th largest of the parts' j-th, r j >= top.
+        // Keys that the best `top` are not below: the largest of the parts' last, and the r-th largest of the lanes' j-th (of
+        // a lane's parts the largest j-th), r j >= top.
         if (threadIdx.x < 64) {
-            const int32_t half = from.n > 1 ? from.n / 2 : 1, j = (top + half - 1) / half, r = (top + j - 1) / j;
-            const uint64_t own = lane < from.n ? k[(int64_t)lane * top + j - 1] : 0ull, last = lane < from.n ? k[(int64_t)lane * top + top - 1] : 0ull;
+            const int32_t lanes = from.n < 64 ? from.n : 64, half = lanes > 1 ? lanes / 2 : 1, j = (top + half - 1) / half, r = (top + j - 1) / j;
+            uint64_t own = 0, last = 0;
+            for (int32_t g = lane; g < from.n; g += 64) {
+                const uint64_t o = k[(int64_t)g * top + j - 1], l = k[(int64_t)g * top + top - 1];
+                own = o > own ? o : own;
+                last = l > last ? l : last;
+            }
             int32_t above = 0;
-            for (int32_t l = 0; l < from.n; ++l) {
+            for (int32_t l = 0; l < lanes; ++l) {
                 const uint64_t o = lane_value(own, l);
                 above += o > own || (o == own && l < lane);
             }
-            const uint64_t bound = lane_value(own, __builtin_ctzll(__ballot(lane < from.n && above == r - 1))), most = wave_max_key(last);
+            const uint64_t bound = lane_value(own, __builtin_ctzll(__ballot(lane < lanes && above == r - 1))), most = wave_max_key(last);
             if (lane == 0) {
                 floor_ = bound > most ? bound : most;
                 n_list = 0;
@@ -454,19 +468,21 @@ struct GradientArgs {
     float *d_scores;
 };
 
-// Waits for a group of THREADS: a wave's own LDS accesses, or a workgroup's.
-template <int THREADS>
+// Waits for a group of THREADS: a wave's own accesses of LDS (GLOBAL: and of memory), or a workgroup's.
+template <int THREADS, bool GLOBAL = false>
 __device__ __forceinline__ void group_barrier()
 {
     if constexpr (THREADS > 64) {
-        __syncthreads();
+        if constexpr (GLOBAL) __syncthreads();
+        else lds_barrier();
     } else {
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+        if constexpr (GLOBAL) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+        else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
         __builtin_amdgcn_wave_barrier();
     }
 }
 
-// Picks' gradients in fixed point: sums do not depend on their order.
+// Picks' gradients in fixed point: sums do not depend on their order.  Of acc only the picked candidates' entries are used.
 template <int PART>
 struct Fixed {
     unsigned long long acc[PART];
@@ -474,8 +490,10 @@ struct Fixed {
     uint32_t most;
 };
 
-// Candidates [from, to) of a problem by THREADS threads (this one the t-th), PART at a time.
-// The unit is 2^e: the largest |d_logp| is below 2^x, n of them below 2^(62 + e).
+// Candidates [from, to) of a problem by THREADS threads (this one the t-th), PART at a time: all of them as
+// if none were picked, then the picked ones again by their picks' threads (each of several picks of one
+// candidate stores the same).  The unit of fixed point is 2^e: the largest |d_logp| is below 2^x, n of them
+// below 2^(62 + e).
 template <int THREADS, int PART, bool PICKS>
 __device__ __forceinline__ void gradient_of(const GradientArgs &a, int32_t p, const Problem &q, int32_t from, int32_t to, int t,
                                             Fixed<PICKS ? PART : 1> &fx)
@@ -485,107 +503,133 @@ __device__ __forceinline__ void gradient_of(const GradientArgs &a, int32_t p, co
         for (int32_t i = from + t; i < to; i += THREADS) d[i] = 0.0f;
         return;
     }
+    constexpr int kEach = PART / THREADS;
     const Norm z = {a.norm[2 * (int64_t)p], a.norm[2 * (int64_t)p + 1], a.d_entropy ? a.entropy[p] : 0.0f, -1};
     const float de = a.d_entropy ? a.d_entropy[p] : 0.0f;
     const int32_t *picks = a.picks + (int64_t)p * a.n_picks;
     const float *dl = a.d_logp + (int64_t)p * a.n_picks;
-    // a pick's candidate and gradient; -1 where it does not count: outside, or without a probability
-    auto pick_at = [&](uint32_t i, float &g) {
-        int32_t j = picks[i];
-        g = dl[i];
-        if (j < 0 || j >= q.n || !(log_probability(q, z, j, q.s[j]) > kNone)) j = -1;
-        return j;
+    // a thread's first pick stays with it
+    int32_t own_j = -1;
+    float own_g = 0.0f, own_s = kNone;
+    if constexpr (PICKS) {
+        if (t < a.n_picks) {
+            own_j = picks[t];
+            own_g = dl[t];
+        }
+    }
+    // a part's scores: four in a row a thread where it is whole, else one
+    float s[kEach];
+    auto fetch = [&](int32_t part) {
+        if (to - part >= PART) {
+#pragma unroll
+            for (int k = 0; k < kEach; k += 4) {
+                const f32x4u_t w = *reinterpret_cast<const f32x4u_t *>(q.s + part + (k * THREADS + t * 4));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[k + i] = w[i];
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kEach; ++k) s[k] = part + k * THREADS + t < to ? q.s[part + k * THREADS + t] : kNone;
+        }
+    };
+    fetch(from);
+    // a pick's score, and its candidate: -1 where it does not count, outside or without a probability
+    auto counted = [&](int32_t j, float &v) {
+        if (j < 0 || j >= q.n) return -1;
+        v = q.s[j];
+        return log_probability(q, z, j, v) > kNone ? j : -1;
     };
     float S = 0.0f;
-    int32_t own_j = -1;
-    float own_g = 0.0f;
     int e = 0;
     bool fine = true;
+    auto fixed = [&](float v) { return (unsigned long long)(long long)__builtin_rint(__builtin_ldexp((double)v, -e)); };
+    auto value = [&](unsigned long long v) { return (float)__builtin_ldexp((double)(long long)v, e); };
     if constexpr (PICKS) {
         if (t == 0) {
             fx.most = 0;
             fx.total = 0;
         }
-        for (int32_t i = t; i < PART; i += THREADS) fx.acc[i] = 0;
-        if (t < a.n_picks) own_j = pick_at((uint32_t)t, own_g);
+        own_j = counted(own_j, own_s);
         group_barrier<THREADS>();
         uint32_t most = own_j >= 0 ? __float_as_uint(own_g) & 0x7fffffffu : 0u;
         for (uint32_t i = t + THREADS; i < (uint32_t)a.n_picks; i += THREADS) {
-            float g;
-            const uint32_t b = pick_at(i, g) >= 0 ? __float_as_uint(g) & 0x7fffffffu : 0u;
+            float v;
+            const uint32_t b = counted(picks[i], v) >= 0 ? __float_as_uint(dl[i]) & 0x7fffffffu : 0u;
             most = b > most ? b : most;
         }
         most = wave_max_u32(most);
         if constexpr (THREADS > 64) {
-            if ((threadIdx.x & 63) == 0) atomicMax(&fx.most, most);
+            if ((threadIdx.x & 63) == 0 && most != 0) atomicMax(&fx.most, most);
             group_barrier<THREADS>();
             most = fx.most;
         }
         fine = most < 0x7f800000u;
         e = (int)(most >> 23) - 126 + (32 - __builtin_clz((uint32_t)a.n_picks)) - 62;
-        S = __uint_as_float(most);                          // (as it is where it is not finite)
+        if (fine) {
+            if (own_j >= 0) atomicAdd(&fx.total, fixed(own_g));
+            for (uint32_t i = t + THREADS; i < (uint32_t)a.n_picks; i += THREADS) {
+                float v;
+                if (counted(picks[i], v) >= 0) atomicAdd(&fx.total, fixed(dl[i]));
+            }
+        }
+        group_barrier<THREADS>();
+        S = fine ? value(fx.total) : __uint_as_float(most);
     }
-    auto fixed = [&](float v) { return (unsigned long long)(long long)__builtin_rint(__builtin_ldexp((double)v, -e)); };
-    auto value = [&](unsigned long long v) { return (float)__builtin_ldexp((double)(long long)v, e); };
     const float rate = kLog2e / q.T, by_T = fminf(1.0f / q.T, 3.4028235e38f);
     const float log2_mass = z.log_mass * kLog2e;
+    // lt: log2 of a score's weight.  No weight (NaN and -inf, and below the numbers): no gradient
+    auto lt_of = [&](float v) { return v == z.best ? 0.0f : (v - z.best) * rate; };
+    auto done = [&](float v, float lt, float r) { return v > kNone && lt > kNone ? r * by_T : 0.0f; };
+    auto of_entropy = [&](float pr, float lp) { return de * (pr > 0.0f ? pr * (lp + z.entropy) : 0.0f); };
     for (int32_t part = from; part < to; part += PART) {
         const int32_t n = to - part < PART ? to - part : PART;
+        auto each = [&](auto &&f) {                         // of the picks in this part that count
+            if (own_j >= part && own_j - part < n) f(own_j - part, own_s, own_g);
+            for (uint32_t i = t + THREADS; i < (uint32_t)a.n_picks; i += THREADS) {
+                float v;
+                const int32_t j = counted(picks[i], v);
+                if (j >= part && j - part < n) f(j - part, v, dl[i]);
+            }
+        };
         if constexpr (PICKS) {
             if (fine) {                                     // (uniform)
-                auto add = [&](int32_t j, float g, bool first) {
-                    if (j < 0) return;
-                    const unsigned long long v = fixed(g);
-                    if (first) atomicAdd(&fx.total, v);
-                    if (j >= part && j - part < n) atomicAdd(&fx.acc[j - part], v);
-                };
-                add(own_j, own_g, part == from);
-                for (uint32_t i = t + THREADS; i < (uint32_t)a.n_picks; i += THREADS) {
-                    float g;
-                    const int32_t j = pick_at(i, g);
-                    add(j, g, part == from);
-                }
+                each([&](int32_t i, float, float) { fx.acc[i] = 0; });
+                group_barrier<THREADS>();
+                each([&](int32_t i, float, float g) { atomicAdd(&fx.acc[i], fixed(g)); });
             }
-            group_barrier<THREADS>();
-            if (fine) S = value(fx.total);
         }
-        auto grad = [&](int32_t j, float s) {
-            const float delta = s - z.best, lt = s == z.best ? 0.0f : delta * rate;      // log2 of the weight
-            const float pr = __builtin_amdgcn_exp2f(lt - log2_mass);
-            float own = 0.0f, others = S;
-            if constexpr (PICKS) {
-                const unsigned long long f = fx.acc[j - part];
-                if (f != 0) {
-                    // g (1 - p) without the difference where p is nearly 1
-                    const float g = value(f);
-                    own = -g * expm1f(log_probability(q, z, j, s));
-                    others = S - g;
-                }
-            }
-            const float lp = lt * kLn2 - z.log_mass;
-            const float v = own - pr * others - de * (pr > 0.0f ? pr * (lp + z.entropy) : 0.0f);
-            // (a weight below the normal numbers is 0, and so is the gradient but where it was picked)
-            return s > kNone && lt > kNone ? v * by_T : 0.0f;
-        };
-        if (n == PART) {
-#pragma unroll 4
-            for (int32_t i = t * 4; i < PART; i += THREADS * 4) {
-                const f32x4u_t s = *reinterpret_cast<const f32x4u_t *>(q.s + part + i);
-                f32x4u_t o;
+        float o[kEach];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) o[k] = grad(part + i + k, s[k]);
-                *reinterpret_cast<f32x4u_t *>(d + part + i) = o;
-            }
-        } else {
-#pragma unroll 4
-            for (int32_t i = t; i < n; i += THREADS) d[part + i] = grad(part + i, q.s[part + i]);
+        for (int k = 0; k < kEach; ++k) {
+            const float lt = lt_of(s[k]), pr = __builtin_amdgcn_exp2f(lt - log2_mass);
+            o[k] = done(s[k], lt, -pr * S - of_entropy(pr, lt * kLn2 - z.log_mass));
         }
-        if constexpr (PICKS)
-            if (part + PART < to) {                         // cleared for the next part
-                group_barrier<THREADS>();
-                for (int32_t i = t; i < PART; i += THREADS) fx.acc[i] = 0;
-                group_barrier<THREADS>();
+        if (n == PART) {
+#pragma unroll
+            for (int k = 0; k < kEach; k += 4)
+                *reinterpret_cast<f32x4u_t *>(d + part + (k * THREADS + t * 4)) = (f32x4u_t){o[k], o[k + 1], o[k + 2], o[k + 3]};
+        } else {
+#pragma unroll
+            for (int k = 0; k < kEach; ++k)
+                if (k * THREADS + t < n) d[part + k * THREADS + t] = o[k];
+        }
+        if (part + PART < to) fetch(part + PART);
+        if constexpr (PICKS) {
+            if (fine) {
+                group_barrier<THREADS, true>();
+                auto again = [&](int32_t i, float v, float) {
+                    const float lt = lt_of(v), pr = __builtin_amdgcn_exp2f(lt - log2_mass), lp = lt * kLn2 - z.log_mass;
+                    // g (1 - p): where p is above 0.6 by the series of 1 - exp(lp), without the difference
+                    float x = 1.0f / 9.0f;
+#pragma unroll
+                    for (int m = 8; m >= 1; --m) x = (1.0f + lp * x) * (1.0f / (float)m);
+                    const float g = value(fx.acc[i]), own = g * (lp > -0.5f ? -lp * x : 1.0f - pr);
+                    d[part + i] = done(v, lt, own - pr * (S - g) - of_entropy(pr, lp));
+                };
+                each(again);
+                if (part + PART < to) group_barrier<THREADS>();   // the next part's entries
             }
+        }
     }
 }
 
@@ -610,13 +654,12 @@ __global__ __launch_bounds__(kThreads) void k_logprob_gradient(GradientArgs a)
 {
     __shared__ Fixed<PICKS ? kPart : 1> fx;
     const int32_t p = a.p0 + (int32_t)blockIdx.y;
-    clear_others(a, ((int64_t)p * gridDim.x + blockIdx.x) * kThreads + threadIdx.x, (int64_t)a.P * gridDim.x * kThreads);
     const Problem q = problem_of(a, p);
     // whole parts to each, the last ones to the last
     const int32_t parts = (q.n + kPart - 1) / kPart, each = (parts + (int32_t)gridDim.x - 1) / (int32_t)gridDim.x;
     const int64_t from = (int64_t)blockIdx.x * each * kPart, to = from + (int64_t)each * kPart;
-    if (from >= q.n) return;
-    gradient_of<kThreads, kPart, PICKS>(a, p, q, (int32_t)from, (int32_t)(to < q.n ? to : q.n), threadIdx.x, fx);
+    if (from < q.n) gradient_of<kThreads, kPart, PICKS>(a, p, q, (int32_t)from, (int32_t)(to < q.n ? to : q.n), threadIdx.x, fx);
+    clear_others(a, ((int64_t)p * gridDim.x + blockIdx.x) * kThreads + threadIdx.x, (int64_t)a.P * gridDim.x * kThreads);
 }
 
 // A wave has a problem of up to kSmallPart candidates; longer ones follow, by the whole workgroup.
@@ -632,9 +675,8 @@ __global__ __launch_bounds__(kThreads) void k_logprob_gradient_waves(GradientArg
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int32_t p0 = a.p0 + (int32_t)blockIdx.x * kWaves, p = p0 + wave;
     if (p < a.P) {
-        clear_others(a, (int64_t)p * 64 + (threadIdx.x & 63), (int64_t)a.P * 64);
         const Problem q = problem_of(a, p);
-        if (q.n <= kSmallPart) gradient_of<64, kSmallPart, PICKS>(a, p, q, 0, q.n, threadIdx.x & 63, reinterpret_cast<Small *>(lds)[wave]);
+        if (q.n <= kSmallPart && q.n > 0) gradient_of<64, kSmallPart, PICKS>(a, p, q, 0, q.n, threadIdx.x & 63, reinterpret_cast<Small *>(lds)[wave]);
     }
     for (int32_t i = 0; i < kWaves && p0 + i < a.P; ++i) {
         const Problem q = problem_of(a, p0 + i);
@@ -642,6 +684,7 @@ __global__ __launch_bounds__(kThreads) void k_logprob_gradient_waves(GradientArg
         __syncthreads();
         gradient_of<kThreads, kPart, PICKS>(a, p0 + i, q, 0, q.n, threadIdx.x, *reinterpret_cast<Large *>(lds));
     }
+    if (p < a.P) clear_others(a, (int64_t)p * 64 + (threadIdx.x & 63), (int64_t)a.P * 64);
 }
 
 }  // namespace
@@ -649,12 +692,13 @@ __global__ __launch_bounds__(kThreads) void k_logprob_gradient_waves(GradientArg
 namespace {
 
 // Problems' lengths are not known here; their mean is.
-int32_t parts_of(int64_t R, int32_t P)
+int32_t parts_of(int64_t R, int32_t P, int32_t top)
 {
     const int64_t mean = R / P, n_cu = compute_units();
-    if (2 * (int64_t)P > n_cu || mean < 4 * kTile) return 1;
-    const int64_t by_units = 2 * n_cu / P, by_length = mean / kTile, n = by_units < by_length ? by_units : by_length;
-    return (int32_t)(n < kMostParts ? n : kMostParts);
+    if (2 * (int64_t)P > n_cu || mean < 8 * kWideTile) return 1;
+    const int64_t by_units = 2 * n_cu / P, by_length = (mean + kWideTile - 1) / kWideTile, n = by_units < by_length ? by_units : by_length;
+    const int64_t most = kMostKeys / (top > 16 ? top : 16);
+    return (int32_t)(n < most ? n : most);
 }
 
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -663,7 +707,7 @@ size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 size_t logprob_workspace_bytes(int64_t R, int32_t P, int32_t top)
 {
-    const int32_t n = parts_of(R, P);
+    const int32_t n = parts_of(R, P, top);
     return n == 1 ? 0 : up256((size_t)P * n * sizeof(Part)) + (size_t)P * n * top * 8;
 }
 
@@ -672,7 +716,7 @@ hipError_t launch_logprob(const float *scores, int64_t R, const int64_t *seg, in
                           float *top_logp, void *ws, hipStream_t s)
 {
     LogprobArgs a{scores, R, seg, temperature, temperature_of, picks, n_picks, top, logp, entropy, norm, top_idx, top_logp, P, 0};
-    const int32_t parts = parts_of(R, P);
+    const int32_t parts = parts_of(R, P, top);
     const int64_t mean = R / P;
     auto go = [&]<bool TOP>() {
         if (parts > 1) {
@@ -686,11 +730,13 @@ hipError_t launch_logprob(const float *scores, int64_t R, const int64_t *seg, in
                 else hipLaunchKernelGGL((k_logprob_waves<16, TOP>), dim3((n + 3) / 4), dim3(kThreads), 0, s, a);
             });
         } else if (P <= compute_units()) {
-            hipLaunchKernelGGL((k_logprob<1024, TOP>), dim3(P), dim3(1024), 0, s, a);
+            hipLaunchKernelGGL((k_logprob<1024, kTile, TOP>), dim3(P), dim3(1024), 0, s, a);
         } else {
             each_span(P, [&](int32_t p0, int32_t n) {
                 a.p0 = p0;
-                hipLaunchKernelGGL((k_logprob<256, TOP>), dim3(n), dim3(256), 0, s, a);
+                if (mean <= 2048) hipLaunchKernelGGL((k_logprob<256, 2048, TOP>), dim3(n), dim3(256), 0, s, a);
+                else if (mean <= 8192) hipLaunchKernelGGL((k_logprob<256, 4096, TOP>), dim3(n), dim3(256), 0, s, a);
+                else hipLaunchKernelGGL((k_logprob<512, kTile, TOP>), dim3(n), dim3(512), 0, s, a);
             });
         }
     };
@@ -713,7 +759,9 @@ hipError_t launch_logprob_gradient(const float *scores, int64_t R, const int64_t
             });
             return;
         }
-        const int64_t by_length = (2 * mean + kPart - 1) / kPart, each = by_length < 64 ? by_length : 64;
+        // parts of up to twice the mean length; several to a workgroup where there are more of them than run at once
+        const int64_t by_length = (2 * mean + kPart - 1) / kPart, at_once = 5 * (int64_t)compute_units() / P;
+        const int64_t most = at_once > 2 ? at_once : 2, each = by_length < most ? by_length : most;
         for (a.p0 = 0; a.p0 < P; a.p0 += 1 << 15) {         // (a grid's second dimension)
             const int32_t n = P - a.p0 < 1 << 15 ? P - a.p0 : 1 << 15;
             hipLaunchKernelGGL((k_logprob_gradient<PICKS>), dim3((unsigned)each, n), dim3(kThreads), 0, s, a);
