@@ -29,8 +29,17 @@ __device__ __forceinline__ Problem problem_of(const float *scores, int64_t R, co
     return {scores + a, a, (int32_t)(b > a ? b - a : 0), T, !(T > 0.0f)};
 }
 
-// NaN takes no part, as -inf does.
-__device__ __forceinline__ float taking_part(float s) { return s > kNone ? s : kNone; }
+typedef float f32x4u_t __attribute__((ext_vector_type(4), aligned(4)));   // four scores from any segment's start
+
+// Scores i .. i + 3 of n, -inf past the last.
+__device__ __forceinline__ f32x4u_t load4(const float *s, int32_t i, int32_t n)
+{
+    if (i + 4 <= n) return *reinterpret_cast<const f32x4u_t *>(s + i);
+    f32x4u_t w;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = i + k < n ? s[i + k] : kNone;
+    return w;
+}
 
 // log2 of a candidate's weight against the best one's; -200 (weight 0) for what
 // has none: -inf against anything, and NaN, as of 0 times infinity.
@@ -56,21 +65,25 @@ __device__ __forceinline__ Mass joined(const Mass &a, const Mass &b, float rate)
     return {x.best, x.equal + y.equal, x.less + y.less, x.weighted + y.weighted};
 }
 
+// N more scores.  NaN takes no part: it is above nothing, equals nothing and its weight is 0.
 template <int N>
 __device__ __forceinline__ void take(Mass &m, const float (&v)[N], float rate)
 {
-    float top = v[0];
+    float top = m.best;
 #pragma unroll
-    for (int i = 1; i < N; ++i) top = fmaxf(top, v[i]);
+    for (int i = 0; i < N; ++i) top = v[i] > top ? v[i] : top;
     if (top > m.best) m = lowered(m, top, rate);
+    uint32_t equal = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
+        // (of the best itself t is 0, or -200 where it is +inf: it adds nothing to the third sum)
         const float t = weight_exponent(v[i], m.best, rate), e = __builtin_amdgcn_exp2f(t);
         const bool is_best = v[i] == m.best;
-        m.equal += is_best ? 1.0f : 0.0f;
+        equal += is_best;
         m.less += is_best ? 0.0f : e;
-        m.weighted += is_best ? 0.0f : e * t;
+        m.weighted = __builtin_fmaf(e, t, m.weighted);
     }
+    m.equal += (float)equal;
 }
 
 template <int CTRL, int ROW_MASK>
@@ -207,12 +220,10 @@ __device__ __forceinline__ void take_tile(Mass &m, const uint32_t (&bits)[N], ui
     for (int i = 0; i < N; ++i) {
         const uint32_t b = bits[i];
         const float s = __uint_as_float(b ^ (~(uint32_t)((int32_t)b >> 31) | 0x80000000u));
-        v[i] = t0 + threadIdx.x + i * NT < (uint32_t)n ? taking_part(s) : kNone;
+        v[i] = t0 + threadIdx.x + i * NT < (uint32_t)n ? s : kNone;
     }
     take(m, v, rate);
 }
-
-typedef float f32x4u_t __attribute__((ext_vector_type(4), aligned(4)));   // four scores from any segment's start
 
 // n scores by a workgroup, 16 a thread and step.
 template <int NT>
@@ -220,24 +231,14 @@ __device__ __forceinline__ Mass take_all(const float *s, int32_t n, float rate)
 {
     Mass m = kNothing;
     constexpr int kStep = 16 * NT;
-    int32_t at = 0;
-    for (; at <= n - kStep; at += kStep) {
+    for (int32_t at = 0; at < n; at += kStep) {
+        const int32_t left = n - at;
         f32x4u_t w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const f32x4u_t *>(s + at + (i * NT + (int)threadIdx.x) * 4);
+        for (int i = 0; i < 4; ++i) w[i] = load4(s + at, (i * NT + (int)threadIdx.x) * 4, left);
         float v[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = taking_part(w[i >> 2][i & 3]);
-        take(m, v, rate);
-    }
-    // the rest: at most 16 a thread
-    if (at < n) {
-        float v[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int32_t j = at + i * NT + (int)threadIdx.x;
-            v[i] = j < n ? taking_part(s[j]) : kNone;
-        }
+        for (int i = 0; i < 16; ++i) v[i] = w[i >> 2][i & 3];
         take(m, v, rate);
     }
     return m;
@@ -316,7 +317,7 @@ __global__ __launch_bounds__(kThreads) void k_logprob_waves(LogprobArgs a)
             const float rate = kLog2e / q.T;
             float v[EACH];
 #pragma unroll
-            for (int e = 0; e < EACH; ++e) v[e] = lane + 64 * e < q.n ? taking_part(q.s[lane + 64 * e]) : kNone;
+            for (int e = 0; e < EACH; ++e) v[e] = lane + 64 * e < q.n ? q.s[lane + 64 * e] : kNone;
             Mass m = kNothing;
             take(m, v, rate);
             m = wave_mass(m, rate);
@@ -482,6 +483,26 @@ __device__ __forceinline__ void group_barrier()
     }
 }
 
+template <int CTRL, int ROW_MASK, bool ZERO_FILL>
+__device__ __forceinline__ uint64_t dpp_add64(uint64_t v)
+{
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROW_MASK, 0xf, ZERO_FILL);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROW_MASK, 0xf, ZERO_FILL);
+    return v + (((uint64_t)hi << 32) | lo);
+}
+
+// Sum over the wave, in every lane.  (An atomic to LDS by 64 lanes is a loop over them: 2 us.)
+__device__ __forceinline__ uint64_t wave_sum(uint64_t v)
+{
+    v = dpp_add64<0x111, 0xf, true>(v);
+    v = dpp_add64<0x112, 0xf, true>(v);
+    v = dpp_add64<0x114, 0xf, true>(v);
+    v = dpp_add64<0x118, 0xf, true>(v);
+    v = dpp_add64<0x142, 0xa, false>(v);
+    v = dpp_add64<0x143, 0xc, false>(v);
+    return lane_value(v, 63);
+}
+
 // Picks' gradients in fixed point: sums do not depend on their order.  Of acc only the picked candidates' entries are used.
 template <int PART>
 struct Fixed {
@@ -517,19 +538,14 @@ __device__ __forceinline__ void gradient_of(const GradientArgs &a, int32_t p, co
             own_g = dl[t];
         }
     }
-    // a part's scores: four in a row a thread where it is whole, else one
+    // a part's scores, four in a row a thread
     float s[kEach];
     auto fetch = [&](int32_t part) {
-        if (to - part >= PART) {
 #pragma unroll
-            for (int k = 0; k < kEach; k += 4) {
-                const f32x4u_t w = *reinterpret_cast<const f32x4u_t *>(q.s + part + (k * THREADS + t * 4));
+        for (int k = 0; k < kEach; k += 4) {
+            const f32x4u_t w = load4(q.s + part, k * THREADS + t * 4, to - part);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[k + i] = w[i];
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < kEach; ++k) s[k] = part + k * THREADS + t < to ? q.s[part + k * THREADS + t] : kNone;
+            for (int i = 0; i < 4; ++i) s[k + i] = w[i];
         }
     };
     fetch(from);
@@ -565,15 +581,18 @@ __device__ __forceinline__ void gradient_of(const GradientArgs &a, int32_t p, co
         }
         fine = most < 0x7f800000u;
         e = (int)(most >> 23) - 126 + (32 - __builtin_clz((uint32_t)a.n_picks)) - 62;
-        if (fine) {
-            if (own_j >= 0) atomicAdd(&fx.total, fixed(own_g));
-            for (uint32_t i = t + THREADS; i < (uint32_t)a.n_picks; i += THREADS) {
-                float v;
-                if (counted(picks[i], v) >= 0) atomicAdd(&fx.total, fixed(dl[i]));
-            }
+        unsigned long long sum = fine && own_j >= 0 ? fixed(own_g) : 0ull;
+        for (uint32_t i = t + THREADS; i < (uint32_t)a.n_picks; i += THREADS) {
+            float v;
+            if (fine && counted(picks[i], v) >= 0) sum += fixed(dl[i]);
         }
-        group_barrier<THREADS>();
-        S = fine ? value(fx.total) : __uint_as_float(most);
+        sum = wave_sum(sum);
+        if constexpr (THREADS > 64) {
+            if ((threadIdx.x & 63) == 0 && sum != 0) atomicAdd(&fx.total, sum);
+            group_barrier<THREADS>();
+            sum = fx.total;
+        }
+        S = fine ? value(sum) : __uint_as_float(most);
     }
     const float rate = kLog2e / q.T, by_T = fminf(1.0f / q.T, 3.4028235e38f);
     const float log2_mass = z.log_mass * kLog2e;
@@ -604,14 +623,16 @@ __device__ __forceinline__ void gradient_of(const GradientArgs &a, int32_t p, co
             const float lt = lt_of(s[k]), pr = __builtin_amdgcn_exp2f(lt - log2_mass);
             o[k] = done(s[k], lt, -pr * S - of_entropy(pr, lt * kLn2 - z.log_mass));
         }
-        if (n == PART) {
 #pragma unroll
-            for (int k = 0; k < kEach; k += 4)
-                *reinterpret_cast<f32x4u_t *>(d + part + (k * THREADS + t * 4)) = (f32x4u_t){o[k], o[k + 1], o[k + 2], o[k + 3]};
-        } else {
+        for (int k = 0; k < kEach; k += 4) {
+            const int32_t i = k * THREADS + t * 4;
+            if (i + 4 <= n) {
+                *reinterpret_cast<f32x4u_t *>(d + part + i) = (f32x4u_t){o[k], o[k + 1], o[k + 2], o[k + 3]};
+            } else {
 #pragma unroll
-            for (int k = 0; k < kEach; ++k)
-                if (k * THREADS + t < n) d[part + k * THREADS + t] = o[k];
+                for (int j = 0; j < 4; ++j)
+                    if (i + j < n) d[part + i + j] = o[k + j];
+            }
         }
         if (part + PART < to) fetch(part + PART);
         if constexpr (PICKS) {
