@@ -361,7 +361,7 @@ __global__ __launch_bounds__(kThreads) void k_logprob_waves(LogprobArgs a)
 
 // Few long problems: each goes in parts to workgroups of its own, whose sums and
 // best candidates one workgroup joins.
-constexpr int kWide = 512, kWideTile = 4096, kMostKeys = 4096;
+constexpr int kWide = 512, kWideTile = 4096;
 
 struct Part {
     Mass m;
@@ -389,62 +389,83 @@ __global__ __launch_bounds__(kWide) void k_logprob_parts(LogprobArgs a, Parts to
         for (int32_t r = threadIdx.x; r < a.top; r += kWide) to.keys[at * a.top + r] = lds.keys[r] ? lds.keys[r] - (uint32_t)from : 0ull;
 }
 
+// The most parts of a problem, and of their candidates (each part's `top`).
+constexpr int kMostParts = 256, kMostKeys = 4096;
+
+// One load of each thread's share of the parts and their candidates, all on their way at once; then the
+// candidates that can be among the best are ranked by counting the larger ones.
 template <bool TOP>
-__global__ __launch_bounds__(kThreads) void k_logprob_join(LogprobArgs a, Parts from)
+__global__ __launch_bounds__(kWide) void k_logprob_join(LogprobArgs a, Parts from)
 {
+    constexpr int kKeys = kMostKeys / kWide, kEach = kMostParts / 64;
     __shared__ uint64_t list[TOP ? kMostKeys : 1], keys[64];
-    __shared__ uint64_t floor_;
     __shared__ int32_t n_list;
-    const int32_t p = blockIdx.x;
+    const int32_t p = blockIdx.x, top = a.top;
     const int lane = threadIdx.x & 63;
-    const Problem q = problem_of(a, p);
-    const Pick pick = pick_of(a, q, p, threadIdx.x);
-    // a lane has every 64th part
-    const float rate = kLog2e / q.T;
-    Mass own_mass = kNothing;
-    const Part *part = from.part + (int64_t)p * from.n;
-    for (int32_t g = lane; g < from.n; g += 64) own_mass = joined(own_mass, part[g].m, rate);
-    const Mass m = wave_mass(own_mass, rate);
-    int32_t first = -1;
-    if (q.cold) {                                           // parts are in the candidates' order: the first that has the best score
-        int32_t g = lane;
-        while (g < from.n && part[g].m.best != m.best) g += 64;
-        g = (int32_t)(0xffffffffu - wave_max_u32(0xffffffffu - (uint32_t)g));
-        if (g < from.n) first = part[g].first;
+    uint64_t key[kKeys], own = 0, last = 0;
+    const uint64_t *k = from.keys + (int64_t)p * from.n * top;
+    const int32_t lanes = from.n < 64 ? from.n : 64, half = lanes > 1 ? lanes / 2 : 1;
+    // j-th best of r lanes' parts at least: j r >= top
+    const int32_t j = (top + half - 1) / half, r = TOP ? (top + j - 1) / j : 0;
+    Part part[kEach];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+        const int32_t g = lane + 64 * e;
+        part[e] = g < from.n ? from.part[(int64_t)p * from.n + g] : Part{kNothing, -1};
     }
     if constexpr (TOP) {
-        const uint64_t *k = from.keys + (int64_t)p * from.n * a.top;
-        const int32_t top = a.top;
-        // Keys that the best `top` are not below: the largest of the parts' last, and the r-th largest of the lanes' j-th (of
-        // a lane's parts the largest j-th), r j >= top.
-        if (threadIdx.x < 64) {
-            const int32_t lanes = from.n < 64 ? from.n : 64, half = lanes > 1 ? lanes / 2 : 1, j = (top + half - 1) / half, r = (top + j - 1) / j;
-            uint64_t own = 0, last = 0;
-            for (int32_t g = lane; g < from.n; g += 64) {
-                const uint64_t o = k[(int64_t)g * top + j - 1], l = k[(int64_t)g * top + top - 1];
-                own = o > own ? o : own;
-                last = l > last ? l : last;
-            }
-            int32_t above = 0;
-            for (int32_t l = 0; l < lanes; ++l) {
-                const uint64_t o = lane_value(own, l);
-                above += o > own || (o == own && l < lane);
-            }
-            const uint64_t bound = lane_value(own, __builtin_ctzll(__ballot(lane < lanes && above == r - 1))), most = wave_max_key(last);
-            if (lane == 0) {
-                floor_ = bound > most ? bound : most;
-                n_list = 0;
-            }
-            if (lane < top) keys[lane] = 0;
+#pragma unroll
+        for (int e = 0; e < kKeys; ++e) {
+            const int32_t i = (int32_t)threadIdx.x + e * kWide;
+            key[e] = i < from.n * top ? k[i] : 0ull;
         }
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const int32_t g = lane + 64 * e;
+            const uint64_t o = g < from.n ? k[(int64_t)g * top + j - 1] : 0ull, l = g < from.n ? k[(int64_t)g * top + top - 1] : 0ull;
+            own = o > own ? o : own;
+            last = l > last ? l : last;
+        }
+        if (threadIdx.x == 0) n_list = 0;
+        if (threadIdx.x < 64) keys[threadIdx.x] = 0;
+    }
+    const Problem q = problem_of(a, p);
+    const Pick pick = pick_of(a, q, p, threadIdx.x);
+    // every wave joins the parts for itself
+    const float rate = kLog2e / q.T;
+    Mass m = part[0].m;
+#pragma unroll
+    for (int e = 1; e < kEach; ++e) m = joined(m, part[e].m, rate);
+    m = wave_mass(m, rate);
+    int32_t first = -1;
+    if (q.cold) {                                           // parts are in the candidates' order: the first that has the best score
+        uint32_t g = 0xffffffffu;
+        int32_t of = -1;
+#pragma unroll
+        for (int e = kEach - 1; e >= 0; --e)
+            if (part[e].m.best == m.best && lane + 64 * e < from.n) {
+                g = (uint32_t)(lane + 64 * e);
+                of = part[e].first;
+            }
+        const uint32_t low = 0xffffffffu - wave_max_u32(0xffffffffu - g);
+        const uint64_t has = __ballot(g == low && low != 0xffffffffu);
+        if (has) first = __builtin_amdgcn_readlane(of, __builtin_ctzll(has));
+    }
+    if constexpr (TOP) {
+        // What the best `top` are not below: the largest of the parts' last candidates, and the score that r lanes' j-th
+        // best reach (of a lane's parts the one whose j-th is best), to 24 bits.
+        uint32_t bits = 0;
+#pragma unroll
+        for (int b = 31; b >= 8; --b)
+            if (__popcll(__ballot((uint32_t)(own >> 32) >= (bits | 1u << b))) >= r) bits |= 1u << b;
+        const uint64_t most = wave_max_key(last), floor = (uint64_t)bits << 32 > most ? (uint64_t)bits << 32 : most;
         __syncthreads();
-        for (int32_t i = threadIdx.x; i < from.n * top; i += kThreads) {
-            const uint64_t v = k[i];
-            if (v != 0 && v >= floor_) list[atomicAdd(&n_list, 1)] = v;
-        }
+#pragma unroll
+        for (int e = 0; e < kKeys; ++e)
+            if (key[e] != 0 && key[e] >= floor) list[atomicAdd(&n_list, 1)] = key[e];
         __syncthreads();
         const int32_t n = n_list;
-        for (int32_t i = threadIdx.x; i < n; i += kThreads) {
+        for (int32_t i = threadIdx.x; i < n; i += kWide) {
             const uint64_t v = list[i];
             int32_t rank = 0;
 #pragma unroll 8
@@ -453,7 +474,7 @@ __global__ __launch_bounds__(kThreads) void k_logprob_join(LogprobArgs a, Parts 
         }
         __syncthreads();
     }
-    write_problem<kThreads>(a, q, p, norm_of(m, q, first), threadIdx.x, pick, keys);
+    write_problem<kWide>(a, q, p, norm_of(m, q, first), threadIdx.x, pick, keys);
 }
 
 struct GradientArgs {
@@ -718,7 +739,7 @@ int32_t parts_of(int64_t R, int32_t P, int32_t top)
     const int64_t mean = R / P, n_cu = compute_units();
     if (2 * (int64_t)P > n_cu || mean < 8 * kWideTile) return 1;
     const int64_t by_units = 2 * n_cu / P, by_length = (mean + kWideTile - 1) / kWideTile, n = by_units < by_length ? by_units : by_length;
-    const int64_t most = kMostKeys / (top > 16 ? top : 16);
+    const int64_t most = top * kMostParts > kMostKeys ? kMostKeys / top : kMostParts;
     return (int32_t)(n < most ? n : most);
 }
 
@@ -743,7 +764,7 @@ hipError_t launch_logprob(const float *scores, int64_t R, const int64_t *seg, in
         if (parts > 1) {
             const Parts w{static_cast<Part *>(ws), reinterpret_cast<uint64_t *>(static_cast<char *>(ws) + up256((size_t)P * parts * sizeof(Part))), parts};
             hipLaunchKernelGGL((k_logprob_parts<TOP>), dim3(parts, P), dim3(kWide), 0, s, a, w);
-            hipLaunchKernelGGL((k_logprob_join<TOP>), dim3(P), dim3(kThreads), 0, s, a, w);
+            hipLaunchKernelGGL((k_logprob_join<TOP>), dim3(P), dim3(kWide), 0, s, a, w);
         } else if (mean <= 1024) {
             each_span(P, [&](int32_t p0, int32_t n) {
                 a.p0 = p0;
