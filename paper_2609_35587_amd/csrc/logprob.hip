@@ -149,6 +149,20 @@ __device__ __forceinline__ float log_probability(const Problem &q, const Norm &z
     return t > kNone ? t - z.log_mass : kNone;              // (NaN: a finite score below +inf at T = inf)
 }
 
+// Waits for a group of THREADS: a wave's own accesses of LDS (GLOBAL: and of memory), or a workgroup's.
+template <int THREADS, bool GLOBAL = false>
+__device__ __forceinline__ void group_barrier()
+{
+    if constexpr (THREADS > 64) {
+        if constexpr (GLOBAL) __syncthreads();
+        else lds_barrier();
+    } else {
+        if constexpr (GLOBAL) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+        else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
 constexpr int kThreads = 256;
 
 struct LogprobArgs {
@@ -211,17 +225,13 @@ __device__ __forceinline__ void write_problem(const LogprobArgs &a, const Proble
     }
 }
 
-// The scores of a thread's rows of a tile, from their ordered bits.
-template <int NT, int N>
-__device__ __forceinline__ void take_tile(Mass &m, const uint32_t (&bits)[N], uint32_t t0, int32_t n, float rate)
+// The scores of a thread's rows of a tile, from their ordered bits (0, NaN's, takes no part).
+template <int N>
+__device__ __forceinline__ void take_tile(Mass &m, const uint32_t (&bits)[N], float rate)
 {
     float v[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const uint32_t b = bits[i];
-        const float s = __uint_as_float(b ^ (~(uint32_t)((int32_t)b >> 31) | 0x80000000u));
-        v[i] = t0 + threadIdx.x + i * NT < (uint32_t)n ? s : kNone;
-    }
+    for (int i = 0; i < N; ++i) v[i] = __uint_as_float(bits[i] ^ (~(uint32_t)((int32_t)bits[i] >> 31) | 0x80000000u));
     take(m, v, rate);
 }
 
@@ -260,7 +270,7 @@ __device__ __forceinline__ Mass block_scores(const float *s, int32_t n, int32_t 
     Mass m = kNothing;
     if constexpr (TOP) {
         topk_tiles<NT, TILE>(
-            s, n, top, lds.topk, [&](uint32_t t0, const auto &bits) { take_tile<NT>(m, bits, t0, n, rate); },
+            s, n, top, lds.topk, [&](const auto &bits) { take_tile(m, bits, rate); },
             [&](int32_t j, uint64_t key) { lds.keys[j] = key; });
         m = block_mass<NT>(m, rate, lds.part);              // (its barrier: the keys are there)
         if (cold) first = (int32_t)(0xffffffffu - (uint32_t)lds.keys[0]);
@@ -300,60 +310,99 @@ __global__ __launch_bounds__(NT) void k_logprob(LogprobArgs a)
     block_problem<NT, TILE, TOP>(a, a.p0 + (int32_t)blockIdx.x, lds);
 }
 
-// A wave has a problem of up to 64 EACH candidates, its scores in registers;
-// longer ones follow, by the whole workgroup.
+// A wave has a problem of up to 64 EACH candidates, its scores in registers.  A lone wave takes some 7 cycles an
+// instruction, so what it does goes by how many there are.
+constexpr int kSmall = 1024, kFew = 8;                      // kFew: alternatives for which lanes' best give a bound
+constexpr int kWaveList = 16 * kFew;
+
 template <int EACH, bool TOP>
+__device__ __forceinline__ void wave_problem(const LogprobArgs &a, const Problem &q, int32_t p, int lane, uint64_t *list, uint64_t *keys)
+{
+    const Pick pick = pick_of(a, q, p, lane);
+    const float rate = kLog2e / q.T;
+    float v[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) v[e] = lane + 64 * e < q.n ? q.s[lane + 64 * e] : kNone;
+    Mass m = kNothing;
+    take(m, v, rate);
+    m = wave_mass(m, rate);
+    int32_t first = -1;
+    const int32_t rounds = TOP ? a.top : q.cold ? 1 : 0;
+    if (rounds > 0) {
+        // What the best are not below: bits hi, of those that equal them ~index lo.  Found bit by bit: for few, what
+        // that many lanes' best reach; else what that many candidates do.  It is good once no more than that many do.
+        uint32_t bits[EACH], best = 0, at = 0;
+#pragma unroll
+        for (int e = EACH - 1; e >= 0; --e) {
+            bits[e] = v[e] > kNone ? order_key(v[e] + 0.0f) : 0u;
+            at = bits[e] >= best ? (uint32_t)(lane + 64 * e) : at;
+            best = bits[e] >= best ? bits[e] : best;
+        }
+        const bool few = rounds <= kFew;
+        auto reach = [&](uint32_t h, uint32_t l) {  // how many are not below (h, l)
+            if (few) return (int32_t)__popcll(__ballot(best > h || (best == h && 1023u - at >= l)));
+            int32_t c = 0;
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) c += __popcll(__ballot(bits[e] > h || (bits[e] == h && 1023u - (uint32_t)(lane + 64 * e) >= l)));
+            return c;
+        };
+        uint32_t hi = 0, lo = 0;
+        bool open = true;
+        for (int b = 31; b >= 0 && open; --b) {
+            const int32_t c = reach(hi | 1u << b, 0u);
+            if (c >= rounds) hi |= 1u << b;
+            open = c != rounds;
+        }
+        for (int b = 9; b >= 0 && open; --b) {
+            const int32_t c = reach(hi, lo | 1u << b);
+            if (c >= rounds) lo |= 1u << b;
+            open = c != rounds;
+        }
+        hi = hi > 1u ? hi : 1u;                     // (0: takes no part)
+        int32_t n_list = 0;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const uint32_t j = (uint32_t)(lane + 64 * e);
+            const bool in = bits[e] > hi || (bits[e] == hi && 1023u - j >= lo);
+            const uint64_t take = __ballot(in);
+            if (in)
+                list[n_list + (int32_t)__builtin_amdgcn_mbcnt_hi((uint32_t)(take >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)take, 0u))] =
+                    ((uint64_t)bits[e] << 32) | (0xffffffffu - j);
+            n_list += __popcll(take);
+        }
+        keys[lane] = 0;
+        group_barrier<64>();
+        for (int32_t i = lane; i < n_list; i += 64) {
+            const uint64_t own = list[i];
+            int32_t rank = 0;
+#pragma unroll 4
+            for (int32_t e = 0; e < n_list; ++e) rank += list[e] > own;
+            if (rank < rounds) keys[rank] = own;
+        }
+        group_barrier<64>();
+        first = (int32_t)(0xffffffffu - (uint32_t)keys[0]);
+    }
+    write_problem<64>(a, q, p, norm_of(m, q, q.cold ? first : -1), lane, pick, keys);
+}
+
+// Longer ones among them follow, by the whole workgroup.
+template <bool TOP>
 __global__ __launch_bounds__(kThreads) void k_logprob_waves(LogprobArgs a)
 {
     constexpr int kWaves = kThreads / 64;
     __shared__ Lds<kThreads> lds;
-    __shared__ uint64_t keys[kWaves][64];
+    __shared__ uint64_t keys[kWaves][64], list[kWaves][kWaveList];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int32_t p0 = a.p0 + (int32_t)blockIdx.x * kWaves, p = p0 + wave;
     if (p < a.P) {
         const Problem q = problem_of(a, p);
-        if (q.n <= 64 * EACH) {
-            const Pick pick = pick_of(a, q, p, lane);
-            const float rate = kLog2e / q.T;
-            float v[EACH];
-#pragma unroll
-            for (int e = 0; e < EACH; ++e) v[e] = lane + 64 * e < q.n ? q.s[lane + 64 * e] : kNone;
-            Mass m = kNothing;
-            take(m, v, rate);
-            m = wave_mass(m, rate);
-            int32_t first = -1;
-            const int32_t rounds = TOP ? a.top : q.cold ? 1 : 0;
-            if (rounds > 0) {
-                // the best that is left, round by round: its bits (0: none), the lowest index that has them
-                uint32_t bits[EACH];
-#pragma unroll
-                for (int e = 0; e < EACH; ++e) bits[e] = v[e] > kNone ? order_key(v[e] + 0.0f) : 0u;
-                uint64_t mine = 0;
-                for (int32_t r = 0; r < rounds; ++r) {
-                    uint32_t b = 0, at = 0;
-#pragma unroll
-                    for (int e = EACH - 1; e >= 0; --e) {
-                        at = bits[e] >= b ? (uint32_t)(lane + 64 * e) : at;
-                        b = bits[e] >= b ? bits[e] : b;
-                    }
-                    const uint32_t most = wave_max_u32(b);
-                    if (most == 0) break;
-                    const uint32_t low = wave_max_u32(b == most ? 0xffffffffu - at : 0u);
-                    if (lane == r) mine = ((uint64_t)most << 32) | low;
-                    const uint32_t j = 0xffffffffu - low;
-                    if (r == 0) first = (int32_t)j;
-#pragma unroll
-                    for (int e = 0; e < EACH; ++e) bits[e] = j == (uint32_t)(lane + 64 * e) ? 0u : bits[e];
-                }
-                if constexpr (TOP) keys[wave][lane] = mine;  // (read by its own wave alone)
-            }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
-            __builtin_amdgcn_wave_barrier();
-            write_problem<64>(a, q, p, norm_of(m, q, q.cold ? first : -1), lane, pick, keys[wave]);
-        }
+        if (q.n <= 64) wave_problem<1, TOP>(a, q, p, lane, list[wave], keys[wave]);
+        else if (q.n <= 256) wave_problem<4, TOP>(a, q, p, lane, list[wave], keys[wave]);
+        else if (q.n <= 512) wave_problem<8, TOP>(a, q, p, lane, list[wave], keys[wave]);
+        else if (q.n <= kSmall) wave_problem<16, TOP>(a, q, p, lane, list[wave], keys[wave]);
     }
     for (int32_t i = 0; i < kWaves && p0 + i < a.P; ++i) {
-        if (problem_of(a, p0 + i).n <= 64 * EACH) continue;  // (one answer for the workgroup)
+        if (problem_of(a, p0 + i).n <= kSmall) continue;     // (one answer for the workgroup)
         block_problem<kThreads, 2048, TOP>(a, p0 + i, lds);
         __syncthreads();
     }
@@ -489,20 +538,6 @@ struct GradientArgs {
     const float *d_logp, *entropy, *d_entropy;
     float *d_scores;
 };
-
-// Waits for a group of THREADS: a wave's own accesses of LDS (GLOBAL: and of memory), or a workgroup's.
-template <int THREADS, bool GLOBAL = false>
-__device__ __forceinline__ void group_barrier()
-{
-    if constexpr (THREADS > 64) {
-        if constexpr (GLOBAL) __syncthreads();
-        else lds_barrier();
-    } else {
-        if constexpr (GLOBAL) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
-        else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
-        __builtin_amdgcn_wave_barrier();
-    }
-}
 
 template <int CTRL, int ROW_MASK, bool ZERO_FILL>
 __device__ __forceinline__ uint64_t dpp_add64(uint64_t v)
@@ -765,11 +800,10 @@ hipError_t launch_logprob(const float *scores, int64_t R, const int64_t *seg, in
             const Parts w{static_cast<Part *>(ws), reinterpret_cast<uint64_t *>(static_cast<char *>(ws) + up256((size_t)P * parts * sizeof(Part))), parts};
             hipLaunchKernelGGL((k_logprob_parts<TOP>), dim3(parts, P), dim3(kWide), 0, s, a, w);
             hipLaunchKernelGGL((k_logprob_join<TOP>), dim3(P), dim3(kWide), 0, s, a, w);
-        } else if (mean <= 1024) {
+        } else if (mean <= kSmall) {
             each_span(P, [&](int32_t p0, int32_t n) {
                 a.p0 = p0;
-                if (mean <= 128) hipLaunchKernelGGL((k_logprob_waves<4, TOP>), dim3((n + 3) / 4), dim3(kThreads), 0, s, a);
-                else hipLaunchKernelGGL((k_logprob_waves<16, TOP>), dim3((n + 3) / 4), dim3(kThreads), 0, s, a);
+                hipLaunchKernelGGL((k_logprob_waves<TOP>), dim3((n + 3) / 4), dim3(kThreads), 0, s, a);
             });
         } else if (P <= compute_units()) {
             hipLaunchKernelGGL((k_logprob<1024, kTile, TOP>), dim3(P), dim3(1024), 0, s, a);

@@ -22,7 +22,7 @@ __device__ __forceinline__ uint32_t asc_bits(float t)
 constexpr int kShort = 1024, kShortThreads = 256;
 
 template <int NT>
-__global__ __launch_bounds__(NT) void k_topk(const float *__restrict__ scores, const int64_t *__restrict__ seg, int32_t k,
+__global__ __launch_bounds__(NT, 3) void k_topk(const float *__restrict__ scores, const int64_t *__restrict__ seg, int32_t k,
                                              int32_t *__restrict__ idx, float *__restrict__ vals)
 {
     __shared__ TopkLds<NT> lds;
@@ -31,7 +31,7 @@ __global__ __launch_bounds__(NT) void k_topk(const float *__restrict__ scores, c
     const float *s = scores + seg[p];
     idx += (int64_t)p * k;
     if (vals) vals += (int64_t)p * k;
-    auto each = [](uint32_t, const auto &) {};
+    auto each = [](const auto &) {};
     auto emit = [&](int32_t j, uint64_t key) {
         const int32_t li = key ? (int32_t)(0xffffffffu - (uint32_t)key) : -1;
         idx[j] = li;

@@ -28,14 +28,8 @@ namespace hwsel {
 // rows of a tile: 32 keys per thread of a small workgroup, 8 of a large one
 constexpr int kTile = 8192;
 
-// Larger key = better score.  NaN ranks lowest, -0 equals +0.
-__device__ __forceinline__ uint32_t desc_bits(float s)
-{
-    if (s != s) return 0u;
-    uint32_t b = __float_as_uint(s);
-    if ((b << 1) == 0u) b = 0u;
-    return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
-}
+// Larger key = better score.  NaN ranks lowest, -0 equals +0 (the sum makes it that).
+__device__ __forceinline__ uint32_t desc_bits(float s) { return s != s ? 0u : order_key(s + 0.0f); }
 
 template <int CTRL, int ROW_MASK, bool ZERO_FILL>
 __device__ __forceinline__ uint32_t dpp_max_u32(uint32_t v)
@@ -110,8 +104,8 @@ struct TopkLds {
 };
 
 // The k best of one segment by NT threads, TILE rows at a time (lds: for at
-// least as many threads).  each(t0, bits): the score bits of a tile's rows t0
-// + threadIdx.x + q NT (0.0's past the end), every tile once; emit(j, key): the j-th best, by one
+// least as many threads).  each(bits): the score bits of the thread's rows
+// of a tile (NaN's past the end), every tile once; emit(j, key): the j-th best, by one
 // thread (0: there is none).
 template <int NT, int TILE, class Lds, class Each, class Emit>
 __device__ __forceinline__ void topk_tiles(const float *__restrict__ s, int32_t n, int32_t k, Lds &lds, Each &&each, Emit &&emit)
@@ -130,7 +124,7 @@ __device__ __forceinline__ void topk_tiles(const float *__restrict__ s, int32_t 
 #pragma unroll
         for (int q = 0; q < kPer; ++q) {
             const uint32_t i = (uint32_t)t0 + threadIdx.x + q * NT;
-            next[q] = i < (uint32_t)n ? s[i] : 0.0f;
+            next[q] = i < (uint32_t)n ? s[i] : __builtin_nanf("");
         }
     };
     fetch(0);
@@ -146,14 +140,16 @@ __device__ __forceinline__ void topk_tiles(const float *__restrict__ s, int32_t 
 #pragma unroll
         for (int q = 0; q < kPer; ++q) hi[q] = desc_bits(next[q]);
         if (t0 + TILE < (uint32_t)n) fetch(t0 + TILE);
-        each(t0, hi);
-        uint64_t most = 0;                                  // the lane's largest key
+        each(hi);
+        uint32_t most_hi = 0;                               // of the lane's largest key
 #pragma unroll
-        for (int q = 0; q < kPer; ++q) most = key(q) > most ? key(q) : most;
+        for (int q = 0; q < kPer; ++q) most_hi = hi[q] > most_hi ? hi[q] : most_hi;
 
         // A key that is at most the k-th best of the tile and of the kept ones.
         auto bound = [&]() -> uint64_t {
-            uint64_t m = most, v = 0;
+            uint64_t m = 0, v = 0;                          // m: the lane's largest key
+#pragma unroll
+            for (int q = 0; q < kPer; ++q) m = key(q) > m ? key(q) : m;
             for (int32_t j = 0; j < j_of; ++j) {
                 v = wave_max_key(m);
                 m = m == v ? 0ull : m;
@@ -170,7 +166,7 @@ __device__ __forceinline__ void topk_tiles(const float *__restrict__ s, int32_t 
             return lane_value(mine, __builtin_ctzll(__ballot(lane < kWaves && above == r_of - 1)));
         };
         auto append = [&](uint64_t limit) {                 // keys above limit to cand; counted beyond its end too
-            if (__ballot(most > limit) == 0) return;
+            if (__ballot(most_hi >= (uint32_t)(limit >> 32)) == 0) return;
 #pragma unroll
             for (int q = 0; q < kPer; ++q) {
                 const uint64_t v = key(q);
