@@ -760,7 +760,7 @@ typedef struct hwsel_dropout {
  * gradient itself.  Y may be X or the residual (same data, ld and dtype); no other overlap.
  * Returns HWSEL_EINVAL for null pointers, sizes < 1, p outside [0, 1] or NaN,
  * a bad ld or alignment, a residual of another dtype; HWSEL_EUNSUPPORTED for
- * another dtype, rows or cols >= 2^31.
+ * another dtype, rows >= 2^31 or cols > 2^30.
  */
 int hwsel_dropout(const hwsel_dropout_t *how, int64_t rows, int64_t cols, const hwsel_matrix_t *X,
                   const hwsel_matrix_t *residual, const hwsel_matrix_t *Y, void *stream);
@@ -785,7 +785,7 @@ int hwsel_dropout(const hwsel_dropout_t *how, int64_t rows, int64_t cols, const 
  * Returns HWSEL_EINVAL for null pointers, sizes < 1, eps not > 0, scales that
  * are not finite, p outside [0, 1], bad flags, ld or alignment, dtypes that
  * differ where they are to be one; HWSEL_EUNSUPPORTED for another dtype, rows
- * or cols >= 2^31.
+ * >= 2^31 or cols > 2^30.
  */
 typedef struct hwsel_join {
     int64_t rows, cols;

@@ -698,12 +698,12 @@ static const hwsel_matrix_t kNoMatrix = {nullptr, 0, HWSEL_DTYPE_FP32};
 
 static const hwsel_matrix_t &or_none(const hwsel_matrix_t *m) { return m && m->data ? *m : kNoMatrix; }
 
-// Rows and columns of plain matrices are 32-bit numbers in the kernels.
+// Rows and columns of plain matrices are 32-bit numbers in the kernels, with room to step past the last column.
 static int check_plain_sizes(int64_t rows, int64_t cols, const char *fn)
 {
     if (rows < 1 || cols < 1) return fail(HWSEL_EINVAL, fn, "%lld x %lld", (long long)rows, (long long)cols);
-    if (rows > INT32_MAX || cols > INT32_MAX)
-        return fail(HWSEL_EUNSUPPORTED, fn, "%lld x %lld (below 2^31 each)", (long long)rows, (long long)cols);
+    if (rows > INT32_MAX || cols > (int64_t)1 << 30)
+        return fail(HWSEL_EUNSUPPORTED, fn, "%lld x %lld (rows below 2^31, at most 2^30 columns)", (long long)rows, (long long)cols);
     return HWSEL_OK;
 }
 

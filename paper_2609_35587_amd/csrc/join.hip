@@ -4,6 +4,8 @@
 // With d = d_x1 + r1 (dn - xn mean(dn xn)), dn = d_z w_pre, xn = x1 r1:
 //   dx = stream d;  dv = dropout(branch d);  dg = dv u;  du = dv g;  dw_branch = sum du yn;
 //   dy = r (dn' - yn mean(dn' yn)), dn' = du w_branch;  dw_pre = sum d_z xn
+#include <type_traits>
+
 #include "rows.hpp"
 
 namespace hwsel {
@@ -24,8 +26,8 @@ struct Out {
 enum { kNoGate = 0, kRowGate = 1, kElementGate = 2 };
 
 struct Common {
-    int64_t cols;
-    int32_t rows;
+    int32_t rows, cols;
+    Ends ends;
     const float *wb, *wp;
     float eps, inv_cols, stream, branch;
     int32_t post_norm, gate_kind, sigmoid;
@@ -81,10 +83,12 @@ __device__ __forceinline__ void block_sums(float (&v)[N], float (&sh)[N][NT / 64
     }
 }
 
-__device__ __forceinline__ void weights8(const float *w, int64_t col, int64_t n, float (&v)[8])
+template <class E>
+__device__ __forceinline__ void weights8(const float *w, int32_t col, const Common &c, const E &ends, float (&v)[8])
 {
     if (w) {
-        const Eight<false> e = load8<false>(w, col, n);
+        Eight<false> e = load8<false>(w, col, c.cols - col, ends);
+        settle8(e, c.cols - col, ends);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = e.at(i);
     } else {
@@ -99,11 +103,19 @@ struct Stream8 {
     Eight<SBF> x1, dx1;
     Eight<BBF> dz;
 
-    __device__ __forceinline__ void load(const Backward &a, int64_t row, int64_t col, int64_t n)
+    template <class E>
+    __device__ __forceinline__ void load(const Backward &a, int64_t row, int32_t col, int32_t n, const E &ends)
     {
-        x1 = load8<SBF>(a.x1.p, row * a.x1.ld + col, a.dz.p ? n : 0);   // (of no use without d_z)
-        dx1 = load8<SBF>(a.dx1.p, row * a.dx1.ld + col, a.dx1.p ? n : 0);
-        dz = load8<BBF>(a.dz.p, row * a.dz.ld + col, a.dz.p ? n : 0);
+        x1 = load8<SBF>(a.x1.p, row * a.x1.ld + col, a.dz.p ? n : 0, ends);   // (of no use without d_z)
+        dx1 = load8<SBF>(a.dx1.p, row * a.dx1.ld + col, a.dx1.p ? n : 0, ends);
+        dz = load8<BBF>(a.dz.p, row * a.dz.ld + col, a.dz.p ? n : 0, ends);
+    }
+    template <class E>
+    __device__ __forceinline__ void settle(int32_t n, const E &ends)
+    {
+        settle8(x1, n, ends);
+        settle8(dx1, n, ends);
+        settle8(dz, n, ends);
     }
     __device__ __forceinline__ float d(int i, float wp, float r1, float m1) const
     {
@@ -112,7 +124,7 @@ struct Stream8 {
 };
 
 // dv of eight columns from their d.
-__device__ __forceinline__ void branch8(const Common &c, const Mask &m, int64_t row, int64_t col, const float (&d)[8], float (&dv)[8])
+__device__ __forceinline__ void branch8(const Common &c, const Mask &m, int64_t row, int32_t col, const float (&d)[8], float (&dv)[8])
 {
 #pragma unroll
     for (int i = 0; i < 8; ++i) dv[i] = c.branch * d[i];
@@ -120,35 +132,39 @@ __device__ __forceinline__ void branch8(const Common &c, const Mask &m, int64_t 
 }
 
 template <int CTRL>
-__device__ __forceinline__ float ror_add(float v)
+__device__ __forceinline__ float dpp_moved_add(float v)
 {
     return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
 }
 
-// Sums of N values over LANES neighbouring threads, in each of them: rotations
-// within 16 lanes, the four rows of a wave by scalar reads, waves through LDS
-// (two buffers in turn, so that a sum costs one barrier).
-template <int LANES>
+// Sums of N values over LANES neighbouring threads (0: the workgroup's), in
+// each of them: lane moves within 8 or 16 lanes, the four rows of a wave by
+// scalar reads, waves through LDS (two buffers in turn, so that a sum costs one
+// barrier).
 struct Shared {
-    float v[2][4][LANES / 64 > 0 ? LANES / 64 : 1];
+    float v[2][3][16];
 };
 
 template <int LANES, int N>
-__device__ __forceinline__ void lane_sums(float (&v)[N], Shared<LANES> &sh, int &turn)
+__device__ __forceinline__ void lane_sums(float (&v)[N], Shared &sh, int &turn)
 {
-    static_assert(N <= 4, "room in Shared");
+    static_assert(N <= 3, "room in Shared");
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = ror_add<0x121>(ror_add<0x122>(ror_add<0x124>(ror_add<0x128>(v[i]))));
-    if constexpr (LANES >= 64) {
+    for (int i = 0; i < N; ++i) {
+        // lanes i ^ 1, i ^ 2, then the other four of eight; rotations by 8 of 16
+        v[i] = dpp_moved_add<0x141>(dpp_moved_add<0x4e>(dpp_moved_add<0xb1>(v[i])));
+        if constexpr (LANES != 8) v[i] = dpp_moved_add<0x128>(v[i]);
+    }
+    if constexpr (LANES == 0 || LANES >= 32) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int b = __float_as_int(v[i]);
-            v[i] = (__int_as_float(__builtin_amdgcn_readlane(b, 0)) + __int_as_float(__builtin_amdgcn_readlane(b, 16))) +
-                   (__int_as_float(__builtin_amdgcn_readlane(b, 32)) + __int_as_float(__builtin_amdgcn_readlane(b, 48)));
+            const float low = __int_as_float(__builtin_amdgcn_readlane(b, 0)) + __int_as_float(__builtin_amdgcn_readlane(b, 16));
+            const float high = __int_as_float(__builtin_amdgcn_readlane(b, 32)) + __int_as_float(__builtin_amdgcn_readlane(b, 48));
+            v[i] = LANES != 32 ? low + high : threadIdx.x & 32 ? high : low;
         }
     }
-    if constexpr (LANES > 64) {
-        constexpr int kWaves = LANES / 64;
+    if constexpr (LANES == 0) {
         auto &to = sh.v[turn];
         turn ^= 1;
         if ((threadIdx.x & 63) == 0) {
@@ -156,11 +172,11 @@ __device__ __forceinline__ void lane_sums(float (&v)[N], Shared<LANES> &sh, int 
             for (int i = 0; i < N; ++i) to[i][threadIdx.x >> 6] = v[i];
         }
         lds_barrier();
+        const int waves = (int)blockDim.x >> 6;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            v[i] = 0.0f;
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) v[i] += to[i][w];
+            v[i] = to[i][0];
+            for (int w = 1; w < waves; ++w) v[i] += to[i][w];
         }
     }
 }
@@ -169,41 +185,66 @@ __device__ __forceinline__ void lane_sums(float (&v)[N], Shared<LANES> &sh, int 
 // Rows that fit the registers of LANES threads, 8 K columns each: a row is read
 // once and written once.  Threads keep their columns from row to row.
 // ---------------------------------------------------------------------------
-constexpr int threads_of(int lanes) { return lanes > 256 ? lanes : 256; }
+template <bool EDGE>
+__device__ __forceinline__ std::conditional_t<EDGE, Ends, NoEnds> ends_in(const Common &c)
+{
+    if constexpr (EDGE) return c.ends;
+    else return {};
+}
+
+// Rows that a workgroup has at once: of 256 threads, or one.
+template <int LANES>
+constexpr int kRows = LANES ? 256 / LANES : 1;
 
 template <int LANES>
 __device__ __forceinline__ int64_t first_row()
 {
-    constexpr int kGroups = threads_of(LANES) / LANES;
-    const int group = (int)threadIdx.x / LANES;
-    return (int64_t)blockIdx.x * kGroups + (LANES >= 64 ? __builtin_amdgcn_readfirstlane(group) : group);
+    if constexpr (LANES == 0) return blockIdx.x;
+    const int group = (int)threadIdx.x / (LANES ? LANES : 1);
+    return (int64_t)blockIdx.x * kRows<LANES> + (LANES == 64 ? __builtin_amdgcn_readfirstlane(group) : group);
 }
 
-template <bool SBF, bool BBF, int LANES, int K>
-__global__ __launch_bounds__(threads_of(LANES)) void k_join(Forward a)
+// The first of a thread's columns in its k-th eight.
+template <int LANES>
+__device__ __forceinline__ int32_t column(int k)
 {
-    __shared__ Shared<LANES> sh;
-    constexpr int kGroups = threads_of(LANES) / LANES;
+    const int lanes = LANES ? LANES : (int)blockDim.x;
+    return (LANES ? threadIdx.x % (LANES ? LANES : 1) : threadIdx.x) * 8 + k * lanes * 8;
+}
+
+template <bool SBF, bool BBF, int LANES, int K, bool EDGE>
+__global__ __launch_bounds__(LANES ? 256 : 1024) void k_join(Forward a)
+{
+    __shared__ Shared sh;
     const Common &c = a.c;
+    const std::conditional_t<EDGE, Ends, NoEnds> ends = ends_in<EDGE>(c);
     const Mask m = mask_of(c.drop);
-    const int64_t col0 = (threadIdx.x % LANES) * 8;
-    auto col_of = [&](int k) { return col0 + (int64_t)k * LANES * 8; };
+    auto col_of = [&](int k) { return column<LANES>(k); };
     float wb[K][8], wp[K][8];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        weights8(c.wb, col_of(k), c.cols - col_of(k), wb[k]);
-        weights8(c.wp, col_of(k), c.cols - col_of(k), wp[k]);
+        weights8(c.wb, col_of(k), c, ends, wb[k]);
+        weights8(c.wp, col_of(k), c, ends, wp[k]);
     }
     int turn = 0;
-    for (int64_t row = first_row<LANES>(); row < c.rows; row += (int64_t)gridDim.x * kGroups) {
+    for (int64_t row = first_row<LANES>(); row < c.rows; row += (int64_t)gridDim.x * kRows<LANES>) {
         Eight<SBF> x[K];
         Eight<BBF> y[K], g[K];
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const int64_t col = col_of(k), n = c.cols - col;
-            x[k] = load8<SBF>(a.x.p, row * a.x.ld + col, n);
-            if (a.y.p) y[k] = load8<BBF>(a.y.p, row * a.y.ld + col, n);
-            if (c.gate_kind == kElementGate) g[k] = load8<BBF>(a.gate.p, row * a.gate.ld + col, n);
+            const int32_t col = col_of(k), n = c.cols - col;
+            x[k] = load8<SBF>(a.x.p, row * a.x.ld + col, n, ends);
+            if (a.y.p) y[k] = load8<BBF>(a.y.p, row * a.y.ld + col, n, ends);
+            if (c.gate_kind == kElementGate) g[k] = load8<BBF>(a.gate.p, row * a.gate.ld + col, n, ends);
+        }
+        if (ends.shift != 0) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int32_t n = c.cols - col_of(k);
+                settle8(x[k], n, ends);
+                if (a.y.p) settle8(y[k], n, ends);
+                if (c.gate_kind == kElementGate) settle8(g[k], n, ends);
+            }
         }
         float x1[K][8];
         if (a.y.p) {
@@ -240,7 +281,7 @@ __global__ __launch_bounds__(threads_of(LANES)) void k_join(Forward a)
         }
         if (a.x1.p) {
 #pragma unroll
-            for (int k = 0; k < K; ++k) store8<SBF>(a.x1.p, row * a.x1.ld + col_of(k), c.cols - col_of(k), x1[k]);
+            for (int k = 0; k < K; ++k) store8<SBF>(a.x1.p, row * a.x1.ld + col_of(k), c.cols - col_of(k), ends, x1[k]);
         }
         if (a.z.p) {
             float t[1] = {0.0f};
@@ -255,7 +296,7 @@ __global__ __launch_bounds__(threads_of(LANES)) void k_join(Forward a)
                 float z[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) z[i] = x1[k][i] * r1 * wp[k][i];
-                store8<BBF>(a.z.p, row * a.z.ld + col_of(k), c.cols - col_of(k), z);
+                store8<BBF>(a.z.p, row * a.z.ld + col_of(k), c.cols - col_of(k), ends, z);
             }
         }
     }
@@ -263,32 +304,41 @@ __global__ __launch_bounds__(threads_of(LANES)) void k_join(Forward a)
 
 // Two rounds of sums a row: x1^2, dn x1 and y^2 together, then what goes by d.
 // A workgroup's sums over its rows go to a part of their own.
-template <bool SBF, bool BBF, int LANES, int K>
-__global__ __launch_bounds__(threads_of(LANES)) void k_join_gradient(Backward a)
+template <bool SBF, bool BBF, int LANES, int K, bool EDGE>
+__global__ __launch_bounds__(LANES ? 256 : 512, K == 2 ? 2 : LANES == 64 || LANES == 0 ? 4 : 3) void k_join_gradient(Backward a)
 {
-    constexpr int kGroups = threads_of(LANES) / LANES;
-    __shared__ Shared<LANES> sh;
-    __shared__ __attribute__((aligned(16))) float sums[kGroups > 1 ? kGroups : 1][kGroups > 1 ? LANES * 8 * K : 1];
+    constexpr int kGroups = kRows<LANES>;
+    __shared__ Shared sh;
+    __shared__ __attribute__((aligned(16))) float sums[kGroups][LANES ? LANES * 8 * K : 1];
     const Common &c = a.c;
+    const std::conditional_t<EDGE, Ends, NoEnds> ends = ends_in<EDGE>(c);
     const Mask m = mask_of(c.drop);
-    const int64_t col0 = (threadIdx.x % LANES) * 8;
-    auto col_of = [&](int k) { return col0 + (int64_t)k * LANES * 8; };
+    auto col_of = [&](int k) { return column<LANES>(k); };
     float wb[K][8], wp[K][8], swb[K][8] = {}, swp[K][8] = {};
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        weights8(c.wb, col_of(k), c.cols - col_of(k), wb[k]);
-        weights8(c.wp, col_of(k), c.cols - col_of(k), wp[k]);
+        weights8(c.wb, col_of(k), c, ends, wb[k]);
+        weights8(c.wp, col_of(k), c, ends, wp[k]);
     }
     int turn = 0;
-    for (int64_t row = first_row<LANES>(); row < c.rows; row += (int64_t)gridDim.x * kGroups) {
+    for (int64_t row = first_row<LANES>(); row < c.rows; row += (int64_t)gridDim.x * kRows<LANES>) {
         Stream8<SBF, BBF> q[K];
         Eight<BBF> y[K], g[K];
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const int64_t col = col_of(k), n = c.cols - col;
-            q[k].load(a, row, col, n);
-            y[k] = load8<BBF>(a.y.p, row * a.y.ld + col, a.y.p ? n : 0);
-            g[k] = load8<BBF>(a.gate.p, row * a.gate.ld + col, c.gate_kind == kElementGate ? n : 0);
+            const int32_t col = col_of(k), n = c.cols - col;
+            q[k].load(a, row, col, n, ends);
+            y[k] = load8<BBF>(a.y.p, row * a.y.ld + col, a.y.p ? n : 0, ends);
+            g[k] = load8<BBF>(a.gate.p, row * a.gate.ld + col, c.gate_kind == kElementGate ? n : 0, ends);
+        }
+        if (ends.shift != 0) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int32_t n = c.cols - col_of(k);
+                q[k].settle(n, ends);
+                settle8(y[k], n, ends);
+                settle8(g[k], n, ends);
+            }
         }
         float s[3] = {};
 #pragma unroll
@@ -311,7 +361,7 @@ __global__ __launch_bounds__(threads_of(LANES)) void k_join_gradient(Backward a)
                 swp[k][i] += q[k].dz.at(i) * (q[k].x1.at(i) * r1);
                 o[i] = c.stream * d[k][i];
             }
-            if (a.dx.p) store8<SBF>(a.dx.p, row * a.dx.ld + col_of(k), c.cols - col_of(k), o);
+            if (a.dx.p) store8<SBF>(a.dx.p, row * a.dx.ld + col_of(k), c.cols - col_of(k), ends, o);
         }
         if (!a.y.p) continue;
         const float r = c.post_norm ? norm_factor(s[2], c) : 1.0f;
@@ -335,7 +385,7 @@ __global__ __launch_bounds__(threads_of(LANES)) void k_join_gradient(Backward a)
             if (a.dgate.p && c.gate_kind == kElementGate) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) dg[i] *= gate_slope(g[k].at(i), c.sigmoid);
-                store8<BBF>(a.dgate.p, row * a.dgate.ld + col_of(k), c.cols - col_of(k), dg);
+                store8<BBF>(a.dgate.p, row * a.dgate.ld + col_of(k), c.cols - col_of(k), ends, dg);
             }
         }
         if (c.post_norm || c.gate_kind == kRowGate) lane_sums<LANES>(t, sh, turn);
@@ -346,10 +396,10 @@ __global__ __launch_bounds__(threads_of(LANES)) void k_join_gradient(Backward a)
                 float o[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) o[i] = r * (d[k][i] - y[k].at(i) * r * mean);
-                store8<BBF>(a.dy.p, row * a.dy.ld + col_of(k), c.cols - col_of(k), o);
+                store8<BBF>(a.dy.p, row * a.dy.ld + col_of(k), c.cols - col_of(k), ends, o);
             }
         }
-        if (threadIdx.x % LANES == 0 && a.dgate.p && c.gate_kind == kRowGate) {
+        if (col_of(0) == 0 && a.dgate.p && c.gate_kind == kRowGate) {
             const float dg = t[1] * gate_slope(gate, c.sigmoid);
             if constexpr (BBF) static_cast<uint16_t *>(a.dgate.p)[row * a.dgate.ld] = (uint16_t)bf16_pair(dg, 0.0f);
             else static_cast<float *>(a.dgate.p)[row * a.dgate.ld] = dg;
@@ -360,9 +410,9 @@ __global__ __launch_bounds__(threads_of(LANES)) void k_join_gradient(Backward a)
         if constexpr (kGroups > 1) {
             __syncthreads();
 #pragma unroll
-            for (int k = 0; k < K; ++k) store8<false>(&sums[threadIdx.x / LANES][0], (int)col_of(k), 8, v[k]);
+            for (int k = 0; k < K; ++k) store8<false>(&sums[threadIdx.x / LANES][0], col_of(k), 8, ends, v[k]);
             __syncthreads();
-            for (int col = threadIdx.x; col < LANES * 8 * K && col < c.cols; col += threads_of(LANES)) {
+            for (int col = threadIdx.x; col < LANES * 8 * K && col < c.cols; col += 256) {
                 float t = sums[0][col];
 #pragma unroll
                 for (int i = 1; i < kGroups; ++i) t += sums[i][col];
@@ -370,7 +420,7 @@ __global__ __launch_bounds__(threads_of(LANES)) void k_join_gradient(Backward a)
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < K; ++k) store8<false>(to, col_of(k), c.cols - col_of(k), v[k]);
+            for (int k = 0; k < K; ++k) store8<false>(to, col_of(k), c.cols - col_of(k), ends, v[k]);
         }
     };
     if (a.want_wb) hand_on(swb, part);
@@ -380,20 +430,22 @@ __global__ __launch_bounds__(threads_of(LANES)) void k_join_gradient(Backward a)
 // ---------------------------------------------------------------------------
 // Rows of any length: a workgroup goes through a row several times.
 // ---------------------------------------------------------------------------
-constexpr int kLong = 1024;
+constexpr int kLong = 512;
 
 template <bool SBF, bool BBF>
 __global__ __launch_bounds__(kLong) void k_join_long(Forward a)
 {
     __shared__ float sh[1][kLong / 64];
     const Common &c = a.c;
+    const Ends ends = c.ends;
     const int64_t row = c.row0 + blockIdx.x;
     const Mask m = mask_of(c.drop);
     float r = 1.0f;
     if (a.y.p && c.post_norm) {
         float s[1] = {0.0f};
-        for (int64_t col = threadIdx.x * 8; col < c.cols; col += kLong * 8) {
-            const Eight<BBF> y = load8<BBF>(a.y.p, row * a.y.ld + col, c.cols - col);
+        for (int32_t col = threadIdx.x * 8; col < c.cols; col += kLong * 8) {
+            Eight<BBF> y = load8<BBF>(a.y.p, row * a.y.ld + col, c.cols - col, ends);
+            settle8(y, c.cols - col, ends);
 #pragma unroll
             for (int i = 0; i < 8; ++i) s[0] += y.at(i) * y.at(i);
         }
@@ -401,18 +453,21 @@ __global__ __launch_bounds__(kLong) void k_join_long(Forward a)
         r = norm_factor(s[0], c);
     }
     const float row_gate = c.gate_kind == kRowGate ? gate_value(load1<BBF>(a.gate.p, row * a.gate.ld), c.sigmoid) : 1.0f;
-    auto joined = [&](int64_t col, float (&x1)[8]) {
-        const int64_t n = c.cols - col;
-        const Eight<SBF> x = load8<SBF>(a.x.p, row * a.x.ld + col, n);
+    auto joined = [&](int32_t col, float (&x1)[8]) {
+        const int32_t n = c.cols - col;
+        Eight<SBF> x = load8<SBF>(a.x.p, row * a.x.ld + col, n, ends);
+        settle8(x, n, ends);
         float v[8] = {};
         if (a.y.p) {
-            const Eight<BBF> y = load8<BBF>(a.y.p, row * a.y.ld + col, n);
+            Eight<BBF> y = load8<BBF>(a.y.p, row * a.y.ld + col, n, ends);
+            settle8(y, n, ends);
             float w[8];
-            weights8(c.wb, col, n, w);
+            weights8(c.wb, col, c, ends, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = c.branch * row_gate * (y.at(i) * r * w[i]);
             if (c.gate_kind == kElementGate) {
-                const Eight<BBF> g = load8<BBF>(a.gate.p, row * a.gate.ld + col, n);
+                Eight<BBF> g = load8<BBF>(a.gate.p, row * a.gate.ld + col, n, ends);
+                settle8(g, n, ends);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] *= gate_value(g.at(i), c.sigmoid);
             }
@@ -424,7 +479,7 @@ __global__ __launch_bounds__(kLong) void k_join_long(Forward a)
     float r1 = 1.0f;
     if (a.z.p) {
         float s[1] = {0.0f};
-        for (int64_t col = threadIdx.x * 8; col < c.cols; col += kLong * 8) {
+        for (int32_t col = threadIdx.x * 8; col < c.cols; col += kLong * 8) {
             float x1[8];
             joined(col, x1);
 #pragma unroll
@@ -433,17 +488,17 @@ __global__ __launch_bounds__(kLong) void k_join_long(Forward a)
         block_sums<kLong>(s, sh);
         r1 = norm_factor(s[0], c);
     }
-    for (int64_t col = threadIdx.x * 8; col < c.cols; col += kLong * 8) {
-        const int64_t n = c.cols - col;
+    for (int32_t col = threadIdx.x * 8; col < c.cols; col += kLong * 8) {
+        const int32_t n = c.cols - col;
         float x1[8];
         joined(col, x1);
-        if (a.x1.p) store8<SBF>(a.x1.p, row * a.x1.ld + col, n, x1);
+        if (a.x1.p) store8<SBF>(a.x1.p, row * a.x1.ld + col, n, ends, x1);
         if (a.z.p) {
             float w[8], z[8];
-            weights8(c.wp, col, n, w);
+            weights8(c.wp, col, c, ends, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) z[i] = x1[i] * r1 * w[i];
-            store8<BBF>(a.z.p, row * a.z.ld + col, n, z);
+            store8<BBF>(a.z.p, row * a.z.ld + col, n, ends, z);
         }
     }
 }
@@ -454,16 +509,19 @@ __global__ __launch_bounds__(kLong) void k_join_long_stats(Backward a)
 {
     __shared__ float sh3[3][kLong / 64], sh2[2][kLong / 64];
     const Common &c = a.c;
+    const Ends ends = c.ends;
     const int64_t row = c.row0 + blockIdx.x;
     const Mask m = mask_of(c.drop);
     float s[3] = {};
-    for (int64_t col = threadIdx.x * 8; col < c.cols; col += kLong * 8) {
-        const int64_t n = c.cols - col;
+    for (int32_t col = threadIdx.x * 8; col < c.cols; col += kLong * 8) {
+        const int32_t n = c.cols - col;
         if (a.dz.p) {
-            const Eight<SBF> x1 = load8<SBF>(a.x1.p, row * a.x1.ld + col, n);
-            const Eight<BBF> dz = load8<BBF>(a.dz.p, row * a.dz.ld + col, n);
+            Eight<SBF> x1 = load8<SBF>(a.x1.p, row * a.x1.ld + col, n, ends);
+            settle8(x1, n, ends);
+            Eight<BBF> dz = load8<BBF>(a.dz.p, row * a.dz.ld + col, n, ends);
+            settle8(dz, n, ends);
             float w[8];
-            weights8(c.wp, col, n, w);
+            weights8(c.wp, col, c, ends, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 s[0] += x1.at(i) * x1.at(i);
@@ -471,7 +529,8 @@ __global__ __launch_bounds__(kLong) void k_join_long_stats(Backward a)
             }
         }
         if (a.y.p && c.post_norm) {
-            const Eight<BBF> y = load8<BBF>(a.y.p, row * a.y.ld + col, n);
+            Eight<BBF> y = load8<BBF>(a.y.p, row * a.y.ld + col, n, ends);
+            settle8(y, n, ends);
 #pragma unroll
             for (int i = 0; i < 8; ++i) s[2] += y.at(i) * y.at(i);
         }
@@ -483,15 +542,18 @@ __global__ __launch_bounds__(kLong) void k_join_long_stats(Backward a)
     if (a.y.p && (c.post_norm || c.gate_kind == kRowGate)) {
         const float gate = c.gate_kind == kRowGate ? load1<BBF>(a.gate.p, row * a.gate.ld) : 1.0f;
         const float row_gate = c.gate_kind == kRowGate ? gate_value(gate, c.sigmoid) : 1.0f;
-        for (int64_t col = threadIdx.x * 8; col < c.cols; col += kLong * 8) {
-            const int64_t n = c.cols - col;
+        for (int32_t col = threadIdx.x * 8; col < c.cols; col += kLong * 8) {
+            const int32_t n = c.cols - col;
             Stream8<SBF, BBF> q;
-            q.load(a, row, col, n);
-            const Eight<BBF> y = load8<BBF>(a.y.p, row * a.y.ld + col, n);
-            const Eight<BBF> g = load8<BBF>(a.gate.p, row * a.gate.ld + col, c.gate_kind == kElementGate ? n : 0);
+            q.load(a, row, col, n, ends);
+            q.settle(n, ends);
+            Eight<BBF> y = load8<BBF>(a.y.p, row * a.y.ld + col, n, ends);
+            settle8(y, n, ends);
+            Eight<BBF> g = load8<BBF>(a.gate.p, row * a.gate.ld + col, c.gate_kind == kElementGate ? n : 0, ends);
+            settle8(g, n, ends);
             float wp[8], wb[8], d[8], dv[8];
-            weights8(c.wp, col, n, wp);
-            weights8(c.wb, col, n, wb);
+            weights8(c.wp, col, c, ends, wp);
+            weights8(c.wb, col, c, ends, wb);
 #pragma unroll
             for (int i = 0; i < 8; ++i) d[i] = q.d(i, wp[i], r1, m1);
             branch8(c, m, row, col, d, dv);
@@ -525,18 +587,20 @@ template <bool SBF, bool BBF>
 __global__ __launch_bounds__(kTile) void k_join_long_columns(Backward a)
 {
     const Common &c = a.c;
-    const int64_t col = ((int64_t)blockIdx.x * kTile + threadIdx.x) * 8, n = c.cols - col;
+    const Ends ends = c.ends;
+    const int32_t col = (int32_t)(blockIdx.x * kTile + threadIdx.x) * 8, n = c.cols - col;
     if (n <= 0) return;
     const Mask m = mask_of(c.drop);
     float wp[8], wb[8], swb[8] = {}, swp[8] = {};
-    weights8(c.wp, col, n, wp);
-    weights8(c.wb, col, n, wb);
+    weights8(c.wp, col, c, ends, wp);
+    weights8(c.wb, col, c, ends, wb);
     const int64_t first = (int64_t)blockIdx.y * a.rows_each, last = first + a.rows_each < c.rows ? first + a.rows_each : c.rows;
     for (int64_t row = first; row < last; ++row) {
         const float *st = a.stats + row * 4;
         const float r1 = st[0], m1 = st[1], r = st[2], mean = st[3];
         Stream8<SBF, BBF> q;
-        q.load(a, row, col, n);
+        q.load(a, row, col, n, ends);
+        q.settle(n, ends);
         float d[8], o[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -544,9 +608,11 @@ __global__ __launch_bounds__(kTile) void k_join_long_columns(Backward a)
             swp[i] += q.dz.at(i) * (q.x1.at(i) * r1);
             o[i] = c.stream * d[i];
         }
-        const Eight<BBF> y = load8<BBF>(a.y.p, row * a.y.ld + col, a.y.p ? n : 0);
-        const Eight<BBF> g = load8<BBF>(a.gate.p, row * a.gate.ld + col, c.gate_kind == kElementGate ? n : 0);
-        if (a.dx.p) store8<SBF>(a.dx.p, row * a.dx.ld + col, n, o);
+        Eight<BBF> y = load8<BBF>(a.y.p, row * a.y.ld + col, a.y.p ? n : 0, ends);
+        settle8(y, n, ends);
+        Eight<BBF> g = load8<BBF>(a.gate.p, row * a.gate.ld + col, c.gate_kind == kElementGate ? n : 0, ends);
+        settle8(g, n, ends);
+        if (a.dx.p) store8<SBF>(a.dx.p, row * a.dx.ld + col, n, ends, o);
         if (!a.y.p) continue;
         const float row_gate = c.gate_kind == kRowGate ? gate_value(load1<BBF>(a.gate.p, row * a.gate.ld), c.sigmoid) : 1.0f;
         float dv[8];
@@ -560,44 +626,54 @@ __global__ __launch_bounds__(kTile) void k_join_long_columns(Backward a)
             swb[i] += du * yn;
             o[i] = r * (du * wb[i] - yn * mean);
         }
-        if (a.dy.p) store8<BBF>(a.dy.p, row * a.dy.ld + col, n, o);
-        if (a.dgate.p && c.gate_kind == kElementGate) store8<BBF>(a.dgate.p, row * a.dgate.ld + col, n, dg);
+        if (a.dy.p) store8<BBF>(a.dy.p, row * a.dy.ld + col, n, ends, o);
+        if (a.dgate.p && c.gate_kind == kElementGate) store8<BBF>(a.dgate.p, row * a.dgate.ld + col, n, ends, dg);
     }
     float *part = a.parts + (int64_t)blockIdx.y * 2 * c.cols;
-    if (a.want_wb) store8<false>(part, col, n, swb);
-    if (a.want_wp) store8<false>(part, c.cols + col, n, swp);
+    if (a.want_wb) store8<false>(part, col, n, ends, swb);
+    if (a.want_wp) store8<false>(part, c.cols + col, n, ends, swp);
 }
 
-// Sums of the parts: dw_branch and dw_pre.  A workgroup has 32 columns, eight
-// threads each, every one an eighth of the parts.
-constexpr int kSumCols = 32;
+// Sums of the parts: dw_branch and dw_pre.  A workgroup has 32 columns, 32
+// threads each, every one a 32nd of the parts: 512 parts of 1,024 columns in two
+// rounds of eight loads.
+constexpr int kSumCols = 32, kSumThreads = 1024;
 
-__global__ __launch_bounds__(kTile) void k_join_sums(const float *__restrict__ parts, int32_t n_parts, int64_t cols, float *dwb, float *dwp)
+__global__ __launch_bounds__(kSumThreads) void k_join_sums(const float *__restrict__ parts, int32_t n_parts, int64_t cols, float *dwb, float *dwp)
 {
-    constexpr int kSlices = kTile / kSumCols;
-    __shared__ float sh[kSlices][kSumCols];
+    constexpr int kSlices = kSumThreads / kSumCols;
+    __shared__ float sh[kSlices][kSumCols + 1];
     float *out = blockIdx.y ? dwp : dwb;
     if (!out) return;
-    const int slice = threadIdx.x / kSumCols;
-    const int64_t col = (int64_t)blockIdx.x * kSumCols + threadIdx.x % kSumCols;
+    const int slice = threadIdx.x / kSumCols, at = threadIdx.x % kSumCols;
+    const int64_t col = (int64_t)blockIdx.x * kSumCols + at;
     float s = 0.0f;
     if (col < cols) {
-        const float *at = parts + (int64_t)blockIdx.y * cols + col;
-#pragma unroll 8
-        for (int32_t i = slice; i < n_parts; i += kSlices) s += at[(int64_t)i * 2 * cols];
+        const float *from = parts + (int64_t)blockIdx.y * cols + col;
+        for (int32_t i = slice; i < n_parts; i += 8 * kSlices) {
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int32_t g = i + k * kSlices;
+                v[k] = g < n_parts ? from[(int64_t)g * 2 * cols] : 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s += v[k];
+        }
     }
-    sh[slice][threadIdx.x % kSumCols] = s;
+    sh[slice][at] = s;
     __syncthreads();
     if (slice != 0 || col >= cols) return;
 #pragma unroll
-    for (int i = 1; i < kSlices; ++i) s += sh[i][threadIdx.x];
+    for (int i = 1; i < kSlices; ++i) s += sh[i][at];
     out[col] = s;
 }
 
 Common common_of(const hwsel_join_t &j, bool has_y)
 {
     Common c{};
-    c.cols = j.cols;
+    c.cols = (int32_t)j.cols;
+    c.ends = ends_of(j.cols);
     c.rows = (int32_t)j.rows;
     c.wb = j.w_branch;
     c.wp = j.w_pre;
@@ -634,29 +710,55 @@ void each_row_span(Common &c, F &&f)
 
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// The longest rows that registers hold, and workgroups of a compute unit.
+// The longest rows that registers hold.
 constexpr int64_t kLongestForward = 16384, kLongestBackward = 8192;
-constexpr int32_t kForwardGroups = 8, kBackwardGroups = 4;
 
-// go<LANES, K>() for rows of `cols` columns.
-template <class F>
-void by_length(int64_t cols, F &&go)
+// How rows of some length lie in registers: `lanes` threads of K eights each (0: all of the workgroup's `threads`).
+struct Shape {
+    int lanes, K, threads;
+    int rows() const { return lanes ? 256 / lanes : 1; }
+};
+
+Shape shape_of(int64_t cols)
 {
-    if (cols <= 128) go.template operator()<16, 1>();
-    else if (cols <= 512) go.template operator()<64, 1>();
-    else if (cols <= 1024) go.template operator()<64, 2>();
-    else if (cols <= 2048) go.template operator()<256, 1>();
-    else if (cols <= 4096) go.template operator()<256, 2>();
-    else go.template operator()<512, 2>();                  // (1,024 threads of 8 columns spill in the gradient)
+    if (cols <= 64) return {8, 1, 256};
+    if (cols <= 128) return {16, 1, 256};
+    if (cols <= 256) return {32, 1, 256};
+    if (cols <= 512) return {64, 1, 256};
+    if (cols <= 1024) return {64, 2, 256};
+    if (cols <= 1536) return {0, 1, 192};                   // (128 threads of two eights leave more of them without columns)
+    return {0, 2, (int)((cols + 1023) / 1024) * 64};
 }
 
-int rows_at_once(int64_t cols) { return cols <= 128 ? 16 : cols <= 1024 ? 4 : 1; }
+// Workgroups that run at once where a SIMD holds `waves` of their waves, at most one for each row (or rows).
+int32_t groups_of(const Shape &f, int64_t rows, int waves)
+{
+    const int64_t each = 4 * waves * 64 / f.threads, most = (int64_t)compute_units() * (each > 1 ? each : 1), need = (rows + f.rows() - 1) / f.rows();
+    return (int32_t)(need < most ? need : most);
+}
 
-// Workgroups of the gradient, each with a part of its own: as many as run at once.
+int32_t forward_groups(const hwsel_join_t &j)
+{
+    const Shape f = shape_of(j.cols);
+    return groups_of(f, j.rows, f.K == 1 ? (f.lanes && f.lanes < 64 ? 4 : 6) : f.lanes ? 8 : 4);
+}
+
+// A workgroup of the gradient has a part of the sums over rows.
 int32_t gradient_parts(const hwsel_join_t &j)
 {
-    const int64_t most = (int64_t)compute_units() * (j.cols <= 4096 ? kBackwardGroups : 1), need = (j.rows + rows_at_once(j.cols) - 1) / rows_at_once(j.cols);
-    return (int32_t)(need < most ? need : most);
+    const Shape f = shape_of(j.cols);
+    return groups_of(f, j.rows, f.K == 1 && !f.lanes ? 4 : 2);
+}
+
+// go<LANES, K>() of a shape.
+template <class F>
+void by_shape(const Shape &f, F &&go)
+{
+    if (f.lanes == 8) go.template operator()<8, 1>();
+    else if (f.lanes == 16) go.template operator()<16, 1>();
+    else if (f.lanes == 32) go.template operator()<32, 1>();
+    else if (f.lanes == 64) f.K == 1 ? go.template operator()<64, 1>() : go.template operator()<64, 2>();
+    else f.K == 1 ? go.template operator()<0, 1>() : go.template operator()<0, 2>();
 }
 
 // Of rows that are too long, the columns' pass has its rows in this many parts.
@@ -682,13 +784,11 @@ hipError_t launch_block_join(const hwsel_join_t &j, const hwsel_matrix_t &x, con
             each_row_span(a.c, [&](unsigned n) { hipLaunchKernelGGL((k_join_long<SBF, BBF>), dim3(n), dim3(kLong), 0, s, a); });
             return;
         }
-        auto go = [&]<int LANES, int K>() {
-            constexpr int kThreads = threads_of(LANES), kRows = kThreads / LANES;
-            const int64_t need = (j.rows + kRows - 1) / kRows, most = (int64_t)compute_units() * kForwardGroups;
-            hipLaunchKernelGGL((k_join<SBF, BBF, LANES, K>), dim3((unsigned)(need < most ? need : most)), dim3(kThreads), 0, s, a);
-        };
-        if (j.cols > 8192) go.template operator()<1024, 2>();
-        else by_length(j.cols, go);
+        const Shape f = shape_of(j.cols);
+        by_shape(f, [&]<int LANES, int K>() {
+            const auto kernel = j.cols % 8 ? k_join<SBF, BBF, LANES, K, true> : k_join<SBF, BBF, LANES, K, false>;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)forward_groups(j)), dim3(f.threads), 0, s, a);
+        });
     });
     return hipGetLastError();
 }
@@ -703,8 +803,10 @@ hipError_t launch_block_join_gradient(const hwsel_join_t &j, const hwsel_matrix_
     if (j.cols <= kLongestBackward) {
         a.n_parts = gradient_parts(j);
         by_types(sbf, bbf, [&]<bool SBF, bool BBF>() {
-            by_length(j.cols, [&]<int LANES, int K>() {
-                hipLaunchKernelGGL((k_join_gradient<SBF, BBF, LANES, K>), dim3((unsigned)a.n_parts), dim3(threads_of(LANES)), 0, s, a);
+            const Shape f = shape_of(j.cols);
+            by_shape(f, [&]<int LANES, int K>() {
+                const auto kernel = j.cols % 8 ? k_join_gradient<SBF, BBF, LANES, K, true> : k_join_gradient<SBF, BBF, LANES, K, false>;
+                hipLaunchKernelGGL(kernel, dim3((unsigned)a.n_parts), dim3(f.threads), 0, s, a);
             });
         });
     } else {
@@ -719,7 +821,7 @@ hipError_t launch_block_join_gradient(const hwsel_join_t &j, const hwsel_matrix_
         });
     }
     if (dwb || dwp)
-        hipLaunchKernelGGL(k_join_sums, dim3((unsigned)((j.cols + kSumCols - 1) / kSumCols), 2), dim3(kTile), 0, s, a.parts, a.n_parts, j.cols, dwb, dwp);
+        hipLaunchKernelGGL(k_join_sums, dim3((unsigned)((j.cols + kSumCols - 1) / kSumCols), 2), dim3(kSumThreads), 0, s, a.parts, a.n_parts, j.cols, dwb, dwp);
     return hipGetLastError();
 }
 

@@ -22,23 +22,53 @@ struct Eight<false> {
     __device__ __forceinline__ float at(int i) const { return i < 4 ? a[i & 3] : b[i & 3]; }
 };
 
-// Elements at .. at + 7 of X, zeros from the n-th on (n >= 8: all; n <= 0: none is read).
-template <bool BF16>
-__device__ __forceinline__ Eight<BF16> load8(const void *X, int64_t at, int64_t n)
+typedef float f32x2_any_t __attribute__((ext_vector_type(2), aligned(4)));
+typedef uint32_t u32_any_t __attribute__((aligned(2)));
+
+// How rows of some length are read eight elements at a time.  The last ones of
+// a row that is no whole number of eights are read with those before them, as
+// one load like all others, and moved down once they are there: loads wait for
+// nothing and go the same way in every thread.  (The last ones as four, two and
+// one, with waits in between, 30,000 rows of 1,100 took 229 us.)
+struct Ends {
+    int32_t tail, shift;                                    // elements past the last whole eight; places they are moved
+    bool narrow;                                            // rows of less than eight
+};
+
+// Rows of whole eights, known when a kernel is compiled.
+struct NoEnds {
+    static constexpr int32_t tail = 0, shift = 0;
+    static constexpr bool narrow = false;
+};
+
+inline Ends ends_of(int64_t cols)
 {
-    Eight<BF16> v;
-    if (n >= 8) {
-        if constexpr (BF16) {
-            v.w = *reinterpret_cast<const u32x4_any_t *>(static_cast<const uint16_t *>(X) + at);
-        } else {
-            const f32x4_any_t *p = reinterpret_cast<const f32x4_any_t *>(static_cast<const float *>(X) + at);
-            v.a = p[0];
-            v.b = p[1];
+    const int32_t tail = (int32_t)(cols & 7);
+    return {tail, cols > 8 && tail ? 8 - tail : 0, cols < 8};
+}
+
+typedef float f32x2_any_t __attribute__((ext_vector_type(2), aligned(4)));
+typedef uint32_t u32_any_t __attribute__((aligned(2)));
+
+// Elements at .. of X, n of them left in the row (none is read where n <= 0: zeros); settle8 comes before their use.
+template <bool BF16, class E>
+__device__ __forceinline__ Eight<BF16> load8(const void *X, int64_t at, int32_t n, const E &ends)
+{
+    Eight<BF16> v{};
+    if (!ends.narrow) {
+        if (n > 0) {
+            if (ends.shift != 0) at += n < 8 ? n - 8 : 0;
+            if constexpr (BF16) {
+                v.w = *reinterpret_cast<const u32x4_any_t *>(static_cast<const uint16_t *>(X) + at);
+            } else {
+                v.a = *reinterpret_cast<const f32x4_any_t *>(static_cast<const float *>(X) + at);
+                v.b = *reinterpret_cast<const f32x4_any_t *>(static_cast<const float *>(X) + at + 4);
+            }
         }
         return v;
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 7; ++i) {
         if constexpr (BF16) {
             const uint32_t e = i < n ? static_cast<const uint16_t *>(X)[at + i] : 0u;
             v.w[i >> 1] = i & 1 ? v.w[i >> 1] | (e << 16) : e;
@@ -51,27 +81,75 @@ __device__ __forceinline__ Eight<BF16> load8(const void *X, int64_t at, int64_t 
     return v;
 }
 
-// The first n of eight values to elements at .. of X, rounded to nearest even.
-template <bool BF16>
-__device__ __forceinline__ void store8(void *X, int64_t at, int64_t n, const float (&v)[8])
+// A row's last elements to their places, zeros behind them (ends.shift is the same for all threads).
+template <bool BF16, class E>
+__device__ __forceinline__ void settle8(Eight<BF16> &v, int32_t n, const E &ends)
 {
-    if (n >= 8) {
-        if constexpr (BF16) {
-            *reinterpret_cast<u32x4_any_t *>(static_cast<uint16_t *>(X) + at) =
-                (u32x4_any_t){bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
-        } else {
-            f32x4_any_t *p = reinterpret_cast<f32x4_any_t *>(static_cast<float *>(X) + at);
-            p[0] = (f32x4_any_t){v[0], v[1], v[2], v[3]};
-            p[1] = (f32x4_any_t){v[4], v[5], v[6], v[7]};
-        }
-        return;
-    }
+    if (ends.shift == 0) return;
+    const bool mine = n > 0 && n < 8;
+    if constexpr (BF16) {
+        uint32_t w[5] = {v.w[0], v.w[1], v.w[2], v.w[3], 0u};
+        if (ends.shift & 4) w[0] = w[2], w[1] = w[3], w[2] = 0u, w[3] = 0u;
+        if (ends.shift & 2) w[0] = w[1], w[1] = w[2], w[2] = w[3], w[3] = 0u;
+        if (ends.shift & 1) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (i < n) {
-            if constexpr (BF16) static_cast<uint16_t *>(X)[at + i] = (uint16_t)bf16_pair(v[i], 0.0f);
-            else static_cast<float *>(X)[at + i] = v[i];
+            for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_alignbit(w[i + 1], w[i], 16);
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v.w[i] = mine ? w[i] : v.w[i];
+    } else {
+        float w[9] = {v.a.x, v.a.y, v.a.z, v.a.w, v.b.x, v.b.y, v.b.z, v.b.w, 0.0f};
+        if (ends.shift & 4) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = i < 4 ? w[i + 4] : 0.0f;
+        }
+        if (ends.shift & 2) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = i < 6 ? w[i + 2] : 0.0f;
+        }
+        if (ends.shift & 1) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = w[i + 1];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v.a[i] = mine ? w[i] : v.a[i];
+            v.b[i] = mine ? w[i + 4] : v.b[i];
+        }
+    }
+}
+
+// The first n of eight values to elements at .. of X, rounded to nearest even; a
+// row's last ones as four, two and one.
+template <bool BF16, class E>
+__device__ __forceinline__ void store8(void *X, int64_t at, int32_t n, const E &ends, const float (&v)[8])
+{
+    const int32_t tail = ends.tail;
+    const bool two = tail & 2, four = tail & 4;
+    if constexpr (BF16) {
+        uint16_t *p = static_cast<uint16_t *>(X) + at;
+        const uint32_t w[4] = {bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
+        if (n >= 8) {
+            *reinterpret_cast<u32x4_any_t *>(p) = (u32x4_any_t){w[0], w[1], w[2], w[3]};
+        } else if (n > 0) {
+            const uint32_t first = four ? w[2] : w[0], second = four ? w[3] : w[1];
+            if (four) *reinterpret_cast<u32x2_any_t *>(p) = (u32x2_any_t){w[0], w[1]};
+            if (two) *reinterpret_cast<u32_any_t *>(p + (tail & 4)) = first;
+            if (tail & 1) p[tail & 6] = (uint16_t)(two ? second : first);
+        }
+    } else {
+        float *p = static_cast<float *>(X) + at;
+        const f32x4_any_t a = {v[0], v[1], v[2], v[3]}, b = {v[4], v[5], v[6], v[7]};
+        if (n >= 8) {
+            *reinterpret_cast<f32x4_any_t *>(p) = a;
+            *reinterpret_cast<f32x4_any_t *>(p + 4) = b;
+        } else if (n > 0) {
+            const f32x4_any_t rest = four ? b : a;
+            if (four) *reinterpret_cast<f32x4_any_t *>(p) = a;
+            if (two) *reinterpret_cast<f32x2_any_t *>(p + (tail & 4)) = (f32x2_any_t){rest.x, rest.y};
+            if (tail & 1) p[tail & 6] = two ? rest.z : rest.x;
+        }
+    }
 }
 
 template <bool BF16>
