@@ -4,8 +4,6 @@
 // With d = d_x1 + r1 (dn - xn mean(dn xn)), dn = d_z w_pre, xn = x1 r1:
 //   dx = stream d;  dv = dropout(branch d);  dg = dv u;  du = dv g;  dw_branch = sum du yn;
 //   dy = r (dn' - yn mean(dn' yn)), dn' = du w_branch;  dw_pre = sum d_z xn
-#include <type_traits>
-
 #include "rows.hpp"
 
 namespace hwsel {
@@ -106,9 +104,9 @@ struct Stream8 {
     template <class E>
     __device__ __forceinline__ void load(const Backward &a, int64_t row, int32_t col, int32_t n, const E &ends)
     {
-        x1 = load8<SBF>(a.x1.p, row * a.x1.ld + col, a.dz.p ? n : 0, ends);   // (of no use without d_z)
-        dx1 = load8<SBF>(a.dx1.p, row * a.dx1.ld + col, a.dx1.p ? n : 0, ends);
-        dz = load8<BBF>(a.dz.p, row * a.dz.ld + col, a.dz.p ? n : 0, ends);
+        x1 = load8<SBF>(a.dz.p ? a.x1.p : nullptr, row * a.x1.ld + col, n, ends);   // (of no use without d_z)
+        dx1 = load8<SBF>(a.dx1.p, row * a.dx1.ld + col, n, ends);
+        dz = load8<BBF>(a.dz.p, row * a.dz.ld + col, n, ends);
     }
     template <class E>
     __device__ __forceinline__ void settle(int32_t n, const E &ends)
@@ -185,11 +183,21 @@ __device__ __forceinline__ void lane_sums(float (&v)[N], Shared &sh, int &turn)
 // Rows that fit the registers of LANES threads, 8 K columns each: a row is read
 // once and written once.  Threads keep their columns from row to row.
 // ---------------------------------------------------------------------------
-template <bool EDGE>
-__device__ __forceinline__ std::conditional_t<EDGE, Ends, NoEnds> ends_in(const Common &c)
+// How a thread's k-th eight of K is read: but for the last all are there.
+template <bool EDGE, int K, int k>
+__device__ __forceinline__ auto ends_of_eight(const Common &c)
 {
-    if constexpr (EDGE) return c.ends;
-    else return {};
+    if constexpr (k < K - 1) return AllThere{};
+    else if constexpr (EDGE) return c.ends;
+    else return NoEnds{};
+}
+
+// f(k, ends) for a thread's K eights.
+template <bool EDGE, int K, class F>
+__device__ __forceinline__ void each_eight(const Common &c, F &&f)
+{
+    if constexpr (K == 2) f(0, ends_of_eight<EDGE, K, 0>(c));
+    f(K - 1, ends_of_eight<EDGE, K, K - 1>(c));
 }
 
 // Rows that a workgroup has at once: of 256 threads, or one.
@@ -212,39 +220,41 @@ __device__ __forceinline__ int32_t column(int k)
     return (LANES ? threadIdx.x % (LANES ? LANES : 1) : threadIdx.x) * 8 + k * lanes * 8;
 }
 
+// Whether a thread of this wave has the last columns of rows that are no whole number of eights.
+template <int LANES, int K>
+__device__ __forceinline__ bool has_last(const Common &c)
+{
+    const int32_t n = c.cols - column<LANES>(K - 1);
+    return c.ends.shift != 0 && __ballot(n > 0 && n < 8) != 0;
+}
+
 template <bool SBF, bool BBF, int LANES, int K, bool EDGE>
 __global__ __launch_bounds__(LANES ? 256 : 1024) void k_join(Forward a)
 {
     __shared__ Shared sh;
     const Common &c = a.c;
-    const std::conditional_t<EDGE, Ends, NoEnds> ends = ends_in<EDGE>(c);
     const Mask m = mask_of(c.drop);
     auto col_of = [&](int k) { return column<LANES>(k); };
     float wb[K][8], wp[K][8];
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
+    each_eight<EDGE, K>(c, [&](int k, const auto &ends) {
         weights8(c.wb, col_of(k), c, ends, wb[k]);
         weights8(c.wp, col_of(k), c, ends, wp[k]);
-    }
+    });
+    const bool ragged = EDGE && has_last<LANES, K>(c);
     int turn = 0;
     for (int64_t row = first_row<LANES>(); row < c.rows; row += (int64_t)gridDim.x * kRows<LANES>) {
         Eight<SBF> x[K];
         Eight<BBF> y[K], g[K];
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
+        each_eight<EDGE, K>(c, [&](int k, const auto &ends) {
             const int32_t col = col_of(k), n = c.cols - col;
             x[k] = load8<SBF>(a.x.p, row * a.x.ld + col, n, ends);
-            if (a.y.p) y[k] = load8<BBF>(a.y.p, row * a.y.ld + col, n, ends);
-            if (c.gate_kind == kElementGate) g[k] = load8<BBF>(a.gate.p, row * a.gate.ld + col, n, ends);
-        }
-        if (ends.shift != 0) {
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                const int32_t n = c.cols - col_of(k);
-                settle8(x[k], n, ends);
-                if (a.y.p) settle8(y[k], n, ends);
-                if (c.gate_kind == kElementGate) settle8(g[k], n, ends);
-            }
+            y[k] = load8<BBF>(a.y.p, row * a.y.ld + col, n, ends);
+            g[k] = load8<BBF>(c.gate_kind == kElementGate ? a.gate.p : nullptr, row * a.gate.ld + col, n, ends);
+        });
+        if (ragged) {
+            settle8(x[K - 1], c.cols - col_of(K - 1), c.ends);
+            settle8(y[K - 1], c.cols - col_of(K - 1), c.ends);
+            if (c.gate_kind == kElementGate) settle8(g[K - 1], c.cols - col_of(K - 1), c.ends);
         }
         float x1[K][8];
         if (a.y.p) {
@@ -279,10 +289,8 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void k_join(Forward a)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x1[k][i] = c.stream * x[k].at(i);
         }
-        if (a.x1.p) {
-#pragma unroll
-            for (int k = 0; k < K; ++k) store8<SBF>(a.x1.p, row * a.x1.ld + col_of(k), c.cols - col_of(k), ends, x1[k]);
-        }
+        if (a.x1.p)
+            each_eight<EDGE, K>(c, [&](int k, const auto &ends) { store8<SBF>(a.x1.p, row * a.x1.ld + col_of(k), c.cols - col_of(k), ends, x1[k]); });
         if (a.z.p) {
             float t[1] = {0.0f};
 #pragma unroll
@@ -291,13 +299,12 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void k_join(Forward a)
                 for (int i = 0; i < 8; ++i) t[0] += col_of(k) + i < c.cols ? x1[k][i] * x1[k][i] : 0.0f;
             lane_sums<LANES>(t, sh, turn);
             const float r1 = norm_factor(t[0], c);
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
+            each_eight<EDGE, K>(c, [&](int k, const auto &ends) {
                 float z[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) z[i] = x1[k][i] * r1 * wp[k][i];
                 store8<BBF>(a.z.p, row * a.z.ld + col_of(k), c.cols - col_of(k), ends, z);
-            }
+            });
         }
     }
 }
@@ -311,34 +318,28 @@ __global__ __launch_bounds__(LANES ? 256 : 512, K == 2 ? 2 : LANES == 64 || LANE
     __shared__ Shared sh;
     __shared__ __attribute__((aligned(16))) float sums[kGroups][LANES ? LANES * 8 * K : 1];
     const Common &c = a.c;
-    const std::conditional_t<EDGE, Ends, NoEnds> ends = ends_in<EDGE>(c);
     const Mask m = mask_of(c.drop);
     auto col_of = [&](int k) { return column<LANES>(k); };
     float wb[K][8], wp[K][8], swb[K][8] = {}, swp[K][8] = {};
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
+    each_eight<EDGE, K>(c, [&](int k, const auto &ends) {
         weights8(c.wb, col_of(k), c, ends, wb[k]);
         weights8(c.wp, col_of(k), c, ends, wp[k]);
-    }
+    });
+    const bool ragged = EDGE && has_last<LANES, K>(c);
     int turn = 0;
     for (int64_t row = first_row<LANES>(); row < c.rows; row += (int64_t)gridDim.x * kRows<LANES>) {
         Stream8<SBF, BBF> q[K];
         Eight<BBF> y[K], g[K];
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
+        each_eight<EDGE, K>(c, [&](int k, const auto &ends) {
             const int32_t col = col_of(k), n = c.cols - col;
             q[k].load(a, row, col, n, ends);
-            y[k] = load8<BBF>(a.y.p, row * a.y.ld + col, a.y.p ? n : 0, ends);
-            g[k] = load8<BBF>(a.gate.p, row * a.gate.ld + col, c.gate_kind == kElementGate ? n : 0, ends);
-        }
-        if (ends.shift != 0) {
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                const int32_t n = c.cols - col_of(k);
-                q[k].settle(n, ends);
-                settle8(y[k], n, ends);
-                settle8(g[k], n, ends);
-            }
+            y[k] = load8<BBF>(a.y.p, row * a.y.ld + col, n, ends);
+            g[k] = load8<BBF>(c.gate_kind == kElementGate ? a.gate.p : nullptr, row * a.gate.ld + col, n, ends);
+        });
+        if (ragged) {
+            q[K - 1].settle(c.cols - col_of(K - 1), c.ends);
+            settle8(y[K - 1], c.cols - col_of(K - 1), c.ends);
+            if (c.gate_kind == kElementGate) settle8(g[K - 1], c.cols - col_of(K - 1), c.ends);
         }
         float s[3] = {};
 #pragma unroll
@@ -352,8 +353,7 @@ __global__ __launch_bounds__(LANES ? 256 : 512, K == 2 ? 2 : LANES == 64 || LANE
         lane_sums<LANES>(s, sh, turn);
         const float r1 = a.dz.p ? norm_factor(s[0], c) : 0.0f, m1 = r1 * s[1] * c.inv_cols;
         float d[K][8];
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
+        each_eight<EDGE, K>(c, [&](int k, const auto &ends) {
             float o[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -362,14 +362,13 @@ __global__ __launch_bounds__(LANES ? 256 : 512, K == 2 ? 2 : LANES == 64 || LANE
                 o[i] = c.stream * d[k][i];
             }
             if (a.dx.p) store8<SBF>(a.dx.p, row * a.dx.ld + col_of(k), c.cols - col_of(k), ends, o);
-        }
+        });
         if (!a.y.p) continue;
         const float r = c.post_norm ? norm_factor(s[2], c) : 1.0f;
         const float gate = c.gate_kind == kRowGate ? load1<BBF>(a.gate.p, row * a.gate.ld) : 1.0f;
         const float row_gate = c.gate_kind == kRowGate ? gate_value(gate, c.sigmoid) : 1.0f;
         float t[2] = {};                                    // of dn' yn; of dv u, the gradient of a row's gate
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
+        each_eight<EDGE, K>(c, [&](int k, const auto &ends) {
             float dv[8], dg[8];
             branch8(c, m, row, col_of(k), d[k], dv);
 #pragma unroll
@@ -387,17 +386,16 @@ __global__ __launch_bounds__(LANES ? 256 : 512, K == 2 ? 2 : LANES == 64 || LANE
                 for (int i = 0; i < 8; ++i) dg[i] *= gate_slope(g[k].at(i), c.sigmoid);
                 store8<BBF>(a.dgate.p, row * a.dgate.ld + col_of(k), c.cols - col_of(k), ends, dg);
             }
-        }
+        });
         if (c.post_norm || c.gate_kind == kRowGate) lane_sums<LANES>(t, sh, turn);
         const float mean = c.post_norm ? t[0] * c.inv_cols : 0.0f;
         if (a.dy.p) {
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
+            each_eight<EDGE, K>(c, [&](int k, const auto &ends) {
                 float o[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) o[i] = r * (d[k][i] - y[k].at(i) * r * mean);
                 store8<BBF>(a.dy.p, row * a.dy.ld + col_of(k), c.cols - col_of(k), ends, o);
-            }
+            });
         }
         if (col_of(0) == 0 && a.dgate.p && c.gate_kind == kRowGate) {
             const float dg = t[1] * gate_slope(gate, c.sigmoid);
@@ -409,8 +407,7 @@ __global__ __launch_bounds__(LANES ? 256 : 512, K == 2 ? 2 : LANES == 64 || LANE
     auto hand_on = [&](float (&v)[K][8], float *to) {
         if constexpr (kGroups > 1) {
             __syncthreads();
-#pragma unroll
-            for (int k = 0; k < K; ++k) store8<false>(&sums[threadIdx.x / LANES][0], col_of(k), 8, ends, v[k]);
+            each_eight<EDGE, K>(c, [&](int k, const auto &ends) { store8<false>(&sums[threadIdx.x / LANES][0], col_of(k), 8, ends, v[k]); });
             __syncthreads();
             for (int col = threadIdx.x; col < LANES * 8 * K && col < c.cols; col += 256) {
                 float t = sums[0][col];
@@ -419,8 +416,7 @@ __global__ __launch_bounds__(LANES ? 256 : 512, K == 2 ? 2 : LANES == 64 || LANE
                 to[col] = t;
             }
         } else {
-#pragma unroll
-            for (int k = 0; k < K; ++k) store8<false>(to, col_of(k), c.cols - col_of(k), ends, v[k]);
+            each_eight<EDGE, K>(c, [&](int k, const auto &ends) { store8<false>(to, col_of(k), c.cols - col_of(k), ends, v[k]); });
         }
     };
     if (a.want_wb) hand_on(swb, part);
@@ -549,7 +545,7 @@ __global__ __launch_bounds__(kLong) void k_join_long_stats(Backward a)
             q.settle(n, ends);
             Eight<BBF> y = load8<BBF>(a.y.p, row * a.y.ld + col, n, ends);
             settle8(y, n, ends);
-            Eight<BBF> g = load8<BBF>(a.gate.p, row * a.gate.ld + col, c.gate_kind == kElementGate ? n : 0, ends);
+            Eight<BBF> g = load8<BBF>(c.gate_kind == kElementGate ? a.gate.p : nullptr, row * a.gate.ld + col, n, ends);
             settle8(g, n, ends);
             float wp[8], wb[8], d[8], dv[8];
             weights8(c.wp, col, c, ends, wp);
@@ -608,9 +604,9 @@ __global__ __launch_bounds__(kTile) void k_join_long_columns(Backward a)
             swp[i] += q.dz.at(i) * (q.x1.at(i) * r1);
             o[i] = c.stream * d[i];
         }
-        Eight<BBF> y = load8<BBF>(a.y.p, row * a.y.ld + col, a.y.p ? n : 0, ends);
+        Eight<BBF> y = load8<BBF>(a.y.p, row * a.y.ld + col, n, ends);
         settle8(y, n, ends);
-        Eight<BBF> g = load8<BBF>(a.gate.p, row * a.gate.ld + col, c.gate_kind == kElementGate ? n : 0, ends);
+        Eight<BBF> g = load8<BBF>(c.gate_kind == kElementGate ? a.gate.p : nullptr, row * a.gate.ld + col, n, ends);
         settle8(g, n, ends);
         if (a.dx.p) store8<SBF>(a.dx.p, row * a.dx.ld + col, n, ends, o);
         if (!a.y.p) continue;

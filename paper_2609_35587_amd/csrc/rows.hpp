@@ -2,6 +2,8 @@
 // and sums over lanes: shared by dropout.hip and join.hip.
 #pragma once
 
+#include <type_traits>
+
 #include "fp8.hpp"
 
 namespace hwsel {
@@ -35,11 +37,13 @@ struct Ends {
     bool narrow;                                            // rows of less than eight
 };
 
-// Rows of whole eights, known when a kernel is compiled.
+// Rows of whole eights, and eights that every thread has, known when a kernel is compiled.
 struct NoEnds {
     static constexpr int32_t tail = 0, shift = 0;
     static constexpr bool narrow = false;
 };
+
+struct AllThere : NoEnds {};
 
 inline Ends ends_of(int64_t cols)
 {
@@ -50,13 +54,14 @@ inline Ends ends_of(int64_t cols)
 typedef float f32x2_any_t __attribute__((ext_vector_type(2), aligned(4)));
 typedef uint32_t u32_any_t __attribute__((aligned(2)));
 
-// Elements at .. of X, n of them left in the row (none is read where n <= 0: zeros); settle8 comes before their use.
+// Elements at .. of X, n of them left in the row (zeros where n <= 0 or there is no X: none is read); settle8 comes
+// before their use.
 template <bool BF16, class E>
 __device__ __forceinline__ Eight<BF16> load8(const void *X, int64_t at, int32_t n, const E &ends)
 {
     Eight<BF16> v{};
     if (!ends.narrow) {
-        if (n > 0) {
+        if (X && (std::is_same_v<E, AllThere> || n > 0)) {
             if (ends.shift != 0) at += n < 8 ? n - 8 : 0;
             if constexpr (BF16) {
                 v.w = *reinterpret_cast<const u32x4_any_t *>(static_cast<const uint16_t *>(X) + at);
@@ -70,10 +75,10 @@ __device__ __forceinline__ Eight<BF16> load8(const void *X, int64_t at, int32_t 
 #pragma unroll
     for (int i = 0; i < 7; ++i) {
         if constexpr (BF16) {
-            const uint32_t e = i < n ? static_cast<const uint16_t *>(X)[at + i] : 0u;
+            const uint32_t e = X && i < n ? static_cast<const uint16_t *>(X)[at + i] : 0u;
             v.w[i >> 1] = i & 1 ? v.w[i >> 1] | (e << 16) : e;
         } else {
-            const float e = i < n ? static_cast<const float *>(X)[at + i] : 0.0f;
+            const float e = X && i < n ? static_cast<const float *>(X)[at + i] : 0.0f;
             if (i < 4) v.a[i & 3] = e;
             else v.b[i & 3] = e;
         }
@@ -129,7 +134,7 @@ __device__ __forceinline__ void store8(void *X, int64_t at, int32_t n, const E &
     if constexpr (BF16) {
         uint16_t *p = static_cast<uint16_t *>(X) + at;
         const uint32_t w[4] = {bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
-        if (n >= 8) {
+        if (std::is_same_v<E, AllThere> || n >= 8) {
             *reinterpret_cast<u32x4_any_t *>(p) = (u32x4_any_t){w[0], w[1], w[2], w[3]};
         } else if (n > 0) {
             const uint32_t first = four ? w[2] : w[0], second = four ? w[3] : w[1];
@@ -140,7 +145,7 @@ __device__ __forceinline__ void store8(void *X, int64_t at, int32_t n, const E &
     } else {
         float *p = static_cast<float *>(X) + at;
         const f32x4_any_t a = {v[0], v[1], v[2], v[3]}, b = {v[4], v[5], v[6], v[7]};
-        if (n >= 8) {
+        if (std::is_same_v<E, AllThere> || n >= 8) {
             *reinterpret_cast<f32x4_any_t *>(p) = a;
             *reinterpret_cast<f32x4_any_t *>(p + 4) = b;
         } else if (n > 0) {
