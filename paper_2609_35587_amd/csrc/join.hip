@@ -736,7 +736,7 @@ int32_t groups_of(const Shape &f, int64_t rows, int waves)
 int32_t forward_groups(const hwsel_join_t &j)
 {
     const Shape f = shape_of(j.cols);
-    return groups_of(f, j.rows, f.K == 1 ? (f.lanes && f.lanes < 64 ? 4 : 6) : f.lanes ? 8 : 4);
+    return groups_of(f, j.rows, f.K == 1 && (f.lanes == 64 || f.lanes == 0) ? 6 : 4);
 }
 
 // A workgroup of the gradient has a part of the sums over rows.
