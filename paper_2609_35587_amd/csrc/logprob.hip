@@ -216,9 +216,8 @@ __device__ __forceinline__ void write_problem(const LogprobArgs &a, const Proble
     }
     for (int32_t r = t; r < a.top; r += N) {
         const uint64_t k = keys[r];
-        const uint32_t b = (uint32_t)(k >> 32);
         const int32_t j = (int32_t)(0xffffffffu - (uint32_t)k);
-        const float s = b & 0x80000000u ? __uint_as_float(b ^ 0x80000000u) : __uint_as_float(~b);   // (NaN for key 0)
+        const float s = desc_value((uint32_t)(k >> 32));    // (NaN for key 0)
         const float lp = log_probability(q, z, j, s);
         a.top_idx[(int64_t)p * a.top + r] = lp > kNone ? j : -1;
         a.top_logp[(int64_t)p * a.top + r] = lp;
@@ -259,23 +258,103 @@ struct Lds {
     TopkLds<NT> topk;
     uint64_t keys[64];
     Mass part[NT / 64];
-    int32_t first;
+    uint32_t best[NT / 64][64];                             // each thread's best score, as ordered bits
+    int32_t first, n_list;
 };
 
+constexpr uint32_t kLeastBits = 0x00800000u;                // of the least finite score; below them are -inf and NaN
+
+// The best `top` of n scores, read once more: a score is listed if it is not below what the best scores of `top`
+// threads reach (of 256 threads, or of 64 groups of them; more are taken together), and the listed ones are ranked by counting the larger.  False, and nothing
+// written, if they do not fit the list.  (A problem's length of registers for tiles and the rounds of a bound by
+// waves instead: 600 of up to 8,192 scores, 10 of each, 13.7 us, @@.)
+template <int NT>
+__device__ __forceinline__ bool list_best(const float *s, int32_t n, int32_t top, Lds<NT> &lds)
+{
+    const int lane = threadIdx.x & 63;
+    uint32_t best[4] = {}, bits = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) best[w & 3] = lds.best[w][lane] > best[w & 3] ? lds.best[w][lane] : best[w & 3];
+    const bool few = top <= 16;                             // 64 are enough: a quarter of the comparisons
+    if (few) {
+#pragma unroll
+        for (int w = 1; w < 4; ++w) best[0] = best[w] > best[0] ? best[w] : best[0];
+    }
+    for (int b = 31; b >= 0; --b) {                         // (every wave for itself)
+        int32_t c = (int32_t)__popcll(__ballot(best[0] >= (bits | 1u << b)));
+        if (!few) {
+#pragma unroll
+            for (int w = 1; w < 4; ++w) c += (int32_t)__popcll(__ballot(best[w] >= (bits | 1u << b)));
+        }
+        if (c >= top) bits |= 1u << b;
+        if (c == top) break;
+    }
+    const float least = bits > kLeastBits ? desc_value(bits) : -3.4028235e38f;
+    constexpr int kStep = 16 * NT;
+    for (int32_t at = 0; at < n; at += kStep) {
+        f32x4u_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = load4(s + at, (i * NT + (int)threadIdx.x) * 4, n - at);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float v = w[i >> 2][i & 3];
+            const bool in = v >= least;
+            const uint64_t take = __ballot(in);
+            if (take == 0) continue;
+            int32_t to = 0;
+            if (lane == 0) to = atomicAdd(&lds.n_list, __popcll(take));
+            to = __builtin_amdgcn_readfirstlane(to) +
+                 (int32_t)__builtin_amdgcn_mbcnt_hi((uint32_t)(take >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)take, 0u));
+            const uint32_t j = (uint32_t)(at + ((i >> 2) * NT + (int)threadIdx.x) * 4 + (i & 3));
+            if (in && to < kList) lds.topk.cand[to] = ((uint64_t)order_key(v + 0.0f) << 32) | (0xffffffffu - j);
+        }
+    }
+    __syncthreads();
+    const int32_t m = lds.n_list;
+    if (m > kList) return false;
+    for (int32_t i = threadIdx.x; i < m; i += NT) {
+        const uint64_t own = lds.topk.cand[i];
+        int32_t rank = 0;
+#pragma unroll 8
+        for (int32_t e = 0; e < m; ++e) rank += lds.topk.cand[e] > own;
+        if (rank < top) lds.keys[rank] = own;
+    }
+    __syncthreads();
+    return true;
+}
+
+// Up to this many scores are read twice, from the caches the second time, longer problems once.
+constexpr int32_t kTwice = 16384;
+
 // The sums and best candidates of n scores by a workgroup; first: of a cold problem its best candidate (else -1).
-template <int NT, int TILE, bool TOP>
+template <int NT, int TILE, bool TOP, bool TWICE = true>
 __device__ __forceinline__ Mass block_scores(const float *s, int32_t n, int32_t top, bool cold, float rate, Lds<NT> &lds, int32_t &first)
 {
     first = -1;
-    Mass m = kNothing;
     if constexpr (TOP) {
-        topk_tiles<NT, TILE>(
-            s, n, top, lds.topk, [&](const auto &bits) { take_tile(m, bits, rate); },
-            [&](int32_t j, uint64_t key) { lds.keys[j] = key; });
-        m = block_mass<NT>(m, rate, lds.part);              // (its barrier: the keys are there)
+        Mass m = kNothing;
+        bool listed = false;
+        if (TWICE && n <= kTwice) {
+            m = take_all<NT>(s, n, rate);
+            lds.best[threadIdx.x >> 6][threadIdx.x & 63] = m.best > kNone ? order_key(m.best + 0.0f) : 0u;
+            if (threadIdx.x < 64) lds.keys[threadIdx.x] = 0;
+            if (threadIdx.x == 0) lds.n_list = 0;
+            m = block_mass<NT>(m, rate, lds.part);          // (its barrier)
+            listed = list_best<NT>(s, n, top, lds);
+            if (!listed) {                                  // many scores are one: by tiles
+                __syncthreads();
+                topk_tiles<NT, TILE>(s, n, top, lds.topk, [](const auto &) {}, [&](int32_t j, uint64_t key) { lds.keys[j] = key; });
+                __syncthreads();
+            }
+        } else {
+            topk_tiles<NT, TILE>(
+                s, n, top, lds.topk, [&](const auto &bits) { take_tile(m, bits, rate); }, [&](int32_t j, uint64_t key) { lds.keys[j] = key; });
+            m = block_mass<NT>(m, rate, lds.part);          // (its barrier: the keys are there)
+        }
         if (cold) first = (int32_t)(0xffffffffu - (uint32_t)lds.keys[0]);
+        return m;
     } else {
-        m = block_mass<NT>(take_all<NT>(s, n, rate), rate, lds.part);
+        const Mass m = block_mass<NT>(take_all<NT>(s, n, rate), rate, lds.part);
         if (cold) {
             if (threadIdx.x == 0) lds.first = 0x7fffffff;
             __syncthreads();
@@ -287,19 +366,19 @@ __device__ __forceinline__ Mass block_scores(const float *s, int32_t n, int32_t 
             __syncthreads();
             first = lds.first;
         }
+        return m;
     }
-    return m;
 }
 
 // A workgroup has a problem.
-template <int NT, int TILE, bool TOP>
+template <int NT, int TILE, bool TOP, bool TWICE = true>
 __device__ __forceinline__ void block_problem(const LogprobArgs &a, int32_t p, Lds<NT> &lds)
 {
     const Problem q = problem_of(a, p);
     const Pick pick = pick_of(a, q, p, threadIdx.x);
     const float rate = kLog2e / q.T;
     int32_t first;
-    const Mass m = block_scores<NT, TILE, TOP>(q.s, q.n, a.top, q.cold, rate, lds, first);
+    const Mass m = block_scores<NT, TILE, TOP, TWICE>(q.s, q.n, a.top, q.cold, rate, lds, first);
     write_problem<NT>(a, q, p, norm_of(m, q, first), threadIdx.x, pick, lds.keys);
 }
 
@@ -403,7 +482,7 @@ __global__ __launch_bounds__(kThreads) void k_logprob_waves(LogprobArgs a)
     }
     for (int32_t i = 0; i < kWaves && p0 + i < a.P; ++i) {
         if (problem_of(a, p0 + i).n <= kSmall) continue;     // (one answer for the workgroup)
-        block_problem<kThreads, 2048, TOP>(a, p0 + i, lds);
+        block_problem<kThreads, 2048, TOP, false>(a, p0 + i, lds);
         __syncthreads();
     }
 }
@@ -810,8 +889,7 @@ hipError_t launch_logprob(const float *scores, int64_t R, const int64_t *seg, in
         } else {
             each_span(P, [&](int32_t p0, int32_t n) {
                 a.p0 = p0;
-                if (mean <= 2048) hipLaunchKernelGGL((k_logprob<256, 2048, TOP>), dim3(n), dim3(256), 0, s, a);
-                else if (mean <= 8192) hipLaunchKernelGGL((k_logprob<256, 4096, TOP>), dim3(n), dim3(256), 0, s, a);
+                if (mean <= 8192) hipLaunchKernelGGL((k_logprob<256, 2048, TOP>), dim3(n), dim3(256), 0, s, a);
                 else hipLaunchKernelGGL((k_logprob<512, kTile, TOP>), dim3(n), dim3(512), 0, s, a);
             });
         }

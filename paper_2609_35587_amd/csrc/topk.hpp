@@ -31,6 +31,9 @@ constexpr int kTile = 8192;
 // Larger key = better score.  NaN ranks lowest, -0 equals +0 (the sum makes it that).
 __device__ __forceinline__ uint32_t desc_bits(float s) { return s != s ? 0u : order_key(s + 0.0f); }
 
+// The score that has these bits (a NaN for 0).
+__device__ __forceinline__ float desc_value(uint32_t b) { return __uint_as_float(b & 0x80000000u ? b ^ 0x80000000u : ~b); }
+
 template <int CTRL, int ROW_MASK, bool ZERO_FILL>
 __device__ __forceinline__ uint32_t dpp_max_u32(uint32_t v)
 {
