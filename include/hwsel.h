@@ -708,7 +708,7 @@ int hwsel_logprob_per_problem(const float *scores, int64_t R, const int64_t *seg
  * matter.  Candidates without probability, problems with T <= 0 or NaN and rows of no
  * problem get 0.  A d_logp or d_entropy that is not finite makes its
  * problem's gradients not finite.
- *   d_scores fp32 [R]; picks, d_logp NULL where n_picks is 0; entropy and
+ *   d_scores fp32 [R], not the scores themselves; picks, d_logp NULL where n_picks is 0; entropy and
  *   d_entropy (fp32 [P]) both NULL or both given; norm as written.
  * Returns HWSEL_EINVAL for null pointers, P < 1, R < 0, n_picks < 0;
  * HWSEL_EUNSUPPORTED for R > 2^30.

@@ -717,6 +717,14 @@ static int check_matrix(const hwsel_matrix_t &m, const char *name, int64_t cols,
     return HWSEL_OK;
 }
 
+// A result in the place of an operand lies as that does.
+static int check_in_place(const hwsel_matrix_t &out, const hwsel_matrix_t &in, const char *name, const char *fn)
+{
+    if (out.data && out.data == in.data && (out.ld != in.ld || out.dtype != in.dtype))
+        return fail(HWSEL_EINVAL, fn, "%s in place, with another ld or dtype", name);
+    return HWSEL_OK;
+}
+
 static int check_dropout(const hwsel_dropout_t &d, const char *fn)
 {
     if (!(d.p >= 0.0f && d.p <= 1.0f)) return fail(HWSEL_EINVAL, fn, "p=%g (0..1)", (double)d.p);
@@ -734,6 +742,8 @@ int hwsel_dropout(const hwsel_dropout_t *how, int64_t rows, int64_t cols, const 
     if (int st = check_matrix(*X, "X", cols, -1, fn)) return st;
     if (int st = check_matrix(*Y, "Y", cols, -1, fn)) return st;
     if (int st = check_matrix(or_none(residual), "residual", cols, Y->dtype, fn)) return st;
+    if (int st = check_in_place(*Y, *X, "Y", fn)) return st;
+    if (int st = check_in_place(*Y, or_none(residual), "Y", fn)) return st;
     return launched(hwsel::launch_dropout(*how, rows, cols, *X, or_none(residual), *Y, (hipStream_t)stream), fn);
 }
 
@@ -775,6 +785,7 @@ int hwsel_block_join(const hwsel_join_t *j, const hwsel_matrix_t *x, const hwsel
     if (int st = check_matrix(gate, "gate", j->gate_cols, block, fn)) return st;
     if (int st = check_matrix(x1, "x1", j->cols, x->dtype, fn)) return st;
     if (int st = check_matrix(z, "z", j->cols, block, fn)) return st;
+    if (int st = check_in_place(x1, *x, "x1", fn)) return st;
     const bool bbf = (y.data ? y.dtype : z.dtype) == HWSEL_DTYPE_BF16;
     return launched(hwsel::launch_block_join(*j, *x, y, gate, x1, z, x->dtype == HWSEL_DTYPE_BF16, bbf, (hipStream_t)stream), fn);
 }
@@ -812,6 +823,7 @@ int hwsel_block_join_gradient(const hwsel_join_t *j, const hwsel_matrix_t *x1, c
     if (int st = check_matrix(dx, "dx", j->cols, x1->dtype, fn)) return st;
     if (int st = check_matrix(dy, "dy", j->cols, block, fn)) return st;
     if (int st = check_matrix(dgate, "dgate", j->gate_cols, block, fn)) return st;
+    if (int st = check_in_place(dx, d_x1, "dx", fn)) return st;
     if (((uintptr_t)dw_branch & 3u) || ((uintptr_t)dw_pre & 3u)) return fail(HWSEL_EINVAL, fn, "weights' gradients misaligned");
     const size_t need = hwsel::join_gradient_workspace_bytes(*j);
     if (need && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need))

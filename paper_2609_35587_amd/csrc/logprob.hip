@@ -224,16 +224,6 @@ __device__ __forceinline__ void write_problem(const LogprobArgs &a, const Proble
     }
 }
 
-// The scores of a thread's rows of a tile, from their ordered bits (0, NaN's, takes no part).
-template <int N>
-__device__ __forceinline__ void take_tile(Mass &m, const uint32_t (&bits)[N], float rate)
-{
-    float v[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = __uint_as_float(bits[i] ^ (~(uint32_t)((int32_t)bits[i] >> 31) | 0x80000000u));
-    take(m, v, rate);
-}
-
 // n scores by a workgroup, 16 a thread and step.
 template <int NT>
 __device__ __forceinline__ Mass take_all(const float *s, int32_t n, float rate)
@@ -265,9 +255,10 @@ struct Lds {
 constexpr uint32_t kLeastBits = 0x00800000u;                // of the least finite score; below them are -inf and NaN
 
 // The best `top` of n scores, read once more: a score is listed if it is not below what the best scores of `top`
-// threads reach (of 256 threads, or of 64 groups of them; more are taken together), and the listed ones are ranked by counting the larger.  False, and nothing
-// written, if they do not fit the list.  (A problem's length of registers for tiles and the rounds of a bound by
-// waves instead: 600 of up to 8,192 scores, 10 of each, 13.7 us, @@.)
+// threads reach (of 256 threads, or of 64 groups of them; more are taken together), and the listed ones, few more
+// than `top`, are ranked by counting the larger.  False, and nothing written, if they do not fit the list.
+// (By tiles, each score with its key against a running bound, the sums on the way: 600 of up to 8,192 scores, 10 of
+// each, 13.7 us, 10.1 so; 256 of 65,536 with 64 of each 77 and 24; 256 of 131,072, 134 MB, 90 and 44.)
 template <int NT>
 __device__ __forceinline__ bool list_best(const float *s, int32_t n, int32_t top, Lds<NT> &lds)
 {
@@ -323,33 +314,21 @@ __device__ __forceinline__ bool list_best(const float *s, int32_t n, int32_t top
     return true;
 }
 
-// Up to this many scores are read twice, from the caches the second time, longer problems once.
-constexpr int32_t kTwice = 16384;
-
 // The sums and best candidates of n scores by a workgroup; first: of a cold problem its best candidate (else -1).
-template <int NT, int TILE, bool TOP, bool TWICE = true>
+template <int NT, int TILE, bool TOP>
 __device__ __forceinline__ Mass block_scores(const float *s, int32_t n, int32_t top, bool cold, float rate, Lds<NT> &lds, int32_t &first)
 {
     first = -1;
     if constexpr (TOP) {
-        Mass m = kNothing;
-        bool listed = false;
-        if (TWICE && n <= kTwice) {
-            m = take_all<NT>(s, n, rate);
-            lds.best[threadIdx.x >> 6][threadIdx.x & 63] = m.best > kNone ? order_key(m.best + 0.0f) : 0u;
-            if (threadIdx.x < 64) lds.keys[threadIdx.x] = 0;
-            if (threadIdx.x == 0) lds.n_list = 0;
-            m = block_mass<NT>(m, rate, lds.part);          // (its barrier)
-            listed = list_best<NT>(s, n, top, lds);
-            if (!listed) {                                  // many scores are one: by tiles
-                __syncthreads();
-                topk_tiles<NT, TILE>(s, n, top, lds.topk, [](const auto &) {}, [&](int32_t j, uint64_t key) { lds.keys[j] = key; });
-                __syncthreads();
-            }
-        } else {
-            topk_tiles<NT, TILE>(
-                s, n, top, lds.topk, [&](const auto &bits) { take_tile(m, bits, rate); }, [&](int32_t j, uint64_t key) { lds.keys[j] = key; });
-            m = block_mass<NT>(m, rate, lds.part);          // (its barrier: the keys are there)
+        Mass m = take_all<NT>(s, n, rate);
+        lds.best[threadIdx.x >> 6][threadIdx.x & 63] = m.best > kNone ? order_key(m.best + 0.0f) : 0u;
+        if (threadIdx.x < 64) lds.keys[threadIdx.x] = 0;
+        if (threadIdx.x == 0) lds.n_list = 0;
+        m = block_mass<NT>(m, rate, lds.part);              // (its barrier)
+        if (!list_best<NT>(s, n, top, lds)) {               // many scores are one: by tiles
+            __syncthreads();
+            topk_tiles<NT, TILE>(s, n, top, lds.topk, [&](int32_t j, uint64_t key) { lds.keys[j] = key; });
+            __syncthreads();
         }
         if (cold) first = (int32_t)(0xffffffffu - (uint32_t)lds.keys[0]);
         return m;
@@ -371,14 +350,14 @@ __device__ __forceinline__ Mass block_scores(const float *s, int32_t n, int32_t 
 }
 
 // A workgroup has a problem.
-template <int NT, int TILE, bool TOP, bool TWICE = true>
+template <int NT, int TILE, bool TOP>
 __device__ __forceinline__ void block_problem(const LogprobArgs &a, int32_t p, Lds<NT> &lds)
 {
     const Problem q = problem_of(a, p);
     const Pick pick = pick_of(a, q, p, threadIdx.x);
     const float rate = kLog2e / q.T;
     int32_t first;
-    const Mass m = block_scores<NT, TILE, TOP, TWICE>(q.s, q.n, a.top, q.cold, rate, lds, first);
+    const Mass m = block_scores<NT, TILE, TOP>(q.s, q.n, a.top, q.cold, rate, lds, first);
     write_problem<NT>(a, q, p, norm_of(m, q, first), threadIdx.x, pick, lds.keys);
 }
 
@@ -482,7 +461,7 @@ __global__ __launch_bounds__(kThreads) void k_logprob_waves(LogprobArgs a)
     }
     for (int32_t i = 0; i < kWaves && p0 + i < a.P; ++i) {
         if (problem_of(a, p0 + i).n <= kSmall) continue;     // (one answer for the workgroup)
-        block_problem<kThreads, 2048, TOP, false>(a, p0 + i, lds);
+        block_problem<kThreads, 2048, TOP>(a, p0 + i, lds);
         __syncthreads();
     }
 }
@@ -890,7 +869,7 @@ hipError_t launch_logprob(const float *scores, int64_t R, const int64_t *seg, in
             each_span(P, [&](int32_t p0, int32_t n) {
                 a.p0 = p0;
                 if (mean <= 8192) hipLaunchKernelGGL((k_logprob<256, 2048, TOP>), dim3(n), dim3(256), 0, s, a);
-                else hipLaunchKernelGGL((k_logprob<512, kTile, TOP>), dim3(n), dim3(512), 0, s, a);
+                else hipLaunchKernelGGL((k_logprob<512, 4096, TOP>), dim3(n), dim3(512), 0, s, a);
             });
         }
     };

@@ -31,7 +31,6 @@ __global__ __launch_bounds__(NT, 3) void k_topk(const float *__restrict__ scores
     const float *s = scores + seg[p];
     idx += (int64_t)p * k;
     if (vals) vals += (int64_t)p * k;
-    auto each = [](const auto &) {};
     auto emit = [&](int32_t j, uint64_t key) {
         const int32_t li = key ? (int32_t)(0xffffffffu - (uint32_t)key) : -1;
         idx[j] = li;
@@ -51,9 +50,9 @@ __global__ __launch_bounds__(NT, 3) void k_topk(const float *__restrict__ scores
         }
     } else if (n <= kShort) {
         if (threadIdx.x >= kShortThreads) return;
-        topk_tiles<kShortThreads, kShort>(s, n, k, lds, each, emit);
+        topk_tiles<kShortThreads, kShort>(s, n, k, lds, emit);
     } else {
-        topk_tiles<NT, kTile>(s, n, k, lds, each, emit);
+        topk_tiles<NT, kTile>(s, n, k, lds, emit);
     }
 }
 

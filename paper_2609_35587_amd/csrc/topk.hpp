@@ -107,11 +107,10 @@ struct TopkLds {
 };
 
 // The k best of one segment by NT threads, TILE rows at a time (lds: for at
-// least as many threads).  each(bits): the score bits of the thread's rows
-// of a tile (NaN's past the end), every tile once; emit(j, key): the j-th best, by one
-// thread (0: there is none).
-template <int NT, int TILE, class Lds, class Each, class Emit>
-__device__ __forceinline__ void topk_tiles(const float *__restrict__ s, int32_t n, int32_t k, Lds &lds, Each &&each, Emit &&emit)
+// least as many threads).  emit(j, key): the j-th best, by one thread (0: there
+// is none).
+template <int NT, int TILE, class Lds, class Emit>
+__device__ __forceinline__ void topk_tiles(const float *__restrict__ s, int32_t n, int32_t k, Lds &lds, Emit &&emit)
 {
     constexpr int kWaves = NT / 64, kPer = TILE / NT;       // keys per thread and tile
     auto &top = lds.top;
@@ -143,7 +142,6 @@ __device__ __forceinline__ void topk_tiles(const float *__restrict__ s, int32_t 
 #pragma unroll
         for (int q = 0; q < kPer; ++q) hi[q] = desc_bits(next[q]);
         if (t0 + TILE < (uint32_t)n) fetch(t0 + TILE);
-        each(hi);
         uint32_t most_hi = 0;                               // of the lane's largest key
 #pragma unroll
         for (int q = 0; q < kPer; ++q) most_hi = hi[q] > most_hi ? hi[q] : most_hi;

@@ -75,6 +75,17 @@ def test_dropout_rejects(L, over, status):
     assert L.hwsel_last_error().startswith(b"hwsel_dropout: ")
 
 
+def test_results_in_place_lie_as_their_operands(L):
+    """The same address with another step or type would be read where it has been written."""
+    how, m, other = hwsel.hwsel_dropout_t(1, 2, None, 0.5), mat(), 0x2000
+    call = lambda x, r, y: L.hwsel_dropout(C.byref(how), 10, 64, C.byref(x), C.byref(r), C.byref(y), None)  # noqa: E731
+    assert call(mat(ld=65), mat(other), m) == 1 and call(mat(dtype=B), mat(other), m) == 1 and call(mat(other), mat(ld=65), m) == 1
+    assert forward(L, join(), x=mat(ld=65), y=mat(other), gate=mat(other), x1=m, z=mat(other)) == 1
+    far = {n: mat(other) for n in ("x1", "y", "gate", "d_z", "dy", "dgate")}
+    assert backward(L, join(), **far, d_x1=mat(ld=65), dx=m) == 1
+    assert L.hwsel_last_error().startswith(b"hwsel_block_join_gradient: dx in place")
+
+
 def join(**over):
     a = dict(rows=10, cols=64, w_branch=FAKE, w_pre=FAKE, eps=1e-6, stream_scale=1.0, branch_scale=1.0, post_norm=1, gate_sigmoid=0,
              gate_cols=64)
