@@ -674,6 +674,16 @@ __device__ __forceinline__ void gradient_of(const GradientArgs &a, int32_t p, co
     bool fine = true;
     auto fixed = [&](float v) { return (unsigned long long)(long long)__builtin_rint(__builtin_ldexp((double)v, -e)); };
     auto value = [&](unsigned long long v) { return (float)__builtin_ldexp((double)(long long)v, e); };
+    // f(candidate, its score, gradient) for this thread's picks that count
+    auto each = [&](auto &&f) {
+        if (own_j >= 0) f(own_j, own_s, own_g);
+        for (uint32_t i = t + THREADS; i < (uint32_t)a.n_picks; i += THREADS) {
+            float v;
+            const int32_t j = counted(picks[i], v);
+            if (j >= 0) f(j, v, dl[i]);
+        }
+    };
+    auto inside = [](int32_t i) { return (uint32_t)i < (uint32_t)PART; };
     if constexpr (PICKS) {
         if (t == 0) {
             fx.most = 0;
@@ -681,32 +691,36 @@ __device__ __forceinline__ void gradient_of(const GradientArgs &a, int32_t p, co
         }
         own_j = counted(own_j, own_s);
         group_barrier<THREADS>();
-        uint32_t most = own_j >= 0 ? __float_as_uint(own_g) & 0x7fffffffu : 0u;
-        for (uint32_t i = t + THREADS; i < (uint32_t)a.n_picks; i += THREADS) {
-            float v;
-            const uint32_t b = counted(picks[i], v) >= 0 ? __float_as_uint(dl[i]) & 0x7fffffffu : 0u;
+        uint32_t most = 0;
+        each([&](int32_t j, float, float g) {
+            const uint32_t b = __float_as_uint(g) & 0x7fffffffu;
             most = b > most ? b : most;
-        }
+            if (inside(j - from)) fx.acc[j - from] = 0;
+        });
         most = wave_max_u32(most);
         if constexpr (THREADS > 64) {
             if ((threadIdx.x & 63) == 0 && most != 0) atomicMax(&fx.most, most);
-            group_barrier<THREADS>();
-            most = fx.most;
         }
+        group_barrier<THREADS>();
+        if constexpr (THREADS > 64) most = fx.most;
         fine = most < 0x7f800000u;
-        e = (int)(most >> 23) - 126 + (32 - __builtin_clz((uint32_t)a.n_picks)) - 62;
-        unsigned long long sum = fine && own_j >= 0 ? fixed(own_g) : 0ull;
-        for (uint32_t i = t + THREADS; i < (uint32_t)a.n_picks; i += THREADS) {
-            float v;
-            if (fine && counted(picks[i], v) >= 0) sum += fixed(dl[i]);
+        S = __uint_as_float(most);
+        if (fine) {                                         // (uniform)
+            e = (int)(most >> 23) - 126 + (32 - __builtin_clz((uint32_t)a.n_picks)) - 62;
+            unsigned long long sum = 0;
+            each([&](int32_t j, float, float g) {
+                const unsigned long long u = fixed(g);
+                sum += u;
+                if (inside(j - from)) atomicAdd(&fx.acc[j - from], u);
+            });
+            sum = wave_sum(sum);
+            if constexpr (THREADS > 64) {
+                if ((threadIdx.x & 63) == 0 && sum != 0) atomicAdd(&fx.total, sum);
+                group_barrier<THREADS>();
+                sum = fx.total;
+            }
+            S = value(sum);
         }
-        sum = wave_sum(sum);
-        if constexpr (THREADS > 64) {
-            if ((threadIdx.x & 63) == 0 && sum != 0) atomicAdd(&fx.total, sum);
-            group_barrier<THREADS>();
-            sum = fx.total;
-        }
-        S = fine ? value(sum) : __uint_as_float(most);
     }
     const float rate = kLog2e / q.T, by_T = fminf(1.0f / q.T, 3.4028235e38f);
     const float log2_mass = z.log_mass * kLog2e;
@@ -716,19 +730,16 @@ __device__ __forceinline__ void gradient_of(const GradientArgs &a, int32_t p, co
     auto of_entropy = [&](float pr, float lp) { return de * (pr > 0.0f ? pr * (lp + z.entropy) : 0.0f); };
     for (int32_t part = from; part < to; part += PART) {
         const int32_t n = to - part < PART ? to - part : PART;
-        auto each = [&](auto &&f) {                         // of the picks in this part that count
-            if (own_j >= part && own_j - part < n) f(own_j - part, own_s, own_g);
-            for (uint32_t i = t + THREADS; i < (uint32_t)a.n_picks; i += THREADS) {
-                float v;
-                const int32_t j = counted(picks[i], v);
-                if (j >= part && j - part < n) f(j - part, v, dl[i]);
-            }
-        };
         if constexpr (PICKS) {
-            if (fine) {                                     // (uniform)
-                each([&](int32_t i, float, float) { fx.acc[i] = 0; });
+            if (part > from && fine) {
+                group_barrier<THREADS>();                   // the last part's entries have been read
+                each([&](int32_t j, float, float) {
+                    if (inside(j - part)) fx.acc[j - part] = 0;
+                });
                 group_barrier<THREADS>();
-                each([&](int32_t i, float, float g) { atomicAdd(&fx.acc[i], fixed(g)); });
+                each([&](int32_t j, float, float g) {
+                    if (inside(j - part)) atomicAdd(&fx.acc[j - part], fixed(g));
+                });
             }
         }
         float o[kEach];
@@ -752,7 +763,9 @@ __device__ __forceinline__ void gradient_of(const GradientArgs &a, int32_t p, co
         if constexpr (PICKS) {
             if (fine) {
                 group_barrier<THREADS, true>();
-                auto again = [&](int32_t i, float v, float) {
+                each([&](int32_t j, float v, float) {
+                    const int32_t i = j - part;
+                    if (!inside(i)) return;
                     const float lt = lt_of(v), pr = __builtin_amdgcn_exp2f(lt - log2_mass), lp = lt * kLn2 - z.log_mass;
                     // g (1 - p): where p is above 0.6 by the series of 1 - exp(lp), without the difference
                     float x = 1.0f / 9.0f;
@@ -760,9 +773,7 @@ __device__ __forceinline__ void gradient_of(const GradientArgs &a, int32_t p, co
                     for (int m = 8; m >= 1; --m) x = (1.0f + lp * x) * (1.0f / (float)m);
                     const float g = value(fx.acc[i]), own = g * (lp > -0.5f ? -lp * x : 1.0f - pr);
                     d[part + i] = done(v, lt, own - pr * (S - g) - of_entropy(pr, lp));
-                };
-                each(again);
-                if (part + PART < to) group_barrier<THREADS>();   // the next part's entries
+                });
             }
         }
     }
