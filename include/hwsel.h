@@ -710,8 +710,8 @@ int hwsel_logprob_per_problem(const float *scores, int64_t R, const int64_t *seg
  * problem's gradients not finite.
  *   d_scores fp32 [R], not the scores themselves; picks, d_logp NULL where n_picks is 0; entropy and
  *   d_entropy (fp32 [P]) both NULL or both given; norm as written.
- * Returns HWSEL_EINVAL for null pointers, P < 1, R < 0, n_picks < 0;
- * HWSEL_EUNSUPPORTED for R > 2^30.
+ * Returns HWSEL_EINVAL for null pointers, P < 1, R < 0, n_picks < 0, d_scores
+ * that overlaps the scores; HWSEL_EUNSUPPORTED for R > 2^30.
  */
 int hwsel_logprob_gradient(const float *scores, int64_t R, const int64_t *seg_offsets, int32_t P, float temperature,
                            const float *temperature_of, const float *norm, const int32_t *picks, int32_t n_picks,
@@ -781,7 +781,8 @@ int hwsel_dropout(const hwsel_dropout_t *how, int64_t rows, int64_t cols, const 
  *              g = gate, or 1 / (1 + exp(-gate)) with gate_sigmoid.
  *   w_branch, w_pre  fp32 [cols] or NULL (ones).
  *   x1 or z may be none, not both.
- * x1 may be x itself (same data, ld); outputs overlap nothing else.
+ * x1 may be x itself (same data, ld); outputs overlap nothing else (the same
+ * data is refused).
  * Returns HWSEL_EINVAL for null pointers, sizes < 1, eps not > 0, scales that
  * are not finite, p outside [0, 1], bad flags, ld or alignment, dtypes that
  * differ where they are to be one; HWSEL_EUNSUPPORTED for another dtype, rows
@@ -811,7 +812,8 @@ int hwsel_block_join(const hwsel_join_t *join, const hwsel_matrix_t *x, const hw
  *   workspace  hwsel_block_join_gradient_workspace_bytes(join) bytes of
  *   device memory, 256-byte aligned (NULL where that is 0).
  * Sums over rows are fp32 in an order fixed by the sizes.  dx may be d_x1
- * itself (same data, ld); outputs overlap nothing else.
+ * itself (same data, ld); outputs overlap nothing else (the same data is
+ * refused).
  * Returns as hwsel_block_join does, and HWSEL_EINVAL for a short or misaligned
  * workspace and for an output whose input is missing.
  */

@@ -3,6 +3,9 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <initializer_list>
+
+
 #include "internal.hpp"
 
 namespace {
@@ -689,6 +692,7 @@ int hwsel_logprob_gradient(const float *scores, int64_t R, const int64_t *seg_of
     if (((!scores || !d_scores) && R > 0) || !seg_offsets || !norm || (n_picks > 0 && (!picks || !d_logp)))
         return fail(HWSEL_EINVAL, fn, "null pointer");
     if (!entropy != !d_entropy) return fail(HWSEL_EINVAL, fn, "entropy and d_entropy go together");
+    if (scores < d_scores + R && d_scores < scores + R) return fail(HWSEL_EINVAL, fn, "d_scores overlaps the scores");
     return launched(hwsel::launch_logprob_gradient(scores, R, seg_offsets, P, temperature, temperature_of, norm, picks, n_picks,
                                                    d_logp, entropy, d_entropy, d_scores, (hipStream_t)stream),
                     fn);
@@ -722,6 +726,14 @@ static int check_in_place(const hwsel_matrix_t &out, const hwsel_matrix_t &in, c
 {
     if (out.data && out.data == in.data && (out.ld != in.ld || out.dtype != in.dtype))
         return fail(HWSEL_EINVAL, fn, "%s in place, with another ld or dtype", name);
+    return HWSEL_OK;
+}
+
+// A result lies in no operand's place, and in no other result's, but those that the caller leaves out.
+static int check_apart(const hwsel_matrix_t &out, const char *name, std::initializer_list<const hwsel_matrix_t *> others, const char *fn)
+{
+    for (const hwsel_matrix_t *m : others)
+        if (out.data && out.data == m->data) return fail(HWSEL_EINVAL, fn, "%s in the place of another matrix", name);
     return HWSEL_OK;
 }
 
@@ -786,6 +798,8 @@ int hwsel_block_join(const hwsel_join_t *j, const hwsel_matrix_t *x, const hwsel
     if (int st = check_matrix(x1, "x1", j->cols, x->dtype, fn)) return st;
     if (int st = check_matrix(z, "z", j->cols, block, fn)) return st;
     if (int st = check_in_place(x1, *x, "x1", fn)) return st;
+    if (int st = check_apart(x1, "x1", {&y, &gate, &z}, fn)) return st;
+    if (int st = check_apart(z, "z", {x, &y, &gate}, fn)) return st;
     const bool bbf = (y.data ? y.dtype : z.dtype) == HWSEL_DTYPE_BF16;
     return launched(hwsel::launch_block_join(*j, *x, y, gate, x1, z, x->dtype == HWSEL_DTYPE_BF16, bbf, (hipStream_t)stream), fn);
 }
@@ -828,6 +842,9 @@ int hwsel_block_join_gradient(const hwsel_join_t *j, const hwsel_matrix_t *x1, c
     const size_t need = hwsel::join_gradient_workspace_bytes(*j);
     if (need && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need))
         return fail(HWSEL_EINVAL, fn, "workspace of %zu bytes, %zu needed, 256-byte aligned", workspace_bytes, need);
+    if (int st = check_apart(dx, "dx", {x1, &y, &gate, &d_z, &dy, &dgate}, fn)) return st;
+    if (int st = check_apart(dy, "dy", {x1, &y, &gate, &d_x1, &d_z, &dgate}, fn)) return st;
+    if (int st = check_apart(dgate, "dgate", {x1, &y, &gate, &d_x1, &d_z}, fn)) return st;
     const bool bbf = (y.data ? y.dtype : d_z.dtype) == HWSEL_DTYPE_BF16;
     return launched(hwsel::launch_block_join_gradient(*j, *x1, y, gate, d_x1, d_z, dx, dy, dgate, dw_branch, dw_pre, workspace,
                                                       x1->dtype == HWSEL_DTYPE_BF16, bbf, (hipStream_t)stream),

@@ -51,9 +51,6 @@ inline Ends ends_of(int64_t cols)
     return {tail, cols > 8 && tail ? 8 - tail : 0, cols < 8};
 }
 
-typedef float f32x2_any_t __attribute__((ext_vector_type(2), aligned(4)));
-typedef uint32_t u32_any_t __attribute__((aligned(2)));
-
 // Elements at .. of X, n of them left in the row (zeros where n <= 0 or there is no X: none is read); settle8 comes
 // before their use.
 template <bool BF16, class E>

@@ -86,6 +86,22 @@ def test_results_in_place_lie_as_their_operands(L):
     assert L.hwsel_last_error().startswith(b"hwsel_block_join_gradient: dx in place")
 
 
+def test_results_lie_apart(L):
+    place = {n: mat(0x10000 * (i + 1)) for i, n in enumerate(("x", "y", "gate", "x1", "z", "d_x1", "d_z", "dx", "dy", "dgate"))}
+    for out, others in dict(x1=("y", "gate", "z"), z=("x", "y", "gate")).items():
+        for n in others:
+            m = {k: place[k] for k in ("x", "y", "gate", "x1", "z")} | {out: place[n]}
+            assert forward(L, join(), **m) == 1 and b"in the place of another" in L.hwsel_last_error(), (out, n)
+    ins = ("x1", "y", "gate", "d_z")
+    for out, others in dict(dx=ins, dy=ins + ("d_x1", "dx"), dgate=ins + ("d_x1", "dx", "dy")).items():
+        for n in others:
+            m = {k: place[k] for k in ("x1", "y", "gate", "d_x1", "d_z", "dx", "dy", "dgate")} | {out: place[n]}
+            assert backward(L, join(), **m) == 1 and b"in the place of another" in L.hwsel_last_error(), (out, n)
+    for out in (0x10000, 0x10000 + 4 * 99, 0x10000 - 4 * 99):
+        assert L.hwsel_logprob_gradient(0x10000, 100, FAKE, 4, 1.0, None, FAKE, None, 0, None, FAKE, FAKE, out, None) == 1
+        assert L.hwsel_last_error() == b"hwsel_logprob_gradient: d_scores overlaps the scores"
+
+
 def join(**over):
     a = dict(rows=10, cols=64, w_branch=FAKE, w_pre=FAKE, eps=1e-6, stream_scale=1.0, branch_scale=1.0, post_norm=1, gate_sigmoid=0,
              gate_cols=64)
