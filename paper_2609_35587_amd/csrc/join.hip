@@ -635,14 +635,15 @@ __global__ __launch_bounds__(kTile) void k_join_long_columns(Backward a)
 // rounds of eight loads.
 constexpr int kSumCols = 32, kSumThreads = 1024;
 
-__global__ __launch_bounds__(kSumThreads) void k_join_sums(const float *__restrict__ parts, int32_t n_parts, int64_t cols, float *dwb, float *dwp)
+__global__ __launch_bounds__(kSumThreads) void k_join_sums(const float *__restrict__ parts, int32_t n_parts, int64_t cols, int64_t col0, float *dwb,
+                                                           float *dwp)
 {
     constexpr int kSlices = kSumThreads / kSumCols;
     __shared__ float sh[kSlices][kSumCols + 1];
     float *out = blockIdx.y ? dwp : dwb;
     if (!out) return;
     const int slice = threadIdx.x / kSumCols, at = threadIdx.x % kSumCols;
-    const int64_t col = (int64_t)blockIdx.x * kSumCols + at;
+    const int64_t col = col0 + (int64_t)blockIdx.x * kSumCols + at;
     float s = 0.0f;
     if (col < cols) {
         const float *from = parts + (int64_t)blockIdx.y * cols + col;
@@ -816,8 +817,11 @@ hipError_t launch_block_join_gradient(const hwsel_join_t &j, const hwsel_matrix_
             hipLaunchKernelGGL((k_join_long_columns<SBF, BBF>), dim3(strips, (unsigned)a.n_parts), dim3(kTile), 0, s, a);
         });
     }
-    if (dwb || dwp)
-        hipLaunchKernelGGL(k_join_sums, dim3((unsigned)((j.cols + kSumCols - 1) / kSumCols), 2), dim3(kSumThreads), 0, s, a.parts, a.n_parts, j.cols, dwb, dwp);
+    constexpr int64_t kSpan = (int64_t)1 << 26;             // columns of a launch: fewer than 2^32 threads
+    for (int64_t c0 = 0; (dwb || dwp) && c0 < j.cols; c0 += kSpan) {
+        const int64_t n = j.cols - c0 < kSpan ? j.cols - c0 : kSpan;
+        hipLaunchKernelGGL(k_join_sums, dim3((unsigned)((n + kSumCols - 1) / kSumCols), 2), dim3(kSumThreads), 0, s, a.parts, a.n_parts, j.cols, c0, dwb, dwp);
+    }
     return hipGetLastError();
 }
 

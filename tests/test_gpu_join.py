@@ -1,6 +1,7 @@
 """Joins of blocks to a residual stream and their gradients against binary64, within bounds counted from
 their fp32 operations and the rounding of their results."""
 import itertools
+import math
 
 import pytest
 import torch
@@ -179,3 +180,20 @@ def test_same_bits():
         x1, _ = hwsel.hwsel_block_join(d["join"], d["x"], d["y"], d["gate"])
         got = [hwsel.hwsel_block_join_gradient(d["join"], x1, d["y"], d["gate"], d["d_x1"], d["d_z"]) for _ in range(3)]
         assert all(torch.equal(a, b) for g in got[1:] for a, b in zip(g, got[0]))
+
+
+def test_weights_of_the_longest_rows():
+    """More columns than the threads of one launch can sum."""
+    cols = (1 << 27) + 40
+    g = torch.Generator(device="cuda").manual_seed(8)
+    x1 = torch.randn(1, cols, generator=g, device="cuda")
+    d_z = torch.randn(1, cols, generator=g, device="cuda")
+    join = dict(w_pre=torch.ones(cols, device="cuda"))
+    dw = hwsel.hwsel_block_join_gradient(join, x1, d_z=d_z)[4]
+    r1 = 1.0 / math.sqrt(sum(float(p.double().square().sum()) for p in x1.split(1 << 24, 1)) / cols + 1e-6)
+    # a thread adds 2^18 squares, 8 + 2 more to join threads, each rounding of a sum of positive terms within
+    # 2^-24 of it; r1 has half of that; mean, root, quotient and two products here and there
+    bound = (2**18 + 10) * 2.0**-24 / 2 + 10 * 2.0**-24
+    want = d_z[0] * (x1[0] * r1)
+    assert bool(((dw - want).abs() <= bound * want.abs() + 2.0**-126).all())
+    assert bool((dw[-40:] != 0).all())
