@@ -224,15 +224,14 @@ __device__ __forceinline__ void write_problem(const LogprobArgs &a, const Proble
     }
 }
 
-// n scores by a workgroup, 16 a thread and step.
+// n scores by a workgroup, 16 a thread and step; the last step's stay in w.
 template <int NT>
-__device__ __forceinline__ Mass take_all(const float *s, int32_t n, float rate)
+__device__ __forceinline__ Mass take_all(const float *s, int32_t n, float rate, f32x4u_t (&w)[4])
 {
     Mass m = kNothing;
     constexpr int kStep = 16 * NT;
     for (int32_t at = 0; at < n; at += kStep) {
         const int32_t left = n - at;
-        f32x4u_t w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = load4(s + at, (i * NT + (int)threadIdx.x) * 4, left);
         float v[16];
@@ -254,13 +253,13 @@ struct Lds {
 
 constexpr uint32_t kLeastBits = 0x00800000u;                // of the least finite score; below them are -inf and NaN
 
-// The best `top` of n scores, read once more: a score is listed if it is not below what the best scores of `top`
+// The best `top` of n scores, read once more unless one step (w) has them: a score is listed if it is not below what the best scores of `top`
 // threads reach (of 256 threads, or of 64 groups of them; more are taken together), and the listed ones, few more
 // than `top`, are ranked by counting the larger.  False, and nothing written, if they do not fit the list.
 // (By tiles, each score with its key against a running bound, the sums on the way: 600 of up to 8,192 scores, 10 of
 // each, 13.7 us, 10.1 so; 256 of 65,536 with 64 of each 77 and 24; 256 of 131,072, 134 MB, 90 and 44.)
 template <int NT>
-__device__ __forceinline__ bool list_best(const float *s, int32_t n, int32_t top, Lds<NT> &lds)
+__device__ __forceinline__ bool list_best(const float *s, int32_t n, int32_t top, Lds<NT> &lds, f32x4u_t (&w)[4])
 {
     const int lane = threadIdx.x & 63;
     uint32_t best[4] = {}, bits = 0;
@@ -283,9 +282,10 @@ __device__ __forceinline__ bool list_best(const float *s, int32_t n, int32_t top
     const float least = bits > kLeastBits ? desc_value(bits) : -3.4028235e38f;
     constexpr int kStep = 16 * NT;
     for (int32_t at = 0; at < n; at += kStep) {
-        f32x4u_t w[4];
+        if (n > kStep) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = load4(s + at, (i * NT + (int)threadIdx.x) * 4, n - at);
+            for (int i = 0; i < 4; ++i) w[i] = load4(s + at, (i * NT + (int)threadIdx.x) * 4, n - at);
+        }
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const float v = w[i >> 2][i & 3];
@@ -319,13 +319,14 @@ template <int NT, int TILE, bool TOP>
 __device__ __forceinline__ Mass block_scores(const float *s, int32_t n, int32_t top, bool cold, float rate, Lds<NT> &lds, int32_t &first)
 {
     first = -1;
+    f32x4u_t w[4];
     if constexpr (TOP) {
-        Mass m = take_all<NT>(s, n, rate);
+        Mass m = take_all<NT>(s, n, rate, w);
         lds.best[threadIdx.x >> 6][threadIdx.x & 63] = m.best > kNone ? order_key(m.best + 0.0f) : 0u;
         if (threadIdx.x < 64) lds.keys[threadIdx.x] = 0;
         if (threadIdx.x == 0) lds.n_list = 0;
         m = block_mass<NT>(m, rate, lds.part);              // (its barrier)
-        if (!list_best<NT>(s, n, top, lds)) {               // many scores are one: by tiles
+        if (!list_best<NT>(s, n, top, lds, w)) {               // many scores are one: by tiles
             __syncthreads();
             topk_tiles<NT, TILE>(s, n, top, lds.topk, [&](int32_t j, uint64_t key) { lds.keys[j] = key; });
             __syncthreads();
@@ -333,7 +334,7 @@ __device__ __forceinline__ Mass block_scores(const float *s, int32_t n, int32_t 
         if (cold) first = (int32_t)(0xffffffffu - (uint32_t)lds.keys[0]);
         return m;
     } else {
-        const Mass m = block_mass<NT>(take_all<NT>(s, n, rate), rate, lds.part);
+        const Mass m = block_mass<NT>(take_all<NT>(s, n, rate, w), rate, lds.part);
         if (cold) {
             if (threadIdx.x == 0) lds.first = 0x7fffffff;
             __syncthreads();
