@@ -838,7 +838,9 @@ __global__ __launch_bounds__(kThreads) void k_logprob_gradient_waves(GradientArg
 
 namespace {
 
-// Problems' lengths are not known here; their mean is.
+// Problems' lengths are not known here; their mean is.  Parts and the kernel that joins them against a workgroup a
+// problem, us: 64 x 20,000, 16 alternatives 13.3 / 10.3, 8 x 40,000 11.4 / 12.1, 64 x 40,000 13.4 / 12.3, 128 x 65,536 16.2 / 14.5, 3 x 100,000
+// 11.4 / 19.6, 64 x 100,000 16.2 / 20.1, 3 x 534,600 14.1 / 67.9.
 int32_t parts_of(int64_t R, int32_t P, int32_t top)
 {
     const int64_t mean = R / P, n_cu = compute_units();
@@ -875,13 +877,18 @@ hipError_t launch_logprob(const float *scores, int64_t R, const int64_t *seg, in
                 a.p0 = p0;
                 hipLaunchKernelGGL((k_logprob_waves<TOP>), dim3((n + 3) / 4), dim3(kThreads), 0, s, a);
             });
-        } else if (P <= compute_units()) {
-            hipLaunchKernelGGL((k_logprob<1024, kTile, TOP>), dim3(P), dim3(1024), 0, s, a);
         } else {
+            // Threads of a problem.  Fewer start and meet sooner, more read a long one with fewer steps; where a unit has
+            // several problems those fill it.  Best of 256 / 512 / 1,024, us: 600 x 4,096, 10 alternatives 7.4 / 9.4 / 19.5, 600
+            // of 2,000 .. 16,000 13.3 / 12.5 / 19.5, 300 of 6,000 .. 50,000 26.1 / 20.5 / 21.9; 200 x 4,096 6.4 / 6.6 / 7.9,
+            // 1 x 8,192 7.2 / 5.9 / 7.0, 100 x 16,000 10.6 / 8.2 / 7.5, 200 x 100,000 50 / 31.5 / 29.2; none asked for: 100 x 16,000
+            // 6.3 / 5.1 / 5.5, and of 512 / 1,024 with scores from memory: 256 x 65,536 17.0 / 16.2, 200 x 100,000 24 / 19.3.
+            const bool alone = P <= compute_units();
             each_span(P, [&](int32_t p0, int32_t n) {
                 a.p0 = p0;
-                if (mean <= 8192) hipLaunchKernelGGL((k_logprob<256, 2048, TOP>), dim3(n), dim3(256), 0, s, a);
-                else hipLaunchKernelGGL((k_logprob<512, 4096, TOP>), dim3(n), dim3(512), 0, s, a);
+                if (mean <= (alone ? 4096 : 8192)) hipLaunchKernelGGL((k_logprob<256, 2048, TOP>), dim3(n), dim3(256), 0, s, a);
+                else if (!alone || mean <= 8192) hipLaunchKernelGGL((k_logprob<512, 4096, TOP>), dim3(n), dim3(512), 0, s, a);
+                else hipLaunchKernelGGL((k_logprob<1024, kTile, TOP>), dim3(n), dim3(1024), 0, s, a);
             });
         }
     };
