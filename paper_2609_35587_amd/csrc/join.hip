@@ -4,6 +4,10 @@
 // With d = d_x1 + r1 (dn - xn mean(dn xn)), dn = d_z w_pre, xn = x1 r1:
 //   dx = stream d;  dv = dropout(branch d);  dg = dv u;  du = dv g;  dw_branch = sum du yn;
 //   dy = r (dn' - yn mean(dn' yn)), dn' = du w_branch;  dw_pre = sum d_z xn
+//
+// Bound by memory: each operand is read once and each result written once where a row fits the registers of the threads
+// that have it.  Measured (HBM bytes over time): 1,048,576 x 512, fp32 stream and bf16 block with an element gate, 1,456 us, 5.2
+// TB/s, what a copy reaches; 65,536 x 1,024 in bf16 with gate and dropout forward 128 us, 5.2 TB/s, backward 209 us, 5.2 TB/s.
 #include "rows.hpp"
 
 namespace hwsel {
@@ -181,7 +185,8 @@ __device__ __forceinline__ void lane_sums(float (&v)[N], Shared &sh, int &turn)
 
 // ---------------------------------------------------------------------------
 // Rows that fit the registers of LANES threads, 8 K columns each: a row is read
-// once and written once.  Threads keep their columns from row to row.
+// once and written once.  Threads keep their columns from row to row, so weights
+// are read once a launch and their gradients are summed in registers.
 // ---------------------------------------------------------------------------
 // How a thread's k-th eight of K is read: but for the last all are there.
 template <bool EDGE, int K, int k>
@@ -310,7 +315,9 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void k_join(Forward a)
 }
 
 // Two rounds of sums a row: x1^2, dn x1 and y^2 together, then what goes by d.
-// A workgroup's sums over its rows go to a part of their own.
+// A workgroup's sums over its rows go to a part of their own, joined in a fixed
+// order by k_join_sums: atomics would add in any order.  The second launch takes 5 us.
+// Five operands and two sums of 16 columns are 190 to 225 registers, two waves a SIMD; vector units are busy 59 % of the time.
 template <bool SBF, bool BBF, int LANES, int K, bool EDGE>
 __global__ __launch_bounds__(LANES ? 256 : 512, K == 2 ? 2 : LANES == 64 || LANES == 0 ? 4 : 3) void k_join_gradient(Backward a)
 {
@@ -424,7 +431,10 @@ __global__ __launch_bounds__(LANES ? 256 : 512, K == 2 ? 2 : LANES == 64 || LANE
 }
 
 // ---------------------------------------------------------------------------
-// Rows of any length: a workgroup goes through a row several times.
+// Rows of any length: a workgroup goes through a row several times, from the
+// second on out of the caches where it fits them.  Forward: 2,000 x 30,000 in bf16 188 us (3.2 TB/s of each operand once).
+// Backward: two kernels, the rows' sums, then columns, whose sums over rows stay in registers: 4,000 x 16,384 379 us
+// (2.8 TB/s), 2,000 x 30,000 380 us (2.5 TB/s).
 // ---------------------------------------------------------------------------
 constexpr int kLong = 512;
 
@@ -707,10 +717,14 @@ void each_row_span(Common &c, F &&f)
 
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// The longest rows that registers hold.
+// The longest rows that registers hold: 1,024 threads of two eights forward; backward 512, since 1,024 threads leave each
+// 128 registers and the gradient takes up to 225.
 constexpr int64_t kLongestForward = 16384, kLongestBackward = 8192;
 
 // How rows of some length lie in registers: `lanes` threads of K eights each (0: all of the workgroup's `threads`).
+// Fewer threads a row leave fewer without columns and add up in fewer steps; two eights a thread have more loads on the way.
+// Forward in bf16, us: 1,000,000 x 64 by 8 lanes 113, by 16 227; 200,000 x 250 by 32 lanes 115, by 64 205; 65,536 x 1,024 by one
+// wave of two eights 131, by two waves of one 147; 16,384 x 4,096 with two eights 127, with one 147; 8,192 x 8,192 130 and 152.
 struct Shape {
     int lanes, K, threads;
     int rows() const { return lanes ? 256 / lanes : 1; }
@@ -728,6 +742,7 @@ Shape shape_of(int64_t cols)
 }
 
 // Workgroups that run at once where a SIMD holds `waves` of their waves, at most one for each row (or rows).
+// 65,536 x 1,024 in bf16, us: forward 4 waves 131, 6 142, 8 136; backward 2 waves 213, 3 231, 4 215 (and twice the parts).
 int32_t groups_of(const Shape &f, int64_t rows, int waves)
 {
     const int64_t each = 4 * waves * 64 / f.threads, most = (int64_t)compute_units() * (each > 1 ? each : 1), need = (rows + f.rows() - 1) / f.rows();

@@ -1,7 +1,11 @@
 // Log probabilities of given candidates with entropy and best alternatives, and
 // their gradient with respect to the scores.
 //   t = (s - best) / T;  Z = sum exp t;  log p = t - log Z;  H = log Z - sum(exp(t) t) / Z
-// Scores are read once, with the running best score and the sums that go by it.
+// Scores are read once, with the running best score and the sums that go by it; for alternatives once more where
+// a workgroup's registers do not hold them.
+//
+// Bound by latency where problems are few or short (a launch, the offsets, the scores, barriers: 4 us for any), by memory
+// where they are long: 256 x 65,536 scores, 67 MB, 15 us (4.5 TB/s), their gradient 26 us (5.2 TB/s read and written).
 #include "topk.hpp"
 
 namespace hwsel {
