@@ -433,8 +433,9 @@ __global__ __launch_bounds__(LANES ? 256 : 512, K == 2 ? 2 : LANES == 64 || LANE
 // ---------------------------------------------------------------------------
 // Rows of any length: a workgroup goes through a row several times, from the
 // second on out of the caches where it fits them.  Forward: 2,000 x 30,000 in bf16 188 us (3.2 TB/s of each operand once).
-// Backward: two kernels, the rows' sums, then columns, whose sums over rows stay in registers: 4,000 x 16,384 379 us
-// (2.8 TB/s), 2,000 x 30,000 380 us (2.5 TB/s).
+// Backward: two kernels, the rows' sums, then columns, whose sums over rows stay in registers, at 4.6 and 6.0 TB/s of what each
+// of them moves: 4,000 x 16,384 370 us (2.8 TB/s of each operand once), 2,000 x 30,000 355 us (2.7 TB/s); 395 and 385 with
+// what goes by d in a second pass of the first kernel.
 // ---------------------------------------------------------------------------
 constexpr int kLong = 512;
 
@@ -509,81 +510,70 @@ __global__ __launch_bounds__(kLong) void k_join_long(Forward a)
     }
 }
 
-// What the columns' pass needs of each row, and the gradient of its gate.
+// What the columns' pass needs of each row, and the gradient of its gate, in one pass over the row.  d is linear in
+// d_x1, dn and x1 with factors that are known once the row has been read, so what goes by d is made of three
+// sums with h = dropout(branch) w_branch y (and an element's gate): sum h d = sum h d_x1 + r1 (sum h dn - r1 m1 sum h x1).
 template <bool SBF, bool BBF>
 __global__ __launch_bounds__(kLong) void k_join_long_stats(Backward a)
 {
-    __shared__ float sh3[3][kLong / 64], sh2[2][kLong / 64];
+    __shared__ float sh[6][kLong / 64];
     const Common &c = a.c;
     const Ends ends = c.ends;
     const int64_t row = c.row0 + blockIdx.x;
     const Mask m = mask_of(c.drop);
-    float s[3] = {};
+    const bool by_d = a.y.p && (c.post_norm || c.gate_kind == kRowGate);
+    float s[6] = {};
     for (int32_t col = threadIdx.x * 8; col < c.cols; col += kLong * 8) {
         const int32_t n = c.cols - col;
-        if (a.dz.p) {
-            Eight<SBF> x1 = load8<SBF>(a.x1.p, row * a.x1.ld + col, n, ends);
-            settle8(x1, n, ends);
-            Eight<BBF> dz = load8<BBF>(a.dz.p, row * a.dz.ld + col, n, ends);
-            settle8(dz, n, ends);
-            float w[8];
-            weights8(c.wp, col, c, ends, w);
+        Stream8<SBF, BBF> q;
+        q.load(a, row, col, n, ends);
+        Eight<BBF> y = load8<BBF>(by_d ? a.y.p : nullptr, row * a.y.ld + col, n, ends);
+        Eight<BBF> g = load8<BBF>(by_d && c.gate_kind == kElementGate ? a.gate.p : nullptr, row * a.gate.ld + col, n, ends);
+        float wp[8], wb[8];
+        weights8(c.wp, col, c, ends, wp);
+        weights8(c.wb, col, c, ends, wb);
+        q.settle(n, ends);
+        settle8(y, n, ends);
+        settle8(g, n, ends);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                s[0] += x1.at(i) * x1.at(i);
-                s[1] += dz.at(i) * w[i] * x1.at(i);
-            }
+        for (int i = 0; i < 8; ++i) {
+            s[0] += q.x1.at(i) * q.x1.at(i);
+            s[1] += q.dz.at(i) * wp[i] * q.x1.at(i);
+            s[2] += y.at(i) * y.at(i);
         }
-        if (a.y.p && c.post_norm) {
-            Eight<BBF> y = load8<BBF>(a.y.p, row * a.y.ld + col, n, ends);
-            settle8(y, n, ends);
+        if (!by_d) continue;
+        float share[8];                                     // of the branch: 0 where it is dropped
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s[2] += y.at(i) * y.at(i);
+        for (int i = 0; i < 8; ++i) share[i] = 1.0f;
+        if (m.least != 0) drop8(m, (uint32_t)row, (uint32_t)(col >> 3), share);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float h = share[i] * c.branch * wb[i] * y.at(i) * (c.gate_kind == kElementGate ? gate_value(g.at(i), c.sigmoid) : 1.0f);
+            s[3] += share[i] != 0.0f ? h * q.dx1.at(i) : 0.0f;
+            s[4] += h * (q.dz.at(i) * wp[i]);
+            s[5] += h * q.x1.at(i);
         }
     }
-    block_sums<kLong>(s, sh3);
+    block_sums<kLong>(s, sh);
+    if (threadIdx.x != 0) return;
     const float r1 = a.dz.p ? norm_factor(s[0], c) : 0.0f, m1 = r1 * s[1] * c.inv_cols;
     const float r = c.post_norm ? norm_factor(s[2], c) : 1.0f;
-    float t[2] = {};
-    if (a.y.p && (c.post_norm || c.gate_kind == kRowGate)) {
-        const float gate = c.gate_kind == kRowGate ? load1<BBF>(a.gate.p, row * a.gate.ld) : 1.0f;
-        const float row_gate = c.gate_kind == kRowGate ? gate_value(gate, c.sigmoid) : 1.0f;
-        for (int32_t col = threadIdx.x * 8; col < c.cols; col += kLong * 8) {
-            const int32_t n = c.cols - col;
-            Stream8<SBF, BBF> q;
-            q.load(a, row, col, n, ends);
-            q.settle(n, ends);
-            Eight<BBF> y = load8<BBF>(a.y.p, row * a.y.ld + col, n, ends);
-            settle8(y, n, ends);
-            Eight<BBF> g = load8<BBF>(c.gate_kind == kElementGate ? a.gate.p : nullptr, row * a.gate.ld + col, n, ends);
-            settle8(g, n, ends);
-            float wp[8], wb[8], d[8], dv[8];
-            weights8(c.wp, col, c, ends, wp);
-            weights8(c.wb, col, c, ends, wb);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) d[i] = q.d(i, wp[i], r1, m1);
-            branch8(c, m, row, col, d, dv);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float yn = y.at(i) * r, gi = c.gate_kind == kElementGate ? gate_value(g.at(i), c.sigmoid) : row_gate;
-                t[0] += dv[i] * gi * wb[i] * yn;
-                t[1] += dv[i] * wb[i] * yn;
-            }
-        }
-        block_sums<kLong>(t, sh2);
-        if (threadIdx.x == 0 && a.dgate.p && c.gate_kind == kRowGate) {
-            const float dg = t[1] * gate_slope(gate, c.sigmoid);
+    const float t = r * (s[3] + r1 * (s[4] - r1 * m1 * s[5]));   // of dv u, the gradient of a row's gate; its gate times that: of dn' yn
+    float row_gate = 1.0f;
+    if (c.gate_kind == kRowGate) {
+        const float gate = load1<BBF>(a.gate.p, row * a.gate.ld);
+        row_gate = gate_value(gate, c.sigmoid);
+        if (a.dgate.p) {
+            const float dg = t * gate_slope(gate, c.sigmoid);
             if constexpr (BBF) static_cast<uint16_t *>(a.dgate.p)[row * a.dgate.ld] = (uint16_t)bf16_pair(dg, 0.0f);
             else static_cast<float *>(a.dgate.p)[row * a.dgate.ld] = dg;
         }
     }
-    if (threadIdx.x == 0) {
-        float *st = a.stats + row * 4;
-        st[0] = r1;
-        st[1] = m1;
-        st[2] = r;
-        st[3] = c.post_norm ? t[0] * c.inv_cols : 0.0f;
-    }
+    float *st = a.stats + row * 4;
+    st[0] = r1;
+    st[1] = m1;
+    st[2] = r;
+    st[3] = c.post_norm ? row_gate * t * c.inv_cols : 0.0f;
 }
 
 // The gradients of 2,048 columns of some rows, and their sums over those rows.
@@ -606,7 +596,11 @@ __global__ __launch_bounds__(kTile) void k_join_long_columns(Backward a)
         const float r1 = st[0], m1 = st[1], r = st[2], mean = st[3];
         Stream8<SBF, BBF> q;
         q.load(a, row, col, n, ends);
+        Eight<BBF> y = load8<BBF>(a.y.p, row * a.y.ld + col, n, ends);
+        Eight<BBF> g = load8<BBF>(c.gate_kind == kElementGate ? a.gate.p : nullptr, row * a.gate.ld + col, n, ends);
         q.settle(n, ends);
+        settle8(y, n, ends);
+        settle8(g, n, ends);
         float d[8], o[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -614,10 +608,6 @@ __global__ __launch_bounds__(kTile) void k_join_long_columns(Backward a)
             swp[i] += q.dz.at(i) * (q.x1.at(i) * r1);
             o[i] = c.stream * d[i];
         }
-        Eight<BBF> y = load8<BBF>(a.y.p, row * a.y.ld + col, n, ends);
-        settle8(y, n, ends);
-        Eight<BBF> g = load8<BBF>(c.gate_kind == kElementGate ? a.gate.p : nullptr, row * a.gate.ld + col, n, ends);
-        settle8(g, n, ends);
         if (a.dx.p) store8<SBF>(a.dx.p, row * a.dx.ld + col, n, ends, o);
         if (!a.y.p) continue;
         const float row_gate = c.gate_kind == kRowGate ? gate_value(load1<BBF>(a.gate.p, row * a.gate.ld), c.sigmoid) : 1.0f;

@@ -197,3 +197,18 @@ def test_weights_of_the_longest_rows():
     want = d_z[0] * (x1[0] * r1)
     assert bool(((dw - want).abs() <= bound * want.abs() + 2.0**-126).all())
     assert bool((dw[-40:] != 0).all())
+
+
+@pytest.mark.parametrize("cols", [64, 900, 2600, 9000, 20_000])
+@pytest.mark.parametrize("gate", ["none", "row", "element"])
+def test_gradients_that_are_dropped(cols, gate):
+    """The branch has no part in what is dropped: a NaN there stays in the stream."""
+    d = made(6, cols, F, B, p=0.5, gate=gate)
+    x1, _ = hwsel.hwsel_block_join(d["join"], d["x"], d["y"], d["gate"])
+    kept = hwsel.hwsel_dropout(torch.ones(6, cols, device="cuda"), 0.5, d["join"]["seed"], d["join"]["offset"]) != 0
+    at = (~kept[2]).nonzero()[3, 0]
+    clean = hwsel.hwsel_block_join_gradient(d["join"], x1, d["y"], d["gate"], d["d_x1"], d["d_z"])
+    d["d_x1"][2, at] = float("nan")
+    got = hwsel.hwsel_block_join_gradient(d["join"], x1, d["y"], d["gate"], d["d_x1"], d["d_z"])
+    assert bool(torch.isnan(got[0][2, at])) and int(torch.isnan(got[0]).sum()) == 1
+    assert all(a is b or torch.equal(a, b) for a, b in zip(got[1:], clean[1:]))
