@@ -57,7 +57,7 @@ def _binding() -> None:
     # (the defines that the runtime's and torch's own headers ask of a host compiler)
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *[a for i in include for a in ("-isystem", i)],
-           os.path.join(CSRC, BINDING_SRC), "-L" + os.path.join(t, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10_hip", "-lc10",
+           os.path.join(CSRC, BINDING_SRC), "-L" + os.path.join(t, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch_hip", "-lc10_hip", "-lc10",
            "-o", tmp]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode:

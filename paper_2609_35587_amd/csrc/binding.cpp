@@ -11,7 +11,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
-#include <ATen/ops/empty.h>
+#include <ATen/hip/EmptyTensor.h>
 #include <c10/hip/HIPCachingAllocator.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
@@ -154,7 +154,8 @@ public:
 private:
     at::Tensor empty(at::IntArrayRef sizes, at::ScalarType type) const
     {
-        return at::empty(sizes, at::TensorOptions().dtype(type).device(at::kCUDA, (c10::DeviceIndex)device_));
+        // (at::empty finds the same by torch's dispatcher, 0.25 us a tensor later)
+        return at::detail::empty_cuda(sizes, type, c10::Device(at::kCUDA, (c10::DeviceIndex)device_), std::nullopt);
     }
 
     int device_;
