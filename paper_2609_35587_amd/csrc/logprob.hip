@@ -876,7 +876,10 @@ hipError_t launch_logprob(const float *scores, int64_t R, const int64_t *seg, in
             const Parts w{static_cast<Part *>(ws), reinterpret_cast<uint64_t *>(static_cast<char *>(ws) + up256((size_t)P * parts * sizeof(Part))), parts};
             hipLaunchKernelGGL((k_logprob_parts<TOP>), dim3(parts, P), dim3(kWide), 0, s, a, w);
             hipLaunchKernelGGL((k_logprob_join<TOP>), dim3(P), dim3(kWide), 0, s, a, w);
-        } else if (mean <= kSmall) {
+        } else if (mean <= (TOP && P <= 4 * compute_units() ? 256 : kSmall)) {
+            // A wave a problem, four in a workgroup, against a workgroup each, us: without alternatives always (100 x 700 4.2 / 4.2,
+            // 3,000 x 1,000 5.8 / 12.2); with ten 100 x 200 7.2 / 6.3, 600 x 64 5.8 / 7.5, 100 x 512 8.0 / 6.2, 600 x 1,000 12.5 / 7.6, 1,500 x 700 13.1 / 10.3,
+            // 3,000 x 700 15.5 / 16.4, 8,000 x 700 28 / 34; with 64 100 x 200 7.7 / 10.4, 600 x 512 10.2 / 9.2.
             each_span(P, [&](int32_t p0, int32_t n) {
                 a.p0 = p0;
                 hipLaunchKernelGGL((k_logprob_waves<TOP>), dim3((n + 3) / 4), dim3(kThreads), 0, s, a);
@@ -908,16 +911,18 @@ hipError_t launch_logprob_gradient(const float *scores, int64_t R, const int64_t
     GradientArgs a{scores, R, seg, P, 0, temperature, temperature_of, norm, picks, n_picks, d_logp, entropy, d_entropy, d_scores};
     const int64_t mean = R / P;
     auto go = [&]<bool PICKS>() {
-        if (mean <= 1024) {
+        if (mean <= 1024) {                                 // (a wave / a workgroup each, us: 1 x 1,000 3.7 / 4.5, 2,000 x 900 6.4 / 12.0)
             each_span(P, [&](int32_t p0, int32_t n) {
                 a.p0 = p0;
                 hipLaunchKernelGGL((k_logprob_gradient_waves<PICKS>), dim3((n + 3) / 4), dim3(kThreads), 0, s, a);
             });
             return;
         }
-        // parts of up to twice the mean length; several to a workgroup where there are more of them than run at once
-        const int64_t by_length = (2 * mean + kPart - 1) / kPart, at_once = 5 * (int64_t)compute_units() / P;
-        const int64_t most = at_once > 2 ? at_once : 2, each = by_length < most ? by_length : most;
+        // Parts of up to twice the mean length; several to a workgroup where there are more of them than run at once (four a
+        // unit, by their LDS): each goes through all picks.  One / two / five workgroups a problem, us: 600 of 1,000 .. 8,192 9.1 / 10.2 / 10.5, 2,000 x
+        // 4,000 15.6 / 22.2 / 19.9, 256 x 65,536 29.0 / 24.1 / 25.1, 64 x 8,192 5.6 / 4.4 / 4.8; 8 x 200,000 64 / 35 / 16 and 5.7 with 98.
+        const int64_t by_length = (2 * mean + kPart - 1) / kPart, at_once = 4 * (int64_t)compute_units() / P;
+        const int64_t most = at_once > 1 ? at_once : 1, each = by_length < most ? by_length : most;
         for (a.p0 = 0; a.p0 < P; a.p0 += 1 << 15) {         // (a grid's second dimension)
             const int32_t n = P - a.p0 < 1 << 15 ? P - a.p0 : 1 << 15;
             hipLaunchKernelGGL((k_logprob_gradient<PICKS>), dim3((unsigned)each, n), dim3(kThreads), 0, s, a);
