@@ -5,7 +5,7 @@
 // a workgroup's registers do not hold them.
 //
 // Bound by latency where problems are few or short (a launch, the offsets, the scores, barriers: 4 us for any), by memory
-// where they are long: 256 x 65,536 scores, 67 MB, 15 us (4.5 TB/s), their gradient 26 us (5.2 TB/s read and written).
+// where they are long: 256 x 65,536 scores, 67 MB, 15 us (4.5 TB/s), their gradient 23.5 us (5.7 TB/s read and written).
 #include "topk.hpp"
 
 namespace hwsel {
