@@ -85,6 +85,26 @@ __device__ __forceinline__ void block_sums(float (&v)[N], float (&sh)[N][NT / 64
     }
 }
 
+template <int CTRL, int ROW_MASK, bool ZERO_FILL>
+__device__ __forceinline__ double dpp_add64(double v)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, ROW_MASK, 0xf, ZERO_FILL);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, ROW_MASK, 0xf, ZERO_FILL);
+    return v + __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
+}
+
+// The wave's sum, in its last lane.
+__device__ __forceinline__ double wave_total(double v)
+{
+    v = dpp_add64<0x111, 0xf, true>(v);
+    v = dpp_add64<0x112, 0xf, true>(v);
+    v = dpp_add64<0x114, 0xf, true>(v);
+    v = dpp_add64<0x118, 0xf, true>(v);
+    v = dpp_add64<0x142, 0xa, false>(v);
+    return dpp_add64<0x143, 0xc, false>(v);
+}
+
 template <class E>
 __device__ __forceinline__ void weights8(const float *w, int32_t col, const Common &c, const E &ends, float (&v)[8])
 {
@@ -434,7 +454,7 @@ __global__ __launch_bounds__(LANES ? 256 : 512, K == 2 ? 2 : LANES == 64 || LANE
 // Rows of any length: a workgroup goes through a row several times, from the
 // second on out of the caches where it fits them.  Forward: 2,000 x 30,000 in bf16 188 us (3.2 TB/s of each operand once).
 // Backward: two kernels, the rows' sums, then columns, whose sums over rows stay in registers, at 4.6 and 6.0 TB/s of what each
-// of them moves: 4,000 x 16,384 370 us (2.8 TB/s of each operand once), 2,000 x 30,000 355 us (2.7 TB/s); 395 and 385 with
+// of them moves: 4,000 x 16,384 385 us (2.7 TB/s of each operand once), 2,000 x 30,000 355 us (2.7 TB/s); 401 and 385 with
 // what goes by d in a second pass of the first kernel.
 // ---------------------------------------------------------------------------
 constexpr int kLong = 512;
@@ -513,16 +533,20 @@ __global__ __launch_bounds__(kLong) void k_join_long(Forward a)
 // What the columns' pass needs of each row, and the gradient of its gate, in one pass over the row.  d is linear in
 // d_x1, dn and x1 with factors that are known once the row has been read, so what goes by d is made of three
 // sums with h = dropout(branch) w_branch y (and an element's gate): sum h d = sum h d_x1 + r1 (sum h dn - r1 m1 sum h x1).
+// Where the parts of d cancel so do the three sums, but not their errors: they are made in 64 bits, of products that these
+// hold whole.  (In 32 bits 4,000 x 16,384 took 376 us, and lost thousands of units where little of d was left.)
 template <bool SBF, bool BBF>
 __global__ __launch_bounds__(kLong) void k_join_long_stats(Backward a)
 {
-    __shared__ float sh[6][kLong / 64];
+    __shared__ float sh[3][kLong / 64];
+    __shared__ double sh64[3][kLong / 64];
     const Common &c = a.c;
     const Ends ends = c.ends;
     const int64_t row = c.row0 + blockIdx.x;
     const Mask m = mask_of(c.drop);
     const bool by_d = a.y.p && (c.post_norm || c.gate_kind == kRowGate);
-    float s[6] = {};
+    float s[3] = {};
+    double t[3] = {};
     for (int32_t col = threadIdx.x * 8; col < c.cols; col += kLong * 8) {
         const int32_t n = c.cols - col;
         Stream8<SBF, BBF> q;
@@ -549,22 +573,34 @@ __global__ __launch_bounds__(kLong) void k_join_long_stats(Backward a)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float h = share[i] * c.branch * wb[i] * y.at(i) * (c.gate_kind == kElementGate ? gate_value(g.at(i), c.sigmoid) : 1.0f);
-            s[3] += share[i] != 0.0f ? h * q.dx1.at(i) : 0.0f;
-            s[4] += h * (q.dz.at(i) * wp[i]);
-            s[5] += h * q.x1.at(i);
+            t[0] += share[i] != 0.0f ? (double)h * q.dx1.at(i) : 0.0;
+            t[1] += (double)h * ((double)q.dz.at(i) * wp[i]);
+            t[2] += (double)h * q.x1.at(i);
         }
     }
-    block_sums<kLong>(s, sh);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        t[i] = wave_total(t[i]);
+        if ((threadIdx.x & 63) == 63) sh64[i][threadIdx.x >> 6] = t[i];
+    }
+    block_sums<kLong>(s, sh);                               // (its barriers)
     if (threadIdx.x != 0) return;
     const float r1 = a.dz.p ? norm_factor(s[0], c) : 0.0f, m1 = r1 * s[1] * c.inv_cols;
     const float r = c.post_norm ? norm_factor(s[2], c) : 1.0f;
-    const float t = r * (s[3] + r1 * (s[4] - r1 * m1 * s[5]));   // of dv u, the gradient of a row's gate; its gate times that: of dn' yn
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        t[i] = sh64[i][0];
+#pragma unroll
+        for (int w = 1; w < kLong / 64; ++w) t[i] += sh64[i][w];
+    }
+    // of dv u, the gradient of a row's gate; its gate times that: of dn' yn
+    const float by_u = (float)(r * (t[0] + (double)r1 * (t[1] - (double)r1 * m1 * t[2])));
     float row_gate = 1.0f;
     if (c.gate_kind == kRowGate) {
         const float gate = load1<BBF>(a.gate.p, row * a.gate.ld);
         row_gate = gate_value(gate, c.sigmoid);
         if (a.dgate.p) {
-            const float dg = t * gate_slope(gate, c.sigmoid);
+            const float dg = by_u * gate_slope(gate, c.sigmoid);
             if constexpr (BBF) static_cast<uint16_t *>(a.dgate.p)[row * a.dgate.ld] = (uint16_t)bf16_pair(dg, 0.0f);
             else static_cast<float *>(a.dgate.p)[row * a.dgate.ld] = dg;
         }
@@ -573,7 +609,7 @@ __global__ __launch_bounds__(kLong) void k_join_long_stats(Backward a)
     st[0] = r1;
     st[1] = m1;
     st[2] = r;
-    st[3] = c.post_norm ? row_gate * t * c.inv_cols : 0.0f;
+    st[3] = c.post_norm ? row_gate * by_u * c.inv_cols : 0.0f;
 }
 
 // The gradients of 2,048 columns of some rows, and their sums over those rows.
