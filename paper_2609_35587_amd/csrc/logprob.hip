@@ -675,6 +675,7 @@ __device__ __forceinline__ void gradient_of(const GradientArgs &a, int32_t p, co
         return log_probability(q, z, j, v) > kNone ? j : -1;
     };
     float S = 0.0f;
+    unsigned long long sum = 0;                             // S in fixed point
     int e = 0;
     bool fine = true;
     auto fixed = [&](float v) { return (unsigned long long)(long long)__builtin_rint(__builtin_ldexp((double)v, -e)); };
@@ -712,7 +713,6 @@ __device__ __forceinline__ void gradient_of(const GradientArgs &a, int32_t p, co
         S = __uint_as_float(most);
         if (fine) {                                         // (uniform)
             e = (int)(most >> 23) - 126 + (32 - __builtin_clz((uint32_t)a.n_picks)) - 62;
-            unsigned long long sum = 0;
             each([&](int32_t j, float, float g) {
                 const unsigned long long u = fixed(g);
                 sum += u;
@@ -776,8 +776,9 @@ __device__ __forceinline__ void gradient_of(const GradientArgs &a, int32_t p, co
                     float x = 1.0f / 9.0f;
 #pragma unroll
                     for (int m = 8; m >= 1; --m) x = (1.0f + lp * x) * (1.0f / (float)m);
-                    const float g = value(fx.acc[i]), own = g * (lp > -0.5f ? -lp * x : 1.0f - pr);
-                    d[part + i] = done(v, lt, own - pr * (S - g) - of_entropy(pr, lp));
+                    // (the others' sum S - g too: in whole numbers, rounded once)
+                    const float g = value(fx.acc[i]), others = value(sum - fx.acc[i]), own = g * (lp > -0.5f ? -lp * x : 1.0f - pr);
+                    d[part + i] = done(v, lt, own - pr * others - of_entropy(pr, lp));
                 });
             }
         }
