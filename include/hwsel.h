@@ -757,7 +757,8 @@ typedef struct hwsel_dropout {
  * sum in fp32, then rounded to Y's dtype.  Y and residual have one dtype, X its
  * own.  The gradient of X
  * is the same call on Y's gradient without a residual; the residual's is Y's
- * gradient itself.  Y may be X or the residual (same data, ld and dtype); no other overlap.
+ * gradient itself.  Y may be X or the residual (same data, ld and dtype); any
+ * other overlap is refused.
  * Returns HWSEL_EINVAL for null pointers, sizes < 1, p outside [0, 1] or NaN,
  * a bad ld or alignment, a residual of another dtype; HWSEL_EUNSUPPORTED for
  * another dtype, rows >= 2^31 or cols > 2^30.
@@ -781,8 +782,8 @@ int hwsel_dropout(const hwsel_dropout_t *how, int64_t rows, int64_t cols, const 
  *              g = gate, or 1 / (1 + exp(-gate)) with gate_sigmoid.
  *   w_branch, w_pre  fp32 [cols] or NULL (ones).
  *   x1 or z may be none, not both.
- * x1 may be x itself (same data, ld); outputs overlap nothing else (the same
- * data is refused).
+ * x1 may be x itself (same data, ld); an output that overlaps anything else is
+ * refused (columns of one buffer, each matrix its own, do not overlap).
  * Returns HWSEL_EINVAL for null pointers, sizes < 1, eps not > 0, scales that
  * are not finite, p outside [0, 1], bad flags, ld or alignment, dtypes that
  * differ where they are to be one; HWSEL_EUNSUPPORTED for another dtype, rows
@@ -812,8 +813,8 @@ int hwsel_block_join(const hwsel_join_t *join, const hwsel_matrix_t *x, const hw
  *   workspace  hwsel_block_join_gradient_workspace_bytes(join) bytes of
  *   device memory, 256-byte aligned (NULL where that is 0).
  * Sums over rows are fp32 in an order fixed by the sizes.  dx may be d_x1
- * itself (same data, ld); outputs overlap nothing else (the same data is
- * refused).
+ * itself (same data, ld); an output or a workspace that overlaps anything else
+ * is refused.
  * Returns as hwsel_block_join does, and HWSEL_EINVAL for a short or misaligned
  * workspace and for an output whose input is missing.
  */

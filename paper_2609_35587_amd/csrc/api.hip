@@ -4,7 +4,7 @@
 #include <string.h>
 
 #include <initializer_list>
-
+#include <numeric>
 
 #include "internal.hpp"
 
@@ -729,12 +729,58 @@ static int check_in_place(const hwsel_matrix_t &out, const hwsel_matrix_t &in, c
     return HWSEL_OK;
 }
 
-// A result lies in no operand's place, and in no other result's, but those that the caller leaves out.
-static int check_apart(const hwsel_matrix_t &out, const char *name, std::initializer_list<const hwsel_matrix_t *> others, const char *fn)
+// Memory that a call reads or writes, [at, end): runs of `width` bytes, `step` bytes from one to the next (0: one run).
+struct Region {
+    uintptr_t at, end;
+    int64_t width, step;
+};
+
+static Region region_of(const void *p, int64_t bytes)
 {
-    for (const hwsel_matrix_t *m : others)
-        if (out.data && out.data == m->data) return fail(HWSEL_EINVAL, fn, "%s in the place of another matrix", name);
+    const uintptr_t at = p ? (uintptr_t)p : 0;
+    return {at, at + (p ? (uintptr_t)bytes : 0), p ? bytes : 0, 0};
+}
+
+static Region region_of(const hwsel_matrix_t &m, int64_t rows, int64_t cols)
+{
+    const int64_t each = m.dtype == HWSEL_DTYPE_BF16 ? 2 : 4;
+    Region r = region_of(m.data, cols * each);
+    if (!m.data || rows == 1) return r;
+    r.step = m.ld * each;                                   // (at most 2^42, rows below 2^31)
+    const __int128 end = (__int128)r.end + (__int128)(rows - 1) * r.step;
+    r.end = end < (__int128)UINTPTR_MAX ? (uintptr_t)end : UINTPTR_MAX;
+    return r;
+}
+
+// Whether two regions may share a byte.  Both repeat with the greatest common divisor of their steps, within which columns
+// of one buffer, each matrix its own, lie apart.
+static bool overlap(const Region &a, const Region &b)
+{
+    if (a.width == 0 || b.width == 0 || a.end <= b.at || b.end <= a.at) return false;
+    const int64_t period = std::gcd(a.step, b.step);
+    if (period == 0) return true;
+    const int64_t from = (int64_t)((((__int128)b.at - (__int128)a.at) % period + period) % period);
+    return a.width > from || from + b.width > period;
+}
+
+// A result overlaps nothing else that the call reads or writes.
+struct Named {
+    const char *name;
+    Region region;
+};
+
+static int check_apart(const Named &out, std::initializer_list<Region> others, const char *fn)
+{
+    for (const Region &r : others)
+        if (overlap(out.region, r)) return fail(HWSEL_EINVAL, fn, "%s in the place of another operand or result", out.name);
     return HWSEL_OK;
+}
+
+// The same, but for an operand whose place it may take whole.
+static int check_in_place_or_apart(const Named &out, const hwsel_matrix_t &m, const hwsel_matrix_t &in, const Region &at, const char *fn)
+{
+    if (int st = check_in_place(m, in, out.name, fn)) return st;
+    return m.data == in.data ? HWSEL_OK : check_apart(out, {at}, fn);
 }
 
 static int check_dropout(const hwsel_dropout_t &d, const char *fn)
@@ -754,8 +800,10 @@ int hwsel_dropout(const hwsel_dropout_t *how, int64_t rows, int64_t cols, const 
     if (int st = check_matrix(*X, "X", cols, -1, fn)) return st;
     if (int st = check_matrix(*Y, "Y", cols, -1, fn)) return st;
     if (int st = check_matrix(or_none(residual), "residual", cols, Y->dtype, fn)) return st;
-    if (int st = check_in_place(*Y, *X, "Y", fn)) return st;
-    if (int st = check_in_place(*Y, or_none(residual), "Y", fn)) return st;
+    const Named y = {"Y", region_of(*Y, rows, cols)};
+    if (int st = check_in_place_or_apart(y, *Y, *X, region_of(*X, rows, cols), fn)) return st;
+    if (int st = check_in_place_or_apart(y, *Y, or_none(residual), region_of(or_none(residual), rows, cols), fn)) return st;
+    if (int st = check_apart(y, {region_of(how->state, 16)}, fn)) return st;
     return launched(hwsel::launch_dropout(*how, rows, cols, *X, or_none(residual), *Y, (hipStream_t)stream), fn);
 }
 
@@ -797,9 +845,12 @@ int hwsel_block_join(const hwsel_join_t *j, const hwsel_matrix_t *x, const hwsel
     if (int st = check_matrix(gate, "gate", j->gate_cols, block, fn)) return st;
     if (int st = check_matrix(x1, "x1", j->cols, x->dtype, fn)) return st;
     if (int st = check_matrix(z, "z", j->cols, block, fn)) return st;
-    if (int st = check_in_place(x1, *x, "x1", fn)) return st;
-    if (int st = check_apart(x1, "x1", {&y, &gate, &z}, fn)) return st;
-    if (int st = check_apart(z, "z", {x, &y, &gate}, fn)) return st;
+    const Region at_x = region_of(*x, j->rows, j->cols), at_y = region_of(y, j->rows, j->cols), at_gate = region_of(gate, j->rows, j->gate_cols),
+                 at_wb = region_of(j->w_branch, 4 * j->cols), at_wp = region_of(j->w_pre, 4 * j->cols), at_state = region_of(j->dropout.state, 16);
+    const Named to_x1 = {"x1", region_of(x1, j->rows, j->cols)}, to_z = {"z", region_of(z, j->rows, j->cols)};
+    if (int st = check_in_place_or_apart(to_x1, x1, *x, at_x, fn)) return st;
+    if (int st = check_apart(to_x1, {at_y, at_gate, at_wb, at_wp, at_state, to_z.region}, fn)) return st;
+    if (int st = check_apart(to_z, {at_x, at_y, at_gate, at_wb, at_wp, at_state}, fn)) return st;
     const bool bbf = (y.data ? y.dtype : z.dtype) == HWSEL_DTYPE_BF16;
     return launched(hwsel::launch_block_join(*j, *x, y, gate, x1, z, x->dtype == HWSEL_DTYPE_BF16, bbf, (hipStream_t)stream), fn);
 }
@@ -842,9 +893,19 @@ int hwsel_block_join_gradient(const hwsel_join_t *j, const hwsel_matrix_t *x1, c
     const size_t need = hwsel::join_gradient_workspace_bytes(*j);
     if (need && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need))
         return fail(HWSEL_EINVAL, fn, "workspace of %zu bytes, %zu needed, 256-byte aligned", workspace_bytes, need);
-    if (int st = check_apart(dx, "dx", {x1, &y, &gate, &d_z, &dy, &dgate}, fn)) return st;
-    if (int st = check_apart(dy, "dy", {x1, &y, &gate, &d_x1, &d_z, &dgate}, fn)) return st;
-    if (int st = check_apart(dgate, "dgate", {x1, &y, &gate, &d_x1, &d_z}, fn)) return st;
+    const int64_t cols = j->cols;
+    auto at = [&](const hwsel_matrix_t &m, int64_t width) { return region_of(m, j->rows, width); };
+    const Named outs[] = {{"dx", at(dx, cols)}, {"dy", at(dy, cols)}, {"dgate", at(dgate, j->gate_cols)}, {"dw_branch", region_of(dw_branch, 4 * cols)},
+                          {"dw_pre", region_of(dw_pre, 4 * cols)}, {"the workspace", region_of(workspace, (int64_t)need)}};
+    const Region ins[] = {at(d_x1, cols), at(*x1, cols), at(y, cols), at(gate, j->gate_cols), at(d_z, cols), region_of(j->w_branch, 4 * cols),
+                          region_of(j->w_pre, 4 * cols), region_of(j->dropout.state, 16)};
+    for (const Named &out : outs) {
+        for (const Region &in : ins)
+            if (&out != outs || &in != ins || dx.data != d_x1.data)
+                if (int st = check_apart(out, {in}, fn)) return st;
+        for (const Named *other = outs; other < &out; ++other)
+            if (int st = check_apart(out, {other->region}, fn)) return st;
+    }
     const bool bbf = (y.data ? y.dtype : d_z.dtype) == HWSEL_DTYPE_BF16;
     return launched(hwsel::launch_block_join_gradient(*j, *x1, y, gate, d_x1, d_z, dx, dy, dgate, dw_branch, dw_pre, workspace,
                                                       x1->dtype == HWSEL_DTYPE_BF16, bbf, (hipStream_t)stream),
