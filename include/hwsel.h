@@ -688,8 +688,8 @@ int hwsel_sample_per_problem(const float *scores, int64_t R, const int64_t *seg_
  * hwsel_logprob_workspace_bytes(R, P, top) bytes (device, 256-byte aligned;
  * NULL where that is 0).  Sums are fp32 in an order fixed by the sizes.
  * Returns HWSEL_EINVAL for null pointers, P < 1, R < 0, n_picks < 0, top
- * outside 0..64, a short or misaligned workspace; HWSEL_EUNSUPPORTED for R >
- * 2^30.
+ * outside 0..64, a short or misaligned workspace, results or a workspace that
+ * overlap each other or an operand; HWSEL_EUNSUPPORTED for R > 2^30.
  */
 int hwsel_logprob_workspace_bytes(int64_t R, int32_t P, int32_t top, size_t *bytes);
 int hwsel_logprob_per_problem(const float *scores, int64_t R, const int64_t *seg_offsets, int32_t P, float temperature,
@@ -708,10 +708,10 @@ int hwsel_logprob_per_problem(const float *scores, int64_t R, const int64_t *seg
  * matter.  Candidates without probability, problems with T <= 0 or NaN and rows of no
  * problem get 0.  A d_logp or d_entropy that is not finite makes its
  * problem's gradients not finite.
- *   d_scores fp32 [R], not the scores themselves; picks, d_logp NULL where n_picks is 0; entropy and
+ *   d_scores fp32 [R], in no operand's place; picks, d_logp NULL where n_picks is 0; entropy and
  *   d_entropy (fp32 [P]) both NULL or both given; norm as written.
  * Returns HWSEL_EINVAL for null pointers, P < 1, R < 0, n_picks < 0, d_scores
- * that overlaps the scores; HWSEL_EUNSUPPORTED for R > 2^30.
+ * that overlaps an operand; HWSEL_EUNSUPPORTED for R > 2^30.
  */
 int hwsel_logprob_gradient(const float *scores, int64_t R, const int64_t *seg_offsets, int32_t P, float temperature,
                            const float *temperature_of, const float *norm, const int32_t *picks, int32_t n_picks,

@@ -640,6 +640,42 @@ int hwsel_sample_per_problem(const float *scores, int64_t R, const int64_t *seg_
                     fn);
 }
 
+// Memory that a call reads or writes, [at, end): runs of `width` bytes, `step` bytes from one to the next (0: one run).
+struct Region {
+    uintptr_t at, end;
+    int64_t width, step;
+};
+
+static Region region_of(const void *p, int64_t bytes)
+{
+    const uintptr_t at = p ? (uintptr_t)p : 0;
+    return {at, at + (p ? (uintptr_t)bytes : 0), p ? bytes : 0, 0};
+}
+
+// Whether two regions may share a byte.  Both repeat with the greatest common divisor of their steps, within which columns
+// of one buffer, each matrix its own, lie apart.
+static bool overlap(const Region &a, const Region &b)
+{
+    if (a.width == 0 || b.width == 0 || a.end <= b.at || b.end <= a.at) return false;
+    const int64_t period = std::gcd(a.step, b.step);
+    if (period == 0) return true;
+    const int64_t from = (int64_t)((((__int128)b.at - (__int128)a.at) % period + period) % period);
+    return a.width > from || from + b.width > period;
+}
+
+// A result overlaps nothing else that the call reads or writes.
+struct Named {
+    const char *name;
+    Region region;
+};
+
+static int check_apart(const Named &out, std::initializer_list<Region> others, const char *fn)
+{
+    for (const Region &r : others)
+        if (overlap(out.region, r)) return fail(HWSEL_EINVAL, fn, "%s in the place of another operand or result", out.name);
+    return HWSEL_OK;
+}
+
 static int check_logprob_sizes(int64_t R, int32_t P, const char *fn)
 {
     if (R < 0 || P < 1) return fail(HWSEL_EINVAL, fn, "R=%lld P=%d", (long long)R, P);
@@ -677,6 +713,17 @@ int hwsel_logprob_per_problem(const float *scores, int64_t R, const int64_t *seg
     const size_t need = hwsel::logprob_workspace_bytes(R, P, top);
     if (need && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need))
         return fail(HWSEL_EINVAL, fn, "workspace of %zu bytes, %zu needed, 256-byte aligned", workspace_bytes, need);
+    const Region ins[] = {region_of(scores, 4 * R), region_of(seg_offsets, 8 * ((int64_t)P + 1)), region_of(temperature_of, 4 * (int64_t)P),
+                          region_of(n_picks ? picks : nullptr, 4 * (int64_t)P * n_picks)};
+    const Named outs[] = {{"logp", region_of(n_picks ? logp : nullptr, 4 * (int64_t)P * n_picks)}, {"entropy", region_of(entropy, 4 * (int64_t)P)},
+                          {"norm", region_of(norm, 8 * (int64_t)P)}, {"top_idx", region_of(top ? top_idx : nullptr, 4 * (int64_t)P * top)},
+                          {"top_logp", region_of(top ? top_logp : nullptr, 4 * (int64_t)P * top)}, {"the workspace", region_of(workspace, (int64_t)need)}};
+    for (const Named &out : outs) {
+        for (const Region &in : ins)
+            if (int st = check_apart(out, {in}, fn)) return st;
+        for (const Named *other = outs; other < &out; ++other)
+            if (int st = check_apart(out, {other->region}, fn)) return st;
+    }
     return launched(hwsel::launch_logprob(scores, R, seg_offsets, P, temperature, temperature_of, picks, n_picks, top, logp, entropy,
                                           norm, top_idx, top_logp, workspace, (hipStream_t)stream),
                     fn);
@@ -693,6 +740,12 @@ int hwsel_logprob_gradient(const float *scores, int64_t R, const int64_t *seg_of
         return fail(HWSEL_EINVAL, fn, "null pointer");
     if (!entropy != !d_entropy) return fail(HWSEL_EINVAL, fn, "entropy and d_entropy go together");
     if (scores < d_scores + R && d_scores < scores + R) return fail(HWSEL_EINVAL, fn, "d_scores overlaps the scores");
+    const int64_t of_problems = 4 * (int64_t)P, of_picks = 4 * (int64_t)P * n_picks;
+    if (int st = check_apart({"d_scores", region_of(d_scores, 4 * R)},
+                             {region_of(seg_offsets, 8 * ((int64_t)P + 1)), region_of(temperature_of, of_problems), region_of(norm, 2 * of_problems),
+                              region_of(n_picks ? picks : nullptr, of_picks), region_of(n_picks ? d_logp : nullptr, of_picks),
+                              region_of(entropy, of_problems), region_of(d_entropy, of_problems)}, fn))
+        return st;
     return launched(hwsel::launch_logprob_gradient(scores, R, seg_offsets, P, temperature, temperature_of, norm, picks, n_picks,
                                                    d_logp, entropy, d_entropy, d_scores, (hipStream_t)stream),
                     fn);
@@ -729,18 +782,7 @@ static int check_in_place(const hwsel_matrix_t &out, const hwsel_matrix_t &in, c
     return HWSEL_OK;
 }
 
-// Memory that a call reads or writes, [at, end): runs of `width` bytes, `step` bytes from one to the next (0: one run).
-struct Region {
-    uintptr_t at, end;
-    int64_t width, step;
-};
-
-static Region region_of(const void *p, int64_t bytes)
-{
-    const uintptr_t at = p ? (uintptr_t)p : 0;
-    return {at, at + (p ? (uintptr_t)bytes : 0), p ? bytes : 0, 0};
-}
-
+// rows x cols of a matrix.
 static Region region_of(const hwsel_matrix_t &m, int64_t rows, int64_t cols)
 {
     const int64_t each = m.dtype == HWSEL_DTYPE_BF16 ? 2 : 4;
@@ -750,30 +792,6 @@ static Region region_of(const hwsel_matrix_t &m, int64_t rows, int64_t cols)
     const __int128 end = (__int128)r.end + (__int128)(rows - 1) * r.step;
     r.end = end < (__int128)UINTPTR_MAX ? (uintptr_t)end : UINTPTR_MAX;
     return r;
-}
-
-// Whether two regions may share a byte.  Both repeat with the greatest common divisor of their steps, within which columns
-// of one buffer, each matrix its own, lie apart.
-static bool overlap(const Region &a, const Region &b)
-{
-    if (a.width == 0 || b.width == 0 || a.end <= b.at || b.end <= a.at) return false;
-    const int64_t period = std::gcd(a.step, b.step);
-    if (period == 0) return true;
-    const int64_t from = (int64_t)((((__int128)b.at - (__int128)a.at) % period + period) % period);
-    return a.width > from || from + b.width > period;
-}
-
-// A result overlaps nothing else that the call reads or writes.
-struct Named {
-    const char *name;
-    Region region;
-};
-
-static int check_apart(const Named &out, std::initializer_list<Region> others, const char *fn)
-{
-    for (const Region &r : others)
-        if (overlap(out.region, r)) return fail(HWSEL_EINVAL, fn, "%s in the place of another operand or result", out.name);
-    return HWSEL_OK;
 }
 
 // The same, but for an operand whose place it may take whole.
