@@ -3,7 +3,6 @@
 #include <stdio.h>
 #include <string.h>
 
-#include <initializer_list>
 #include <numeric>
 
 #include "internal.hpp"
@@ -32,6 +31,59 @@ int launched(hipError_t e, const char *fn)
 }
 
 bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
+
+// Memory that a call reads or writes, [at, end): runs of `width` bytes, `step` bytes from one to the next (0: one run).
+struct Region {
+    uintptr_t at, end;
+    int64_t width, step;
+};
+
+Region region_of(const void *p, int64_t bytes)
+{
+    const uintptr_t at = p ? (uintptr_t)p : 0;
+    return {at, at + (p ? (uintptr_t)bytes : 0), p ? bytes : 0, 0};
+}
+
+// rows x cols of a matrix.
+Region region_of(const hwsel_matrix_t &m, int64_t rows, int64_t cols)
+{
+    const int64_t each = m.dtype == HWSEL_DTYPE_BF16 ? 2 : 4;
+    Region r = region_of(m.data, cols * each);
+    if (!m.data || rows == 1) return r;
+    r.step = m.ld * each;                                   // (at most 2^42, rows below 2^31)
+    const __int128 end = (__int128)r.end + (__int128)(rows - 1) * r.step;
+    r.end = end < (__int128)UINTPTR_MAX ? (uintptr_t)end : UINTPTR_MAX;
+    return r;
+}
+
+// Whether two regions may share a byte.  Both repeat with the greatest common divisor of their steps, within which columns
+// of one buffer, each matrix its own, lie apart.
+bool overlap(const Region &a, const Region &b)
+{
+    if (a.end <= b.at || b.end <= a.at || a.width == 0 || b.width == 0) return false;
+    const int64_t period = std::gcd(a.step, b.step);
+    if (period == 0) return true;
+    const int64_t from = (int64_t)((((__int128)b.at - (__int128)a.at) % period + period) % period);
+    return a.width > from || from + b.width > period;
+}
+
+// Results overlap nothing else that the call reads or writes, but result `whole` (-1: none) the first operand.
+struct Named {
+    const char *name;
+    Region region;
+};
+
+template <int N, int M>
+int check_apart(const Named (&outs)[N], const Region (&ins)[M], int whole, const char *fn)
+{
+    for (int o = 0; o < N; ++o) {
+        bool apart = true;
+        for (int i = o == whole; i < M; ++i) apart = apart && !overlap(outs[o].region, ins[i]);
+        for (int i = 0; i < o; ++i) apart = apart && !overlap(outs[o].region, outs[i].region);
+        if (!apart) return fail(HWSEL_EINVAL, fn, "%s in the place of another operand or result", outs[o].name);
+    }
+    return HWSEL_OK;
+}
 
 }  // namespace
 
@@ -640,42 +692,6 @@ int hwsel_sample_per_problem(const float *scores, int64_t R, const int64_t *seg_
                     fn);
 }
 
-// Memory that a call reads or writes, [at, end): runs of `width` bytes, `step` bytes from one to the next (0: one run).
-struct Region {
-    uintptr_t at, end;
-    int64_t width, step;
-};
-
-static Region region_of(const void *p, int64_t bytes)
-{
-    const uintptr_t at = p ? (uintptr_t)p : 0;
-    return {at, at + (p ? (uintptr_t)bytes : 0), p ? bytes : 0, 0};
-}
-
-// Whether two regions may share a byte.  Both repeat with the greatest common divisor of their steps, within which columns
-// of one buffer, each matrix its own, lie apart.
-static bool overlap(const Region &a, const Region &b)
-{
-    if (a.width == 0 || b.width == 0 || a.end <= b.at || b.end <= a.at) return false;
-    const int64_t period = std::gcd(a.step, b.step);
-    if (period == 0) return true;
-    const int64_t from = (int64_t)((((__int128)b.at - (__int128)a.at) % period + period) % period);
-    return a.width > from || from + b.width > period;
-}
-
-// A result overlaps nothing else that the call reads or writes.
-struct Named {
-    const char *name;
-    Region region;
-};
-
-static int check_apart(const Named &out, std::initializer_list<Region> others, const char *fn)
-{
-    for (const Region &r : others)
-        if (overlap(out.region, r)) return fail(HWSEL_EINVAL, fn, "%s in the place of another operand or result", out.name);
-    return HWSEL_OK;
-}
-
 static int check_logprob_sizes(int64_t R, int32_t P, const char *fn)
 {
     if (R < 0 || P < 1) return fail(HWSEL_EINVAL, fn, "R=%lld P=%d", (long long)R, P);
@@ -718,12 +734,7 @@ int hwsel_logprob_per_problem(const float *scores, int64_t R, const int64_t *seg
     const Named outs[] = {{"logp", region_of(n_picks ? logp : nullptr, 4 * (int64_t)P * n_picks)}, {"entropy", region_of(entropy, 4 * (int64_t)P)},
                           {"norm", region_of(norm, 8 * (int64_t)P)}, {"top_idx", region_of(top ? top_idx : nullptr, 4 * (int64_t)P * top)},
                           {"top_logp", region_of(top ? top_logp : nullptr, 4 * (int64_t)P * top)}, {"the workspace", region_of(workspace, (int64_t)need)}};
-    for (const Named &out : outs) {
-        for (const Region &in : ins)
-            if (int st = check_apart(out, {in}, fn)) return st;
-        for (const Named *other = outs; other < &out; ++other)
-            if (int st = check_apart(out, {other->region}, fn)) return st;
-    }
+    if (int st = check_apart(outs, ins, -1, fn)) return st;
     return launched(hwsel::launch_logprob(scores, R, seg_offsets, P, temperature, temperature_of, picks, n_picks, top, logp, entropy,
                                           norm, top_idx, top_logp, workspace, (hipStream_t)stream),
                     fn);
@@ -741,11 +752,11 @@ int hwsel_logprob_gradient(const float *scores, int64_t R, const int64_t *seg_of
     if (!entropy != !d_entropy) return fail(HWSEL_EINVAL, fn, "entropy and d_entropy go together");
     if (scores < d_scores + R && d_scores < scores + R) return fail(HWSEL_EINVAL, fn, "d_scores overlaps the scores");
     const int64_t of_problems = 4 * (int64_t)P, of_picks = 4 * (int64_t)P * n_picks;
-    if (int st = check_apart({"d_scores", region_of(d_scores, 4 * R)},
-                             {region_of(seg_offsets, 8 * ((int64_t)P + 1)), region_of(temperature_of, of_problems), region_of(norm, 2 * of_problems),
-                              region_of(n_picks ? picks : nullptr, of_picks), region_of(n_picks ? d_logp : nullptr, of_picks),
-                              region_of(entropy, of_problems), region_of(d_entropy, of_problems)}, fn))
-        return st;
+    const Region ins[] = {region_of(seg_offsets, 8 * ((int64_t)P + 1)), region_of(temperature_of, of_problems), region_of(norm, 2 * of_problems),
+                          region_of(n_picks ? picks : nullptr, of_picks), region_of(n_picks ? d_logp : nullptr, of_picks),
+                          region_of(entropy, of_problems), region_of(d_entropy, of_problems)};
+    const Named outs[] = {{"d_scores", region_of(d_scores, 4 * R)}};
+    if (int st = check_apart(outs, ins, -1, fn)) return st;
     return launched(hwsel::launch_logprob_gradient(scores, R, seg_offsets, P, temperature, temperature_of, norm, picks, n_picks,
                                                    d_logp, entropy, d_entropy, d_scores, (hipStream_t)stream),
                     fn);
@@ -782,25 +793,6 @@ static int check_in_place(const hwsel_matrix_t &out, const hwsel_matrix_t &in, c
     return HWSEL_OK;
 }
 
-// rows x cols of a matrix.
-static Region region_of(const hwsel_matrix_t &m, int64_t rows, int64_t cols)
-{
-    const int64_t each = m.dtype == HWSEL_DTYPE_BF16 ? 2 : 4;
-    Region r = region_of(m.data, cols * each);
-    if (!m.data || rows == 1) return r;
-    r.step = m.ld * each;                                   // (at most 2^42, rows below 2^31)
-    const __int128 end = (__int128)r.end + (__int128)(rows - 1) * r.step;
-    r.end = end < (__int128)UINTPTR_MAX ? (uintptr_t)end : UINTPTR_MAX;
-    return r;
-}
-
-// The same, but for an operand whose place it may take whole.
-static int check_in_place_or_apart(const Named &out, const hwsel_matrix_t &m, const hwsel_matrix_t &in, const Region &at, const char *fn)
-{
-    if (int st = check_in_place(m, in, out.name, fn)) return st;
-    return m.data == in.data ? HWSEL_OK : check_apart(out, {at}, fn);
-}
-
 static int check_dropout(const hwsel_dropout_t &d, const char *fn)
 {
     if (!(d.p >= 0.0f && d.p <= 1.0f)) return fail(HWSEL_EINVAL, fn, "p=%g (0..1)", (double)d.p);
@@ -818,11 +810,14 @@ int hwsel_dropout(const hwsel_dropout_t *how, int64_t rows, int64_t cols, const 
     if (int st = check_matrix(*X, "X", cols, -1, fn)) return st;
     if (int st = check_matrix(*Y, "Y", cols, -1, fn)) return st;
     if (int st = check_matrix(or_none(residual), "residual", cols, Y->dtype, fn)) return st;
-    const Named y = {"Y", region_of(*Y, rows, cols)};
-    if (int st = check_in_place_or_apart(y, *Y, *X, region_of(*X, rows, cols), fn)) return st;
-    if (int st = check_in_place_or_apart(y, *Y, or_none(residual), region_of(or_none(residual), rows, cols), fn)) return st;
-    if (int st = check_apart(y, {region_of(how->state, 16)}, fn)) return st;
-    return launched(hwsel::launch_dropout(*how, rows, cols, *X, or_none(residual), *Y, (hipStream_t)stream), fn);
+    const hwsel_matrix_t &r = or_none(residual);
+    if (int st = check_in_place(*Y, *X, "Y", fn)) return st;
+    if (int st = check_in_place(*Y, r, "Y", fn)) return st;
+    const Region ins[] = {Y->data == X->data ? Region{} : region_of(*X, rows, cols), Y->data == r.data ? Region{} : region_of(r, rows, cols),
+                          region_of(how->state, 16)};
+    const Named outs[] = {{"Y", region_of(*Y, rows, cols)}};
+    if (int st = check_apart(outs, ins, -1, fn)) return st;
+    return launched(hwsel::launch_dropout(*how, rows, cols, *X, r, *Y, (hipStream_t)stream), fn);
 }
 
 // What both passes of a join share.
@@ -863,12 +858,12 @@ int hwsel_block_join(const hwsel_join_t *j, const hwsel_matrix_t *x, const hwsel
     if (int st = check_matrix(gate, "gate", j->gate_cols, block, fn)) return st;
     if (int st = check_matrix(x1, "x1", j->cols, x->dtype, fn)) return st;
     if (int st = check_matrix(z, "z", j->cols, block, fn)) return st;
-    const Region at_x = region_of(*x, j->rows, j->cols), at_y = region_of(y, j->rows, j->cols), at_gate = region_of(gate, j->rows, j->gate_cols),
-                 at_wb = region_of(j->w_branch, 4 * j->cols), at_wp = region_of(j->w_pre, 4 * j->cols), at_state = region_of(j->dropout.state, 16);
-    const Named to_x1 = {"x1", region_of(x1, j->rows, j->cols)}, to_z = {"z", region_of(z, j->rows, j->cols)};
-    if (int st = check_in_place_or_apart(to_x1, x1, *x, at_x, fn)) return st;
-    if (int st = check_apart(to_x1, {at_y, at_gate, at_wb, at_wp, at_state, to_z.region}, fn)) return st;
-    if (int st = check_apart(to_z, {at_x, at_y, at_gate, at_wb, at_wp, at_state}, fn)) return st;
+    if (int st = check_in_place(x1, *x, "x1", fn)) return st;
+    auto at = [&](const hwsel_matrix_t &m, int64_t width) { return region_of(m, j->rows, width); };
+    const Region ins[] = {at(*x, j->cols), at(y, j->cols), at(gate, j->gate_cols), region_of(j->w_branch, 4 * j->cols),
+                          region_of(j->w_pre, 4 * j->cols), region_of(j->dropout.state, 16)};
+    const Named outs[] = {{"z", at(z, j->cols)}, {"x1", at(x1, j->cols)}};
+    if (int st = check_apart(outs, ins, x1.data == x->data ? 1 : -1, fn)) return st;
     const bool bbf = (y.data ? y.dtype : z.dtype) == HWSEL_DTYPE_BF16;
     return launched(hwsel::launch_block_join(*j, *x, y, gate, x1, z, x->dtype == HWSEL_DTYPE_BF16, bbf, (hipStream_t)stream), fn);
 }
@@ -917,13 +912,7 @@ int hwsel_block_join_gradient(const hwsel_join_t *j, const hwsel_matrix_t *x1, c
                           {"dw_pre", region_of(dw_pre, 4 * cols)}, {"the workspace", region_of(workspace, (int64_t)need)}};
     const Region ins[] = {at(d_x1, cols), at(*x1, cols), at(y, cols), at(gate, j->gate_cols), at(d_z, cols), region_of(j->w_branch, 4 * cols),
                           region_of(j->w_pre, 4 * cols), region_of(j->dropout.state, 16)};
-    for (const Named &out : outs) {
-        for (const Region &in : ins)
-            if (&out != outs || &in != ins || dx.data != d_x1.data)
-                if (int st = check_apart(out, {in}, fn)) return st;
-        for (const Named *other = outs; other < &out; ++other)
-            if (int st = check_apart(out, {other->region}, fn)) return st;
-    }
+    if (int st = check_apart(outs, ins, dx.data == d_x1.data ? 0 : -1, fn)) return st;
     const bool bbf = (y.data ? y.dtype : d_z.dtype) == HWSEL_DTYPE_BF16;
     return launched(hwsel::launch_block_join_gradient(*j, *x1, y, gate, d_x1, d_z, dx, dy, dgate, dw_branch, dw_pre, workspace,
                                                       x1->dtype == HWSEL_DTYPE_BF16, bbf, (hipStream_t)stream),
