@@ -10,8 +10,11 @@
 // passes them on.
 #include <Python.h>
 
+#include <ATen/Context.h>
 #include <ATen/core/Tensor.h>
 #include <ATen/hip/EmptyTensor.h>
+#include <ATen/ops/empty.h>
+#include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPCachingAllocator.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
@@ -127,7 +130,7 @@ hipStream_t stream_of(PyObject *stream)
 // them on the current stream: they are noted there too.
 class Queue {
 public:
-    Queue(PyObject *given, int device) : device_(device), stream_(stream_of(given))
+    Queue(PyObject *given, int device) : device_(device), stream_(stream_of(given)), seen_(is_seen())
     {
         if (given == Py_None) return;
         const auto current = c10::hip::getCurrentHIPStream((c10::DeviceIndex)device);
@@ -155,11 +158,20 @@ private:
     at::Tensor empty(at::IntArrayRef sizes, at::ScalarType type) const
     {
         // (at::empty finds the same by torch's dispatcher, 0.25 us a tensor later)
+        if (seen_) return at::empty(sizes, at::TensorOptions().dtype(type).device(at::kCUDA, (c10::DeviceIndex)device_));
         return at::detail::empty_cuda(sizes, type, c10::Device(at::kCUDA, (c10::DeviceIndex)device_), std::nullopt);
+    }
+
+    // Whether somebody is there to see new tensors, or to fill them: dispatch modes, and deterministic algorithms.
+    static bool is_seen()
+    {
+        const auto &context = at::globalContext();
+        return c10::impl::dispatch_mode_enabled() || (context.deterministicAlgorithms() && context.deterministicFillUninitializedMemory());
     }
 
     int device_;
     hipStream_t stream_;
+    bool seen_;
     std::optional<c10::hip::HIPStream> current_;            // torch's, where the call is on another
 };
 
