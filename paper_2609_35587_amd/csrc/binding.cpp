@@ -2,7 +2,7 @@
 // probabilities, of dropout and of joins: argument checks, results' tensors and
 // the current stream in C++.  A call that takes
 // the GPU 3.5 us (a row through one layer) took the host 13.9 us in Python, most
-// of it in attributes of tensors; it takes 5.6 so, half of it the launch.  Nothing
+// of it in attributes of tensors; it takes 5.3 so, half of it the launch.  Nothing
 // is computed here, and nothing is kept from one call for the next but the
 // addresses of the C functions.
 //

@@ -337,7 +337,9 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void k_join(Forward a)
 // Two rounds of sums a row: x1^2, dn x1 and y^2 together, then what goes by d.
 // A workgroup's sums over its rows go to a part of their own, joined in a fixed
 // order by k_join_sums: atomics would add in any order.  The second launch takes 5 us.
-// Five operands and two sums of 16 columns are 190 to 225 registers, two waves a SIMD; vector units are busy 59 % of the time.
+// Five operands and two sums of 16 columns are 190 to 225 registers, two waves a SIMD; vector units are busy 59 % of the time.  One
+// eight a thread takes 103 to 125 where a wave or a workgroup has a row, up to 151 for several rows of a wave: the waves that
+// the launch bounds promise are what the compiler reaches without them too, and what groups_of counts on.
 template <bool SBF, bool BBF, int LANES, int K, bool EDGE>
 __global__ __launch_bounds__(LANES ? 256 : 512, K == 2 ? 2 : LANES == 64 || LANES == 0 ? 4 : 3) void k_join_gradient(Backward a)
 {
@@ -453,9 +455,10 @@ __global__ __launch_bounds__(LANES ? 256 : 512, K == 2 ? 2 : LANES == 64 || LANE
 // ---------------------------------------------------------------------------
 // Rows of any length: a workgroup goes through a row several times, from the
 // second on out of the caches where it fits them.  Forward: 2,000 x 30,000 in bf16 188 us (3.2 TB/s of each operand once).
-// Backward: two kernels, the rows' sums, then columns, whose sums over rows stay in registers, at 4.6 and 6.0 TB/s of what each
-// of them moves: 4,000 x 16,384 385 us (2.7 TB/s of each operand once), 2,000 x 30,000 355 us (2.7 TB/s); 401 and 385 with
-// what goes by d in a second pass of the first kernel.
+// Backward: two kernels, the rows' sums, then columns, whose sums over a part of the rows stay in registers, at 4.1 and 5.0 TB/s
+// of their operands: 4,000 x 16,384 385 us (2.7 TB/s of each operand once), 2,000 x 30,000 355 us (2.7 TB/s); 401 and 385 with
+// what goes by d in a second pass of the first kernel.  Rows are in 256 parts: up to 256 rows are a part each, whose sums are
+// its own terms, written and read again (8 bytes a column and part).
 // ---------------------------------------------------------------------------
 constexpr int kLong = 512;
 
@@ -534,7 +537,7 @@ __global__ __launch_bounds__(kLong) void k_join_long(Forward a)
 // d_x1, dn and x1 with factors that are known once the row has been read, so what goes by d is made of three
 // sums with h = dropout(branch) w_branch y (and an element's gate): sum h d = sum h d_x1 + r1 (sum h dn - r1 m1 sum h x1).
 // Where the parts of d cancel so do the three sums, but not their errors: they are made in 64 bits, of products that these
-// hold whole.  (In 32 bits 4,000 x 16,384 took 376 us, and lost thousands of units where little of d was left.)
+// hold whole.  (In 32 bits 4,000 x 16,384 took 376 us, and dy kept the error of what had cancelled.)
 template <bool SBF, bool BBF>
 __global__ __launch_bounds__(kLong) void k_join_long_stats(Backward a)
 {
@@ -769,6 +772,10 @@ Shape shape_of(int64_t cols)
 
 // Workgroups that run at once where a SIMD holds `waves` of their waves, at most one for each row (or rows).
 // 65,536 x 1,024 in bf16, us: forward 4 waves 131, 6 142, 8 136; backward 2 waves 213, 3 231, 4 215 (and twice the parts).
+// One eight a thread, bf16, forward 4 / 6 / 8 waves: several rows of a wave 1,000,000 x 64 121 / 123 / 139, 250,000 x 256 119 / 124 / 139;
+// else 262,144 x 512 246 / 261 / 272, but rows that are no whole number of eights 200,000 x 300 226 / 183 / 215, 60,000 x 1,500 248 / 194 / 245: 6.
+// Backward 2 / 3 / 4: 1,000,000 x 64 196 / 204 / 211, 262,144 x 512 439 / 438 / 464 (though 200,000 x 300 366 / 303 / 283): 2; a workgroup's row
+// 60,000 x 1,500 500 / 339 / 333: 4.
 int32_t groups_of(const Shape &f, int64_t rows, int waves)
 {
     const int64_t each = 4 * waves * 64 / f.threads, most = (int64_t)compute_units() * (each > 1 ? each : 1), need = (rows + f.rows() - 1) / f.rows();

@@ -4,8 +4,8 @@
 // Scores are read once, with the running best score and the sums that go by it; for alternatives once more where
 // a workgroup's registers do not hold them.
 //
-// Bound by latency where problems are few or short (a launch, the offsets, the scores, barriers: 4 us for any), by memory
-// where they are long: 256 x 65,536 scores, 67 MB, 15 us (4.5 TB/s), their gradient 23.5 us (5.7 TB/s read and written).
+// Bound by latency where problems are few or short (a launch, the offsets, the scores, barriers: 100 problems of 700 3.9 us,
+// launches in a row), by memory where they are long: 256 x 65,536 scores, 67 MB, 15 us (4.5 TB/s), their gradient 23.5 us (5.7 TB/s read and written).
 #include "topk.hpp"
 
 namespace hwsel {
@@ -261,7 +261,9 @@ constexpr uint32_t kLeastBits = 0x00800000u;                // of the least fini
 // threads reach (of 256 threads, or of 64 groups of them; more are taken together), and the listed ones, few more
 // than `top`, are ranked by counting the larger.  False, and nothing written, if they do not fit the list.
 // (By tiles, each score with its key against a running bound, the sums on the way: 600 of up to 8,192 scores, 10 of
-// each, 13.7 us, 10.1 so; 256 of 65,536 with 64 of each 77 and 24; 256 of 131,072, 134 MB, 90 and 44.)
+// each, 13.7 us, 10.1 so; 256 of 65,536 with 64 of each 77 and 24; 256 of 131,072, 134 MB, 90 and 44.  Where the best are the same
+// few values over and over they do not fit and the tiles follow: of twelve values 600 x 8,192 with 10 20 us, 9 of distinct ones; 256 x
+// 65,536 with 64 46 and 26.)
 template <int NT>
 __device__ __forceinline__ bool list_best(const float *s, int32_t n, int32_t top, Lds<NT> &lds, f32x4u_t (&w)[4])
 {
@@ -843,9 +845,11 @@ __global__ __launch_bounds__(kThreads) void k_logprob_gradient_waves(GradientArg
 
 namespace {
 
-// Problems' lengths are not known here; their mean is.  Parts and the kernel that joins them against a workgroup a
-// problem, us: 64 x 20,000, 16 alternatives 13.3 / 10.3, 8 x 40,000 11.4 / 12.1, 64 x 40,000 13.4 / 12.3, 128 x 65,536 16.2 / 14.5, 3 x 100,000
-// 11.4 / 19.6, 64 x 100,000 16.2 / 20.1, 3 x 534,600 14.1 / 67.9.
+// Problems' lengths are not known here; their mean is.  (600 problems of 500 and one of 534,600, a single workgroup's: 103 us, with
+// 10 alternatives 178, the gradient 169.)  Parts and the kernel that joins them against a workgroup a problem, 16
+// alternatives, us: 64 x 20,000 13.3 / 10.3, 8 x 40,000 11.1 / 12.1, 3 x 100,000 10.8 / 20.0, 64 x 100,000 15.7 / 20.8, 3 x 534,600
+// 13.5 / 70.5.  Many of just enough are faster without parts, which they get all the same: 64 x 40,000 12.6 / 12.3,
+// 128 x 65,536 16.2 / 14.6.
 int32_t parts_of(int64_t R, int32_t P, int32_t top)
 {
     const int64_t mean = R / P, n_cu = compute_units();
@@ -878,19 +882,21 @@ hipError_t launch_logprob(const float *scores, int64_t R, const int64_t *seg, in
             hipLaunchKernelGGL((k_logprob_parts<TOP>), dim3(parts, P), dim3(kWide), 0, s, a, w);
             hipLaunchKernelGGL((k_logprob_join<TOP>), dim3(P), dim3(kWide), 0, s, a, w);
         } else if (mean <= (TOP && P <= 4 * compute_units() ? 256 : kSmall)) {
-            // A wave a problem, four in a workgroup, against a workgroup each, us: without alternatives always (100 x 700 4.2 / 4.2,
-            // 3,000 x 1,000 5.8 / 12.2); with ten 100 x 200 7.2 / 6.3, 600 x 64 5.8 / 7.5, 100 x 512 8.0 / 6.2, 600 x 1,000 12.5 / 7.6, 1,500 x 700 13.1 / 10.3,
-            // 3,000 x 700 15.5 / 16.4, 8,000 x 700 28 / 34; with 64 100 x 200 7.7 / 10.4, 600 x 512 10.2 / 9.2.
+            // A wave a problem, four in a workgroup, against a workgroup each, us: without alternatives always (100 x 700 3.9 / 4.0,
+            // 3,000 x 1,000 5.6 / 11.5); with ten 600 x 64 5.6 / 7.3, 100 x 512 8.0 / 6.0, 600 x 1,000 11.6 / 7.3, 3,000 x 700 14.3 / 15.8,
+            // 8,000 x 700 28 / 33; with 64 100 x 200 7.2 / 10.1, 600 x 512 9.8 / 8.9.  Two limits do not part them everywhere: 100
+            // x 200 with ten 6.7 / 6.1 and 1,500 x 700 12.8 / 9.8 go by waves.
             each_span(P, [&](int32_t p0, int32_t n) {
                 a.p0 = p0;
                 hipLaunchKernelGGL((k_logprob_waves<TOP>), dim3((n + 3) / 4), dim3(kThreads), 0, s, a);
             });
         } else {
             // Threads of a problem.  Fewer start and meet sooner, more read a long one with fewer steps; where a unit has
-            // several problems those fill it.  Best of 256 / 512 / 1,024, us: 600 x 4,096, 10 alternatives 7.4 / 9.4 / 19.5, 600
-            // of 2,000 .. 16,000 13.3 / 12.5 / 19.5, 300 of 6,000 .. 50,000 26.1 / 20.5 / 21.9; 200 x 4,096 6.4 / 6.6 / 7.9,
-            // 1 x 8,192 7.2 / 5.9 / 7.0, 100 x 16,000 10.6 / 8.2 / 7.5, 200 x 100,000 50 / 31.5 / 29.2; none asked for: 100 x 16,000
-            // 6.3 / 5.1 / 5.5, and of 512 / 1,024 with scores from memory: 256 x 65,536 17.0 / 16.2, 200 x 100,000 24 / 19.3.
+            // several problems those fill it.  256 / 512 / 1,024, 10 alternatives, us: 600 x 4,096 7.4 / 9.0 / 19.2, 600
+            // of 2,000 .. 16,000 13.3 / 12.5 / 19.5, 300 of 6,000 .. 50,000 26.1 / 20.5 / 21.9; 200 x 4,096 6.2 / 6.4 / 7.7,
+            // 1 x 8,192 7.1 / 5.9 / 7.1, 100 x 16,000 10.5 / 8.1 / 7.5, 200 x 100,000 50 / 31 / 29; none asked for: 100 x 16,000 6.0 /
+            // 5.0 / 5.4, 256 x 65,536 19.5 / 14.0 / 14.9 and 200 x 100,000 28 / 18.5 / 17.4 out of the caches, but from memory 512
+            // and 1,024 17.0 / 16.2 and 24 / 19.3: 1,024 for both.
             const bool alone = P <= compute_units();
             each_span(P, [&](int32_t p0, int32_t n) {
                 a.p0 = p0;
