@@ -31,3 +31,17 @@ def test_joins_of_long_rows():
     for part in x[:-1].split(2 ** 18):
         low, high = torch.aminmax(part)
         assert float(low) == 2.0 and float(high) == 2.0
+
+
+def test_gradients_of_joins_of_long_rows():
+    """The rows' sums have 2^21 rows a launch: the same row again and again has the same gradient."""
+    rows, cols = 2 ** 21 + 5, 8200
+    g = torch.Generator(device="cuda").manual_seed(6)
+    one = lambda: torch.randn(1, cols, generator=g, device="cuda").to(B)  # noqa: E731
+    x1, d_z = one(), one()
+    want = hwsel.hwsel_block_join_gradient({}, x1, d_z=d_z)[0]
+    dx = torch.zeros(rows, cols, dtype=B, device="cuda")
+    x1, d_z = x1.repeat(rows, 1), d_z.repeat(rows, 1)
+    assert hwsel.hwsel_block_join_gradient({}, x1, d_z=d_z, dx=dx)[0] is dx
+    del x1, d_z
+    assert all(bool((part == want).all()) for part in dx.split(2 ** 18))
